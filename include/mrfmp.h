@@ -51,7 +51,7 @@ typedef enum {
     MRF_OK = 0,
     MRF_ERR_NULL_POINTER = -1,      /* a required pointer is NULL */
     MRF_ERR_BAD_SHAPE = -2,         /* B, H or W < 1, or a tensor would exceed 2^31-1 label vectors */
-    MRF_ERR_BAD_LABELS = -3,        /* L outside [1, 256] (p, q are 8-bit, Sec. 4) */
+    MRF_ERR_BAD_LABELS = -3,        /* L outside [1, 256] (p, q are 8-bit, Sec. 4), or L < 1 with 32-bit labels */
     MRF_ERR_BAD_ITERATIONS = -4,    /* K < 1 */
     MRF_ERR_BAD_DIRECTIONS = -5,    /* R outside [1, 16], a zero step, or a repeated direction */
     MRF_ERR_WORKSPACE_TOO_SMALL = -6,
@@ -59,7 +59,8 @@ typedef enum {
     MRF_ERR_BAD_ALGORITHM = -8,     /* algo argument is neither MRF_ISGMR nor MRF_TRWP */
     MRF_ERR_HIP = -9,               /* a HIP runtime call or kernel launch failed */
     MRF_ERR_SCRATCH_LIMIT = -10,    /* the problem exceeds the fixed scratch of a no-allocation entry point */
-    MRF_ERR_WAIT_EXPIRED = -11      /* reported by mrf_workspace_fault: a wait between wavefronts ran out */
+    MRF_ERR_WAIT_EXPIRED = -11,     /* reported by mrf_workspace_fault: a wait between wavefronts ran out */
+    MRF_ERR_BAD_ARGUMENT = -12      /* a learning operator's type, map or parameter is outside its range */
 } mrf_status;
 
 enum { MRF_ISGMR = 0, MRF_TRWP = 1 };
@@ -231,6 +232,104 @@ int mrf_softmin_l1(int64_t n_pixels, int32_t L, const float *cost, const float *
 int mrf_softmin_smooth_l1(int64_t n_pixels, int32_t L, const float *cost, const float *target, const uint8_t *mask,
                           float beta, float *disparity, double *loss, float *grad_cost, void *workspace,
                           size_t workspace_bytes, void *hip_stream);
+
+/* ---- Learning operators around the message passing -------------------------------------------------
+ * What makes unaries out of a network's scores (layer norm), a pairwise function out of a few learned
+ * values (distance buckets), and a gradient of the final costs out of rewards (policy loss).
+ *
+ * Their tensors are dense and row-major like all others and need no alignment beyond that of their elements;
+ * buffers of one call must not overlap.  Elements are of the types below; statistics, sums, parameters and
+ * their gradients are 32 bits (sums over rows or pixels that end in a loss 64), and a value is rounded once, to
+ * nearest, where it is stored.  No order of a sum depends on anything but the sizes, so results are the
+ * same from run to run.  Rows, groups and pixels may be none (then nothing is read; gradients of parameters and the loss
+ * are set to 0) and are at most 2^31 - 1; matrices may have more than 2^32 entries.  NaN and infinity in one row (group,
+ * pixel) stay in its outputs and in the sums that it belongs to.  Asynchronous on hip_stream, nothing allocated, no memset:
+ * the calls can be captured into a graph. */
+typedef enum { MRF_F32 = 0, MRF_F16 = 1, MRF_BF16 = 2 } mrf_type;
+
+/* Layer norm over the last index of x [n_rows][C]:
+ *   mu = sum_c x / C,  v = sum_c (x - mu)^2 / C,  s = 1 / sqrt(v + eps),  h = (x - mu) s,  y = h gamma + beta
+ *   x       DEVICE [n_rows][C] of x_type
+ *   gamma, beta  DEVICE [C] float, either may be NULL (then 1, 0)
+ *   eps     > 0 and finite, else MRF_ERR_BAD_ARGUMENT
+ *   y       DEVICE [n_rows][C] of y_type: x_type, or MRF_F32 (what the sweeps take as unaries); assigned
+ *   mean, rstd  DEVICE [n_rows] float or NULL, assigned: mu and s, which the backward call reads */
+int mrf_layer_norm_forward(int64_t n_rows, int32_t C, const void *x, int x_type, const float *gamma, const float *beta, float eps,
+                           void *y, int y_type, float *mean, float *rstd, void *hip_stream);
+
+/* Its gradients, with a = grad_y gamma:
+ *   grad_x = s (a - sum_c a / C - h sum_c (a h) / C),  grad_gamma = sum_rows grad_y h,  grad_beta = sum_rows grad_y
+ *   grad_y  DEVICE [n_rows][C] of y_type
+ *   grad_x  DEVICE [n_rows][C] of x_type, grad_gamma, grad_beta  DEVICE [C] float: each may be NULL, assigned
+ *   workspace  DEVICE, at least mrf_layer_norm_workspace_bytes(n_rows, C) (0 for sizes out of range), 256-byte aligned; may be
+ *           NULL where neither grad_gamma nor grad_beta is asked for */
+size_t mrf_layer_norm_workspace_bytes(int64_t n_rows, int32_t C);
+int mrf_layer_norm_backward(int64_t n_rows, int32_t C, const void *grad_y, int y_type, const void *x, int x_type, const float *gamma,
+                            const float *mean, const float *rstd, void *grad_x, float *grad_gamma, float *grad_beta, void *workspace,
+                            size_t workspace_bytes, void *hip_stream);
+
+/* The usual map of offsets d = first_offset, first_offset + 1, ... to buckets, for the two calls below.  Of the buckets of one
+ * sign (all n_buckets, or with two_sided the lower half for d <= 0 and the upper half for d > 0; one-sided, d > 0 is taken
+ * as d = 0) the first half hold one distance each, the others distances up to far_distance by their logarithm, and the last one
+ * all beyond.
+ *   bucket_of  HOST [n_offsets], assigned.  Host arithmetic.  A caller may as well make a map of its own. */
+int mrf_distance_buckets(int32_t n_buckets, int64_t far_distance, int two_sided, int64_t first_offset, int64_t n_offsets, int32_t *bucket_of);
+
+/* A pairwise function that depends on the distance of its labels, from a learned value per bucket of distances -- or any
+ * bias by relative position, with heads or edges for groups:
+ *   out[g][q][k] = table[g][bucket(k - q - query_offset)]
+ * One group with Q = K = L gives `pairwise` (V[mu][lambda], q = mu, k = lambda), R B H W groups give `pairwise_edge`;
+ * Q = 1 with query_offset = position of the row gives one row of a longer matrix.
+ *   table      DEVICE [n_groups][n_buckets] float, or [n_buckets][n_groups] with heads_last
+ *   bucket_of  DEVICE [n_offsets] int32: bucket of the offset first_offset + i.  Entries outside [0, n_buckets) are
+ *              clamped; a map that does not hold every offset of the call gives MRF_ERR_BAD_ARGUMENT
+ *   out        DEVICE [n_groups][Q][K] of out_type, assigned
+ * n_buckets 1..65536, Q and K may be 0. */
+int mrf_bucket_pairwise_forward(int64_t n_groups, int32_t Q, int32_t K, int32_t n_buckets, const float *table, int heads_last,
+                                const int32_t *bucket_of, int64_t first_offset, int64_t n_offsets, int64_t query_offset, void *out,
+                                int out_type, void *hip_stream);
+
+/* Its gradient: grad_table[g][b] = sum over the (q, k) of bucket b of grad_out[g][q][k], 0 for buckets without any.
+ *   grad_table DEVICE, laid out like table, assigned
+ *   workspace  DEVICE, at least mrf_bucket_pairwise_workspace_bytes(..) (0 for sizes out of range), 256-byte aligned */
+size_t mrf_bucket_pairwise_workspace_bytes(int64_t n_groups, int32_t Q, int32_t K, int32_t n_buckets);
+int mrf_bucket_pairwise_backward(int64_t n_groups, int32_t Q, int32_t K, int32_t n_buckets, const void *grad_out, int out_type,
+                                 int heads_last, const int32_t *bucket_of, int64_t first_offset, int64_t n_offsets, int64_t query_offset,
+                                 float *grad_table, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Log-probability of a label per pixel under the SoftMin of its costs (Eq. supp-isgmr-confidence):
+ *   logp = -c(a) - log sum_lambda exp(-c(lambda))
+ *   cost    DEVICE [n_pixels][L] of cost_type; +infinity = the label is not allowed (all of them: logp = -infinity)
+ *   labels  DEVICE [n_pixels] uint8 (label_bytes = 1, L <= 256) or int32 (label_bytes = 4, any L >= 1); values outside [0, L) are
+ *           clamped
+ *   logp    DEVICE [n_pixels] float, assigned */
+int mrf_softmin_logp(int64_t n_pixels, int32_t L, const void *cost, int cost_type, const void *labels, int label_bytes, float *logp,
+                     void *hip_stream);
+
+/* Clipped policy loss with a KL term: labels a that were drawn from the SoftMin probabilities f of earlier costs (log-
+ * probability old_logp) and earned an advantage A teach the present costs.  Per pixel, with lp = logp of a as above,
+ *   r = exp(lp - old_logp),  J = min(r A, min(max(r, 1 - clip_low), 1 + clip_high) A),  d = ref_logp - lp,  k = exp(d) - d - 1
+ *   loss = (1/n) sum over counted pixels (-J + kl_weight k)
+ *   grad_cost(lambda) = grad_scale d loss / d c(lambda) = grad_scale g / n (f(lambda) - [lambda = a]),
+ *   g = d loss_i / d lp = (-r A if r A <= the other term, else 0) + kl_weight (1 - exp(d))
+ * n = number of counted pixels; 0 for pixels that do not count, whose costs are not read, and for those without an allowed
+ * label, which stay in n.  A counted pixel whose own label is not allowed has r = 0 and an infinite k.
+ *   cost, labels  as above
+ *   advantage   DEVICE float: entry i / pixels_per_advantage is that of pixel i (1: one per pixel; H W: one per image)
+ *   old_logp    DEVICE [n_pixels] float, or NULL: that of the present costs (r = 1, and its gradient that of r)
+ *   ref_logp    DEVICE [n_pixels] float, or NULL (kl_weight must be 0): log-probability under reference costs
+ *   mask        DEVICE [n_pixels] uint8 or NULL: non-zero = the pixel counts (NULL: all count)
+ *   clip_low in [0, 1), clip_high >= 0, kl_weight >= 0, grad_scale finite (a power of two keeps MRF_F16 gradients in range),
+ *   else MRF_ERR_BAD_ARGUMENT
+ *   loss        DEVICE [3] float, assigned: the loss, its first term -(1/n) sum J, and (1/n) sum k (0 without ref_logp)
+ *   logp        DEVICE [n_pixels] float or NULL, assigned: lp, 0 for pixels that do not count
+ *   grad_cost   DEVICE [n_pixels][L] of cost_type or NULL, assigned: with MRF_F32 the grad_cost of mrf_*_backward
+ *   workspace   DEVICE, at least mrf_softmin_policy_workspace_bytes(), 256-byte aligned */
+size_t mrf_softmin_policy_workspace_bytes(void);
+int mrf_softmin_policy(int64_t n_pixels, int32_t L, const void *cost, int cost_type, const void *labels, int label_bytes,
+                       const float *advantage, int64_t pixels_per_advantage, const float *old_logp, const float *ref_logp,
+                       const uint8_t *mask, float clip_low, float clip_high, float kl_weight, float grad_scale, float *loss, float *logp,
+                       void *grad_cost, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* Some sweep layouts spread a scanline over several wavefronts that hand nodes to each other
  * through rings in on-chip memory.  A wavefront that still finds itself waiting for another four

@@ -2065,8 +2065,8 @@ const char *mrf_strerror(int status)
     switch (status) {
     case MRF_OK: return "ok";
     case MRF_ERR_NULL_POINTER: return "a required pointer is NULL";
-    case MRF_ERR_BAD_SHAPE: return "B, H, W must be >= 1 and B*H*W < 2^31";
-    case MRF_ERR_BAD_LABELS: return "L must be in [1, 256]";
+    case MRF_ERR_BAD_SHAPE: return "B, H, W must be >= 1 and B*H*W < 2^31 (rows, groups, pixels: 0 to 2^31 - 1)";
+    case MRF_ERR_BAD_LABELS: return "L must be in [1, 256] (32-bit labels: >= 1)";
     case MRF_ERR_BAD_ITERATIONS: return "K must be >= 1";
     case MRF_ERR_BAD_DIRECTIONS: return "R must be in [1, 16], steps non-zero and distinct";
     case MRF_ERR_WORKSPACE_TOO_SMALL: return "workspace smaller than mrf_workspace_bytes()";
@@ -2075,6 +2075,7 @@ const char *mrf_strerror(int status)
     case MRF_ERR_HIP: return "HIP runtime call or kernel launch failed";
     case MRF_ERR_WAIT_EXPIRED: return "a wait between wavefronts of a sweep ran out of its budget: the results of that call are incomplete";
     case MRF_ERR_SCRATCH_LIMIT: return "problem exceeds the fixed scratch of a no-allocation entry point (batch > 64)";
+    case MRF_ERR_BAD_ARGUMENT: return "a learning operator's type, map or parameter is outside its range";
     default: return "unknown status";
     }
 }

@@ -7,6 +7,7 @@ the shared library is missing, loading raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from dataclasses import dataclass
 from typing import Optional, Sequence
@@ -16,6 +17,7 @@ import numpy as np
 from .build import LIB_PATH
 
 MRF_ISGMR, MRF_TRWP = 0, 1
+MRF_F32, MRF_F16, MRF_BF16 = 0, 1, 2
 _lib = None
 
 
@@ -103,6 +105,27 @@ def load_library():
     lib.mrf_softmin_l1.argtypes = [ctypes.c_int64, ctypes.c_int32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.mrf_softmin_smooth_l1.restype = ci
     lib.mrf_softmin_smooth_l1.argtypes = [ctypes.c_int64, ctypes.c_int32, vp, vp, vp, ctypes.c_float, vp, vp, vp, vp, sz, vp]
+    i32, i64, f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+    lib.mrf_layer_norm_workspace_bytes.restype = sz
+    lib.mrf_layer_norm_workspace_bytes.argtypes = [i64, i32]
+    lib.mrf_layer_norm_forward.restype = ci
+    lib.mrf_layer_norm_forward.argtypes = [i64, i32, vp, ci, vp, vp, f32, vp, ci, vp, vp, vp]
+    lib.mrf_layer_norm_backward.restype = ci
+    lib.mrf_layer_norm_backward.argtypes = [i64, i32, vp, ci, vp, ci, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.mrf_distance_buckets.restype = ci
+    lib.mrf_distance_buckets.argtypes = [i32, i64, ci, i64, i64, vp]
+    lib.mrf_bucket_pairwise_workspace_bytes.restype = sz
+    lib.mrf_bucket_pairwise_workspace_bytes.argtypes = [i64, i32, i32, i32]
+    lib.mrf_bucket_pairwise_forward.restype = ci
+    lib.mrf_bucket_pairwise_forward.argtypes = [i64, i32, i32, i32, vp, ci, vp, i64, i64, i64, vp, ci, vp]
+    lib.mrf_bucket_pairwise_backward.restype = ci
+    lib.mrf_bucket_pairwise_backward.argtypes = [i64, i32, i32, i32, vp, ci, ci, vp, i64, i64, i64, vp, vp, sz, vp]
+    lib.mrf_softmin_logp.restype = ci
+    lib.mrf_softmin_logp.argtypes = [i64, i32, vp, ci, vp, ci, vp, vp]
+    lib.mrf_softmin_policy_workspace_bytes.restype = sz
+    lib.mrf_softmin_policy_workspace_bytes.argtypes = []
+    lib.mrf_softmin_policy.restype = ci
+    lib.mrf_softmin_policy.argtypes = [i64, i32, vp, ci, vp, ci, vp, i64, vp, vp, vp, f32, f32, f32, f32, vp, vp, vp, vp, sz, vp]
     lib.mrf_workspace_fault.restype = ci
     lib.mrf_workspace_fault.argtypes = [vp, vp]
     lib.mrf_strerror.argtypes = [ci]
@@ -333,6 +356,146 @@ def mrf_softmin_smooth_l1(cost, target, mask, beta, disparity, loss, grad_cost, 
                                               _dev_ptr(workspace), _ws_size(workspace), _stream_handle(stream))
     if rc != 0:
         raise MrfError(rc, "mrf_softmin_smooth_l1")
+
+
+# ---- learning operators: element types and sizes come from the tensors, which have to fit each other (ValueError)
+
+_TYPES = {"torch.float32": MRF_F32, "torch.float16": MRF_F16, "torch.bfloat16": MRF_BF16}
+
+
+def _type_of(t, what) -> int:
+    code = _TYPES.get(str(t.dtype))
+    if code is None:
+        raise ValueError("%s must be float32, float16 or bfloat16, got %s" % (what, t.dtype))
+    return code
+
+
+def _same_size(what, t, *shape):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError("%s has shape %s, expected %s" % (what, tuple(t.shape), tuple(shape)))
+
+
+def _checked(rc, name):
+    if rc != 0:
+        raise MrfError(rc, name)
+
+
+def mrf_layer_norm_workspace_bytes(n_rows: int, C: int) -> int:
+    return int(load_library().mrf_layer_norm_workspace_bytes(int(n_rows), int(C)))
+
+
+def mrf_layer_norm_forward(x, gamma, beta, eps, y, mean, rstd, stream=None):
+    """x [..., C] float32, float16 or bfloat16, gamma and beta [C] float32 or None, y like x (or float32), mean and rstd
+    [...] float32 or None."""
+    C, rows = int(x.shape[-1]), tuple(x.shape[:-1])
+    _same_size("y", y, *x.shape)
+    for name, t in (("gamma", gamma), ("beta", beta)):
+        _same_size(name, t, C)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _same_size(name, t, *rows)
+    _checked(load_library().mrf_layer_norm_forward(
+        math.prod(rows), C, _dev_ptr(x), _type_of(x, "x"), _dev_ptr(gamma, "float32"), _dev_ptr(beta, "float32"), float(eps),
+        _dev_ptr(y), _type_of(y, "y"), _dev_ptr(mean, "float32"), _dev_ptr(rstd, "float32"), _stream_handle(stream)),
+        "mrf_layer_norm_forward")
+
+
+def mrf_layer_norm_backward(grad_y, x, gamma, mean, rstd, grad_x, grad_gamma, grad_beta, workspace, stream=None):
+    """grad_y [..., C] of y's type, x, gamma, mean, rstd of the forward call; grad_x like x, grad_gamma and grad_beta [C] float32,
+    each of the three or None."""
+    C, rows = int(x.shape[-1]), tuple(x.shape[:-1])
+    _same_size("grad_y", grad_y, *x.shape)
+    _same_size("grad_x", grad_x, *x.shape)
+    for name, t in (("gamma", gamma), ("grad_gamma", grad_gamma), ("grad_beta", grad_beta)):
+        _same_size(name, t, C)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _same_size(name, t, *rows)
+    if grad_x is not None and grad_x.dtype != x.dtype:
+        raise ValueError("grad_x must be %s like x, got %s" % (x.dtype, grad_x.dtype))
+    _checked(load_library().mrf_layer_norm_backward(
+        math.prod(rows), C, _dev_ptr(grad_y), _type_of(grad_y, "grad_y"), _dev_ptr(x), _type_of(x, "x"), _dev_ptr(gamma, "float32"),
+        _dev_ptr(mean, "float32"), _dev_ptr(rstd, "float32"), _dev_ptr(grad_x), _dev_ptr(grad_gamma, "float32"),
+        _dev_ptr(grad_beta, "float32"), _dev_ptr(workspace), _ws_size(workspace), _stream_handle(stream)), "mrf_layer_norm_backward")
+
+
+def mrf_distance_buckets(n_buckets: int, far_distance: int, first_offset: int, n_offsets: int, two_sided: bool = True):
+    """Host array [n_offsets] int32: bucket of the offsets first_offset, first_offset + 1, .. (see the header)."""
+    out = np.empty(max(int(n_offsets), 0), np.int32)
+    _checked(load_library().mrf_distance_buckets(int(n_buckets), int(far_distance), int(bool(two_sided)), int(first_offset),
+                                                 int(n_offsets), out.ctypes.data), "mrf_distance_buckets")
+    return out
+
+
+def mrf_bucket_pairwise_workspace_bytes(n_groups: int, Q: int, K: int, n_buckets: int) -> int:
+    return int(load_library().mrf_bucket_pairwise_workspace_bytes(int(n_groups), int(Q), int(K), int(n_buckets)))
+
+
+def _bucket_sizes(table, out, heads_last):
+    """Groups, rows, columns and buckets of a table [..., n_buckets] (heads_last: [n_buckets, ...]) and a matrix [..., Q, K]."""
+    groups = tuple(out.shape[:-2])
+    NB = int(table.shape[0] if heads_last else table.shape[-1])
+    _same_size("table", table, *((NB, *groups) if heads_last else (*groups, NB)))
+    return math.prod(groups), int(out.shape[-2]), int(out.shape[-1]), NB
+
+
+def mrf_bucket_pairwise_forward(table, bucket_of, first_offset, out, query_offset=0, heads_last=False, stream=None):
+    """table [..., n_buckets] float32 (heads_last: [n_buckets, ...]), bucket_of [n] int32 on the GPU for the offsets from
+    first_offset on, out [..., Q, K] float32, float16 or bfloat16."""
+    G, Q, K, NB = _bucket_sizes(table, out, heads_last)
+    _checked(load_library().mrf_bucket_pairwise_forward(
+        G, Q, K, NB, _dev_ptr(table, "float32"), int(bool(heads_last)), _dev_ptr(bucket_of, "int32"), int(first_offset),
+        int(bucket_of.numel()), int(query_offset), _dev_ptr(out), _type_of(out, "out"), _stream_handle(stream)),
+        "mrf_bucket_pairwise_forward")
+
+
+def mrf_bucket_pairwise_backward(grad_out, bucket_of, first_offset, grad_table, workspace, query_offset=0, heads_last=False, stream=None):
+    """grad_out [..., Q, K], grad_table like the table of the forward call."""
+    G, Q, K, NB = _bucket_sizes(grad_table, grad_out, heads_last)
+    _checked(load_library().mrf_bucket_pairwise_backward(
+        G, Q, K, NB, _dev_ptr(grad_out), _type_of(grad_out, "grad_out"), int(bool(heads_last)), _dev_ptr(bucket_of, "int32"),
+        int(first_offset), int(bucket_of.numel()), int(query_offset), _dev_ptr(grad_table, "float32"), _dev_ptr(workspace),
+        _ws_size(workspace), _stream_handle(stream)), "mrf_bucket_pairwise_backward")
+
+
+def _label_bytes(labels) -> int:
+    size = {"torch.uint8": 1, "torch.int32": 4}.get(str(labels.dtype))
+    if size is None:
+        raise ValueError("labels must be uint8 or int32, got %s" % labels.dtype)
+    return size
+
+
+def mrf_softmin_logp(cost, labels, logp, stream=None):
+    """cost [..., L] float32, float16 or bfloat16, labels [...] uint8 (L <= 256) or int32, logp [...] float32."""
+    pixels, L = tuple(cost.shape[:-1]), int(cost.shape[-1])
+    _same_size("labels", labels, *pixels)
+    _same_size("logp", logp, *pixels)
+    _checked(load_library().mrf_softmin_logp(math.prod(pixels), L, _dev_ptr(cost), _type_of(cost, "cost"), _dev_ptr(labels),
+                                             _label_bytes(labels), _dev_ptr(logp, "float32"), _stream_handle(stream)), "mrf_softmin_logp")
+
+
+def mrf_softmin_policy_workspace_bytes() -> int:
+    return int(load_library().mrf_softmin_policy_workspace_bytes())
+
+
+def mrf_softmin_policy(cost, labels, advantage, old_logp, ref_logp, mask, clip_low, clip_high, kl_weight, loss, logp, grad_cost,
+                       workspace, pixels_per_advantage=1, grad_scale=1.0, stream=None):
+    """cost [..., L] float32, float16 or bfloat16, labels [...] uint8 or int32, advantage float32 with an entry per
+    pixels_per_advantage pixels, old_logp and ref_logp [...] float32 or None, mask [...] uint8 or None, loss [3] float32, logp
+    [...] float32 or None, grad_cost like cost or None."""
+    pixels, L = tuple(cost.shape[:-1]), int(cost.shape[-1])
+    n, per = math.prod(pixels), int(pixels_per_advantage)
+    for name, t in (("labels", labels), ("old_logp", old_logp), ("ref_logp", ref_logp), ("mask", mask), ("logp", logp)):
+        _same_size(name, t, *pixels)
+    _same_size("grad_cost", grad_cost, *cost.shape)
+    _same_size("loss", loss, 3)
+    if grad_cost is not None and grad_cost.dtype != cost.dtype:
+        raise ValueError("grad_cost must be %s like cost, got %s" % (cost.dtype, grad_cost.dtype))
+    if per >= 1 and int(advantage.numel()) != -(-n // per):
+        raise ValueError("advantage has %d entries, expected %d" % (advantage.numel(), -(-n // per)))
+    _checked(load_library().mrf_softmin_policy(
+        n, L, _dev_ptr(cost), _type_of(cost, "cost"), _dev_ptr(labels), _label_bytes(labels), _dev_ptr(advantage, "float32"), per,
+        _dev_ptr(old_logp, "float32"), _dev_ptr(ref_logp, "float32"), _dev_ptr(mask, "uint8"), float(clip_low), float(clip_high),
+        float(kl_weight), float(grad_scale), _dev_ptr(loss, "float32"), _dev_ptr(logp, "float32"), _dev_ptr(grad_cost),
+        _dev_ptr(workspace), _ws_size(workspace), _stream_handle(stream)), "mrf_softmin_policy")
 
 
 def mrf_workspace_fault(workspace, stream=None) -> int:
