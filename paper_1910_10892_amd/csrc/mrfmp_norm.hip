@@ -1,5 +1,5 @@
 // Layer norm over the rows of a matrix, forward and backward (see mrf_layer_norm_forward in the header for the formulas).
-#include "mrfmp_learn.h"
+#include "mrfmp_rows.h"
 
 struct MrfNormParams {
     long long N;
@@ -14,7 +14,157 @@ struct MrfNormParams {
     int P;
 };
 
-// ---- a wavefront per row: any length, any alignment
+// ---- rows in registers: one reading of x (forward), of x and dy (backward).  The variance is the mean square of the differences from the
+// mean, both taken from the registers.
+constexpr int mrf_norm_threads(int TL) { return TL <= 256 ? 256 : TL; }
+
+template <class X, class Y, int TL, int V, int CH>
+__global__ void __launch_bounds__(mrf_norm_threads(TL)) mrf_norm_fwd(const MrfNormParams Q)
+{
+    typedef MrfRow<TL, V, CH> Row;
+    constexpr int NT = mrf_norm_threads(TL), G = NT / TL;
+    __shared__ float scratch[2][NT / 64];
+    const int l = threadIdx.x % TL, C = Q.C;
+    const float inv = 1.0f / (float)C;
+    // (weight and bias of the lane's columns: kept for short rows, read again from the caches for long ones)
+    constexpr bool KEEP = Row::E <= 16;
+    float gamma[KEEP ? Row::E : 1], beta[KEEP ? Row::E : 1];
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int c = Row::column(l, i) + j;
+                gamma[i * V + j] = Q.gamma && c < C ? Q.gamma[c] : 1.0f;
+                beta[i * V + j] = Q.beta && c < C ? Q.beta[c] : 0.0f;
+            }
+    }
+    const long long step = (long long)gridDim.x * G;
+    for (long long base = (long long)blockIdx.x * G; base < Q.N; base += step) {
+        const long long r = base + threadIdx.x / TL, rr = r < Q.N ? r : Q.N - 1;
+        float x[Row::E];
+        Row::load((const X *)Q.x + (size_t)rr * C, C, l, x, 0.0f);
+        float s = 0.0f;
+#pragma unroll
+        for (int e = 0; e < Row::E; ++e) s += x[e];
+        const float mu = Row::sum(s, scratch[0]) * inv;
+        s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float &d = x[i * V + j];
+                d = Row::column(l, i) < C ? d - mu : 0.0f;
+                s = fmaf(d, d, s);
+            }
+        const float rs = 1.0f / sqrtf(Row::sum(s, scratch[1]) * inv + Q.eps);
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int c = Row::column(l, i) + j, e = i * V + j;
+                if constexpr (KEEP) x[e] = fmaf(x[e] * rs, gamma[e], beta[e]);
+                else if (c < C) x[e] = fmaf(x[e] * rs, Q.gamma ? Q.gamma[c] : 1.0f, Q.beta ? Q.beta[c] : 0.0f);
+            }
+        if (r < Q.N) {
+            Row::store((Y *)Q.y + (size_t)r * C, C, l, x);
+            if (l == 0 && Q.mean) Q.mean[r] = mu;
+            if (l == 0 && Q.rstd) Q.rstd[r] = rs;
+        }
+    }
+}
+
+// sum over the lanes of a wavefront that are a multiple of TL apart, in all of them
+template <int TL> __device__ inline float mrf_norm_across(float v)
+{
+    if constexpr (TL <= 4) v += mrf_dpp_f32<0x124>(v);       // row_ror:4
+    if constexpr (TL <= 8) v += mrf_dpp_f32<0x128>(v);       // row_ror:8
+    if constexpr (TL <= 16) v = mrf_xor16_f32(v, true);
+    if constexpr (TL <= 32) v = mrf_xor32_f32(v, true);
+    return v;
+}
+
+constexpr int mrf_norm_bwd_threads(int TL) { return TL <= 64 ? 512 : 1024; }
+
+// The sums over rows stay in registers while a workgroup goes through its rows, and end as one partial sum per workgroup and column.
+template <class X, class Y, int TL, int V, int CH>
+__global__ void __launch_bounds__(mrf_norm_bwd_threads(TL)) mrf_norm_bwd(const MrfNormParams Q)
+{
+    typedef MrfRow<TL, V, CH> Row;
+    constexpr int NT = mrf_norm_bwd_threads(TL), G = NT / TL, SLOTS = TL < 64 ? NT / 64 : G;
+    __shared__ float scratch[2][NT / 64];
+    __shared__ float share[SLOTS > 1 ? SLOTS * TL * V : 1];
+    const int l = threadIdx.x % TL, C = Q.C;
+    const float inv = 1.0f / (float)C;
+    float gamma[Row::E], sg[Row::E], sb[Row::E];
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int c = Row::column(l, i) + j;
+            gamma[i * V + j] = Q.gamma && c < C ? Q.gamma[c] : 1.0f;
+            sg[i * V + j] = sb[i * V + j] = 0.0f;
+        }
+    const long long step = (long long)gridDim.x * G;
+    for (long long base = (long long)blockIdx.x * G; base < Q.N; base += step) {
+        const long long r = base + threadIdx.x / TL, rr = r < Q.N ? r : Q.N - 1;
+        float x[Row::E], dy[Row::E];
+        Row::load((const X *)Q.x + (size_t)rr * C, C, l, x, 0.0f);
+        Row::load((const Y *)Q.dy + (size_t)rr * C, C, l, dy, 0.0f);
+        const float mu = Q.mean[rr], rs = Q.rstd[rr];
+        float sa = 0.0f, sh = 0.0f;
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int e = i * V + j;
+                x[e] = Row::column(l, i) < C ? (x[e] - mu) * rs : 0.0f;
+                if (r < Q.N) {
+                    sg[e] = fmaf(dy[e], x[e], sg[e]);
+                    sb[e] += dy[e];
+                }
+                dy[e] *= gamma[e];
+                sa += dy[e];
+                sh = fmaf(dy[e], x[e], sh);
+            }
+        sa = Row::sum(sa, scratch[0]) * inv;
+        sh = Row::sum(sh, scratch[1]) * inv;
+#pragma unroll
+        for (int e = 0; e < Row::E; ++e) dy[e] = rs * (dy[e] - sa - x[e] * sh);
+        if (r < Q.N && Q.dx) Row::store((X *)Q.dx + (size_t)r * C, C, l, dy);
+    }
+    if (!Q.partial) return;
+    float *partial = Q.partial + (size_t)blockIdx.x * 2 * C;
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            float v[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = mrf_norm_across<TL>(which ? sb[i * V + j] : sg[i * V + j]);
+            float *out = partial + (which ? C : 0);
+            if constexpr (SLOTS == 1) {
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (Row::column(l, i) + j < C) out[Row::column(l, i) + j] = v[j];
+            } else {
+                const int slot = TL < 64 ? threadIdx.x >> 6 : threadIdx.x / TL;
+                if (TL >= 64 || (threadIdx.x & 63) < TL)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) share[slot * TL * V + l * V + j] = v[j];
+                __syncthreads();
+                for (int k = threadIdx.x; k < TL * V; k += NT) {
+                    float t = share[k];
+#pragma unroll
+                    for (int w = 1; w < SLOTS; ++w) t += share[w * TL * V + k];
+                    if (TL * V * i + k < C) out[TL * V * i + k] = t;
+                }
+                __syncthreads();
+            }
+        }
+}
+
+// ---- a wavefront per row: any length
 template <class X, class Y>
 __global__ void __launch_bounds__(256) mrf_norm_fwd_any(const MrfNormParams Q)
 {
@@ -96,20 +246,26 @@ __global__ void __launch_bounds__(256) mrf_norm_param_any(const MrfNormParams Q)
     }
 }
 
-// weight and bias gradients from the P partial sums of a column, in order; grid (2 C / 64), 16 wavefronts share the partials
+// Weight and bias gradients from the P partial sums of a column: 16 columns per workgroup, 64 threads share a column's partial sums
+// (thread k takes every 64th from the k-th on) and add up by halves.
 __global__ void __launch_bounds__(1024) mrf_norm_param_sum(const MrfNormParams Q)
 {
-    __shared__ float sums[16][64];
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    const long long c = (long long)blockIdx.x * 64 + lane;      // [0, C) weight, [C, 2 C) bias
+    __shared__ float sums[64][17];
+    const int col = threadIdx.x & 15, part = threadIdx.x >> 4;
+    const long long c = (long long)blockIdx.x * 16 + col;      // [0, C) weight, [C, 2 C) bias
     float s = 0.0f;
     if (c < 2LL * Q.C)
-        for (int p = wv; p < Q.P; p += 16) s += Q.partial[(size_t)p * 2 * Q.C + c];
-    sums[wv][lane] = s;
+#pragma unroll 4
+        for (int p = part; p < Q.P; p += 64) s += Q.partial[(size_t)p * 2 * Q.C + c];
+    sums[part][col] = s;
     __syncthreads();
-    if (wv == 0 && c < 2LL * Q.C) {
-        s = 0.0f;
-        for (int w = 0; w < 16; ++w) s += sums[w][lane];
+#pragma unroll
+    for (int half = 32; half > 0; half >>= 1) {
+        if (part < half) sums[part][col] += sums[part + half][col];
+        __syncthreads();
+    }
+    if (part == 0 && c < 2LL * Q.C) {
+        s = sums[0][col];
         if (c < Q.C) {
             if (Q.dgamma) Q.dgamma[c] = s;
         } else if (Q.dbeta) {
@@ -122,13 +278,13 @@ using namespace mrf_host;
 
 namespace {
 
-// partial sums of the weight's gradient: no more than rows in fours, 8 MiB of them for rows of up to 16,384
+// Workgroups of a backward call at most: as many as run at once (two of 512 threads on each of 256 compute units and twice that, so that they
+// end at different times), but no more than make 4 MiB of partial sums, and 256 at least.
 int norm_partials(int64_t n_rows, int32_t C)
 {
-    long long p = (1LL << 20) / C;
-    p = p < 64 ? 64 : (p > 1024 ? 1024 : p);
-    const long long rows = (n_rows + 3) / 4;
-    return (int)(p < rows ? p : rows);
+    long long p = (1LL << 19) / C;
+    p = p < 256 ? 256 : (p > 1024 ? 1024 : p);
+    return (int)(p < n_rows ? p : n_rows);
 }
 
 int norm_check(int64_t n_rows, int32_t C, int x_type, int y_type)
@@ -138,28 +294,99 @@ int norm_check(int64_t n_rows, int32_t C, int x_type, int y_type)
     return MRF_OK;
 }
 
-template <class X, class Y> int norm_forward(const MrfNormParams &Q, hipStream_t st)
+template <class X, class Y, int TL, int V, int CH> int norm_fwd_rows(const MrfNormParams &Q, hipStream_t st)
 {
-    const long long rows = (Q.N + 3) / 4;
-    hipLaunchKernelGGL((mrf_norm_fwd_any<X, Y>), dim3((unsigned)(rows < 8192 ? rows : 8192)), dim3(256), 0, st, Q);
+    constexpr int NT = mrf_norm_threads(TL), G = NT / TL;
+    const long long need = (Q.N + G - 1) / G, most = NT == 256 ? 4096 : 1024;
+    hipLaunchKernelGGL((mrf_norm_fwd<X, Y, TL, V, CH>), dim3((unsigned)(need < most ? need : most)), dim3(NT), 0, st, Q);
     return launch_status("mrf_norm_fwd");
 }
 
-template <class X, class Y> int norm_backward(const MrfNormParams &Q, hipStream_t st)
+template <class X, class Y, int TL, int V, int CH> int norm_bwd_rows(const MrfNormParams &Q, hipStream_t st, int &blocks)
 {
+    constexpr int G = mrf_norm_bwd_threads(TL) / TL;
+    const long long need = (Q.N + G - 1) / G;
+    blocks = (int)(need < Q.P ? need : Q.P);
+    hipLaunchKernelGGL((mrf_norm_bwd<X, Y, TL, V, CH>), dim3((unsigned)blocks), dim3(mrf_norm_bwd_threads(TL)), 0, st, Q);
+    return launch_status("mrf_norm_bwd");
+}
+
+// elements per access
+int norm_vector(const MrfNormParams &Q, int x_bytes, int y_bytes)
+{
+    const void *at[4] = {Q.x, Q.y, Q.dy, Q.dx};
+    const int bytes[4] = {x_bytes, y_bytes, y_bytes, x_bytes};
+    if (x_bytes == 2 && Q.C > 256 && row_vector_8(Q.C, at, 4)) return 8;
+    return row_vector(Q.C, at, bytes, 4);
+}
+
+// Forward a lane holds three values per column: 16 columns at most where a workgroup of 1,024 threads leaves 128 registers.
+#define MRF_NORM_FWD_8(F) F(64, 8, 1) F(64, 8, 2) F(64, 8, 3) F(64, 8, 4) F(256, 8, 2) F(256, 8, 3) F(256, 8, 4) F(1024, 8, 2)
+#define MRF_NORM_FWD_4(F) \
+    F(4, 4, 1) F(8, 4, 1) F(8, 4, 2) F(8, 4, 3) F(16, 4, 2) F(16, 4, 3) F(16, 4, 4) F(64, 4, 2) F(64, 4, 3) F(64, 4, 4) F(64, 4, 6) F(64, 4, 8) \
+    F(256, 4, 4) F(256, 4, 6) F(256, 4, 8) F(1024, 4, 4)
+#define MRF_NORM_FWD_1(F) \
+    F(4, 1, 1) F(4, 1, 2) F(4, 1, 3) F(4, 1, 4) F(8, 1, 3) F(8, 1, 4) F(8, 1, 5) F(8, 1, 6) F(8, 1, 7) F(8, 1, 8) F(16, 1, 5) F(16, 1, 6) F(16, 1, 7) F(16, 1, 8) \
+    F(32, 1, 5) F(32, 1, 6) F(32, 1, 7) F(32, 1, 8) F(64, 1, 6) F(64, 1, 8) F(64, 1, 12) F(64, 1, 16) F(64, 1, 24) F(64, 1, 32) \
+    F(256, 1, 12) F(256, 1, 16) F(256, 1, 24) F(256, 1, 32) F(1024, 1, 12) F(1024, 1, 16)
+
+template <class X, class Y> int norm_forward(const MrfNormParams &Q, hipStream_t st)
+{
+    const int v = norm_vector(Q, sizeof(X), sizeof(Y));
+#define MRF_LAUNCH(TL, V, CH) \
+    if (Q.C <= TL * V * CH) return norm_fwd_rows<X, Y, TL, V, CH>(Q, st);
+    if constexpr (sizeof(X) == 2) {
+        if (v == 8) { MRF_NORM_FWD_8(MRF_LAUNCH) }
+    }
+    if (v == 4) { MRF_NORM_FWD_4(MRF_LAUNCH) }
+    if (v == 1) { MRF_NORM_FWD_1(MRF_LAUNCH) }
+#undef MRF_LAUNCH
     const long long rows = (Q.N + 3) / 4;
-    if (Q.N > 0 && Q.dx) {
+    hipLaunchKernelGGL((mrf_norm_fwd_any<X, Y>), dim3((unsigned)(rows < 8192 ? rows : 8192)), dim3(256), 0, st, Q);
+    return launch_status("mrf_norm_fwd_any");
+}
+
+// Backward a lane holds five values per column (x, dy, the weight, two sums): eight columns at most where a workgroup of 1,024 threads
+// leaves 128 registers, 16 else.
+#define MRF_NORM_BWD_8(F) F(64, 8, 1) F(64, 8, 2) F(256, 8, 1) F(1024, 8, 1)
+#define MRF_NORM_BWD_4(F) \
+    F(4, 4, 1) F(8, 4, 1) F(8, 4, 2) F(8, 4, 3) F(16, 4, 2) F(16, 4, 3) F(16, 4, 4) F(64, 4, 2) F(64, 4, 3) F(64, 4, 4) F(256, 4, 2) F(1024, 4, 1) F(1024, 4, 2)
+#define MRF_NORM_BWD_1(F) \
+    F(4, 1, 1) F(4, 1, 2) F(4, 1, 3) F(4, 1, 4) F(8, 1, 3) F(8, 1, 4) F(8, 1, 5) F(8, 1, 6) F(8, 1, 7) F(8, 1, 8) F(16, 1, 5) F(16, 1, 6) F(16, 1, 7) F(16, 1, 8) \
+    F(32, 1, 5) F(32, 1, 6) F(32, 1, 7) F(32, 1, 8) F(64, 1, 6) F(64, 1, 8) F(64, 1, 12) F(64, 1, 16) F(256, 1, 6) F(256, 1, 8) F(1024, 1, 4) F(1024, 1, 6) F(1024, 1, 8)
+
+template <class X, class Y> int norm_bwd_launch(MrfNormParams &Q, hipStream_t st)
+{
+    const int v = norm_vector(Q, sizeof(X), sizeof(Y));
+#define MRF_LAUNCH(TL, V, CH) \
+    if (Q.C <= TL * V * CH) return norm_bwd_rows<X, Y, TL, V, CH>(Q, st, Q.P);
+    if constexpr (sizeof(X) == 2) {
+        if (v == 8) { MRF_NORM_BWD_8(MRF_LAUNCH) }
+    }
+    if (v == 4) { MRF_NORM_BWD_4(MRF_LAUNCH) }
+    if (v == 1) { MRF_NORM_BWD_1(MRF_LAUNCH) }
+#undef MRF_LAUNCH
+    if (Q.dx) {
+        const long long rows = (Q.N + 3) / 4;
         hipLaunchKernelGGL((mrf_norm_bwd_any<X, Y>), dim3((unsigned)(rows < 8192 ? rows : 8192)), dim3(256), 0, st, Q);
-        const int rc = launch_status("mrf_norm_bwd");
+        const int rc = launch_status("mrf_norm_bwd_any");
         if (rc != MRF_OK) return rc;
     }
-    if (!Q.dgamma && !Q.dbeta) return MRF_OK;
-    if (Q.N > 0) {
-        hipLaunchKernelGGL((mrf_norm_param_any<X, Y>), dim3((unsigned)((Q.C + 63) / 64), (unsigned)Q.P), dim3(256), 0, st, Q);
-        const int rc = launch_status("mrf_norm_param");
+    if (!Q.partial) return MRF_OK;
+    hipLaunchKernelGGL((mrf_norm_param_any<X, Y>), dim3((unsigned)((Q.C + 63) / 64), (unsigned)Q.P), dim3(256), 0, st, Q);
+    return launch_status("mrf_norm_param_any");
+}
+
+template <class X, class Y> int norm_backward(MrfNormParams Q, hipStream_t st)
+{
+    const bool params = Q.dgamma || Q.dbeta;
+    if (!params) Q.partial = nullptr;
+    if (Q.N > 0 && (params || Q.dx)) {
+        const int rc = norm_bwd_launch<X, Y>(Q, st);
         if (rc != MRF_OK) return rc;
     }
-    hipLaunchKernelGGL(mrf_norm_param_sum, dim3((unsigned)((2LL * Q.C + 63) / 64)), dim3(1024), 0, st, Q);
+    if (!params) return MRF_OK;
+    hipLaunchKernelGGL(mrf_norm_param_sum, dim3((unsigned)((2LL * Q.C + 15) / 16)), dim3(1024), 0, st, Q);
     return launch_status("mrf_norm_param_sum");
 }
 
