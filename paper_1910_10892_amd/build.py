@@ -9,7 +9,7 @@ CSRC = os.path.join(os.path.dirname(os.path.abspath(__file__)), "csrc")
 LIB_PATH = os.path.join(CSRC, "libmrfmp.so")
 SOURCES = ["mrfmp.hip"]
 LEARN_SOURCES = ["mrfmp_norm.hip", "mrfmp_bucket.hip", "mrfmp_policy.hip"]
-HEADERS = ["mrfmp_learn.h", "mrfmp_device.h", "mrfmp_fwd.h", "mrfmp_bwd.h", "mrfmp_bwd_sum.h", "mrfmp_head.h", "../../include/mrfmp.h"]
+HEADERS = ["mrfmp_learn.h", "mrfmp_rows.h", "mrfmp_device.h", "mrfmp_fwd.h", "mrfmp_bwd.h", "mrfmp_bwd_sum.h", "mrfmp_head.h", "../../include/mrfmp.h"]
 
 # -ffp-contract=off: the only fused multiply-add is the explicit one of the message update,
 #   so that floating point decisions (argmins) match a plain C evaluation order.

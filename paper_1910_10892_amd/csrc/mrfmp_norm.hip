@@ -1,6 +1,8 @@
 // Layer norm over the rows of a matrix, forward and backward (see mrf_layer_norm_forward in the header for the formulas).
 #include "mrfmp_rows.h"
 
+#include <type_traits>
+
 struct MrfNormParams {
     long long N;
     int C;
@@ -18,65 +20,117 @@ struct MrfNormParams {
 // mean, both taken from the registers.
 constexpr int mrf_norm_threads(int TL) { return TL <= 256 ? 256 : TL; }
 
+// rows of a lane that are on their way at once: a launch of short rows would otherwise wait for memory most of its time
+constexpr int mrf_norm_batch(int E) { return E <= 4 ? 4 : (E <= 12 ? 2 : 1); }
+
 template <class X, class Y, int TL, int V, int CH>
 __global__ void __launch_bounds__(mrf_norm_threads(TL)) mrf_norm_fwd(const MrfNormParams Q)
 {
     typedef MrfRow<TL, V, CH> Row;
-    constexpr int NT = mrf_norm_threads(TL), G = NT / TL;
+    constexpr int NT = mrf_norm_threads(TL), G = NT / TL, U = TL <= 64 ? mrf_norm_batch(Row::E) : 1;
     __shared__ float scratch[2][NT / 64];
     const int l = threadIdx.x % TL, C = Q.C;
     const float inv = 1.0f / (float)C;
-    // (weight and bias of the lane's columns: kept for short rows, read again from the caches for long ones)
-    constexpr bool KEEP = Row::E <= 16;
-    float gamma[KEEP ? Row::E : 1], beta[KEEP ? Row::E : 1];
-    if constexpr (KEEP) {
+    float gamma[Row::E], beta[Row::E], in_row[Row::E];      // (in_row: 1 in the row's columns, 0 behind them)
+    Row::load_columns(Q.gamma, C, l, gamma, 1.0f);
+    Row::load_columns(Q.beta, C, l, beta, 0.0f);
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
+    for (int e = 0; e < Row::E; ++e) in_row[e] = Row::column(l, e / V) + e % V < C ? 1.0f : 0.0f;
+    const unsigned group = threadIdx.x / TL, mine = group * (unsigned)C;
+
+    const long long step = (long long)gridDim.x * G;      // rows that a launch takes at once
+
+    // n rows of every group of lanes, `step` apart
+    const auto rows = [&](auto fast, auto batch, const long long base) {
+        constexpr bool FAST = decltype(fast)::value;
+        constexpr int n = decltype(batch)::value;
+        typename Row::template Raw<X> in[n];
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int c = Row::column(l, i) + j;
-                gamma[i * V + j] = Q.gamma && c < C ? Q.gamma[c] : 1.0f;
-                beta[i * V + j] = Q.beta && c < C ? Q.beta[c] : 0.0f;
+        for (int u = 0; u < n; ++u)
+            Row::template load<FAST>((const X *)Q.x + (size_t)(base + u * step) * C, mine, FAST || base + group < Q.N, C, l, in[u]);
+#pragma unroll
+        for (int u = 0; u < n; ++u) {
+            const long long first = base + u * step;
+            float x[Row::E];
+            Row::convert(in[u], C, l, x, 0.0f);
+            float s = 0.0f;
+#pragma unroll
+            for (int e = 0; e < Row::E; ++e) s += x[e];
+            const float mu = Row::sum(s, scratch[0]) * inv;
+            s = 0.0f;
+#pragma unroll
+            for (int e = 0; e < Row::E; ++e) {
+                x[e] = fmaf(-mu, in_row[e], x[e]);
+                s = fmaf(x[e], x[e], s);
             }
+            const float rs = rsqrtf(Row::sum(s, scratch[1]) * inv + Q.eps);
+#pragma unroll
+            for (int e = 0; e < Row::E; ++e) x[e] = fmaf(x[e] * rs, gamma[e], beta[e]);
+            if (FAST || first + group < Q.N) {
+                Row::store((Y *)Q.y + (size_t)first * C + mine, C, l, x);
+                if (l == 0 && Q.mean) Q.mean[first + group] = mu;
+                if (l == 0 && Q.rstd) Q.rstd[first + group] = rs;
+            }
+        }
+    };
+    for (long long base = (long long)blockIdx.x * G; base < Q.N;) {
+        if (U > 1 && mrf_rows_fast(base + (U - 1) * step, G, V, Q.N)) {
+            rows(std::true_type{}, std::integral_constant<int, U>{}, base);
+            base += U * step;
+        } else {
+            if (mrf_rows_fast(base, G, V, Q.N)) rows(std::true_type{}, std::integral_constant<int, 1>{}, base);
+            else rows(std::false_type{}, std::integral_constant<int, 1>{}, base);
+            base += step;
+        }
     }
-    const long long step = (long long)gridDim.x * G;
-    for (long long base = (long long)blockIdx.x * G; base < Q.N; base += step) {
-        const long long r = base + threadIdx.x / TL, rr = r < Q.N ? r : Q.N - 1;
-        float x[Row::E];
-        Row::load((const X *)Q.x + (size_t)rr * C, C, l, x, 0.0f);
+}
+
+// the same for short rows through LDS (MrfTile)
+template <class X, class Y, int TL, int E>
+__global__ void __launch_bounds__(256) mrf_norm_fwd_tile(const MrfNormParams Q)
+{
+    typedef MrfTile<TL, E> Tile;
+    __shared__ __align__(16) char lds[4][Tile::BYTES];
+    const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, l = lane % TL, g = lane / TL, C = Q.C;
+    const float inv = 1.0f / (float)C;
+    float gamma[E], beta[E];
+    Tile::load_columns(Q.gamma, C, l, gamma, 1.0f);
+    Tile::load_columns(Q.beta, C, l, beta, 0.0f);
+    const long long step = (long long)gridDim.x * 4 * Tile::ROWS;
+    for (long long base = ((long long)blockIdx.x * 4 + wv) * Tile::ROWS; base < Q.N; base += step) {
+        const int rows = Q.N - base < Tile::ROWS ? (int)(Q.N - base) : Tile::ROWS;
+        Tile::fetch((const X *)Q.x + (size_t)base * C, rows, C, (X *)lds[wv]);
+        mrf_wave_lds_fence();
+        float x[E];
+        Tile::take((const X *)lds[wv], g, C, l, x, 0.0f);
         float s = 0.0f;
 #pragma unroll
-        for (int e = 0; e < Row::E; ++e) s += x[e];
-        const float mu = Row::sum(s, scratch[0]) * inv;
+        for (int e = 0; e < E; ++e) s += x[e];
+        const float mu = Tile::sum(s) * inv;
         s = 0.0f;
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                float &d = x[i * V + j];
-                d = Row::column(l, i) < C ? d - mu : 0.0f;
-                s = fmaf(d, d, s);
-            }
-        const float rs = 1.0f / sqrtf(Row::sum(s, scratch[1]) * inv + Q.eps);
-#pragma unroll
-        for (int i = 0; i < CH; ++i)
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int c = Row::column(l, i) + j, e = i * V + j;
-                if constexpr (KEEP) x[e] = fmaf(x[e] * rs, gamma[e], beta[e]);
-                else if (c < C) x[e] = fmaf(x[e] * rs, Q.gamma ? Q.gamma[c] : 1.0f, Q.beta ? Q.beta[c] : 0.0f);
-            }
-        if (r < Q.N) {
-            Row::store((Y *)Q.y + (size_t)r * C, C, l, x);
-            if (l == 0 && Q.mean) Q.mean[r] = mu;
-            if (l == 0 && Q.rstd) Q.rstd[r] = rs;
+        for (int e = 0; e < E; ++e) {
+            x[e] = Tile::column(l, e) < C ? x[e] - mu : 0.0f;
+            s = fmaf(x[e], x[e], s);
         }
+        const float rs = rsqrtf(Tile::sum(s) * inv + Q.eps);
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = fmaf(x[e] * rs, gamma[e], beta[e]);
+        mrf_wave_lds_fence();
+        Tile::put((Y *)lds[wv], g, C, l, x);
+        mrf_wave_lds_fence();
+        Tile::flush((Y *)Q.y + (size_t)base * C, rows, C, (const Y *)lds[wv]);
+        if (l == 0 && g < rows && Q.mean) Q.mean[base + g] = mu;
+        if (l == 0 && g < rows && Q.rstd) Q.rstd[base + g] = rs;
+        mrf_wave_lds_fence();
     }
 }
 
 // sum over the lanes of a wavefront that are a multiple of TL apart, in all of them
 template <int TL> __device__ inline float mrf_norm_across(float v)
 {
+    if constexpr (TL <= 1) v += mrf_dpp_f32<0x121>(v);       // row_ror:1
+    if constexpr (TL <= 2) v += mrf_dpp_f32<0x122>(v);       // row_ror:2
     if constexpr (TL <= 4) v += mrf_dpp_f32<0x124>(v);       // row_ror:4
     if constexpr (TL <= 8) v += mrf_dpp_f32<0x128>(v);       // row_ror:8
     if constexpr (TL <= 16) v = mrf_xor16_f32(v, true);
@@ -91,47 +145,68 @@ template <class X, class Y, int TL, int V, int CH>
 __global__ void __launch_bounds__(mrf_norm_bwd_threads(TL)) mrf_norm_bwd(const MrfNormParams Q)
 {
     typedef MrfRow<TL, V, CH> Row;
-    constexpr int NT = mrf_norm_bwd_threads(TL), G = NT / TL, SLOTS = TL < 64 ? NT / 64 : G;
+    constexpr int NT = mrf_norm_bwd_threads(TL), G = NT / TL, U = TL == 256 ? 2 : (TL < 256 ? mrf_norm_batch(2 * Row::E) : 1), SLOTS = TL < 64 ? NT / 64 : G;
     __shared__ float scratch[2][NT / 64];
     __shared__ float share[SLOTS > 1 ? SLOTS * TL * V : 1];
     const int l = threadIdx.x % TL, C = Q.C;
     const float inv = 1.0f / (float)C;
     float gamma[Row::E], sg[Row::E], sb[Row::E];
+    Row::load_columns(Q.gamma, C, l, gamma, 1.0f);
 #pragma unroll
-    for (int i = 0; i < CH; ++i)
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int c = Row::column(l, i) + j;
-            gamma[i * V + j] = Q.gamma && c < C ? Q.gamma[c] : 1.0f;
-            sg[i * V + j] = sb[i * V + j] = 0.0f;
-        }
+    for (int e = 0; e < Row::E; ++e) sg[e] = sb[e] = 0.0f;
+    const unsigned group = threadIdx.x / TL, mine = group * (unsigned)C;
+
     const long long step = (long long)gridDim.x * G;
-    for (long long base = (long long)blockIdx.x * G; base < Q.N; base += step) {
-        const long long r = base + threadIdx.x / TL, rr = r < Q.N ? r : Q.N - 1;
-        float x[Row::E], dy[Row::E];
-        Row::load((const X *)Q.x + (size_t)rr * C, C, l, x, 0.0f);
-        Row::load((const Y *)Q.dy + (size_t)rr * C, C, l, dy, 0.0f);
-        const float mu = Q.mean[rr], rs = Q.rstd[rr];
-        float sa = 0.0f, sh = 0.0f;
+
+    const auto rows = [&](auto fast, auto batch, const long long base) {
+        constexpr bool FAST = decltype(fast)::value;
+        constexpr int n = decltype(batch)::value;
+        typename Row::template Raw<X> in[n];
+        typename Row::template Raw<Y> grad[n];
+        float mean[n], rstd[n];
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
+        for (int u = 0; u < n; ++u) {
+            const long long first = base + u * step;
+            const bool there = FAST || first + group < Q.N;
+            Row::template load<FAST>((const X *)Q.x + (size_t)first * C, mine, there, C, l, in[u]);
+            Row::template load<FAST>((const Y *)Q.dy + (size_t)first * C, mine, there, C, l, grad[u]);
+            mean[u] = there ? Q.mean[first + group] : 0.0f;
+            rstd[u] = there ? Q.rstd[first + group] : 0.0f;
+        }
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int e = i * V + j;
-                x[e] = Row::column(l, i) < C ? (x[e] - mu) * rs : 0.0f;
-                if (r < Q.N) {
-                    sg[e] = fmaf(dy[e], x[e], sg[e]);
-                    sb[e] += dy[e];
-                }
+        for (int u = 0; u < n; ++u) {
+            const long long first = base + u * step;
+            const float mu = mean[u], rs = rstd[u];
+            float x[Row::E], dy[Row::E];
+            Row::convert(in[u], C, l, x, 0.0f);
+            Row::convert(grad[u], C, l, dy, 0.0f);
+            float sa = 0.0f, sh = 0.0f;
+            // (behind a row's end, and behind the last row, dy is 0: nothing is added)
+#pragma unroll
+            for (int e = 0; e < Row::E; ++e) {
+                x[e] = (x[e] - mu) * rs;
+                sg[e] = fmaf(dy[e], x[e], sg[e]);
+                sb[e] += dy[e];
                 dy[e] *= gamma[e];
                 sa += dy[e];
                 sh = fmaf(dy[e], x[e], sh);
             }
-        sa = Row::sum(sa, scratch[0]) * inv;
-        sh = Row::sum(sh, scratch[1]) * inv;
+            sa = Row::sum(sa, scratch[0]) * inv;
+            sh = Row::sum(sh, scratch[1]) * inv;
 #pragma unroll
-        for (int e = 0; e < Row::E; ++e) dy[e] = rs * (dy[e] - sa - x[e] * sh);
-        if (r < Q.N && Q.dx) Row::store((X *)Q.dx + (size_t)r * C, C, l, dy);
+            for (int e = 0; e < Row::E; ++e) dy[e] = rs * (dy[e] - sa - x[e] * sh);
+            if (Q.dx && (FAST || first + group < Q.N)) Row::store((X *)Q.dx + (size_t)first * C + mine, C, l, dy);
+        }
+    };
+    for (long long base = (long long)blockIdx.x * G; base < Q.N;) {
+        if (U > 1 && mrf_rows_fast(base + (U - 1) * step, G, V, Q.N)) {
+            rows(std::true_type{}, std::integral_constant<int, U>{}, base);
+            base += U * step;
+        } else {
+            if (mrf_rows_fast(base, G, V, Q.N)) rows(std::true_type{}, std::integral_constant<int, 1>{}, base);
+            else rows(std::false_type{}, std::integral_constant<int, 1>{}, base);
+            base += step;
+        }
     }
     if (!Q.partial) return;
     float *partial = Q.partial + (size_t)blockIdx.x * 2 * C;
@@ -182,7 +257,7 @@ __global__ void __launch_bounds__(256) mrf_norm_fwd_any(const MrfNormParams Q)
             const float d = mrf_to_f32(x[c]) - mu;
             s += d * d;
         }
-        const float rs = 1.0f / sqrtf(mrf_lanes_sum<64>(s) * inv + Q.eps);
+        const float rs = rsqrtf(mrf_lanes_sum<64>(s) * inv + Q.eps);
         for (int c = lane; c < Q.C; c += 64) {
             const float h = (mrf_to_f32(x[c]) - mu) * rs;
             const float g = Q.gamma ? Q.gamma[c] : 1.0f, b = Q.beta ? Q.beta[c] : 0.0f;
@@ -278,13 +353,12 @@ using namespace mrf_host;
 
 namespace {
 
-// Workgroups of a backward call at most: as many as run at once (two of 512 threads on each of 256 compute units and twice that, so that they
-// end at different times), but no more than make 4 MiB of partial sums, and 256 at least.
+// Workgroups of a backward call at most, each of which leaves a partial sum: two of 512 threads on each compute unit; one of 1,024
+// for long rows, whose partial sums take memory traffic of their own.
 int norm_partials(int64_t n_rows, int32_t C)
 {
-    long long p = (1LL << 19) / C;
-    p = p < 256 ? 256 : (p > 1024 ? 1024 : p);
-    return (int)(p < n_rows ? p : n_rows);
+    const int most = C <= 1024 ? 512 : 256;
+    return (int)(most < n_rows ? most : n_rows);
 }
 
 int norm_check(int64_t n_rows, int32_t C, int x_type, int y_type)
@@ -311,60 +385,60 @@ template <class X, class Y, int TL, int V, int CH> int norm_bwd_rows(const MrfNo
     return launch_status("mrf_norm_bwd");
 }
 
-// elements per access
-int norm_vector(const MrfNormParams &Q, int x_bytes, int y_bytes)
-{
-    const void *at[4] = {Q.x, Q.y, Q.dy, Q.dx};
-    const int bytes[4] = {x_bytes, y_bytes, y_bytes, x_bytes};
-    if (x_bytes == 2 && Q.C > 256 && row_vector_8(Q.C, at, 4)) return 8;
-    return row_vector(Q.C, at, bytes, 4);
-}
+// F(TL, V, CH) for each layout, shortest rows first.  Forward a lane holds three values per column (x, weight, bias), backward five (x, dy,
+// the weight, two sums): 16 and 8 columns at most where a workgroup of 1,024 threads leaves 128 registers.
+#define MRF_NORM_FWD_SHORT(F) \
+    F(1, 4, 1) F(2, 4, 1) F(4, 4, 1) F(8, 4, 1) F(8, 4, 2) F(8, 4, 3) F(16, 4, 2) F(16, 4, 3) F(16, 4, 4)
+#define MRF_NORM_FWD_LONG(F) \
+    F(64, 4, 2) F(64, 4, 3) F(64, 4, 4) F(256, 4, 2) F(256, 4, 3) F(256, 4, 4) F(1024, 4, 2) F(1024, 4, 3) F(1024, 4, 4)
+#define MRF_NORM_FWD_LONG_16(F) F(64, 8, 1) F(64, 8, 2) F(256, 8, 1) F(256, 8, 2) F(1024, 8, 1) F(1024, 8, 2)
+#define MRF_NORM_BWD_SHORT(F) F(1, 4, 1) F(2, 4, 1) F(4, 4, 1) F(8, 4, 1) F(8, 4, 2) F(16, 4, 2) F(16, 4, 3) F(16, 4, 4)
+#define MRF_NORM_BWD_LONG(F) F(64, 4, 2) F(64, 4, 3) F(64, 4, 4) F(256, 4, 2) F(1024, 4, 1) F(1024, 4, 2)
+#define MRF_NORM_BWD_LONG_16(F) F(64, 8, 1) F(64, 8, 2) F(256, 8, 1) F(1024, 8, 1)
 
-// Forward a lane holds three values per column: 16 columns at most where a workgroup of 1,024 threads leaves 128 registers.
-#define MRF_NORM_FWD_8(F) F(64, 8, 1) F(64, 8, 2) F(64, 8, 3) F(64, 8, 4) F(256, 8, 2) F(256, 8, 3) F(256, 8, 4) F(1024, 8, 2)
-#define MRF_NORM_FWD_4(F) \
-    F(4, 4, 1) F(8, 4, 1) F(8, 4, 2) F(8, 4, 3) F(16, 4, 2) F(16, 4, 3) F(16, 4, 4) F(64, 4, 2) F(64, 4, 3) F(64, 4, 4) F(64, 4, 6) F(64, 4, 8) \
-    F(256, 4, 4) F(256, 4, 6) F(256, 4, 8) F(1024, 4, 4)
-#define MRF_NORM_FWD_1(F) \
-    F(4, 1, 1) F(4, 1, 2) F(4, 1, 3) F(4, 1, 4) F(8, 1, 3) F(8, 1, 4) F(8, 1, 5) F(8, 1, 6) F(8, 1, 7) F(8, 1, 8) F(16, 1, 5) F(16, 1, 6) F(16, 1, 7) F(16, 1, 8) \
-    F(32, 1, 5) F(32, 1, 6) F(32, 1, 7) F(32, 1, 8) F(64, 1, 6) F(64, 1, 8) F(64, 1, 12) F(64, 1, 16) F(64, 1, 24) F(64, 1, 32) \
-    F(256, 1, 12) F(256, 1, 16) F(256, 1, 24) F(256, 1, 32) F(1024, 1, 12) F(1024, 1, 16)
+// rows of C columns through LDS?
+bool norm_tiles(int C) { return C % 4 != 0 && C <= MRF_TILES_LONGEST; }
+
+template <class X, class Y, int TL, int E> int norm_fwd_tiles(const MrfNormParams &Q, hipStream_t st)
+{
+    constexpr int G = 4 * MrfTile<TL, E>::ROWS;
+    const long long need = (Q.N + G - 1) / G;
+    hipLaunchKernelGGL((mrf_norm_fwd_tile<X, Y, TL, E>), dim3((unsigned)(need < 2048 ? need : 2048)), dim3(256), 0, st, Q);
+    return launch_status("mrf_norm_fwd_tile");
+}
 
 template <class X, class Y> int norm_forward(const MrfNormParams &Q, hipStream_t st)
 {
-    const int v = norm_vector(Q, sizeof(X), sizeof(Y));
+    if (norm_tiles(Q.C)) {
+#define MRF_LAUNCH(TL, E) \
+        if (Q.C <= TL * E) return norm_fwd_tiles<X, Y, TL, E>(Q, st);
+        MRF_TILES(MRF_LAUNCH)
+#undef MRF_LAUNCH
+    }
 #define MRF_LAUNCH(TL, V, CH) \
     if (Q.C <= TL * V * CH) return norm_fwd_rows<X, Y, TL, V, CH>(Q, st);
+    MRF_NORM_FWD_SHORT(MRF_LAUNCH)
     if constexpr (sizeof(X) == 2) {
-        if (v == 8) { MRF_NORM_FWD_8(MRF_LAUNCH) }
+        MRF_NORM_FWD_LONG_16(MRF_LAUNCH)
+    } else {
+        MRF_NORM_FWD_LONG(MRF_LAUNCH)
     }
-    if (v == 4) { MRF_NORM_FWD_4(MRF_LAUNCH) }
-    if (v == 1) { MRF_NORM_FWD_1(MRF_LAUNCH) }
 #undef MRF_LAUNCH
     const long long rows = (Q.N + 3) / 4;
     hipLaunchKernelGGL((mrf_norm_fwd_any<X, Y>), dim3((unsigned)(rows < 8192 ? rows : 8192)), dim3(256), 0, st, Q);
     return launch_status("mrf_norm_fwd_any");
 }
 
-// Backward a lane holds five values per column (x, dy, the weight, two sums): eight columns at most where a workgroup of 1,024 threads
-// leaves 128 registers, 16 else.
-#define MRF_NORM_BWD_8(F) F(64, 8, 1) F(64, 8, 2) F(256, 8, 1) F(1024, 8, 1)
-#define MRF_NORM_BWD_4(F) \
-    F(4, 4, 1) F(8, 4, 1) F(8, 4, 2) F(8, 4, 3) F(16, 4, 2) F(16, 4, 3) F(16, 4, 4) F(64, 4, 2) F(64, 4, 3) F(64, 4, 4) F(256, 4, 2) F(1024, 4, 1) F(1024, 4, 2)
-#define MRF_NORM_BWD_1(F) \
-    F(4, 1, 1) F(4, 1, 2) F(4, 1, 3) F(4, 1, 4) F(8, 1, 3) F(8, 1, 4) F(8, 1, 5) F(8, 1, 6) F(8, 1, 7) F(8, 1, 8) F(16, 1, 5) F(16, 1, 6) F(16, 1, 7) F(16, 1, 8) \
-    F(32, 1, 5) F(32, 1, 6) F(32, 1, 7) F(32, 1, 8) F(64, 1, 6) F(64, 1, 8) F(64, 1, 12) F(64, 1, 16) F(256, 1, 6) F(256, 1, 8) F(1024, 1, 4) F(1024, 1, 6) F(1024, 1, 8)
-
 template <class X, class Y> int norm_bwd_launch(MrfNormParams &Q, hipStream_t st)
 {
-    const int v = norm_vector(Q, sizeof(X), sizeof(Y));
 #define MRF_LAUNCH(TL, V, CH) \
     if (Q.C <= TL * V * CH) return norm_bwd_rows<X, Y, TL, V, CH>(Q, st, Q.P);
+    MRF_NORM_BWD_SHORT(MRF_LAUNCH)
     if constexpr (sizeof(X) == 2) {
-        if (v == 8) { MRF_NORM_BWD_8(MRF_LAUNCH) }
+        MRF_NORM_BWD_LONG_16(MRF_LAUNCH)
+    } else {
+        MRF_NORM_BWD_LONG(MRF_LAUNCH)
     }
-    if (v == 4) { MRF_NORM_BWD_4(MRF_LAUNCH) }
-    if (v == 1) { MRF_NORM_BWD_1(MRF_LAUNCH) }
 #undef MRF_LAUNCH
     if (Q.dx) {
         const long long rows = (Q.N + 3) / 4;

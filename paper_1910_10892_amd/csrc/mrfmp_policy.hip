@@ -1,6 +1,8 @@
 // Log-probabilities of labels under the SoftMin of the final costs, and the clipped policy loss with its gradient with
 // respect to the costs (see mrf_softmin_policy in the header for the formulas).
-#include "mrfmp_learn.h"
+#include "mrfmp_rows.h"
+
+#include <type_traits>
 
 constexpr int MRF_POLICY_BLOCKS = 4096;      // workgroups at most: partial sums of the loss
 constexpr int MRF_POLICY_COUNTS = 256;       // workgroups that count the mask
@@ -72,7 +74,7 @@ __global__ void __launch_bounds__(1024) mrf_policy_count(const MrfPolicyParams P
     }
 }
 
-// number of counted pixels, at least 1; every thread of a workgroup of 256 calls it
+// number of counted pixels, at least 1; every thread of the workgroup calls it
 __device__ inline long long mrf_policy_counted(const MrfPolicyParams &P, int blocks)
 {
     __shared__ long long total;
@@ -87,66 +89,226 @@ __device__ inline long long mrf_policy_counted(const MrfPolicyParams &P, int blo
     return total;
 }
 
-// ---- a wavefront per row: any length, any alignment.  The first pass keeps a running minimum and the sum under it
-template <class T, bool TRAIN>
-__global__ void __launch_bounds__(256) mrf_policy_any(const MrfPolicyParams P, int count_blocks)
+// what a wavefront's rows add to the two sums ends as one partial sum per workgroup
+__device__ inline void mrf_policy_partial(const MrfPolicyParams &P, double gain, double div)
 {
-    __shared__ double sums[2][4];
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    const float inv_n = TRAIN ? 1.0f / (float)mrf_policy_counted(P, count_blocks) : 0.0f;
+    __shared__ double sums[2][16];
+    gain = mrf_wave_sum_f64(gain);
+    div = mrf_wave_sum_f64(div);
+    if ((threadIdx.x & 63) == 0) {
+        sums[0][threadIdx.x >> 6] = gain;
+        sums[1][threadIdx.x >> 6] = div;
+    }
+    __syncthreads();
+    if (threadIdx.x < 2) {
+        double t = 0.0;
+        for (int w = 0; w < (int)(blockDim.x >> 6); ++w) t += sums[threadIdx.x][w];
+        P.partial[2 * (size_t)blockIdx.x + threadIdx.x] = t;
+    }
+}
+
+// A row of costs c (infinite behind its end) becomes the exponentials of their distance from the smallest; returns their sum, and the
+// smallest.  A row without an allowed label gives zeros.
+template <class Row, int E, class Min, class Sum> __device__ inline float mrf_policy_exponentials(float (&c)[E], float &low, Min min, Sum sum)
+{
+    float v = INFINITY;
+#pragma unroll
+    for (int e = 0; e < E; ++e) v = fminf(v, c[e]);
+    low = min(v);
+    const float from = low < INFINITY ? low : 0.0f;
+    v = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        c[e] = mrf_exp_small(from - c[e]);
+        v += c[e];
+    }
+    return sum(v);
+}
+
+// Log-probability of the label whose cost is `ca`, from the row's smallest cost and sum; -infinity where no label is allowed
+__device__ inline float mrf_policy_logp(float low, float ca, float s) { return s == 0.0f ? -INFINITY : (low - ca) - logf(s); }
+
+// ---- rows in registers (MrfRow): one reading of the costs, one writing of the gradient
+constexpr int mrf_policy_threads(int TL) { return TL <= 256 ? 256 : TL; }
+constexpr int mrf_policy_batch(int E) { return E <= 4 ? 4 : (E <= 12 ? 2 : 1); }
+
+template <class T, bool TRAIN, int TL, int V, int CH>
+__global__ void __launch_bounds__(mrf_policy_threads(TL)) mrf_policy_rows(const MrfPolicyParams P, int count_blocks)
+{
+    typedef MrfRow<TL, V, CH> Row;
+    constexpr int NT = mrf_policy_threads(TL), G = NT / TL, U = TL <= 64 ? mrf_policy_batch(Row::E) : 1;
+    __shared__ float scratch[2][NT / 64];
+    const int l = threadIdx.x % TL, L = P.L;
+    const unsigned group = threadIdx.x / TL, mine = group * (unsigned)L;
+    const float inv_n = TRAIN ? P.scale / (float)mrf_policy_counted(P, count_blocks) : 0.0f;
     double total_gain = 0.0, total_div = 0.0;
-    for (long long i = (long long)blockIdx.x * 4 + wv; i < P.N; i += (long long)gridDim.x * 4) {
-        const T *c = (const T *)P.cost + (size_t)i * P.L;
-        T *dc = TRAIN ? (T *)P.dcost + (size_t)i * P.L : nullptr;
-        if (TRAIN && P.mask && P.mask[i] == 0) {
-            if (P.dcost)
-                for (int l = lane; l < P.L; l += 64) dc[l] = mrf_from_f32<T>(0.0f);
-            if (lane == 0 && P.logp) P.logp[i] = 0.0f;
-            continue;
+    const long long step = (long long)gridDim.x * G;
+
+    const auto rows = [&](auto fast, auto batch, const long long base) {
+        constexpr bool FAST = decltype(fast)::value;
+        constexpr int n = decltype(batch)::value;
+        typename Row::template Raw<T> in[n];
+        int label[n];
+        float own[n];
+        bool counts[n];
+#pragma unroll
+        for (int u = 0; u < n; ++u) {
+            const long long i = base + u * step + group;
+            const bool there = FAST || i < P.N;
+            label[u] = there ? mrf_policy_label(P, i) : 0;
+            counts[u] = there && !(TRAIN && P.mask && P.mask[i] == 0);
         }
-        float mn = INFINITY, s = 0.0f;
-        for (int l = lane; l < P.L; l += 64) {
-            const float v = mrf_to_f32(c[l]);
-            if (v < mn) {
-                s = s * mrf_exp_neg(v - mn) + 1.0f;
-                mn = v;
-            } else if (v < INFINITY || v != v) {
-                s += mrf_exp_neg(mn - v);
+#pragma unroll
+        for (int u = 0; u < n; ++u) {
+            const long long first = base + u * step;
+            const bool there = FAST || first + group < P.N;
+            const T *at = (const T *)P.cost + (size_t)first * L;
+            Row::template load<FAST>(at, mine, there, L, l, in[u]);
+            own[u] = there ? mrf_to_f32(at[mine + (unsigned)label[u]]) : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < n; ++u) {
+            const long long first = base + u * step, i = first + group;
+            const bool there = FAST || i < P.N;
+            float c[Row::E], low;
+            Row::convert(in[u], L, l, c, INFINITY);
+            if (TRAIN && P.mask) {
+                // (costs of pixels that do not count may be anything)
+#pragma unroll
+                for (int e = 0; e < Row::E; ++e) c[e] = counts[u] ? c[e] : 0.0f;
             }
-        }
-        const float low = mrf_lanes_min<64>(mn);
-        s = mrf_lanes_sum<64>(mn < INFINITY || s != s ? s * mrf_exp_neg(low - mn) : 0.0f);
-        const int a = mrf_policy_label(P, i);
-        const float ca = mrf_to_f32(c[a]);
-        // (no label allowed: nothing is added, and the gradient is 0)
-        const bool none = low == INFINITY && s == 0.0f;
-        const float lp = none ? -INFINITY : (low - ca) - logf(s);
-        if (lane == 0 && P.logp) P.logp[i] = lp;
-        if constexpr (TRAIN) {
-            float gain = 0.0f, div = 0.0f, slope = 0.0f;
-            if (!none) mrf_policy_terms(P, i, lp, gain, div, slope);
-            total_gain += (double)gain;
-            total_div += (double)div;
-            if (P.dcost) {
-                const float g = slope * inv_n * P.scale, f = none ? 0.0f : g / s;
-                for (int l = lane; l < P.L; l += 64) {
-                    const float e = none ? 0.0f : mrf_exp_small(low - mrf_to_f32(c[l]));
-                    dc[l] = mrf_from_f32<T>(f * e - (l == a ? g : 0.0f));
+            const float s = mrf_policy_exponentials<Row>(c, low, [&](float v) { return Row::min(v, scratch[0]); },
+                                                         [&](float v) { return Row::sum(v, scratch[1]); });
+            const float lp = mrf_policy_logp(low, own[u], s);
+            if (P.logp && there && l == 0) P.logp[i] = counts[u] ? lp : 0.0f;
+            if constexpr (TRAIN) {
+                float gain = 0.0f, div = 0.0f, slope = 0.0f;
+                const bool adds = counts[u] && s != 0.0f;
+                if (adds) mrf_policy_terms(P, i, lp, gain, div, slope);
+                if (l == 0) {
+                    total_gain += (double)gain;
+                    total_div += (double)div;
+                }
+                if (P.dcost && there) {
+                    const float g = slope * inv_n, f = adds ? g / s : 0.0f;
+#pragma unroll
+                    for (int e = 0; e < Row::E; ++e) c[e] = f * c[e] - (Row::column(l, e / V) + e % V == label[u] ? g : 0.0f);
+                    Row::store((T *)P.dcost + (size_t)first * L + mine, L, l, c);
                 }
             }
         }
+    };
+    for (long long base = (long long)blockIdx.x * G; base < P.N;) {
+        if (U > 1 && mrf_rows_fast(base + (U - 1) * step, G, V, P.N)) {
+            rows(std::true_type{}, std::integral_constant<int, U>{}, base);
+            base += U * step;
+        } else {
+            if (mrf_rows_fast(base, G, V, P.N)) rows(std::true_type{}, std::integral_constant<int, 1>{}, base);
+            else rows(std::false_type{}, std::integral_constant<int, 1>{}, base);
+            base += step;
+        }
     }
-    if constexpr (TRAIN) {
-        if (lane == 0) {
-            sums[0][wv] = total_gain;
-            sums[1][wv] = total_div;
+    if constexpr (TRAIN) mrf_policy_partial(P, total_gain, total_div);
+}
+
+// the same for short rows through LDS (MrfTile)
+template <class T, bool TRAIN, int TL, int E>
+__global__ void __launch_bounds__(256) mrf_policy_tile(const MrfPolicyParams P, int count_blocks)
+{
+    typedef MrfTile<TL, E> Tile;
+    __shared__ __align__(16) char lds[4][Tile::BYTES];
+    const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, l = lane % TL, g = lane / TL, L = P.L;
+    const float inv_n = TRAIN ? P.scale / (float)mrf_policy_counted(P, count_blocks) : 0.0f;
+    double total_gain = 0.0, total_div = 0.0;
+    T *mine = (T *)lds[wv];
+    const long long step = (long long)gridDim.x * 4 * Tile::ROWS;
+    for (long long base = ((long long)blockIdx.x * 4 + wv) * Tile::ROWS; base < P.N; base += step) {
+        const int rows = P.N - base < Tile::ROWS ? (int)(P.N - base) : Tile::ROWS;
+        const long long i = base + g;
+        const bool there = g < rows;
+        const int label = there ? mrf_policy_label(P, i) : 0;
+        const bool counts = there && !(TRAIN && P.mask && P.mask[i] == 0);
+        Tile::fetch((const T *)P.cost + (size_t)base * L, rows, L, mine);
+        mrf_wave_lds_fence();
+        float c[E], low;
+        Tile::take(mine, g, L, l, c, INFINITY);
+        const float own = mrf_to_f32(mine[g * L + label]);
+        if (TRAIN && P.mask) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) c[e] = counts ? c[e] : 0.0f;
+        }
+        const float s = mrf_policy_exponentials<Tile>(c, low, [](float v) { return Tile::min(v); }, [](float v) { return Tile::sum(v); });
+        const float lp = mrf_policy_logp(low, own, s);
+        if (P.logp && there && l == 0) P.logp[i] = counts ? lp : 0.0f;
+        if constexpr (TRAIN) {
+            float gain = 0.0f, div = 0.0f, slope = 0.0f;
+            const bool adds = counts && s != 0.0f;
+            if (adds) mrf_policy_terms(P, i, lp, gain, div, slope);
+            if (l == 0) {
+                total_gain += (double)gain;
+                total_div += (double)div;
+            }
+            if (P.dcost) {
+                const float gs = slope * inv_n, f = adds ? gs / s : 0.0f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) c[e] = f * c[e] - (Tile::column(l, e) == label ? gs : 0.0f);
+                mrf_wave_lds_fence();
+                Tile::put(mine, g, L, l, c);
+                mrf_wave_lds_fence();
+                Tile::flush((T *)P.dcost + (size_t)base * L, rows, L, mine);
+            }
+        }
+        mrf_wave_lds_fence();
+    }
+    if constexpr (TRAIN) mrf_policy_partial(P, total_gain, total_div);
+}
+
+// ---- a workgroup per row of any length.  The first pass keeps a running minimum and the sum under it; the second reads the row again
+template <class T, bool TRAIN>
+__global__ void __launch_bounds__(1024) mrf_policy_any(const MrfPolicyParams P, int count_blocks)
+{
+    __shared__ float scratch[2][16];
+    typedef MrfRow<1024, 1, 1> Row;
+    const int t = threadIdx.x, L = P.L;
+    const float inv_n = TRAIN ? P.scale / (float)mrf_policy_counted(P, count_blocks) : 0.0f;
+    double total_gain = 0.0, total_div = 0.0;
+    for (long long i = blockIdx.x; i < P.N; i += gridDim.x) {
+        const T *c = (const T *)P.cost + (size_t)i * L;
+        T *dc = TRAIN && P.dcost ? (T *)P.dcost + (size_t)i * L : nullptr;
+        if (TRAIN && P.mask && P.mask[i] == 0) {
+            if (dc)
+                for (int k = t; k < L; k += 1024) dc[k] = mrf_from_f32<T>(0.0f);
+            if (t == 0 && P.logp) P.logp[i] = 0.0f;
+            continue;
+        }
+        float mn = INFINITY, s = 0.0f;
+#pragma unroll 8
+        for (int k = t; k < L; k += 1024) {
+            const float v = mrf_to_f32(c[k]), to = fminf(mn, v), from = to < INFINITY ? to : 0.0f;
+            s = s * mrf_exp_neg(mn < INFINITY ? from - mn : 0.0f) + mrf_exp_neg(from - v);
+            mn = to;
+        }
+        const float low = Row::min(mn, scratch[0]), from = low < INFINITY ? low : 0.0f;
+        s = Row::sum(s * mrf_exp_neg(mn < INFINITY ? from - mn : 0.0f), scratch[1]);
+        const int a = mrf_policy_label(P, i);
+        const float lp = mrf_policy_logp(low, mrf_to_f32(c[a]), s);
+        if (t == 0 && P.logp) P.logp[i] = lp;
+        if constexpr (TRAIN) {
+            float gain = 0.0f, div = 0.0f, slope = 0.0f;
+            if (s != 0.0f) mrf_policy_terms(P, i, lp, gain, div, slope);
+            if (t == 0) {
+                total_gain += (double)gain;
+                total_div += (double)div;
+            }
+            if (dc) {
+                const float g = slope * inv_n, f = s != 0.0f ? g / s : 0.0f;
+#pragma unroll 8
+                for (int k = t; k < L; k += 1024) dc[k] = mrf_from_f32<T>(f * mrf_exp_small(from - mrf_to_f32(c[k])) - (k == a ? g : 0.0f));
+            }
         }
         __syncthreads();
-        if (threadIdx.x < 2) {
-            const double *w = sums[threadIdx.x];
-            P.partial[2 * (size_t)blockIdx.x + threadIdx.x] = (w[0] + w[1]) + (w[2] + w[3]);
-        }
     }
+    if constexpr (TRAIN) mrf_policy_partial(P, total_gain, total_div);
 }
 
 // the loss from the partial sums: one workgroup, the first 256 threads add every 256th of the first sum, the others of the second
@@ -181,16 +343,60 @@ int policy_check(int64_t N, int32_t L, int type, int label_bytes)
     return known_type(type) ? MRF_OK : MRF_ERR_BAD_ARGUMENT;
 }
 
+template <class T, bool TRAIN, int TL, int V, int CH> int policy_rows(const MrfPolicyParams &P, int counts, int &blocks, hipStream_t st)
+{
+    constexpr int NT = mrf_policy_threads(TL), G = NT / TL;
+    const long long need = (P.N + G - 1) / G;
+    blocks = (int)(need < MRF_POLICY_BLOCKS ? need : MRF_POLICY_BLOCKS);
+    hipLaunchKernelGGL((mrf_policy_rows<T, TRAIN, TL, V, CH>), dim3((unsigned)blocks), dim3(NT), 0, st, P, counts);
+    return launch_status("mrf_policy_rows");
+}
+
+template <class T, bool TRAIN, int TL, int E> int policy_tile(const MrfPolicyParams &P, int counts, int &blocks, hipStream_t st)
+{
+    constexpr int G = 4 * MrfTile<TL, E>::ROWS;
+    const long long need = (P.N + G - 1) / G;
+    blocks = (int)(need < 2048 ? need : 2048);
+    hipLaunchKernelGGL((mrf_policy_tile<T, TRAIN, TL, E>), dim3((unsigned)blocks), dim3(256), 0, st, P, counts);
+    return launch_status("mrf_policy_tile");
+}
+
+// F(TL, V, CH) for each layout, shortest rows first
+#define MRF_POLICY_SHORT(F) F(1, 4, 1) F(2, 4, 1) F(4, 4, 1) F(8, 4, 1) F(8, 4, 2) F(8, 4, 3) F(16, 4, 2) F(16, 4, 3) F(16, 4, 4)
+#define MRF_POLICY_LONG(F) F(64, 4, 2) F(64, 4, 4) F(64, 4, 8) F(256, 4, 4) F(256, 4, 8) F(1024, 4, 4) F(1024, 4, 8)
+#define MRF_POLICY_LONG_16(F) F(64, 8, 1) F(64, 8, 2) F(64, 8, 4) F(256, 8, 2) F(256, 8, 4) F(1024, 8, 2) F(1024, 8, 4)
+
+template <class T, bool TRAIN> int policy_any_layout(const MrfPolicyParams &P, int counts, int &blocks, hipStream_t st)
+{
+    if (P.L % 4 != 0 && P.L <= MRF_TILES_LONGEST) {
+#define MRF_LAUNCH(TL, E) \
+        if (P.L <= TL * E) return policy_tile<T, TRAIN, TL, E>(P, counts, blocks, st);
+        MRF_TILES(MRF_LAUNCH)
+#undef MRF_LAUNCH
+    }
+#define MRF_LAUNCH(TL, V, CH) \
+    if (P.L <= TL * V * CH) return policy_rows<T, TRAIN, TL, V, CH>(P, counts, blocks, st);
+    MRF_POLICY_SHORT(MRF_LAUNCH)
+    if constexpr (sizeof(T) == 2) {
+        MRF_POLICY_LONG_16(MRF_LAUNCH)
+    } else {
+        MRF_POLICY_LONG(MRF_LAUNCH)
+    }
+#undef MRF_LAUNCH
+    blocks = (int)(P.N < MRF_POLICY_BLOCKS ? P.N : MRF_POLICY_BLOCKS);
+    hipLaunchKernelGGL((mrf_policy_any<T, TRAIN>), dim3((unsigned)blocks), dim3(1024), 0, st, P, counts);
+    return launch_status("mrf_policy_any");
+}
+
 template <class T> int logp_launch(const MrfPolicyParams &P, hipStream_t st)
 {
-    const long long rows = (P.N + 3) / 4;
-    hipLaunchKernelGGL((mrf_policy_any<T, false>), dim3((unsigned)(rows < MRF_POLICY_BLOCKS ? rows : MRF_POLICY_BLOCKS)), dim3(256), 0, st, P, 0);
-    return launch_status("mrf_softmin_logp");
+    int blocks = 0;
+    return policy_any_layout<T, false>(P, 0, blocks, st);
 }
 
 template <class T> int policy_launch(const MrfPolicyParams &P, hipStream_t st)
 {
-    int counts = 0;
+    int counts = 0, blocks = 0;
     if (P.mask) {
         const long long need = (P.N + 1023) / 1024;
         counts = (int)(need < MRF_POLICY_COUNTS ? need : MRF_POLICY_COUNTS);
@@ -198,10 +404,7 @@ template <class T> int policy_launch(const MrfPolicyParams &P, hipStream_t st)
         const int rc = launch_status("mrf_policy_count");
         if (rc != MRF_OK) return rc;
     }
-    const long long rows = (P.N + 3) / 4;
-    const int blocks = (int)(rows < MRF_POLICY_BLOCKS ? rows : MRF_POLICY_BLOCKS);
-    hipLaunchKernelGGL((mrf_policy_any<T, true>), dim3((unsigned)blocks), dim3(256), 0, st, P, counts);
-    const int rc = launch_status("mrf_policy");
+    const int rc = policy_any_layout<T, true>(P, counts, blocks, st);
     if (rc != MRF_OK) return rc;
     hipLaunchKernelGGL(mrf_policy_sum, dim3(1), dim3(512), 0, st, P, blocks, counts);
     return launch_status("mrf_policy_sum");
