@@ -2,6 +2,8 @@
 // mrf_bucket_pairwise_forward in the header for the formulas).
 #include "mrfmp_rows.h"
 
+#include <type_traits>
+
 struct MrfBucketParams {
     long long G;
     int Q, K, NB;
@@ -11,10 +13,11 @@ struct MrfBucketParams {
     void *out;                   // forward [G][Q][K]
     const void *dout;            // backward
     float *dtable;
-    float *diagonals;            // [G][T][Q + K - 1] sums over the rows of a part (long matrices)
+    float *diagonals;            // [G][T][strips][..] sums along diagonals over a strip's columns and a part's rows (long matrices)
     int quads;                   // forward, many small matrices: fours of groups whose tables are in LDS at once
     int KL, TR;                  // forward, long matrices: lanes of a row, rows of a lane
-    int T, TQ;                   // backward, long matrices: parts of TQ rows
+    int groups, tile;            // backward, many small matrices: matrices of a wavefront, bytes of LDS for them
+    int T, TQ, strips;           // backward, long matrices: parts of the rows, rows of a wavefront, strips of the columns
 };
 
 __device__ inline int mrf_bucket_clamped(int b, int NB) { return b < 0 ? 0 : (b < NB ? b : NB - 1); }
@@ -139,135 +142,239 @@ __global__ void __launch_bounds__(256) mrf_bucket_fwd_long(const MrfBucketParams
 // ---- backward.  A diagonal has one bucket: sums go down the diagonals first, where the lanes of a wavefront, one diagonal each, read neighbours in
 // every row, and then over the diagonals of a bucket.
 
-// Many small matrices (Q, K <= 64): lanes j < K of a matrix go down its rows from column j on and begin again at column 0, so that none idles: a
-// wavefront takes as many matrices as have room.  Where a lane begins again, a diagonal's sum is complete.
-constexpr int MRF_BUCKET_SIDE = 64, MRF_BUCKET_DIAG = 1024, MRF_BUCKET_MANY = 1024;      // Q, K; diagonals of a wavefront; buckets
+// Many small matrices (Q, K <= 64): a wavefront takes as many as have room in its lanes, neighbours in memory, into LDS as whole chunks.  Lanes
+// j < K of a matrix go down its rows from column j on and begin again at column 0, so that none idles; where a lane begins again, a
+// diagonal's sum is complete.
+constexpr int MRF_BUCKET_SIDE = 64, MRF_BUCKET_DIAG = 512, MRF_BUCKET_MANY = 512, MRF_BUCKET_WAVES = 2;      // Q, K; diagonals of a wavefront; buckets; wavefronts
 
-template <class T>
-__global__ void __launch_bounds__(256) mrf_bucket_bwd_small(const MrfBucketParams P)
+template <class T, bool WIDE>
+__global__ void __launch_bounds__(64 * MRF_BUCKET_WAVES) mrf_bucket_bwd_small(const MrfBucketParams P)
 {
-    __shared__ float diag[4][MRF_BUCKET_DIAG];
-    __shared__ int bucket[2 * MRF_BUCKET_SIDE], order[2 * MRF_BUCKET_SIDE], begin[MRF_BUCKET_MANY + 1];
+    typedef typename MrfChunk<sizeof(T)>::type chunk;
+    typedef typename MrfChunk<16>::type quad;
+    constexpr int NT = 64 * MRF_BUCKET_WAVES, PER = 16 / (int)sizeof(T);
+    extern __shared__ __align__(16) char staged[];      // [MRF_BUCKET_WAVES][P.tile] bytes
+    __shared__ float diag[MRF_BUCKET_WAVES][MRF_BUCKET_DIAG];
+    __shared__ int bucket[2 * MRF_BUCKET_SIDE], place[2 * MRF_BUCKET_SIDE], begin[MRF_BUCKET_MANY + 1];
     const int Q = P.Q, K = P.K, NB = P.NB, S = Q * K, D = Q + K - 1;
-    // the diagonals in the order of their buckets, and where each bucket begins
-    for (int d = threadIdx.x; d < D; d += 256) bucket[d] = mrf_bucket_clamped(P.bucket_of[d], NB);
+    // where each bucket begins in the order of buckets, and the place of each diagonal there
+    for (int d = threadIdx.x; d < D; d += NT) bucket[d] = mrf_bucket_clamped(P.bucket_of[d], NB);
     __syncthreads();
-    for (int b = threadIdx.x; b <= NB; b += 256) {
+    for (int b = threadIdx.x; b <= NB; b += NT) {
         int n = 0;
         for (int d = 0; d < D; ++d) n += bucket[d] < b;
         begin[b] = n;
     }
-    for (int d = threadIdx.x; d < D; d += 256) {
+    for (int d = threadIdx.x; d < D; d += NT) {
         int n = 0;
         for (int e = 0; e < D; ++e) n += bucket[e] < bucket[d] || (bucket[e] == bucket[d] && e < d);
-        order[n] = d;
+        place[d] = n;
     }
     __syncthreads();
-    const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-    const int fit = 64 / K, room = MRF_BUCKET_DIAG / D, groups = fit < room ? fit : room;
+    const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, groups = P.groups;
     const int mine = lane / K, j = lane - mine * K;
     float *sums = diag[wv];
-    for (long long g0 = ((long long)blockIdx.x * 4 + wv) * groups; g0 < P.G; g0 += (long long)gridDim.x * 4 * groups) {
-        const int here = P.G - g0 < groups ? (int)(P.G - g0) : groups;
+    T *tile = (T *)(staged + wv * P.tile);
+    for (long long g0 = ((long long)blockIdx.x * MRF_BUCKET_WAVES + wv) * groups; g0 < P.G; g0 += (long long)gridDim.x * MRF_BUCKET_WAVES * groups) {
+        const int here = P.G - g0 < groups ? (int)(P.G - g0) : groups, n = here * S, chunks = n / PER;
+        const T *from = (const T *)P.dout + (size_t)g0 * S;
+        for (int k = lane; k < chunks; k += 64 * 8) {
+            quad r[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (k + 64 * i < chunks) r[i] = *(const chunk *)(from + (unsigned)(k + 64 * i) * PER);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (k + 64 * i < chunks) ((quad *)tile)[k + 64 * i] = r[i];
+        }
+        if (chunks * PER + lane < n) tile[chunks * PER + lane] = from[chunks * PER + lane];
+        mrf_wave_lds_fence();
         if (mine < here) {
-            const T *x = (const T *)P.dout + (size_t)(g0 + mine) * S;
-            int k = j, write = mine * D + j + (Q - 1);      // place of the diagonal that the lane is on
-            float s = 0.0f;
+            const T *x = tile + mine * S;
+            float *to = sums + mine * D;
+            int at = j, turn = K - 1 - j, d = j + (Q - 1);      // element; row in which the lane begins again; its diagonal
+            float s = 0.0f, done = 0.0f;
             for (int q = 0; q < Q; q += 8) {
-                T v[8];
-                int c = k;
+                float v[8];
+                int t = turn;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    if (q + i < Q) v[i] = x[(q + i) * K + c];
-                    c = c + 1 == K ? 0 : c + 1;
+                    v[i] = mrf_to_f32(x[q + i < Q ? at : j]);
+                    at += q + i == t ? 1 : K + 1;
+                    if (!WIDE) t += q + i == t ? K : 0;
                 }
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     if (q + i < Q) {
-                        s += mrf_to_f32(v[i]);
-                        if (++k == K) {
-                            sums[write] = s;
+                        s += v[i];
+                        if constexpr (WIDE) {
+                            done = q + i == turn ? s : done;
+                            s = q + i == turn ? 0.0f : s;
+                        } else if (q + i == turn) {
+                            to[place[d]] = s;
                             s = 0.0f;
-                            k = 0;
-                            write -= K;
+                            d -= K;
+                            turn += K;
                         }
                     }
             }
-            if (k > 0) sums[write] = s;
+            if constexpr (WIDE) {
+                // (Q <= K: a lane begins again once at most)
+                if (turn < Q) {
+                    to[place[d]] = done;
+                    d -= K;
+                }
+                if (turn != Q - 1) to[place[d]] = s;
+            } else if (turn - K != Q - 1) {
+                to[place[d]] = s;
+            }
         }
         mrf_wave_lds_fence();
         for (int i = lane; i < here * NB; i += 64) {
-            const int g = i / NB, b = i - g * NB;
+            const int g = i / NB, b = i - g * NB, last = begin[b + 1];
             float s = 0.0f;
-            for (int d = begin[b]; d < begin[b + 1]; ++d) s += sums[g * D + order[d]];
+#pragma unroll 4
+            for (int d = begin[b]; d < last; ++d) s += sums[g * D + d];
             P.dtable[(g0 + g) * P.sg + b * P.sb] = s;
         }
         mrf_wave_lds_fence();
     }
 }
 
-// Long matrices: a wavefront takes 64 neighbouring diagonals through the rows of a part; a lane's rows are those in which its diagonal has a
-// column.
+// Long matrices: a wavefront goes down a strip of 256 columns, four of them a lane, whole chunks of the matrix, and the sums move instead: after
+// four rows, the diagonals that a lane's columns are on are those of the lane before it.  Entry j of row r (of four) is on the lane's
+// diagonal j - r: sums 0 .. 3 go to the next lane, and those below 0, the new lane's 1 .. 3, meet them there.  What leaves the last
+// lane is complete for the strip.  Eight wavefronts with consecutive rows add up theirs in LDS.
+constexpr int MRF_BUCKET_STRIP = 256, MRF_BUCKET_STACK = 8, MRF_BUCKET_TQ = 64;      // columns; wavefronts of a workgroup; rows of one at most
+
 template <class T>
-__global__ void __launch_bounds__(256) mrf_bucket_bwd_long(const MrfBucketParams P)
+__global__ void __launch_bounds__(64 * MRF_BUCKET_STACK) mrf_bucket_bwd_long(const MrfBucketParams P)
 {
+    typedef typename MrfVec<T, 4>::type vec;
+    constexpr int R = 16;      // rows on their way at once
+    __shared__ float slots[MRF_BUCKET_STACK][MRF_BUCKET_STRIP + MRF_BUCKET_TQ];      // by diagonal, from that of the first column and the last row on
     const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
-    const int Q = P.Q, K = P.K, D = Q + K - 1;
-    const unsigned tiles = (unsigned)((D + 255) / 256);
-    const int part = (int)(blockIdx.x / tiles), d0 = (int)(blockIdx.x % tiles) * 256 + wv * 64;
-    if (d0 >= D) return;
-    const int d = d0 + lane, off = d - (Q - 1);      // column = row + off
-    const int q0 = part * P.TQ, q1 = Q - q0 < P.TQ ? Q : q0 + P.TQ;
-    // the wavefront's rows; those in which every lane has a column
-    const int offlast = (d0 + 63 < D ? d0 + 63 : D - 1) - (Q - 1), off0 = d0 - (Q - 1);
-    const int from = q0 > -offlast ? q0 : -offlast, to = q1 < K - off0 ? q1 : K - off0;
-    const bool whole = d0 + 63 < D;
-    const int in0 = whole ? (from > -off0 ? from : -off0) : to, in1 = whole ? (to < K - offlast ? to : K - offlast) : to;
+    const int Q = P.Q, K = P.K, TQ = P.TQ;
+    const int strip = (int)(blockIdx.x % (unsigned)P.strips), part = (int)(blockIdx.x / (unsigned)P.strips);
+    const int c0 = strip * MRF_BUCKET_STRIP, c = c0 + 4 * lane, q0 = (part * MRF_BUCKET_STACK + wv) * TQ;
+    const int rows = Q - q0 < TQ ? Q - q0 : TQ;
+    // (the row's last chunk, where it is not full, is read as the row's last four columns; lanes behind the row read its first)
+    const int in = c + 4 <= K ? c : (c < K && K >= 4 ? K - 4 : 0), gone = c < K ? c - in : 4;
+    const bool ragged = c0 + MRF_BUCKET_STRIP > K;
     for (long long g = blockIdx.y; g < P.G; g += gridDim.y) {
-        const T *x = (const T *)P.dout + (size_t)g * Q * K;
-        float s = 0.0f;
-        const auto some = [&](int a, int b) {
-            for (int q = a; q < b; ++q) {
-                const int k = q + off;
-                if (d < D && k >= 0 && k < K) s += mrf_to_f32(x[(size_t)q * K + k]);
-            }
-        };
-        if (in0 < in1) {
-            some(from, in0);
-            int q = in0;
-            for (; q + 16 <= in1; q += 16) {
-                T v[16];
+        const T *x = (const T *)P.dout + (size_t)g * Q * K;      // (a wavefront may have no row at all: its first is not read then)
+        float s[7] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        float *mine = slots[wv];
+        for (int q = 0; q < TQ; q += R) {
+            vec w[R];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = x[(size_t)(q + i) * K + (q + i + off)];
-                float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            for (int i = 0; i < R; i += 4) {
+                if (q + i + 4 <= rows && K >= 4) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) a[i & 3] += mrf_to_f32(v[i]);
-                s += (a[0] + a[1]) + (a[2] + a[3]);
+                    for (int r = i; r < i + 4; ++r) w[r] = *(const vec *)(x + (long long)(q0 + q + r) * K + (unsigned)in);
+                } else {
+                    // the last rows, entry by entry (what is not there is read as the matrix's first entry, and not used)
+#pragma unroll
+                    for (int r = i; r < i + 4; ++r)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const bool there = q + r < rows && (K >= 4 || j < K);
+                            w[r][j] = x[there ? (long long)(q0 + q + r) * K + (in + j) : 0];
+                        }
+                }
             }
-            some(q, to);
-        } else {
-            some(from, to);
+            float v[R][4];
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[i][j] = q + i < rows ? mrf_to_f32((T)w[i][j]) : 0.0f;
+            if (ragged) {
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    v[i][0] = gone == 0 ? v[i][0] : (gone == 1 ? v[i][1] : (gone == 2 ? v[i][2] : (gone == 3 ? v[i][3] : 0.0f)));
+                    v[i][1] = gone == 0 ? v[i][1] : (gone == 1 ? v[i][2] : (gone == 2 ? v[i][3] : 0.0f));
+                    v[i][2] = gone == 0 ? v[i][2] : (gone == 1 ? v[i][3] : 0.0f);
+                    v[i][3] = gone == 0 ? v[i][3] : 0.0f;
+                }
+                if (K < 4) {
+#pragma unroll
+                    for (int i = 0; i < R; ++i)
+#pragma unroll
+                        for (int j = 1; j < 4; ++j) v[i][j] = j < K ? v[i][j] : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < R; i += 4) {
+                if (q + i >= TQ) break;
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[j - r + 3] += v[i + r][j];
+                if (lane == 63) {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) mine[MRF_BUCKET_STRIP + (TQ - q - i - 4) + t] = s[t + 3];
+                }
+#pragma unroll
+                for (int t = 3; t >= 0; --t) {
+                    const float up = __shfl_up(s[t + 3], 1);
+                    s[t + 3] = (lane > 0 ? up : 0.0f) + (t > 0 ? s[t - 1] : 0.0f);
+                }
+                s[0] = s[1] = s[2] = 0.0f;
+            }
         }
-        if (d < D) P.diagonals[((size_t)g * P.T + part) * D + d] = s;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) mine[4 * lane + t] = s[t + 3];
+        __syncthreads();
+        const int n = MRF_BUCKET_STRIP + MRF_BUCKET_STACK * TQ;
+        float *out = P.diagonals + (((size_t)g * P.T + part) * P.strips + strip) * n;
+        for (int i = threadIdx.x; i < n; i += 64 * MRF_BUCKET_STACK) {
+            float t = 0.0f;
+#pragma unroll
+            for (int w = 0; w < MRF_BUCKET_STACK; ++w) {
+                const int k = i - (MRF_BUCKET_STACK - 1 - w) * TQ;
+                if (k >= 0 && k < MRF_BUCKET_STRIP + TQ) t += slots[w][k];
+            }
+            out[i] = t;
+        }
+        __syncthreads();
     }
 }
 
-// a workgroup per bucket and group: the diagonals of that bucket, over the parts in order
-__global__ void __launch_bounds__(256) mrf_bucket_bwd_sum(const MrfBucketParams P)
+// A workgroup per bucket and group: the diagonals of that bucket, over the parts and the strips that they cross.
+constexpr int MRF_BUCKET_SUM = 1024;
+__global__ void __launch_bounds__(MRF_BUCKET_SUM) mrf_bucket_bwd_sum(const MrfBucketParams P)
 {
-    __shared__ float waves[4];
-    const int D = P.Q + P.K - 1, b = blockIdx.x;
+    __shared__ float waves[MRF_BUCKET_SUM / 64];
+    const int Q = P.Q, D = Q + P.K - 1, b = blockIdx.x, rows = MRF_BUCKET_STACK * P.TQ, n = MRF_BUCKET_STRIP + rows;
     for (long long g = blockIdx.y; g < P.G; g += gridDim.y) {
-        const float *x = P.diagonals + (size_t)g * P.T * D;
+        const float *x = P.diagonals + (size_t)g * P.T * P.strips * n;
         float s = 0.0f;
         if (P.T > 0)
-            for (int d = threadIdx.x; d < D; d += 256)
-                if (mrf_bucket_clamped(P.bucket_of[d], P.NB) == b)
-                    for (int t = 0; t < P.T; ++t) s += x[(size_t)t * D + d];
+            for (int d = threadIdx.x; d < D; d += MRF_BUCKET_SUM)
+                if (mrf_bucket_clamped(P.bucket_of[d], P.NB) == b) {
+                    float a = 0.0f;
+#pragma unroll 4
+                    for (int p = 0; p < P.T; ++p) {
+                        // slot i of strip k is the diagonal 256 k + i - (p + 1) rows + Q - 1: in three strips at most
+                        const int at = d + (p + 1) * rows - (Q - 1), k0 = at >> 8;
+                        static_assert(MRF_BUCKET_STRIP == 256 && MRF_BUCKET_STACK * MRF_BUCKET_TQ <= 2 * MRF_BUCKET_STRIP, "strips of a diagonal");
+#pragma unroll
+                        for (int u = 0; u < 3; ++u) {
+                            const int k = k0 - u, i = at - k * MRF_BUCKET_STRIP;
+                            const bool there = k >= 0 && k < P.strips && i < n;
+                            const float y = x[there ? ((size_t)p * P.strips + k) * n + i : 0];
+                            a += there ? y : 0.0f;
+                        }
+                    }
+                    s += a;
+                }
         s = mrf_lanes_sum<64>(s);
         if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = s;
         __syncthreads();
-        if (threadIdx.x == 0) P.dtable[g * P.sg + b * P.sb] = (waves[0] + waves[1]) + (waves[2] + waves[3]);
+        if (threadIdx.x < 64) {
+            s = mrf_lanes_sum<16>(threadIdx.x < MRF_BUCKET_SUM / 64 ? waves[threadIdx.x] : 0.0f);
+            if (threadIdx.x == 0) P.dtable[g * P.sg + b * P.sb] = s;
+        }
         __syncthreads();
     }
 }
@@ -303,14 +410,12 @@ void bucket_strides(MrfBucketParams &P, int heads_last)
 
 bool bucket_small_backward(const MrfBucketParams &P) { return P.Q <= MRF_BUCKET_SIDE && P.K <= MRF_BUCKET_SIDE && P.NB <= MRF_BUCKET_MANY; }
 
-// parts of the rows: about 8,192 wavefronts in all, of at least 32 rows
+// rows of a wavefront: 64, or so few (a multiple of four) that there are 4,096 wavefronts
 void bucket_parts(MrfBucketParams &P)
 {
-    const long long D = (long long)P.Q + P.K - 1, columns = P.G * ((D + 63) / 64), most = (P.Q + 31) / 32;
-    long long t = (8192 + columns - 1) / columns;
-    t = t < most ? t : most;
-    P.TQ = (int)((P.Q + t - 1) / t);
-    P.T = (P.Q + P.TQ - 1) / P.TQ;
+    P.strips = (int)(((long long)P.K + MRF_BUCKET_STRIP - 1) / MRF_BUCKET_STRIP);
+    for (P.TQ = MRF_BUCKET_TQ; P.TQ > 4 && P.G * P.strips * ((P.Q + P.TQ - 1LL) / P.TQ) < 4096; P.TQ /= 2) {}
+    P.T = (int)((P.Q + (long long)MRF_BUCKET_STACK * P.TQ - 1) / (MRF_BUCKET_STACK * P.TQ));
 }
 
 template <class T> int bucket_forward(MrfBucketParams P, hipStream_t st)
@@ -345,21 +450,26 @@ template <class T> int bucket_forward(MrfBucketParams P, hipStream_t st)
 
 int bucket_sum(const MrfBucketParams &P, hipStream_t st)
 {
-    hipLaunchKernelGGL(mrf_bucket_bwd_sum, dim3((unsigned)P.NB, (unsigned)(P.G < 65535 ? P.G : 65535)), dim3(256), 0, st, P);
+    hipLaunchKernelGGL(mrf_bucket_bwd_sum, dim3((unsigned)P.NB, (unsigned)(P.G < 65535 ? P.G : 65535)), dim3(MRF_BUCKET_SUM), 0, st, P);
     return launch_status("mrf_bucket_bwd_sum");
 }
 
 template <class T> int bucket_backward(MrfBucketParams P, hipStream_t st)
 {
     if (bucket_small_backward(P)) {
-        const int fit = 64 / P.K, room = MRF_BUCKET_DIAG / (P.Q + P.K - 1), groups = 4 * (fit < room ? fit : room);
-        const long long need = (P.G + groups - 1) / groups;
-        hipLaunchKernelGGL(mrf_bucket_bwd_small<T>, dim3((unsigned)(need < 2048 ? need : 2048)), dim3(256), 0, st, P);
+        const int fit = 64 / P.K, room = MRF_BUCKET_DIAG / (P.Q + P.K - 1);
+        P.groups = fit < room ? fit : room;
+        P.tile = (P.groups * P.Q * P.K * (int)sizeof(T) + 15) / 16 * 16;
+        const long long need = (P.G + MRF_BUCKET_WAVES * P.groups - 1) / (MRF_BUCKET_WAVES * P.groups);
+        const dim3 grid((unsigned)(need < 8192 ? need : 8192)), block(64 * MRF_BUCKET_WAVES);
+        if (P.Q <= P.K) hipLaunchKernelGGL((mrf_bucket_bwd_small<T, true>), grid, block, MRF_BUCKET_WAVES * P.tile, st, P);
+        else hipLaunchKernelGGL((mrf_bucket_bwd_small<T, false>), grid, block, MRF_BUCKET_WAVES * P.tile, st, P);
         return launch_status("mrf_bucket_bwd_small");
     }
     bucket_parts(P);
-    const long long tiles = ((long long)P.Q + P.K - 1 + 255) / 256 * P.T;
-    hipLaunchKernelGGL(mrf_bucket_bwd_long<T>, dim3((unsigned)tiles, (unsigned)(P.G < 65535 ? P.G : 65535)), dim3(256), 0, st, P);
+    const long long blocks = (long long)P.strips * P.T;
+    if (blocks > 0x7fffffffLL) return MRF_ERR_BAD_SHAPE;
+    hipLaunchKernelGGL(mrf_bucket_bwd_long<T>, dim3((unsigned)blocks, (unsigned)(P.G < 65535 ? P.G : 65535)), dim3(64 * MRF_BUCKET_STACK), 0, st, P);
     const int rc = launch_status("mrf_bucket_bwd_long");
     return rc != MRF_OK ? rc : bucket_sum(P, st);
 }
@@ -396,7 +506,7 @@ size_t mrf_bucket_pairwise_workspace_bytes(int64_t n_groups, int32_t Q, int32_t 
     P.G = n_groups; P.Q = Q; P.K = K; P.NB = n_buckets;
     if (n_groups == 0 || Q == 0 || K == 0 || bucket_small_backward(P)) return 256;
     bucket_parts(P);
-    return sizeof(float) * (size_t)n_groups * (size_t)P.T * ((size_t)Q + K - 1);
+    return sizeof(float) * (size_t)n_groups * (size_t)P.T * (size_t)P.strips * (MRF_BUCKET_STRIP + MRF_BUCKET_STACK * (size_t)P.TQ);
 }
 
 int mrf_bucket_pairwise_forward(int64_t n_groups, int32_t Q, int32_t K, int32_t n_buckets, const float *table, int heads_last,
