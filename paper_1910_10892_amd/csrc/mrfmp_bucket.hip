@@ -13,6 +13,7 @@ struct MrfBucketParams {
     void *out;                   // forward [G][Q][K]
     const void *dout;            // backward
     float *dtable;
+    float *totals;               // [G][Q + K - 1] sums along whole diagonals (long matrices)
     float *diagonals;            // [G][T][strips][..] sums along diagonals over a strip's columns and a part's rows (long matrices)
     int quads;                   // forward, many small matrices: fours of groups whose tables are in LDS at once
     int KL, TR;                  // forward, long matrices: lanes of a row, rows of a lane
@@ -247,12 +248,16 @@ __global__ void __launch_bounds__(64 * MRF_BUCKET_WAVES) mrf_bucket_bwd_small(co
 // lane is complete for the strip.  Eight wavefronts with consecutive rows add up theirs in LDS.
 constexpr int MRF_BUCKET_STRIP = 256, MRF_BUCKET_STACK = 8, MRF_BUCKET_TQ = 64;      // columns; wavefronts of a workgroup; rows of one at most
 
-template <class T>
+// ONE: a workgroup has a whole matrix (256 columns, 512 rows at most), and sums its buckets at once.
+template <class T, bool ONE>
 __global__ void __launch_bounds__(64 * MRF_BUCKET_STACK) mrf_bucket_bwd_long(const MrfBucketParams P)
 {
     typedef typename MrfVec<T, 4>::type vec;
     constexpr int R = 16;      // rows on their way at once
+    constexpr int SLOTS = MRF_BUCKET_STRIP + MRF_BUCKET_STACK * MRF_BUCKET_TQ;
     __shared__ float slots[MRF_BUCKET_STACK][MRF_BUCKET_STRIP + MRF_BUCKET_TQ];      // by diagonal, from that of the first column and the last row on
+    __shared__ float sums[ONE ? SLOTS : 1];
+    __shared__ int bucket[ONE ? SLOTS : 1];
     const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
     const int Q = P.Q, K = P.K, TQ = P.TQ;
     const int strip = (int)(blockIdx.x % (unsigned)P.strips), part = (int)(blockIdx.x / (unsigned)P.strips);
@@ -261,6 +266,14 @@ __global__ void __launch_bounds__(64 * MRF_BUCKET_STACK) mrf_bucket_bwd_long(con
     // (the row's last chunk, where it is not full, is read as the row's last four columns; lanes behind the row read its first)
     const int in = c + 4 <= K ? c : (c < K && K >= 4 ? K - 4 : 0), gone = c < K ? c - in : 4;
     const bool ragged = c0 + MRF_BUCKET_STRIP > K;
+    const int n = MRF_BUCKET_STRIP + MRF_BUCKET_STACK * TQ;
+    if constexpr (ONE) {
+        // slot i is the diagonal i - 8 TQ + Q - 1; those without an entry get no bucket
+        for (int i = threadIdx.x; i < n; i += 64 * MRF_BUCKET_STACK) {
+            const int d = i - MRF_BUCKET_STACK * TQ + Q - 1;
+            bucket[i] = d >= 0 && d < Q + K - 1 ? mrf_bucket_clamped(P.bucket_of[d], P.NB) : -1;
+        }
+    }
     for (long long g = blockIdx.y; g < P.G; g += gridDim.y) {
         const T *x = (const T *)P.dout + (size_t)g * Q * K;      // (a wavefront may have no row at all: its first is not read then)
         float s[7] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
@@ -325,8 +338,7 @@ __global__ void __launch_bounds__(64 * MRF_BUCKET_STACK) mrf_bucket_bwd_long(con
 #pragma unroll
         for (int t = 0; t < 4; ++t) mine[4 * lane + t] = s[t + 3];
         __syncthreads();
-        const int n = MRF_BUCKET_STRIP + MRF_BUCKET_STACK * TQ;
-        float *out = P.diagonals + (((size_t)g * P.T + part) * P.strips + strip) * n;
+        float *out = ONE ? sums : P.diagonals + (((size_t)g * P.T + part) * P.strips + strip) * n;
         for (int i = threadIdx.x; i < n; i += 64 * MRF_BUCKET_STACK) {
             float t = 0.0f;
 #pragma unroll
@@ -337,37 +349,73 @@ __global__ void __launch_bounds__(64 * MRF_BUCKET_STACK) mrf_bucket_bwd_long(con
             out[i] = t;
         }
         __syncthreads();
+        if constexpr (ONE) {
+            if (P.NB <= 64 * MRF_BUCKET_STACK) {
+                // a wavefront per bucket
+                for (int b = wv; b < P.NB; b += MRF_BUCKET_STACK) {
+                    float t = 0.0f;
+                    for (int i = lane; i < n; i += 64) t += bucket[i] == b ? sums[i] : 0.0f;
+                    t = mrf_lanes_sum<64>(t);
+                    if (lane == 0) P.dtable[g * P.sg + b * P.sb] = t;
+                }
+            } else {
+                // a thread per bucket, most of which are empty
+                for (int b = threadIdx.x; b < P.NB; b += 64 * MRF_BUCKET_STACK) {
+                    float t = 0.0f;
+                    for (int i = 0; i < n; ++i) t += bucket[i] == b ? sums[i] : 0.0f;
+                    P.dtable[g * P.sg + b * P.sb] = t;
+                }
+            }
+            __syncthreads();
+        }
     }
 }
 
-// A workgroup per bucket and group: the diagonals of that bucket, over the parts and the strips that they cross.
+// a thread per diagonal: its sums over the parts and the strips that it crosses
+__global__ void __launch_bounds__(256) mrf_bucket_bwd_diagonals(const MrfBucketParams P)
+{
+    static_assert(MRF_BUCKET_STRIP == 256 && MRF_BUCKET_STACK * MRF_BUCKET_TQ <= 2 * MRF_BUCKET_STRIP, "strips of a diagonal");
+    const int Q = P.Q, D = Q + P.K - 1, d = (int)(blockIdx.x * 256 + threadIdx.x), rows = MRF_BUCKET_STACK * P.TQ, n = MRF_BUCKET_STRIP + rows;
+    if (d >= D) return;
+    for (long long g = blockIdx.y; g < P.G; g += gridDim.y) {
+        const float *x = P.diagonals + (size_t)g * P.T * P.strips * n;
+        float s = 0.0f;
+#pragma unroll 4
+        for (int p = 0; p < P.T; ++p) {
+            // slot i of strip k is the diagonal 256 k + i - (p + 1) rows + Q - 1: in three strips at most
+            const int at = d + (p + 1) * rows - (Q - 1), k0 = at >> 8, i0 = at & 255;
+#pragma unroll
+            for (int v = 0; v < 3; ++v) {
+                const int k = k0 - v, i = i0 + v * MRF_BUCKET_STRIP;
+                const bool there = k >= 0 && k < P.strips && i < n;
+                const float y = x[there ? ((size_t)p * P.strips + k) * n + i : 0];
+                s += there ? y : 0.0f;
+            }
+        }
+        P.totals[g * D + d] = s;
+    }
+}
+
+// A workgroup per bucket and group: the diagonals of that bucket, four of a thread's looked up at once.
 constexpr int MRF_BUCKET_SUM = 1024;
 __global__ void __launch_bounds__(MRF_BUCKET_SUM) mrf_bucket_bwd_sum(const MrfBucketParams P)
 {
     __shared__ float waves[MRF_BUCKET_SUM / 64];
-    const int Q = P.Q, D = Q + P.K - 1, b = blockIdx.x, rows = MRF_BUCKET_STACK * P.TQ, n = MRF_BUCKET_STRIP + rows;
+    const int D = P.T > 0 ? P.Q + P.K - 1 : 0, b = blockIdx.x;
     for (long long g = blockIdx.y; g < P.G; g += gridDim.y) {
-        const float *x = P.diagonals + (size_t)g * P.T * P.strips * n;
         float s = 0.0f;
-        if (P.T > 0)
-            for (int d = threadIdx.x; d < D; d += MRF_BUCKET_SUM)
-                if (mrf_bucket_clamped(P.bucket_of[d], P.NB) == b) {
-                    float a = 0.0f;
-#pragma unroll 4
-                    for (int p = 0; p < P.T; ++p) {
-                        // slot i of strip k is the diagonal 256 k + i - (p + 1) rows + Q - 1: in three strips at most
-                        const int at = d + (p + 1) * rows - (Q - 1), k0 = at >> 8;
-                        static_assert(MRF_BUCKET_STRIP == 256 && MRF_BUCKET_STACK * MRF_BUCKET_TQ <= 2 * MRF_BUCKET_STRIP, "strips of a diagonal");
+        for (int first = threadIdx.x; first < D; first += 4 * MRF_BUCKET_SUM) {
+            int bucket[4];
+            float total[4];
 #pragma unroll
-                        for (int u = 0; u < 3; ++u) {
-                            const int k = k0 - u, i = at - k * MRF_BUCKET_STRIP;
-                            const bool there = k >= 0 && k < P.strips && i < n;
-                            const float y = x[there ? ((size_t)p * P.strips + k) * n + i : 0];
-                            a += there ? y : 0.0f;
-                        }
-                    }
-                    s += a;
-                }
+            for (int u = 0; u < 4; ++u) {
+                const int d = first + u * MRF_BUCKET_SUM;
+                bucket[u] = P.bucket_of[d < D ? d : D - 1];
+                total[u] = P.totals[g * D + (d < D ? d : D - 1)];
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) s += first + u * MRF_BUCKET_SUM < D && mrf_bucket_clamped(bucket[u], P.NB) == b ? total[u] : 0.0f;
+        }
         s = mrf_lanes_sum<64>(s);
         if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = s;
         __syncthreads();
@@ -410,11 +458,17 @@ void bucket_strides(MrfBucketParams &P, int heads_last)
 
 bool bucket_small_backward(const MrfBucketParams &P) { return P.Q <= MRF_BUCKET_SIDE && P.K <= MRF_BUCKET_SIDE && P.NB <= MRF_BUCKET_MANY; }
 
-// rows of a wavefront: 64, or so few (a multiple of four) that there are 4,096 wavefronts
+bool bucket_one_workgroup(const MrfBucketParams &P) { return P.K <= MRF_BUCKET_STRIP && P.Q <= MRF_BUCKET_STACK * MRF_BUCKET_TQ; }
+
+// rows of a wavefront (a multiple of four): an eighth of a matrix that a workgroup has as a whole, else 64, or so few that there are 4,096
+// wavefronts
 void bucket_parts(MrfBucketParams &P)
 {
     P.strips = (int)(((long long)P.K + MRF_BUCKET_STRIP - 1) / MRF_BUCKET_STRIP);
-    for (P.TQ = MRF_BUCKET_TQ; P.TQ > 4 && P.G * P.strips * ((P.Q + P.TQ - 1LL) / P.TQ) < 4096; P.TQ /= 2) {}
+    P.TQ = MRF_BUCKET_TQ;
+    if (bucket_one_workgroup(P)) P.TQ = ((P.Q + MRF_BUCKET_STACK - 1) / MRF_BUCKET_STACK + 3) / 4 * 4;
+    else
+        while (P.TQ > 4 && P.G * P.strips * ((P.Q + P.TQ - 1LL) / P.TQ) < 4096) P.TQ /= 2;
     P.T = (int)((P.Q + (long long)MRF_BUCKET_STACK * P.TQ - 1) / (MRF_BUCKET_STACK * P.TQ));
 }
 
@@ -467,10 +521,19 @@ template <class T> int bucket_backward(MrfBucketParams P, hipStream_t st)
         return launch_status("mrf_bucket_bwd_small");
     }
     bucket_parts(P);
+    const unsigned groups = (unsigned)(P.G < 65535 ? P.G : 65535);
+    if (bucket_one_workgroup(P)) {
+        hipLaunchKernelGGL((mrf_bucket_bwd_long<T, true>), dim3(1, groups), dim3(64 * MRF_BUCKET_STACK), 0, st, P);
+        return launch_status("mrf_bucket_bwd_long");
+    }
+    P.totals = P.diagonals + (size_t)P.G * P.T * P.strips * (MRF_BUCKET_STRIP + MRF_BUCKET_STACK * (size_t)P.TQ);
     const long long blocks = (long long)P.strips * P.T;
     if (blocks > 0x7fffffffLL) return MRF_ERR_BAD_SHAPE;
-    hipLaunchKernelGGL(mrf_bucket_bwd_long<T>, dim3((unsigned)blocks, (unsigned)(P.G < 65535 ? P.G : 65535)), dim3(64 * MRF_BUCKET_STACK), 0, st, P);
-    const int rc = launch_status("mrf_bucket_bwd_long");
+    hipLaunchKernelGGL((mrf_bucket_bwd_long<T, false>), dim3((unsigned)blocks, groups), dim3(64 * MRF_BUCKET_STACK), 0, st, P);
+    int rc = launch_status("mrf_bucket_bwd_long");
+    if (rc != MRF_OK) return rc;
+    hipLaunchKernelGGL(mrf_bucket_bwd_diagonals, dim3((unsigned)(((long long)P.Q + P.K - 1 + 255) / 256), groups), dim3(256), 0, st, P);
+    rc = launch_status("mrf_bucket_bwd_diagonals");
     return rc != MRF_OK ? rc : bucket_sum(P, st);
 }
 
@@ -504,9 +567,10 @@ size_t mrf_bucket_pairwise_workspace_bytes(int64_t n_groups, int32_t Q, int32_t 
     if (bucket_check(n_groups, Q, K, n_buckets) != MRF_OK) return 0;
     MrfBucketParams P = {};
     P.G = n_groups; P.Q = Q; P.K = K; P.NB = n_buckets;
-    if (n_groups == 0 || Q == 0 || K == 0 || bucket_small_backward(P)) return 256;
+    if (n_groups == 0 || Q == 0 || K == 0 || bucket_small_backward(P) || bucket_one_workgroup(P)) return 256;
     bucket_parts(P);
-    return sizeof(float) * (size_t)n_groups * (size_t)P.T * (size_t)P.strips * (MRF_BUCKET_STRIP + MRF_BUCKET_STACK * (size_t)P.TQ);
+    return sizeof(float) * (size_t)n_groups *
+           ((size_t)P.T * (size_t)P.strips * (MRF_BUCKET_STRIP + MRF_BUCKET_STACK * (size_t)P.TQ) + (size_t)Q + K - 1);
 }
 
 int mrf_bucket_pairwise_forward(int64_t n_groups, int32_t Q, int32_t K, int32_t n_buckets, const float *table, int heads_last,
