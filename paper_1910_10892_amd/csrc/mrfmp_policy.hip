@@ -5,6 +5,7 @@
 #include <type_traits>
 
 constexpr int MRF_POLICY_BLOCKS = 4096;      // workgroups at most: partial sums of the loss
+constexpr int MRF_POLICY_LONG_BLOCKS = 256;  // workgroups of 1,024 threads: one a compute unit (two: 70.8 instead of 66.0 us, 2,047 rows of 32,000)
 constexpr int MRF_POLICY_COUNTS = 256;       // workgroups that count the mask
 
 struct MrfPolicyParams {
@@ -14,7 +15,7 @@ struct MrfPolicyParams {
     const void *labels;          // [N] of label_bytes bytes
     int label_bytes;
     const float *advantage;      // entry i / per
-    long long per;
+    unsigned per;
     const float *old_logp, *ref_logp;
     const uint8_t *mask;
     float low, high;             // bounds of the ratio
@@ -35,25 +36,58 @@ __device__ inline int mrf_policy_label(const MrfPolicyParams &P, long long i)
 // relative, 6e-6 where it is smallest (x = -87).  The instruction gives 0 below 2^-126: fine for a sum that holds a 1
 __device__ inline float mrf_exp_neg(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
 
-// the same for probabilities, which may be that small: 2^(t + 64) 2^-64 there
+// the same for probabilities, which may be that small: the square of exp(x / 2), twice as far off
 __device__ inline float mrf_exp_small(float x)
 {
-    const float t = x * 1.44269504088896340736f;
-    const bool small = t < -126.0f;
-    return __builtin_amdgcn_exp2f(small ? t + 64.0f : t) * (small ? 0x1p-64f : 1.0f);
+    const float h = __builtin_amdgcn_exp2f(x * (0.5f * 1.44269504088896340736f));
+    return h * h;
+}
+
+// exp(d) - 1: the series up to d^8 near 0 (relative error 2e-10 at 0.3), where the difference would lose its digits
+__device__ inline float mrf_exp_minus_1(float d)
+{
+    float p = 1.0f / 40320.0f;
+    p = fmaf(p, d, 1.0f / 5040.0f);
+    p = fmaf(p, d, 1.0f / 720.0f);
+    p = fmaf(p, d, 1.0f / 120.0f);
+    p = fmaf(p, d, 1.0f / 24.0f);
+    p = fmaf(p, d, 1.0f / 6.0f);
+    p = fmaf(p, d, 0.5f);
+    p = fmaf(p, d, 1.0f);
+    return fabsf(d) < 0.3f ? p * d : __builtin_amdgcn_exp2f(d * 1.44269504088896340736f) - 1.0f;
+}
+
+// what is given of a pixel (read before its costs are worked on)
+struct MrfPixel {
+    int label;
+    bool counts;
+    float advantage, old_logp, ref_logp;
+};
+
+template <bool TRAIN> __device__ inline MrfPixel mrf_policy_pixel(const MrfPolicyParams &P, long long i, bool there)
+{
+    MrfPixel x = {0, there, 0.0f, 0.0f, 0.0f};
+    if (!there) return x;
+    x.label = mrf_policy_label(P, i);
+    if constexpr (TRAIN) {
+        x.counts = !P.mask || P.mask[i] != 0;
+        x.advantage = P.advantage[P.per == 1u ? (unsigned)i : (unsigned)i / P.per];
+        if (P.old_logp) x.old_logp = P.old_logp[i];
+        if (P.ref_logp) x.ref_logp = P.ref_logp[i];
+    }
+    return x;
 }
 
 // what a pixel adds to the two sums, and the slope of the loss in its log-probability (before 1 / n)
-__device__ inline void mrf_policy_terms(const MrfPolicyParams &P, long long i, float lp, float &gain, float &div, float &slope)
+__device__ inline void mrf_policy_terms(const MrfPolicyParams &P, const MrfPixel &x, float lp, float &gain, float &div, float &slope)
 {
-    const float A = P.advantage[P.per == 1 ? i : i / P.per];
-    const float r = P.old_logp ? expf(lp - P.old_logp[i]) : 1.0f;
-    const float open = r * A, held = fminf(fmaxf(r, P.low), P.high) * A;
+    const float r = P.old_logp ? __builtin_amdgcn_exp2f((lp - x.old_logp) * 1.44269504088896340736f) : 1.0f;
+    const float open = r * x.advantage, held = fminf(fmaxf(r, P.low), P.high) * x.advantage;
     gain = fminf(open, held);
     slope = open <= held ? -open : 0.0f;
     div = 0.0f;
     if (P.ref_logp) {
-        const float d = P.ref_logp[i] - lp, em = expm1f(d);
+        const float d = x.ref_logp - lp, em = mrf_exp_minus_1(d);
         div = em - d;
         if (P.kl > 0.0f) slope -= P.kl * em;
     }
@@ -125,8 +159,12 @@ template <class Row, int E, class Min, class Sum> __device__ inline float mrf_po
     return sum(v);
 }
 
-// Log-probability of the label whose cost is `ca`, from the row's smallest cost and sum; -infinity where no label is allowed
-__device__ inline float mrf_policy_logp(float low, float ca, float s) { return s == 0.0f ? -INFINITY : (low - ca) - logf(s); }
+// Log-probability of the label whose cost is `ca`, from the row's smallest cost and sum (at least 1: the hardware's logarithm to base 2 is off by
+// an ulp of it); -infinity where no label is allowed
+__device__ inline float mrf_policy_logp(float low, float ca, float s)
+{
+    return s == 0.0f ? -INFINITY : (low - ca) - __builtin_amdgcn_logf(s) * 0.69314718055994530942f;
+}
 
 // ---- rows in registers (MrfRow): one reading of the costs, one writing of the gradient
 constexpr int mrf_policy_threads(int TL) { return TL <= 256 ? 256 : TL; }
@@ -144,68 +182,95 @@ __global__ void __launch_bounds__(mrf_policy_threads(TL)) mrf_policy_rows(const 
     double total_gain = 0.0, total_div = 0.0;
     const long long step = (long long)gridDim.x * G;
 
-    const auto rows = [&](auto fast, auto batch, const long long base) {
-        constexpr bool FAST = decltype(fast)::value;
-        constexpr int n = decltype(batch)::value;
-        typename Row::template Raw<T> in[n];
-        int label[n];
-        float own[n];
-        bool counts[n];
+    // a row whose costs are `c`
+    const auto finish = [&](float (&c)[Row::E], const MrfPixel &pixel, float own, const long long first, bool there) {
+        const long long i = first + group;
+        float low;
+        if (TRAIN && P.mask) {
+            // (costs of pixels that do not count may be anything)
 #pragma unroll
-        for (int u = 0; u < n; ++u) {
-            const long long i = base + u * step + group;
-            const bool there = FAST || i < P.N;
-            label[u] = there ? mrf_policy_label(P, i) : 0;
-            counts[u] = there && !(TRAIN && P.mask && P.mask[i] == 0);
+            for (int e = 0; e < Row::E; ++e) c[e] = pixel.counts ? c[e] : 0.0f;
         }
-#pragma unroll
-        for (int u = 0; u < n; ++u) {
-            const long long first = base + u * step;
-            const bool there = FAST || first + group < P.N;
-            const T *at = (const T *)P.cost + (size_t)first * L;
-            Row::template load<FAST>(at, mine, there, L, l, in[u]);
-            own[u] = there ? mrf_to_f32(at[mine + (unsigned)label[u]]) : 0.0f;
-        }
-#pragma unroll
-        for (int u = 0; u < n; ++u) {
-            const long long first = base + u * step, i = first + group;
-            const bool there = FAST || i < P.N;
-            float c[Row::E], low;
-            Row::convert(in[u], L, l, c, INFINITY);
-            if (TRAIN && P.mask) {
-                // (costs of pixels that do not count may be anything)
-#pragma unroll
-                for (int e = 0; e < Row::E; ++e) c[e] = counts[u] ? c[e] : 0.0f;
+        const float s = mrf_policy_exponentials<Row>(c, low, [&](float v) { return Row::min(v, scratch[0]); },
+                                                     [&](float v) { return Row::sum(v, scratch[1]); });
+        const float lp = mrf_policy_logp(low, own, s);
+        if (P.logp && there && l == 0) P.logp[i] = pixel.counts ? lp : 0.0f;
+        if constexpr (TRAIN) {
+            float gain = 0.0f, div = 0.0f, slope = 0.0f;
+            const bool adds = pixel.counts && s != 0.0f;
+            if (adds) mrf_policy_terms(P, pixel, lp, gain, div, slope);
+            if (l == 0) {
+                total_gain += (double)gain;
+                total_div += (double)div;
             }
-            const float s = mrf_policy_exponentials<Row>(c, low, [&](float v) { return Row::min(v, scratch[0]); },
-                                                         [&](float v) { return Row::sum(v, scratch[1]); });
-            const float lp = mrf_policy_logp(low, own[u], s);
-            if (P.logp && there && l == 0) P.logp[i] = counts[u] ? lp : 0.0f;
-            if constexpr (TRAIN) {
-                float gain = 0.0f, div = 0.0f, slope = 0.0f;
-                const bool adds = counts[u] && s != 0.0f;
-                if (adds) mrf_policy_terms(P, i, lp, gain, div, slope);
-                if (l == 0) {
-                    total_gain += (double)gain;
-                    total_div += (double)div;
-                }
-                if (P.dcost && there) {
-                    const float g = slope * inv_n, f = adds ? g / s : 0.0f;
+            if (P.dcost && there) {
+                const float g = slope * inv_n, f = adds ? g / s : 0.0f;
 #pragma unroll
-                    for (int e = 0; e < Row::E; ++e) c[e] = f * c[e] - (Row::column(l, e / V) + e % V == label[u] ? g : 0.0f);
-                    Row::store((T *)P.dcost + (size_t)first * L + mine, L, l, c);
-                }
+                for (int e = 0; e < Row::E; ++e) c[e] *= f;
+                T *to = (T *)P.dcost + (size_t)first * L + mine;
+                Row::store(to, L, l, c);
+                // (the label's entry once more, by the lane that has stored it)
+                if (pixel.label / V % TL == l) to[pixel.label] = mrf_from_f32<T>(adds ? f * mrf_exp_small(low - own) - g : 0.0f);
             }
         }
     };
-    for (long long base = (long long)blockIdx.x * G; base < P.N;) {
-        if (U > 1 && mrf_rows_fast(base + (U - 1) * step, G, V, P.N)) {
-            rows(std::true_type{}, std::integral_constant<int, U>{}, base);
-            base += U * step;
-        } else {
-            if (mrf_rows_fast(base, G, V, P.N)) rows(std::true_type{}, std::integral_constant<int, 1>{}, base);
-            else rows(std::false_type{}, std::integral_constant<int, 1>{}, base);
-            base += step;
+    if constexpr (TL > 64) {
+        // long rows: the next one is on its way while this one is worked on
+        typename Row::template Raw<T> in;
+        MrfPixel pixel;
+        const auto fetch = [&](const long long base) {
+            const T *at = (const T *)P.cost + (size_t)base * L;
+            pixel = mrf_policy_pixel<TRAIN>(P, base + group, base + group < P.N);
+            if (mrf_rows_fast(base, G, V, P.N)) Row::template load<true>(at, mine, true, L, l, in);
+            else Row::template load<false>(at, mine, base + group < P.N, L, l, in);
+        };
+        if ((long long)blockIdx.x * G < P.N) fetch((long long)blockIdx.x * G);
+        for (long long base = (long long)blockIdx.x * G; base < P.N; base += step) {
+            const bool there = base + group < P.N;
+            const MrfPixel here = pixel;
+            const float own = there ? mrf_to_f32(((const T *)P.cost + (size_t)base * L)[mine + (unsigned)here.label]) : 0.0f;
+            float c[Row::E];
+            Row::convert(in, L, l, c, INFINITY);
+            if (base + step < P.N) fetch(base + step);
+            finish(c, here, own, base, there);
+        }
+    } else {
+        const auto rows = [&](auto fast, auto batch, const long long base) {
+            constexpr bool FAST = decltype(fast)::value;
+            constexpr int n = decltype(batch)::value;
+            typename Row::template Raw<T> in[n];
+            MrfPixel pixel[n];
+            float own[n];
+#pragma unroll
+            for (int u = 0; u < n; ++u) {
+                const long long i = base + u * step + group;
+                pixel[u] = mrf_policy_pixel<TRAIN>(P, i, FAST || i < P.N);
+            }
+#pragma unroll
+            for (int u = 0; u < n; ++u) {
+                const long long first = base + u * step;
+                const bool there = FAST || first + group < P.N;
+                const T *at = (const T *)P.cost + (size_t)first * L;
+                Row::template load<FAST>(at, mine, there, L, l, in[u]);
+                own[u] = there ? mrf_to_f32(at[mine + (unsigned)pixel[u].label]) : 0.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < n; ++u) {
+                const long long first = base + u * step;
+                float c[Row::E];
+                Row::convert(in[u], L, l, c, INFINITY);
+                finish(c, pixel[u], own[u], first, FAST || first + group < P.N);
+            }
+        };
+        for (long long base = (long long)blockIdx.x * G; base < P.N;) {
+            if (U > 1 && mrf_rows_fast(base + (U - 1) * step, G, V, P.N)) {
+                rows(std::true_type{}, std::integral_constant<int, U>{}, base);
+                base += U * step;
+            } else {
+                if (mrf_rows_fast(base, G, V, P.N)) rows(std::true_type{}, std::integral_constant<int, 1>{}, base);
+                else rows(std::false_type{}, std::integral_constant<int, 1>{}, base);
+                base += step;
+            }
         }
     }
     if constexpr (TRAIN) mrf_policy_partial(P, total_gain, total_div);
@@ -226,24 +291,23 @@ __global__ void __launch_bounds__(256) mrf_policy_tile(const MrfPolicyParams P, 
         const int rows = P.N - base < Tile::ROWS ? (int)(P.N - base) : Tile::ROWS;
         const long long i = base + g;
         const bool there = g < rows;
-        const int label = there ? mrf_policy_label(P, i) : 0;
-        const bool counts = there && !(TRAIN && P.mask && P.mask[i] == 0);
+        const MrfPixel pixel = mrf_policy_pixel<TRAIN>(P, i, there);
         Tile::fetch((const T *)P.cost + (size_t)base * L, rows, L, mine);
         mrf_wave_lds_fence();
         float c[E], low;
         Tile::take(mine, g, L, l, c, INFINITY);
-        const float own = mrf_to_f32(mine[g * L + label]);
+        const float own = mrf_to_f32(mine[g * L + pixel.label]);
         if (TRAIN && P.mask) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) c[e] = counts ? c[e] : 0.0f;
+            for (int e = 0; e < E; ++e) c[e] = pixel.counts ? c[e] : 0.0f;
         }
         const float s = mrf_policy_exponentials<Tile>(c, low, [](float v) { return Tile::min(v); }, [](float v) { return Tile::sum(v); });
         const float lp = mrf_policy_logp(low, own, s);
-        if (P.logp && there && l == 0) P.logp[i] = counts ? lp : 0.0f;
+        if (P.logp && there && l == 0) P.logp[i] = pixel.counts ? lp : 0.0f;
         if constexpr (TRAIN) {
             float gain = 0.0f, div = 0.0f, slope = 0.0f;
-            const bool adds = counts && s != 0.0f;
-            if (adds) mrf_policy_terms(P, i, lp, gain, div, slope);
+            const bool adds = pixel.counts && s != 0.0f;
+            if (adds) mrf_policy_terms(P, pixel, lp, gain, div, slope);
             if (l == 0) {
                 total_gain += (double)gain;
                 total_div += (double)div;
@@ -251,9 +315,11 @@ __global__ void __launch_bounds__(256) mrf_policy_tile(const MrfPolicyParams P, 
             if (P.dcost) {
                 const float gs = slope * inv_n, f = adds ? gs / s : 0.0f;
 #pragma unroll
-                for (int e = 0; e < E; ++e) c[e] = f * c[e] - (Tile::column(l, e) == label ? gs : 0.0f);
+                for (int e = 0; e < E; ++e) c[e] *= f;
                 mrf_wave_lds_fence();
                 Tile::put(mine, g, L, l, c);
+                // (the label's entry once more, by the lane that has put it)
+                if (there && pixel.label % TL == l) mine[g * L + pixel.label] = mrf_from_f32<T>(adds ? f * mrf_exp_small(low - own) - gs : 0.0f);
                 mrf_wave_lds_fence();
                 Tile::flush((T *)P.dcost + (size_t)base * L, rows, L, mine);
             }
@@ -275,7 +341,8 @@ __global__ void __launch_bounds__(1024) mrf_policy_any(const MrfPolicyParams P, 
     for (long long i = blockIdx.x; i < P.N; i += gridDim.x) {
         const T *c = (const T *)P.cost + (size_t)i * L;
         T *dc = TRAIN && P.dcost ? (T *)P.dcost + (size_t)i * L : nullptr;
-        if (TRAIN && P.mask && P.mask[i] == 0) {
+        const MrfPixel pixel = mrf_policy_pixel<TRAIN>(P, i, true);
+        if (!pixel.counts) {
             if (dc)
                 for (int k = t; k < L; k += 1024) dc[k] = mrf_from_f32<T>(0.0f);
             if (t == 0 && P.logp) P.logp[i] = 0.0f;
@@ -290,12 +357,12 @@ __global__ void __launch_bounds__(1024) mrf_policy_any(const MrfPolicyParams P, 
         }
         const float low = Row::min(mn, scratch[0]), from = low < INFINITY ? low : 0.0f;
         s = Row::sum(s * mrf_exp_neg(mn < INFINITY ? from - mn : 0.0f), scratch[1]);
-        const int a = mrf_policy_label(P, i);
+        const int a = pixel.label;
         const float lp = mrf_policy_logp(low, mrf_to_f32(c[a]), s);
         if (t == 0 && P.logp) P.logp[i] = lp;
         if constexpr (TRAIN) {
             float gain = 0.0f, div = 0.0f, slope = 0.0f;
-            if (s != 0.0f) mrf_policy_terms(P, i, lp, gain, div, slope);
+            if (s != 0.0f) mrf_policy_terms(P, pixel, lp, gain, div, slope);
             if (t == 0) {
                 total_gain += (double)gain;
                 total_div += (double)div;
@@ -346,8 +413,8 @@ int policy_check(int64_t N, int32_t L, int type, int label_bytes)
 template <class T, bool TRAIN, int TL, int V, int CH> int policy_rows(const MrfPolicyParams &P, int counts, int &blocks, hipStream_t st)
 {
     constexpr int NT = mrf_policy_threads(TL), G = NT / TL;
-    const long long need = (P.N + G - 1) / G;
-    blocks = (int)(need < MRF_POLICY_BLOCKS ? need : MRF_POLICY_BLOCKS);
+    const long long need = (P.N + G - 1) / G, most = TL > 256 ? MRF_POLICY_LONG_BLOCKS : MRF_POLICY_BLOCKS;
+    blocks = (int)(need < most ? need : most);
     hipLaunchKernelGGL((mrf_policy_rows<T, TRAIN, TL, V, CH>), dim3((unsigned)blocks), dim3(NT), 0, st, P, counts);
     return launch_status("mrf_policy_rows");
 }
@@ -363,8 +430,11 @@ template <class T, bool TRAIN, int TL, int E> int policy_tile(const MrfPolicyPar
 
 // F(TL, V, CH) for each layout, shortest rows first
 #define MRF_POLICY_SHORT(F) F(1, 4, 1) F(2, 4, 1) F(4, 4, 1) F(8, 4, 1) F(8, 4, 2) F(8, 4, 3) F(16, 4, 2) F(16, 4, 3) F(16, 4, 4)
-#define MRF_POLICY_LONG(F) F(64, 4, 2) F(64, 4, 4) F(64, 4, 8) F(256, 4, 4) F(256, 4, 8) F(1024, 4, 4) F(1024, 4, 8)
-#define MRF_POLICY_LONG_16(F) F(64, 8, 1) F(64, 8, 2) F(64, 8, 4) F(256, 8, 2) F(256, 8, 4) F(1024, 8, 2) F(1024, 8, 4)
+#define MRF_POLICY_LONG(F) \
+    F(64, 4, 2) F(64, 4, 3) F(64, 4, 4) F(64, 4, 6) F(64, 4, 8) F(256, 4, 3) F(256, 4, 4) F(256, 4, 6) F(256, 4, 8) \
+    F(1024, 4, 3) F(1024, 4, 4) F(1024, 4, 6) F(1024, 4, 8)
+#define MRF_POLICY_LONG_16(F) \
+    F(64, 8, 1) F(64, 8, 2) F(64, 8, 3) F(64, 8, 4) F(256, 8, 2) F(256, 8, 3) F(256, 8, 4) F(1024, 8, 2) F(1024, 8, 3) F(1024, 8, 4)
 
 template <class T, bool TRAIN> int policy_any_layout(const MrfPolicyParams &P, int counts, int &blocks, hipStream_t st)
 {
@@ -448,7 +518,7 @@ int mrf_softmin_policy(int64_t n_pixels, int32_t L, const void *cost, int cost_t
     if (workspace_bytes < mrf_softmin_policy_workspace_bytes()) return MRF_ERR_WORKSPACE_TOO_SMALL;
     MrfPolicyParams P = {};
     P.N = n_pixels; P.L = L; P.cost = cost; P.labels = labels; P.label_bytes = label_bytes; P.advantage = advantage;
-    P.per = pixels_per_advantage; P.old_logp = old_logp; P.ref_logp = ref_logp; P.mask = mask; P.low = 1.0f - clip_low;
+    P.per = (unsigned)(pixels_per_advantage < n_pixels ? pixels_per_advantage : (n_pixels > 0 ? n_pixels : 1)); P.old_logp = old_logp; P.ref_logp = ref_logp; P.mask = mask; P.low = 1.0f - clip_low;
     P.high = 1.0f + clip_high; P.kl = kl_weight; P.scale = grad_scale; P.loss = loss; P.logp = logp; P.dcost = grad_cost;
     P.counts = (long long *)workspace;
     P.partial = (double *)((char *)workspace + sizeof(long long) * MRF_POLICY_COUNTS);

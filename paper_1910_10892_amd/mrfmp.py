@@ -144,9 +144,19 @@ def _dev_ptr(t, dtype_name: Optional[str] = None):
         return None
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError("tensors must be contiguous and on the GPU")
-    if dtype_name is not None and str(t.dtype) != "torch." + dtype_name:
+    if dtype_name is not None and _dtype_name(t) != dtype_name:
         raise ValueError("expected %s tensor, got %s" % (dtype_name, t.dtype))
     return ctypes.c_void_p(t.data_ptr())
+
+
+_dtype_names = {}      # torch dtype -> its name without "torch." (the text costs more than the call otherwise)
+
+
+def _dtype_name(t) -> str:
+    name = _dtype_names.get(t.dtype)
+    if name is None:
+        name = _dtype_names[t.dtype] = str(t.dtype).rsplit(".", 1)[-1]
+    return name
 
 
 @dataclass
@@ -198,9 +208,10 @@ class MrfProblem:
 
 
 def _stream_handle(stream):
-    import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+    if stream is None:
+        from torch.cuda import current_device, current_stream
+        stream = current_stream(current_device())      # (with the device named the call takes half as long)
+    return ctypes.c_void_p(stream.cuda_stream)
 
 
 def mrf_strerror(status: int) -> str:
@@ -360,19 +371,19 @@ def mrf_softmin_smooth_l1(cost, target, mask, beta, disparity, loss, grad_cost, 
 
 # ---- learning operators: element types and sizes come from the tensors, which have to fit each other (ValueError)
 
-_TYPES = {"torch.float32": MRF_F32, "torch.float16": MRF_F16, "torch.bfloat16": MRF_BF16}
+_TYPES = {"float32": MRF_F32, "float16": MRF_F16, "bfloat16": MRF_BF16}
 
 
 def _type_of(t, what) -> int:
-    code = _TYPES.get(str(t.dtype))
+    code = _TYPES.get(_dtype_name(t))
     if code is None:
         raise ValueError("%s must be float32, float16 or bfloat16, got %s" % (what, t.dtype))
     return code
 
 
 def _same_size(what, t, *shape):
-    if t is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError("%s has shape %s, expected %s" % (what, tuple(t.shape), tuple(shape)))
+    if t is not None and t.shape != shape:      # (a torch.Size is a tuple)
+        raise ValueError("%s has shape %s, expected %s" % (what, tuple(t.shape), shape))
 
 
 def _checked(rc, name):
@@ -457,7 +468,7 @@ def mrf_bucket_pairwise_backward(grad_out, bucket_of, first_offset, grad_table, 
 
 
 def _label_bytes(labels) -> int:
-    size = {"torch.uint8": 1, "torch.int32": 4}.get(str(labels.dtype))
+    size = {"uint8": 1, "int32": 4}.get(_dtype_name(labels))
     if size is None:
         raise ValueError("labels must be uint8 or int32, got %s" % labels.dtype)
     return size
