@@ -145,9 +145,9 @@ template <class X, class Y, int TL, int V, int CH>
 __global__ void __launch_bounds__(mrf_norm_bwd_threads(TL)) mrf_norm_bwd(const MrfNormParams Q)
 {
     typedef MrfRow<TL, V, CH> Row;
-    constexpr int NT = mrf_norm_bwd_threads(TL), G = NT / TL, U = TL == 256 ? 2 : (TL < 256 ? mrf_norm_batch(2 * Row::E) : 1), SLOTS = TL < 64 ? NT / 64 : G;
+    constexpr int NT = mrf_norm_bwd_threads(TL), G = NT / TL, U = TL == 256 ? 2 : (TL < 256 ? (Row::E <= 4 ? 4 : mrf_norm_batch(2 * Row::E)) : 1), SLOTS = TL < 64 ? NT / 64 : G;
     __shared__ float scratch[2][NT / 64];
-    __shared__ float share[SLOTS > 1 ? SLOTS * TL * V : 1];
+    __shared__ float share[SLOTS > 1 ? SLOTS * Row::W : 1];
     const int l = threadIdx.x % TL, C = Q.C;
     const float inv = 1.0f / (float)C;
     float gamma[Row::E], sg[Row::E], sb[Row::E];
@@ -209,34 +209,35 @@ __global__ void __launch_bounds__(mrf_norm_bwd_threads(TL)) mrf_norm_bwd(const M
         }
     }
     if (!Q.partial) return;
+    // the groups' sums of all columns meet in LDS, those of the weight first; a launch of one workgroup then has the whole sums
+    const bool whole = gridDim.x == 1;
     float *partial = Q.partial + (size_t)blockIdx.x * 2 * C;
 #pragma unroll
-    for (int i = 0; i < CH; ++i)
+    for (int which = 0; which < 2; ++which) {
+        float *out = whole ? (which ? Q.dbeta : Q.dgamma) : partial + (which ? C : 0);
+        if (!out) continue;      // (for the whole workgroup)
+        const int slot = TL < 64 ? threadIdx.x >> 6 : threadIdx.x / TL;
 #pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            float v[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = mrf_norm_across<TL>(which ? sb[i * V + j] : sg[i * V + j]);
-            float *out = partial + (which ? C : 0);
+        for (int e = 0; e < Row::E; ++e) {
+            const int c = Row::column(l, e / V) + e % V;
+            const float v = mrf_norm_across<TL>(which ? sb[e] : sg[e]);
             if constexpr (SLOTS == 1) {
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    if (Row::column(l, i) + j < C) out[Row::column(l, i) + j] = v[j];
-            } else {
-                const int slot = TL < 64 ? threadIdx.x >> 6 : threadIdx.x / TL;
-                if (TL >= 64 || (threadIdx.x & 63) < TL)
-#pragma unroll
-                    for (int j = 0; j < V; ++j) share[slot * TL * V + l * V + j] = v[j];
-                __syncthreads();
-                for (int k = threadIdx.x; k < TL * V; k += NT) {
-                    float t = share[k];
-#pragma unroll
-                    for (int w = 1; w < SLOTS; ++w) t += share[w * TL * V + k];
-                    if (TL * V * i + k < C) out[TL * V * i + k] = t;
-                }
-                __syncthreads();
+                if (c < C) out[c] = v;
+            } else if (TL >= 64 || (threadIdx.x & 63) < TL) {
+                share[slot * Row::W + c] = v;
             }
         }
+        if constexpr (SLOTS > 1) {
+            __syncthreads();
+            for (int c = threadIdx.x; c < C; c += NT) {
+                float t = share[c];
+#pragma unroll
+                for (int w = 1; w < SLOTS; ++w) t += share[w * Row::W + c];
+                out[c] = t;
+            }
+            __syncthreads();
+        }
+    }
 }
 
 // ---- a wavefront per row: any length
@@ -330,7 +331,7 @@ __global__ void __launch_bounds__(1024) mrf_norm_param_sum(const MrfNormParams Q
     const long long c = (long long)blockIdx.x * 16 + col;      // [0, C) weight, [C, 2 C) bias
     float s = 0.0f;
     if (c < 2LL * Q.C)
-#pragma unroll 4
+#pragma unroll 8
         for (int p = part; p < Q.P; p += 64) s += Q.partial[(size_t)p * 2 * Q.C + c];
     sums[part][col] = s;
     __syncthreads();
@@ -353,11 +354,12 @@ using namespace mrf_host;
 
 namespace {
 
-// Workgroups of a backward call at most, each of which leaves a partial sum: two of 512 threads on each compute unit; one of 1,024
+// Workgroups of a backward call at most, each of which leaves a partial sum: one for so little that a second launch would take longer than its rows
+// (2,048 x 16: 8 us with one, 5.7 us with 16 and a sum of theirs, but 9.7 us through the binding); else two of 512 threads on each compute unit; one of 1,024
 // for long rows, whose partial sums take memory traffic of their own.
 int norm_partials(int64_t n_rows, int32_t C)
 {
-    const int most = C <= 1024 ? 512 : 256;
+    const int most = (long long)C * n_rows <= 32768 && C <= 1024 ? 1 : (C <= 1024 ? 512 : 256);
     return (int)(most < n_rows ? most : n_rows);
 }
 
@@ -429,10 +431,15 @@ template <class X, class Y> int norm_forward(const MrfNormParams &Q, hipStream_t
     return launch_status("mrf_norm_fwd_any");
 }
 
-template <class X, class Y> int norm_bwd_launch(MrfNormParams &Q, hipStream_t st)
+// `summed`: one workgroup has written the weight's and the bias's gradient itself
+template <class X, class Y> int norm_bwd_launch(MrfNormParams &Q, bool &summed, hipStream_t st)
 {
 #define MRF_LAUNCH(TL, V, CH) \
-    if (Q.C <= TL * V * CH) return norm_bwd_rows<X, Y, TL, V, CH>(Q, st, Q.P);
+    if (Q.C <= TL * V * CH) { \
+        const int rc = norm_bwd_rows<X, Y, TL, V, CH>(Q, st, Q.P); \
+        summed = Q.P == 1; \
+        return rc; \
+    }
     MRF_NORM_BWD_SHORT(MRF_LAUNCH)
     if constexpr (sizeof(X) == 2) {
         MRF_NORM_BWD_LONG_16(MRF_LAUNCH)
@@ -456,8 +463,9 @@ template <class X, class Y> int norm_backward(MrfNormParams Q, hipStream_t st)
     const bool params = Q.dgamma || Q.dbeta;
     if (!params) Q.partial = nullptr;
     if (Q.N > 0 && (params || Q.dx)) {
-        const int rc = norm_bwd_launch<X, Y>(Q, st);
-        if (rc != MRF_OK) return rc;
+        bool summed = false;
+        const int rc = norm_bwd_launch<X, Y>(Q, summed, st);
+        if (rc != MRF_OK || summed) return rc;
     }
     if (!params) return MRF_OK;
     hipLaunchKernelGGL(mrf_norm_param_sum, dim3((unsigned)((2LL * Q.C + 15) / 16)), dim3(1024), 0, st, Q);

@@ -93,38 +93,72 @@ __device__ inline void mrf_policy_terms(const MrfPolicyParams &P, const MrfPixel
     }
 }
 
-__global__ void __launch_bounds__(1024) mrf_policy_count(const MrfPolicyParams P)
+// counted pixels among n entries of the mask, for this thread's share of `threads` (16 entries a load where the address allows it)
+__device__ inline int mrf_policy_count_share(const uint8_t *mask, long long n, long long thread, long long threads)
 {
-    __shared__ int waves[16];
     int c = 0;
-    for (long long i = (long long)blockIdx.x * 1024 + threadIdx.x; i < P.N; i += (long long)gridDim.x * 1024) c += P.mask[i] != 0;
+    long long done = 0;
+    if (((uintptr_t)mask & 15) == 0) {
+        done = n & ~15LL;
+        for (long long k = thread * 16; k < done; k += threads * 16) {
+            typedef unsigned quad __attribute__((ext_vector_type(4)));
+            const quad v = *(const quad *)(mask + k);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                // the highest bit of every byte that is not 0
+                const unsigned w = v[j];
+                c += __popc((((w & 0x7f7f7f7fu) + 0x7f7f7f7fu) | w) & 0x80808080u);
+            }
+        }
+    }
+    for (long long k = done + thread; k < n; k += threads) c += mask[k] != 0;
+    return c;
+}
+
+__device__ inline long long mrf_policy_lanes_count(long long c)
+{
     for (int m = 1; m < 64; m <<= 1) c += __shfl_xor(c, m);
+    return c;
+}
+
+__global__ void __launch_bounds__(256) mrf_policy_count(const MrfPolicyParams P)
+{
+    __shared__ long long waves[4];
+    const long long c = mrf_policy_lanes_count(mrf_policy_count_share(P.mask, P.N, (long long)blockIdx.x * 256 + threadIdx.x, (long long)gridDim.x * 256));
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = c;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        long long t = 0;
-        for (int w = 0; w < 16; ++w) t += waves[w];
-        P.counts[blockIdx.x] = t;
-    }
+    if (threadIdx.x == 0) P.counts[blockIdx.x] = (waves[0] + waves[1]) + (waves[2] + waves[3]);
 }
 
-// number of counted pixels, at least 1; every thread of the workgroup calls it
+// Number of counted pixels, at least 1, from the counts of `blocks` workgroups, or from the mask itself where there are none (a
+// launch of one workgroup); every thread of the workgroup calls it.
 __device__ inline long long mrf_policy_counted(const MrfPolicyParams &P, int blocks)
 {
-    __shared__ long long total;
+    __shared__ long long total[16];
     if (!P.mask) return P.N > 0 ? P.N : 1;
-    if (threadIdx.x < 64) {
-        long long c = 0;
-        for (int k = threadIdx.x; k < blocks; k += 64) c += P.counts[k];
-        for (int m = 1; m < 64; m <<= 1) c += __shfl_xor(c, m);
-        if (threadIdx.x == 0) total = c > 0 ? c : 1;
-    }
+    long long c = 0;
+    if (blocks == 0) c = mrf_policy_count_share(P.mask, P.N, threadIdx.x, blockDim.x);
+    else
+        for (int k = threadIdx.x; k < blocks; k += blockDim.x) c += P.counts[k];
+    c = mrf_policy_lanes_count(c);
+    if ((threadIdx.x & 63) == 0) total[threadIdx.x >> 6] = c;
     __syncthreads();
-    return total;
+    c = 0;
+    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) c += total[w];
+    return c > 0 ? c : 1;
 }
 
-// what a wavefront's rows add to the two sums ends as one partial sum per workgroup
-__device__ inline void mrf_policy_partial(const MrfPolicyParams &P, double gain, double div)
+__device__ inline void mrf_policy_loss(const MrfPolicyParams &P, double gain, double div, long long n)
+{
+    gain /= (double)n;
+    div /= (double)n;
+    P.loss[0] = (float)(P.kl > 0.0f ? (double)P.kl * div - gain : -gain);
+    P.loss[1] = (float)-gain;
+    P.loss[2] = (float)div;
+}
+
+// what a wavefront's rows add to the two sums ends as one partial sum per workgroup, or as the loss where there is only one
+__device__ inline void mrf_policy_partial(const MrfPolicyParams &P, double gain, double div, long long n)
 {
     __shared__ double sums[2][16];
     gain = mrf_wave_sum_f64(gain);
@@ -134,10 +168,18 @@ __device__ inline void mrf_policy_partial(const MrfPolicyParams &P, double gain,
         sums[1][threadIdx.x >> 6] = div;
     }
     __syncthreads();
-    if (threadIdx.x < 2) {
-        double t = 0.0;
-        for (int w = 0; w < (int)(blockDim.x >> 6); ++w) t += sums[threadIdx.x][w];
-        P.partial[2 * (size_t)blockIdx.x + threadIdx.x] = t;
+    if (threadIdx.x == 0) {
+        gain = div = 0.0;
+        for (int w = 0; w < (int)(blockDim.x >> 6); ++w) {
+            gain += sums[0][w];
+            div += sums[1][w];
+        }
+        if (gridDim.x == 1) {
+            mrf_policy_loss(P, gain, div, n);
+        } else {
+            P.partial[2 * (size_t)blockIdx.x] = gain;
+            P.partial[2 * (size_t)blockIdx.x + 1] = div;
+        }
     }
 }
 
@@ -178,7 +220,8 @@ __global__ void __launch_bounds__(mrf_policy_threads(TL)) mrf_policy_rows(const 
     __shared__ float scratch[2][NT / 64];
     const int l = threadIdx.x % TL, L = P.L;
     const unsigned group = threadIdx.x / TL, mine = group * (unsigned)L;
-    const float inv_n = TRAIN ? P.scale / (float)mrf_policy_counted(P, count_blocks) : 0.0f;
+    const long long counted = TRAIN ? mrf_policy_counted(P, count_blocks) : 1;
+    const float inv_n = P.scale / (float)counted;
     double total_gain = 0.0, total_div = 0.0;
     const long long step = (long long)gridDim.x * G;
 
@@ -273,7 +316,7 @@ __global__ void __launch_bounds__(mrf_policy_threads(TL)) mrf_policy_rows(const 
             }
         }
     }
-    if constexpr (TRAIN) mrf_policy_partial(P, total_gain, total_div);
+    if constexpr (TRAIN) mrf_policy_partial(P, total_gain, total_div, counted);
 }
 
 // the same for short rows through LDS (MrfTile)
@@ -283,7 +326,8 @@ __global__ void __launch_bounds__(256) mrf_policy_tile(const MrfPolicyParams P, 
     typedef MrfTile<TL, E> Tile;
     __shared__ __align__(16) char lds[4][Tile::BYTES];
     const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, l = lane % TL, g = lane / TL, L = P.L;
-    const float inv_n = TRAIN ? P.scale / (float)mrf_policy_counted(P, count_blocks) : 0.0f;
+    const long long counted = TRAIN ? mrf_policy_counted(P, count_blocks) : 1;
+    const float inv_n = P.scale / (float)counted;
     double total_gain = 0.0, total_div = 0.0;
     T *mine = (T *)lds[wv];
     const long long step = (long long)gridDim.x * 4 * Tile::ROWS;
@@ -326,7 +370,7 @@ __global__ void __launch_bounds__(256) mrf_policy_tile(const MrfPolicyParams P, 
         }
         mrf_wave_lds_fence();
     }
-    if constexpr (TRAIN) mrf_policy_partial(P, total_gain, total_div);
+    if constexpr (TRAIN) mrf_policy_partial(P, total_gain, total_div, counted);
 }
 
 // ---- a workgroup per row of any length.  The first pass keeps a running minimum and the sum under it; the second reads the row again
@@ -336,7 +380,8 @@ __global__ void __launch_bounds__(1024) mrf_policy_any(const MrfPolicyParams P, 
     __shared__ float scratch[2][16];
     typedef MrfRow<1024, 1, 1> Row;
     const int t = threadIdx.x, L = P.L;
-    const float inv_n = TRAIN ? P.scale / (float)mrf_policy_counted(P, count_blocks) : 0.0f;
+    const long long counted = TRAIN ? mrf_policy_counted(P, count_blocks) : 1;
+    const float inv_n = P.scale / (float)counted;
     double total_gain = 0.0, total_div = 0.0;
     for (long long i = blockIdx.x; i < P.N; i += gridDim.x) {
         const T *c = (const T *)P.cost + (size_t)i * L;
@@ -375,26 +420,31 @@ __global__ void __launch_bounds__(1024) mrf_policy_any(const MrfPolicyParams P, 
         }
         __syncthreads();
     }
-    if constexpr (TRAIN) mrf_policy_partial(P, total_gain, total_div);
+    if constexpr (TRAIN) mrf_policy_partial(P, total_gain, total_div, counted);
 }
 
-// the loss from the partial sums: one workgroup, the first 256 threads add every 256th of the first sum, the others of the second
-__global__ void __launch_bounds__(512) mrf_policy_sum(const MrfPolicyParams P, int blocks, int count_blocks)
+// The loss from the partial sums: one workgroup, the first 512 threads add every 512th of the first sum, the others of the second.
+__global__ void __launch_bounds__(1024) mrf_policy_sum(const MrfPolicyParams P, int blocks, int count_blocks)
 {
-    __shared__ double waves[8];
+    static_assert(MRF_POLICY_BLOCKS <= 8 * 512, "partial sums of a thread");
+    __shared__ double waves[16];
+    const int which = threadIdx.x >> 9;
+    double x[8], v = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int k = (int)(threadIdx.x & 511) + 512 * i;
+        x[i] = k < blocks ? P.partial[2 * (size_t)k + which] : 0.0;
+    }
     const long long n = mrf_policy_counted(P, count_blocks);
-    const int which = threadIdx.x >> 8;
-    double v = 0.0;
-    for (int k = threadIdx.x & 255; k < blocks; k += 256) v += P.partial[2 * (size_t)k + which];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v += x[i];
     v = mrf_wave_sum_f64(v);
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = v;
     __syncthreads();
     if (threadIdx.x == 0) {
-        const double gain = ((waves[0] + waves[1]) + (waves[2] + waves[3])) / (double)n;
-        const double div = ((waves[4] + waves[5]) + (waves[6] + waves[7])) / (double)n;
-        P.loss[0] = (float)(P.kl > 0.0f ? (double)P.kl * div - gain : -gain);
-        P.loss[1] = (float)-gain;
-        P.loss[2] = (float)div;
+        double sum[2] = {0.0, 0.0};
+        for (int w = 0; w < 16; ++w) sum[w >> 3] += waves[w];
+        mrf_policy_loss(P, sum[0], sum[1], n);
     }
 }
 
@@ -410,20 +460,39 @@ int policy_check(int64_t N, int32_t L, int type, int label_bytes)
     return known_type(type) ? MRF_OK : MRF_ERR_BAD_ARGUMENT;
 }
 
-template <class T, bool TRAIN, int TL, int V, int CH> int policy_rows(const MrfPolicyParams &P, int counts, int &blocks, hipStream_t st)
+// counts the mask where more than one workgroup needs the number: `counts` workgroups' counts
+int policy_count(const MrfPolicyParams &P, int blocks, int &counts, hipStream_t st)
+{
+    counts = 0;
+    if (!P.mask || blocks <= 1) return MRF_OK;
+    const long long need = (P.N + 4095) / 4096;
+    counts = (int)(need < MRF_POLICY_COUNTS ? need : MRF_POLICY_COUNTS);
+    hipLaunchKernelGGL(mrf_policy_count, dim3((unsigned)counts), dim3(256), 0, st, P);
+    return launch_status("mrf_policy_count");
+}
+
+template <class T, bool TRAIN, int TL, int V, int CH> int policy_rows(const MrfPolicyParams &P, int &counts, int &blocks, hipStream_t st)
 {
     constexpr int NT = mrf_policy_threads(TL), G = NT / TL;
     const long long need = (P.N + G - 1) / G, most = TL > 256 ? MRF_POLICY_LONG_BLOCKS : MRF_POLICY_BLOCKS;
     blocks = (int)(need < most ? need : most);
+    if (TRAIN) {
+        const int rc = policy_count(P, blocks, counts, st);
+        if (rc != MRF_OK) return rc;
+    }
     hipLaunchKernelGGL((mrf_policy_rows<T, TRAIN, TL, V, CH>), dim3((unsigned)blocks), dim3(NT), 0, st, P, counts);
     return launch_status("mrf_policy_rows");
 }
 
-template <class T, bool TRAIN, int TL, int E> int policy_tile(const MrfPolicyParams &P, int counts, int &blocks, hipStream_t st)
+template <class T, bool TRAIN, int TL, int E> int policy_tile(const MrfPolicyParams &P, int &counts, int &blocks, hipStream_t st)
 {
     constexpr int G = 4 * MrfTile<TL, E>::ROWS;
     const long long need = (P.N + G - 1) / G;
     blocks = (int)(need < 2048 ? need : 2048);
+    if (TRAIN) {
+        const int rc = policy_count(P, blocks, counts, st);
+        if (rc != MRF_OK) return rc;
+    }
     hipLaunchKernelGGL((mrf_policy_tile<T, TRAIN, TL, E>), dim3((unsigned)blocks), dim3(256), 0, st, P, counts);
     return launch_status("mrf_policy_tile");
 }
@@ -436,7 +505,7 @@ template <class T, bool TRAIN, int TL, int E> int policy_tile(const MrfPolicyPar
 #define MRF_POLICY_LONG_16(F) \
     F(64, 8, 1) F(64, 8, 2) F(64, 8, 3) F(64, 8, 4) F(256, 8, 2) F(256, 8, 3) F(256, 8, 4) F(1024, 8, 2) F(1024, 8, 3) F(1024, 8, 4)
 
-template <class T, bool TRAIN> int policy_any_layout(const MrfPolicyParams &P, int counts, int &blocks, hipStream_t st)
+template <class T, bool TRAIN> int policy_any_layout(const MrfPolicyParams &P, int &counts, int &blocks, hipStream_t st)
 {
     if (P.L % 4 != 0 && P.L <= MRF_TILES_LONGEST) {
 #define MRF_LAUNCH(TL, E) \
@@ -454,29 +523,26 @@ template <class T, bool TRAIN> int policy_any_layout(const MrfPolicyParams &P, i
     }
 #undef MRF_LAUNCH
     blocks = (int)(P.N < MRF_POLICY_BLOCKS ? P.N : MRF_POLICY_BLOCKS);
+    if (TRAIN) {
+        const int rc = policy_count(P, blocks, counts, st);
+        if (rc != MRF_OK) return rc;
+    }
     hipLaunchKernelGGL((mrf_policy_any<T, TRAIN>), dim3((unsigned)blocks), dim3(1024), 0, st, P, counts);
     return launch_status("mrf_policy_any");
 }
 
 template <class T> int logp_launch(const MrfPolicyParams &P, hipStream_t st)
 {
-    int blocks = 0;
-    return policy_any_layout<T, false>(P, 0, blocks, st);
+    int counts = 0, blocks = 0;
+    return policy_any_layout<T, false>(P, counts, blocks, st);
 }
 
 template <class T> int policy_launch(const MrfPolicyParams &P, hipStream_t st)
 {
     int counts = 0, blocks = 0;
-    if (P.mask) {
-        const long long need = (P.N + 1023) / 1024;
-        counts = (int)(need < MRF_POLICY_COUNTS ? need : MRF_POLICY_COUNTS);
-        hipLaunchKernelGGL(mrf_policy_count, dim3((unsigned)counts), dim3(1024), 0, st, P);
-        const int rc = launch_status("mrf_policy_count");
-        if (rc != MRF_OK) return rc;
-    }
     const int rc = policy_any_layout<T, true>(P, counts, blocks, st);
-    if (rc != MRF_OK) return rc;
-    hipLaunchKernelGGL(mrf_policy_sum, dim3(1), dim3(512), 0, st, P, blocks, counts);
+    if (rc != MRF_OK || blocks == 1) return rc;
+    hipLaunchKernelGGL(mrf_policy_sum, dim3(1), dim3(1024), 0, st, P, blocks, counts);
     return launch_status("mrf_policy_sum");
 }
 
@@ -525,7 +591,7 @@ int mrf_softmin_policy(int64_t n_pixels, int32_t L, const void *cost, int cost_t
     hipStream_t st = (hipStream_t)hip_stream;
     if (n_pixels == 0) {
         P.mask = nullptr;
-        hipLaunchKernelGGL(mrf_policy_sum, dim3(1), dim3(512), 0, st, P, 0, 0);
+        hipLaunchKernelGGL(mrf_policy_sum, dim3(1), dim3(1024), 0, st, P, 0, 0);
         return launch_status("mrf_policy_sum");
     }
     if (cost_type == MRF_F32) return policy_launch<float>(P, st);

@@ -19,6 +19,9 @@ from .build import LIB_PATH
 MRF_ISGMR, MRF_TRWP = 0, 1
 MRF_F32, MRF_F16, MRF_BF16 = 0, 1, 2
 _lib = None
+# handle of a device's current stream without a stream object around it, where torch has it (a tenth of a microsecond instead of 2.7, as much as
+# a launch); looked up with the library
+_raw_stream = _current_device = None
 
 
 class MrfError(RuntimeError):
@@ -64,7 +67,9 @@ def load_library():
     # that the library's dependency on libamdhip64 binds to the copy torch has loaded; loaded
     # the other way round the process ends up with two runtimes and the library's own sees
     # no initialised device.
-    import torch  # noqa: F401
+    import torch
+    global _raw_stream, _current_device
+    _raw_stream, _current_device = getattr(torch._C, "_cuda_getCurrentRawStream", None), torch.cuda.current_device
     lib = ctypes.CDLL(LIB_PATH)
     vp, sz, ci = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int
     P = ctypes.POINTER(_CProblem)
@@ -208,10 +213,12 @@ class MrfProblem:
 
 
 def _stream_handle(stream):
-    if stream is None:
-        from torch.cuda import current_device, current_stream
-        stream = current_stream(current_device())      # (with the device named the call takes half as long)
-    return ctypes.c_void_p(stream.cuda_stream)
+    if stream is not None:
+        return ctypes.c_void_p(stream.cuda_stream)
+    if _raw_stream is not None:
+        return _raw_stream(_current_device())
+    import torch
+    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
 def mrf_strerror(status: int) -> str:
@@ -381,6 +388,17 @@ def _type_of(t, what) -> int:
     return code
 
 
+def _ptr(t, dtype_name: Optional[str]):
+    """_dev_ptr for an argument that is declared a pointer: the plain address."""
+    if t is None:
+        return None
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("tensors must be contiguous and on the GPU")
+    if dtype_name is not None and _dtype_name(t) != dtype_name:
+        raise ValueError("expected %s tensor, got %s" % (dtype_name, t.dtype))
+    return t.data_ptr()
+
+
 def _same_size(what, t, *shape):
     if t is not None and t.shape != shape:      # (a torch.Size is a tuple)
         raise ValueError("%s has shape %s, expected %s" % (what, tuple(t.shape), shape))
@@ -405,8 +423,8 @@ def mrf_layer_norm_forward(x, gamma, beta, eps, y, mean, rstd, stream=None):
     for name, t in (("mean", mean), ("rstd", rstd)):
         _same_size(name, t, *rows)
     _checked(load_library().mrf_layer_norm_forward(
-        math.prod(rows), C, _dev_ptr(x), _type_of(x, "x"), _dev_ptr(gamma, "float32"), _dev_ptr(beta, "float32"), float(eps),
-        _dev_ptr(y), _type_of(y, "y"), _dev_ptr(mean, "float32"), _dev_ptr(rstd, "float32"), _stream_handle(stream)),
+        math.prod(rows), C, _ptr(x, None), _type_of(x, "x"), _ptr(gamma, "float32"), _ptr(beta, "float32"), float(eps),
+        _ptr(y, None), _type_of(y, "y"), _ptr(mean, "float32"), _ptr(rstd, "float32"), _stream_handle(stream)),
         "mrf_layer_norm_forward")
 
 
@@ -423,9 +441,9 @@ def mrf_layer_norm_backward(grad_y, x, gamma, mean, rstd, grad_x, grad_gamma, gr
     if grad_x is not None and grad_x.dtype != x.dtype:
         raise ValueError("grad_x must be %s like x, got %s" % (x.dtype, grad_x.dtype))
     _checked(load_library().mrf_layer_norm_backward(
-        math.prod(rows), C, _dev_ptr(grad_y), _type_of(grad_y, "grad_y"), _dev_ptr(x), _type_of(x, "x"), _dev_ptr(gamma, "float32"),
-        _dev_ptr(mean, "float32"), _dev_ptr(rstd, "float32"), _dev_ptr(grad_x), _dev_ptr(grad_gamma, "float32"),
-        _dev_ptr(grad_beta, "float32"), _dev_ptr(workspace), _ws_size(workspace), _stream_handle(stream)), "mrf_layer_norm_backward")
+        math.prod(rows), C, _ptr(grad_y, None), _type_of(grad_y, "grad_y"), _ptr(x, None), _type_of(x, "x"), _ptr(gamma, "float32"),
+        _ptr(mean, "float32"), _ptr(rstd, "float32"), _ptr(grad_x, None), _ptr(grad_gamma, "float32"),
+        _ptr(grad_beta, "float32"), _ptr(workspace, None), _ws_size(workspace), _stream_handle(stream)), "mrf_layer_norm_backward")
 
 
 def mrf_distance_buckets(n_buckets: int, far_distance: int, first_offset: int, n_offsets: int, two_sided: bool = True):
@@ -453,8 +471,8 @@ def mrf_bucket_pairwise_forward(table, bucket_of, first_offset, out, query_offse
     first_offset on, out [..., Q, K] float32, float16 or bfloat16."""
     G, Q, K, NB = _bucket_sizes(table, out, heads_last)
     _checked(load_library().mrf_bucket_pairwise_forward(
-        G, Q, K, NB, _dev_ptr(table, "float32"), int(bool(heads_last)), _dev_ptr(bucket_of, "int32"), int(first_offset),
-        int(bucket_of.numel()), int(query_offset), _dev_ptr(out), _type_of(out, "out"), _stream_handle(stream)),
+        G, Q, K, NB, _ptr(table, "float32"), int(bool(heads_last)), _ptr(bucket_of, "int32"), int(first_offset),
+        int(bucket_of.numel()), int(query_offset), _ptr(out, None), _type_of(out, "out"), _stream_handle(stream)),
         "mrf_bucket_pairwise_forward")
 
 
@@ -462,8 +480,8 @@ def mrf_bucket_pairwise_backward(grad_out, bucket_of, first_offset, grad_table, 
     """grad_out [..., Q, K], grad_table like the table of the forward call."""
     G, Q, K, NB = _bucket_sizes(grad_table, grad_out, heads_last)
     _checked(load_library().mrf_bucket_pairwise_backward(
-        G, Q, K, NB, _dev_ptr(grad_out), _type_of(grad_out, "grad_out"), int(bool(heads_last)), _dev_ptr(bucket_of, "int32"),
-        int(first_offset), int(bucket_of.numel()), int(query_offset), _dev_ptr(grad_table, "float32"), _dev_ptr(workspace),
+        G, Q, K, NB, _ptr(grad_out, None), _type_of(grad_out, "grad_out"), int(bool(heads_last)), _ptr(bucket_of, "int32"),
+        int(first_offset), int(bucket_of.numel()), int(query_offset), _ptr(grad_table, "float32"), _ptr(workspace, None),
         _ws_size(workspace), _stream_handle(stream)), "mrf_bucket_pairwise_backward")
 
 
@@ -479,8 +497,8 @@ def mrf_softmin_logp(cost, labels, logp, stream=None):
     pixels, L = tuple(cost.shape[:-1]), int(cost.shape[-1])
     _same_size("labels", labels, *pixels)
     _same_size("logp", logp, *pixels)
-    _checked(load_library().mrf_softmin_logp(math.prod(pixels), L, _dev_ptr(cost), _type_of(cost, "cost"), _dev_ptr(labels),
-                                             _label_bytes(labels), _dev_ptr(logp, "float32"), _stream_handle(stream)), "mrf_softmin_logp")
+    _checked(load_library().mrf_softmin_logp(math.prod(pixels), L, _ptr(cost, None), _type_of(cost, "cost"), _ptr(labels, None),
+                                             _label_bytes(labels), _ptr(logp, "float32"), _stream_handle(stream)), "mrf_softmin_logp")
 
 
 def mrf_softmin_policy_workspace_bytes() -> int:
@@ -503,10 +521,10 @@ def mrf_softmin_policy(cost, labels, advantage, old_logp, ref_logp, mask, clip_l
     if per >= 1 and int(advantage.numel()) != -(-n // per):
         raise ValueError("advantage has %d entries, expected %d" % (advantage.numel(), -(-n // per)))
     _checked(load_library().mrf_softmin_policy(
-        n, L, _dev_ptr(cost), _type_of(cost, "cost"), _dev_ptr(labels), _label_bytes(labels), _dev_ptr(advantage, "float32"), per,
-        _dev_ptr(old_logp, "float32"), _dev_ptr(ref_logp, "float32"), _dev_ptr(mask, "uint8"), float(clip_low), float(clip_high),
-        float(kl_weight), float(grad_scale), _dev_ptr(loss, "float32"), _dev_ptr(logp, "float32"), _dev_ptr(grad_cost),
-        _dev_ptr(workspace), _ws_size(workspace), _stream_handle(stream)), "mrf_softmin_policy")
+        n, L, _ptr(cost, None), _type_of(cost, "cost"), _ptr(labels, None), _label_bytes(labels), _ptr(advantage, "float32"), per,
+        _ptr(old_logp, "float32"), _ptr(ref_logp, "float32"), _ptr(mask, "uint8"), float(clip_low), float(clip_high),
+        float(kl_weight), float(grad_scale), _ptr(loss, "float32"), _ptr(logp, "float32"), _ptr(grad_cost, None),
+        _ptr(workspace, None), _ws_size(workspace), _stream_handle(stream)), "mrf_softmin_policy")
 
 
 def mrf_workspace_fault(workspace, stream=None) -> int:
