@@ -1,0 +1,150 @@
+"""The learning operators through torch.autograd, alone against their fp64 definitions and together with the message passing
+as the example runs them."""
+import importlib.util
+import os
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_layer_norm_through_autograd(dtype):
+    import torch
+    from oracle import mrf_learn_oracle as lo
+    from paper_1910_10892_amd.autograd import layer_norm
+    rng = np.random.default_rng(1)
+    # (a transposed view: the wrapper makes it contiguous)
+    x = torch.from_numpy(rng.normal(1.0, 2.0, (21, 40, 3)).astype(np.float32)).cuda().to(getattr(torch, dtype)).permute(2, 1, 0)
+    x.requires_grad_(True)
+    w = torch.from_numpy(rng.normal(1.0, 0.3, 21).astype(np.float32)).cuda().requires_grad_(True)
+    b = torch.zeros(21, device="cuda:0", requires_grad=True)
+    y = layer_norm(x, w, b, dtype=torch.float32)
+    assert y.dtype == torch.float32 and y.shape == x.shape
+    up = torch.from_numpy(rng.normal(size=(3, 40, 21)).astype(np.float32)).cuda()
+    y.backward(up)
+    xd = x.detach().double().cpu().numpy().reshape(-1, 21)
+    want, _, _ = lo.layer_norm(xd, w.detach().cpu().numpy(), b.detach().cpu().numpy())
+    gx, gw, gb = lo.layer_norm_grad(up.double().cpu().numpy().reshape(-1, 21), xd, w.detach().cpu().numpy())
+    np.testing.assert_allclose(y.detach().cpu().numpy().reshape(-1, 21), want, rtol=1e-5, atol=1e-5)
+    assert x.grad.dtype == x.dtype
+    np.testing.assert_allclose(x.grad.double().cpu().numpy().reshape(-1, 21), gx, rtol=1e-5 if dtype == "float32" else 2.0 ** -8, atol=1e-5)
+    np.testing.assert_allclose(w.grad.cpu().numpy(), gw, rtol=1e-5, atol=1e-4)
+    np.testing.assert_allclose(b.grad.cpu().numpy(), gb, rtol=1e-5, atol=1e-4)
+    # without parameters, and with the input alone asking for a gradient
+    z = x.detach().requires_grad_(True)
+    layer_norm(z).float().sum().backward()
+    assert z.grad is not None
+    v = w.detach().requires_grad_(True)
+    layer_norm(x.detach(), v, None).float().sum().backward()
+    assert v.grad is not None
+
+
+def test_bucket_pairwise_through_autograd_as_heads_and_as_edges():
+    import torch
+    import paper_1910_10892_amd as mrf
+    from oracle import mrf_learn_oracle as lo
+    from paper_1910_10892_amd.autograd import bucket_pairwise
+    rng = np.random.default_rng(2)
+    m = mrf.mrf_distance_buckets(8, 16, -30, 61)
+    bucket_of = torch.from_numpy(m).cuda()
+    for heads_last, shape in ((True, (8, 5)), (False, (2, 3, 4, 8))):
+        table = torch.from_numpy(rng.normal(size=shape).astype(np.float32)).cuda().requires_grad_(True)
+        out = bucket_pairwise(table, bucket_of, -30, 9, 13, query_offset=4, heads_last=heads_last)
+        assert out.shape == ((5, 9, 13) if heads_last else (2, 3, 4, 9, 13))
+        up = torch.from_numpy(rng.normal(size=out.shape).astype(np.float32)).cuda()
+        out.backward(up)
+        t = table.detach().cpu().numpy()
+        t = t.T if heads_last else t.reshape(-1, 8)
+        np.testing.assert_array_equal(out.detach().cpu().numpy().reshape(-1, 9, 13), lo.bucket_pairwise(t, 9, 13, m, -30, 4).astype(np.float32))
+        want, _ = lo.bucket_pairwise_grad(up.cpu().numpy().reshape(-1, 9, 13), 8, m, -30, 4)
+        np.testing.assert_allclose(table.grad.cpu().numpy(), want.T if heads_last else want.reshape(shape), rtol=1e-5, atol=1e-5)
+    # a table that several groups share by broadcasting: torch sums its gradient
+    shared = torch.from_numpy(rng.normal(size=(1, 8)).astype(np.float32)).cuda().requires_grad_(True)
+    bucket_pairwise(shared.expand(6, 8), bucket_of, -30, 4, 4).sum().backward()
+    want, _ = lo.bucket_pairwise_grad(np.ones((1, 4, 4)), 8, m, -30)
+    np.testing.assert_allclose(shared.grad.cpu().numpy(), 6 * want, rtol=1e-6)
+
+
+def test_policy_loss_through_autograd():
+    import torch
+    from oracle import mrf_learn_oracle as lo
+    from paper_1910_10892_amd.autograd import policy_loss, softmin_logp
+    rng = np.random.default_rng(3)
+    c = rng.normal(size=(2, 5, 7, 6)).astype(np.float32)
+    a = rng.integers(0, 6, (2, 5, 7)).astype(np.uint8)
+    A = np.array([0.7, -0.4], np.float32)
+    cost = torch.from_numpy(c).cuda().requires_grad_(True)
+    labels = torch.from_numpy(a).cuda()
+    old = softmin_logp(cost, labels)
+    assert not old.requires_grad
+    old = old - 0.05
+    loss, terms, logp = policy_loss(cost, labels, torch.from_numpy(A).cuda(), old, old, kl_weight=0.1, pixels_per_advantage=35)
+    (3.0 * loss).backward()
+    want, wlp, wgrad = lo.policy(c.reshape(-1, 6), a.reshape(-1), A, old.cpu().numpy().reshape(-1), old.cpu().numpy().reshape(-1), None, 0.2, 0.2, 0.1, 35)
+    assert loss.shape == () and float(loss.detach()) == pytest.approx(want[0], rel=1e-5)
+    np.testing.assert_allclose(terms.cpu().numpy(), want[1:], rtol=1e-4, atol=1e-7)
+    np.testing.assert_allclose(logp.cpu().numpy().reshape(-1), wlp, rtol=1e-5, atol=1e-6)
+    np.testing.assert_allclose(cost.grad.cpu().numpy().reshape(-1, 6), 3.0 * wgrad, rtol=1e-4, atol=1e-7)
+    # a scaled 16-bit gradient comes back in its own size
+    half = torch.from_numpy(c).cuda().half().requires_grad_(True)
+    policy_loss(half, labels, torch.from_numpy(A).cuda(), old, None, pixels_per_advantage=35, grad_scale=1024.0)[0].backward()
+    _, _, wgrad = lo.policy(half.detach().double().cpu().numpy().reshape(-1, 6), a.reshape(-1), A, old.cpu().numpy().reshape(-1), None, None, 0.2, 0.2, 0.0, 35)
+    np.testing.assert_allclose(half.grad.double().cpu().numpy().reshape(-1, 6), wgrad, rtol=2.0 ** -9, atol=2.0 ** -24)
+
+
+def test_gradients_of_the_whole_chain_are_differences():
+    """Scores -> layer norm -> unaries, values -> pairwise function, message passing, policy loss: the gradients that reach the scores, the
+    norm's parameters and the pairwise values against differences of the whole chain (the minima keep their places for steps
+    this small, so the chain is smooth there)."""
+    import torch
+    import paper_1910_10892_amd as mrf
+    from oracle import mrf_learn_oracle as lo, mrf_oracle
+    from paper_1910_10892_amd.autograd import bucket_pairwise, layer_norm, message_passing, policy_loss, softmin_logp
+    rng = np.random.default_rng(5)
+    B, H, W, L, NB = 1, 5, 6, 7, 6
+    dirs = ((0, 1), (0, -1), (1, 0), (-1, 0))
+    p = {"x": rng.normal(size=(B, H, W, L)), "w": rng.normal(1.0, 0.2, L), "b": rng.normal(size=L), "t": rng.random(NB)}
+    p = {k: v.astype(np.float32).astype(np.float64) for k, v in p.items()}
+    m = mrf.mrf_distance_buckets(NB, L - 1, -(L - 1), 2 * L - 1)
+    g = {k: torch.from_numpy(v.astype(np.float32)).cuda().requires_grad_(True) for k, v in p.items()}
+    bucket_of = torch.from_numpy(m).cuda()
+    cost, _ = message_passing(layer_norm(g["x"], g["w"], g["b"]), bucket_pairwise(g["t"], bucket_of, -(L - 1), L, L), dirs=dirs, K=2)
+    a = rng.integers(0, L, (B, H, W)).astype(np.uint8)
+    A = rng.normal(size=B * H * W).astype(np.float32)
+    labels = torch.from_numpy(a).cuda()
+    old = softmin_logp(cost, labels) - torch.from_numpy(rng.choice([-0.4, -0.05, 0.05, 0.4], (B, H, W)).astype(np.float32)).cuda()
+    loss, _, _ = policy_loss(cost, labels, torch.from_numpy(A).cuda(), old)
+    loss.backward()
+    old = old.double().cpu().numpy().reshape(-1)
+
+    def chain(q):
+        u = lo.layer_norm(q["x"].reshape(-1, L), q["w"], q["b"])[0].reshape(B, H, W, L)
+        V = lo.bucket_pairwise(q["t"][None], L, L, m, -(L - 1))[0]
+        f = mrf_oracle.forward("isgmr", u, V, np.array(dirs), 2, dtype=np.float64)
+        return lo.policy(f.cost.reshape(-1, L), a.reshape(-1), A, old)[0][0]
+
+    assert float(loss.detach()) == pytest.approx(chain(p), rel=1e-4, abs=1e-5)
+    h = 1e-6
+    for k in p:
+        for _ in range(3):
+            v = rng.normal(size=p[k].shape)
+            up, down = dict(p), dict(p)
+            up[k], down[k] = p[k] + h * v, p[k] - h * v
+            want = (chain(up) - chain(down)) / (2 * h)
+            assert float((g[k].grad.double().cpu().numpy() * v).sum()) == pytest.approx(want, rel=2e-3, abs=2e-5), k
+
+
+def test_the_example_learns_from_rewards():
+    spec = importlib.util.spec_from_file_location("learn_by_reward", os.path.join(ROOT, "examples", "learn_by_reward.py"))
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    print("case example", flush=True)
+    rewards, values, loss = example.learn(steps=12)
+    print("rewards", rewards, "values", values.tolist(), flush=True)
+    assert np.isfinite(loss) and rewards[-1] > rewards[0] + 0.1
+    # labels apart cost more than equal ones
+    assert float(values[1:].mean()) > float(values[0])
