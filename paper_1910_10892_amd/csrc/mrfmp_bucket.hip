@@ -176,6 +176,8 @@ __global__ void __launch_bounds__(64 * MRF_BUCKET_WAVES) mrf_bucket_bwd_small(co
     const int mine = lane / K, j = lane - mine * K;
     float *sums = diag[wv];
     T *tile = (T *)(staged + wv * P.tile);
+    // the first entry of the tables that the lane sums, the only one for most sizes
+    const int item_g = lane / NB, item_b = lane - item_g * NB, item_first = item_g * D + begin[item_b], item_end = item_g * D + begin[item_b + 1];
     for (long long g0 = ((long long)blockIdx.x * MRF_BUCKET_WAVES + wv) * groups; g0 < P.G; g0 += (long long)gridDim.x * MRF_BUCKET_WAVES * groups) {
         const int here = P.G - g0 < groups ? (int)(P.G - g0) : groups, n = here * S, chunks = n / PER;
         const T *from = (const T *)P.dout + (size_t)g0 * S;
@@ -232,10 +234,16 @@ __global__ void __launch_bounds__(64 * MRF_BUCKET_WAVES) mrf_bucket_bwd_small(co
         }
         mrf_wave_lds_fence();
         for (int i = lane; i < here * NB; i += 64) {
-            const int g = i / NB, b = i - g * NB, last = begin[b + 1];
+            int g = item_g, b = item_b, d = item_first, last = item_end;
+            if (i >= 64) {
+                g = i / NB;
+                b = i - g * NB;
+                d = g * D + begin[b];
+                last = g * D + begin[b + 1];
+            }
             float s = 0.0f;
 #pragma unroll 4
-            for (int d = begin[b]; d < last; ++d) s += sums[g * D + d];
+            for (; d < last; ++d) s += sums[d];
             P.dtable[(g0 + g) * P.sg + b * P.sb] = s;
         }
         mrf_wave_lds_fence();

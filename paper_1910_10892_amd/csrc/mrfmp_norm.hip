@@ -392,8 +392,8 @@ template <class X, class Y, int TL, int V, int CH> int norm_bwd_rows(const MrfNo
 #define MRF_NORM_FWD_SHORT(F) \
     F(1, 4, 1) F(2, 4, 1) F(4, 4, 1) F(8, 4, 1) F(8, 4, 2) F(8, 4, 3) F(16, 4, 2) F(16, 4, 3) F(16, 4, 4)
 #define MRF_NORM_FWD_LONG(F) \
-    F(64, 4, 2) F(64, 4, 3) F(64, 4, 4) F(256, 4, 2) F(256, 4, 3) F(256, 4, 4) F(1024, 4, 2) F(1024, 4, 3) F(1024, 4, 4)
-#define MRF_NORM_FWD_LONG_16(F) F(64, 8, 1) F(64, 8, 2) F(256, 8, 1) F(256, 8, 2) F(1024, 8, 1) F(1024, 8, 2)
+    F(64, 4, 2) F(64, 4, 3) F(64, 4, 4) F(256, 4, 2) F(256, 4, 3) F(256, 4, 4) F(256, 4, 6) F(256, 4, 8) F(1024, 4, 3) F(1024, 4, 4)
+#define MRF_NORM_FWD_LONG_16(F) F(64, 8, 1) F(64, 8, 2) F(256, 8, 1) F(256, 8, 2) F(256, 8, 3) F(256, 8, 4) F(1024, 8, 2)
 #define MRF_NORM_BWD_SHORT(F) F(1, 4, 1) F(2, 4, 1) F(4, 4, 1) F(8, 4, 1) F(8, 4, 2) F(16, 4, 2) F(16, 4, 3) F(16, 4, 4)
 #define MRF_NORM_BWD_LONG(F) F(64, 4, 2) F(64, 4, 3) F(64, 4, 4) F(256, 4, 2) F(1024, 4, 1) F(1024, 4, 2)
 #define MRF_NORM_BWD_LONG_16(F) F(64, 8, 1) F(64, 8, 2) F(256, 8, 1) F(1024, 8, 1)
