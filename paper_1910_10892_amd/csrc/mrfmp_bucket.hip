@@ -148,7 +148,8 @@ __global__ void __launch_bounds__(256) mrf_bucket_fwd_long(const MrfBucketParams
 // diagonal's sum is complete.
 constexpr int MRF_BUCKET_SIDE = 64, MRF_BUCKET_DIAG = 512, MRF_BUCKET_MANY = 512, MRF_BUCKET_WAVES = 2;      // Q, K; diagonals of a wavefront; buckets; wavefronts
 
-template <class T, bool WIDE>
+// NQ: chunks of a lane; the next matrices' are on their way while these are summed.
+template <class T, bool WIDE, int NQ>
 __global__ void __launch_bounds__(64 * MRF_BUCKET_WAVES) mrf_bucket_bwd_small(const MrfBucketParams P)
 {
     typedef typename MrfChunk<sizeof(T)>::type chunk;
@@ -178,19 +179,26 @@ __global__ void __launch_bounds__(64 * MRF_BUCKET_WAVES) mrf_bucket_bwd_small(co
     T *tile = (T *)(staged + wv * P.tile);
     // the first entry of the tables that the lane sums, the only one for most sizes
     const int item_g = lane / NB, item_b = lane - item_g * NB, item_first = item_g * D + begin[item_b], item_end = item_g * D + begin[item_b + 1];
-    for (long long g0 = ((long long)blockIdx.x * MRF_BUCKET_WAVES + wv) * groups; g0 < P.G; g0 += (long long)gridDim.x * MRF_BUCKET_WAVES * groups) {
-        const int here = P.G - g0 < groups ? (int)(P.G - g0) : groups, n = here * S, chunks = n / PER;
+    quad next[NQ];
+    T rest = (T)0.0f;      // the entry behind the last whole chunk that is the lane's
+    const auto fetch = [&](long long g0) {
+        const int n = (P.G - g0 < groups ? (int)(P.G - g0) : groups) * S, chunks = n / PER;
         const T *from = (const T *)P.dout + (size_t)g0 * S;
-        for (int k = lane; k < chunks; k += 64 * 8) {
-            quad r[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (k + 64 * i < chunks) r[i] = *(const chunk *)(from + (unsigned)(k + 64 * i) * PER);
+        for (int i = 0; i < NQ; ++i)
+            if (lane + 64 * i < chunks) next[i] = *(const chunk *)(from + (unsigned)(lane + 64 * i) * PER);
+        if (chunks * PER + lane < n) rest = from[chunks * PER + lane];
+    };
+    const long long step = (long long)gridDim.x * MRF_BUCKET_WAVES * groups;
+    long long g0 = ((long long)blockIdx.x * MRF_BUCKET_WAVES + wv) * groups;
+    if (g0 < P.G) fetch(g0);
+    for (; g0 < P.G; g0 += step) {
+        const int here = P.G - g0 < groups ? (int)(P.G - g0) : groups, n = here * S, chunks = n / PER;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (k + 64 * i < chunks) ((quad *)tile)[k + 64 * i] = r[i];
-        }
-        if (chunks * PER + lane < n) tile[chunks * PER + lane] = from[chunks * PER + lane];
+        for (int i = 0; i < NQ; ++i)
+            if (lane + 64 * i < chunks) ((quad *)tile)[lane + 64 * i] = next[i];
+        if (chunks * PER + lane < n) tile[chunks * PER + lane] = rest;
+        if (g0 + step < P.G) fetch(g0 + step);
         mrf_wave_lds_fence();
         if (mine < here) {
             const T *x = tile + mine * S;
@@ -293,6 +301,11 @@ __global__ void __launch_bounds__(64 * MRF_BUCKET_STACK) mrf_bucket_bwd_long(con
                 if (q + i + 4 <= rows && K >= 4) {
 #pragma unroll
                     for (int r = i; r < i + 4; ++r) w[r] = *(const vec *)(x + (long long)(q0 + q + r) * K + (unsigned)in);
+                } else if (q + i >= rows) {
+#pragma unroll
+                    for (int r = i; r < i + 4; ++r)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) w[r][j] = (T)0.0f;
                 } else {
                     // the last rows, entry by entry (what is not there is read as the matrix's first entry, and not used)
 #pragma unroll
@@ -385,11 +398,13 @@ __global__ void __launch_bounds__(256) mrf_bucket_bwd_diagonals(const MrfBucketP
     static_assert(MRF_BUCKET_STRIP == 256 && MRF_BUCKET_STACK * MRF_BUCKET_TQ <= 2 * MRF_BUCKET_STRIP, "strips of a diagonal");
     const int Q = P.Q, D = Q + P.K - 1, d = (int)(blockIdx.x * 256 + threadIdx.x), rows = MRF_BUCKET_STACK * P.TQ, n = MRF_BUCKET_STRIP + rows;
     if (d >= D) return;
+    // the parts of its rows
+    const int off = d - (Q - 1), top = off < 0 ? -off : 0, bottom = Q - 1 < P.K - 1 - off ? Q - 1 : P.K - 1 - off;
     for (long long g = blockIdx.y; g < P.G; g += gridDim.y) {
         const float *x = P.diagonals + (size_t)g * P.T * P.strips * n;
         float s = 0.0f;
 #pragma unroll 4
-        for (int p = 0; p < P.T; ++p) {
+        for (int p = top / rows; p <= bottom / rows; ++p) {
             // slot i of strip k is the diagonal 256 k + i - (p + 1) rows + Q - 1: in three strips at most
             const int at = d + (p + 1) * rows - (Q - 1), k0 = at >> 8, i0 = at & 255;
 #pragma unroll
@@ -522,10 +537,19 @@ template <class T> int bucket_backward(MrfBucketParams P, hipStream_t st)
         const int fit = 64 / P.K, room = MRF_BUCKET_DIAG / (P.Q + P.K - 1);
         P.groups = fit < room ? fit : room;
         P.tile = (P.groups * P.Q * P.K * (int)sizeof(T) + 15) / 16 * 16;
+        // (no more workgroups than run at once: each sorts the diagonals first)
         const long long need = (P.G + MRF_BUCKET_WAVES * P.groups - 1) / (MRF_BUCKET_WAVES * P.groups);
-        const dim3 grid((unsigned)(need < 8192 ? need : 8192)), block(64 * MRF_BUCKET_WAVES);
-        if (P.Q <= P.K) hipLaunchKernelGGL((mrf_bucket_bwd_small<T, true>), grid, block, MRF_BUCKET_WAVES * P.tile, st, P);
-        else hipLaunchKernelGGL((mrf_bucket_bwd_small<T, false>), grid, block, MRF_BUCKET_WAVES * P.tile, st, P);
+        const int lds = MRF_BUCKET_WAVES * (P.tile + 4 * MRF_BUCKET_DIAG) + 16 * MRF_BUCKET_SIDE + 4 * MRF_BUCKET_MANY + 16;
+        const int most = 256 * (160 * 1024 / lds < 16 ? 160 * 1024 / lds : 16);
+        const dim3 grid((unsigned)(need < most ? need : most)), block(64 * MRF_BUCKET_WAVES);
+        const unsigned shared = (unsigned)(MRF_BUCKET_WAVES * P.tile);
+        if (P.tile <= 8 * 64 * 16) {
+            if (P.Q <= P.K) hipLaunchKernelGGL((mrf_bucket_bwd_small<T, true, 8>), grid, block, shared, st, P);
+            else hipLaunchKernelGGL((mrf_bucket_bwd_small<T, false, 8>), grid, block, shared, st, P);
+        } else {
+            if (P.Q <= P.K) hipLaunchKernelGGL((mrf_bucket_bwd_small<T, true, 16>), grid, block, shared, st, P);
+            else hipLaunchKernelGGL((mrf_bucket_bwd_small<T, false, 16>), grid, block, shared, st, P);
+        }
         return launch_status("mrf_bucket_bwd_small");
     }
     bucket_parts(P);

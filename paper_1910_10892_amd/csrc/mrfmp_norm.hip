@@ -145,13 +145,14 @@ template <class X, class Y, int TL, int V, int CH>
 __global__ void __launch_bounds__(mrf_norm_bwd_threads(TL)) mrf_norm_bwd(const MrfNormParams Q)
 {
     typedef MrfRow<TL, V, CH> Row;
-    constexpr int NT = mrf_norm_bwd_threads(TL), G = NT / TL, U = TL == 256 ? 2 : (TL < 256 ? (Row::E <= 4 ? 4 : mrf_norm_batch(2 * Row::E)) : 1), SLOTS = TL < 64 ? NT / 64 : G;
+    constexpr int NT = mrf_norm_bwd_threads(TL), G = NT / TL, U = TL >= 256 ? (Row::E <= 8 ? 2 : 1) : (Row::E <= 4 ? 4 : mrf_norm_batch(2 * Row::E)), SLOTS = TL < 64 ? NT / 64 : G;
     __shared__ float scratch[2][NT / 64];
     __shared__ float share[SLOTS > 1 ? SLOTS * Row::W : 1];
     const int l = threadIdx.x % TL, C = Q.C;
     const float inv = 1.0f / (float)C;
-    float gamma[Row::E], sg[Row::E], sb[Row::E];
-    Row::load_columns(Q.gamma, C, l, gamma, 1.0f);
+    constexpr bool KEEP = TL < 1024 || Row::E <= 8;      // (else the weight is read again for every row: there are no registers for it)
+    float gamma[KEEP ? Row::E : 1], sg[Row::E], sb[Row::E];
+    if constexpr (KEEP) Row::load_columns(Q.gamma, C, l, gamma, 1.0f);
 #pragma unroll
     for (int e = 0; e < Row::E; ++e) sg[e] = sb[e] = 0.0f;
     const unsigned group = threadIdx.x / TL, mine = group * (unsigned)C;
@@ -187,7 +188,15 @@ __global__ void __launch_bounds__(mrf_norm_bwd_threads(TL)) mrf_norm_bwd(const M
                 x[e] = (x[e] - mu) * rs;
                 sg[e] = fmaf(dy[e], x[e], sg[e]);
                 sb[e] += dy[e];
-                dy[e] *= gamma[e];
+            }
+            if constexpr (KEEP) {
+#pragma unroll
+                for (int e = 0; e < Row::E; ++e) dy[e] *= gamma[e];
+            } else if (Q.gamma) {
+                Row::scale_columns(Q.gamma, C, l, dy);
+            }
+#pragma unroll
+            for (int e = 0; e < Row::E; ++e) {
                 sa += dy[e];
                 sh = fmaf(dy[e], x[e], sh);
             }
@@ -387,16 +396,16 @@ template <class X, class Y, int TL, int V, int CH> int norm_bwd_rows(const MrfNo
     return launch_status("mrf_norm_bwd");
 }
 
-// F(TL, V, CH) for each layout, shortest rows first.  Forward a lane holds three values per column (x, weight, bias), backward five (x, dy,
-// the weight, two sums): 16 and 8 columns at most where a workgroup of 1,024 threads leaves 128 registers.
+// F(TL, V, CH) for each layout, shortest rows first.  Forward a lane holds three values per column (x, weight, bias), backward four or five (x,
+// dy, two sums, the weight): 16 and 12 columns at most where a workgroup of 1,024 threads leaves 128 registers.
 #define MRF_NORM_FWD_SHORT(F) \
     F(1, 4, 1) F(2, 4, 1) F(4, 4, 1) F(8, 4, 1) F(8, 4, 2) F(8, 4, 3) F(16, 4, 2) F(16, 4, 3) F(16, 4, 4)
 #define MRF_NORM_FWD_LONG(F) \
     F(64, 4, 2) F(64, 4, 3) F(64, 4, 4) F(256, 4, 2) F(256, 4, 3) F(256, 4, 4) F(256, 4, 6) F(256, 4, 8) F(1024, 4, 3) F(1024, 4, 4)
 #define MRF_NORM_FWD_LONG_16(F) F(64, 8, 1) F(64, 8, 2) F(256, 8, 1) F(256, 8, 2) F(256, 8, 3) F(256, 8, 4) F(1024, 8, 2)
 #define MRF_NORM_BWD_SHORT(F) F(1, 4, 1) F(2, 4, 1) F(4, 4, 1) F(8, 4, 1) F(8, 4, 2) F(16, 4, 2) F(16, 4, 3) F(16, 4, 4)
-#define MRF_NORM_BWD_LONG(F) F(64, 4, 2) F(64, 4, 3) F(64, 4, 4) F(256, 4, 2) F(1024, 4, 1) F(1024, 4, 2)
-#define MRF_NORM_BWD_LONG_16(F) F(64, 8, 1) F(64, 8, 2) F(256, 8, 1) F(1024, 8, 1)
+#define MRF_NORM_BWD_LONG(F) F(64, 4, 2) F(64, 4, 3) F(64, 4, 4) F(256, 4, 2) F(1024, 4, 1) F(1024, 4, 2) F(1024, 4, 3)
+#define MRF_NORM_BWD_LONG_16(F) F(64, 8, 1) F(64, 8, 2) F(256, 8, 1) F(1024, 8, 1) F(1024, 4, 3)
 
 // rows of C columns through LDS?
 bool norm_tiles(int C) { return C % 4 != 0 && C <= MRF_TILES_LONGEST; }

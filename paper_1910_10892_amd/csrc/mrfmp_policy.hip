@@ -373,13 +373,16 @@ __global__ void __launch_bounds__(256) mrf_policy_tile(const MrfPolicyParams P, 
     if constexpr (TRAIN) mrf_policy_partial(P, total_gain, total_div, counted);
 }
 
-// ---- a workgroup per row of any length.  The first pass keeps a running minimum and the sum under it; the second reads the row again
+// ---- a workgroup per row of any length.  The first pass keeps a running minimum and the sum under it; the second reads the row again, from the
+// caches for the most part.
 template <class T, bool TRAIN>
 __global__ void __launch_bounds__(1024) mrf_policy_any(const MrfPolicyParams P, int count_blocks)
 {
+    constexpr int V = 16 / (int)sizeof(T);
+    typedef MrfRow<1024, V, 1> Row;
+    typedef typename MrfVec<T, V>::type vec;
     __shared__ float scratch[2][16];
-    typedef MrfRow<1024, 1, 1> Row;
-    const int t = threadIdx.x, L = P.L;
+    const int t = threadIdx.x, L = P.L, whole = L / V * V;      // (chunks of V labels, and the labels behind them)
     const long long counted = TRAIN ? mrf_policy_counted(P, count_blocks) : 1;
     const float inv_n = P.scale / (float)counted;
     double total_gain = 0.0, total_div = 0.0;
@@ -393,17 +396,35 @@ __global__ void __launch_bounds__(1024) mrf_policy_any(const MrfPolicyParams P, 
             if (t == 0 && P.logp) P.logp[i] = 0.0f;
             continue;
         }
+        const float own = mrf_to_f32(c[pixel.label]);
         float mn = INFINITY, s = 0.0f;
-#pragma unroll 8
-        for (int k = t; k < L; k += 1024) {
-            const float v = mrf_to_f32(c[k]), to = fminf(mn, v), from = to < INFINITY ? to : 0.0f;
-            s = s * mrf_exp_neg(mn < INFINITY ? from - mn : 0.0f) + mrf_exp_neg(from - v);
+        const auto take = [&](const float (&v)[V]) {
+            float to = mn;
+#pragma unroll
+            for (int j = 0; j < V; ++j) to = fminf(to, v[j]);
+            const float from = to < INFINITY ? to : 0.0f;
+            s *= mrf_exp_neg(mn < INFINITY ? from - mn : 0.0f);
+#pragma unroll
+            for (int j = 0; j < V; ++j) s += mrf_exp_neg(from - v[j]);
             mn = to;
+        };
+#pragma unroll 4
+        for (int k = t * V; k < whole; k += 1024 * V) {
+            const vec x = *(const vec *)(c + k);
+            float v[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = mrf_to_f32((T)x[j]);
+            take(v);
+        }
+        if (whole + t < L) {
+            float v[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = j == 0 ? mrf_to_f32(c[whole + t]) : INFINITY;
+            take(v);
         }
         const float low = Row::min(mn, scratch[0]), from = low < INFINITY ? low : 0.0f;
         s = Row::sum(s * mrf_exp_neg(mn < INFINITY ? from - mn : 0.0f), scratch[1]);
-        const int a = pixel.label;
-        const float lp = mrf_policy_logp(low, mrf_to_f32(c[a]), s);
+        const float lp = mrf_policy_logp(low, own, s);
         if (t == 0 && P.logp) P.logp[i] = lp;
         if constexpr (TRAIN) {
             float gain = 0.0f, div = 0.0f, slope = 0.0f;
@@ -414,8 +435,15 @@ __global__ void __launch_bounds__(1024) mrf_policy_any(const MrfPolicyParams P, 
             }
             if (dc) {
                 const float g = slope * inv_n, f = s != 0.0f ? g / s : 0.0f;
-#pragma unroll 8
-                for (int k = t; k < L; k += 1024) dc[k] = mrf_from_f32<T>(f * mrf_exp_small(from - mrf_to_f32(c[k])) - (k == a ? g : 0.0f));
+                const auto entry = [&](float v, int k) { return f * mrf_exp_small(from - v) - (k == pixel.label ? g : 0.0f); };
+#pragma unroll 4
+                for (int k = t * V; k < whole; k += 1024 * V) {
+                    vec x = *(const vec *)(c + k);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) x[j] = mrf_from_f32<T>(entry(mrf_to_f32((T)x[j]), k + j));
+                    *(vec *)(dc + k) = x;
+                }
+                if (whole + t < L) dc[whole + t] = mrf_from_f32<T>(entry(mrf_to_f32(c[whole + t]), whole + t));
             }
         }
         __syncthreads();
@@ -498,7 +526,9 @@ template <class T, bool TRAIN, int TL, int E> int policy_tile(const MrfPolicyPar
 }
 
 // F(TL, V, CH) for each layout, shortest rows first
-#define MRF_POLICY_SHORT(F) F(1, 4, 1) F(2, 4, 1) F(4, 4, 1) F(8, 4, 1) F(8, 4, 2) F(8, 4, 3) F(16, 4, 2) F(16, 4, 3) F(16, 4, 4)
+#define MRF_POLICY_FEW(F) F(1, 4, 1) F(2, 4, 1)
+#define MRF_POLICY_FEW_32(F) F(4, 4, 1) F(8, 4, 1)
+#define MRF_POLICY_SHORT(F) F(8, 4, 2) F(8, 4, 3) F(16, 4, 2) F(16, 4, 3) F(16, 4, 4)
 // (long rows: 512 threads against 256 or 1,024 for 8,000 and 12,000 labels in 16 bits 33 and 50 us instead of 38 and 59, 4,000 pixels; the
 // same in 32 bits)
 #define MRF_POLICY_LONG(F) \
@@ -507,9 +537,18 @@ template <class T, bool TRAIN, int TL, int E> int policy_tile(const MrfPolicyPar
 #define MRF_POLICY_LONG_16(F) \
     F(64, 8, 1) F(64, 8, 2) F(64, 8, 3) F(64, 8, 4) F(256, 8, 2) F(512, 8, 2) F(512, 8, 3) F(1024, 8, 2) F(1024, 8, 3) F(1024, 8, 4)
 
+// Rows through LDS: those that are no whole chunks; and of 9 to 32 labels, where a lane has a whole row and its terms of the loss once (4 million
+// pixels of 12 labels in 32 bits 88 against 107 us, 2 million of 24 in 16 bits 44 against 82), except those of 16 and 32 labels in 32 bits, whose
+// entries of a column share LDS banks (137 against 137 and 245 against 132 us).
+bool policy_tiles(int L, int bytes)
+{
+    if (L > MRF_TILES_LONGEST) return false;
+    return L % 4 != 0 || (L > 8 && L <= 32 && !(bytes == 4 && L % 16 == 0));
+}
+
 template <class T, bool TRAIN> int policy_any_layout(const MrfPolicyParams &P, int &counts, int &blocks, hipStream_t st)
 {
-    if (P.L % 4 != 0 && P.L <= MRF_TILES_LONGEST) {
+    if (policy_tiles(P.L, (int)sizeof(T))) {
 #define MRF_LAUNCH(TL, E) \
         if (P.L <= TL * E) return policy_tile<T, TRAIN, TL, E>(P, counts, blocks, st);
         MRF_TILES(MRF_LAUNCH)
@@ -517,6 +556,10 @@ template <class T, bool TRAIN> int policy_any_layout(const MrfPolicyParams &P, i
     }
 #define MRF_LAUNCH(TL, V, CH) \
     if (P.L <= TL * V * CH) return policy_rows<T, TRAIN, TL, V, CH>(P, counts, blocks, st);
+    MRF_POLICY_FEW(MRF_LAUNCH)
+    if constexpr (sizeof(T) == 4) {
+        MRF_POLICY_FEW_32(MRF_LAUNCH)
+    }
     MRF_POLICY_SHORT(MRF_LAUNCH)
     if constexpr (sizeof(T) == 2) {
         MRF_POLICY_LONG_16(MRF_LAUNCH)

@@ -7,7 +7,7 @@
 // smaller pieces.  TL is the smallest that keeps a lane's part at about a dozen values: the steps across lanes, which every row
 // pays, stay few, and there are still enough rows in flight.
 //
-// MrfTile: short rows whose ends do not fall on a chunk's (C % 4).  The 64 / TL rows of a wavefront are neighbours in memory, one piece of
+// MrfTile: short rows, above all those whose ends do not fall on a chunk's (C % 4).  The 64 / TL rows of a wavefront are neighbours in memory, one piece of
 // 16-byte chunks: it goes through LDS as such, and a lane takes its columns l, l + TL, ... of its row from there.  No piece of a chunk
 // is read or written alone, and for up to 32 columns a lane has a whole row: no step across lanes at all.
 #pragma once
@@ -122,6 +122,25 @@ template <int TL_, int V_, int CH_> struct MrfRow {
             }
 #pragma unroll
             for (int j = 0; j < V; ++j) v[i * V + j] = x[j];
+        }
+    }
+
+    // v times the parameters of its columns, a chunk at a time
+    static __device__ inline void scale_columns(const float *at, int C, int l, float (&v)[E])
+    {
+        typedef typename MrfVec<float, V>::type vec;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int c = column(l, i);
+            if (c + V <= C) {
+                const vec x = *(const vec *)(at + c);
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[i * V + j] *= x[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (c + j < C) v[i * V + j] *= at[c + j];
+            }
         }
     }
 
