@@ -242,7 +242,7 @@ int mrf_softmin_smooth_l1(int64_t n_pixels, int32_t L, const float *cost, const 
  * their gradients are 32 bits (sums over rows or pixels that end in a loss 64), and a value is rounded once, to
  * nearest, where it is stored.  No order of a sum depends on anything but the sizes, so results are the
  * same from run to run.  Rows, groups and pixels may be none (then nothing is read; gradients of parameters and the loss
- * are set to 0) and are at most 2^31 - 1; matrices may have more than 2^32 entries.  NaN and infinity in one row (group,
+ * are set to 0) and are at most 2^31 - 1, entries of a row (C, L, Q + K) at most 2^31 - 2^16; matrices may have more than 2^32 entries.  NaN and infinity in one row (group,
  * pixel) stay in its outputs and in the sums that it belongs to.  Asynchronous on hip_stream, nothing allocated, no memset:
  * the calls can be captured into a graph. */
 typedef enum { MRF_F32 = 0, MRF_F16 = 1, MRF_BF16 = 2 } mrf_type;
@@ -313,7 +313,8 @@ int mrf_softmin_logp(int64_t n_pixels, int32_t L, const void *cost, int cost_typ
  *   grad_cost(lambda) = grad_scale d loss / d c(lambda) = grad_scale g / n (f(lambda) - [lambda = a]),
  *   g = d loss_i / d lp = (-r A if r A <= the other term, else 0) + kl_weight (1 - exp(d))
  * n = number of counted pixels; 0 for pixels that do not count, whose costs may be anything (NaN too), and for those without an
- * allowed label, which stay in n.  A counted pixel whose own label is not allowed has r = 0 and an infinite k.
+ * allowed label, which stay in n.  A counted pixel whose own label is not allowed has r = 0 and an
+ * infinite k: with kl_weight > 0 the loss is infinite and the gradient of that pixel not finite.
  *   cost, labels  as above
  *   advantage   DEVICE float: entry i / pixels_per_advantage is that of pixel i (1: one per pixel; H W: one per image)
  *   old_logp    DEVICE [n_pixels] float, or NULL: that of the present costs (r = 1, and its gradient that of r)

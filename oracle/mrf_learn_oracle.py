@@ -112,7 +112,7 @@ def policy(cost, labels, advantage, old_logp=None, ref_logp=None, mask=None, cli
         g = -r * A if r * A <= held else 0.0
         if ref_logp is not None:
             d = float(ref_logp[i]) - lp
-            divergence += np.expm1(d) - d
+            divergence += np.expm1(d) - d if d < np.inf else np.inf
             if kl_weight > 0:
                 g += kl_weight * (1.0 - np.exp(d))
         # lp = -c_a - log sum exp(-c):  d lp / d c_l = f_l - [l = a]

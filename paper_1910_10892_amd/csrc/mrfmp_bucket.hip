@@ -457,7 +457,7 @@ namespace {
 int bucket_check(int64_t G, int32_t Q, int32_t K, int32_t NB)
 {
     if (G < 0 || G > 0x7fffffffLL || Q < 0 || K < 0 || NB < 1 || NB > 65536) return MRF_ERR_BAD_SHAPE;
-    if ((int64_t)Q + K > 0x7fffffffLL || (double)G * Q * K > 1e15) return MRF_ERR_BAD_SHAPE;
+    if ((int64_t)Q + K > LONGEST_ROW || (double)G * Q * K > 1e15) return MRF_ERR_BAD_SHAPE;
     return MRF_OK;
 }
 
@@ -479,29 +479,51 @@ void bucket_strides(MrfBucketParams &P, int heads_last)
     P.sb = heads_last ? P.G : 1;
 }
 
-bool bucket_small_backward(const MrfBucketParams &P) { return P.Q <= MRF_BUCKET_SIDE && P.K <= MRF_BUCKET_SIDE && P.NB <= MRF_BUCKET_MANY; }
+// Small matrices by the wavefront, unless they are few and not very small: then the workgroup's sort of the diagonals is most of the call, and a
+// workgroup for each matrix is faster (32-bit square matrices, one against the other: 64 sides 10.5 / 7.5 us for 1 matrix, 11.2 / 9.3 for 512, 15.8 / 29.8
+// for 2,048; 32 sides 7.0 / 7.2, 7.7 / 9.3, 7.8 / 27.4; 262,144 of 21 sides 98 / 3,106).
+bool bucket_small_backward(const MrfBucketParams &P)
+{
+    return P.Q <= MRF_BUCKET_SIDE && P.K <= MRF_BUCKET_SIDE && P.NB <= MRF_BUCKET_MANY && (P.G > 512 || (P.Q <= 32 && P.K <= 32));
+}
 
+// A workgroup for a whole matrix needs no partial sums: 1,000 of 256 x 256 in 32 bits 56 us, with them 120; 1 such matrix 8.5 and 12.1; 1 of 512 x 256
+// 13.2 and 12.9.
 bool bucket_one_workgroup(const MrfBucketParams &P) { return P.K <= MRF_BUCKET_STRIP && P.Q <= MRF_BUCKET_STACK * MRF_BUCKET_TQ; }
 
-// rows of a wavefront (a multiple of four): an eighth of a matrix that a workgroup has as a whole, else 64, or so few that there are 4,096
-// wavefronts
+// Rows of a wavefront (a multiple of four): an eighth of a matrix that a workgroup has as a whole, else 64, or so few that there are 1,024
+// wavefronts: four a compute unit read fast enough, and more of them leave more partial sums (32-bit, 64 rows always / 1,024 / 4,096 wavefronts: 1 of
+// 2,048 x 2,048 19 / 15 / 25 us, 4 of 600 x 600 25 / 16 / 16, 32 of 300 x 300 25 / 15 / 20).
 void bucket_parts(MrfBucketParams &P)
 {
     P.strips = (int)(((long long)P.K + MRF_BUCKET_STRIP - 1) / MRF_BUCKET_STRIP);
     P.TQ = MRF_BUCKET_TQ;
     if (bucket_one_workgroup(P)) P.TQ = ((P.Q + MRF_BUCKET_STACK - 1) / MRF_BUCKET_STACK + 3) / 4 * 4;
     else
-        while (P.TQ > 4 && P.G * P.strips * ((P.Q + P.TQ - 1LL) / P.TQ) < 4096) P.TQ /= 2;
+        while (P.TQ > 4 && P.G * P.strips * ((P.Q + P.TQ - 1LL) / P.TQ) < 1024) P.TQ /= 2;
     P.T = (int)((P.Q + (long long)MRF_BUCKET_STACK * P.TQ - 1) / (MRF_BUCKET_STACK * P.TQ));
+}
+
+// Many small matrices by whole chunks.  Few of them (below 4,096, or up to 16,384 of nearly 64 x 64 whose rows are whole chunks) are faster row by row from a
+// line, where no thread has an index to work out first (32 bits, chunks / lines: 2,048 of 16 x 16 5.7 / 4.9 us, of 64 x 64 20 / 8.4; 16,384 of
+// 64 x 64 58 / 49, of 63 x 63 58 / 68, of 24 x 24 11 / 25; 262,144 of 21 x 21 103 / 315).
+bool bucket_small_forward(const MrfBucketParams &P, int V)
+{
+    const long long S = (long long)P.Q * P.K;
+    if (S > MRF_BUCKET_SMALL || P.NB > MRF_BUCKET_LDS / 4 || P.G < 4096) return false;
+    return !(S >= 56 * 56 && P.K % V == 0 && P.G <= 16384);
 }
 
 template <class T> int bucket_forward(MrfBucketParams P, hipStream_t st)
 {
     const long long S = (long long)P.Q * P.K;
     const unsigned groups = (unsigned)(P.G < 65535 ? P.G : 65535);
-    if (S <= MRF_BUCKET_SMALL && P.NB <= MRF_BUCKET_LDS / 4) {
+    constexpr int V = 16 / (int)sizeof(T);
+    if (bucket_small_forward(P, V)) {
+        // 16 fours of matrices a workgroup, or so many that the tables have room, and that the launch has many a workgroup (of 1,024 threads: 25,000 of 63 x 63
+        // 88 us instead of 100) or fills the machine (of 256)
         P.quads = 16;
-        while (P.quads > 1 && (P.quads * 4 * P.NB > MRF_BUCKET_LDS || (P.G + 2 * P.quads - 1) / (2 * P.quads) < 1024)) P.quads /= 2;
+        while (P.quads > 1 && (P.quads * 4 * P.NB > MRF_BUCKET_LDS || P.G < (S <= 256 * MRF_BUCKET_CHUNKS ? 2048LL : 16384LL) * P.quads)) P.quads /= 2;
         const long long need = (P.G + 4 * P.quads - 1) / (4 * P.quads);
         if (S <= 256 * MRF_BUCKET_CHUNKS)
             hipLaunchKernelGGL((mrf_bucket_fwd_small<T, 256>), dim3((unsigned)(need < 2048 ? need : 2048)), dim3(256), 0, st, P);
@@ -509,7 +531,6 @@ template <class T> int bucket_forward(MrfBucketParams P, hipStream_t st)
             hipLaunchKernelGGL((mrf_bucket_fwd_small<T, 1024>), dim3((unsigned)(need < 512 ? need : 512)), dim3(1024), 0, st, P);
         return launch_status("mrf_bucket_fwd_small");
     }
-    constexpr int V = 16 / (int)sizeof(T);
     P.KL = 1;
     while (P.KL < 64 && P.KL * V < P.K) P.KL *= 2;
     const int runs = 64 / P.KL;

@@ -20,6 +20,9 @@ inline int launch_status(const char *what)
     return MRF_ERR_HIP;
 }
 
+// Entries of a row at most: a lane's index may run past the row's end by what a launch takes at once (8,192 entries), and stays below 2^31.
+constexpr long long LONGEST_ROW = 0x7fff0000LL;
+
 inline bool known_type(int t) { return t == MRF_F32 || t == MRF_F16 || t == MRF_BF16; }
 }  // namespace mrf_host
 

@@ -20,14 +20,11 @@ struct MrfNormParams {
 // mean, both taken from the registers.
 constexpr int mrf_norm_threads(int TL) { return TL <= 256 ? 256 : TL; }
 
-// rows of a lane that are on their way at once: a launch of short rows would otherwise wait for memory most of its time
-constexpr int mrf_norm_batch(int E) { return E <= 4 ? 4 : (E <= 12 ? 2 : 1); }
-
 template <class X, class Y, int TL, int V, int CH>
 __global__ void __launch_bounds__(mrf_norm_threads(TL)) mrf_norm_fwd(const MrfNormParams Q)
 {
     typedef MrfRow<TL, V, CH> Row;
-    constexpr int NT = mrf_norm_threads(TL), G = NT / TL, U = TL <= 64 ? mrf_norm_batch(Row::E) : 1;
+    constexpr int NT = mrf_norm_threads(TL), G = NT / TL;
     __shared__ float scratch[2][NT / 64];
     const int l = threadIdx.x % TL, C = Q.C;
     const float inv = 1.0f / (float)C;
@@ -40,48 +37,34 @@ __global__ void __launch_bounds__(mrf_norm_threads(TL)) mrf_norm_fwd(const MrfNo
 
     const long long step = (long long)gridDim.x * G;      // rows that a launch takes at once
 
-    // n rows of every group of lanes, `step` apart
-    const auto rows = [&](auto fast, auto batch, const long long base) {
+    const auto rows = [&](auto fast, const long long first) {
         constexpr bool FAST = decltype(fast)::value;
-        constexpr int n = decltype(batch)::value;
-        typename Row::template Raw<X> in[n];
+        typename Row::template Raw<X> in;
+        Row::template load<FAST>((const X *)Q.x + (size_t)first * C, mine, FAST || first + group < Q.N, C, l, in);
+        float x[Row::E];
+        Row::convert(in, C, l, x, 0.0f);
+        float s = 0.0f;
 #pragma unroll
-        for (int u = 0; u < n; ++u)
-            Row::template load<FAST>((const X *)Q.x + (size_t)(base + u * step) * C, mine, FAST || base + group < Q.N, C, l, in[u]);
+        for (int e = 0; e < Row::E; ++e) s += x[e];
+        const float mu = Row::sum(s, scratch[0]) * inv;
+        s = 0.0f;
 #pragma unroll
-        for (int u = 0; u < n; ++u) {
-            const long long first = base + u * step;
-            float x[Row::E];
-            Row::convert(in[u], C, l, x, 0.0f);
-            float s = 0.0f;
+        for (int e = 0; e < Row::E; ++e) {
+            x[e] = fmaf(-mu, in_row[e], x[e]);
+            s = fmaf(x[e], x[e], s);
+        }
+        const float rs = rsqrtf(Row::sum(s, scratch[1]) * inv + Q.eps);
 #pragma unroll
-            for (int e = 0; e < Row::E; ++e) s += x[e];
-            const float mu = Row::sum(s, scratch[0]) * inv;
-            s = 0.0f;
-#pragma unroll
-            for (int e = 0; e < Row::E; ++e) {
-                x[e] = fmaf(-mu, in_row[e], x[e]);
-                s = fmaf(x[e], x[e], s);
-            }
-            const float rs = rsqrtf(Row::sum(s, scratch[1]) * inv + Q.eps);
-#pragma unroll
-            for (int e = 0; e < Row::E; ++e) x[e] = fmaf(x[e] * rs, gamma[e], beta[e]);
-            if (FAST || first + group < Q.N) {
-                Row::store((Y *)Q.y + (size_t)first * C + mine, C, l, x);
-                if (l == 0 && Q.mean) Q.mean[first + group] = mu;
-                if (l == 0 && Q.rstd) Q.rstd[first + group] = rs;
-            }
+        for (int e = 0; e < Row::E; ++e) x[e] = fmaf(x[e] * rs, gamma[e], beta[e]);
+        if (FAST || first + group < Q.N) {
+            Row::store((Y *)Q.y + (size_t)first * C + mine, C, l, x);
+            if (l == 0 && Q.mean) Q.mean[first + group] = mu;
+            if (l == 0 && Q.rstd) Q.rstd[first + group] = rs;
         }
     };
-    for (long long base = (long long)blockIdx.x * G; base < Q.N;) {
-        if (U > 1 && mrf_rows_fast(base + (U - 1) * step, G, V, Q.N)) {
-            rows(std::true_type{}, std::integral_constant<int, U>{}, base);
-            base += U * step;
-        } else {
-            if (mrf_rows_fast(base, G, V, Q.N)) rows(std::true_type{}, std::integral_constant<int, 1>{}, base);
-            else rows(std::false_type{}, std::integral_constant<int, 1>{}, base);
-            base += step;
-        }
+    for (long long base = (long long)blockIdx.x * G; base < Q.N; base += step) {
+        if (mrf_rows_fast(base, G, V, Q.N)) rows(std::true_type{}, base);
+        else rows(std::false_type{}, base);
     }
 }
 
@@ -145,7 +128,7 @@ template <class X, class Y, int TL, int V, int CH>
 __global__ void __launch_bounds__(mrf_norm_bwd_threads(TL)) mrf_norm_bwd(const MrfNormParams Q)
 {
     typedef MrfRow<TL, V, CH> Row;
-    constexpr int NT = mrf_norm_bwd_threads(TL), G = NT / TL, U = TL >= 256 ? (Row::E <= 8 ? 2 : 1) : (Row::E <= 4 ? 4 : mrf_norm_batch(2 * Row::E)), SLOTS = TL < 64 ? NT / 64 : G;
+    constexpr int NT = mrf_norm_bwd_threads(TL), G = NT / TL, SLOTS = TL < 64 ? NT / 64 : G;
     __shared__ float scratch[2][NT / 64];
     __shared__ float share[SLOTS > 1 ? SLOTS * Row::W : 1];
     const int l = threadIdx.x % TL, C = Q.C;
@@ -159,63 +142,45 @@ __global__ void __launch_bounds__(mrf_norm_bwd_threads(TL)) mrf_norm_bwd(const M
 
     const long long step = (long long)gridDim.x * G;
 
-    const auto rows = [&](auto fast, auto batch, const long long base) {
+    const auto rows = [&](auto fast, const long long first) {
         constexpr bool FAST = decltype(fast)::value;
-        constexpr int n = decltype(batch)::value;
-        typename Row::template Raw<X> in[n];
-        typename Row::template Raw<Y> grad[n];
-        float mean[n], rstd[n];
+        const bool there = FAST || first + group < Q.N;
+        typename Row::template Raw<X> in;
+        typename Row::template Raw<Y> grad;
+        Row::template load<FAST>((const X *)Q.x + (size_t)first * C, mine, there, C, l, in);
+        Row::template load<FAST>((const Y *)Q.dy + (size_t)first * C, mine, there, C, l, grad);
+        const float mu = there ? Q.mean[first + group] : 0.0f, rs = there ? Q.rstd[first + group] : 0.0f;
+        float x[Row::E], dy[Row::E];
+        Row::convert(in, C, l, x, 0.0f);
+        Row::convert(grad, C, l, dy, 0.0f);
+        float sa = 0.0f, sh = 0.0f;
+        // (behind a row's end, and behind the last row, dy is 0: nothing is added)
 #pragma unroll
-        for (int u = 0; u < n; ++u) {
-            const long long first = base + u * step;
-            const bool there = FAST || first + group < Q.N;
-            Row::template load<FAST>((const X *)Q.x + (size_t)first * C, mine, there, C, l, in[u]);
-            Row::template load<FAST>((const Y *)Q.dy + (size_t)first * C, mine, there, C, l, grad[u]);
-            mean[u] = there ? Q.mean[first + group] : 0.0f;
-            rstd[u] = there ? Q.rstd[first + group] : 0.0f;
+        for (int e = 0; e < Row::E; ++e) {
+            x[e] = (x[e] - mu) * rs;
+            sg[e] = fmaf(dy[e], x[e], sg[e]);
+            sb[e] += dy[e];
+        }
+        if constexpr (KEEP) {
+#pragma unroll
+            for (int e = 0; e < Row::E; ++e) dy[e] *= gamma[e];
+        } else if (Q.gamma) {
+            Row::scale_columns(Q.gamma, C, l, dy);
         }
 #pragma unroll
-        for (int u = 0; u < n; ++u) {
-            const long long first = base + u * step;
-            const float mu = mean[u], rs = rstd[u];
-            float x[Row::E], dy[Row::E];
-            Row::convert(in[u], C, l, x, 0.0f);
-            Row::convert(grad[u], C, l, dy, 0.0f);
-            float sa = 0.0f, sh = 0.0f;
-            // (behind a row's end, and behind the last row, dy is 0: nothing is added)
-#pragma unroll
-            for (int e = 0; e < Row::E; ++e) {
-                x[e] = (x[e] - mu) * rs;
-                sg[e] = fmaf(dy[e], x[e], sg[e]);
-                sb[e] += dy[e];
-            }
-            if constexpr (KEEP) {
-#pragma unroll
-                for (int e = 0; e < Row::E; ++e) dy[e] *= gamma[e];
-            } else if (Q.gamma) {
-                Row::scale_columns(Q.gamma, C, l, dy);
-            }
-#pragma unroll
-            for (int e = 0; e < Row::E; ++e) {
-                sa += dy[e];
-                sh = fmaf(dy[e], x[e], sh);
-            }
-            sa = Row::sum(sa, scratch[0]) * inv;
-            sh = Row::sum(sh, scratch[1]) * inv;
-#pragma unroll
-            for (int e = 0; e < Row::E; ++e) dy[e] = rs * (dy[e] - sa - x[e] * sh);
-            if (Q.dx && (FAST || first + group < Q.N)) Row::store((X *)Q.dx + (size_t)first * C + mine, C, l, dy);
+        for (int e = 0; e < Row::E; ++e) {
+            sa += dy[e];
+            sh = fmaf(dy[e], x[e], sh);
         }
+        sa = Row::sum(sa, scratch[0]) * inv;
+        sh = Row::sum(sh, scratch[1]) * inv;
+#pragma unroll
+        for (int e = 0; e < Row::E; ++e) dy[e] = rs * (dy[e] - sa - x[e] * sh);
+        if (Q.dx && there) Row::store((X *)Q.dx + (size_t)first * C + mine, C, l, dy);
     };
-    for (long long base = (long long)blockIdx.x * G; base < Q.N;) {
-        if (U > 1 && mrf_rows_fast(base + (U - 1) * step, G, V, Q.N)) {
-            rows(std::true_type{}, std::integral_constant<int, U>{}, base);
-            base += U * step;
-        } else {
-            if (mrf_rows_fast(base, G, V, Q.N)) rows(std::true_type{}, std::integral_constant<int, 1>{}, base);
-            else rows(std::false_type{}, std::integral_constant<int, 1>{}, base);
-            base += step;
-        }
+    for (long long base = (long long)blockIdx.x * G; base < Q.N; base += step) {
+        if (mrf_rows_fast(base, G, V, Q.N)) rows(std::true_type{}, base);
+        else rows(std::false_type{}, base);
     }
     if (!Q.partial) return;
     // the groups' sums of all columns meet in LDS, those of the weight first; a launch of one workgroup then has the whole sums
@@ -368,13 +333,13 @@ namespace {
 // for long rows, whose partial sums take memory traffic of their own.
 int norm_partials(int64_t n_rows, int32_t C)
 {
-    const int most = (long long)C * n_rows <= 32768 && C <= 1024 ? 1 : (C <= 1024 ? 512 : 256);
+    const int most = (long long)C * n_rows <= 32768 && C <= 1024 ? 1 : (C <= 128 ? 512 : 256);
     return (int)(most < n_rows ? most : n_rows);
 }
 
 int norm_check(int64_t n_rows, int32_t C, int x_type, int y_type)
 {
-    if (n_rows < 0 || n_rows > 0x7fffffffLL || C < 1) return MRF_ERR_BAD_SHAPE;
+    if (n_rows < 0 || n_rows > 0x7fffffffLL || C < 1 || C > LONGEST_ROW) return MRF_ERR_BAD_SHAPE;
     if (!known_type(x_type) || !known_type(y_type) || (y_type != x_type && y_type != MRF_F32)) return MRF_ERR_BAD_ARGUMENT;
     return MRF_OK;
 }
@@ -407,8 +372,11 @@ template <class X, class Y, int TL, int V, int CH> int norm_bwd_rows(const MrfNo
 #define MRF_NORM_BWD_LONG(F) F(64, 4, 2) F(64, 4, 3) F(64, 4, 4) F(256, 4, 2) F(1024, 4, 1) F(1024, 4, 2) F(1024, 4, 3)
 #define MRF_NORM_BWD_LONG_16(F) F(64, 8, 1) F(64, 8, 2) F(256, 8, 1) F(1024, 8, 1) F(1024, 4, 3)
 
-// rows of C columns through LDS?
-bool norm_tiles(int C) { return C % 4 != 0 && C <= MRF_TILES_LONGEST; }
+// Forward, rows through LDS: those that are no whole chunks (in 32 bits, registers / LDS: 1 million of 21 44 / 37 us, 300,000 of 149 71 / 68), and those of 20
+// to 60 columns, which leave lanes of a power of two idle (1 million of 36: 66 / 59, from 16 bits to 32 60 / 45, in 16 bits 43 / 32; of 20: 37 / 35, 32 / 26,
+// 19 / 18), except multiples of 16, whose entries of a column share LDS banks (32: 52 / 122).  Longer whole chunks in registers (262,144 of
+// 100 in 16 bits 20 / 28).
+bool norm_tiles(int C) { return C <= MRF_TILES_LONGEST && (C % 4 != 0 || (C > 16 && C < 64 && C % 16 != 0)); }
 
 template <class X, class Y, int TL, int E> int norm_fwd_tiles(const MrfNormParams &Q, hipStream_t st)
 {

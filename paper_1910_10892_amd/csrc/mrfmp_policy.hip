@@ -83,12 +83,13 @@ __device__ inline void mrf_policy_terms(const MrfPolicyParams &P, const MrfPixel
 {
     const float r = P.old_logp ? __builtin_amdgcn_exp2f((lp - x.old_logp) * 1.44269504088896340736f) : 1.0f;
     const float open = r * x.advantage, held = fminf(fmaxf(r, P.low), P.high) * x.advantage;
-    gain = fminf(open, held);
-    slope = open <= held ? -open : 0.0f;
+    const bool clipped = open > held;      // (not where either is NaN, which so reaches the loss)
+    gain = clipped ? held : open;
+    slope = clipped ? 0.0f : -open;
     div = 0.0f;
     if (P.ref_logp) {
         const float d = x.ref_logp - lp, em = mrf_exp_minus_1(d);
-        div = em - d;
+        div = em < INFINITY ? em - d : em;      // (a label that is not allowed: infinite, not infinity less infinity)
         if (P.kl > 0.0f) slope -= P.kl * em;
     }
 }
@@ -210,6 +211,8 @@ __device__ inline float mrf_policy_logp(float low, float ca, float s)
 
 // ---- rows in registers (MrfRow): one reading of the costs, one writing of the gradient
 constexpr int mrf_policy_threads(int TL) { return TL <= 256 ? 256 : TL; }
+
+// rows of a lane that are on their way at once (200,000 pixels of 400 labels in 16 bits 92 us, 100 with one; 32 bits the same either way)
 constexpr int mrf_policy_batch(int E) { return E <= 4 ? 4 : (E <= 12 ? 2 : 1); }
 
 template <class T, bool TRAIN, int TL, int V, int CH>
@@ -484,7 +487,7 @@ int policy_check(int64_t N, int32_t L, int type, int label_bytes)
 {
     if (N < 0 || N > 0x7fffffffLL) return MRF_ERR_BAD_SHAPE;
     if (label_bytes != 1 && label_bytes != 4) return MRF_ERR_BAD_ARGUMENT;
-    if (L < 1 || (label_bytes == 1 && L > MRF_MAX_LABELS)) return MRF_ERR_BAD_LABELS;
+    if (L < 1 || L > LONGEST_ROW || (label_bytes == 1 && L > MRF_MAX_LABELS)) return MRF_ERR_BAD_LABELS;
     return known_type(type) ? MRF_OK : MRF_ERR_BAD_ARGUMENT;
 }
 
@@ -537,25 +540,35 @@ template <class T, bool TRAIN, int TL, int E> int policy_tile(const MrfPolicyPar
 #define MRF_POLICY_LONG_16(F) \
     F(64, 8, 1) F(64, 8, 2) F(64, 8, 3) F(64, 8, 4) F(256, 8, 2) F(512, 8, 2) F(512, 8, 3) F(1024, 8, 2) F(1024, 8, 3) F(1024, 8, 4)
 
-// Rows through LDS: those that are no whole chunks; and of 9 to 32 labels, where a lane has a whole row and its terms of the loss once (4 million
-// pixels of 12 labels in 32 bits 88 against 107 us, 2 million of 24 in 16 bits 44 against 82), except those of 16 and 32 labels in 32 bits, whose
-// entries of a column share LDS banks (137 against 137 and 245 against 132 us).
-bool policy_tiles(int L, int bytes)
+// Rows through LDS?  Registers / LDS, 40 million costs:
+// With the gradient LDS is faster for rows that are no whole chunks (32 bits, 33 labels 96 / 68 us, 149 71 / 66; 16 bits 70 / 44 and 53 / 41) except the shortest
+// (6: 108 / 113 and 77 / 87), and for most others of more than 8 labels, as lanes of a power of two idle less and a pixel's terms are worked out
+// by fewer of them: 32 bits, 40 labels 84 / 67, 100 72 / 67; 16 bits 61 / 40 and 52 / 41, 192 43 / 41.  Not where a column's entries share LDS
+// banks (32 bits: multiples of 32, 64 67 / 90; 16 bits: powers of two, 64 49 / 84), nor for 32-bit rows so long that both only copy (176 66 / 67).
+// Log-probabilities alone write nothing that could be in pieces: LDS up to 60 labels (32 bits: 7 42 / 38, 40 32 / 30, 70 30 / 31, 149 27 / 30; 16 bits: 21 / 17 for 40),
+// but for multiples of 16 in 32 bits (16: 36 / 45).
+template <bool TRAIN> bool policy_tiles(int L, int bytes)
 {
     if (L > MRF_TILES_LONGEST) return false;
-    return L % 4 != 0 || (L > 8 && L <= 32 && !(bytes == 4 && L % 16 == 0));
+    if (!TRAIN) return L <= 60 && (L % 4 != 0 || (L > 8 && (bytes == 2 || L % 16 != 0)));
+    if (L % 4 != 0) return L > 6;
+    return L > 8 && (bytes == 2 ? L < 64 || (L & (L - 1)) != 0 : L <= 150 && L % 32 != 0);
 }
 
 template <class T, bool TRAIN> int policy_any_layout(const MrfPolicyParams &P, int &counts, int &blocks, hipStream_t st)
 {
-    if (policy_tiles(P.L, (int)sizeof(T))) {
+    if (policy_tiles<TRAIN>(P.L, (int)sizeof(T))) {
+        // (log-probabilities alone: rows of one or two lanes)
 #define MRF_LAUNCH(TL, E) \
-        if (P.L <= TL * E) return policy_tile<T, TRAIN, TL, E>(P, counts, blocks, st);
+        if constexpr (TRAIN || TL <= 2) \
+            if (P.L <= TL * E) return policy_tile<T, TRAIN, TL, E>(P, counts, blocks, st);
         MRF_TILES(MRF_LAUNCH)
 #undef MRF_LAUNCH
     }
+    // (with the gradient, no row of 9 to 16 labels in 32 bits is left, and of 16-bit rows up to 256 only the powers of two)
 #define MRF_LAUNCH(TL, V, CH) \
-    if (P.L <= TL * V * CH) return policy_rows<T, TRAIN, TL, V, CH>(P, counts, blocks, st);
+    if constexpr (!TRAIN || !(sizeof(T) == 4 ? TL == 4 : TL <= 16 && CH == 3)) \
+        if (P.L <= TL * V * CH) return policy_rows<T, TRAIN, TL, V, CH>(P, counts, blocks, st);
     MRF_POLICY_FEW(MRF_LAUNCH)
     if constexpr (sizeof(T) == 4) {
         MRF_POLICY_FEW_32(MRF_LAUNCH)

@@ -122,6 +122,13 @@ def test_layer_norm_at_odd_addresses(N, C, shift, types):
     _check_norm(N, C, *types, shift=shift)
 
 
+@pytest.mark.parametrize("types", TYPE_PAIRS, ids="-".join)
+@pytest.mark.parametrize("C", [12, 20, 28, 36, 40, 44, 48, 52, 60, 68])
+def test_layer_norm_of_whole_chunks_that_leave_lanes_idle(C, types):
+    _check_norm(203, C, *types)
+    _check_norm(1, C, *types, shift=1)
+
+
 @pytest.mark.parametrize("N,C", [(40000, 21), (70001, 16), (9000, 192), (20003, 70), (3001, 1024), (1100, 2048)])
 def test_layer_norm_of_many_rows(N, C):
     """More rows than a launch has room for at once."""
@@ -241,6 +248,21 @@ def test_bucket_pairwise_matches_definition(G, Q, K, NB, dtype):
 @pytest.mark.parametrize("shape,shift", [((101, 21, 21, 16), 1), ((40, 32, 32, 8), 3), ((3, 260, 256, 32), 1), ((2, 64, 1024, 32), 5), ((7, 8, 8, 8), 2)])
 def test_bucket_pairwise_at_odd_addresses(shape, shift, dtype):
     _check_bucket(*shape, dtype, shift=shift, query_offset=-7, random_map=True)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("G,Q,K,NB", [(4097, 21, 21, 16), (4099, 5, 7, 3), (4100, 33, 31, 9), (4103, 56, 56, 8), (4500, 1, 1, 1), (4098, 3, 1, 2), (6000, 1, 100, 20),
+                                      (4097, 4, 256, 300), (4099, 32, 64, 1000), (4096, 16, 16, 1025), (600, 64, 64, 32), (513, 40, 64, 20), (512, 64, 40, 20),
+                                      (511, 33, 32, 600)])
+def test_bucket_pairwise_of_thousands_of_groups(G, Q, K, NB, dtype):
+    """On both sides of the numbers of groups at which the launches change."""
+    _check_bucket(G, Q, K, NB, dtype)
+    _check_bucket(G, Q, K, NB, dtype, heads_last=True, query_offset=3, spare=1, shift=1, random_map=True)
+
+
+def test_bucket_pairwise_of_many_nearly_largest_matrices():
+    _check_bucket(16385, 56, 56, 8, "float32")
+    _check_bucket(5001, 63, 63, 16, "float32", heads_last=True)
 
 
 @pytest.mark.parametrize("shape", [(70001, 9, 9, 8), (20011, 21, 21, 16), (3, 2048, 2048, 32), (9001, 64, 64, 40), (100003, 3, 4, 2)])
@@ -386,6 +408,13 @@ def test_policy_at_odd_addresses(N, L, shift, dtype):
     _check_policy(N, L, dtype, shift=shift, masked=True)
 
 
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("L", [4, 6, 9, 20, 28, 36, 40, 44, 48, 52, 60, 80, 100, 112, 148, 152, 160, 176, 224])
+def test_policy_of_labels_in_whole_chunks(L, dtype):
+    _check_policy(131, L, dtype, scale=128.0 if dtype == "float16" else 1.0)
+    _check_policy(67, L, dtype, shift=1, masked=True, barred=True, per=20)
+
+
 @pytest.mark.parametrize("N,L", [(70001, 21), (20000, 16), (40003, 70), (9001, 192), (2100, 1024), (600, 4099)])
 def test_policy_of_many_pixels(N, L):
     """More pixels than a launch has room for at once."""
@@ -436,6 +465,15 @@ def test_policy_pixels_without_labels_and_labels_that_are_barred(L):
     mrf.mrf_softmin_logp(cost, a, lp)
     np.testing.assert_allclose(_np(lp)[rows], wlp[rows], rtol=1e-5, atol=1e-5)
     assert lp[2] == -float("inf") and lp[4] == -float("inf")
+    # with a KL term the pixel whose own label is barred has an infinite k: the loss is infinite, the other pixels' gradients are as ever
+    ref = torch.full((N,), -2.0, device="cuda:0")
+    mrf.mrf_softmin_policy(cost, a, A, old, ref, None, 0.2, 0.2, 0.1, loss, logp, grad, ws)
+    assert loss[0] == float("inf") and loss[2] == float("inf") and torch.isfinite(loss[1])
+    allowed = c.copy()
+    allowed[4, 3] = 0.0
+    _, _, wgrad = lo.policy(allowed, a.cpu().numpy(), np.ones(N), old.cpu().numpy(), ref.cpu().numpy(), None, 0.2, 0.2, 0.1)
+    others = [0, 1, 2, 3, 5, 6, 7, 8]
+    np.testing.assert_allclose(_np(grad)[others], wgrad[others], rtol=1e-4, atol=1e-6)
     # nothing counts: no loss, no gradient
     mrf.mrf_softmin_policy(cost, a, A, old, None, torch.zeros(N, dtype=torch.uint8, device="cuda:0"), 0.2, 0.2, 0.0, loss, logp, grad, ws)
     assert (loss == 0).all() and (logp == 0).all() and (grad == 0).all()
@@ -443,6 +481,17 @@ def test_policy_pixels_without_labels_and_labels_that_are_barred(L):
     cost[1, L - 1] = float("nan")
     mrf.mrf_softmin_policy(cost, a, A, old, None, None, 0.2, 0.2, 0.0, loss, logp, grad, ws)
     assert grad[1].isnan().all() and torch.isfinite(grad[[0, 2, 3, 4, 5, 6, 7, 8]]).all()
+    # ... and reaches the loss, from the costs, an advantage or an old log-probability
+    assert loss[:2].isnan().all()
+    cost[1, L - 1] = 0.0
+    for given in (A, old):
+        kept = given.clone()
+        given[7] = float("nan")
+        mrf.mrf_softmin_policy(cost, a, A, old, None, None, 0.2, 0.2, 0.0, loss, logp, grad, ws)
+        assert loss[:2].isnan().all() and grad[7].isnan().all() and torch.isfinite(grad[[0, 1, 2, 3, 4, 5, 6, 8]]).all()
+        given.copy_(kept)
+    mrf.mrf_softmin_policy(cost, a, A, old, None, None, 0.2, 0.2, 0.0, loss, logp, grad, ws)
+    assert torch.isfinite(loss).all()
 
 
 def test_policy_without_pixels():

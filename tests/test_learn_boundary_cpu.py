@@ -16,6 +16,7 @@ def test_layer_norm_refusals():
         return lib.mrf_layer_norm_forward(N, C, x, xt, None, None, eps, y, yt, None, None, None)
 
     assert forward(N=-1) == -2 and forward(C=0) == -2 and forward(N=1 << 31) == -2 and forward(C=-3) == -2
+    assert forward(C=0x7fff0001) == -2 and mrf.mrf_layer_norm_workspace_bytes(1, 0x7fff0001) == 0 < mrf.mrf_layer_norm_workspace_bytes(1, 0x7fff0000)
     assert forward(xt=3) == -12 and forward(xt=-1) == -12 and forward(yt=1) == -12 and forward(xt=1, yt=2) == -12 and forward(yt=9) == -12
     for eps in (0.0, -1e-5, INF, NAN):
         assert forward(eps=eps) == -12
@@ -42,6 +43,7 @@ def test_bucket_pairwise_refusals():
 
     assert forward(G=-1) == -2 and forward(Q=-1) == -2 and forward(K=-1) == -2 and forward(NB=0) == -2 and forward(NB=65537) == -2
     assert forward(G=1 << 31) == -2 and forward(G=(1 << 31) - 1, Q=1 << 20, K=1 << 20) == -2 and forward(Q=1 << 30, K=1 << 30) == -2
+    assert forward(Q=1, K=0x7fff0000) == -2 and forward(Q=0x7fff0000, K=1) == -2
     assert forward(t=3) == -12
     assert forward(table=None) == -1 and forward(m=None) == -1 and forward(out=None) == -1
     # the map holds the offsets -2..4: one less at either side, or moved queries, and it does not
@@ -76,6 +78,7 @@ def test_policy_refusals():
         return lib.mrf_softmin_logp(N, L, c, t, a, lb, out, None)
 
     assert logp(N=-1) == -2 and logp(N=1 << 31) == -2 and logp(L=0) == -3 and logp(L=257) == -3 and logp(L=0, lb=4) == -3
+    assert logp(L=0x7fff0001, lb=4) == -3
     assert logp(lb=2) == -12 and logp(lb=8) == -12 and logp(t=3) == -12
     assert logp(c=None) == -1 and logp(a=None) == -1 and logp(out=None) == -1 and logp(N=0, c=None, a=None, out=None) == 0
 
