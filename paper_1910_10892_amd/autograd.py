@@ -12,6 +12,7 @@ mrf_trwp_backward (Alg. 3 / 4).  No arithmetic of the method happens here.
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import mrfmp as _m
 
@@ -138,6 +139,7 @@ class _LayerNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_y):
         x, weight, mean, rstd = ctx.saved_tensors
         need_x, need_w, need_b = ctx.needs_input_grad[:3]
@@ -172,6 +174,7 @@ class _BucketPairwise(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_out):
         (bucket_of,) = ctx.saved_tensors
         first_offset, Q, K, query_offset, heads_last, dtype = ctx.cfg
@@ -209,6 +212,7 @@ class _PolicyLoss(torch.autograd.Function):
         return total, terms, logp
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_total, _grad_terms, _grad_logp):
         # (the gradient came with the loss, in one reading of the costs)
         return (ctx.grad * (grad_total / ctx.scale)).to(ctx.grad.dtype), None, None, None, None, None, None

@@ -404,6 +404,13 @@ def _same_size(what, t, *shape):
         raise ValueError("%s has shape %s, expected %s" % (what, tuple(t.shape), shape))
 
 
+def _size(n) -> int:
+    # (an argument that does not fit its 32 bits would lose the others on the way to the library)
+    if n > 0x7fffffff:
+        raise ValueError("sizes of the last indices are at most 2^31 - 1, got %d" % n)
+    return int(n)
+
+
 def _checked(rc, name):
     if rc != 0:
         raise MrfError(rc, name)
@@ -416,7 +423,7 @@ def mrf_layer_norm_workspace_bytes(n_rows: int, C: int) -> int:
 def mrf_layer_norm_forward(x, gamma, beta, eps, y, mean, rstd, stream=None):
     """x [..., C] float32, float16 or bfloat16, gamma and beta [C] float32 or None, y like x (or float32), mean and rstd
     [...] float32 or None."""
-    C, rows = int(x.shape[-1]), tuple(x.shape[:-1])
+    C, rows = _size(x.shape[-1]), tuple(x.shape[:-1])
     _same_size("y", y, *x.shape)
     for name, t in (("gamma", gamma), ("beta", beta)):
         _same_size(name, t, C)
@@ -431,7 +438,7 @@ def mrf_layer_norm_forward(x, gamma, beta, eps, y, mean, rstd, stream=None):
 def mrf_layer_norm_backward(grad_y, x, gamma, mean, rstd, grad_x, grad_gamma, grad_beta, workspace, stream=None):
     """grad_y [..., C] of y's type, x, gamma, mean, rstd of the forward call; grad_x like x, grad_gamma and grad_beta [C] float32,
     each of the three or None."""
-    C, rows = int(x.shape[-1]), tuple(x.shape[:-1])
+    C, rows = _size(x.shape[-1]), tuple(x.shape[:-1])
     _same_size("grad_y", grad_y, *x.shape)
     _same_size("grad_x", grad_x, *x.shape)
     for name, t in (("gamma", gamma), ("grad_gamma", grad_gamma), ("grad_beta", grad_beta)):
@@ -461,9 +468,9 @@ def mrf_bucket_pairwise_workspace_bytes(n_groups: int, Q: int, K: int, n_buckets
 def _bucket_sizes(table, out, heads_last):
     """Groups, rows, columns and buckets of a table [..., n_buckets] (heads_last: [n_buckets, ...]) and a matrix [..., Q, K]."""
     groups = tuple(out.shape[:-2])
-    NB = int(table.shape[0] if heads_last else table.shape[-1])
+    NB = _size(table.shape[0] if heads_last else table.shape[-1])
     _same_size("table", table, *((NB, *groups) if heads_last else (*groups, NB)))
-    return math.prod(groups), int(out.shape[-2]), int(out.shape[-1]), NB
+    return math.prod(groups), _size(out.shape[-2]), _size(out.shape[-1]), NB
 
 
 def mrf_bucket_pairwise_forward(table, bucket_of, first_offset, out, query_offset=0, heads_last=False, stream=None):
@@ -494,7 +501,7 @@ def _label_bytes(labels) -> int:
 
 def mrf_softmin_logp(cost, labels, logp, stream=None):
     """cost [..., L] float32, float16 or bfloat16, labels [...] uint8 (L <= 256) or int32, logp [...] float32."""
-    pixels, L = tuple(cost.shape[:-1]), int(cost.shape[-1])
+    pixels, L = tuple(cost.shape[:-1]), _size(cost.shape[-1])
     _same_size("labels", labels, *pixels)
     _same_size("logp", logp, *pixels)
     _checked(load_library().mrf_softmin_logp(math.prod(pixels), L, _ptr(cost, None), _type_of(cost, "cost"), _ptr(labels, None),
@@ -510,7 +517,7 @@ def mrf_softmin_policy(cost, labels, advantage, old_logp, ref_logp, mask, clip_l
     """cost [..., L] float32, float16 or bfloat16, labels [...] uint8 or int32, advantage float32 with an entry per
     pixels_per_advantage pixels, old_logp and ref_logp [...] float32 or None, mask [...] uint8 or None, loss [3] float32, logp
     [...] float32 or None, grad_cost like cost or None."""
-    pixels, L = tuple(cost.shape[:-1]), int(cost.shape[-1])
+    pixels, L = tuple(cost.shape[:-1]), _size(cost.shape[-1])
     n, per = math.prod(pixels), int(pixels_per_advantage)
     for name, t in (("labels", labels), ("old_logp", old_logp), ("ref_logp", ref_logp), ("mask", mask), ("logp", logp)):
         _same_size(name, t, *pixels)

@@ -148,3 +148,20 @@ def test_the_example_learns_from_rewards():
     assert np.isfinite(loss) and rewards[-1] > rewards[0] + 0.1
     # labels apart cost more than equal ones
     assert float(values[1:].mean()) > float(values[0])
+
+
+def test_second_derivatives_are_refused():
+    """The gradients come from the library: a derivative of them is an error, not a part of it."""
+    import torch
+    from paper_1910_10892_amd.autograd import bucket_pairwise, layer_norm, policy_loss
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(3)
+    x = torch.randn((6, 5), generator=gen, device="cuda:0", requires_grad=True)
+    bucket_of = torch.zeros(9, dtype=torch.int32, device="cuda:0")
+    labels = torch.zeros(6, dtype=torch.uint8, device="cuda:0")
+    scale = torch.ones((), device="cuda:0", requires_grad=True)
+    for out in (layer_norm(x).square().sum(), bucket_pairwise(x, bucket_of, -4, 5, 5).square().sum(),
+                scale * policy_loss(x, labels, torch.ones(6, device="cuda:0"))[0]):
+        (grad,) = torch.autograd.grad(out, x, create_graph=True)
+        with pytest.raises(RuntimeError):
+            grad.sum().backward()

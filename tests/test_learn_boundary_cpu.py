@@ -98,3 +98,25 @@ def test_policy_refusals():
     assert policy(c=None) == -1 and policy(a=None) == -1 and policy(A=None) == -1 and policy(loss=None) == -1 and policy(ws=None) == -1
     assert policy(size=need - 1) == -6
     assert "learning operator" in mrf.mrf_strerror(-12)
+
+
+def test_binding_refuses_sizes_beyond_32_bits():
+    """The library's row lengths are 32-bit arguments: a longer one is refused, not cut off."""
+    import torch
+
+    def empty(*shape, dtype=torch.float32):
+        return torch.empty(shape, dtype=dtype, device="meta")
+
+    n = (1 << 32) + 8
+    with pytest.raises(ValueError, match="at most"):
+        mrf.mrf_layer_norm_forward(empty(1, n), None, None, 1e-5, empty(1, n), None, None)
+    with pytest.raises(ValueError, match="at most"):
+        mrf.mrf_layer_norm_backward(empty(1, n), empty(1, n), None, empty(1), empty(1), empty(1, n), None, None, None)
+    with pytest.raises(ValueError, match="at most"):
+        mrf.mrf_bucket_pairwise_forward(empty(1, 4), empty(8, dtype=torch.int32), 0, empty(1, n, 2))
+    with pytest.raises(ValueError, match="at most"):
+        mrf.mrf_bucket_pairwise_backward(empty(1, 2, n), empty(8, dtype=torch.int32), 0, empty(1, 4), None)
+    with pytest.raises(ValueError, match="at most"):
+        mrf.mrf_softmin_logp(empty(1, n), empty(1, dtype=torch.int32), empty(1))
+    with pytest.raises(ValueError, match="at most"):
+        mrf.mrf_softmin_policy(empty(1, n), empty(1, dtype=torch.int32), empty(1), None, None, None, 0.2, 0.2, 0.0, empty(3), None, None, None)
