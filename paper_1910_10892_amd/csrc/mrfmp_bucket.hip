@@ -424,30 +424,30 @@ __global__ void __launch_bounds__(256) mrf_bucket_bwd_diagonals(const MrfBucketP
 }
 
 // A workgroup per bucket and group: the diagonals of that bucket, four of a thread's looked up at once.
-constexpr int MRF_BUCKET_SUM = 1024;
-__global__ void __launch_bounds__(MRF_BUCKET_SUM) mrf_bucket_bwd_sum(const MrfBucketParams P)
+template <int NT>
+__global__ void __launch_bounds__(NT) mrf_bucket_bwd_sum(const MrfBucketParams P)
 {
-    __shared__ float waves[MRF_BUCKET_SUM / 64];
+    __shared__ float waves[NT / 64];
     const int D = P.T > 0 ? P.Q + P.K - 1 : 0, b = blockIdx.x;
     for (long long g = blockIdx.y; g < P.G; g += gridDim.y) {
         float s = 0.0f;
-        for (int first = threadIdx.x; first < D; first += 4 * MRF_BUCKET_SUM) {
+        for (int first = threadIdx.x; first < D; first += 4 * NT) {
             int bucket[4];
             float total[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int d = first + u * MRF_BUCKET_SUM;
+                const int d = first + u * NT;
                 bucket[u] = P.bucket_of[d < D ? d : D - 1];
                 total[u] = P.totals[g * D + (d < D ? d : D - 1)];
             }
 #pragma unroll
-            for (int u = 0; u < 4; ++u) s += first + u * MRF_BUCKET_SUM < D && mrf_bucket_clamped(bucket[u], P.NB) == b ? total[u] : 0.0f;
+            for (int u = 0; u < 4; ++u) s += first + u * NT < D && mrf_bucket_clamped(bucket[u], P.NB) == b ? total[u] : 0.0f;
         }
         s = mrf_lanes_sum<64>(s);
         if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = s;
         __syncthreads();
         if (threadIdx.x < 64) {
-            s = mrf_lanes_sum<16>(threadIdx.x < MRF_BUCKET_SUM / 64 ? waves[threadIdx.x] : 0.0f);
+            s = mrf_lanes_sum<NT / 64>(threadIdx.x < NT / 64 ? waves[threadIdx.x] : 0.0f);
             if (threadIdx.x == 0) P.dtable[g * P.sg + b * P.sb] = s;
         }
         __syncthreads();
@@ -551,9 +551,13 @@ template <class T> int bucket_forward(MrfBucketParams P, hipStream_t st)
     return launch_status("mrf_bucket_fwd_long");
 }
 
+// 1,024 threads for a bucket, 256 where there are more than 1,024 buckets in all and starting so many large workgroups takes longest (backward calls, 64
+// groups of 300 x 300 and 64 buckets 25.7 / 19.8 us, 23 of 29 x 4,702 18.3 / 16.8; 4 of 300 x 600 and 16 buckets 14.0 / 15.2).
 int bucket_sum(const MrfBucketParams &P, hipStream_t st)
 {
-    hipLaunchKernelGGL(mrf_bucket_bwd_sum, dim3((unsigned)P.NB, (unsigned)(P.G < 65535 ? P.G : 65535)), dim3(MRF_BUCKET_SUM), 0, st, P);
+    const dim3 grid((unsigned)P.NB, (unsigned)(P.G < 65535 ? P.G : 65535));
+    if (P.G * P.NB > 1024) hipLaunchKernelGGL(mrf_bucket_bwd_sum<256>, grid, dim3(256), 0, st, P);
+    else hipLaunchKernelGGL(mrf_bucket_bwd_sum<1024>, grid, dim3(1024), 0, st, P);
     return launch_status("mrf_bucket_bwd_sum");
 }
 

@@ -253,7 +253,7 @@ def test_bucket_pairwise_at_odd_addresses(shape, shift, dtype):
 @pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
 @pytest.mark.parametrize("G,Q,K,NB", [(4097, 21, 21, 16), (4099, 5, 7, 3), (4100, 33, 31, 9), (4103, 56, 56, 8), (4500, 1, 1, 1), (4098, 3, 1, 2), (6000, 1, 100, 20),
                                       (4097, 4, 256, 300), (4099, 32, 64, 1000), (4096, 16, 16, 1025), (600, 64, 64, 32), (513, 40, 64, 20), (512, 64, 40, 20),
-                                      (511, 33, 32, 600)])
+                                      (511, 33, 32, 600), (40, 70, 300, 64), (3, 300, 260, 700)])
 def test_bucket_pairwise_of_thousands_of_groups(G, Q, K, NB, dtype):
     """On both sides of the numbers of groups at which the launches change."""
     _check_bucket(G, Q, K, NB, dtype)
