@@ -544,6 +544,136 @@ def test_gradients_of_the_kernels_are_differences_of_the_definitions():
         assert float((_np(grad) * v).sum()) == pytest.approx((f(c + h * v) - f(c - h * v)) / (2 * h), rel=1e-4, abs=1e-5)
 
 
+# ---- more than 2^32 entries: a block of rows (groups, pixels) repeated, so that every block has to come out like one alone
+
+def _repeated(block, k):
+    torch = _torch()
+    out = torch.empty((k, *block.shape), dtype=block.dtype, device="cuda:0")
+    out.copy_(block.expand(k, *block.shape))
+    return out
+
+
+def _blocks_alike(many, block):
+    torch = _torch()
+    for i in (0, len(many) // 2, len(many) - 2, len(many) - 1):
+        assert torch.equal(many[i], block), i
+
+
+@pytest.fixture
+def _memory_back():
+    yield
+    _torch().cuda.empty_cache()
+
+
+@pytest.mark.parametrize("M,C", [(1000003, 21), (100003, 208), (7001, 2050)])
+def test_layer_norm_beyond_32_bit_offsets(M, C, _memory_back):
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    k = (1 << 32) // (M * C) + 2
+    print("case norm", k * M, C, flush=True)
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(C)
+    x = torch.randn((M, C), generator=gen, device="cuda:0").to(torch.bfloat16)
+    dy = torch.randn((M, C), generator=gen, device="cuda:0").to(torch.bfloat16)
+    gamma = torch.rand(C, generator=gen, device="cuda:0") + 0.5
+
+    def both(x, dy):
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        mean, rstd = torch.empty(x.shape[:-1], device="cuda:0"), torch.empty(x.shape[:-1], device="cuda:0")
+        gg, gb = torch.empty(C, device="cuda:0"), torch.empty(C, device="cuda:0")
+        ws = torch.empty(mrf.mrf_layer_norm_workspace_bytes(mean.numel(), C), dtype=torch.uint8, device="cuda:0")
+        mrf.mrf_layer_norm_forward(x, gamma, None, 1e-5, y, mean, rstd)
+        mrf.mrf_layer_norm_backward(dy, x, gamma, mean, rstd, dx, gg, gb, ws)
+        return y, dx, mean, rstd, gg, gb
+
+    one = both(x, dy)
+    many = both(_repeated(x, k), _repeated(dy, k))
+    for a, b in zip(many[:4], one[:4]):
+        _blocks_alike(a, b)
+    # sums over rows: at most k M rows one after the other over 256 workgroups (the least), then the workgroups'
+    h = (x.double() - one[2].double()[:, None]) * one[3].double()[:, None]
+    size = [(dy.double() * h).abs().sum(0), dy.double().abs().sum(0)]
+    for a, b, s in zip(many[4:], one[4:], size):
+        bound = (k * M / 256 + 512) * U * k * s
+        assert ((a.double() - k * b.double()).abs() <= bound).all()
+
+
+def test_bucket_pairwise_beyond_32_bit_offsets_many_matrices(_memory_back):
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    M, Q, NB = 100003, 21, 16
+    k = (1 << 32) // (M * Q * Q) + 2
+    print("case bucket", k * M, Q, flush=True)
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(1)
+    m = torch.from_numpy(mrf.mrf_distance_buckets(NB, 20, -(Q - 1), 2 * Q - 1)).cuda()
+    table = torch.randn((M, NB), generator=gen, device="cuda:0")
+    dout = torch.randn((M, Q, Q), generator=gen, device="cuda:0").to(torch.bfloat16)
+
+    def both(table, dout):
+        out, grad = torch.empty_like(dout), torch.empty_like(table)
+        ws = torch.empty(mrf.mrf_bucket_pairwise_workspace_bytes(table.numel() // NB, Q, Q, NB), dtype=torch.uint8, device="cuda:0")
+        mrf.mrf_bucket_pairwise_forward(table, m, -(Q - 1), out)
+        mrf.mrf_bucket_pairwise_backward(dout, m, -(Q - 1), grad, ws)
+        return out, grad
+
+    one, many = both(table, dout), both(_repeated(table, k), _repeated(dout, k))
+    for a, b in zip(many, one):
+        _blocks_alike(a, b)
+
+
+def test_bucket_pairwise_beyond_32_bit_offsets_one_matrix(_memory_back):
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    L, NB = 66001, 32
+    print("case bucket", 1, L, flush=True)
+    host = mrf.mrf_distance_buckets(NB, 40000, -(L - 1), 2 * L - 1)
+    m = torch.from_numpy(host).cuda()
+    table = torch.arange(NB, dtype=torch.float32, device="cuda:0")[None]
+    out = torch.empty((1, L, L), dtype=torch.bfloat16, device="cuda:0")
+    mrf.mrf_bucket_pairwise_forward(table, m, -(L - 1), out)
+    rows = [0, 31000, 65074, 65075, 65076, L - 1]      # (row 65,075 holds entry 2^32)
+    for q in rows:
+        want = table[0].index_select(0, m[L - 1 - q:2 * L - 1 - q].long()).to(torch.bfloat16)
+        assert torch.equal(out[0, q], want), q
+    out.zero_()
+    for q in rows:
+        out[0, q] = 1.0
+    grad = torch.empty_like(table)
+    ws = torch.empty(mrf.mrf_bucket_pairwise_workspace_bytes(1, L, L, NB), dtype=torch.uint8, device="cuda:0")
+    mrf.mrf_bucket_pairwise_backward(out, m, -(L - 1), grad, ws)
+    # (sums of ones below 2^24: exact)
+    want = sum(np.bincount(host[L - 1 - q:2 * L - 1 - q], minlength=NB) for q in rows)
+    np.testing.assert_array_equal(grad.cpu().numpy()[0], want)
+
+
+@pytest.mark.parametrize("M,L", [(1000003, 21), (130001, 128), (2003, 9000), (301, 40001)])
+def test_policy_beyond_32_bit_offsets(M, L, _memory_back):
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    k = (1 << 32) // (M * L) + 2
+    print("case policy", k * M, L, flush=True)
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(L)
+    cost = torch.randn((M, L), generator=gen, device="cuda:0").to(torch.bfloat16)
+    labels = torch.randint(0, L, (M,), generator=gen, device="cuda:0", dtype=torch.int32)
+    A = torch.randn(M, generator=gen, device="cuda:0")
+    ws = torch.empty(mrf.mrf_softmin_policy_workspace_bytes(), dtype=torch.uint8, device="cuda:0")
+
+    def both(cost, labels, A):
+        loss, logp, grad, alone = torch.empty(3, device="cuda:0"), torch.empty_like(A), torch.empty_like(cost), torch.empty_like(A)
+        # (scaled by the number of pixels: 1 / n cancels exactly)
+        mrf.mrf_softmin_policy(cost, labels, A, None, None, None, 0.2, 0.2, 0.0, loss, logp, grad, ws, grad_scale=float(np.float32(A.numel())))
+        mrf.mrf_softmin_logp(cost, labels, alone)
+        return loss, logp, grad, alone
+
+    one, many = both(cost, labels, A), both(_repeated(cost, k), _repeated(labels, k), _repeated(A, k))
+    for a, b in zip(many[1:], one[1:]):
+        _blocks_alike(a, b)
+    # the mean over k times the same pixels, in 64 bits, rounded once
+    assert abs(float(many[0][0]) - float(one[0][0])) <= 4 * U * float(A.abs().mean())
+
+
 # ---- streams, graphs, refusals
 
 def test_learning_operators_replayed_from_a_graph_on_a_stream_of_its_own():
