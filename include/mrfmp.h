@@ -332,6 +332,15 @@ int mrf_softmin_policy(int64_t n_pixels, int32_t L, const void *cost, int cost_t
                        const uint8_t *mask, float clip_low, float clip_high, float kl_weight, float grad_scale, float *loss, float *logp,
                        void *grad_cost, void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* The gradient alone, of a loss that something else is made from: grad_cost(lambda) = grad_loss[0] d loss / d c(lambda), in 32 bits up
+ * to the one rounding to cost_type, so that a loss scaler's factor keeps MRF_F16 gradients in range.  Arguments as above;
+ *   grad_loss   DEVICE [1] float: the gradient of what is made from the loss with respect to the loss
+ *   grad_cost   DEVICE [n_pixels][L] of cost_type, assigned */
+int mrf_softmin_policy_backward(int64_t n_pixels, int32_t L, const void *cost, int cost_type, const void *labels, int label_bytes,
+                                const float *advantage, int64_t pixels_per_advantage, const float *old_logp, const float *ref_logp,
+                                const uint8_t *mask, float clip_low, float clip_high, float kl_weight, const float *grad_loss, void *grad_cost,
+                                void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* Some sweep layouts spread a scanline over several wavefronts that hand nodes to each other
  * through rings in on-chip memory.  A wavefront that still finds itself waiting for another four
  * seconds after its workgroup started (sweeps take milliseconds) ends at once, those that wait for it

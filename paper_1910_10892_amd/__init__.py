@@ -11,6 +11,6 @@ from .mrfmp import (  # noqa: F401
     mrf_energy, mrf_energy_noalloc, mrf_energy_workspace_bytes, mrf_softmin_l1, mrf_softmin_smooth_l1, mrf_softmin_l1_workspace_bytes,
     MRF_BF16, MRF_F16, MRF_F32, mrf_bucket_pairwise_backward, mrf_bucket_pairwise_forward, mrf_bucket_pairwise_workspace_bytes,
     mrf_distance_buckets, mrf_layer_norm_backward, mrf_layer_norm_forward, mrf_layer_norm_workspace_bytes,
-    mrf_softmin_logp, mrf_softmin_policy, mrf_softmin_policy_workspace_bytes,
+    mrf_softmin_logp, mrf_softmin_policy, mrf_softmin_policy_backward, mrf_softmin_policy_workspace_bytes,
     mrf_trwp_backward, mrf_trwp_forward, mrf_tune, mrf_workspace_fault, mrf_validate, mrf_version, mrf_workspace_bytes,
 )

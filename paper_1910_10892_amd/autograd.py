@@ -202,11 +202,12 @@ class _PolicyLoss(torch.autograd.Function):
         dev = cost.device
         loss = torch.empty((3,), dtype=torch.float32, device=dev)
         logp = torch.empty(cost.shape[:-1], dtype=torch.float32, device=dev)
-        grad = torch.empty_like(cost) if ctx.needs_input_grad[0] else None
         ws = torch.empty(_m.mrf_softmin_policy_workspace_bytes(), dtype=torch.uint8, device=dev)
-        _m.mrf_softmin_policy(cost, labels, advantage, old_logp, ref_logp, mask, clip_low, clip_high, kl_weight, loss, logp, grad, ws,
+        _m.mrf_softmin_policy(cost, labels, advantage, old_logp, ref_logp, mask, clip_low, clip_high, kl_weight, loss, logp, None, ws,
                               pixels_per_advantage=per, grad_scale=scale)
-        ctx.grad, ctx.scale = grad, scale
+        ctx.save_for_backward(cost, labels, advantage, old_logp, ref_logp, mask)
+        ctx.given = labels.numel(), cost.shape[-1], per, _m._type_of(cost, "cost"), _m._label_bytes(labels), clip_low, clip_high, kl_weight
+        ctx.ws = ws
         total, terms = loss[0].clone(), loss[1:]
         ctx.mark_non_differentiable(terms, logp)
         return total, terms, logp
@@ -214,16 +215,21 @@ class _PolicyLoss(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, grad_total, _grad_terms, _grad_logp):
-        # (the gradient came with the loss, in one reading of the costs)
-        return (ctx.grad * (grad_total / ctx.scale)).to(ctx.grad.dtype), None, None, None, None, None, None
+        # (the gradient is not made with the loss: what comes from above is multiplied in before its entries are rounded to 16 bits)
+        cost, labels, advantage, old_logp, ref_logp, mask = ctx.saved_tensors
+        grad = torch.empty_like(cost)
+        # (the forward call has checked all but the gradients; checks here cost more than the launch)
+        _m._policy_backward(ctx.given, cost, labels, advantage, old_logp, ref_logp, mask, grad_total.float(), grad, ctx.ws)
+        return grad, None, None, None, None, None, None
 
 
 def policy_loss(cost, labels, advantage, old_logp=None, ref_logp=None, mask=None, *, clip_low=0.2, clip_high=0.2, kl_weight=0.0,
                 pixels_per_advantage=1, grad_scale=1.0):
     """Clipped policy loss of labels [...] (uint8 or int32) under the SoftMin of cost [..., L], as
     mrf_softmin_policy states it: (loss, terms, logp) with terms = [first term, mean k] and logp [...]
-    the labels' log-probabilities.  The gradient flows from loss to cost; grad_scale keeps a float16
-    gradient in range on the way (it is divided out again)."""
+    the labels' log-probabilities.  The gradient flows from loss to cost: it is formed in 32 bits, times what comes
+    from above, and rounded once to cost's type (a loss scaler keeps float16 gradients in range).  grad_scale is the
+    library's factor on the gradient of a call that knows no other; it changes nothing here."""
     return _PolicyLoss.apply(cost, labels, advantage, old_logp, ref_logp, mask,
                              (float(clip_low), float(clip_high), float(kl_weight), int(pixels_per_advantage), float(grad_scale)))
 

@@ -20,6 +20,7 @@ struct MrfPolicyParams {
     const uint8_t *mask;
     float low, high;             // bounds of the ratio
     float kl, scale;             // weight of the KL term, factor on the gradient
+    const float *upstream;       // another one, in device memory (NULL: 1)
     float *loss, *logp;
     void *dcost;
     long long *counts;           // [MRF_POLICY_COUNTS] counted pixels of a workgroup's share of the mask
@@ -158,10 +159,15 @@ __device__ inline void mrf_policy_loss(const MrfPolicyParams &P, double gain, do
     P.loss[2] = (float)div;
 }
 
-// what a wavefront's rows add to the two sums ends as one partial sum per workgroup, or as the loss where there is only one
+// factor on the slopes of the pixels
+__device__ inline float mrf_policy_factor(const MrfPolicyParams &P, long long n) { return P.scale * (P.upstream ? *P.upstream : 1.0f) / (float)n; }
+
+// what a wavefront's rows add to the two sums ends as one partial sum per workgroup, or as the loss where there is only one (nothing where
+// the gradient alone is asked for)
 __device__ inline void mrf_policy_partial(const MrfPolicyParams &P, double gain, double div, long long n)
 {
     __shared__ double sums[2][16];
+    if (!P.loss) return;
     gain = mrf_wave_sum_f64(gain);
     div = mrf_wave_sum_f64(div);
     if ((threadIdx.x & 63) == 0) {
@@ -226,7 +232,7 @@ __global__ void __launch_bounds__(mrf_policy_threads(TL)) mrf_policy_rows(const 
     const int l = threadIdx.x % TL, L = P.L;
     const unsigned group = threadIdx.x / TL, mine = group * (unsigned)L;
     const long long counted = TRAIN ? mrf_policy_counted(P, count_blocks) : 1;
-    const float inv_n = P.scale / (float)counted;
+    const float inv_n = TRAIN ? mrf_policy_factor(P, counted) : 0.0f;
     double total_gain = 0.0, total_div = 0.0;
     const long long step = (long long)gridDim.x * G;
 
@@ -332,7 +338,7 @@ __global__ void __launch_bounds__(256) mrf_policy_tile(const MrfPolicyParams P, 
     __shared__ __align__(16) char lds[4][Tile::BYTES];
     const int wv = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, l = lane % TL, g = lane / TL, L = P.L;
     const long long counted = TRAIN ? mrf_policy_counted(P, count_blocks) : 1;
-    const float inv_n = P.scale / (float)counted;
+    const float inv_n = TRAIN ? mrf_policy_factor(P, counted) : 0.0f;
     double total_gain = 0.0, total_div = 0.0;
     T *mine = (T *)lds[wv];
     const long long step = (long long)gridDim.x * 4 * Tile::ROWS;
@@ -390,7 +396,7 @@ __global__ void __launch_bounds__(1024) mrf_policy_any(const MrfPolicyParams P, 
     __shared__ float scratch[2][16];
     const int t = threadIdx.x, L = P.L, whole = L / V * V;      // (chunks of V labels, and the labels behind them)
     const long long counted = TRAIN ? mrf_policy_counted(P, count_blocks) : 1;
-    const float inv_n = P.scale / (float)counted;
+    const float inv_n = TRAIN ? mrf_policy_factor(P, counted) : 0.0f;
     double total_gain = 0.0, total_div = 0.0;
     for (long long i = blockIdx.x; i < P.N; i += gridDim.x) {
         const T *c = (const T *)P.cost + (size_t)i * L;
@@ -602,9 +608,35 @@ template <class T> int policy_launch(const MrfPolicyParams &P, hipStream_t st)
 {
     int counts = 0, blocks = 0;
     const int rc = policy_any_layout<T, true>(P, counts, blocks, st);
-    if (rc != MRF_OK || blocks == 1) return rc;
+    if (rc != MRF_OK || blocks == 1 || !P.loss) return rc;
     hipLaunchKernelGGL(mrf_policy_sum, dim3(1), dim3(1024), 0, st, P, blocks, counts);
     return launch_status("mrf_policy_sum");
+}
+
+int policy_of_type(const MrfPolicyParams &P, int cost_type, hipStream_t st)
+{
+    if (cost_type == MRF_F32) return policy_launch<float>(P, st);
+    return cost_type == MRF_F16 ? policy_launch<mrf_f16>(P, st) : policy_launch<mrf_bf16>(P, st);
+}
+
+// Checks of the loss and its gradient, and the parameters that follow from the arguments; `required`: what else must not be NULL.
+int policy_arguments(MrfPolicyParams &P, int cost_type, int64_t per, float clip_low, float clip_high, void *workspace, size_t workspace_bytes,
+                     const void *required)
+{
+    const int rc = policy_check(P.N, P.L, cost_type, P.label_bytes);
+    if (rc != MRF_OK) return rc;
+    if (per < 1 || !(clip_low >= 0.0f) || !(clip_low < 1.0f) || !(clip_high >= 0.0f) || !(clip_high < INFINITY) || !(P.kl >= 0.0f) ||
+        !(P.kl < INFINITY) || !(fabsf(P.scale) < INFINITY))
+        return MRF_ERR_BAD_ARGUMENT;
+    if (!required || !workspace || (P.N > 0 && (!P.cost || !P.labels || !P.advantage)) || (P.kl > 0.0f && P.N > 0 && !P.ref_logp))
+        return MRF_ERR_NULL_POINTER;
+    if (workspace_bytes < mrf_softmin_policy_workspace_bytes()) return MRF_ERR_WORKSPACE_TOO_SMALL;
+    P.per = (unsigned)(per < P.N ? per : (P.N > 0 ? P.N : 1));
+    P.low = 1.0f - clip_low;
+    P.high = 1.0f + clip_high;
+    P.counts = (long long *)workspace;
+    P.partial = (double *)((char *)workspace + sizeof(long long) * MRF_POLICY_COUNTS);
+    return MRF_OK;
 }
 
 }  // namespace
@@ -635,28 +667,32 @@ int mrf_softmin_policy(int64_t n_pixels, int32_t L, const void *cost, int cost_t
                        const uint8_t *mask, float clip_low, float clip_high, float kl_weight, float grad_scale, float *loss, float *logp,
                        void *grad_cost, void *workspace, size_t workspace_bytes, void *hip_stream)
 {
-    const int rc = policy_check(n_pixels, L, cost_type, label_bytes);
-    if (rc != MRF_OK) return rc;
-    if (pixels_per_advantage < 1 || !(clip_low >= 0.0f) || !(clip_low < 1.0f) || !(clip_high >= 0.0f) || !(clip_high < INFINITY) ||
-        !(kl_weight >= 0.0f) || !(kl_weight < INFINITY) || !(fabsf(grad_scale) < INFINITY))
-        return MRF_ERR_BAD_ARGUMENT;
-    if (!loss || !workspace || (n_pixels > 0 && (!cost || !labels || !advantage)) || (kl_weight > 0.0f && n_pixels > 0 && !ref_logp))
-        return MRF_ERR_NULL_POINTER;
-    if (workspace_bytes < mrf_softmin_policy_workspace_bytes()) return MRF_ERR_WORKSPACE_TOO_SMALL;
     MrfPolicyParams P = {};
-    P.N = n_pixels; P.L = L; P.cost = cost; P.labels = labels; P.label_bytes = label_bytes; P.advantage = advantage;
-    P.per = (unsigned)(pixels_per_advantage < n_pixels ? pixels_per_advantage : (n_pixels > 0 ? n_pixels : 1)); P.old_logp = old_logp; P.ref_logp = ref_logp; P.mask = mask; P.low = 1.0f - clip_low;
-    P.high = 1.0f + clip_high; P.kl = kl_weight; P.scale = grad_scale; P.loss = loss; P.logp = logp; P.dcost = grad_cost;
-    P.counts = (long long *)workspace;
-    P.partial = (double *)((char *)workspace + sizeof(long long) * MRF_POLICY_COUNTS);
+    P.N = n_pixels; P.L = L; P.cost = cost; P.labels = labels; P.label_bytes = label_bytes; P.advantage = advantage; P.old_logp = old_logp;
+    P.ref_logp = ref_logp; P.mask = mask; P.kl = kl_weight; P.scale = grad_scale; P.loss = loss; P.logp = logp; P.dcost = grad_cost;
+    const int rc = policy_arguments(P, cost_type, pixels_per_advantage, clip_low, clip_high, workspace, workspace_bytes, loss);
+    if (rc != MRF_OK) return rc;
     hipStream_t st = (hipStream_t)hip_stream;
     if (n_pixels == 0) {
         P.mask = nullptr;
         hipLaunchKernelGGL(mrf_policy_sum, dim3(1), dim3(1024), 0, st, P, 0, 0);
         return launch_status("mrf_policy_sum");
     }
-    if (cost_type == MRF_F32) return policy_launch<float>(P, st);
-    return cost_type == MRF_F16 ? policy_launch<mrf_f16>(P, st) : policy_launch<mrf_bf16>(P, st);
+    return policy_of_type(P, cost_type, st);
+}
+
+int mrf_softmin_policy_backward(int64_t n_pixels, int32_t L, const void *cost, int cost_type, const void *labels, int label_bytes,
+                                const float *advantage, int64_t pixels_per_advantage, const float *old_logp, const float *ref_logp,
+                                const uint8_t *mask, float clip_low, float clip_high, float kl_weight, const float *grad_loss, void *grad_cost,
+                                void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    MrfPolicyParams P = {};
+    P.N = n_pixels; P.L = L; P.cost = cost; P.labels = labels; P.label_bytes = label_bytes; P.advantage = advantage; P.old_logp = old_logp;
+    P.ref_logp = ref_logp; P.mask = mask; P.kl = kl_weight; P.scale = 1.0f; P.upstream = grad_loss; P.dcost = grad_cost;
+    const int rc = policy_arguments(P, cost_type, pixels_per_advantage, clip_low, clip_high, workspace, workspace_bytes, grad_loss);
+    if (rc != MRF_OK || n_pixels == 0) return rc;
+    if (!grad_cost) return MRF_ERR_NULL_POINTER;
+    return policy_of_type(P, cost_type, (hipStream_t)hip_stream);
 }
 
 }  // extern "C"

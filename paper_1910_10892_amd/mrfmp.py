@@ -131,6 +131,8 @@ def load_library():
     lib.mrf_softmin_policy_workspace_bytes.argtypes = []
     lib.mrf_softmin_policy.restype = ci
     lib.mrf_softmin_policy.argtypes = [i64, i32, vp, ci, vp, ci, vp, i64, vp, vp, vp, f32, f32, f32, f32, vp, vp, vp, vp, sz, vp]
+    lib.mrf_softmin_policy_backward.restype = ci
+    lib.mrf_softmin_policy_backward.argtypes = [i64, i32, vp, ci, vp, ci, vp, i64, vp, vp, vp, f32, f32, f32, vp, vp, vp, sz, vp]
     lib.mrf_workspace_fault.restype = ci
     lib.mrf_workspace_fault.argtypes = [vp, vp]
     lib.mrf_strerror.argtypes = [ci]
@@ -512,26 +514,57 @@ def mrf_softmin_policy_workspace_bytes() -> int:
     return int(load_library().mrf_softmin_policy_workspace_bytes())
 
 
-def mrf_softmin_policy(cost, labels, advantage, old_logp, ref_logp, mask, clip_low, clip_high, kl_weight, loss, logp, grad_cost,
-                       workspace, pixels_per_advantage=1, grad_scale=1.0, stream=None):
-    """cost [..., L] float32, float16 or bfloat16, labels [...] uint8 or int32, advantage float32 with an entry per
-    pixels_per_advantage pixels, old_logp and ref_logp [...] float32 or None, mask [...] uint8 or None, loss [3] float32, logp
-    [...] float32 or None, grad_cost like cost or None."""
+def _policy_sizes(cost, labels, advantage, old_logp, ref_logp, mask, logp, grad_cost, pixels_per_advantage):
+    """Pixels, labels and pixels per advantage of tensors that fit each other."""
     pixels, L = tuple(cost.shape[:-1]), _size(cost.shape[-1])
     n, per = math.prod(pixels), int(pixels_per_advantage)
     for name, t in (("labels", labels), ("old_logp", old_logp), ("ref_logp", ref_logp), ("mask", mask), ("logp", logp)):
         _same_size(name, t, *pixels)
     _same_size("grad_cost", grad_cost, *cost.shape)
-    _same_size("loss", loss, 3)
     if grad_cost is not None and grad_cost.dtype != cost.dtype:
         raise ValueError("grad_cost must be %s like cost, got %s" % (cost.dtype, grad_cost.dtype))
     if per >= 1 and int(advantage.numel()) != -(-n // per):
         raise ValueError("advantage has %d entries, expected %d" % (advantage.numel(), -(-n // per)))
+    return n, L, per
+
+
+def mrf_softmin_policy(cost, labels, advantage, old_logp, ref_logp, mask, clip_low, clip_high, kl_weight, loss, logp, grad_cost,
+                       workspace, pixels_per_advantage=1, grad_scale=1.0, stream=None):
+    """cost [..., L] float32, float16 or bfloat16, labels [...] uint8 or int32, advantage float32 with an entry per
+    pixels_per_advantage pixels, old_logp and ref_logp [...] float32 or None, mask [...] uint8 or None, loss [3] float32, logp
+    [...] float32 or None, grad_cost like cost or None."""
+    n, L, per = _policy_sizes(cost, labels, advantage, old_logp, ref_logp, mask, logp, grad_cost, pixels_per_advantage)
+    _same_size("loss", loss, 3)
     _checked(load_library().mrf_softmin_policy(
         n, L, _ptr(cost, None), _type_of(cost, "cost"), _ptr(labels, None), _label_bytes(labels), _ptr(advantage, "float32"), per,
         _ptr(old_logp, "float32"), _ptr(ref_logp, "float32"), _ptr(mask, "uint8"), float(clip_low), float(clip_high),
         float(kl_weight), float(grad_scale), _ptr(loss, "float32"), _ptr(logp, "float32"), _ptr(grad_cost, None),
         _ptr(workspace, None), _ws_size(workspace), _stream_handle(stream)), "mrf_softmin_policy")
+
+
+def mrf_softmin_policy_backward(cost, labels, advantage, old_logp, ref_logp, mask, clip_low, clip_high, kl_weight, grad_loss, grad_cost,
+                                workspace, pixels_per_advantage=1, stream=None):
+    """As mrf_softmin_policy; grad_loss float32 of one entry on the GPU, grad_cost like cost."""
+    n, L, per = _policy_sizes(cost, labels, advantage, old_logp, ref_logp, mask, None, grad_cost, pixels_per_advantage)
+    if int(grad_loss.numel()) != 1:
+        raise ValueError("grad_loss has %d entries, expected 1" % grad_loss.numel())
+    for t, name in ((cost, None), (labels, None), (advantage, "float32"), (old_logp, "float32"), (ref_logp, "float32"), (mask, "uint8"),
+                    (grad_loss, "float32"), (grad_cost, None), (workspace, None)):
+        _ptr(t, name)
+    _policy_backward((n, L, per, _type_of(cost, "cost"), _label_bytes(labels), float(clip_low), float(clip_high), float(kl_weight)), cost, labels,
+                     advantage, old_logp, ref_logp, mask, grad_loss, grad_cost, workspace, stream)
+
+
+def _policy_backward(given, cost, labels, advantage, old_logp, ref_logp, mask, grad_loss, grad_cost, workspace, stream=None):
+    """The call itself, of tensors that have been checked; `given`: pixels, labels, pixels per advantage, codes of the costs' and labels' types,
+    and the three numbers."""
+    n, L, per, cost_type, label_bytes, clip_low, clip_high, kl_weight = given
+    _checked(load_library().mrf_softmin_policy_backward(
+        n, L, cost.data_ptr(), cost_type, labels.data_ptr(), label_bytes, advantage.data_ptr(), per,
+        None if old_logp is None else old_logp.data_ptr(), None if ref_logp is None else ref_logp.data_ptr(),
+        None if mask is None else mask.data_ptr(), clip_low, clip_high, kl_weight, grad_loss.data_ptr(),
+        None if grad_cost is None else grad_cost.data_ptr(), None if workspace is None else workspace.data_ptr(),
+        _ws_size(workspace), _stream_handle(stream)), "mrf_softmin_policy_backward")
 
 
 def mrf_workspace_fault(workspace, stream=None) -> int:

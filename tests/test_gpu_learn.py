@@ -768,3 +768,49 @@ def test_binding_refuses_tensors_that_do_not_fit():
     with pytest.raises(mrf.MrfError) as e:
         mrf.mrf_softmin_policy(x, lab, z(4), None, None, None, 0.2, 0.2, 0.1, z(3), None, x, ws)
     assert e.value.status == -1
+
+
+# ---- the policy loss's gradient alone
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("N,L", [(1, 1), (2000, 2), (1961, 21), (3001, 16), (66, 64), (411, 70), (37, 128), (9, 257), (5, 1025), (6, 3001), (2, 32000), (1500, 1500), (2, 50257)])
+def test_policy_gradient_alone(N, L, dtype):
+    """That of the call with the loss, bit for bit: its factor comes from device memory instead."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    print("case policy gradient", N, L, dtype, flush=True)
+    rng = np.random.default_rng(N + L)
+    cost = _put(rng.normal(size=(N, L)), dtype, 1)
+    a = _put(rng.integers(0, L, N), "int32")
+    A, old, ref = (_put(rng.normal(m, 0.5, N), "float32") for m in (0.1, -1.0, -1.0))
+    mask = _put(rng.random(N) < 0.7, "uint8", 3)
+    ws, ws_check = _guarded((mrf.mrf_softmin_policy_workspace_bytes(),), torch.uint8)
+    loss, want = torch.empty(3, device="cuda:0"), torch.empty_like(cost)
+    for m, scale in ((None, 1.0), (mask, 0.375)):
+        mrf.mrf_softmin_policy(cost, a, A, old, ref, m, 0.2, 0.3, 0.1, loss, None, want, ws, grad_scale=scale)
+        grad, grad_check = _guarded((N, L), cost.dtype, 1)
+        ws.fill_(0xFF)
+        mrf.mrf_softmin_policy_backward(cost, a, A, old, ref, m, 0.2, 0.3, 0.1, torch.tensor([scale], device="cuda:0"), grad, ws)
+        torch.cuda.synchronize()
+        grad_check()
+        ws_check()
+        assert torch.equal(grad, want)
+
+
+def test_policy_gradient_alone_of_nothing_and_refusals():
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    z = lambda *s, dtype=torch.float32: torch.zeros(s, dtype=dtype, device="cuda:0")
+    ws = z(mrf.mrf_softmin_policy_workspace_bytes(), dtype=torch.uint8)
+    mrf.mrf_softmin_policy_backward(z(0, 5), z(0, dtype=torch.uint8), z(0), None, None, None, 0.2, 0.2, 0.0, z(1), z(0, 5), ws)
+    c, a = z(4, 5), z(4, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="grad_loss"):
+        mrf.mrf_softmin_policy_backward(c, a, z(4), None, None, None, 0.2, 0.2, 0.0, z(2), z(4, 5), ws)
+    with pytest.raises(ValueError, match="grad_cost"):
+        mrf.mrf_softmin_policy_backward(c, a, z(4), None, None, None, 0.2, 0.2, 0.0, z(1), z(4, 5, dtype=torch.float16), ws)
+    with pytest.raises(ValueError, match="advantage"):
+        mrf.mrf_softmin_policy_backward(c, a, z(3), None, None, None, 0.2, 0.2, 0.0, z(1), z(4, 5), ws)
+    for kept in ((None, ws), (z(4, 5), None)):
+        with pytest.raises(mrf.MrfError) as e:
+            mrf.mrf_softmin_policy_backward(c, a, z(4), None, None, None, 0.2, 0.2, 0.0, z(1), *kept)
+        assert e.value.status == -1

@@ -120,3 +120,22 @@ def test_binding_refuses_sizes_beyond_32_bits():
         mrf.mrf_softmin_logp(empty(1, n), empty(1, dtype=torch.int32), empty(1))
     with pytest.raises(ValueError, match="at most"):
         mrf.mrf_softmin_policy(empty(1, n), empty(1, dtype=torch.int32), empty(1), None, None, None, 0.2, 0.2, 0.0, empty(3), None, None, None)
+
+
+def test_policy_backward_refusals():
+    lib = mrf.load_library()
+    need = mrf.mrf_softmin_policy_workspace_bytes()
+
+    def backward(N=4, L=8, c=FAKE, a=FAKE, A=FAKE, per=1, ref=FAKE, low=0.2, high=0.2, kl=0.0, up=FAKE, grad=FAKE, ws=FAKE, size=need, lb=1, t=0):
+        return lib.mrf_softmin_policy_backward(N, L, c, t, a, lb, A, per, None, ref, None, low, high, kl, up, grad, ws, size, None)
+
+    assert backward(N=-1) == -2 and backward(N=1 << 31) == -2 and backward(L=300) == -3 and backward(L=0, lb=4) == -3
+    assert backward(lb=3) == -12 and backward(t=7) == -12 and backward(per=0) == -12
+    for bad in (-0.1, 1.0, NAN, INF):
+        assert backward(low=bad) == -12
+    for bad in (-0.1, NAN, INF):
+        assert backward(high=bad) == -12 and backward(kl=bad) == -12
+    assert backward(kl=0.1, ref=None) == -1
+    assert backward(c=None) == -1 and backward(a=None) == -1 and backward(A=None) == -1 and backward(up=None) == -1 and backward(grad=None) == -1
+    assert backward(ws=None) == -1 and backward(size=need - 1) == -6
+    assert backward(N=0, c=None, a=None, A=None, grad=None) == 0
