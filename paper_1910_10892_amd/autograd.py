@@ -191,7 +191,7 @@ def bucket_pairwise(table, bucket_of, first_offset, Q, K, *, query_offset=0, hea
     (mrf_distance_buckets makes the usual one).  A table [n_buckets] with Q = K = L and first_offset =
     -(L - 1) gives the pairwise function of message_passing, one [R,B,H,W,n_buckets] the tables of
     message_passing_edge_tables.  Gradients flow to the table."""
-    return _BucketPairwise.apply(table, bucket_of, (int(first_offset), int(Q), int(K), int(query_offset), bool(heads_last), dtype))
+    return _BucketPairwise.apply(table, bucket_of.contiguous(), (int(first_offset), int(Q), int(K), int(query_offset), bool(heads_last), dtype))
 
 
 class _PolicyLoss(torch.autograd.Function):
@@ -229,7 +229,13 @@ def policy_loss(cost, labels, advantage, old_logp=None, ref_logp=None, mask=None
     mrf_softmin_policy states it: (loss, terms, logp) with terms = [first term, mean k] and logp [...]
     the labels' log-probabilities.  The gradient flows from loss to cost: it is formed in 32 bits, times what comes
     from above, and rounded once to cost's type (a loss scaler keeps float16 gradients in range).  grad_scale is the
-    library's factor on the gradient of a call that knows no other; it changes nothing here."""
+    library's factor on the gradient of a call that knows no other; it changes nothing here.  advantage, old_logp and
+    ref_logp are given numbers: one that asks for a gradient of its own is refused."""
+    if torch.is_grad_enabled():
+        for name, t in (("advantage", advantage), ("old_logp", old_logp), ("ref_logp", ref_logp)):
+            if t is not None and t.requires_grad:
+                raise ValueError("policy_loss has no gradient with respect to %s: detach it" % name)
+    labels, advantage, old_logp, ref_logp, mask = (None if t is None else t.contiguous() for t in (labels, advantage, old_logp, ref_logp, mask))
     return _PolicyLoss.apply(cost, labels, advantage, old_logp, ref_logp, mask,
                              (float(clip_low), float(clip_high), float(kl_weight), int(pixels_per_advantage), float(grad_scale)))
 
@@ -239,5 +245,5 @@ def softmin_logp(cost, labels):
     old_logp and ref_logp); no gradient."""
     cost = cost.detach().contiguous()
     logp = torch.empty(cost.shape[:-1], dtype=torch.float32, device=cost.device)
-    _m.mrf_softmin_logp(cost, labels, logp)
+    _m.mrf_softmin_logp(cost, labels.contiguous(), logp)
     return logp

@@ -225,3 +225,42 @@ def test_policy_gradient_under_an_upstream_gradient(dtype, up, scale):
     cost.grad = None
     loss.backward(upstream)
     assert torch.equal(cost.grad, first)
+
+
+def test_policy_loss_takes_views_and_refuses_to_drop_gradients():
+    import torch
+    from paper_1910_10892_amd.autograd import bucket_pairwise, policy_loss, softmin_logp
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(11)
+    rand = lambda *s: torch.rand(s, generator=gen, device="cuda:0")
+    cost = rand(4, 6, 5).requires_grad_(True)
+    labels = torch.randint(0, 5, (6, 4), generator=gen, device="cuda:0", dtype=torch.uint8)
+    old, ref, mask = -1.5 - rand(6, 4), -1.5 - rand(6, 4), (rand(6, 4) < 0.8).to(torch.uint8)
+    A = rand(4, 1) - 0.5
+    # views that are not contiguous: transposed maps, one advantage for a row of pixels
+    views = (labels.t(), A.expand(4, 6), old.t(), ref.t(), mask.t())
+    assert not any(v.is_contiguous() for v in views)
+    got, want = [], []
+    for out, args in ((got, views), (want, [v.contiguous() for v in views])):
+        loss, terms, logp = policy_loss(cost, *args, kl_weight=0.1)
+        (grad,) = torch.autograd.grad(loss, cost)
+        out += [loss, terms, logp, grad, softmin_logp(cost, args[0])]
+    for g, w in zip(got, want):
+        assert torch.equal(g, w)
+    steps = torch.arange(18, dtype=torch.int32, device="cuda:0")
+    table = rand(9)
+    assert torch.equal(bucket_pairwise(table, (steps % 9)[::2], -4, 5, 5), bucket_pairwise(table, (steps % 9)[::2].contiguous(), -4, 5, 5))
+    # the loss has no gradient with respect to what it takes for given: asked for one, it says so
+    args = [v.contiguous() for v in views]
+    for at, name in ((1, "advantage"), (2, "old_logp"), (3, "ref_logp")):
+        given = list(args)
+        given[at] = given[at].clone().requires_grad_(True)
+        for c in (cost, cost.detach()):
+            with pytest.raises(ValueError, match=name):
+                policy_loss(c, *given, kl_weight=0.1)
+        with torch.no_grad():
+            assert torch.equal(policy_loss(cost, *given, kl_weight=0.1)[0], want[0])
+        given[at] = given[at].detach()
+        assert torch.equal(policy_loss(cost, *given, kl_weight=0.1)[0], want[0])
+    loss = policy_loss(cost.detach(), *args, kl_weight=0.1)[0]
+    assert not loss.requires_grad and torch.equal(loss, want[0])
