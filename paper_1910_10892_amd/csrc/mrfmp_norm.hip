@@ -276,28 +276,31 @@ __global__ void __launch_bounds__(256) mrf_norm_bwd_any(const MrfNormParams Q)
     }
 }
 
-// sums over rows: grid (columns / 64, P), lane = column, a workgroup takes every P-th run of four rows
+// sums over rows: grid (columns / 64, P), lane = column, a workgroup takes every P-th run of four rows; longer rows than a launch may have columns in turns
 template <class X, class Y>
 __global__ void __launch_bounds__(256) mrf_norm_param_any(const MrfNormParams Q)
 {
     __shared__ float sums[2][4][64];
     const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    const int c = blockIdx.x * 64 + lane;
-    float sg = 0.0f, sb = 0.0f;
-    if (c < Q.C)
-        for (long long r = (long long)blockIdx.y * 4 + wv; r < Q.N; r += (long long)Q.P * 4) {
-            const float dy = mrf_to_f32(((const Y *)Q.dy)[(size_t)r * Q.C + c]);
-            const float h = (mrf_to_f32(((const X *)Q.x)[(size_t)r * Q.C + c]) - Q.mean[r]) * Q.rstd[r];
-            sg = fmaf(dy, h, sg);
-            sb += dy;
+    for (long long first = blockIdx.x * 64LL; first < Q.C; first += gridDim.x * 64LL) {
+        const long long c = first + lane;
+        float sg = 0.0f, sb = 0.0f;
+        if (c < Q.C)
+            for (long long r = (long long)blockIdx.y * 4 + wv; r < Q.N; r += (long long)Q.P * 4) {
+                const float dy = mrf_to_f32(((const Y *)Q.dy)[(size_t)r * Q.C + c]);
+                const float h = (mrf_to_f32(((const X *)Q.x)[(size_t)r * Q.C + c]) - Q.mean[r]) * Q.rstd[r];
+                sg = fmaf(dy, h, sg);
+                sb += dy;
+            }
+        sums[0][wv][lane] = sg;
+        sums[1][wv][lane] = sb;
+        __syncthreads();
+        if (wv == 0 && c < Q.C) {
+            float *p = Q.partial + (size_t)blockIdx.y * 2 * Q.C + c;
+            p[0] = (sums[0][0][lane] + sums[0][1][lane]) + (sums[0][2][lane] + sums[0][3][lane]);
+            p[Q.C] = (sums[1][0][lane] + sums[1][1][lane]) + (sums[1][2][lane] + sums[1][3][lane]);
         }
-    sums[0][wv][lane] = sg;
-    sums[1][wv][lane] = sb;
-    __syncthreads();
-    if (wv == 0 && c < Q.C) {
-        float *p = Q.partial + (size_t)blockIdx.y * 2 * Q.C + c;
-        p[0] = (sums[0][0][lane] + sums[0][1][lane]) + (sums[0][2][lane] + sums[0][3][lane]);
-        p[Q.C] = (sums[1][0][lane] + sums[1][1][lane]) + (sums[1][2][lane] + sums[1][3][lane]);
+        __syncthreads();
     }
 }
 
@@ -307,24 +310,26 @@ __global__ void __launch_bounds__(1024) mrf_norm_param_sum(const MrfNormParams Q
 {
     __shared__ float sums[64][17];
     const int col = threadIdx.x & 15, part = threadIdx.x >> 4;
-    const long long c = (long long)blockIdx.x * 16 + col;      // [0, C) weight, [C, 2 C) bias
-    float s = 0.0f;
-    if (c < 2LL * Q.C)
+    for (long long first = blockIdx.x * 16LL; first < 2LL * Q.C; first += gridDim.x * 16LL) {
+        const long long c = first + col;      // [0, C) weight, [C, 2 C) bias
+        float s = 0.0f;
+        if (c < 2LL * Q.C)
 #pragma unroll 8
-        for (int p = part; p < Q.P; p += 64) s += Q.partial[(size_t)p * 2 * Q.C + c];
-    sums[part][col] = s;
-    __syncthreads();
-#pragma unroll
-    for (int half = 32; half > 0; half >>= 1) {
-        if (part < half) sums[part][col] += sums[part + half][col];
+            for (int p = part; p < Q.P; p += 64) s += Q.partial[(size_t)p * 2 * Q.C + c];
+        sums[part][col] = s;
         __syncthreads();
-    }
-    if (part == 0 && c < 2LL * Q.C) {
-        s = sums[0][col];
-        if (c < Q.C) {
-            if (Q.dgamma) Q.dgamma[c] = s;
-        } else if (Q.dbeta) {
-            Q.dbeta[c - Q.C] = s;
+#pragma unroll
+        for (int half = 32; half > 0; half >>= 1) {
+            if (part < half) sums[part][col] += sums[part + half][col];
+            __syncthreads();
+        }
+        if (part == 0 && c < 2LL * Q.C) {
+            s = sums[0][col];
+            if (c < Q.C) {
+                if (Q.dgamma) Q.dgamma[c] = s;
+            } else if (Q.dbeta) {
+                Q.dbeta[c - Q.C] = s;
+            }
         }
     }
 }
@@ -342,6 +347,10 @@ int norm_partials(int64_t n_rows, int32_t C)
     const int most = (long long)C * n_rows <= 32768 && C <= 1024 ? 1 : (C <= 128 ? 512 : 256);
     return (int)(most < n_rows ? most : n_rows);
 }
+
+// Workgroups for so many runs of columns: a launch has fewer than 2^32 threads along an index, and more than 16,384 workgroups keep no
+// more compute units busy.
+unsigned norm_grid(long long runs) { return (unsigned)(runs < 16384 ? runs : 16384); }
 
 int norm_check(int64_t n_rows, int32_t C, int x_type, int y_type)
 {
@@ -437,7 +446,7 @@ template <class X, class Y> int norm_bwd_launch(MrfNormParams &Q, bool &summed, 
         if (rc != MRF_OK) return rc;
     }
     if (!Q.partial) return MRF_OK;
-    hipLaunchKernelGGL((mrf_norm_param_any<X, Y>), dim3((unsigned)((Q.C + 63) / 64), (unsigned)Q.P), dim3(256), 0, st, Q);
+    hipLaunchKernelGGL((mrf_norm_param_any<X, Y>), dim3(norm_grid((Q.C + 63LL) / 64), (unsigned)Q.P), dim3(256), 0, st, Q);
     return launch_status("mrf_norm_param_any");
 }
 
@@ -451,7 +460,7 @@ template <class X, class Y> int norm_backward(MrfNormParams Q, hipStream_t st)
         if (rc != MRF_OK || summed) return rc;
     }
     if (!params) return MRF_OK;
-    hipLaunchKernelGGL(mrf_norm_param_sum, dim3((unsigned)((2LL * Q.C + 15) / 16)), dim3(1024), 0, st, Q);
+    hipLaunchKernelGGL(mrf_norm_param_sum, dim3(norm_grid((2LL * Q.C + 15) / 16)), dim3(1024), 0, st, Q);
     return launch_status("mrf_norm_param_sum");
 }
 

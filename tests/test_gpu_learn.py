@@ -814,3 +814,25 @@ def test_policy_gradient_alone_of_nothing_and_refusals():
         with pytest.raises(mrf.MrfError) as e:
             mrf.mrf_softmin_policy_backward(c, a, z(4), None, None, None, 0.2, 0.2, 0.0, z(1), *kept)
         assert e.value.status == -1
+
+
+# ---- rows so long that a launch has not a thread for each of their columns
+
+@pytest.mark.parametrize("C,dtype", [((1 << 25) - 3, "float32"), ((1 << 25) + 5, "float32"), ((1 << 25) + 5, "bfloat16"), ((1 << 30) + 67, "bfloat16")])
+def test_layer_norm_parameter_gradients_of_the_longest_rows(C, dtype, _memory_back):
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    print("case layer norm, parameters", C, dtype, flush=True)
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(5)
+    piece = torch.randn((2, 1, 1000003), generator=gen, device="cuda:0").to(getattr(torch, dtype))
+    x, dy = (v.repeat(1, C // 1000003 + 1)[:, :C].contiguous() for v in piece)
+    mean, rstd = torch.tensor([0.25], device="cuda:0"), torch.tensor([1.5], device="cuda:0")
+    gg, gb = (torch.full((C,), float("nan"), device="cuda:0") for _ in range(2))
+    ws = torch.empty(mrf.mrf_layer_norm_workspace_bytes(1, C), dtype=torch.uint8, device="cuda:0")
+    mrf.mrf_layer_norm_backward(dy, x, None, mean, rstd, None, gg, gb, ws)
+    # (one row: products, no sums)
+    assert torch.equal(gb, dy[0].float())
+    del gb
+    for a in range(0, C, 1 << 28):
+        assert torch.equal(gg[a:a + (1 << 28)], dy[0, a:a + (1 << 28)].float() * ((x[0, a:a + (1 << 28)].float() - 0.25) * 1.5)), a
