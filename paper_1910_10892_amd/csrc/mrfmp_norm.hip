@@ -219,27 +219,30 @@ __global__ void __launch_bounds__(mrf_norm_bwd_threads(TL)) mrf_norm_bwd(const M
 }
 
 // ---- a wavefront per row: any length (rows of more than 16,384 columns forward, 12,288 backward, for which a workgroup has no registers).  Three
-// readings, the second and third from the caches for the most part: 1,000 rows of 12,000 in 32 bits 178 and 194 us, 22 and 54 in registers.
+// readings, the second and third from the caches for the most part: 1,000 rows of 12,000 in 32 bits 178 and 194 us, 22 and 54 in registers.  A lane adds
+// up as many as 2^25 values one after the other: in 64 bits (backward, 1,000 x 20,000 in 16 bits: 345 us with sums in 32 bits, 366 in 64, 286 two columns
+// at a time).
 template <class X, class Y>
 __global__ void __launch_bounds__(256) mrf_norm_fwd_any(const MrfNormParams Q)
 {
     const int lane = threadIdx.x & 63;
     const long long step = (long long)gridDim.x * 4;
-    const float inv = 1.0f / (float)Q.C;
     for (long long r = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); r < Q.N; r += step) {
         const X *x = (const X *)Q.x + (size_t)r * Q.C;
         Y *y = (Y *)Q.y + (size_t)r * Q.C;
-        float s = 0.0f;
-        for (int c = lane; c < Q.C; c += 64) s += mrf_to_f32(x[c]);
-        const float mu = mrf_lanes_sum<64>(s) * inv;
-        s = 0.0f;
+        double s = 0.0;
+        for (int c = lane; c < Q.C; c += 64) s += (double)mrf_to_f32(x[c]);
+        const double mean = mrf_wave_sum_f64(s) / (double)Q.C;
+        // (differences from the mean in two steps: what its rounding to 32 bits leaves is taken off as well)
+        const float mu = (float)mean, left = (float)(mean - (double)mu);
+        s = 0.0;
         for (int c = lane; c < Q.C; c += 64) {
-            const float d = mrf_to_f32(x[c]) - mu;
-            s += d * d;
+            const float d = (mrf_to_f32(x[c]) - mu) - left;
+            s = fma((double)d, (double)d, s);
         }
-        const float rs = rsqrtf(mrf_lanes_sum<64>(s) * inv + Q.eps);
+        const float rs = rsqrtf((float)(mrf_wave_sum_f64(s) / (double)Q.C) + Q.eps);
         for (int c = lane; c < Q.C; c += 64) {
-            const float h = (mrf_to_f32(x[c]) - mu) * rs;
+            const float h = ((mrf_to_f32(x[c]) - mu) - left) * rs;
             const float g = Q.gamma ? Q.gamma[c] : 1.0f, b = Q.beta ? Q.beta[c] : 0.0f;
             y[c] = mrf_from_f32<Y>(fmaf(h, g, b));
         }
@@ -253,21 +256,20 @@ __global__ void __launch_bounds__(256) mrf_norm_bwd_any(const MrfNormParams Q)
 {
     const int lane = threadIdx.x & 63;
     const long long step = (long long)gridDim.x * 4;
-    const float inv = 1.0f / (float)Q.C;
     for (long long r = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); r < Q.N; r += step) {
         const X *x = (const X *)Q.x + (size_t)r * Q.C;
         const Y *dy = (const Y *)Q.dy + (size_t)r * Q.C;
         X *dx = (X *)Q.dx + (size_t)r * Q.C;
         const float mu = Q.mean[r], rs = Q.rstd[r];
-        float sa = 0.0f, sh = 0.0f;
+        double sum_a = 0.0, sum_h = 0.0;
+#pragma unroll 2
         for (int c = lane; c < Q.C; c += 64) {
             const float h = (mrf_to_f32(x[c]) - mu) * rs;
             const float a = mrf_to_f32(dy[c]) * (Q.gamma ? Q.gamma[c] : 1.0f);
-            sa += a;
-            sh = fmaf(a, h, sh);
+            sum_a += (double)a;
+            sum_h = fma((double)a, (double)h, sum_h);
         }
-        sa = mrf_lanes_sum<64>(sa) * inv;
-        sh = mrf_lanes_sum<64>(sh) * inv;
+        const float sa = (float)(mrf_wave_sum_f64(sum_a) / (double)Q.C), sh = (float)(mrf_wave_sum_f64(sum_h) / (double)Q.C);
         for (int c = lane; c < Q.C; c += 64) {
             const float h = (mrf_to_f32(x[c]) - mu) * rs;
             const float a = mrf_to_f32(dy[c]) * (Q.gamma ? Q.gamma[c] : 1.0f);

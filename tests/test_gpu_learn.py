@@ -836,3 +836,37 @@ def test_layer_norm_parameter_gradients_of_the_longest_rows(C, dtype, _memory_ba
     del gb
     for a in range(0, C, 1 << 28):
         assert torch.equal(gg[a:a + (1 << 28)], dy[0, a:a + (1 << 28)].float() * ((x[0, a:a + (1 << 28)].float() - 0.25) * 1.5)), a
+
+
+@pytest.mark.parametrize("C", [20001, 300001, 3000001])
+def test_layer_norm_backward_of_long_rows_of_one_sign(C):
+    """Sums over a row of values that are all alike: every rounding of a long chain would go the same way."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    from oracle import mrf_learn_oracle as lo
+    print("case layer norm, long rows", C, flush=True)
+    N = 3
+    rng = np.random.default_rng(C)
+    x = rng.normal(0.5, 1.0, (N, C)).astype(np.float32)
+    dy = np.repeat(np.array([[0.1], [-0.7], [123.4]], np.float32), C, 1)
+    dy[2] += x[2]
+    gamma = np.full(C, 1.1, np.float32)
+    xt, dyt, gt = _put(x, "float32"), _put(dy, "float32"), _put(gamma, "float32")
+    y, mean, rstd, gx, gg, gb = (torch.empty(s, device="cuda:0") for s in ((N, C), (N,), (N,), (N, C), (C,), (C,)))
+    ws = torch.empty(mrf.mrf_layer_norm_workspace_bytes(N, C), dtype=torch.uint8, device="cuda:0")
+    mrf.mrf_layer_norm_forward(xt, gt, None, 1e-5, y, mean, rstd)
+    mrf.mrf_layer_norm_backward(dyt, xt, gt, mean, rstd, gx, gg, gb, ws)
+    want, mu, rs = lo.layer_norm(x, gamma)
+    h, dh = _norm_bounds(x.astype(np.float64), rs, gamma)
+    _close(y, want, 1.1 * dh + U * 2 * np.abs(want))
+    _close(mean, mu, 2 * U * np.abs(mu))
+    _close(rstd, rs, 8 * U * rs)
+    wx, wg, wb = lo.layer_norm_grad(dy, x, gamma)
+    # h is off by a few roundings, and its sum with dy by no more: all sums as good as exact
+    a = np.abs(dy.astype(np.float64) * gamma)
+    dh = 4 * U * (1.0 + np.abs(h))
+    bound = rs[:, None] * (4 * U * a + 2 * U * a.mean(1, keepdims=True) + 4 * U * np.abs(h) * (a * np.abs(h)).mean(1, keepdims=True) +
+                           np.abs(h) * (a * dh).mean(1, keepdims=True) + dh * np.abs((dy * gamma * h).mean(1, keepdims=True)))
+    _close(gx, wx, bound)
+    _close(gg, wg, (np.abs(dy) * dh).sum(0) + SUM * U * np.abs(dy * h).sum(0))
+    _close(gb, wb, SUM * U * np.abs(dy).sum(0))
