@@ -22,12 +22,22 @@ struct MrfNormParams {
 // time; the other wavefronts of the compute unit are what hides its loads (with up to four rows 1 million of 16 in 32 bits 28 instead of 26 us).
 constexpr int mrf_norm_threads(int TL) { return TL <= 256 ? 256 : TL; }
 
+// What the mean of 32 bits is off by, the mean `left` of the differences from it, is small but as large as the contrast of a row far from 0
+// (constant rows of 1,000.1 came out as 0.06): it is taken off the differences, and its square off their mean square (never below 0 but for
+// its rounding; NaN stays).
+__device__ inline float mrf_norm_variance(float square, float left)
+{
+    const float v = fmaf(-left, left, square);
+    return v < 0.0f ? 0.0f : v;
+}
+
 template <class X, class Y, int TL, int V, int CH>
 __global__ void __launch_bounds__(mrf_norm_threads(TL)) mrf_norm_fwd(const MrfNormParams Q)
 {
     typedef MrfRow<TL, V, CH> Row;
     constexpr int NT = mrf_norm_threads(TL), G = NT / TL;
-    __shared__ float scratch[2][NT / 64];
+    __shared__ float scratch[NT / 64];
+    __shared__ __align__(16) float2 pairs[NT / 64];
     const int l = threadIdx.x % TL, C = Q.C;
     const float inv = 1.0f / (float)C;
     float gamma[Row::E], beta[Row::E], in_row[Row::E];      // (in_row: 1 in the row's columns, 0 behind them)
@@ -48,19 +58,23 @@ __global__ void __launch_bounds__(mrf_norm_threads(TL)) mrf_norm_fwd(const MrfNo
         float s = 0.0f;
 #pragma unroll
         for (int e = 0; e < Row::E; ++e) s += x[e];
-        const float mu = Row::sum(s, scratch[0]) * inv;
+        const float mu = Row::sum(s, scratch) * inv;
+        float left = 0.0f;
         s = 0.0f;
 #pragma unroll
         for (int e = 0; e < Row::E; ++e) {
             x[e] = fmaf(-mu, in_row[e], x[e]);
+            left += x[e];
             s = fmaf(x[e], x[e], s);
         }
-        const float rs = rsqrtf(Row::sum(s, scratch[1]) * inv + Q.eps);
+        Row::sums(left, s, pairs);
+        left *= inv;
+        const float rs = rsqrtf(mrf_norm_variance(s * inv, left) + Q.eps);
 #pragma unroll
-        for (int e = 0; e < Row::E; ++e) x[e] = fmaf(x[e] * rs, gamma[e], beta[e]);
+        for (int e = 0; e < Row::E; ++e) x[e] = fmaf((x[e] - left) * rs, gamma[e], beta[e]);
         if (FAST || first + group < Q.N) {
             Row::store((Y *)Q.y + (size_t)first * C + mine, C, l, x);
-            if (l == 0 && Q.mean) Q.mean[first + group] = mu;
+            if (l == 0 && Q.mean) Q.mean[first + group] = mu + left;
             if (l == 0 && Q.rstd) Q.rstd[first + group] = rs;
         }
     };
@@ -92,20 +106,23 @@ __global__ void __launch_bounds__(256) mrf_norm_fwd_tile(const MrfNormParams Q)
 #pragma unroll
         for (int e = 0; e < E; ++e) s += x[e];
         const float mu = Tile::sum(s) * inv;
+        float left = 0.0f;
         s = 0.0f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             x[e] = Tile::column(l, e) < C ? x[e] - mu : 0.0f;
+            left += x[e];
             s = fmaf(x[e], x[e], s);
         }
-        const float rs = rsqrtf(Tile::sum(s) * inv + Q.eps);
+        left = Tile::sum(left) * inv;
+        const float rs = rsqrtf(mrf_norm_variance(Tile::sum(s) * inv, left) + Q.eps);
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = fmaf(x[e] * rs, gamma[e], beta[e]);
+        for (int e = 0; e < E; ++e) x[e] = fmaf((x[e] - left) * rs, gamma[e], beta[e]);
         mrf_wave_lds_fence();
         Tile::put((Y *)lds[wv], g, C, l, x);
         mrf_wave_lds_fence();
         Tile::flush((Y *)Q.y + (size_t)base * C, rows, C, (const Y *)lds[wv]);
-        if (l == 0 && g < rows && Q.mean) Q.mean[base + g] = mu;
+        if (l == 0 && g < rows && Q.mean) Q.mean[base + g] = mu + left;
         if (l == 0 && g < rows && Q.rstd) Q.rstd[base + g] = rs;
         mrf_wave_lds_fence();
     }

@@ -163,6 +163,28 @@ template <int TL_, int V_, int CH_> struct MrfRow {
     }
     static __device__ inline float sum(float v, float *scratch) { return reduce<true>(v, scratch); }
     static __device__ inline float min(float v, float *scratch) { return reduce<false>(v, scratch); }
+
+    // two sums at once, with one barrier
+    static __device__ inline void sums(float &a, float &b, float2 *scratch)
+    {
+        if constexpr (TL <= 64) {
+            a = mrf_lanes_sum<TL>(a);
+            b = mrf_lanes_sum<TL>(b);
+        } else {
+            a = mrf_lanes_sum<64>(a);
+            b = mrf_lanes_sum<64>(b);
+            const int wv = threadIdx.x >> 6, first = wv & ~(TL / 64 - 1);
+            if ((threadIdx.x & 63) == 0) scratch[wv] = make_float2(a, b);
+            __syncthreads();
+            a = scratch[first].x;
+            b = scratch[first].y;
+#pragma unroll
+            for (int w = 1; w < TL / 64; ++w) {
+                a += scratch[first + w].x;
+                b += scratch[first + w].y;
+            }
+        }
+    }
 };
 
 

@@ -870,3 +870,54 @@ def test_layer_norm_backward_of_long_rows_of_one_sign(C):
     _close(gx, wx, bound)
     _close(gg, wg, (np.abs(dy) * dh).sum(0) + SUM * U * np.abs(dy * h).sum(0))
     _close(gb, wb, SUM * U * np.abs(dy).sum(0))
+
+
+# ---- rows whose level is far above their contrast
+
+@pytest.mark.parametrize("level", [1000.1, -30000.3, 0.1])
+@pytest.mark.parametrize("C", [3, 16, 21, 24, 36, 70, 192, 300, 1000, 2048, 5000, 12000, 20000, 300001])
+def test_layer_norm_of_rows_with_little_contrast(C, level):
+    """What single precision loses in a row's mean is found again in the differences from it: a constant row is 0, whatever its value."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    from oracle import mrf_learn_oracle as lo
+    print("case layer norm, level", C, level, flush=True)
+    N = 7
+    rng = np.random.default_rng(C)
+    x = np.full((N, C), level, np.float32)
+    x[3:] += rng.normal(0.0, 0.02, (N - 3, C)).astype(np.float32)
+    dy = rng.normal(0.3, 1.0, (N, C)).astype(np.float32)
+    xt, dyt = _put(x, "float32"), _put(dy, "float32")
+    y, mean, rstd, gx = (torch.empty(s, device="cuda:0") for s in ((N, C), (N,), (N,), (N, C)))
+    mrf.mrf_layer_norm_forward(xt, None, None, 1e-5, y, mean, rstd)
+    mrf.mrf_layer_norm_backward(dyt, xt, None, mean, rstd, gx, None, None, None)
+    want, mu, rs = lo.layer_norm(x)
+    # the mean is off by SUM u of the level at first, then by as much of that and of the contrast (the terms of the second sum), and where it is
+    # stored by a rounding
+    left = (SUM * U) ** 2 * np.abs(x).max()
+    h = np.abs(want)
+    bound = (left + SUM * U * (SUM * U * np.abs(x).max()) ** 2 * rs[:, None]) * rs[:, None] + SUM * U * (h + h.mean(1, keepdims=True))
+    assert (np.abs(_np(y) - want) <= bound).all(), "off by %g" % np.abs(_np(y) - want).max()
+    assert (_np(y)[:3] == 0).all() or np.abs(_np(y)[:3]).max() <= left * rs.max()
+    assert (np.abs(_np(mean) - mu) <= 1.01 * U * np.abs(mu) + left + SUM * U * h.mean(1) / rs).all()
+    _close(rstd, rs, SUM * U * rs + 0.5 * rs ** 3 * SUM * U * (SUM * U * np.abs(x).max()) ** 2)
+    # backward reads the stored mean
+    dh = (U * np.abs(x).max() + left) * rs[:, None] + SUM * U * (h + h.mean(1, keepdims=True))
+    wx, _, _ = lo.layer_norm_grad(dy, x)
+    a = np.abs(dy)
+    ma, mah = a.mean(1, keepdims=True), (a * (h + dh)).mean(1, keepdims=True)
+    bound = rs[:, None] * (U * a + SUM * U * ma + (h + dh) * SUM * U * mah + dh * mah + h * (a * dh).mean(1, keepdims=True) + 4 * U * (a + ma + h * mah))
+    _close(gx, wx, bound + SUM * U * np.abs(wx))
+
+
+@pytest.mark.parametrize("types", TYPE_PAIRS, ids="-".join)
+@pytest.mark.parametrize("C", [21, 24, 300, 2049, 20001])
+def test_layer_norm_of_constant_rows_in_each_type(C, types):
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    x = _put(np.array([1000.1, -4321.7, 0.3, 6.1e4])[:, None].repeat(C, 1), types[0])
+    y, mean, rstd = torch.empty((4, C), dtype=getattr(torch, types[1]), device="cuda:0"), torch.empty(4, device="cuda:0"), torch.empty(4, device="cuda:0")
+    mrf.mrf_layer_norm_forward(x, None, None, 1e-5, y, mean, rstd)
+    left = (SUM * U) ** 2 * np.abs(_np(x))
+    assert (np.abs(_np(y)) <= left / np.sqrt(1e-5)).all(), np.abs(_np(y)).max(1)
+    assert torch.equal(mean, x[:, 0].float())
