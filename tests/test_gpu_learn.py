@@ -921,3 +921,41 @@ def test_layer_norm_of_constant_rows_in_each_type(C, types):
     left = (SUM * U) ** 2 * np.abs(_np(x))
     assert (np.abs(_np(y)) <= left / np.sqrt(1e-5)).all(), np.abs(_np(y)).max(1)
     assert torch.equal(mean, x[:, 0].float())
+
+
+@pytest.mark.parametrize("M,C", [(1000003, 21), (100003, 208), (7001, 2050)])
+def test_layer_norm_parameter_gradients_beyond_32_bit_offsets(M, C, _memory_back):
+    """Sums over rows that do not cancel, so that a missing block of rows, or a sign, is far outside of the bound; those of the bias exactly."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    k = (1 << 32) // (M * C) + 2
+    print("case norm, parameters", k * M, C, flush=True)
+    gen = torch.Generator(device="cuda:0")
+    gen.manual_seed(C)
+    x = torch.randn((M, C), generator=gen, device="cuda:0").to(torch.bfloat16)
+    # towards x: dy h is positive for the most part
+    dy = (x.float() + 0.5 * torch.randn((M, C), generator=gen, device="cuda:0")).to(torch.bfloat16)
+    mean, rstd = torch.empty(M, device="cuda:0"), torch.empty(M, device="cuda:0")
+    y = torch.empty_like(x)
+    mrf.mrf_layer_norm_forward(x, None, None, 1e-5, y, mean, rstd)
+    del y
+    t = dy.double() * ((x.double() - mean.double()[:, None]) * rstd.double()[:, None])
+    want, size = k * t.sum(0), k * t.abs().sum(0)
+    del t
+    xs, ms, rs = _repeated(x, k).view(-1, C), _repeated(mean, k).view(-1), _repeated(rstd, k).view(-1)
+    gg, gb = torch.empty(C, device="cuda:0"), torch.empty(C, device="cuda:0")
+    ws = torch.empty(mrf.mrf_layer_norm_workspace_bytes(k * M, C), dtype=torch.uint8, device="cuda:0")
+    dys = _repeated(dy, k).view(-1, C)
+    mrf.mrf_layer_norm_backward(dys, xs, None, ms, rs, None, gg, gb, ws)
+    # a lane has every (workgroups x rows of a workgroup)-th row, 256 rows at a time at least: a chain of m of k M rows, whose roundings
+    # are independent of each other, and trees
+    m = k * M / 256
+    bound = (np.sqrt(m) + SUM) * U * size
+    assert (bound < 0.05 * want.abs()).all()
+    assert ((gg.double() - want).abs() <= bound).all()
+    # ones in few rows, first and last among them: exact sums
+    dys.zero_()
+    rows = torch.cat([torch.tensor([0, 1, k * M // 2, k * M - 2, k * M - 1], device="cuda:0"), torch.randint(0, k * M, (5000,), generator=gen, device="cuda:0")]).unique()
+    dys[rows] = 1.0
+    mrf.mrf_layer_norm_backward(dys, xs, None, ms, rs, None, gg, gb, ws)
+    assert (gb == float(rows.numel())).all()
