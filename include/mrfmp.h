@@ -313,8 +313,8 @@ int mrf_softmin_logp(int64_t n_pixels, int32_t L, const void *cost, int cost_typ
  *   grad_cost(lambda) = grad_scale d loss / d c(lambda) = grad_scale g / n (f(lambda) - [lambda = a]),
  *   g = d loss_i / d lp = (-r A if r A <= the other term, else 0) + kl_weight (1 - exp(d))
  * n = number of counted pixels; 0 for pixels that do not count, whose costs may be anything (NaN too), and for those without an
- * allowed label, which stay in n.  A counted pixel whose own label is not allowed has r = 0 and an
- * infinite k: with kl_weight > 0 the loss is infinite and the gradient of that pixel not finite.
+ * allowed label, which stay in n.  A counted pixel whose own label is not allowed has r = 0 (1 without old_logp) and an
+ * infinite k, whatever old_logp and ref_logp are: with kl_weight > 0 the loss is infinite and the gradient of that pixel not finite.
  *   cost, labels  as above
  *   advantage   DEVICE float: entry i / pixels_per_advantage is that of pixel i (1: one per pixel; H W: one per image)
  *   old_logp    DEVICE [n_pixels] float, or NULL: that of the present costs (r = 1, and its gradient that of r)

@@ -82,14 +82,17 @@ template <bool TRAIN> __device__ inline MrfPixel mrf_policy_pixel(const MrfPolic
 // what a pixel adds to the two sums, and the slope of the loss in its log-probability (before 1 / n)
 __device__ inline void mrf_policy_terms(const MrfPolicyParams &P, const MrfPixel &x, float lp, float &gain, float &div, float &slope)
 {
-    const float r = P.old_logp ? __builtin_amdgcn_exp2f((lp - x.old_logp) * 1.44269504088896340736f) : 1.0f;
+    // (a label that is not allowed: r = 0 and an infinite d, also where the earlier or the reference costs did not allow it either)
+    const bool barred = lp == -INFINITY;
+    const float over = barred && x.old_logp == lp ? lp : lp - x.old_logp;
+    const float r = P.old_logp ? __builtin_amdgcn_exp2f(over * 1.44269504088896340736f) : 1.0f;
     const float open = r * x.advantage, held = fminf(fmaxf(r, P.low), P.high) * x.advantage;
     const bool clipped = open > held;      // (not where either is NaN, which so reaches the loss)
     gain = clipped ? held : open;
     slope = clipped ? 0.0f : -open;
     div = 0.0f;
     if (P.ref_logp) {
-        const float d = x.ref_logp - lp, em = mrf_exp_minus_1(d);
+        const float d = barred && x.ref_logp == lp ? INFINITY : x.ref_logp - lp, em = mrf_exp_minus_1(d);
         div = em < INFINITY ? em - d : em;      // (a label that is not allowed: infinite, not infinity less infinity)
         if (P.kl > 0.0f) slope -= P.kl * em;
     }

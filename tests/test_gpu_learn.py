@@ -959,3 +959,42 @@ def test_layer_norm_parameter_gradients_beyond_32_bit_offsets(M, C, _memory_back
     dys[rows] = 1.0
     mrf.mrf_layer_norm_backward(dys, xs, None, ms, rs, None, gg, gb, ws)
     assert (gb == float(rows.numel())).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("L", [5, 16, 21, 300, 5000, 33000])
+def test_policy_labels_that_no_costs_allow(L, dtype):
+    """A counted pixel whose label is barred under the present, the old and the reference costs alike: r = 0 and an infinite k, not the
+    difference of two infinities."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    from oracle import mrf_learn_oracle as lo
+    N, inf = 6, float("inf")
+    rng = np.random.default_rng(L)
+    c = rng.normal(size=(N, L))
+    c[2, 3] = c[4, 3] = inf
+    cost = _put(c, dtype)
+    c = _np(cost)
+    a = torch.full((N,), 3, dtype=torch.int32, device="cuda:0")
+    A = torch.tensor([1.0, -1.0, 1.0, 0.5, -2.0, 0.25], device="cuda:0")
+    given = torch.full((N,), -1.0, device="cuda:0")
+    mrf.mrf_softmin_logp(cost, a, given)
+    assert given[2] == -inf and given[4] == -inf
+    old = given.clone()
+    loss, logp, grad = torch.empty(3, device="cuda:0"), torch.empty(N, device="cuda:0"), torch.empty_like(cost)
+    ws = torch.empty(mrf.mrf_softmin_policy_workspace_bytes(), dtype=torch.uint8, device="cuda:0")
+    mrf.mrf_softmin_policy(cost, a, A, old, None, None, 0.2, 0.2, 0.0, loss, logp, grad, ws, grad_scale=float(N))
+    # (r of such a pixel is 0: it is as if its old log-probability were any finite one)
+    finite = np.where(np.isinf(_np(old)), -1.0, _np(old))
+    want, _, wgrad = lo.policy(c, a.cpu().numpy(), _np(A), finite, None, None, 0.2, 0.2)
+    np.testing.assert_allclose(_np(loss), want, rtol=1e-5, atol=1e-6)
+    np.testing.assert_allclose(_np(grad), wgrad * N, rtol=2.0 ** -7 if dtype == "bfloat16" else 2.0 ** -10 if dtype == "float16" else 1e-4, atol=1e-6)
+    # the reference bars it too: k is infinite, the other pixels' gradients are as ever
+    mrf.mrf_softmin_policy(cost, a, A, old, given, None, 0.2, 0.2, 0.1, loss, logp, grad, ws, grad_scale=float(N))
+    assert loss[0] == inf and loss[2] == inf and torch.isfinite(loss[1])
+    rows = [0, 1, 3, 5]
+    np.testing.assert_allclose(_np(grad)[rows], wgrad[rows] * N, rtol=2.0 ** -7 if dtype == "bfloat16" else 2.0 ** -10 if dtype == "float16" else 1e-4, atol=1e-6)
+    # NaN is still NaN
+    old[2] = float("nan")
+    mrf.mrf_softmin_policy(cost, a, A, old, None, None, 0.2, 0.2, 0.0, loss, logp, grad, ws)
+    assert loss[0].isnan()
