@@ -272,7 +272,8 @@ int mrf_layer_norm_backward(int64_t n_rows, int32_t C, const void *grad_y, int y
  * sign (all n_buckets, or with two_sided the lower half for d <= 0 and the upper half for d > 0; one-sided, d > 0 is taken
  * as d = 0) the first half hold one distance each, the others distances up to far_distance by their logarithm, and the last one
  * all beyond.
- *   bucket_of  HOST [n_offsets], assigned.  Host arithmetic.  A caller may as well make a map of its own. */
+ *   bucket_of  HOST [n_offsets], assigned.  Host arithmetic.  A caller may as well make a map of its own.
+ * first_offset within 2^40 of 0 and n_offsets up to 2^40, here and below, else MRF_ERR_BAD_ARGUMENT. */
 int mrf_distance_buckets(int32_t n_buckets, int64_t far_distance, int two_sided, int64_t first_offset, int64_t n_offsets, int32_t *bucket_of);
 
 /* A pairwise function that depends on the distance of its labels, from a learned value per bucket of distances -- or any

@@ -465,12 +465,15 @@ int bucket_check(int64_t G, int32_t Q, int32_t K, int32_t NB)
     return MRF_OK;
 }
 
+// offsets of a map: far from where sums of 64 bits would wrap around
+constexpr int64_t FARTHEST = (int64_t)1 << 40;
+
+bool bucket_offsets(int64_t first, int64_t n) { return first >= -FARTHEST && first <= FARTHEST && n >= 0 && n <= FARTHEST; }
+
 // the call's part of the map: every offset k - q - query_offset has to be in it
 int bucket_map(int32_t Q, int32_t K, const int32_t *bucket_of, int64_t first_offset, int64_t n_offsets, int64_t query_offset, const int **map)
 {
-    const int64_t far = (int64_t)1 << 40;
-    if (first_offset < -far || first_offset > far || n_offsets < 0 || n_offsets > far || query_offset < -far || query_offset > far)
-        return MRF_ERR_BAD_ARGUMENT;
+    if (!bucket_offsets(first_offset, n_offsets) || query_offset < -FARTHEST || query_offset > FARTHEST) return MRF_ERR_BAD_ARGUMENT;
     const int64_t lowest = -(int64_t)(Q - 1) - query_offset, highest = (int64_t)(K - 1) - query_offset;
     if (lowest < first_offset || highest > first_offset + n_offsets - 1) return MRF_ERR_BAD_ARGUMENT;
     *map = bucket_of + (lowest - first_offset);
@@ -605,7 +608,7 @@ extern "C" {
 
 int mrf_distance_buckets(int32_t n_buckets, int64_t far_distance, int two_sided, int64_t first_offset, int64_t n_offsets, int32_t *bucket_of)
 {
-    if (n_buckets < 1 || n_buckets > 65536 || far_distance < 1 || n_offsets < 0) return MRF_ERR_BAD_ARGUMENT;
+    if (n_buckets < 1 || n_buckets > 65536 || far_distance < 1 || !bucket_offsets(first_offset, n_offsets)) return MRF_ERR_BAD_ARGUMENT;
     if (n_offsets == 0) return MRF_OK;
     if (!bucket_of) return MRF_ERR_NULL_POINTER;
     const int side = two_sided && n_buckets > 1 ? n_buckets / 2 : n_buckets;      // buckets of one sign

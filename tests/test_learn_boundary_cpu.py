@@ -139,3 +139,14 @@ def test_policy_backward_refusals():
     assert backward(c=None) == -1 and backward(a=None) == -1 and backward(A=None) == -1 and backward(up=None) == -1 and backward(grad=None) == -1
     assert backward(ws=None) == -1 and backward(size=need - 1) == -6
     assert backward(N=0, c=None, a=None, A=None, grad=None) == 0
+
+
+def test_distance_buckets_of_offsets_at_the_end_of_64_bits():
+    """Offsets that the sums of 64 bits would wrap around, or whose distance has no 64 bits, are refused like those of the calls that read the map."""
+    lib = mrf.load_library()
+    out = (ctypes.c_int32 * 8)()
+    f = lib.mrf_distance_buckets
+    far, last = 1 << 40, (1 << 63) - 1
+    assert f(8, 16, 1, last - 3, 8, out) == -12 and f(8, 16, 1, -last - 1, 1, out) == -12 and f(8, 16, 1, 1 << 62, 1, out) == -12
+    assert f(8, 16, 1, far + 1, 1, out) == -12 and f(8, 16, 1, -far - 1, 1, out) == -12 and f(8, 16, 1, 0, far + 1, None) == -12
+    assert f(8, 16, 1, far, 1, out) == 0 and out[0] == 7 and f(8, 16, 1, -far, 1, out) == 0 and out[0] == 3
