@@ -14,6 +14,7 @@ import argparse
 import os
 import sys
 
+import numpy as np
 import torch
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -43,7 +44,9 @@ def learn(steps=20, B=4, H=32, W=48, L=16, n_buckets=9, updates=3, seed=0, devic
     weight = torch.ones(L, device=device, requires_grad=True)
     bias = torch.zeros(L, device=device, requires_grad=True)
     values = torch.zeros(n_buckets, device=device, requires_grad=True)
-    bucket_of = torch.from_numpy(mrf.mrf_distance_buckets(n_buckets, L - 1, -(L - 1), 2 * L - 1)).to(device)
+    # a symmetric function: buckets of distances, whatever their sign, so that every value has one
+    lower = mrf.mrf_distance_buckets(n_buckets, L - 1, -(L - 1), L, two_sided=False)
+    bucket_of = torch.from_numpy(np.concatenate([lower, lower[-2::-1]])).to(device)
     optimizer = torch.optim.Adam([weight, bias, values], lr=0.05)
 
     def costs():

@@ -271,7 +271,8 @@ int mrf_layer_norm_backward(int64_t n_rows, int32_t C, const void *grad_y, int y
 /* The usual map of offsets d = first_offset, first_offset + 1, ... to buckets, for the two calls below.  Of the buckets of one
  * sign (all n_buckets, or with two_sided the lower half for d <= 0 and the upper half for d > 0; one-sided, d > 0 is taken
  * as d = 0) the first half hold one distance each, the others distances up to far_distance by their logarithm, and the last one
- * all beyond.
+ * all beyond.  With two_sided no offset has the upper half's bucket of distance 0 (of four buckets or more: there is no d > 0
+ * at distance 0), nor, of an odd number, the middle bucket: a table's values there are not used and their gradient is 0.
  *   bucket_of  HOST [n_offsets], assigned.  Host arithmetic.  A caller may as well make a map of its own.
  * first_offset within 2^40 of 0 and n_offsets up to 2^40, here and below, else MRF_ERR_BAD_ARGUMENT. */
 int mrf_distance_buckets(int32_t n_buckets, int64_t far_distance, int two_sided, int64_t first_offset, int64_t n_offsets, int32_t *bucket_of);

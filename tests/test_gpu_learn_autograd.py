@@ -264,3 +264,11 @@ def test_policy_loss_takes_views_and_refuses_to_drop_gradients():
         assert torch.equal(policy_loss(cost, *given, kl_weight=0.1)[0], want[0])
     loss = policy_loss(cost.detach(), *args, kl_weight=0.1)[0]
     assert not loss.requires_grad and torch.equal(loss, want[0])
+
+
+def test_every_pairwise_value_of_the_example_is_learned():
+    spec = importlib.util.spec_from_file_location("learn_by_reward", os.path.join(ROOT, "examples", "learn_by_reward.py"))
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    _, values, _ = example.learn(steps=2)
+    assert values.shape == (9,) and (values != 0).all(), values

@@ -123,3 +123,13 @@ def test_policy_limits():
     # nothing counts
     loss, logp, grad = lo.policy(c, a, np.ones(2), lp, None, np.zeros(2))
     assert (loss == 0).all() and (logp == 0).all() and (grad == 0).all()
+
+
+def test_distance_buckets_that_no_offset_has():
+    """Two-sided: the upper half's distance 0, where a half has more than one bucket, and the middle bucket of an odd number."""
+    for NB, empty in ((8, {4}), (9, {4, 5}), (32, {16}), (33, {16, 17}), (4, {2}), (3, {1}), (2, set()), (1, set())):
+        got = set(mrf.mrf_distance_buckets(NB, 200, -5000, 10001).tolist())
+        assert got == set(range(NB)) - empty, (NB, sorted(got))
+    # one-sided: every bucket has a distance
+    for NB in (1, 2, 9):
+        assert set(mrf.mrf_distance_buckets(NB, 15, -15, 16, two_sided=False).tolist()) == set(range(NB))
