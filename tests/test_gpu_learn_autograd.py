@@ -272,3 +272,41 @@ def test_every_pairwise_value_of_the_example_is_learned():
     spec.loader.exec_module(example)
     _, values, _ = example.learn(steps=2)
     assert values.shape == (9,) and (values != 0).all(), values
+
+
+@pytest.mark.parametrize("algo", ["isgmr", "trwp"])
+def test_bucket_tables_of_edges_through_the_message_passing(algo):
+    """Values per edge and bucket -> tables per edge -> message passing -> policy loss: the values' gradient is the sum, by bucket, of the one that
+    the same tables get as plain tensors."""
+    import torch
+    import paper_1910_10892_amd as mrf
+    from oracle import mrf_learn_oracle as lo
+    from paper_1910_10892_amd.autograd import bucket_pairwise, message_passing_edge_tables, policy_loss
+    rng = np.random.default_rng(8)
+    B, H, W, L, NB = 2, 6, 7, 5, 6
+    dirs = ((0, 1), (0, -1), (1, 0), (-1, 0))
+    m = mrf.mrf_distance_buckets(NB, L - 1, -(L - 1), 2 * L - 1)
+    put = lambda v: torch.from_numpy(v).cuda()
+    values = put(rng.random((len(dirs), B, H, W, NB)).astype(np.float32)).requires_grad_(True)
+    unary = put(rng.normal(size=(B, H, W, L)).astype(np.float32)).requires_grad_(True)
+    labels, A = put(rng.integers(0, L, (B, H, W)).astype(np.uint8)), put(rng.normal(size=B).astype(np.float32))
+    mask = put((rng.random((B, H, W)) < 0.8).astype(np.uint8))
+
+    def loss_of(tables):
+        cost, _ = message_passing_edge_tables(unary, tables, algo=algo, dirs=dirs, K=2, rho=[0.5] * 4 if algo == "trwp" else None)
+        return policy_loss(cost, labels, A, None, None, mask, pixels_per_advantage=H * W)[0]
+
+    tables = bucket_pairwise(values, put(m), -(L - 1), L, L)
+    loss = loss_of(tables)
+    loss.backward()
+    of_unary = unary.grad.clone()
+    want = lo.bucket_pairwise(values.detach().cpu().numpy().reshape(-1, NB), L, L, m, -(L - 1)).astype(np.float32)
+    np.testing.assert_array_equal(tables.detach().cpu().numpy().reshape(-1, L, L), want)
+    plain = put(want.reshape(len(dirs), B, H, W, L, L)).requires_grad_(True)
+    unary.grad = None
+    again = loss_of(plain)
+    again.backward()
+    assert torch.equal(loss, again) and torch.equal(of_unary, unary.grad)
+    grad, size = lo.bucket_pairwise_grad(plain.grad.cpu().numpy().reshape(-1, L, L), NB, m, -(L - 1))
+    assert np.abs(grad).max() > 1e-3
+    assert (np.abs(values.grad.cpu().numpy().reshape(-1, NB) - grad) <= 32 * 2.0 ** -24 * size).all()
