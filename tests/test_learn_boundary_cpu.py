@@ -150,3 +150,10 @@ def test_distance_buckets_of_offsets_at_the_end_of_64_bits():
     assert f(8, 16, 1, last - 3, 8, out) == -12 and f(8, 16, 1, -last - 1, 1, out) == -12 and f(8, 16, 1, 1 << 62, 1, out) == -12
     assert f(8, 16, 1, far + 1, 1, out) == -12 and f(8, 16, 1, -far - 1, 1, out) == -12 and f(8, 16, 1, 0, far + 1, None) == -12
     assert f(8, 16, 1, far, 1, out) == 0 and out[0] == 7 and f(8, 16, 1, -far, 1, out) == 0 and out[0] == 3
+
+
+def test_version_is_that_of_the_learning_operators():
+    """0.3.10 had none of them, and no MRF_ERR_BAD_ARGUMENT."""
+    assert tuple(int(v) for v in mrf.mrf_version().split(".")) >= (0, 3, 11)
+    for name in ("mrf_layer_norm_forward", "mrf_bucket_pairwise_forward", "mrf_softmin_logp", "mrf_softmin_policy", "mrf_softmin_policy_backward"):
+        assert hasattr(mrf.load_library(), name)
