@@ -511,14 +511,16 @@ void bucket_parts(MrfBucketParams &P)
     P.T = (int)((P.Q + (long long)MRF_BUCKET_STACK * P.TQ - 1) / (MRF_BUCKET_STACK * P.TQ));
 }
 
-// Many small matrices by whole chunks.  Few of them (below 4,096, or up to 16,384 of nearly 64 x 64 whose rows are whole chunks) are faster row by row from a
-// line, where no thread has an index to work out first (32 bits, chunks / lines: 2,048 of 16 x 16 5.7 / 4.9 us, of 64 x 64 20 / 8.4; 16,384 of
-// 64 x 64 58 / 49, of 63 x 63 58 / 68, of 24 x 24 11 / 25; 262,144 of 21 x 21 103 / 315).
+// Many small matrices by whole chunks.  Few of them (below 4,096, or in 32 bits up to 16,384, in 16 bits up to 8,192, of nearly 64 x 64 whose rows are whole
+// chunks) are faster row by row from a line, where no thread has an index to work out first.  Calls one behind the other, chunks / lines, 32 bits: 2,048 of 16 x 16 4.0 /
+// 3.9 us, of 64 x 64 21 / 9.5; 16,384 of 56 x 56 42 / 39, of 64 x 64 57 / 49, of 63 x 63 58 / 68, of 24 x 24 12 / 26; 262,144 of 21 x 21 92 to 103 / 309.
+// 16 bits: 2,048 of 64 x 64 19 / 7.1; 4,096 of 56 x 56 17.6 / 13.8; 8,192 of 56 x 56 21.4 / 21.5, of 64 x 64 25 / 21.5; 16,384 of 56 x 56 27 / 35, of 64 x 64
+// 32 / 35; 262,144 of 21 x 21 50 / 366.
 bool bucket_small_forward(const MrfBucketParams &P, int V)
 {
     const long long S = (long long)P.Q * P.K;
     if (S > MRF_BUCKET_SMALL || P.NB > MRF_BUCKET_LDS / 4 || P.G < 4096) return false;
-    return !(S >= 56 * 56 && P.K % V == 0 && P.G <= 16384);
+    return !(S >= 56 * 56 && P.K % V == 0 && P.G <= (V == 4 ? 16384 : 8192));
 }
 
 template <class T> int bucket_forward(MrfBucketParams P, hipStream_t st)

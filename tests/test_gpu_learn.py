@@ -998,3 +998,11 @@ def test_policy_labels_that_no_costs_allow(L, dtype):
     old[2] = float("nan")
     mrf.mrf_softmin_policy(cost, a, A, old, None, None, 0.2, 0.2, 0.0, loss, logp, grad, ws)
     assert loss[0].isnan()
+
+
+# ---- 16-bit matrices of nearly 64 x 64, on both sides of the number of groups at which the forward launch changes
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("G,L", [(8192, 56), (8193, 56), (8193, 64), (16385, 64)])
+def test_bucket_pairwise_of_thousands_of_16_bit_matrices(G, L, dtype):
+    _check_bucket(G, L, L, 16, dtype)
