@@ -25,7 +25,8 @@ __device__ inline int mrf_bucket_clamped(int b, int NB) { return b < 0 ? 0 : (b 
 
 // ---- forward, many small matrices (Q K <= 4096).  Four matrices are Q K chunks of four entries, whatever Q and K: a thread keeps the places in
 // the tables of the four entries of its chunks, in registers, and goes from four matrices to the next.  Chunks of neighbouring threads
-// are neighbours in memory, and no index is computed twice.  Bound by what it writes: 262,144 matrices of 21 x 21 in 32 bits 90 us (5.3 TB/s, tables included).
+// are neighbours in memory, and no index is computed twice.  Bound by what it writes: 262,144 matrices of 21 x 21 in 32 bits 85 to 90 us in a trace
+// of single passes (5.3 TB/s and more, tables included), 92 to 103 where calls follow each other at once.
 constexpr int MRF_BUCKET_SMALL = 4096, MRF_BUCKET_LDS = 4096, MRF_BUCKET_CHUNKS = 4;      // entries of a matrix; floats in LDS; chunks of a thread
 
 template <class T, int NT>
@@ -146,7 +147,7 @@ __global__ void __launch_bounds__(256) mrf_bucket_fwd_long(const MrfBucketParams
 
 // Many small matrices (Q, K <= 64): a wavefront takes as many as have room in its lanes, neighbours in memory, into LDS as whole chunks.  Lanes
 // j < K of a matrix go down its rows from column j on and begin again at column 0, so that none idles; where a lane begins again, a
-// diagonal's sum is complete.  Bound by memory: 262,144 matrices of 21 x 21 in 32 bits 98 us (4.9 TB/s; right behind a forward call 150, which includes that call's
+// diagonal's sum is complete.  Bound by memory: 262,144 matrices of 21 x 21 in 32 bits 96 us (5.0 TB/s; right behind a forward call 147 to 152, which includes that call's
 // writes on their way from the caches).
 constexpr int MRF_BUCKET_SIDE = 64, MRF_BUCKET_DIAG = 512, MRF_BUCKET_MANY = 512, MRF_BUCKET_WAVES = 2;      // Q, K; diagonals of a wavefront; buckets; wavefronts
 
@@ -488,7 +489,7 @@ void bucket_strides(MrfBucketParams &P, int heads_last)
 
 // Small matrices by the wavefront, unless they are few and not very small: then the workgroup's sort of the diagonals is most of the call, and a
 // workgroup for each matrix is faster (32-bit square matrices, one against the other: 64 sides 10.5 / 7.5 us for 1 matrix, 11.2 / 9.3 for 512, 15.8 / 29.8
-// for 2,048; 32 sides 7.0 / 7.2, 7.7 / 9.3, 7.8 / 27.4; 262,144 of 21 sides 98 / 3,106).
+// for 2,048; 32 sides 7.0 / 7.2, 7.7 / 9.3, 7.8 / 27.4; 262,144 of 21 sides 96 / 3,106).
 bool bucket_small_backward(const MrfBucketParams &P)
 {
     return P.Q <= MRF_BUCKET_SIDE && P.K <= MRF_BUCKET_SIDE && P.NB <= MRF_BUCKET_MANY && (P.G > 512 || (P.Q <= 32 && P.K <= 32));
@@ -534,7 +535,8 @@ template <class T> int bucket_forward(MrfBucketParams P, hipStream_t st)
         P.quads = 16;
         while (P.quads > 1 && (P.quads * 4 * P.NB > MRF_BUCKET_LDS || P.G < (S <= 256 * MRF_BUCKET_CHUNKS ? 2048LL : 16384LL) * P.quads)) P.quads /= 2;
         const long long need = (P.G + 4 * P.quads - 1) / (4 * P.quads);
-        // (256 threads where their chunks suffice: 2.4 million of 5 x 5 120 us, 355 with 1,024, of which 25 have work; 262,144 of 21 x 21 103 to 107 and 101)
+        // (256 threads where their chunks suffice: 2.4 million of 5 x 5 120 us, 355 with 1,024, of which 25 have work; 262,144 of 21 x 21,
+        // calls one behind the other, 103 to 107 and 101)
         if (S <= 256 * MRF_BUCKET_CHUNKS)
             hipLaunchKernelGGL((mrf_bucket_fwd_small<T, 256>), dim3((unsigned)(need < 2048 ? need : 2048)), dim3(256), 0, st, P);
         else

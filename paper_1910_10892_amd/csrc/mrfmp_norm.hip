@@ -17,8 +17,8 @@ struct MrfNormParams {
 };
 
 // ---- rows in registers: one reading of x (forward), of x and dy (backward).  The variance is the mean square of the differences from the
-// mean, both taken from the registers.  Some 10 operations an element forward and 14 backward: bound by memory.  479,232 x 192 in 32 bits
-// 135 us (5.5 TB/s, as a copy), 4,096 x 2,048 in 16 bits 10 us (three times a launch that does nothing).  A group of lanes has one row on its way at a
+// mean, both taken from the registers.  Some 12 operations an element forward and 14 backward: bound by memory.  479,232 x 192 in 32 bits
+// 130 to 135 us (5.5 TB/s and more, as a copy), 4,096 x 2,048 in 16 bits 11 us (three times a launch that does nothing).  A group of lanes has one row on its way at a
 // time; the other wavefronts of the compute unit are what hides its loads (with up to four rows 1 million of 16 in 32 bits 28 instead of 26 us).
 constexpr int mrf_norm_threads(int TL) { return TL <= 256 ? 256 : TL; }
 
@@ -143,8 +143,9 @@ template <int TL> __device__ inline float mrf_norm_across(float v)
 constexpr int mrf_norm_bwd_threads(int TL) { return TL <= 64 ? 512 : 1024; }
 
 // The sums over rows stay in registers while a workgroup goes through its rows, and end as one partial sum per workgroup and column: x and dy are read
-// once, and no column is summed in an order that depends on the run.  Bound by memory: 1,048,576 x 21 (x in 16 bits, dy in 32) 41 us (4.6 TB/s; rows of
-// LDS tiles 55), 4,096 x 2,048 in 16 bits 15.5 us and 3.8 for the sum over workgroups.
+// once, and no column is summed in an order that depends on the run.  Bound by memory: 1,048,576 x 21 (x in 16 bits, dy in 32) 40 us (4.7 TB/s; rows of
+// LDS tiles 55), 4,096 x 2,048 in 16 bits 16 us and 3.9 for the sum over workgroups: a row of a workgroup passes two barriers one after the other, and nothing
+// of the next row is on its way meanwhile.
 template <class X, class Y, int TL, int V, int CH>
 __global__ void __launch_bounds__(mrf_norm_bwd_threads(TL)) mrf_norm_bwd(const MrfNormParams Q)
 {
@@ -236,9 +237,9 @@ __global__ void __launch_bounds__(mrf_norm_bwd_threads(TL)) mrf_norm_bwd(const M
 }
 
 // ---- a wavefront per row: any length (rows of more than 16,384 columns forward, 12,288 backward, for which a workgroup has no registers).  Three
-// readings, the second and third from the caches for the most part: 1,000 rows of 12,000 in 32 bits 178 and 194 us, 22 and 54 in registers.  A lane adds
-// up as many as 2^25 values one after the other: in 64 bits (backward, 1,000 x 20,000 in 16 bits: 345 us with sums in 32 bits, 366 in 64, 286 two columns
-// at a time).
+// readings, the second and third from the caches for the most part: 1,000 rows of 20,000 in 32 bits 345 us forward and 305 backward (198 + 39 + 19 of kernels),
+// where 12,000 in registers take 26 and 53.  A lane adds up as many as 2^25 values one after the other: in 64 bits (backward, 1,000 x 20,000 in 16 bits:
+// 345 us with sums in 32 bits, 366 in 64, 286 two columns at a time).
 template <class X, class Y>
 __global__ void __launch_bounds__(256) mrf_norm_fwd_any(const MrfNormParams Q)
 {

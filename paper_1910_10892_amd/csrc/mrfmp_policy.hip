@@ -5,7 +5,10 @@
 #include <type_traits>
 
 constexpr int MRF_POLICY_BLOCKS = 4096;      // workgroups at most: partial sums of the loss
-constexpr int MRF_POLICY_LONG_THREADS = 262144;      // threads of a launch over long rows: 1,024 a compute unit (twice that: 70.8 instead of 66.0 us, 2,047 rows of 32,000)
+// Threads of a launch over long rows: 1,024 a compute unit.  Calls one behind the other with half of that / that / twice that: 16 bits, 2,047 rows of 3,000
+// 16 / 14 / 16 us, of 8,000 27 / 24 / 26, of 12,000 33 / 36 / 39, of 32,000 94 / 64 / 69, 513 of 32,000 39 / 32 / 30, 10,000 of 16,000 254 / 142 / 142; 32 bits,
+// 2,047 of 8,000 30 / 28 / 31, of 12,000 39 / 42 / 46, of 32,000 117 / 109 / 108, 10,000 of 16,000 277 / 242 / 235.
+constexpr int MRF_POLICY_LONG_THREADS = 262144;
 constexpr int MRF_POLICY_COUNTS = 256;       // workgroups that count the mask
 
 struct MrfPolicyParams {

@@ -1006,3 +1006,37 @@ def test_policy_labels_that_no_costs_allow(L, dtype):
 @pytest.mark.parametrize("G,L", [(8192, 56), (8193, 56), (8193, 64), (16385, 64)])
 def test_bucket_pairwise_of_thousands_of_16_bit_matrices(G, L, dtype):
     _check_bucket(G, L, L, 16, dtype)
+
+
+def test_policy_gradient_alone_replayed_from_a_graph():
+    """The factor is read when the graph runs, not when it is captured."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    N, L = 3000, 21
+    rng = np.random.default_rng(13)
+    cost = _put(rng.normal(size=(N, L)), "bfloat16")
+    a, A, old = _put(rng.integers(0, L, N), "uint8"), _put(rng.normal(size=N), "float32"), _put(rng.normal(-3, 0.3, N), "float32")
+    mask = _put(rng.integers(0, 2, N), "uint8")
+    up, grad = torch.ones(1, device="cuda:0"), torch.empty_like(cost)
+    ws = torch.empty(mrf.mrf_softmin_policy_workspace_bytes(), dtype=torch.uint8, device="cuda:0")
+    step = lambda: mrf.mrf_softmin_policy_backward(cost, a, A, old, None, mask, 0.2, 0.2, 0.0, up, grad, ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for factor in (1.0, 65536.0, -0.3):
+        up.fill_(factor)
+        mask.copy_(1 - mask)
+        step()
+        torch.cuda.synchronize()
+        want = grad.clone()
+        grad.fill_(float("nan"))
+        ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(grad, want), factor
