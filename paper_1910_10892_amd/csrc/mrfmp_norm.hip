@@ -18,13 +18,17 @@ struct MrfNormParams {
 
 // ---- rows in registers: one reading of x (forward), of x and dy (backward).  The variance is the mean square of the differences from the
 // mean, both taken from the registers.  Some 12 operations an element forward and 14 backward: bound by memory.  479,232 x 192 in 32 bits
-// 130 to 135 us (5.5 TB/s and more, as a copy), 4,096 x 2,048 in 16 bits 11 us (three times a launch that does nothing).  A group of lanes has one row on its way at a
+// 130 to 135 us (5.5 TB/s and more, as a copy), 4,096 x 2,048 in 16 bits 10 us (three times a launch that does nothing).  A group of lanes has one row on its way at a
 // time; the other wavefronts of the compute unit are what hides its loads (with up to four rows 1 million of 16 in 32 bits 28 instead of 26 us).
 constexpr int mrf_norm_threads(int TL) { return TL <= 256 ? 256 : TL; }
 
 // What the mean of 32 bits is off by, the mean `left` of the differences from it, is small but as large as the contrast of a row far from 0
-// (constant rows of 1,000.1 came out as 0.06): it is taken off the differences, and its square off their mean square (never below 0 but for
-// its rounding; NaN stays).
+// (constant rows of 1,000.1 would come out as 0.06): it is taken off the differences, and its square off their mean square (never below 0 but for
+// its rounding; NaN stays).  It is a second sum over the row.  Not for 16-bit rows of up to 8,192 columns: where their contrast is small against their
+// level, all are multiples of one 2^-11th of it, and a sum of 2^13 of them has room in 32 bits; what the product with 1 / C lost is then what
+// is left of the sum (4,096 x 2,048 in 16 bits 10.1 us instead of 10.7 with the second sum; 9.9 with neither).
+template <class X> constexpr bool mrf_norm_exact(int longest) { return sizeof(X) == 2 && longest <= 8192; }
+
 __device__ inline float mrf_norm_variance(float square, float left)
 {
     const float v = fmaf(-left, left, square);
@@ -58,20 +62,25 @@ __global__ void __launch_bounds__(mrf_norm_threads(TL)) mrf_norm_fwd(const MrfNo
         float s = 0.0f;
 #pragma unroll
         for (int e = 0; e < Row::E; ++e) s += x[e];
-        const float mu = Row::sum(s, scratch) * inv;
+        const float total = Row::sum(s, scratch), mu = total * inv;
         float left = 0.0f;
         s = 0.0f;
 #pragma unroll
         for (int e = 0; e < Row::E; ++e) {
             x[e] = fmaf(-mu, in_row[e], x[e]);
-            left += x[e];
+            if constexpr (!mrf_norm_exact<X>(Row::W)) left += x[e];
             s = fmaf(x[e], x[e], s);
         }
-        Row::sums(left, s, pairs);
-        left *= inv;
-        const float rs = rsqrtf(mrf_norm_variance(s * inv, left) + Q.eps);
+        if constexpr (mrf_norm_exact<X>(Row::W)) {
+            left = fmaf(-mu, (float)C, total) * inv;
+            s = Row::sum(s, (float *)pairs);
+        } else {
+            Row::sums(left, s, pairs);
+            left *= inv;
+        }
+        const float rs = rsqrtf(mrf_norm_variance(s * inv, left) + Q.eps), off = -left * rs;
 #pragma unroll
-        for (int e = 0; e < Row::E; ++e) x[e] = fmaf((x[e] - left) * rs, gamma[e], beta[e]);
+        for (int e = 0; e < Row::E; ++e) x[e] = fmaf(fmaf(x[e], rs, off), gamma[e], beta[e]);
         if (FAST || first + group < Q.N) {
             Row::store((Y *)Q.y + (size_t)first * C + mine, C, l, x);
             if (l == 0 && Q.mean) Q.mean[first + group] = mu + left;
@@ -105,19 +114,19 @@ __global__ void __launch_bounds__(256) mrf_norm_fwd_tile(const MrfNormParams Q)
         float s = 0.0f;
 #pragma unroll
         for (int e = 0; e < E; ++e) s += x[e];
-        const float mu = Tile::sum(s) * inv;
+        const float total = Tile::sum(s), mu = total * inv;
         float left = 0.0f;
         s = 0.0f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             x[e] = Tile::column(l, e) < C ? x[e] - mu : 0.0f;
-            left += x[e];
+            if constexpr (!mrf_norm_exact<X>(Tile::W)) left += x[e];
             s = fmaf(x[e], x[e], s);
         }
-        left = Tile::sum(left) * inv;
-        const float rs = rsqrtf(mrf_norm_variance(Tile::sum(s) * inv, left) + Q.eps);
+        left = (mrf_norm_exact<X>(Tile::W) ? fmaf(-mu, (float)C, total) : Tile::sum(left)) * inv;
+        const float rs = rsqrtf(mrf_norm_variance(Tile::sum(s) * inv, left) + Q.eps), off = -left * rs;
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = fmaf((x[e] - left) * rs, gamma[e], beta[e]);
+        for (int e = 0; e < E; ++e) x[e] = fmaf(fmaf(x[e], rs, off), gamma[e], beta[e]);
         mrf_wave_lds_fence();
         Tile::put((Y *)lds[wv], g, C, l, x);
         mrf_wave_lds_fence();

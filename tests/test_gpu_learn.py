@@ -1040,3 +1040,34 @@ def test_policy_gradient_alone_replayed_from_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(grad, want), factor
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("C", [5, 21, 63, 100, 250, 257, 1000, 2047, 4095, 8191, 8193, 10001, 16383, 16384])
+def test_layer_norm_of_16_bit_rows_that_are_nearly_constant(C, dtype):
+    """Values with all bits of their type set, and a neighbour of theirs in one place (or in every other): the mean lies between two numbers of the
+    type, and its rounding in 32 bits would be as large as the contrast."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    from oracle import mrf_learn_oracle as lo
+    print("case layer norm, nearly constant", C, dtype, flush=True)
+    top, step = (2047.0, 1.0) if dtype == "float16" else (255.0, 1.0)
+    x = np.full((6, C), top, np.float32)
+    x[1, C // 2] -= step
+    x[2, ::2] -= step
+    x[3] = -x[1]
+    x[4] = 16 * x[0]
+    x[5, 0] = 0.0
+    xt = _put(x, dtype)
+    assert (_np(xt) == x).all()
+    y, mean, rstd = (torch.empty(s, device="cuda:0") for s in ((6, C), (6,), (6,)))
+    mrf.mrf_layer_norm_forward(xt, None, None, 1e-5, y, mean, rstd)
+    want, mu, rs = lo.layer_norm(x)
+    # what is left of the mean's error is SUM u of it, or of the contrast
+    left = (SUM * U) ** 2 * np.abs(x).max(1, keepdims=True) * rs[:, None]
+    h = np.abs(want)
+    bound = left + SUM * U * (h + h.mean(1, keepdims=True)) + h * SUM * U * (SUM * U * np.abs(x).max(1, keepdims=True) * rs[:, None]) ** 2
+    off = np.abs(_np(y) - want)
+    assert (off <= bound).all(), "off by %g, allowed %g" % (off[off > bound][0], bound[off > bound][0])
+    assert (np.abs(_np(mean) - mu) <= 1.01 * U * np.abs(mu) + (left + SUM * U * h.mean(1, keepdims=True))[:, 0] / rs).all()
+    _close(rstd, rs, SUM * U * rs * (1.0 + (SUM * U * np.abs(x).max(1) * rs) ** 2))
