@@ -239,8 +239,8 @@ int mrf_softmin_smooth_l1(int64_t n_pixels, int32_t L, const float *cost, const 
  *
  * Their tensors are dense and row-major like all others and need no alignment beyond that of their elements;
  * buffers of one call must not overlap.  Elements are of the types below; statistics, sums, parameters and
- * their gradients are 32 bits (sums over pixels that end in a loss, and over rows too long for registers, 64), and a value is rounded once, to
- * nearest, where it is stored.  No order of a sum depends on anything but the sizes, so results are the
+ * their gradients are 32 bits (sums over pixels that end in a loss, over norm rows too long for registers and over the diagonals of a long matrix 64), and a
+ * value is rounded once, to nearest, where it is stored.  No order of a sum depends on anything but the sizes, so results are the
  * same from run to run.  Rows, groups and pixels may be none (then nothing is read; gradients of parameters and the loss
  * are set to 0) and are at most 2^31 - 1, entries of a row (C, L, Q + K) at most 2^31 - 2^16; matrices may have more than 2^32 entries.  NaN and infinity in one row (group,
  * pixel) stay in its outputs and in the sums that it belongs to.  Asynchronous on hip_stream, nothing allocated, no memset:

@@ -407,7 +407,7 @@ __global__ void __launch_bounds__(256) mrf_bucket_bwd_diagonals(const MrfBucketP
     const int off = d - (Q - 1), top = off < 0 ? -off : 0, bottom = Q - 1 < P.K - 1 - off ? Q - 1 : P.K - 1 - off;
     for (long long g = blockIdx.y; g < P.G; g += gridDim.y) {
         const float *x = P.diagonals + (size_t)g * P.T * P.strips * n;
-        float s = 0.0f;
+        double s = 0.0;      // (of up to 2^22 parts)
 #pragma unroll 4
         for (int p = top / rows; p <= bottom / rows; ++p) {
             // slot i of strip k is the diagonal 256 k + i - (p + 1) rows + Q - 1: in three strips at most
@@ -417,21 +417,22 @@ __global__ void __launch_bounds__(256) mrf_bucket_bwd_diagonals(const MrfBucketP
                 const int k = k0 - v, i = i0 + v * MRF_BUCKET_STRIP;
                 const bool there = k >= 0 && k < P.strips && i < n;
                 const float y = x[there ? ((size_t)p * P.strips + k) * n + i : 0];
-                s += there ? y : 0.0f;
+                s += (double)(there ? y : 0.0f);
             }
         }
-        P.totals[g * D + d] = s;
+        P.totals[g * D + d] = (float)s;
     }
 }
 
-// A workgroup per bucket and group: the diagonals of that bucket, four of a thread's looked up at once.
+// A workgroup per bucket and group: the diagonals of that bucket, four of a thread's looked up at once.  A thread has as many as 2^23 diagonals: its
+// sum in 64 bits (in 32, 30 million entries of one sign in one row were off by 2e-4), those of the threads meet in 32.
 template <int NT>
 __global__ void __launch_bounds__(NT) mrf_bucket_bwd_sum(const MrfBucketParams P)
 {
     __shared__ float waves[NT / 64];
     const int D = P.T > 0 ? P.Q + P.K - 1 : 0, b = blockIdx.x;
     for (long long g = blockIdx.y; g < P.G; g += gridDim.y) {
-        float s = 0.0f;
+        double own = 0.0;
         for (int first = threadIdx.x; first < D; first += 4 * NT) {
             int bucket[4];
             float total[4];
@@ -442,9 +443,10 @@ __global__ void __launch_bounds__(NT) mrf_bucket_bwd_sum(const MrfBucketParams P
                 total[u] = P.totals[g * D + (d < D ? d : D - 1)];
             }
 #pragma unroll
-            for (int u = 0; u < 4; ++u) s += first + u * NT < D && mrf_bucket_clamped(bucket[u], P.NB) == b ? total[u] : 0.0f;
+            for (int u = 0; u < 4; ++u) total[u] = first + u * NT < D && mrf_bucket_clamped(bucket[u], P.NB) == b ? total[u] : 0.0f;
+            own += (double)((total[0] + total[1]) + (total[2] + total[3]));
         }
-        s = mrf_lanes_sum<64>(s);
+        float s = mrf_lanes_sum<64>((float)own);
         if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = s;
         __syncthreads();
         if (threadIdx.x < 64) {

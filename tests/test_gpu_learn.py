@@ -1071,3 +1071,53 @@ def test_layer_norm_of_16_bit_rows_that_are_nearly_constant(C, dtype):
     assert (off <= bound).all(), "off by %g, allowed %g" % (off[off > bound][0], bound[off > bound][0])
     assert (np.abs(_np(mean) - mu) <= 1.01 * U * np.abs(mu) + (left + SUM * U * h.mean(1, keepdims=True))[:, 0] / rs).all()
     _close(rstd, rs, SUM * U * rs * (1.0 + (SUM * U * np.abs(x).max(1) * rs) ** 2))
+
+
+# ---- the longest sums, of values that are all alike: every rounding of a chain in 32 bits would go the same way
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("L", [40001, 3000001, 30000001])
+def test_policy_of_long_rows_of_like_costs(L, dtype):
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    print("case policy, like costs", L, dtype, flush=True)
+    cost = torch.full((2, L), 0.1, device="cuda:0").to(getattr(torch, dtype))
+    cost[:, L // 3] = 0.0
+    a = torch.tensor([L // 3, L - 1], dtype=torch.int32, device="cuda:0")
+    A = torch.ones(2, device="cuda:0")
+    loss, logp, grad, alone = torch.empty(3, device="cuda:0"), torch.empty(2, device="cuda:0"), torch.empty_like(cost), torch.empty(2, device="cuda:0")
+    ws = torch.empty(mrf.mrf_softmin_policy_workspace_bytes(), dtype=torch.uint8, device="cuda:0")
+    mrf.mrf_softmin_policy(cost, a, A, None, None, None, 0.2, 0.2, 0.0, loss, logp, grad, ws, grad_scale=2.0)
+    mrf.mrf_softmin_logp(cost, a, alone)
+    c = float(cost[0, 0])
+    s = 1.0 + (L - 1) * np.exp(-c)
+    want = np.array([0.0, -c]) - np.log(s)
+    # one exponential (2 u and its argument's rounding), a sum as good as exact, a logarithm and two roundings of results of that size
+    bound = U * (4 + 4 * np.abs(want))
+    for got in (logp, alone):
+        assert (np.abs(_np(got) - want) <= bound).all(), (np.abs(_np(got) - want) / U, np.abs(want))
+    # slope -1 for both pixels: the probabilities of the labels that were not taken, but for the sign
+    f = np.array([1.0, np.exp(-c)]) / s
+    g = -_np(grad)
+    for row, at, other in ((0, L // 3, L - 2), (1, L - 1, L // 3)):
+        p = f[1] if row == 0 else f[0]
+        assert abs(g[row, other] - p) <= p * (16 * U + HALF_ULP[dtype] * 1.01)
+        assert abs(g[row, at] - (f[0 if row == 0 else 1] - 1.0)) <= 4 * U + HALF_ULP[dtype] * 1.01
+
+
+@pytest.mark.parametrize("Q,K", [(1, 70001), (1, 3000001), (1, 30000001), (3000001, 1), (30000001, 1), (5, 3000001)])
+def test_bucket_gradient_of_long_rows_of_like_entries(Q, K):
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    print("case bucket, like entries", Q, K, flush=True)
+    NB = 8
+    host = mrf.mrf_distance_buckets(NB, 1000, -(Q - 1), Q + K - 1)
+    m = torch.from_numpy(host).cuda()
+    g = torch.full((1, Q, K), 0.1, device="cuda:0")
+    grad = torch.empty((1, NB), device="cuda:0")
+    ws = torch.empty(mrf.mrf_bucket_pairwise_workspace_bytes(1, Q, K, NB), dtype=torch.uint8, device="cuda:0")
+    mrf.mrf_bucket_pairwise_backward(g, m, -(Q - 1), grad, ws)
+    d = np.arange(-(Q - 1), K)
+    entries = np.minimum(np.minimum(d + Q, K - d), min(Q, K))      # of a diagonal
+    want = np.bincount(host, weights=entries, minlength=NB) * float(np.float32(0.1))
+    _close(grad[0], want, 16 * U * want)
