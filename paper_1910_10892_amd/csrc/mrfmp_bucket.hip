@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(256) mrf_bucket_fwd_long(const MrfBucketParams
 
 // Many small matrices (Q, K <= 64): a wavefront takes as many as have room in its lanes, neighbours in memory, into LDS as whole chunks.  Lanes
 // j < K of a matrix go down its rows from column j on and begin again at column 0, so that none idles; where a lane begins again, a
-// diagonal's sum is complete.  Bound by memory: 262,144 matrices of 21 x 21 in 32 bits 96 us (5.0 TB/s; right behind a forward call 147 to 152, which includes that call's
+// diagonal's sum is complete.  Bound by memory: 262,144 matrices of 21 x 21 in 32 bits 96 to 100 us (4.7 to 5.0 TB/s; right behind a forward call 147 to 152, which includes that call's
 // writes on their way from the caches).
 constexpr int MRF_BUCKET_SIDE = 64, MRF_BUCKET_DIAG = 512, MRF_BUCKET_MANY = 512, MRF_BUCKET_WAVES = 2;      // Q, K; diagonals of a wavefront; buckets; wavefronts
 
