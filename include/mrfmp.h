@@ -343,6 +343,115 @@ int mrf_softmin_policy_backward(int64_t n_pixels, int32_t L, const void *cost, i
                                 const uint8_t *mask, float clip_low, float clip_high, float kl_weight, const float *grad_loss, void *grad_cost,
                                 void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* ---- Sequence operators: what carries information along a scanline, or any sequence, in front of the scores --------------------------
+ * Attention with a bias by distance (the table and the map of mrf_bucket_pairwise_forward, without the matrix), the norm and rotation of its queries
+ * and keys, and a gated recurrence.  What is said above of the learning operators' types, sums, roundings, order, NaN, streams and capture holds here
+ * too; in addition, inputs that come out of one projection may have strides: elements from one batch (row), token (step) and head to the
+ * next, 0 or more, the entries of a head (channels of a step) being neighbours.  Outputs and gradients are dense.  Lengths, offsets and positions of
+ * sequences are int32 on the DEVICE; a length is clamped to [0, the tensor's].  What lies behind a sequence's length is not read, NaN or not, and is 0 in outputs
+ * and gradients. */
+
+#define MRF_ATTENTION_LONGEST_HEAD 128
+#define MRF_NO_FIRST_OFFSET INT64_MIN
+#define MRF_NO_LAST_OFFSET INT64_MAX
+
+/* Attention of Q queries on K keys, in B batches, of Hq heads; Hq / Hk neighbouring heads share a head of keys and values.
+ * Key j counts for query i of batch b if  first_offset <= d <= last_offset  with  d = j - i - query_offset - query_offsets[b],
+ * i < q_lengths[b] and j < k_lengths[b].  last_offset = 0: causal.  first_offset = -(n - 1) as well: the n keys up to the query's own.  Over those keys
+ *   s(i,j) = scale q_i . k_j + table[h][bucket(d)],  lse_i = log sum_j exp(s(i,j)),  P(i,j) = exp(s(i,j) - lse_i),  out_i = sum_j P(i,j) v_j
+ * A query without a key: out_i = 0, lse_i = -infinity, no gradients.  A single query of a long cache (Q = 1, query_offset = its position) divides the keys
+ * among workgroups. */
+typedef struct {
+    int32_t B, Q, K, Hq, Hk, D;       /* D 1..MRF_ATTENTION_LONGEST_HEAD, Hk divides Hq; B, Q, K may be 0 */
+    int32_t type;                     /* of q, k, v, out and their gradients: MRF_F32, MRF_F16, MRF_BF16 */
+    float scale;                      /* > 0 and finite, else MRF_ERR_BAD_ARGUMENT */
+    const void *q, *k, *v;            /* DEVICE [B][Q][Hq][D], [B][K][Hk][D], [B][K][Hk][D] at strides q_stride .. */
+    int64_t q_stride[3], k_stride[3], v_stride[3];      /* batch, token, head */
+    int64_t first_offset, last_offset;
+    int64_t query_offset;             /* within 2^40 of 0, else MRF_ERR_BAD_ARGUMENT */
+    const int32_t *query_offsets;     /* DEVICE [B] or NULL (0) */
+    const int32_t *q_lengths, *k_lengths;      /* DEVICE [B] or NULL (Q, K) */
+    const float *table;               /* DEVICE [Hq][n_buckets], or [n_buckets][Hq] with heads_last, or NULL: no bias */
+    const int32_t *bucket_of;         /* DEVICE [n_offsets]: bucket of d = map_offset + n; clamped to [0, n_buckets).  A d before the map's first has that
+                                         one's bucket, one behind its last that one's */
+    int64_t map_offset, n_offsets;    /* within 2^41 of 0; 1..2^40 */
+    int32_t n_buckets, heads_last;    /* n_buckets 1..65536 */
+} mrf_attention;
+
+/* Bytes of DEVICE workspace (256-byte aligned) of the forward (backward = 0) or backward pass; 0 if the description is invalid, or none is needed.  Backward, with
+ * a table: an eighth of a byte for each pair of a query and a key, and a few for each query and key. */
+size_t mrf_attention_workspace_bytes(const mrf_attention *att, int backward);
+
+/*   out   DEVICE [B][Q][Hq][D], assigned
+ *   lse   DEVICE [B][Hq][Q] float or NULL, assigned: which the backward call reads */
+int mrf_attention_forward(const mrf_attention *att, void *out, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Its gradients; the probabilities are formed again, nothing of Q x K is kept:
+ *   dP(i,j) = grad_out_i . v_j,  dS(i,j) = P(i,j) (dP(i,j) - sum_j P(i,j) dP(i,j)),
+ *   grad_q_i = scale sum_j dS(i,j) k_j,  grad_k_j = scale sum_i dS(i,j) q_i,  grad_v_j = sum_i P(i,j) grad_out_i  (over the heads that share k_j, v_j too),
+ *   grad_table[h][n] = sum of dS(i,j) over batches and pairs of bucket n
+ *   grad_out, out, lse  DEVICE [B][Q][Hq][D], [B][Q][Hq][D], [B][Hq][Q]: the forward call's
+ *   grad_q, grad_k, grad_v  DEVICE, dense, each may be NULL, assigned
+ *   grad_table  DEVICE, laid out like table, or NULL, assigned */
+int mrf_attention_backward(const mrf_attention *att, const void *grad_out, const void *out, const float *lse, void *grad_q, void *grad_k, void *grad_v,
+                           float *grad_table, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Norm of queries and keys for each head, and their rotation by position, in one pass: for each head x of D entries
+ *   h = x / sqrt(sum x^2 / D + eps),  y = h gamma,  out = y with its first `rotary` entries turned in pairs (a, b), by the angle t of pair n:
+ *   (a cos t - b sin t, a sin t + b cos t),  t = (position + position_offset) inv_freq[n],
+ * pairs (n, n + rotary / 2), or (2 n, 2 n + 1) with interleaved.  Angles are formed in 64 bits.  The position is the token's place in its
+ * sequence, or given; with n_axes of them (row and column of a pixel, say) the first rotary / 2 / n_axes pairs turn by the first, and so on. */
+typedef struct {
+    int32_t B, T, Hq, Hk, D;          /* B T tokens; D 1..512; any but D may be 0 */
+    int32_t type;                     /* of q, k, the outputs and the gradients */
+    const void *q, *k;                /* DEVICE [B][T][Hq][D], [B][T][Hk][D] at strides */
+    int64_t q_stride[3], k_stride[3]; /* batch, token, head */
+    const float *gamma_q, *gamma_k;   /* DEVICE [D], each may be NULL (1) */
+    float eps;                        /* > 0 and finite */
+    int32_t rotary, interleaved;      /* rotary even, 0..D */
+    const float *inv_freq;            /* DEVICE [rotary / 2] */
+    const int32_t *positions;         /* DEVICE [B][T][n_axes], or NULL with one axis */
+    int32_t n_axes;                   /* divides rotary / 2 */
+    int64_t position_offset;          /* within 2^40 of 0 */
+} mrf_head_rotation;
+
+/* out_q, out_k  DEVICE [B][T][Hq][D], [B][T][Hk][D], assigned */
+int mrf_head_rotation_forward(const mrf_head_rotation *heads, void *out_q, void *out_k, void *hip_stream);
+
+/* Its gradients:  u = grad_out turned back, a = u gamma,  grad_x = (a - h sum a h / D) / sqrt(sum x^2 / D + eps),  grad_gamma = sum of u h over tokens and heads
+ *   grad_out_q, grad_out_k  DEVICE, dense
+ *   grad_q, grad_k  DEVICE, dense, grad_gamma_q, grad_gamma_k  DEVICE [D] float: each may be NULL, assigned
+ *   workspace  DEVICE, 256-byte aligned; may be NULL where neither grad_gamma_q nor grad_gamma_k is asked for */
+size_t mrf_head_rotation_workspace_bytes(int64_t n_tokens, int32_t Hq, int32_t Hk, int32_t D);
+int mrf_head_rotation_backward(const mrf_head_rotation *heads, const void *grad_out_q, const void *grad_out_k, void *grad_q, void *grad_k,
+                               float *grad_gamma_q, float *grad_gamma_k, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Gated linear recurrence along the T steps of x, z [n_outer][T][n_inner], from the first to the last, or with reverse from the last to the first:
+ *   a = 1 / (1 + exp(-z)),  h_t = a_t h_(t-1) + (1 - a_t) x_t  with complement,  a_t h_(t-1) + x_t without;  y_t = h_t,  h_(-1) = initial
+ * Scanlines of an image [B][H][W][C]: rows are n_outer = B H, T = W, n_inner = C; columns n_outer = B, T = H, n_inner = W C.  One step (T = 1) with initial and
+ * final_state is the form for single tokens.  The state is 32 bits from the first step to the last.
+ *   x, z    DEVICE of type, at strides {row, step} on the HOST, or NULL for dense ones
+ *   initial DEVICE [n_outer][n_inner] float or NULL (0)
+ *   lengths DEVICE [n_outer] int32 or NULL (T): steps of a row; with reverse its last is lengths - 1
+ *   y       DEVICE [n_outer][T][n_inner] of type, assigned
+ *   final_state DEVICE [n_outer][n_inner] float or NULL, assigned: the state behind the last step; may be `initial` itself
+ *   states  DEVICE [n_outer][mrf_gated_scan_states(T)][n_inner] float or NULL, assigned: what the backward call reads
+ *   workspace  DEVICE, at least mrf_gated_scan_workspace_bytes(..), 256-byte aligned; 0 bytes (and NULL) where there are many channels or few steps */
+int64_t mrf_gated_scan_states(int64_t T);
+size_t mrf_gated_scan_workspace_bytes(int64_t n_outer, int64_t T, int64_t n_inner);
+int mrf_gated_scan_forward(int64_t n_outer, int64_t T, int64_t n_inner, int type, const void *x, const int64_t *x_strides, const void *z,
+                           const int64_t *z_strides, int complement, int reverse, const float *initial, const int32_t *lengths, void *y,
+                           float *final_state, float *states, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Its gradients, from the last step to the first:  g_t = grad_y_t + a_(t+1) g_(t+1)  (the last one's: + grad_final),
+ *   grad_x = (1 - a) g  (g without complement),  grad_z = a (1 - a) g (h_(t-1) - x)  (g h_(t-1)),  grad_initial = a_0 g_0
+ *   grad_y  DEVICE, dense;  grad_final  DEVICE [n_outer][n_inner] float or NULL (0);  states: the forward call's
+ *   grad_x, grad_z  DEVICE, dense, grad_initial DEVICE [n_outer][n_inner] float (may be grad_final itself): each may be NULL, assigned */
+int mrf_gated_scan_backward(int64_t n_outer, int64_t T, int64_t n_inner, int type, const void *grad_y, const float *grad_final, const void *x,
+                            const int64_t *x_strides, const void *z, const int64_t *z_strides, int complement, int reverse,
+                            const int32_t *lengths, const float *states, void *grad_x, void *grad_z, float *grad_initial, void *workspace,
+                            size_t workspace_bytes, void *hip_stream);
+
 /* Some sweep layouts spread a scanline over several wavefronts that hand nodes to each other
  * through rings in on-chip memory.  A wavefront that still finds itself waiting for another four
  * seconds after its workgroup started (sweeps take milliseconds) ends at once, those that wait for it

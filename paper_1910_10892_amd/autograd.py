@@ -247,3 +247,153 @@ def softmin_logp(cost, labels):
     logp = torch.empty(cost.shape[:-1], dtype=torch.float32, device=cost.device)
     _m.mrf_softmin_logp(cost, labels.contiguous(), logp)
     return logp
+
+
+# ---- sequence operators in front of the scores
+
+
+def _dense_last(t):
+    """A tensor that the library takes as it is: parts of a projection stay where they are."""
+    return t if t.shape[-1] <= 1 or t.stride(-1) == 1 else t.contiguous()
+
+
+def _given(name, **tensors):
+    if torch.is_grad_enabled():
+        for what, t in tensors.items():
+            if t is not None and t.is_floating_point() and t.requires_grad:
+                raise ValueError("%s has no gradient with respect to %s: detach it" % (name, what))
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, table, how):
+        scale, band, query_offset, query_offsets, q_lengths, k_lengths, bucket_of, map_offset, heads_last = how
+        q, k, v = (_dense_last(t) for t in (q, k, v))
+        table = None if table is None else table.contiguous()
+        make = dict(first_offset=band[0], last_offset=band[1], query_offset=query_offset, query_offsets=query_offsets, q_lengths=q_lengths, k_lengths=k_lengths,
+                    bucket_of=bucket_of, map_offset=map_offset, heads_last=heads_last)
+        att = _m.MrfAttention(q, k, v, scale, table=table, **make)
+        B, Q, K, Hq, Hk, D = att.shape
+        out = torch.empty((B, Q, Hq, D), dtype=q.dtype, device=q.device)
+        lse = torch.empty((B, Hq, Q), dtype=torch.float32, device=q.device)
+        n = _m.mrf_attention_workspace_bytes(att, False)
+        _m.mrf_attention_forward(att, out, lse, torch.empty(n, dtype=torch.uint8, device=q.device) if n else None)
+        ctx.save_for_backward(q, k, v, table, out, lse)
+        ctx.scale, ctx.make = scale, make
+        ctx.mark_non_differentiable(lse)
+        return out, lse
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_out, _grad_lse):
+        q, k, v, table, out, lse = ctx.saved_tensors
+        att = _m.MrfAttention(q, k, v, ctx.scale, table=table, **ctx.make)
+        dense = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
+        gq, gk, gv, gt = (dense(t) if need else None for t, need in zip((q, k, v, table), ctx.needs_input_grad[:4]))
+        ws = torch.empty(_m.mrf_attention_workspace_bytes(att, True), dtype=torch.uint8, device=q.device)
+        _m.mrf_attention_backward(att, grad_out.contiguous().to(q.dtype), out, lse, gq, gk, gv, gt, ws)
+        return gq, gk, gv, gt, None
+
+
+def attention(q, k, v, *, scale=None, causal=False, first_offset=None, last_offset=None, query_offset=0, query_offsets=None, q_lengths=None, k_lengths=None,
+              table=None, bucket_of=None, map_offset=0, heads_last=False):
+    """(out [B,Q,Hq,D], lse [B,Hq,Q]): attention of queries [B,Q,Hq,D] on keys and values [B,K,Hk,D] (float32, float16 or bfloat16, Hk divides Hq), as
+    mrf_attention_forward states it: scale 1 / sqrt(D) by default, a key counts where first_offset <= key - query - query_offset <= last_offset (causal: the
+    latter 0), bias table[head][bucket_of[offset - map_offset]].  Gradients flow from out to q, k, v and table; lse has none."""
+    if causal and last_offset is not None:
+        raise ValueError("causal and last_offset exclude each other")
+    query_offsets, q_lengths, k_lengths, bucket_of = (None if t is None else t.contiguous() for t in (query_offsets, q_lengths, k_lengths, bucket_of))
+    return _Attention.apply(q, k, v, table, (float(q.shape[-1] ** -0.5 if scale is None else scale), (first_offset, 0 if causal else last_offset), int(query_offset),
+                                             query_offsets, q_lengths, k_lengths, bucket_of, int(map_offset), bool(heads_last)))
+
+
+class _HeadRotation(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, gamma_q, gamma_k, how):
+        eps, inv_freq, positions, offset, interleaved = how
+        q, k = _dense_last(q), _dense_last(k)
+        gamma_q, gamma_k = (None if t is None else t.contiguous() for t in (gamma_q, gamma_k))
+        out_q, out_k = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+        _m.mrf_head_rotation_forward(q, k, gamma_q, gamma_k, eps, inv_freq, out_q, out_k, positions, offset, interleaved)
+        ctx.save_for_backward(q, k, gamma_q, gamma_k, inv_freq, positions)
+        ctx.how = eps, offset, interleaved
+        return out_q, out_k
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_q, grad_k):
+        q, k, gamma_q, gamma_k, inv_freq, positions = ctx.saved_tensors
+        eps, offset, interleaved = ctx.how
+        B, T, Hq, D = q.shape
+        gq, gk, ggq, ggk = (torch.empty(t.shape, dtype=t.dtype, device=t.device) if need and t is not None else None
+                            for t, need in zip((q, k, gamma_q, gamma_k), ctx.needs_input_grad[:4]))
+        ws = None
+        if ggq is not None or ggk is not None:
+            ws = torch.empty(_m.mrf_head_rotation_workspace_bytes(B * T, Hq, k.shape[2], D), dtype=torch.uint8, device=q.device)
+        _m.mrf_head_rotation_backward(grad_q.contiguous().to(q.dtype), grad_k.contiguous().to(q.dtype), q, k, gamma_q, gamma_k, eps, inv_freq, gq, gk, ggq, ggk, ws,
+                                      positions, offset, interleaved)
+        return gq, gk, ggq, ggk, None
+
+
+def head_rotation(q, k, gamma_q=None, gamma_k=None, *, eps=1e-6, inv_freq=None, positions=None, position_offset=0, interleaved=False):
+    """Queries [B,T,Hq,D] and keys [B,T,Hk,D], each head divided by its root mean square, times gamma_q and gamma_k [D] (float32 or None), and turned by position,
+    as mrf_head_rotation_forward states it: inv_freq [pairs] float32 (None: no turning), positions [B,T] or [B,T,axes] int32 or None (places in the
+    sequence).  Gradients flow to q, k, gamma_q and gamma_k."""
+    _given("head_rotation", inv_freq=inv_freq)
+    inv_freq, positions = (None if t is None else t.contiguous() for t in (inv_freq, positions))
+    return _HeadRotation.apply(q, k, gamma_q, gamma_k, (float(eps), inv_freq, positions, int(position_offset), bool(interleaved)))
+
+
+class _GatedScan(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, z, initial, lengths, how):
+        complement, reverse = how
+        x, z = _dense_last(x), _dense_last(z)
+        initial = None if initial is None else initial.contiguous()
+        outer, T, inner = x.shape
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        final = torch.empty((outer, inner), dtype=torch.float32, device=x.device)
+        states = None
+        if any(ctx.needs_input_grad[:3]):
+            states = torch.empty((outer, _m.mrf_gated_scan_states(T), inner), dtype=torch.float32, device=x.device)
+        ctx.ws_bytes = _m.mrf_gated_scan_workspace_bytes(outer, T, inner)
+        ws = torch.empty(ctx.ws_bytes, dtype=torch.uint8, device=x.device) if ctx.ws_bytes else None
+        _m.mrf_gated_scan_forward(x, z, initial, lengths, y, final, states, ws, complement, reverse)
+        ctx.save_for_backward(x, z, lengths, states)
+        ctx.how, ctx.carried = how, initial is not None
+        ctx.set_materialize_grads(False)
+        return y, final
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_y, grad_final):
+        x, z, lengths, states = ctx.saved_tensors
+        complement, reverse = ctx.how
+        outer, T, inner = x.shape
+        if grad_y is None:
+            grad_y = torch.zeros(x.shape, dtype=x.dtype, device=x.device)
+        grad_final = None if grad_final is None else grad_final.contiguous().float()
+        gx, gz = (torch.empty(x.shape, dtype=x.dtype, device=x.device) if need else None for need in ctx.needs_input_grad[:2])
+        gi = torch.empty((outer, inner), dtype=torch.float32, device=x.device) if ctx.carried and ctx.needs_input_grad[2] else None
+        ws = torch.empty(ctx.ws_bytes, dtype=torch.uint8, device=x.device) if ctx.ws_bytes else None
+        _m.mrf_gated_scan_backward(grad_y.contiguous().to(x.dtype), grad_final, x, z, lengths, states, gx, gz, gi, ws, complement, reverse)
+        return gx, gz, gi, None, None
+
+
+def gated_scan(x, z, initial=None, *, lengths=None, complement=True, reverse=False):
+    """(y [rows,T,channels], final [rows,channels] float32): h_t = a_t h_(t-1) + (1 - a_t) x_t with a = sigmoid(z) (complement=False: + x_t) along
+    T of x, z [rows,T,channels], as mrf_gated_scan_forward states it; initial [rows,channels] float32 or None, lengths [rows] int32 or None.  Gradients flow from
+    both to x, z and initial."""
+    return _GatedScan.apply(x, z, initial, None if lengths is None else lengths.contiguous(), (bool(complement), bool(reverse)))
+
+
+def scanline_scan(x, z, direction, *, complement=True):
+    """gated_scan along the scanlines of x, z [B,H,W,C] in one of the sweeps' directions (0, 1), (0, -1), (1, 0), (-1, 0), as the step (dh, dw) from a node to
+    the next: y [B,H,W,C]."""
+    dh, dw = (int(n) for n in direction)
+    if (dh, dw) not in ((0, 1), (0, -1), (1, 0), (-1, 0)):
+        raise ValueError("direction must be (0, 1), (0, -1), (1, 0) or (-1, 0)")
+    B, H, W, C = x.shape
+    rows = (B * H, W, C) if dw else (B, H, W * C)
+    y, _ = gated_scan(x.reshape(rows), z.reshape(rows), complement=complement, reverse=dh + dw < 0)
+    return y.view(B, H, W, C)

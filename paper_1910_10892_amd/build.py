@@ -1,4 +1,4 @@
-"""Build step of libmrfmp: twelve hipcc compilations side by side and a link, in-tree output next to
+"""Build step of libmrfmp: sixteen hipcc compilations side by side and a link, in-tree output next to
 the sources."""
 from __future__ import annotations
 
@@ -8,8 +8,9 @@ import subprocess
 CSRC = os.path.join(os.path.dirname(os.path.abspath(__file__)), "csrc")
 LIB_PATH = os.path.join(CSRC, "libmrfmp.so")
 SOURCES = ["mrfmp.hip"]
-LEARN_SOURCES = ["mrfmp_norm.hip", "mrfmp_bucket.hip", "mrfmp_policy.hip"]
-HEADERS = ["mrfmp_learn.h", "mrfmp_rows.h", "mrfmp_device.h", "mrfmp_fwd.h", "mrfmp_bwd.h", "mrfmp_bwd_sum.h", "mrfmp_head.h", "../../include/mrfmp.h"]
+LEARN_SOURCES = ["mrfmp_norm.hip", "mrfmp_bucket.hip", "mrfmp_policy.hip",
+                 "mrfmp_attention.hip", "mrfmp_attention_bwd.hip", "mrfmp_rotate.hip", "mrfmp_scan.hip"]
+HEADERS = ["mrfmp_attention.h", "mrfmp_learn.h", "mrfmp_rows.h", "mrfmp_device.h", "mrfmp_fwd.h", "mrfmp_bwd.h", "mrfmp_bwd_sum.h", "mrfmp_head.h", "../../include/mrfmp.h"]
 
 # -ffp-contract=off: the only fused multiply-add is the explicit one of the message update,
 #   so that floating point decisions (argmins) match a plain C evaluation order.
@@ -27,8 +28,8 @@ def is_stale() -> bool:
 
 def build(verbose: bool = False) -> str:
     """Compile libmrfmp.so for gfx950 (cross-compiles without a GPU): the sweeps' source as nine
-    translation units (the schedules, the entry points, a family of sweeps each) and a source per learning
-    operator side by side, then link."""
+    translation units (the schedules, the entry points, a family of sweeps each) and a source or two per
+    learning and sequence operator side by side, then link."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     objdir = os.path.join(CSRC, "_build")
     os.makedirs(objdir, exist_ok=True)

@@ -1,0 +1,270 @@
+// Shared by the attention's kernels, forward and backward: the problem on the device, products of 32 x 32 x 16 on the matrix unit for the three
+// element types, and tiles of rows in LDS.
+//
+// Products: an operand of 32 rows (columns) and 16 entries along the sum is 8 entries a lane: lane l has row l % 32 and, of the sum, entries that it
+// shares with no lane of the other half.  Which of the 16 these are does not matter as long as both operands agree.  The result's lane l
+// has column l % 32 and the rows 8 (e / 4) + 4 (l / 32) + e % 4 for e = 0 .. 15 -- so entries 8 t .. 8 t + 7 are, as they are, an operand of the next product
+// whose sum runs over those rows: rows 16 t + 4 half + {0, 1, 2, 3, 8, 9, 10, 11}.  Scores (keys x queries) so become an operand
+// of probabilities x values in registers, and the other operand is read in the same order of keys.  In 16 bits a product is one instruction, in 32
+// bits eight of 32 x 32 x 2.
+#pragma once
+
+#include "mrfmp_learn.h"
+
+typedef float mrf_acc __attribute__((ext_vector_type(16)));
+template <class T> struct MrfFrag { typedef T type __attribute__((ext_vector_type(8))); };
+
+__device__ inline mrf_acc mrf_mma(const MrfFrag<mrf_bf16>::type &a, const MrfFrag<mrf_bf16>::type &b, const mrf_acc &c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ inline mrf_acc mrf_mma(const MrfFrag<mrf_f16>::type &a, const MrfFrag<mrf_f16>::type &b, const mrf_acc &c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ inline mrf_acc mrf_mma(const MrfFrag<float>::type &a, const MrfFrag<float>::type &b, mrf_acc c)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+}
+
+__device__ inline int mrf_acc_row(int e, int half) { return 8 * (e / 4) + 4 * half + e % 4; }
+
+template <class T> __device__ inline typename MrfFrag<T>::type mrf_acc_frag(const mrf_acc &c, int t)
+{
+    typename MrfFrag<T>::type f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = mrf_from_f32<T>(c[8 * t + j]);
+    return f;
+}
+
+// PER entries from d on of a row of D that starts at `row`, 0 behind its end and where it is not `there`.  Nothing is left out by a branch: what is not
+// there is read from the row's start (its end) instead, so `row` has to be a row at any rate.
+template <int PER, class T> __device__ inline void mrf_load_part(const T *row, int d, int D, bool there, T (&v)[PER])
+{
+    typedef T vec __attribute__((ext_vector_type(PER), aligned(sizeof(T))));
+    if (D % PER == 0) {
+        there = there && d < D;
+        const vec x = *(const vec *)(row + (d < D ? d : 0));
+#pragma unroll
+        for (int j = 0; j < PER; ++j) v[j] = there ? x[j] : (T)0.0f;
+    } else {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const T x = row[d + j < D ? d + j : D - 1];
+            v[j] = there && d + j < D ? x : (T)0.0f;
+        }
+    }
+}
+
+template <class T> __device__ inline typename MrfFrag<T>::type mrf_load8(const T *row, int d, int D, bool there)
+{
+    T v[8];
+    mrf_load_part<8>(row, d, D, there, v);
+    typename MrfFrag<T>::type f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = v[j];
+    return f;
+}
+
+struct MrfAttnParams {
+    int B, Q, K, Hq, Hk, G, D;
+    float scale, c;                               // c = scale log2(e)
+    const void *q, *k, *v;
+    long long qs[3], ks[3], vs[3];
+    long long first, last, offset;
+    const int *offsets, *q_lengths, *k_lengths;
+    const float *table;
+    const int *bucket_of;
+    long long map_offset, n_offsets;
+    int n_buckets, heads_last;
+    void *out;
+    float *lse;
+    float *part;                                  // of keys divided among `splits`: maximum and sum [splits][rows][2], then [splits][rows][D]
+    int splits;
+    // backward
+    const void *dout;
+    void *dq, *dk, *dv;
+    float *delta;                                 // [B][Hq][Q]
+    float *lines, *diagonals, *dtable;
+    int strips, line;                             // strips of 32 keys; entries of a line
+};
+
+// What holds for a sequence: queries and keys that there are, and i + lo <= j <= i + hi for the keys j of query i
+struct MrfAttnBatch {
+    int nq, nk, lo, hi;
+    long long map;      // place in the map of j - i = 0
+    __device__ inline MrfAttnBatch(const MrfAttnParams &P, int b)
+    {
+        nq = P.Q;
+        nk = P.K;
+        if (P.q_lengths) nq = min(max(P.q_lengths[b], 0), P.Q);
+        if (P.k_lengths) nk = min(max(P.k_lengths[b], 0), P.K);
+        const long long o = P.offset + (P.offsets ? P.offsets[b] : 0);
+        const long long most = P.K, least = -(long long)P.Q - 1;
+        long long l = o + P.first, h = o + P.last;
+        lo = (int)(l < least ? least : l > most ? most : l);
+        hi = (int)(h < least ? least : h > most ? most : h);
+        map = -o - P.map_offset;
+    }
+    // keys that queries i0 .. i1 may see: [from, to)
+    __device__ inline int from(int i0) const { return max(i0 + lo, 0); }
+    __device__ inline int to(int i1) const { return min(i1 + hi + 1, nk); }
+};
+
+// the value of the bias at j - i = d, times log2(e); of head h
+__device__ inline float mrf_attn_bias(const MrfAttnParams &P, const MrfAttnBatch &s, int h, long long d)
+{
+    long long at = s.map + d;
+    at = at < 0 ? 0 : at >= P.n_offsets ? P.n_offsets - 1 : at;
+    int b = P.bucket_of[at];
+    b = b < 0 ? 0 : b >= P.n_buckets ? P.n_buckets - 1 : b;
+    return P.table[P.heads_last ? (size_t)b * P.Hq + h : (size_t)h * P.n_buckets + b] * 1.44269504088896340736f;
+}
+
+// Rows of a tensor in LDS: ROWS of DP entries, 16 bytes apart from one another's place in the banks.  A thread moves chunks of 16 bytes, which wait in
+// its registers between the load and the store.
+template <class T, int DP, int ROWS, int NT> struct MrfRows {
+    static constexpr int PER = 16 / (int)sizeof(T), LD = DP + PER, CHUNKS = ROWS * DP / PER, N = (CHUNKS + NT - 1) / NT;
+    typedef T vec __attribute__((ext_vector_type(PER)));
+    typedef T uvec __attribute__((ext_vector_type(PER), aligned(sizeof(T))));
+    vec r[N];
+
+    // rows from `at` on, `rows` (1 at least) of them; of a row D entries; the others are 0
+    __device__ inline void load(const T *at, long long stride, int rows, int D)
+    {
+        static_assert(CHUNKS % NT == 0, "chunks of a tile");
+        if (rows >= ROWS && D == DP) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int c = (int)threadIdx.x + n * NT, row = c / (DP / PER), d = c % (DP / PER) * PER;
+                const uvec u = *(const uvec *)(at + row * stride + d);
+#pragma unroll
+                for (int j = 0; j < PER; ++j) r[n][j] = u[j];
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int c = (int)threadIdx.x + n * NT, row = c / (DP / PER), d = c % (DP / PER) * PER;
+                T v[PER];
+                mrf_load_part<PER>(at + (row < rows ? row : 0) * stride, d, D, row < rows, v);
+#pragma unroll
+                for (int j = 0; j < PER; ++j) r[n][j] = v[j];
+            }
+        }
+    }
+    __device__ inline void store(T *lds) const
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int c = (int)threadIdx.x + n * NT, row = c / (DP / PER), d = c % (DP / PER) * PER;
+            *(vec *)(lds + row * LD + d) = r[n];
+        }
+    }
+    // operand whose 32 rows are rows row0 ..., and whose sum runs over 16 entries from d on
+    static __device__ inline typename MrfFrag<T>::type along(const T *lds, int row0, int d)
+    {
+        const int lane = threadIdx.x & 63;
+        const T *p = lds + (row0 + (lane & 31)) * LD + d + 8 * (lane >> 5);
+        if constexpr (sizeof(T) == 2) {
+            return *(const typename MrfFrag<T>::type *)p;
+        } else {
+            typename MrfFrag<T>::type f;
+            const vec a = *(const vec *)p, b = *(const vec *)(p + 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[j] = a[j], f[4 + j] = b[j];
+            return f;
+        }
+    }
+    // operand whose 32 rows are the entries d ..., and whose sum runs over rows row0 + 4 half + {0 .. 3, 8 .. 11}
+    static __device__ inline typename MrfFrag<T>::type across(const T *lds, int row0, int d)
+    {
+        const int lane = threadIdx.x & 63, half = lane >> 5;
+        typename MrfFrag<T>::type f;
+        if constexpr (sizeof(T) == 2) {
+            // the transposing read: of 16 lanes, four each point at a row's 16 entries, and each gets the four rows' values of one entry
+            typedef short v4 __attribute__((ext_vector_type(4)));
+            typedef short v8 __attribute__((ext_vector_type(8)));
+            const T *p = lds + (row0 + 4 * half + (lane >> 2 & 3)) * LD + d + (lane & 16) + 4 * (lane & 3);
+            const v4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4 *)p);
+            const v4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4 *)(p + 8 * LD));
+            const v8 ab = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+            f = __builtin_bit_cast(typename MrfFrag<T>::type, ab);
+        } else {
+            const T *p = lds + (row0 + 4 * half) * LD + d + (lane & 31);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = p[(8 * (j / 4) + j % 4) * LD];
+        }
+        return f;
+    }
+};
+
+// Probabilities are at most 1, and most of many keys far below: for a product in MRF_F16 they are taken times 2^15, where all that matter keep their digits
+// (2^-14, the least number with all of them, would be a probability already with 16,384 keys).
+template <class T> constexpr float mrf_attn_shift() { return 0.0f; }
+template <> constexpr float mrf_attn_shift<mrf_f16>() { return 15.0f; }
+template <class T> constexpr float mrf_attn_unshift() { return 1.0f; }
+template <> constexpr float mrf_attn_unshift<mrf_f16>() { return 0x1p-15f; }
+
+// sum (maximum) of the two halves of a wavefront, in both
+__device__ inline float mrf_halves_sum(float v) { return mrf_xor32_f32(v, true); }
+__device__ inline float mrf_halves_max(float v)
+{
+    const unsigned b = __builtin_bit_cast(unsigned, v);
+    const auto s = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    const unsigned u0 = s[0], u1 = s[1];
+    return fmaxf(__builtin_bit_cast(float, u0), __builtin_bit_cast(float, u1));
+}
+
+// What goes into a product in MRF_F16 and has no bound of its own (dS: gradients of any size, over any number of keys) is taken times a power of two,
+// a lane's own, as its column of the product is: the largest one that leaves its largest value so far in range.  What was summed follows where it
+// falls.  Other types have the range of 32 bits.
+template <class T> struct MrfRange {
+    float f = 1.0f, top = 0.0f;      // the factor; values up to `top` are in range with it
+    template <int N> __device__ inline void fit(mrf_acc &x, mrf_acc (&sums)[N])
+    {
+        if constexpr (sizeof(T) == 2 && mrf_attn_shift<T>() != 0.0f) {
+            float big = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) big = fmaxf(big, fabsf(x[e]));
+            big = mrf_halves_max(big);
+            if (__any(big > top)) {
+                if (big > top) {
+                    int ex = __builtin_amdgcn_frexp_expf(big);      // big < 2^ex
+                    ex = ex < -100 ? -100 : ex > 120 ? 120 : ex;
+                    const float g = ldexpf(1.0f, 15 - ex), r = top > 0.0f ? g / f : 0.0f;
+                    f = g;
+                    top = ldexpf(1.0f, ex);
+#pragma unroll
+                    for (int n = 0; n < N; ++n)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) sums[n][e] *= r;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e] *= f;
+        }
+    }
+    __device__ inline float undo() const { return 1.0f / f; }
+};
+
+// entries d .. d + 3 of a row of D
+template <class T> __device__ inline void mrf_store4(T *row, int d, int D, const float (&v)[4])
+{
+    typedef T vec __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    if (d + 4 <= D) {
+        vec x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = mrf_from_f32<T>(v[j]);
+        *(vec *)(row + d) = x;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (d + j < D) row[d + j] = mrf_from_f32<T>(v[j]);
+    }
+}
+
+namespace mrf_host {
+int attention_check(const mrf_attention *a, MrfAttnParams &P);
+}

@@ -1,0 +1,295 @@
+// Attention of heads with a bias by bucketed distance, forward (see mrf_attention_forward in the header for the formulas).
+//
+// A wavefront has 32 queries of a head (or of few queries those of all the heads that share keys), its workgroup goes through the keys that they may
+// see, tile after tile, in one pass: maximum and sum of the exponentials of a query run along, and what was summed is scaled where the
+// maximum rises.  Scores are formed as keys x queries, so that a lane has a single query: its maximum and sum are within two lanes, and its
+// probabilities are an operand of the second product as they are.
+#include "mrfmp_attention.h"
+
+#include <type_traits>
+
+// Keys of a tile: as many as two tiles of keys and values in LDS leave two workgroups (32 bits: one or two) on a compute unit.
+template <class T, int NW> constexpr int mrf_attn_keys() { return sizeof(T) == 4 || NW == 1 ? 32 : 64; }
+
+// NW wavefronts; PACK: a row is a query of a head of the group that shares keys (row = query G + head of the group), else a query of one head;
+// BIAS: with a table.
+template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launch_bounds__(64 * NW) mrf_attn_fwd(const MrfAttnParams P)
+{
+    constexpr int KT = mrf_attn_keys<T, NW>(), NT = 64 * NW, ROWS = 32 * NW, LINE = ROWS + KT;
+    typedef MrfRows<T, DP, KT, NT> Rows;
+    typedef typename MrfFrag<T>::type frag;
+    __shared__ __align__(16) T ldsK[2][KT * Rows::LD], ldsV[2][KT * Rows::LD];
+    __shared__ float line[2][BIAS && !PACK ? LINE : 1];
+    const int lane = threadIdx.x & 63, wv = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5;
+    const int heads = PACK ? P.Hk : P.Hq, rows = PACK ? P.Q * P.G : P.Q, blocks = (rows + ROWS - 1) / ROWS;
+    const int bh = blockIdx.x / blocks, block = blocks - 1 - (int)(blockIdx.x % blocks);      // (the longest rows of causal ones first)
+    const int b = bh / heads, h0 = bh % heads, hk = PACK ? h0 : h0 / P.G;
+    const MrfAttnBatch s(P, b);
+    const int r0 = block * ROWS, row = r0 + wv * 32 + (lane & 31);
+    const int i = PACK ? row / P.G : row, h = PACK ? hk * P.G + row % P.G : h0;
+    const bool there = row < rows && i < s.nq;
+    // queries of the workgroup and of the wavefront
+    const int i0 = PACK ? r0 / P.G : r0, i1 = min((PACK ? (r0 + ROWS - 1) / P.G : r0 + ROWS - 1), s.nq - 1);
+    const int w0 = PACK ? (r0 + wv * 32) / P.G : r0 + wv * 32, w2 = PACK ? (r0 + wv * 32 + 31) / P.G : r0 + wv * 32 + 31, w1 = min(w2, s.nq - 1);
+
+    frag qf[DP / 16] = {};
+    if (w0 <= w1) {
+        const T *q = (const T *)P.q + b * P.qs[0] + min(i, w1) * P.qs[1] + h * P.qs[2];
+#pragma unroll
+        for (int t = 0; t < DP / 16; ++t) qf[t] = mrf_load8(q, 16 * t + 8 * half, P.D, there);
+    }
+
+    int t0 = s.from(i0) / KT, t1 = i0 <= i1 ? (s.to(i1) + KT - 1) / KT : 0;
+    if (P.splits > 1 && t1 > t0) {
+        const int per = (t1 - t0 + P.splits - 1) / P.splits;
+        t0 += blockIdx.y * per;
+        t1 = min(t1, t0 + per);
+    }
+    const T *k = (const T *)P.k + b * P.ks[0] + hk * P.ks[2], *v = (const T *)P.v + b * P.vs[0] + hk * P.vs[2];
+    Rows kr, vr;
+    float bias_next = 0.0f;
+    const auto load = [&](int t) {
+        kr.load(k + (long long)t * KT * P.ks[1], P.ks[1], s.nk - t * KT, P.D);
+        vr.load(v + (long long)t * KT * P.vs[1], P.vs[1], s.nk - t * KT, P.D);
+        if constexpr (BIAS && !PACK)
+            if ((int)threadIdx.x < LINE) bias_next = mrf_attn_bias(P, s, h0, (long long)t * KT - r0 - (ROWS - 1) + (int)threadIdx.x);
+    };
+    const auto store = [&](int buf) {
+        kr.store(ldsK[buf]);
+        vr.store(ldsV[buf]);
+        if constexpr (BIAS && !PACK)
+            if ((int)threadIdx.x < LINE) line[buf][threadIdx.x] = bias_next;
+    };
+
+    mrf_acc o[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
+    float m = -INFINITY, l = 0.0f;      // maximum so far (in units of log2), and this lane's part of the sum
+
+    if (t0 < t1) {
+        load(t0);
+        store(0);
+    }
+    __syncthreads();
+    for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1, k0 = t * KT;
+        if (t + 1 < t1) load(t + 1);
+        if (w0 <= w1 && k0 < s.to(w1) && k0 + KT > s.from(w0)) {
+            mrf_acc c[KT / 32];
+#pragma unroll
+            for (int u = 0; u < KT / 32; ++u) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) c[u][e] = 0.0f;
+#pragma unroll
+                for (int d = 0; d < DP / 16; ++d) c[u] = mrf_mma(Rows::along(ldsK[buf], 32 * u, 16 * d), qf[d], c[u]);
+            }
+            // keys that this lane's query may see: [from, to) of the tile; all of them, for most tiles
+            const bool whole = k0 >= w1 + s.lo && k0 + KT - 1 <= w0 + s.hi && k0 + KT <= s.nk && (w2 == w1 || s.nq == P.Q);
+            const int from = i + s.lo - k0, to = there ? min(i + s.hi + 1, s.nk) - k0 : 0;
+            float top = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < KT / 32; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int j = 32 * u + mrf_acc_row(e, half);
+                    float x = c[u][e] * P.c;
+                    if constexpr (BIAS) {
+                        if constexpr (PACK) x += mrf_attn_bias(P, s, min(h, P.Hq - 1), (long long)k0 + j - i);
+                        else x += line[buf][ROWS - 1 + j - (wv * 32 + (lane & 31))];
+                    }
+                    if (!whole) x = j >= from && j < to ? x : -INFINITY;
+                    c[u][e] = x;
+                    top = fmaxf(top, x);
+                }
+            top = fmaxf(m, mrf_halves_max(top));
+            const float base = top == -INFINITY ? 0.0f : top, low = base - mrf_attn_shift<T>();
+            if (__any(top > m)) {
+                const float less = __builtin_amdgcn_exp2f(m - base);
+                l *= less;
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[d][e] *= less;
+                m = top;
+            }
+#pragma unroll
+            for (int u = 0; u < KT / 32; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    c[u][e] = __builtin_amdgcn_exp2f(c[u][e] - low);
+                    l += c[u][e];
+                }
+#pragma unroll
+            for (int u = 0; u < KT / 32; ++u)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const frag p = mrf_acc_frag<T>(c[u], x);
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) o[d] = mrf_mma(Rows::across(ldsV[buf], 32 * u + 16 * x, 32 * d), p, o[d]);
+                }
+        }
+        if (t + 1 < t1) store(buf ^ 1);
+        __syncthreads();
+    }
+
+    l = mrf_halves_sum(l) * mrf_attn_unshift<T>();
+    if (row >= rows) return;
+    if (P.splits > 1) {
+        const long long n = (long long)P.B * P.Hq * P.Q, at = ((long long)b * P.Hq + h) * P.Q + i;
+        float *const part = P.part + 2 * P.splits * n + (blockIdx.y * n + at) * P.D;
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                float x[4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) x[n] = o[d][e + n] * mrf_attn_unshift<T>();
+                mrf_store4(part, 32 * d + mrf_acc_row(e, half), P.D, x);
+            }
+        if (half == 0) ((float2 *)P.part)[blockIdx.y * n + at] = make_float2(m, l);
+        return;
+    }
+    const float inv = l > 0.0f ? mrf_attn_unshift<T>() / l : l;      // (no keys: 0; NaN stays)
+    T *const out = (T *)P.out + (((long long)b * P.Q + i) * P.Hq + h) * P.D;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const float x[4] = {o[d][e] * inv, o[d][e + 1] * inv, o[d][e + 2] * inv, o[d][e + 3] * inv};
+            mrf_store4(out, 32 * d + mrf_acc_row(e, half), P.D, x);
+        }
+    if (half == 0 && P.lse) P.lse[((long long)b * P.Hq + h) * P.Q + i] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+}
+
+// Parts of the keys, joined in their order.  A wavefront has a query of a head; sums of a part count 2^(its maximum - the largest).
+template <class T> __global__ void __launch_bounds__(256) mrf_attn_join(const MrfAttnParams P)
+{
+    const long long n = (long long)P.B * P.Hq * P.Q, at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (at >= n) return;
+    const int lane = threadIdx.x & 63;
+    const float2 *const ends = (const float2 *)P.part;
+    const float *const part = P.part + 2 * P.splits * n;
+    float top = -INFINITY, l = 0.0f;
+    for (int s = 0; s < P.splits; ++s) top = fmaxf(top, ends[s * n + at].x);
+    const float base = top == -INFINITY ? 0.0f : top;
+    for (int s = 0; s < P.splits; ++s) l += ends[s * n + at].y * __builtin_amdgcn_exp2f(ends[s * n + at].x - base);
+    const float inv = l > 0.0f ? 1.0f / l : l;
+    const long long bh = at / P.Q, i = at - bh * P.Q, b = bh / P.Hq, h = bh - b * P.Hq;
+    T *const out = (T *)P.out + ((b * P.Q + i) * P.Hq + h) * P.D;
+    for (int d = lane; d < P.D; d += 64) {
+        float x = 0.0f;
+        for (int s = 0; s < P.splits; ++s) x = fmaf(part[(s * n + at) * P.D + d], __builtin_amdgcn_exp2f(ends[s * n + at].x - base), x);
+        out[d] = mrf_from_f32<T>(x * inv);
+    }
+    if (lane == 0 && P.lse) P.lse[at] = l == 0.0f ? -INFINITY : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+}
+
+namespace mrf_host {
+
+int attention_check(const mrf_attention *a, MrfAttnParams &P)
+{
+    if (!a) return MRF_ERR_NULL_POINTER;
+    const long long most = 0x7fff0000LL;
+    if (a->B < 0 || a->Q < 0 || a->K < 0 || a->Hq < 1 || a->Hk < 1 || a->Hq % a->Hk || a->D < 1 || a->D > MRF_ATTENTION_LONGEST_HEAD) return MRF_ERR_BAD_SHAPE;
+    if (a->Q > most || a->K > most || a->Hq > 65536) return MRF_ERR_BAD_SHAPE;
+    if (a->B && (long long)a->Hq * ((a->Q + 31) / 32) > most / a->B) return MRF_ERR_BAD_SHAPE;
+    if (a->B && (long long)a->Hq * ((a->K + 31) / 32) > most / a->B) return MRF_ERR_BAD_SHAPE;
+    if (!known_type(a->type) || !(a->scale > 0.0f) || !(a->scale < INFINITY)) return MRF_ERR_BAD_ARGUMENT;
+    const long long far = 1LL << 40;
+    if (a->query_offset > far || a->query_offset < -far) return MRF_ERR_BAD_ARGUMENT;
+    for (int i = 0; i < 3; ++i)
+        if (a->q_stride[i] < 0 || a->k_stride[i] < 0 || a->v_stride[i] < 0) return MRF_ERR_BAD_ARGUMENT;
+    P.B = a->B; P.Q = a->Q; P.K = a->K; P.Hq = a->Hq; P.Hk = a->Hk; P.G = a->Hq / a->Hk; P.D = a->D;
+    P.scale = a->scale; P.c = a->scale * 1.44269504088896340736f;
+    P.q = a->q; P.k = a->k; P.v = a->v;
+    for (int i = 0; i < 3; ++i) P.qs[i] = a->q_stride[i], P.ks[i] = a->k_stride[i], P.vs[i] = a->v_stride[i];
+    // (what lies beyond 2^41 bounds nothing: no sum of these wraps around)
+    const long long edge = 1LL << 41;
+    P.first = a->first_offset < -edge ? -edge : a->first_offset > edge ? edge : a->first_offset;
+    P.last = a->last_offset < -edge ? -edge : a->last_offset > edge ? edge : a->last_offset;
+    P.offset = a->query_offset; P.offsets = a->query_offsets; P.q_lengths = a->q_lengths; P.k_lengths = a->k_lengths;
+    P.table = a->table; P.bucket_of = a->bucket_of; P.map_offset = a->map_offset; P.n_offsets = a->n_offsets; P.n_buckets = a->n_buckets;
+    P.heads_last = a->heads_last != 0;
+    if (a->table) {
+        if (a->n_buckets < 1 || a->n_buckets > 65536) return MRF_ERR_BAD_SHAPE;
+        if (a->map_offset > 2 * far || a->map_offset < -2 * far || a->n_offsets < 1 || a->n_offsets > far) return MRF_ERR_BAD_ARGUMENT;
+        if (!a->bucket_of) return MRF_ERR_NULL_POINTER;
+    }
+    return MRF_OK;
+}
+
+// Few rows on one head of keys: they go together, and the keys are divided so that there are enough workgroups.
+struct AttnPlan { bool pack; int splits; unsigned grid; };
+
+static AttnPlan attention_plan(const MrfAttnParams &P)
+{
+    const long long rows = (long long)P.Q * P.G;
+    if (P.Q > 16 && rows > 64) return {false, 1, (unsigned)((long long)P.B * P.Hq * ((P.Q + 127) / 128))};
+    const long long groups = (long long)P.B * P.Hk * ((rows + 31) / 32), tiles = (P.K + 31) / 32;
+    long long splits = groups ? 2048 / groups : 1;
+    if (splits > tiles / 4) splits = tiles / 4;
+    return {true, (int)(splits < 1 ? 1 : splits), (unsigned)groups};
+}
+
+static size_t attention_forward_bytes(const MrfAttnParams &P)
+{
+    const AttnPlan plan = attention_plan(P);
+    return plan.splits > 1 ? (size_t)plan.splits * P.B * P.Hq * P.Q * (P.D + 2) * sizeof(float) : 0;
+}
+
+template <class T, int DP> static int attention_go(const MrfAttnParams &P, const AttnPlan &plan, hipStream_t st)
+{
+    const dim3 grid(plan.grid, (unsigned)P.splits);
+    if (plan.pack) {
+        if (P.table) mrf_attn_fwd<T, DP, 1, true, true><<<grid, 64, 0, st>>>(P);
+        else mrf_attn_fwd<T, DP, 1, true, false><<<grid, 64, 0, st>>>(P);
+        if (P.splits > 1) mrf_attn_join<T><<<(unsigned)(((long long)P.B * P.Hq * P.Q + 3) / 4), 256, 0, st>>>(P);
+    } else {
+        if (P.table) mrf_attn_fwd<T, DP, 4, false, true><<<grid, 256, 0, st>>>(P);
+        else mrf_attn_fwd<T, DP, 4, false, false><<<grid, 256, 0, st>>>(P);
+    }
+    return launch_status("mrf_attn_fwd");
+}
+
+template <class T> static int attention_typed(const MrfAttnParams &P, const AttnPlan &plan, hipStream_t st)
+{
+    if (P.D <= 32) return attention_go<T, 32>(P, plan, st);
+    return P.D <= 64 ? attention_go<T, 64>(P, plan, st) : attention_go<T, 128>(P, plan, st);
+}
+
+size_t attention_backward_bytes(const MrfAttnParams &P);
+
+}  // namespace mrf_host
+
+using namespace mrf_host;
+
+extern "C" {
+
+size_t mrf_attention_workspace_bytes(const mrf_attention *att, int backward)
+{
+    MrfAttnParams P = {};
+    if (attention_check(att, P) != MRF_OK) return 0;
+    return backward ? attention_backward_bytes(P) : attention_forward_bytes(P);
+}
+
+int mrf_attention_forward(const mrf_attention *att, void *out, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    MrfAttnParams P = {};
+    const int rc = attention_check(att, P);
+    if (rc != MRF_OK || P.B == 0 || P.Q == 0) return rc;
+    if (!P.q || !out || (P.K && (!P.k || !P.v))) return MRF_ERR_NULL_POINTER;
+    const AttnPlan plan = attention_plan(P);
+    P.out = out; P.lse = lse; P.splits = plan.splits;
+    if (plan.splits > 1) {
+        if (!workspace) return MRF_ERR_NULL_POINTER;
+        if (workspace_bytes < attention_forward_bytes(P)) return MRF_ERR_WORKSPACE_TOO_SMALL;
+        P.part = (float *)workspace;
+    }
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (att->type == MRF_F32) return attention_typed<float>(P, plan, st);
+    return att->type == MRF_F16 ? attention_typed<mrf_f16>(P, plan, st) : attention_typed<mrf_bf16>(P, plan, st);
+}
+
+}  // extern "C"

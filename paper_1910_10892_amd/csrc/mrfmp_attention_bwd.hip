@@ -1,0 +1,460 @@
+// Attention, backward: the probabilities are formed again from the scores and the logarithm of their sum (see mrf_attention_backward in the header).
+//
+// Two launches, each with its sums in registers from the first tile to the last, so that none depends on what other workgroups do:
+//   queries  a workgroup has 128 queries of a head and goes through their keys:   scores, dP, dq.  It also sums dS over the keys, which is 0 but
+//            for the rounding of `out` in delta = sum(dout out): what it is not 0, r, is taken off delta, which is then good to 32 bits, and, times
+//            sum(P k), off dq (without that, dq in 16 bits was 1.8 times as far off as its own rounding makes it).
+//   keys     a workgroup has 128 keys of a head of keys and goes through the queries of all heads that share it:  scores, dP, dv, dk; and, for the table's
+//            gradient, sums of dS down the diagonals (below).
+// Five products would do; the scores and dP are formed twice, which spares sums over workgroups in an order that changes.
+#include "mrfmp_attention.h"
+
+#include <type_traits>
+
+template <class T> constexpr int mrf_attn_bwd_rows() { return sizeof(T) == 4 ? 32 : 64; }
+
+// ---- dq, and delta
+template <class T, int DP, bool BIAS> __global__ void __launch_bounds__(256) mrf_attn_bwd_queries(const MrfAttnParams P)
+{
+    constexpr int KT = mrf_attn_bwd_rows<T>(), NT = 256, ROWS = 128, LINE = ROWS + KT;
+    typedef MrfRows<T, DP, KT, NT> Rows;
+    typedef typename MrfFrag<T>::type frag;
+    __shared__ __align__(16) T ldsK[2][KT * Rows::LD], ldsV[2][KT * Rows::LD];
+    __shared__ float line[2][BIAS ? LINE : 1];
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5;
+    const int blocks = (P.Q + ROWS - 1) / ROWS, bh = blockIdx.x / blocks, block = blocks - 1 - (int)(blockIdx.x % blocks);
+    const int b = bh / P.Hq, h = bh % P.Hq, hk = h / P.G;
+    const MrfAttnBatch s(P, b);
+    const int r0 = block * ROWS, i = r0 + wv * 32 + (lane & 31);
+    const bool there = i < s.nq;
+    const int i1 = min(r0 + ROWS - 1, s.nq - 1), w0 = r0 + wv * 32, w1 = min(w0 + 31, s.nq - 1);
+    const long long row = (((long long)b * P.Q + i) * P.Hq + h) * P.D, stat = ((long long)b * P.Hq + h) * P.Q + i;
+
+    frag qf[DP / 16] = {}, gf[DP / 16] = {};
+    float delta = 0.0f;
+    if (w0 <= w1) {
+        const int at = min(i, w1);
+        const long long dense = (((long long)b * P.Q + at) * P.Hq + h) * P.D;
+        const T *q = (const T *)P.q + b * P.qs[0] + at * P.qs[1] + h * P.qs[2], *g = (const T *)P.dout + dense, *o = (const T *)P.out + dense;
+#pragma unroll
+        for (int t = 0; t < DP / 16; ++t) {
+            const int d = 16 * t + 8 * half;
+            qf[t] = mrf_load8(q, d, P.D, there);
+            gf[t] = mrf_load8(g, d, P.D, there);
+            const frag of = mrf_load8(o, d, P.D, there);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) delta = fmaf(mrf_to_f32((T)gf[t][j]), mrf_to_f32((T)of[j]), delta);
+        }
+        delta = mrf_halves_sum(delta);
+    }
+    // a query without keys has no probabilities: those formed with lse = +infinity are 0
+    float lse = there ? P.lse[stat] * 1.44269504088896340736f : INFINITY;
+    lse = lse == -INFINITY ? INFINITY : lse - mrf_attn_shift<T>();
+
+    const int t0 = s.from(r0) / KT, t1 = r0 <= i1 ? (s.to(i1) + KT - 1) / KT : 0;
+    const T *k = (const T *)P.k + b * P.ks[0] + hk * P.ks[2], *v = (const T *)P.v + b * P.vs[0] + hk * P.vs[2];
+    Rows kr, vr;
+    float bias_next = 0.0f;
+    const auto load = [&](int t) {
+        kr.load(k + (long long)t * KT * P.ks[1], P.ks[1], s.nk - t * KT, P.D);
+        vr.load(v + (long long)t * KT * P.vs[1], P.vs[1], s.nk - t * KT, P.D);
+        if constexpr (BIAS)
+            if ((int)threadIdx.x < LINE) bias_next = mrf_attn_bias(P, s, h, (long long)t * KT - r0 - (ROWS - 1) + (int)threadIdx.x);
+    };
+    const auto store = [&](int buf) {
+        kr.store(ldsK[buf]);
+        vr.store(ldsV[buf]);
+        if constexpr (BIAS)
+            if ((int)threadIdx.x < LINE) line[buf][threadIdx.x] = bias_next;
+    };
+    constexpr bool MEAN = sizeof(T) == 2;
+    mrf_acc dq[DP / 32], mean[MEAN ? DP / 32 : 1];      // sums of dS k, and of P k
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dq[d][e] = mean[MEAN ? d : 0][e] = 0.0f;
+    MrfRange<T> range;
+    float left = 0.0f;      // sum of dS
+
+    if (t0 < t1) {
+        load(t0);
+        store(0);
+    }
+    __syncthreads();
+    for (int t = t0; t < t1; ++t) {
+        const int buf = (t - t0) & 1, k0 = t * KT;
+        if (t + 1 < t1) load(t + 1);
+        if (w0 <= w1 && k0 < s.to(w1) && k0 + KT > s.from(w0)) {
+            const bool whole = k0 >= w1 + s.lo && k0 + KT - 1 <= w0 + s.hi && k0 + KT <= s.nk;
+            const int from = i + s.lo - k0, to = min(i + s.hi + 1, s.nk) - k0;
+#pragma unroll 1
+            for (int u = 0; u < KT / 32; ++u) {
+                mrf_acc c, dp;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) c[e] = dp[e] = 0.0f;
+#pragma unroll
+                for (int d = 0; d < DP / 16; ++d) {
+                    c = mrf_mma(Rows::along(ldsK[buf], 32 * u, 16 * d), qf[d], c);
+                    dp = mrf_mma(Rows::along(ldsV[buf], 32 * u, 16 * d), gf[d], dp);
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int j = 32 * u + mrf_acc_row(e, half);
+                    float x;
+                    if constexpr (BIAS) x = fmaf(c[e], P.c, line[buf][ROWS - 1 + j - (wv * 32 + (lane & 31))]) - lse;
+                    else x = fmaf(c[e], P.c, -lse);
+                    float p = __builtin_amdgcn_exp2f(x);
+                    if (!whole) p = j >= from && j < to ? p : 0.0f;
+                    c[e] = p;
+                    dp[e] = p * (dp[e] - delta);
+                    left += dp[e];
+                }
+                range.fit(dp, dq);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const frag sf = mrf_acc_frag<T>(dp, x), pf = mrf_acc_frag<T>(c, x);
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) {
+                        const frag kt = Rows::across(ldsK[buf], 32 * u + 16 * x, 32 * d);
+                        dq[d] = mrf_mma(kt, sf, dq[d]);
+                        if constexpr (MEAN) mean[d] = mrf_mma(kt, pf, mean[d]);
+                    }
+                }
+            }
+        }
+        if (t + 1 < t1) store(buf ^ 1);
+        __syncthreads();
+    }
+    left = mrf_halves_sum(left) * mrf_attn_unshift<T>();
+    if (i >= P.Q) return;
+    if (half == 0) P.delta[stat] = delta + left;
+    if (!P.dq) return;
+    T *const out = (T *)P.dq + row;
+    const float undo = range.undo(), scale = P.scale * mrf_attn_unshift<T>();
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            float x[4];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) x[n] = (MEAN ? fmaf(-left, mean[MEAN ? d : 0][e + n], dq[d][e + n] * undo) : dq[d][e + n]) * scale;
+            mrf_store4(out, 32 * d + mrf_acc_row(e, half), P.D, x);
+        }
+}
+
+// Query tiles that a workgroup of keys k0 .. goes through: those with a query that may see one of its keys
+template <int QT> __device__ inline void mrf_attn_query_tiles(const MrfAttnBatch &s, int k0, int &t0, int &t1)
+{
+    const int k1 = min(k0 + 128, s.nk) - 1;
+    const long long from = max((long long)k0 - s.hi, 0LL), to = min((long long)k1 - s.lo + 1, (long long)s.nq);
+    t0 = k0 <= k1 && from < to ? (int)(from / QT) : 0;
+    t1 = k0 <= k1 && from < to ? (int)((to + QT - 1) / QT) : 0;
+}
+
+// ---- dk, dv, sums of dS along diagonals
+//
+// TABLE: dS of 32 queries x 32 keys is put into LDS with each query's row moved by one against the next, so that a column holds a diagonal (places that none
+// falls on stay 0), and a lane sums a column.  A wavefront has 32 keys and goes through the queries upwards: of the 63 diagonals of a
+// block the later 31 go on in the next one, whose lanes are 32 less, and 32 are done and written.  An entry of the line: query - (key - first key) + 31.
+constexpr int MRF_SKEW = 71;      // from row to row: the halves of a wavefront, four rows apart, fall on the two halves of the banks
+
+template <class T, int DP, bool BIAS, bool TABLE> __global__ void __launch_bounds__(256) mrf_attn_bwd_keys(const MrfAttnParams P)
+{
+    constexpr int QT = mrf_attn_bwd_rows<T>(), NT = 256, KEYS = 128, LINE = KEYS + QT;
+    typedef MrfRows<T, DP, QT, NT> Rows;
+    typedef typename MrfFrag<T>::type frag;
+    __shared__ __align__(16) T ldsQ[2][QT * Rows::LD], ldsG[2][QT * Rows::LD];
+    __shared__ __align__(16) float ldsL[2][QT], ldsD[2][QT];
+    __shared__ float line[2][BIAS ? LINE : 1];
+    __shared__ float skew[TABLE ? 4 : 1][TABLE ? 32 * MRF_SKEW : 1];
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5;
+    const int blocks = (P.K + KEYS - 1) / KEYS, bh = blockIdx.x / blocks, block = (int)(blockIdx.x % blocks);
+    const int b = bh / P.Hk, hk = bh % P.Hk;
+    const MrfAttnBatch s(P, b);
+    const int k0 = block * KEYS, j = k0 + wv * 32 + (lane & 31), w0 = k0 + wv * 32, w1 = min(w0 + 31, s.nk - 1);
+    int t0, t1;
+    mrf_attn_query_tiles<QT>(s, k0, t0, t1);
+
+    frag kf[DP / 16] = {}, vf[DP / 16] = {};
+    if (w0 <= w1) {
+        const int at = min(j, w1);
+        const T *k = (const T *)P.k + b * P.ks[0] + at * P.ks[1] + hk * P.ks[2], *v = (const T *)P.v + b * P.vs[0] + at * P.vs[1] + hk * P.vs[2];
+#pragma unroll
+        for (int t = 0; t < DP / 16; ++t) {
+            kf[t] = mrf_load8(k, 16 * t + 8 * half, P.D, j < s.nk);
+            vf[t] = mrf_load8(v, 16 * t + 8 * half, P.D, j < s.nk);
+        }
+    }
+    if constexpr (TABLE)
+        for (int n = lane; n < 32 * MRF_SKEW; n += 64) skew[wv][n] = 0.0f;
+    mrf_acc dk[DP / 32], dv[DP / 32];
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dk[d][e] = dv[d][e] = 0.0f;
+
+    MrfRange<T> range;
+    Rows qr, gr;
+    float lse_next = 0.0f, delta_next = 0.0f, bias_next = 0.0f;
+    for (int g = 0; g < P.G; ++g) {
+        const int h = hk * P.G + g;
+        const T *q = (const T *)P.q + b * P.qs[0] + h * P.qs[2], *go = (const T *)P.dout + ((long long)b * P.Q * P.Hq + h) * P.D;
+        const long long stat = ((long long)b * P.Hq + h) * P.Q;
+        const auto load = [&](int t) {
+            qr.load(q + (long long)t * QT * P.qs[1], P.qs[1], s.nq - t * QT, P.D);
+            gr.load(go + (long long)t * QT * P.Hq * P.D, (long long)P.Hq * P.D, s.nq - t * QT, P.D);
+            if ((int)threadIdx.x < QT) {
+                const int i = t * QT + (int)threadIdx.x;
+                lse_next = i < s.nq ? P.lse[stat + i] * 1.44269504088896340736f : INFINITY;
+                lse_next = lse_next == -INFINITY ? INFINITY : lse_next - mrf_attn_shift<T>();
+                delta_next = i < s.nq ? P.delta[stat + i] : 0.0f;
+            }
+            if constexpr (BIAS)
+                if ((int)threadIdx.x < LINE) bias_next = mrf_attn_bias(P, s, h, (long long)k0 - t * QT - (QT - 1) + (int)threadIdx.x);
+        };
+        const auto store = [&](int buf) {
+            qr.store(ldsQ[buf]);
+            gr.store(ldsG[buf]);
+            if ((int)threadIdx.x < QT) {
+                ldsL[buf][threadIdx.x] = lse_next;
+                ldsD[buf][threadIdx.x] = delta_next;
+            }
+            if constexpr (BIAS)
+                if ((int)threadIdx.x < LINE) line[buf][threadIdx.x] = bias_next;
+        };
+        float *const to_line = TABLE ? P.lines + (((size_t)b * P.Hq + h) * P.strips + block * 4 + wv) * P.line : nullptr;
+        float goes_on = 0.0f;
+        if (t0 < t1) {
+            load(t0);
+            store(0);
+        }
+        __syncthreads();
+        for (int t = t0; t < t1; ++t) {
+            const int buf = (t - t0) & 1, q0 = t * QT;
+            if (t + 1 < t1) load(t + 1);
+            const int q1 = min(q0 + QT, s.nq) - 1;
+            const bool any = w0 <= w1 && q1 + s.hi >= w0 && q0 + s.lo <= w1;
+            const bool whole = any && w0 >= q1 + s.lo && w0 + 31 <= q0 + s.hi && q0 + QT <= s.nq && w0 + 32 <= s.nk;
+            // queries that may see this lane's key: [from, to) of the tile
+            const int from = j - s.hi - q0, to = j < s.nk ? min(j - s.lo + 1, s.nq) - q0 : 0;
+#pragma unroll 1
+            for (int u = 0; u < QT / 32; ++u) {
+                if (any) {
+                    mrf_acc c, dp;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) c[e] = dp[e] = 0.0f;
+#pragma unroll
+                    for (int d = 0; d < DP / 16; ++d) {
+                        c = mrf_mma(Rows::along(ldsQ[buf], 32 * u, 16 * d), kf[d], c);
+                        dp = mrf_mma(Rows::along(ldsG[buf], 32 * u, 16 * d), vf[d], dp);
+                    }
+#pragma unroll
+                    for (int e4 = 0; e4 < 16; e4 += 4) {
+                        const int r4 = 32 * u + mrf_acc_row(e4, half);
+                        const float4 L = *(const float4 *)&ldsL[buf][r4], D = *(const float4 *)&ldsD[buf][r4];
+                        const float lse[4] = {L.x, L.y, L.z, L.w}, delta[4] = {D.x, D.y, D.z, D.w};
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) {
+                            const int e = e4 + n, r = r4 + n;
+                            float x;
+                            if constexpr (BIAS) x = fmaf(c[e], P.c, line[buf][QT - 1 + (wv * 32 + (lane & 31)) - r]) - lse[n];
+                            else x = fmaf(c[e], P.c, -lse[n]);
+                            float p = __builtin_amdgcn_exp2f(x);
+                            if (!whole) p = r >= from && r < to ? p : 0.0f;
+                            c[e] = p;
+                            dp[e] = p * (dp[e] - delta[n]);
+                        }
+                    }
+                    if constexpr (TABLE) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const int r = mrf_acc_row(e, half);
+                            skew[wv][r * MRF_SKEW + r - (lane & 31) + 31] = dp[e];
+                        }
+                    }
+                    range.fit(dp, dk);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const frag pf = mrf_acc_frag<T>(c, x), sf = mrf_acc_frag<T>(dp, x);
+#pragma unroll
+                        for (int d = 0; d < DP / 32; ++d) {
+                            dv[d] = mrf_mma(Rows::across(ldsG[buf], 32 * u + 16 * x, 32 * d), pf, dv[d]);
+                            dk[d] = mrf_mma(Rows::across(ldsQ[buf], 32 * u + 16 * x, 32 * d), sf, dk[d]);
+                        }
+                    }
+                }
+                if constexpr (TABLE) {
+                    float sum = goes_on;
+                    if (any) {
+                        mrf_wave_lds_fence();
+#pragma unroll 8
+                        for (int r = 0; r < 32; ++r) sum += skew[wv][r * MRF_SKEW + lane];
+                        mrf_wave_lds_fence();
+                    }
+                    if (half == 0) to_line[q0 + 32 * u + lane] = sum * mrf_attn_unshift<T>();
+                    goes_on = __shfl(sum, lane | 32);
+                    if (half) goes_on = 0.0f;
+                }
+            }
+            if (t + 1 < t1) store(buf ^ 1);
+            __syncthreads();
+        }
+        if constexpr (TABLE)
+            if (half == 0 && t0 < t1) to_line[t1 * QT + lane] = goes_on * mrf_attn_unshift<T>();
+    }
+    if (j >= P.K) return;
+    const long long row = (((long long)b * P.K + j) * P.Hk + hk) * P.D;
+    const float ks = P.scale * mrf_attn_unshift<T>() * range.undo(), vs = mrf_attn_unshift<T>();
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const float x[4] = {dk[d][e] * ks, dk[d][e + 1] * ks, dk[d][e + 2] * ks, dk[d][e + 3] * ks};
+            const float y[4] = {dv[d][e] * vs, dv[d][e + 1] * vs, dv[d][e + 2] * vs, dv[d][e + 3] * vs};
+            if (P.dk) mrf_store4((T *)P.dk + row, 32 * d + mrf_acc_row(e, half), P.D, x);
+            if (P.dv) mrf_store4((T *)P.dv + row, 32 * d + mrf_acc_row(e, half), P.D, y);
+        }
+}
+
+// Sums of the lines along a diagonal, over the strips of keys that it crosses: [B][Hq][Q + K - 1], entry key - query + Q - 1
+template <int QT> __global__ void __launch_bounds__(256) mrf_attn_diagonals(const MrfAttnParams P)
+{
+    const long long n = (long long)P.Q + P.K - 1, blocks = (n + 255) / 256;
+    const long long bh = blockIdx.x / blocks, at = (blockIdx.x - bh * blocks) * 256 + threadIdx.x;
+    if (at >= n) return;
+    const MrfAttnBatch s(P, (int)(bh / P.Hq));
+    const float *const lines = P.lines + (size_t)bh * P.strips * P.line;
+    const long long offset = at - (P.Q - 1);
+    // strips whose keys have a query at that offset: key - offset in [0, Q)
+    const long long first = max(offset, 0LL) / 32, last = min(offset + P.Q - 1, (long long)P.K - 1) / 32;
+    float sum = 0.0f;
+    for (long long strip = first; strip <= last; ++strip) {
+        int t0, t1;
+        mrf_attn_query_tiles<QT>(s, (int)(strip / 4 * 128), t0, t1);
+        const long long entry = strip * 32 - offset + 31;
+        if (t0 < t1 && entry >= (long long)t0 * QT && entry < (long long)t1 * QT + 32) sum += lines[strip * P.line + entry];
+    }
+    P.diagonals[bh * n + at] = sum;
+}
+
+// Gradient of the table: a workgroup has 32 buckets of a head, 8 threads each; a diagonal's bucket is that of its offset.
+__global__ void __launch_bounds__(256) mrf_attn_buckets(const MrfAttnParams P)
+{
+    __shared__ float value[1024];
+    __shared__ int bucket[1024];
+    __shared__ float part[8][33];
+    const int blocks = (P.n_buckets + 31) / 32, h = blockIdx.x / blocks, w = threadIdx.x % 32, slice = threadIdx.x / 32;
+    const int mine = (int)(blockIdx.x % blocks) * 32 + w;
+    const long long n = P.B && P.Q && P.K ? (long long)P.Q + P.K - 1 : 0;
+    double sum = 0.0;
+    for (int b = 0; b < P.B; ++b) {
+        const MrfAttnBatch s(P, b);
+        for (long long base = 0; base < n; base += 1024) {
+            __syncthreads();
+            for (int x = threadIdx.x; x < 1024; x += 256) {
+                const long long at = base + x;
+                int k = -1;
+                if (at < n) {
+                    long long m = s.map + at - (P.Q - 1);
+                    m = m < 0 ? 0 : m >= P.n_offsets ? P.n_offsets - 1 : m;
+                    k = P.bucket_of[m];
+                    k = k < 0 ? 0 : k >= P.n_buckets ? P.n_buckets - 1 : k;
+                    value[x] = P.diagonals[((long long)b * P.Hq + h) * n + at];
+                }
+                bucket[x] = k;
+            }
+            __syncthreads();
+            for (int x = slice * 128; x < slice * 128 + 128; ++x)
+                if (bucket[x] == mine) sum += value[x];
+        }
+    }
+    part[slice][w] = (float)sum;
+    __syncthreads();
+    if (slice == 0 && mine < P.n_buckets) {
+        float total = 0.0f;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) total += part[x][w];
+        P.dtable[P.heads_last ? (size_t)mine * P.Hq + h : (size_t)h * P.n_buckets + mine] = total;
+    }
+}
+
+namespace mrf_host {
+
+static size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// a line for every strip of 32 keys: an entry for each query, as far as whole tiles reach, and 32 more
+static void attention_lines(MrfAttnParams &P)
+{
+    P.strips = (int)(((long long)P.K + 127) / 128 * 4);
+    P.line = (int)(((long long)P.Q + 63) / 64 * 64 + 32);
+}
+
+size_t attention_backward_bytes(const MrfAttnParams &given)
+{
+    MrfAttnParams P = given;
+    size_t n = round256((size_t)P.B * P.Hq * P.Q * sizeof(float));
+    if (P.table && P.Q && P.K) {
+        attention_lines(P);
+        n += round256((size_t)P.B * P.Hq * P.strips * P.line * sizeof(float)) + (size_t)P.B * P.Hq * ((size_t)P.Q + P.K - 1) * sizeof(float);
+    }
+    return n ? n : 256;
+}
+
+template <class T, int DP> static int attention_back(const MrfAttnParams &P, hipStream_t st)
+{
+    const bool pairs = P.B && P.Q && P.K;
+    if (P.B && P.Q) {
+        const unsigned grid = (unsigned)((long long)P.B * P.Hq * ((P.Q + 127) / 128));
+        if (P.table) mrf_attn_bwd_queries<T, DP, true><<<grid, 256, 0, st>>>(P);
+        else mrf_attn_bwd_queries<T, DP, false><<<grid, 256, 0, st>>>(P);
+    }
+    if (P.B && P.K && (P.dk || P.dv || P.dtable)) {
+        const unsigned grid = (unsigned)((long long)P.B * P.Hk * ((P.K + 127) / 128));
+        if (P.dtable && pairs) mrf_attn_bwd_keys<T, DP, true, true><<<grid, 256, 0, st>>>(P);
+        else if (P.table) mrf_attn_bwd_keys<T, DP, true, false><<<grid, 256, 0, st>>>(P);
+        else mrf_attn_bwd_keys<T, DP, false, false><<<grid, 256, 0, st>>>(P);
+    }
+    if (P.dtable) {
+        if (pairs) {
+            const long long n = ((long long)P.Q + P.K - 1 + 255) / 256;
+            mrf_attn_diagonals<mrf_attn_bwd_rows<T>()><<<(unsigned)(n * P.B * P.Hq), 256, 0, st>>>(P);
+        }
+        mrf_attn_buckets<<<(unsigned)P.Hq * ((P.n_buckets + 31) / 32), 256, 0, st>>>(P);
+    }
+    return launch_status("mrf_attn_bwd");
+}
+
+template <class T> static int attention_back_typed(const MrfAttnParams &P, hipStream_t st)
+{
+    if (P.D <= 32) return attention_back<T, 32>(P, st);
+    return P.D <= 64 ? attention_back<T, 64>(P, st) : attention_back<T, 128>(P, st);
+}
+
+}  // namespace mrf_host
+
+using namespace mrf_host;
+
+extern "C" {
+
+int mrf_attention_backward(const mrf_attention *att, const void *grad_out, const void *out, const float *lse, void *grad_q, void *grad_k, void *grad_v,
+                           float *grad_table, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    MrfAttnParams P = {};
+    const int rc = attention_check(att, P);
+    if (rc != MRF_OK) return rc;
+    if (grad_table && !P.table) return MRF_ERR_NULL_POINTER;
+    if (P.B && P.Q && (!P.q || !grad_out || !out || !lse)) return MRF_ERR_NULL_POINTER;
+    if (P.B && P.K && (!P.k || !P.v)) return MRF_ERR_NULL_POINTER;
+    if (!workspace) return MRF_ERR_NULL_POINTER;
+    if (workspace_bytes < attention_backward_bytes(P)) return MRF_ERR_WORKSPACE_TOO_SMALL;
+    P.dout = grad_out; P.out = (void *)out; P.lse = (float *)lse; P.dq = grad_q; P.dk = grad_k; P.dv = grad_v; P.dtable = grad_table;
+    attention_lines(P);
+    P.delta = (float *)workspace;
+    P.lines = (float *)((char *)workspace + round256((size_t)P.B * P.Hq * P.Q * sizeof(float)));
+    P.diagonals = (float *)((char *)P.lines + round256((size_t)P.B * P.Hq * P.strips * P.line * sizeof(float)));
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (att->type == MRF_F32) return attention_back_typed<float>(P, st);
+    return att->type == MRF_F16 ? attention_back_typed<mrf_f16>(P, st) : attention_back_typed<mrf_bf16>(P, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,454 @@
+// Gated linear recurrence along the middle index of [outer][T][inner], forward and backward (see mrf_gated_scan_forward in the header for the
+// formulas).
+//
+// A lane has V neighbouring channels and goes through their steps one after the other, MRF_SCAN_STEPS of them loaded ahead.  Some 20 operations
+// and two transcendental ones an element: bound by memory.  Where there are few channels the steps are divided into chunks: what a chunk
+// does to the state it gets is h -> A h + B, which a first launch finds, a second one strings together, and the third goes through the
+// steps again from the right state.  The states before every MRF_SCAN_STEPS-th step are kept for the backward pass, in 32 bits: it forms the steps
+// between them again in registers, whatever the type of y.
+#include "mrfmp_rows.h"
+
+#include <type_traits>
+
+#define MRF_SCAN_STEPS 16
+
+struct MrfScanParams {
+    long long outer, T, inner, groups, lanes;      // groups of V channels in a row of `inner`; lanes = outer groups
+    const void *x, *z, *dy;
+    long long x_outer, x_step, z_outer, z_step;    // elements from one row to the next
+    const int *lengths;
+    const float *start;                            // state before the first step (gradient behind the last): [outer][inner] or NULL
+    void *y, *dx, *dz;
+    float *end;                                    // state behind the last step (gradient before the first) or NULL
+    float *states;                                 // [outer][blocks][inner]
+    float2 *effect;                                // [chunks][outer inner]: A, B of a chunk
+    float *carry;                                  // [chunks][outer inner]: state that a chunk gets
+    long long chunk, blocks;
+    int chunks;
+};
+
+// The logistic function of z and of -z.  The exponential is of a number below 0, so neither loses digits; NaN stays.
+__device__ inline void mrf_gate(float z, float &a, float &rest)
+{
+    const float e = __builtin_amdgcn_exp2f(fabsf(z) * -1.44269504088896340736f);
+    const float r = __builtin_amdgcn_rcpf(1.0f + e), low = e * r;
+    a = z < 0.0f ? low : r;
+    rest = z < 0.0f ? r : low;
+}
+
+template <class X, int V> struct MrfScanLane {
+    typedef typename MrfVec<X, V>::type vec;
+    typedef typename MrfVec<float, V>::type fvec;
+    struct Raw { vec v[MRF_SCAN_STEPS]; };
+
+    long long index, o;      // of outer * inner; row
+    int n, i;                // steps that there are; first channel
+    bool there;
+
+    __device__ inline MrfScanLane(const MrfScanParams &P)
+    {
+        const long long lane = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+        there = lane < P.lanes;
+        o = there ? lane / P.groups : 0;
+        i = (int)(lane - o * P.groups) * V;
+        index = o * P.inner + i;
+        n = (int)P.T;
+        if (there && P.lengths) {
+            n = P.lengths[o];
+            n = n < 0 ? 0 : n > P.T ? (int)P.T : n;
+        }
+    }
+
+    // steps u .. u + MRF_SCAN_STEPS - 1 of rows `step` apart from `row0` on (the row of step 0); nothing from `end` on
+    __device__ inline void load(const X *row0, long long step, long long u, long long end, Raw &r) const
+    {
+        const X *at = row0 + u * step;
+        if (u + MRF_SCAN_STEPS <= end) {
+#pragma unroll
+            for (int s = 0; s < MRF_SCAN_STEPS; ++s) r.v[s] = *(const vec *)(at + s * step);
+        } else {
+#pragma unroll
+            for (int s = 0; s < MRF_SCAN_STEPS; ++s) {
+                vec v;
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[j] = (X)0.0f;
+                if (u + s < end) v = *(const vec *)(at + s * step);
+                r.v[s] = v;
+            }
+        }
+    }
+
+    static __device__ inline void state(const float *at, float (&h)[V])
+    {
+        const fvec v = *(const fvec *)at;
+#pragma unroll
+        for (int j = 0; j < V; ++j) h[j] = v[j];
+    }
+    static __device__ inline void keep(float *at, const float (&h)[V])
+    {
+        fvec v;
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = h[j];
+        *(fvec *)at = v;
+    }
+    static __device__ inline void give(X *at, const float (&h)[V])
+    {
+        vec v;
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = mrf_from_f32<X>(h[j]);
+        *(vec *)at = v;
+    }
+};
+
+// rows of step 0 and the way from one step to the next
+template <class X, bool REV> struct MrfScanRows {
+    const X *row0;
+    long long step;
+    __device__ inline MrfScanRows(const void *base, long long outer, long long way, long long o, int n, int i)
+    {
+        row0 = (const X *)base + o * outer + i + (REV ? (long long)(n - 1) * way : 0);
+        step = REV ? -way : way;
+    }
+};
+
+template <class X, int V, bool COMPLEMENT, bool REV, bool EFFECT>
+__global__ void __launch_bounds__(256) mrf_scan_fwd(const MrfScanParams P)
+{
+    typedef MrfScanLane<X, V> Lane;
+    const Lane me(P);
+    if (!me.there) return;
+    const long long from = (long long)blockIdx.y * P.chunk, to = from + P.chunk < P.T ? from + P.chunk : P.T;
+    const long long last = me.n < to ? me.n : to;
+    float h[V], A[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) h[j] = 0.0f, A[j] = 1.0f;
+    if constexpr (!EFFECT) {
+        if (P.chunks > 1) Lane::state(P.carry + blockIdx.y * (P.outer * P.inner) + me.index, h);
+        else if (P.start) Lane::state(P.start + me.index, h);
+    }
+    const MrfScanRows<X, REV> x(P.x, P.x_outer, P.x_step, me.o, me.n, me.i), z(P.z, P.z_outer, P.z_step, me.o, me.n, me.i);
+    const long long dense = P.T * P.inner;
+    X *const y = (X *)P.y + me.o * dense + me.i;
+
+    const auto run = [&](const typename Lane::Raw &rx, const typename Lane::Raw &rz, const long long u) {
+        if constexpr (!EFFECT)
+            if (P.states) Lane::keep(P.states + (me.o * P.blocks + u / MRF_SCAN_STEPS) * P.inner + me.i, h);
+#pragma unroll
+        for (int s = 0; s < MRF_SCAN_STEPS; ++s) {
+            if (u + s < last) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    float a, rest;
+                    mrf_gate(mrf_to_f32((X)rz.v[s][j]), a, rest);
+                    const float v = mrf_to_f32((X)rx.v[s][j]);
+                    h[j] = fmaf(a, h[j], COMPLEMENT ? rest * v : v);
+                    A[j] *= a;
+                }
+                if constexpr (!EFFECT) Lane::give(y + (REV ? me.n - 1 - (u + s) : u + s) * P.inner, h);
+            } else if (!EFFECT && u + s < to) {
+                const float zero[V] = {};
+                Lane::give(y + (u + s) * P.inner, zero);
+            }
+        }
+    };
+    typename Lane::Raw xa, za, xb, zb;
+    if (from < to) {
+        me.load(x.row0, x.step, from, last, xa);
+        me.load(z.row0, z.step, from, last, za);
+    }
+    for (long long u = from; u < to; u += 2 * MRF_SCAN_STEPS) {
+        const bool more = u + MRF_SCAN_STEPS < to;
+        if (more) {
+            me.load(x.row0, x.step, u + MRF_SCAN_STEPS, last, xb);
+            me.load(z.row0, z.step, u + MRF_SCAN_STEPS, last, zb);
+        }
+        run(xa, za, u);
+        if (u + 2 * MRF_SCAN_STEPS < to) {
+            me.load(x.row0, x.step, u + 2 * MRF_SCAN_STEPS, last, xa);
+            me.load(z.row0, z.step, u + 2 * MRF_SCAN_STEPS, last, za);
+        }
+        if (more) run(xb, zb, u + MRF_SCAN_STEPS);
+    }
+    if constexpr (EFFECT) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) P.effect[blockIdx.y * (P.outer * P.inner) + me.index + j] = make_float2(A[j], h[j]);
+    } else if (blockIdx.y == (unsigned)P.chunks - 1 && P.end) {
+        Lane::keep(P.end + me.index, h);
+    }
+}
+
+// Backward: c is what reaches a step's state from the steps behind it; g = dy + c, and the step before gets a g.
+template <class X, int V, bool COMPLEMENT, bool REV>
+__global__ void __launch_bounds__(256) mrf_scan_bwd(const MrfScanParams P)
+{
+    typedef MrfScanLane<X, V> Lane;
+    const Lane me(P);
+    if (!me.there) return;
+    const long long from = (long long)blockIdx.y * P.chunk, to = from + P.chunk < P.T ? from + P.chunk : P.T;
+    const long long last = me.n < to ? me.n : to;
+    float c[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) c[j] = 0.0f;
+    if (P.chunks > 1) Lane::state(P.carry + blockIdx.y * (P.outer * P.inner) + me.index, c);
+    else if (P.start) Lane::state(P.start + me.index, c);
+    const MrfScanRows<X, REV> x(P.x, P.x_outer, P.x_step, me.o, me.n, me.i), z(P.z, P.z_outer, P.z_step, me.o, me.n, me.i);
+    const long long dense = P.T * P.inner;
+    const MrfScanRows<X, REV> dy(P.dy, dense, P.inner, me.o, me.n, me.i);
+    X *const dx = (X *)P.dx + me.o * dense + me.i, *const dz = (X *)P.dz + me.o * dense + me.i;
+
+    for (long long u = to > from ? (to - 1) / MRF_SCAN_STEPS * MRF_SCAN_STEPS : from - 1; u >= from; u -= MRF_SCAN_STEPS) {
+        if (u < last) {
+            typename Lane::Raw rx, rz, ry;
+            float h[V], before[MRF_SCAN_STEPS][V], a[MRF_SCAN_STEPS][V], rest[MRF_SCAN_STEPS][V];
+            me.load(z.row0, z.step, u, last, rz);
+            me.load(x.row0, x.step, u, last, rx);
+            me.load(dy.row0, dy.step, u, last, ry);
+            Lane::state(P.states + (me.o * P.blocks + u / MRF_SCAN_STEPS) * P.inner + me.i, h);
+#pragma unroll
+            for (int s = 0; s < MRF_SCAN_STEPS; ++s)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    mrf_gate(mrf_to_f32((X)rz.v[s][j]), a[s][j], rest[s][j]);
+                    const float v = mrf_to_f32((X)rx.v[s][j]);
+                    before[s][j] = h[j];
+                    h[j] = fmaf(a[s][j], h[j], COMPLEMENT ? rest[s][j] * v : v);
+                }
+#pragma unroll
+            for (int s = MRF_SCAN_STEPS - 1; s >= 0; --s) {
+                if (u + s < last) {
+                    float gx[V], gz[V];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const float g = mrf_to_f32((X)ry.v[s][j]) + c[j], ag = a[s][j] * g;
+                        gx[j] = COMPLEMENT ? rest[s][j] * g : g;
+                        gz[j] = ag * rest[s][j] * (COMPLEMENT ? before[s][j] - mrf_to_f32((X)rx.v[s][j]) : before[s][j]);
+                        c[j] = ag;
+                    }
+                    const long long t = REV ? me.n - 1 - (u + s) : u + s;
+                    if (P.dx) Lane::give(dx + t * P.inner, gx);
+                    if (P.dz) Lane::give(dz + t * P.inner, gz);
+                }
+            }
+        }
+        const float zero[V] = {};
+        for (int s = 0; s < MRF_SCAN_STEPS; ++s)
+            if (u + s >= last && u + s < to) {
+                if (P.dx) Lane::give(dx + (u + s) * P.inner, zero);
+                if (P.dz) Lane::give(dz + (u + s) * P.inner, zero);
+            }
+    }
+    if (blockIdx.y == 0 && P.end) Lane::keep(P.end + me.index, c);
+}
+
+// What a chunk does to the gradient that reaches it from behind: c -> A c + B
+template <class X, int V, bool REV>
+__global__ void __launch_bounds__(256) mrf_scan_bwd_effect(const MrfScanParams P)
+{
+    typedef MrfScanLane<X, V> Lane;
+    const Lane me(P);
+    if (!me.there) return;
+    const long long from = (long long)blockIdx.y * P.chunk, to = from + P.chunk < P.T ? from + P.chunk : P.T;
+    const long long last = me.n < to ? me.n : to;
+    float A[V], c[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) A[j] = 1.0f, c[j] = 0.0f;
+    const MrfScanRows<X, REV> z(P.z, P.z_outer, P.z_step, me.o, me.n, me.i);
+    const MrfScanRows<X, REV> dy(P.dy, P.T * P.inner, P.inner, me.o, me.n, me.i);
+    for (long long u = to > from ? (to - 1) / MRF_SCAN_STEPS * MRF_SCAN_STEPS : from - 1; u >= from; u -= MRF_SCAN_STEPS) {
+        if (u >= last) continue;
+        typename Lane::Raw rz, ry;
+        me.load(z.row0, z.step, u, last, rz);
+        me.load(dy.row0, dy.step, u, last, ry);
+#pragma unroll
+        for (int s = MRF_SCAN_STEPS - 1; s >= 0; --s)
+            if (u + s < last) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    float a, rest;
+                    mrf_gate(mrf_to_f32((X)rz.v[s][j]), a, rest);
+                    c[j] = a * (mrf_to_f32((X)ry.v[s][j]) + c[j]);
+                    A[j] *= a;
+                }
+            }
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) P.effect[blockIdx.y * (P.outer * P.inner) + me.index + j] = make_float2(A[j], c[j]);
+}
+
+// States that the chunks get, from what each does to them, in the order of the chunks (backward: from the last).  A workgroup has 16 channels, 64 threads
+// for each of them with as many chunks in a row; what those do together meets in LDS.
+template <bool BACK>
+__global__ void __launch_bounds__(1024) mrf_scan_carry(const MrfScanParams P)
+{
+    __shared__ float2 part[64][16];
+    const int w = threadIdx.x % 16, s = threadIdx.x / 16;
+    const long long N = P.outer * P.inner, i = (long long)blockIdx.x * 16 + w;
+    const int per = (P.chunks + 63) / 64, p0 = s * per < P.chunks ? s * per : P.chunks, p1 = p0 + per < P.chunks ? p0 + per : P.chunks;
+    const auto at = [&](int p) { return (size_t)(BACK ? P.chunks - 1 - p : p) * N + i; };
+    float A = 1.0f, B = 0.0f;
+    if (i < N)
+        for (int p = p0; p < p1; ++p) {
+            const float2 e = P.effect[at(p)];
+            B = fmaf(e.x, B, e.y);
+            A *= e.x;
+        }
+    part[s][w] = make_float2(A, B);
+    __syncthreads();
+    for (int d = 1; d < 64; d *= 2) {
+        const float2 mine = part[s][w], other = s >= d ? part[s - d][w] : make_float2(1.0f, 0.0f);
+        __syncthreads();
+        part[s][w] = make_float2(mine.x * other.x, fmaf(mine.x, other.y, mine.y));
+        __syncthreads();
+    }
+    if (i >= N) return;
+    float h = P.start ? P.start[i] : 0.0f;
+    if (s > 0) h = fmaf(part[s - 1][w].x, h, part[s - 1][w].y);
+    for (int p = p0; p < p1; ++p) {
+        P.carry[at(p)] = h;
+        const float2 e = P.effect[at(p)];
+        h = fmaf(e.x, h, e.y);
+    }
+}
+
+namespace mrf_host {
+
+struct ScanSplit { int chunks; long long chunk; };
+
+// Chunks of the steps: none where the channels alone keep the card busy.
+static ScanSplit scan_split(long long outer, long long T, long long inner)
+{
+    const long long N = outer * inner;
+    if (N >= 32768 || T <= 256 || N == 0) return {1, T};
+    long long P = (131072 + N - 1) / N;
+    if (P > (T + 63) / 64) P = (T + 63) / 64;
+    if (P > 16384) P = 16384;
+    const long long chunk = ((T + P - 1) / P + MRF_SCAN_STEPS - 1) / MRF_SCAN_STEPS * MRF_SCAN_STEPS;
+    return {(int)((T + chunk - 1) / chunk), chunk};
+}
+
+static bool scan_sizes_ok(long long outer, long long T, long long inner)
+{
+    const long long most = 0x7fffffffLL;
+    if (outer < 0 || T < 0 || inner < 0 || outer > most || T > most - 2 * MRF_SCAN_STEPS || inner > most) return false;
+    if (outer && inner > (1LL << 38) / outer) return false;      // (channels: a grid has 2^31 workgroups of 256 at most)
+    return !(outer && inner && T) || T <= (1LL << 60) / (outer * inner);
+}
+
+template <class X, int V, bool REV> static int scan_forward(MrfScanParams P, bool complement, hipStream_t st)
+{
+    P.groups = P.inner / V;
+    P.lanes = P.outer * P.groups;
+    const dim3 grid((unsigned)((P.lanes + 255) / 256), (unsigned)P.chunks);
+    if (P.chunks > 1) {
+        if (complement) mrf_scan_fwd<X, V, true, REV, true><<<grid, 256, 0, st>>>(P);
+        else mrf_scan_fwd<X, V, false, REV, true><<<grid, 256, 0, st>>>(P);
+        mrf_scan_carry<false><<<(unsigned)((P.outer * P.inner + 15) / 16), 1024, 0, st>>>(P);
+    }
+    if (complement) mrf_scan_fwd<X, V, true, REV, false><<<grid, 256, 0, st>>>(P);
+    else mrf_scan_fwd<X, V, false, REV, false><<<grid, 256, 0, st>>>(P);
+    return launch_status("mrf_scan_fwd");
+}
+
+template <class X, int V, bool REV> static int scan_backward(MrfScanParams P, bool complement, hipStream_t st)
+{
+    P.groups = P.inner / V;
+    P.lanes = P.outer * P.groups;
+    const dim3 grid((unsigned)((P.lanes + 255) / 256), (unsigned)P.chunks);
+    if (P.chunks > 1) {
+        mrf_scan_bwd_effect<X, V, REV><<<grid, 256, 0, st>>>(P);
+        mrf_scan_carry<true><<<(unsigned)((P.outer * P.inner + 15) / 16), 1024, 0, st>>>(P);
+    }
+    if (complement) mrf_scan_bwd<X, V, true, REV><<<grid, 256, 0, st>>>(P);
+    else mrf_scan_bwd<X, V, false, REV><<<grid, 256, 0, st>>>(P);
+    return launch_status("mrf_scan_bwd");
+}
+
+// two channels a lane where 16 bits and an even row allow it: a load of 4 bytes
+template <bool FORWARD> static int scan_launch(const MrfScanParams &P, int type, bool complement, bool reverse, hipStream_t st)
+{
+    const auto go = [&](auto x, auto v, auto rev) {
+        typedef decltype(x) X;
+        if constexpr (FORWARD) return scan_forward<X, decltype(v)::value, decltype(rev)::value>(P, complement, st);
+        else return scan_backward<X, decltype(v)::value, decltype(rev)::value>(P, complement, st);
+    };
+    const auto typed = [&](auto x) {
+        if constexpr (sizeof(x) == 2)
+            if (P.inner % 2 == 0)
+                return reverse ? go(x, std::integral_constant<int, 2>{}, std::true_type{}) : go(x, std::integral_constant<int, 2>{}, std::false_type{});
+        return reverse ? go(x, std::integral_constant<int, 1>{}, std::true_type{}) : go(x, std::integral_constant<int, 1>{}, std::false_type{});
+    };
+    if (type == MRF_F32) return typed(0.0f);
+    return type == MRF_F16 ? typed((mrf_f16)0.0f) : typed((mrf_bf16)0.0f);
+}
+
+static size_t scan_workspace(long long outer, long long T, long long inner)
+{
+    const ScanSplit s = scan_split(outer, T, inner);
+    return s.chunks > 1 ? (size_t)s.chunks * outer * inner * 12 : 0;
+}
+
+static int scan_prepare(MrfScanParams &P, int type, void *workspace, size_t workspace_bytes)
+{
+    const ScanSplit s = scan_split(P.outer, P.T, P.inner);
+    P.chunks = s.chunks;
+    P.chunk = s.chunk;
+    P.blocks = (P.T + MRF_SCAN_STEPS - 1) / MRF_SCAN_STEPS;
+    if (!known_type(type) || P.x_outer < 0 || P.x_step < 0 || P.z_outer < 0 || P.z_step < 0) return MRF_ERR_BAD_ARGUMENT;
+    if (P.outer == 0 || P.inner == 0) return MRF_OK;
+    if (P.T > 0 && (!P.x || !P.z)) return MRF_ERR_NULL_POINTER;
+    if (s.chunks > 1) {
+        if (!workspace) return MRF_ERR_NULL_POINTER;
+        if (workspace_bytes < scan_workspace(P.outer, P.T, P.inner)) return MRF_ERR_WORKSPACE_TOO_SMALL;
+        P.effect = (float2 *)workspace;
+        P.carry = (float *)(P.effect + (size_t)s.chunks * P.outer * P.inner);
+    }
+    return MRF_OK;
+}
+
+}  // namespace mrf_host
+
+using namespace mrf_host;
+
+extern "C" {
+
+int64_t mrf_gated_scan_states(int64_t T) { return T < 0 ? 0 : (T + MRF_SCAN_STEPS - 1) / MRF_SCAN_STEPS; }
+
+size_t mrf_gated_scan_workspace_bytes(int64_t n_outer, int64_t T, int64_t n_inner)
+{
+    return scan_sizes_ok(n_outer, T, n_inner) ? scan_workspace(n_outer, T, n_inner) : 0;
+}
+
+int mrf_gated_scan_forward(int64_t n_outer, int64_t T, int64_t n_inner, int type, const void *x, const int64_t *x_strides, const void *z,
+                           const int64_t *z_strides, int complement, int reverse, const float *initial, const int32_t *lengths, void *y,
+                           float *final_state, float *states, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (!scan_sizes_ok(n_outer, T, n_inner)) return MRF_ERR_BAD_SHAPE;
+    MrfScanParams P = {};
+    P.outer = n_outer; P.T = T; P.inner = n_inner; P.x = x; P.z = z; P.lengths = lengths; P.start = initial; P.y = y; P.end = final_state;
+    P.states = states;
+    P.x_outer = x_strides ? x_strides[0] : T * n_inner; P.x_step = x_strides ? x_strides[1] : n_inner;
+    P.z_outer = z_strides ? z_strides[0] : T * n_inner; P.z_step = z_strides ? z_strides[1] : n_inner;
+    const int rc = scan_prepare(P, type, workspace, workspace_bytes);
+    if (rc != MRF_OK || n_outer == 0 || n_inner == 0) return rc;
+    if (T > 0 && !y) return MRF_ERR_NULL_POINTER;
+    return scan_launch<true>(P, type, complement != 0, reverse != 0, (hipStream_t)hip_stream);
+}
+
+int mrf_gated_scan_backward(int64_t n_outer, int64_t T, int64_t n_inner, int type, const void *grad_y, const float *grad_final, const void *x,
+                            const int64_t *x_strides, const void *z, const int64_t *z_strides, int complement, int reverse,
+                            const int32_t *lengths, const float *states, void *grad_x, void *grad_z, float *grad_initial, void *workspace,
+                            size_t workspace_bytes, void *hip_stream)
+{
+    if (!scan_sizes_ok(n_outer, T, n_inner)) return MRF_ERR_BAD_SHAPE;
+    MrfScanParams P = {};
+    P.outer = n_outer; P.T = T; P.inner = n_inner; P.x = x; P.z = z; P.dy = grad_y; P.lengths = lengths; P.start = grad_final; P.dx = grad_x;
+    P.dz = grad_z; P.end = grad_initial; P.states = (float *)states;
+    P.x_outer = x_strides ? x_strides[0] : T * n_inner; P.x_step = x_strides ? x_strides[1] : n_inner;
+    P.z_outer = z_strides ? z_strides[0] : T * n_inner; P.z_step = z_strides ? z_strides[1] : n_inner;
+    const int rc = scan_prepare(P, type, workspace, workspace_bytes);
+    if (rc != MRF_OK || n_outer == 0 || n_inner == 0) return rc;
+    if (T > 0 && (!grad_y || !states)) return MRF_ERR_NULL_POINTER;
+    return scan_launch<false>(P, type, complement != 0, reverse != 0, (hipStream_t)hip_stream);
+}
+
+}  // extern "C"

@@ -51,6 +51,30 @@ class _CProblem(ctypes.Structure):
     ]
 
 
+class _CAttention(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "Q", "K", "Hq", "Hk", "D", "type")] + [
+        ("scale", ctypes.c_float),
+        ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3),
+        ("first_offset", ctypes.c_int64), ("last_offset", ctypes.c_int64), ("query_offset", ctypes.c_int64),
+        ("query_offsets", ctypes.c_void_p), ("q_lengths", ctypes.c_void_p), ("k_lengths", ctypes.c_void_p),
+        ("table", ctypes.c_void_p), ("bucket_of", ctypes.c_void_p),
+        ("map_offset", ctypes.c_int64), ("n_offsets", ctypes.c_int64),
+        ("n_buckets", ctypes.c_int32), ("heads_last", ctypes.c_int32),
+    ]
+
+
+class _CHeadRotation(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "T", "Hq", "Hk", "D", "type")] + [
+        ("q", ctypes.c_void_p), ("k", ctypes.c_void_p),
+        ("q_stride", ctypes.c_int64 * 3), ("k_stride", ctypes.c_int64 * 3),
+        ("gamma_q", ctypes.c_void_p), ("gamma_k", ctypes.c_void_p),
+        ("eps", ctypes.c_float), ("rotary", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+        ("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+        ("n_axes", ctypes.c_int32), ("position_offset", ctypes.c_int64),
+    ]
+
+
 def library_path() -> str:
     return LIB_PATH
 
@@ -133,6 +157,27 @@ def load_library():
     lib.mrf_softmin_policy.argtypes = [i64, i32, vp, ci, vp, ci, vp, i64, vp, vp, vp, f32, f32, f32, f32, vp, vp, vp, vp, sz, vp]
     lib.mrf_softmin_policy_backward.restype = ci
     lib.mrf_softmin_policy_backward.argtypes = [i64, i32, vp, ci, vp, ci, vp, i64, vp, vp, vp, f32, f32, f32, vp, vp, vp, sz, vp]
+    A, R = ctypes.POINTER(_CAttention), ctypes.POINTER(_CHeadRotation)
+    lib.mrf_attention_workspace_bytes.restype = sz
+    lib.mrf_attention_workspace_bytes.argtypes = [A, ci]
+    lib.mrf_attention_forward.restype = ci
+    lib.mrf_attention_forward.argtypes = [A, vp, vp, vp, sz, vp]
+    lib.mrf_attention_backward.restype = ci
+    lib.mrf_attention_backward.argtypes = [A, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.mrf_head_rotation_workspace_bytes.restype = sz
+    lib.mrf_head_rotation_workspace_bytes.argtypes = [i64, i32, i32, i32]
+    lib.mrf_head_rotation_forward.restype = ci
+    lib.mrf_head_rotation_forward.argtypes = [R, vp, vp, vp]
+    lib.mrf_head_rotation_backward.restype = ci
+    lib.mrf_head_rotation_backward.argtypes = [R, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.mrf_gated_scan_states.restype = i64
+    lib.mrf_gated_scan_states.argtypes = [i64]
+    lib.mrf_gated_scan_workspace_bytes.restype = sz
+    lib.mrf_gated_scan_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.mrf_gated_scan_forward.restype = ci
+    lib.mrf_gated_scan_forward.argtypes = [i64, i64, i64, ci, vp, vp, vp, vp, ci, ci, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.mrf_gated_scan_backward.restype = ci
+    lib.mrf_gated_scan_backward.argtypes = [i64, i64, i64, ci, vp, vp, vp, vp, vp, vp, ci, ci, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.mrf_workspace_fault.restype = ci
     lib.mrf_workspace_fault.argtypes = [vp, vp]
     lib.mrf_strerror.argtypes = [ci]
@@ -565,6 +610,215 @@ def _policy_backward(given, cost, labels, advantage, old_logp, ref_logp, mask, g
         None if mask is None else mask.data_ptr(), clip_low, clip_high, kl_weight, grad_loss.data_ptr(),
         None if grad_cost is None else grad_cost.data_ptr(), None if workspace is None else workspace.data_ptr(),
         _ws_size(workspace), _stream_handle(stream)), "mrf_softmin_policy_backward")
+
+
+# ---- sequence operators: inputs may be parts of a projection (any strides, the last index dense)
+
+_INT64_MIN, _INT64_MAX = -(1 << 63), (1 << 63) - 1
+
+
+def _here(*tensors):
+    """All on the current device, whose stream the call goes to."""
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != _current_device()):
+            raise ValueError("tensors must be on the current GPU")
+
+
+def _strided(t, what):
+    """Address and strides of a tensor whose last index is dense."""
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError("the last index of %s must be dense" % what)
+    return t.data_ptr(), t.stride()[:-1]
+
+
+def _sequences(t, what, B):
+    if t is not None:
+        _same_size(what, t, B)
+    return _ptr(t, "int32")
+
+
+class MrfAttention:
+    """Mirror of the C struct mrf_attention: q [B,Q,Hq,D], k and v [B,K,Hk,D] of one type at any strides (last index dense), table
+    [Hq,n_buckets] float32 (heads_last: [n_buckets,Hq]) or None, bucket_of [n] int32 for the offsets from map_offset on, query_offsets,
+    q_lengths, k_lengths [B] int32 or None, first_offset and last_offset numbers or None (no bound).  Made once, it can be called again while
+    its tensors live."""
+
+    def __init__(self, q, k, v, scale, *, first_offset=None, last_offset=None, query_offset=0, query_offsets=None, q_lengths=None, k_lengths=None,
+                 table=None, bucket_of=None, map_offset=0, heads_last=False):
+        load_library()
+        if q.dim() != 4 or k.dim() != 4:
+            raise ValueError("q and k must be [batch, token, head, entry]")
+        B, Q, Hq, D = (_size(n) for n in q.shape)
+        K, Hk = _size(k.shape[1]), _size(k.shape[2])
+        _same_size("k", k, B, K, Hk, D)
+        _same_size("v", v, B, K, Hk, D)
+        if k.dtype != q.dtype or v.dtype != q.dtype:
+            raise ValueError("k and v must be %s like q" % q.dtype)
+        _here(q, k, v, query_offsets, q_lengths, k_lengths, table, bucket_of)
+        c = _CAttention(B, Q, K, Hq, Hk, D, _type_of(q, "q"), float(scale))
+        for name, t in (("q", q), ("k", k), ("v", v)):
+            at, strides = _strided(t, name)
+            setattr(c, name, at)
+            setattr(c, name + "_stride", (ctypes.c_int64 * 3)(*strides))
+        c.first_offset = _INT64_MIN if first_offset is None else int(first_offset)
+        c.last_offset = _INT64_MAX if last_offset is None else int(last_offset)
+        c.query_offset = int(query_offset)
+        c.query_offsets, c.q_lengths, c.k_lengths = (_sequences(t, n, B) for t, n in (
+            (query_offsets, "query_offsets"), (q_lengths, "q_lengths"), (k_lengths, "k_lengths")))
+        if table is not None:
+            if bucket_of is None:
+                raise ValueError("a table needs bucket_of")
+            n = _size(table.shape[0] if heads_last else table.shape[-1])
+            _same_size("table", table, *((n, Hq) if heads_last else (Hq, n)))
+            c.table, c.bucket_of = _ptr(table, "float32"), _ptr(bucket_of, "int32")
+            c.map_offset, c.n_offsets, c.n_buckets, c.heads_last = int(map_offset), int(bucket_of.numel()), n, int(bool(heads_last))
+        self.c, self.shape = c, (B, Q, K, Hq, Hk, D)
+        self.q, self.k, self.v, self.table = q, k, v, table
+        self._kept = (query_offsets, q_lengths, k_lengths, bucket_of)
+
+    def _like(self, what, t, *shape, dtype=None):
+        """Address of a dense tensor of that shape, of q's type or of float32."""
+        if t is None:
+            return None
+        _same_size(what, t, *shape)
+        if dtype is None and t.dtype != self.q.dtype:
+            raise ValueError("%s must be %s like q, got %s" % (what, self.q.dtype, t.dtype))
+        _here(t)
+        return _ptr(t, dtype)
+
+
+def mrf_attention_workspace_bytes(att: MrfAttention, backward: bool) -> int:
+    return int(load_library().mrf_attention_workspace_bytes(ctypes.byref(att.c), int(bool(backward))))
+
+
+def mrf_attention_forward(att: MrfAttention, out, lse, workspace, stream=None):
+    """out [B,Q,Hq,D] like q, lse [B,Hq,Q] float32 or None."""
+    B, Q, K, Hq, Hk, D = att.shape
+    _checked(load_library().mrf_attention_forward(
+        ctypes.byref(att.c), att._like("out", out, B, Q, Hq, D), att._like("lse", lse, B, Hq, Q, dtype="float32"), _ptr(workspace, None),
+        _ws_size(workspace), _stream_handle(stream)), "mrf_attention_forward")
+
+
+def mrf_attention_backward(att: MrfAttention, grad_out, out, lse, grad_q, grad_k, grad_v, grad_table, workspace, stream=None):
+    """grad_out and out [B,Q,Hq,D], lse [B,Hq,Q] of the forward call; grad_q, grad_k, grad_v of the shapes of q, k, v (dense), grad_table like
+    the table, each or None."""
+    B, Q, K, Hq, Hk, D = att.shape
+    table = () if att.table is None else tuple(att.table.shape)
+    _checked(load_library().mrf_attention_backward(
+        ctypes.byref(att.c), att._like("grad_out", grad_out, B, Q, Hq, D), att._like("out", out, B, Q, Hq, D),
+        att._like("lse", lse, B, Hq, Q, dtype="float32"), att._like("grad_q", grad_q, B, Q, Hq, D), att._like("grad_k", grad_k, B, K, Hk, D),
+        att._like("grad_v", grad_v, B, K, Hk, D), att._like("grad_table", grad_table, *table, dtype="float32"), _ptr(workspace, None),
+        _ws_size(workspace), _stream_handle(stream)), "mrf_attention_backward")
+
+
+def _head_rotation(q, k, gamma_q, gamma_k, eps, inv_freq, positions, position_offset, interleaved):
+    """The C struct of tensors that fit each other."""
+    load_library()
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q and k must be [batch, token, head, entry]")
+    B, T, Hq, D = (_size(n) for n in q.shape)
+    Hk = _size(k.shape[2])
+    _same_size("k", k, B, T, Hk, D)
+    _same_size("gamma_q", gamma_q, D)
+    _same_size("gamma_k", gamma_k, D)
+    if k.dtype != q.dtype:
+        raise ValueError("k must be %s like q" % q.dtype)
+    _here(q, k, gamma_q, gamma_k, inv_freq, positions)
+    c = _CHeadRotation(B, T, Hq, Hk, D, _type_of(q, "q"))
+    for name, t in (("q", q), ("k", k)):
+        at, strides = _strided(t, name)
+        setattr(c, name, at)
+        setattr(c, name + "_stride", (ctypes.c_int64 * 3)(*strides))
+    c.gamma_q, c.gamma_k, c.eps = _ptr(gamma_q, "float32"), _ptr(gamma_k, "float32"), float(eps)
+    c.rotary, c.interleaved = 0 if inv_freq is None else 2 * _size(inv_freq.numel()), int(bool(interleaved))
+    c.n_axes, c.position_offset = 1, int(position_offset)
+    c.inv_freq, c.positions = _ptr(inv_freq, "float32"), _ptr(positions, "int32")
+    if positions is not None:
+        c.n_axes = _size(positions.shape[2]) if positions.dim() == 3 else 1
+        _same_size("positions", positions, *((B, T, c.n_axes) if positions.dim() == 3 else (B, T)))
+    return c, (B, T, Hq, Hk, D)
+
+
+def _like_heads(what, t, like, *shape):
+    _same_size(what, t, *shape)
+    if t is not None and t.dtype != like.dtype:
+        raise ValueError("%s must be %s like q, got %s" % (what, like.dtype, t.dtype))
+    _here(t)
+    return _ptr(t, None)
+
+
+def mrf_head_rotation_forward(q, k, gamma_q, gamma_k, eps, inv_freq, out_q, out_k, positions=None, position_offset=0, interleaved=False, stream=None):
+    """q [B,T,Hq,D] and k [B,T,Hk,D] of one type at any strides (last index dense), gamma_q, gamma_k [D] float32 or None, inv_freq [pairs that turn]
+    float32 or None (none), out_q and out_k of their shapes, positions [B,T] or [B,T,axes] int32 or None (the token's place)."""
+    c, (B, T, Hq, Hk, D) = _head_rotation(q, k, gamma_q, gamma_k, eps, inv_freq, positions, position_offset, interleaved)
+    _checked(load_library().mrf_head_rotation_forward(ctypes.byref(c), _like_heads("out_q", out_q, q, B, T, Hq, D),
+                                                      _like_heads("out_k", out_k, q, B, T, Hk, D), _stream_handle(stream)), "mrf_head_rotation_forward")
+
+
+def mrf_head_rotation_workspace_bytes(n_tokens: int, Hq: int, Hk: int, D: int) -> int:
+    return int(load_library().mrf_head_rotation_workspace_bytes(int(n_tokens), int(Hq), int(Hk), int(D)))
+
+
+def mrf_head_rotation_backward(grad_out_q, grad_out_k, q, k, gamma_q, gamma_k, eps, inv_freq, grad_q, grad_k, grad_gamma_q, grad_gamma_k, workspace,
+                               positions=None, position_offset=0, interleaved=False, stream=None):
+    """Arguments of the forward call; grad_out_q, grad_out_k, grad_q, grad_k dense, of the shapes of q and k, grad_gamma_q, grad_gamma_k [D] float32;
+    gradients that are not asked for are None."""
+    c, (B, T, Hq, Hk, D) = _head_rotation(q, k, gamma_q, gamma_k, eps, inv_freq, positions, position_offset, interleaved)
+    _same_size("grad_gamma_q", grad_gamma_q, D)
+    _same_size("grad_gamma_k", grad_gamma_k, D)
+    _checked(load_library().mrf_head_rotation_backward(
+        ctypes.byref(c), _like_heads("grad_out_q", grad_out_q, q, B, T, Hq, D), _like_heads("grad_out_k", grad_out_k, q, B, T, Hk, D),
+        _like_heads("grad_q", grad_q, q, B, T, Hq, D), _like_heads("grad_k", grad_k, q, B, T, Hk, D), _ptr(grad_gamma_q, "float32"),
+        _ptr(grad_gamma_k, "float32"), _ptr(workspace, None), _ws_size(workspace), _stream_handle(stream)), "mrf_head_rotation_backward")
+
+
+def mrf_gated_scan_states(T: int) -> int:
+    return int(load_library().mrf_gated_scan_states(int(T)))
+
+
+def mrf_gated_scan_workspace_bytes(n_outer: int, T: int, n_inner: int) -> int:
+    return int(load_library().mrf_gated_scan_workspace_bytes(int(n_outer), int(T), int(n_inner)))
+
+
+def _scan_inputs(x, z, lengths, dense, states, ends):
+    """Sizes, type, and the places of x and z, of tensors that fit each other."""
+    load_library()
+    if x.dim() != 3:
+        raise ValueError("x must be [row, step, channel]")
+    outer, T, inner = (int(n) for n in x.shape)
+    _same_size("z", z, outer, T, inner)
+    if z.dtype != x.dtype:
+        raise ValueError("z must be %s like x" % x.dtype)
+    for name, t in dense:
+        _same_size(name, t, outer, T, inner)
+        if t is not None and t.dtype != x.dtype:
+            raise ValueError("%s must be %s like x, got %s" % (name, x.dtype, t.dtype))
+    for name, t in ends:
+        _same_size(name, t, outer, inner)
+    _same_size("states", states, outer, mrf_gated_scan_states(T), inner)
+    _here(x, z, lengths, states, *(t for _, t in dense), *(t for _, t in ends))
+    (xp, xs), (zp, zs) = _strided(x, "x"), _strided(z, "z")
+    return outer, T, inner, _type_of(x, "x"), xp, (ctypes.c_int64 * 2)(*xs), zp, (ctypes.c_int64 * 2)(*zs), _sequences(lengths, "lengths", outer)
+
+
+def mrf_gated_scan_forward(x, z, initial, lengths, y, final, states, workspace, complement=True, reverse=False, stream=None):
+    """x and z [outer,T,inner] of one type at any strides (last index dense), y dense like them, initial and final [outer,inner] float32 or None (final may be
+    initial), lengths [outer] int32 or None, states [outer,mrf_gated_scan_states(T),inner] float32 or None."""
+    outer, T, inner, code, xp, xs, zp, zs, lp = _scan_inputs(x, z, lengths, (("y", y),), states, (("initial", initial), ("final", final)))
+    _checked(load_library().mrf_gated_scan_forward(
+        outer, T, inner, code, xp, xs, zp, zs, int(bool(complement)), int(bool(reverse)), _ptr(initial, "float32"), lp, _ptr(y, None),
+        _ptr(final, "float32"), _ptr(states, "float32"), _ptr(workspace, None), _ws_size(workspace), _stream_handle(stream)), "mrf_gated_scan_forward")
+
+
+def mrf_gated_scan_backward(grad_y, grad_final, x, z, lengths, states, grad_x, grad_z, grad_initial, workspace, complement=True, reverse=False, stream=None):
+    """grad_y, grad_x, grad_z dense like x, grad_final and grad_initial [outer,inner] float32; states of the forward call; gradients that are not
+    asked for are None, and grad_final may be."""
+    outer, T, inner, code, xp, xs, zp, zs, lp = _scan_inputs(x, z, lengths, (("grad_y", grad_y), ("grad_x", grad_x), ("grad_z", grad_z)), states,
+                                                             (("grad_final", grad_final), ("grad_initial", grad_initial)))
+    _checked(load_library().mrf_gated_scan_backward(
+        outer, T, inner, code, _ptr(grad_y, None), _ptr(grad_final, "float32"), xp, xs, zp, zs, int(bool(complement)), int(bool(reverse)), lp,
+        _ptr(states, "float32"), _ptr(grad_x, None), _ptr(grad_z, None), _ptr(grad_initial, "float32"), _ptr(workspace, None), _ws_size(workspace),
+        _stream_handle(stream)), "mrf_gated_scan_backward")
 
 
 def mrf_workspace_fault(workspace, stream=None) -> int:

@@ -1,0 +1,613 @@
+"""GPU parity of the sequence operators (attention, norm and rotation of heads, gated recurrence) with their fp64 definitions, through the C ABI.
+
+Tolerances follow from the arithmetic, with u = 2^-24: a sum of terms t in single precision, whatever tree or chains form it, is taken
+to be off by at most SUM u sum |t| (SUM = 32, as a chain of 1,024 independent roundings is).  What goes into a 16-bit product is off by half a unit
+in its last place (h of it), and so is what is stored in 16 bits, besides."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+U, SUM = 2.0 ** -24, 32.0
+HALF_ULP = {"float32": 2.0 ** -24, "float16": 2.0 ** -11, "bfloat16": 2.0 ** -8}
+TINY = {"float32": 2.0 ** -149, "float16": 2.0 ** -25, "bfloat16": 2.0 ** -134}
+TYPES = ["float32", "float16", "bfloat16"]
+PAD = 1024      # elements in front of and behind a buffer
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _guarded(shape, dtype):
+    """A buffer of that shape inside a larger one; returns it and a check that nothing around it was written."""
+    torch = _torch()
+    n = int(np.prod(shape))
+    whole = torch.full((n + 2 * PAD,), 77, dtype=dtype, device="cuda:0")
+    inner = whole[PAD:PAD + n]
+    if dtype.is_floating_point:
+        inner.fill_(float("nan"))
+
+    def check():
+        around = torch.cat([whole[:PAD], whole[PAD + n:]])
+        assert (around == 77).all(), "written outside of the buffer"
+    return inner.view(shape), check
+
+
+def _put(a, dtype):
+    torch = _torch()
+    return torch.from_numpy(np.ascontiguousarray(a)).to("cuda:0").to(getattr(torch, dtype))
+
+
+def _strided(t, how):
+    """The same values at other strides: "dense", "heads" (heads before tokens), "fused" (a part of a wider projection), "odd" (an odd row)."""
+    torch = _torch()
+    if how == "dense":
+        return t
+    if how == "heads":
+        return t.transpose(1, 2).contiguous().transpose(1, 2)
+    B, T, H, D = t.shape
+    wide = torch.full((B, T, 3 * H * D + (1 if how == "odd" else 0)), float("nan"), dtype=t.dtype, device=t.device)
+    part = wide[:, :, H * D:2 * H * D].unflatten(2, (H, D))
+    part.copy_(t)
+    return part
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _close(got, want, bound, dtype="float32", what=""):
+    """|got - want| <= bound (in 32 bits) and the rounding of the stored type."""
+    got = _np(got)
+    assert np.isfinite(got).all(), what
+    off = np.abs(got - want)
+    limit = bound + (np.abs(want) + bound) * HALF_ULP[dtype] * 1.01 + TINY[dtype]
+    worst = np.unravel_index(np.argmax(off - limit), off.shape) if off.size else ()
+    assert (off <= limit).all(), "%s off by %g at %s, allowed %g" % (what, off[worst], worst, limit[worst])
+
+
+# ---- attention
+
+def _attention_bounds(q, k, v, g, scale, ok, bias, dtype, so):
+    """Results and bounds of a sequence; P in 16-bit products is off by h, so are dS."""
+    h = 0.0 if dtype == "float32" else HALF_ULP[dtype]
+    G = q.shape[1] // k.shape[1]
+    Hk = k.shape[1]
+    rows, cols = ok.any(1), ok.any(0)
+    q, g = np.where(rows[:, None, None], q, 0.0), np.where(rows[:, None, None], g, 0.0)
+    k, v = np.where(cols[:, None, None], k, 0.0), np.where(cols[:, None, None], v, 0.0)
+    out, lse, p = so.attention(q, k, v, scale, ok, bias)
+    gq, gk, gv, ds, dp = so.attention_grad(g, q, k, v, scale, ok, bias)
+    kr, vr = np.repeat(np.abs(k), G, 1), np.repeat(np.abs(v), G, 1)
+    shared = lambda t: t.reshape(t.shape[0], Hk, G, -1).sum(2)  # noqa: E731
+    size = scale * np.einsum("ihd,jhd->hij", np.abs(q), kr) + (0.0 if bias is None else np.abs(bias))
+    size = np.where(ok[None], size, 0.0)
+    fine = np.where(np.isfinite(lse), np.abs(lse), 0.0)
+    # scores, their differences from the maximum and from lse, the exponential
+    R = (2 * SUM * U * size.max(2, initial=0.0) + 16 * U * (1 + size.max(2, initial=0.0) + fine))[:, :, None]
+    result = {"out": (out, np.einsum("hij,jhd->ihd", p * (R + h + SUM * U), vr)), "lse": (lse, R[:, :, 0] + 4 * U * fine)}
+    B = np.einsum("ihd,jhd->hij", np.abs(g), vr)      # of dP
+    delta = 2 * (p * (R + SUM * U) * B).sum(2, keepdims=True)
+    # (first with delta from the rounded `out`; what is left over, r, comes off with sum(P k), whose P is off by h)
+    r = (HALF_ULP[dtype] + h) * (p * B).sum(2, keepdims=True) + delta
+    eds = p * (2 * R * (np.abs(dp) + np.abs(dp * p).sum(2, keepdims=True)) + SUM * U * B + delta)
+    tilde = np.abs(ds) + p * r
+    result["grad_q"] = gq, scale * np.einsum("hij,jhd->ihd", eds + (h + SUM * U) * tilde + p * r * (2 * h + SUM * U), kr)
+    result["grad_k"] = gk, shared(scale * np.einsum("hij,ihd->jhd", eds + (h + SUM * U) * np.abs(ds), np.abs(q)))
+    result["grad_v"] = gv, shared(np.einsum("hij,ihd->jhd", p * (R + h + SUM * U), np.abs(g)))
+    return result, ds, eds
+
+
+def _check_attention(B, Q, K, Hq, Hk, D, dtype, first=None, last=None, offset=0, ragged=None, NB=0, heads_last=False, how="dense", scale=None, spread=1.0,
+                     step=True, short_map=False, far=16):
+    """ragged: lists (queries, keys, offsets) per sequence, or None each."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    from oracle import mrf_learn_oracle as lo, mrf_sequence_oracle as so
+    print("case attention", B, Q, K, Hq, Hk, D, dtype, first, last, offset, ragged, NB, heads_last, how, flush=True)
+    rng = np.random.default_rng(B * 1000003 + Q * 1009 + K * 31 + D)
+    T = getattr(torch, dtype)
+    q, k, v, g = (_put(spread * rng.normal(size=s), dtype) for s in ((B, Q, Hq, D), (B, K, Hk, D), (B, K, Hk, D), (B, Q, Hq, D)))
+    qn, kn, ko = ragged or (None, None, None)
+    lengths = lambda n: None if n is None else torch.tensor(n, dtype=torch.int32, device="cuda:0")  # noqa: E731
+    for t, n in ((q, qn), (g, qn), (k, kn), (v, kn)):
+        if n is not None:
+            for b in range(B):
+                t[b, max(n[b], 0):] = float("nan")
+    table = bucket_of = None
+    map_offset = -(Q - 1) - offset
+    if NB:
+        count = Q + K - 1
+        if short_map:      # offsets beyond the map's ends have its ends' buckets
+            map_offset, count = -3, 5
+        m = np.array([lo.distance_bucket(map_offset + i, NB, far) for i in range(count)], np.int32)
+        table = _put(rng.normal(size=(NB, Hq) if heads_last else (Hq, NB)), "float32")
+        bucket_of = torch.from_numpy(m).cuda()
+    scale = 1.0 / np.sqrt(D) if scale is None else scale
+    qs, ks, vs = _strided(q, how), _strided(k, how), _strided(v, how)
+    att = mrf.MrfAttention(qs, ks, vs, scale, first_offset=first, last_offset=last, query_offset=offset, query_offsets=lengths(ko), q_lengths=lengths(qn),
+                           k_lengths=lengths(kn), table=table, bucket_of=bucket_of, map_offset=map_offset, heads_last=heads_last)
+    scale = float(att.c.scale)      # as 32 bits have it
+    buffers = {"out": _guarded((B, Q, Hq, D), T), "lse": _guarded((B, Hq, Q), torch.float32)}
+    ws, ws_check = _guarded((max(mrf.mrf_attention_workspace_bytes(att, False), mrf.mrf_attention_workspace_bytes(att, True)),), torch.uint8)
+    mrf.mrf_attention_forward(att, buffers["out"][0], buffers["lse"][0], ws)
+    if step:
+        buffers.update(grad_q=_guarded((B, Q, Hq, D), T), grad_k=_guarded((B, K, Hk, D), T), grad_v=_guarded((B, K, Hk, D), T))
+        if NB:
+            buffers["grad_table"] = _guarded(tuple(table.shape), torch.float32)
+        mrf.mrf_attention_backward(att, g, buffers["out"][0], buffers["lse"][0], *(buffers[n][0] for n in ("grad_q", "grad_k", "grad_v")),
+                                   buffers["grad_table"][0] if NB else None, ws)
+    torch.cuda.synchronize()
+    ws_check()
+    for name, (_, check) in buffers.items():
+        check()
+    got = {n: t for n, (t, _) in buffers.items()}
+    want_table = bound_table = 0.0
+    tab = None if not NB else (_np(table).T if heads_last else _np(table))
+    for b in range(B):
+        ok, d = so.attention_pairs(Q, K, first, last, offset + (ko[b] if ko else 0), qn[b] if qn else None, kn[b] if kn else None)
+        bias, which = so.attention_bias(d, tab, bucket_of.cpu().numpy(), map_offset) if NB else (None, None)
+        want, ds, eds = _attention_bounds(_np(q[b]), _np(k[b]), _np(v[b]), _np(g[b]), scale, ok, bias, dtype, so)
+        lse, lse_bound = want.pop("lse")
+        here = _np(got["lse"][b])
+        none = ~np.isfinite(lse)
+        assert (here[none] == -np.inf).all() and np.isfinite(here[~none]).all()
+        _close(got["lse"][b][torch.from_numpy(~none).cuda()], lse[~none], lse_bound[~none], what="lse")
+        for name, (value, bound) in want.items():
+            if step or name == "out":
+                _close(got[name][b], value, bound, dtype, name)
+                if name in ("out", "grad_q"):
+                    assert (_np(got[name][b])[~ok.any(1)] == 0).all(), name
+                else:
+                    assert (_np(got[name][b])[~ok.any(0)] == 0).all(), name
+        if NB:
+            want_table = want_table + so.table_grad(ds, which, NB)
+            bound_table = bound_table + so.table_grad(eds + SUM * U * np.abs(ds), which, NB)
+    if NB and step:
+        t = got["grad_table"].t() if heads_last else got["grad_table"]
+        _close(t, want_table, bound_table, what="grad_table")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,Q,K,Hq,Hk,D", [(1, 1, 1, 1, 1, 1), (2, 3, 5, 2, 1, 8), (1, 17, 33, 1, 1, 16), (2, 48, 48, 2, 2, 16), (1, 64, 64, 2, 1, 32), (1, 65, 129, 4, 2, 20),
+                                           (1, 128, 200, 2, 2, 64), (1, 129, 63, 3, 1, 33), (2, 200, 130, 4, 1, 100), (1, 257, 300, 2, 2, 128), (1, 70, 1, 1, 1, 7),
+                                           (1, 300, 40, 7, 7, 96), (3, 31, 32, 5, 5, 48)])
+def test_attention_matches_definition(B, Q, K, Hq, Hk, D, dtype):
+    _check_attention(B, Q, K, Hq, Hk, D, dtype)
+    _check_attention(B, Q, K, Hq, Hk, D, dtype, last=0, NB=8, offset=max(K - Q, 0))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("first,last,offset", [(None, 0, 0), (-30, 0, 0), (-96, -1, 0), (-7, 40, 0), (0, 0, 0), (5, None, 0), (None, None, 3), (None, 0, -150), (-64, 0, 97),
+                                               (3, -3, 0), (None, -400, 0), (400, None, 0), (-(1 << 62), 1 << 62, 1 << 40), (None, 0, -(1 << 40))])
+def test_attention_bands(first, last, offset, dtype):
+    _check_attention(2, 150, 170, 4, 2, 32, dtype, first, last, offset, NB=9, heads_last=True)
+    _check_attention(1, 170, 150, 2, 2, 64, dtype, first, last, offset)
+    _check_attention(1, 5, 300, 6, 2, 40, dtype, first, last, offset, NB=4)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attention_of_sequences_of_their_own_length(dtype):
+    n = [130, 0, 1, 64, 97, -5, 200]
+    _check_attention(7, 130, 130, 2, 1, 32, dtype, ragged=(n, n, None), NB=16)
+    _check_attention(7, 130, 130, 2, 2, 64, dtype, last=0, ragged=(n, n, None))
+    _check_attention(7, 90, 130, 2, 2, 24, dtype, ragged=(None, n, None))
+    _check_attention(7, 130, 90, 2, 2, 24, dtype, ragged=(n, None, None), NB=5)
+    _check_attention(3, 100, 140, 4, 2, 32, dtype, last=0, ragged=([100, 50, 7], [140, 60, 0], [40, 10, -7]), NB=6)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("how", ["heads", "fused", "odd"])
+def test_attention_of_parts_of_a_projection(how, dtype):
+    _check_attention(2, 70, 70, 4, 2, 64, dtype, last=0, how=how)
+    _check_attention(2, 70, 70, 4, 2, 30, dtype, how=how, NB=8)
+    _check_attention(2, 2, 150, 4, 2, 128, dtype, how=how, NB=8, offset=148, last=0)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,Q,K,Hq,Hk,D", [(1, 1, 4099, 16, 4, 128), (3, 1, 5000, 8, 8, 64), (2, 1, 1, 4, 1, 32), (2, 5, 3000, 35, 5, 20), (1, 16, 700, 8, 1, 40),
+                                           (1, 2, 20000, 2, 1, 16), (1, 33, 2000, 2, 1, 64)])
+def test_attention_of_few_queries_on_a_long_cache(B, Q, K, Hq, Hk, D, dtype):
+    offsets = [-(17 * b) for b in range(B)]
+    n = [K + o for o in offsets]
+    _check_attention(B, Q, K, Hq, Hk, D, dtype, last=0, offset=K - Q, ragged=(None, n, offsets), step=False)
+    _check_attention(B, Q, K, Hq, Hk, D, dtype, last=0, offset=K - Q, ragged=(None, n, offsets), step=Q > 1, NB=32, far=128)
+    _check_attention(B, Q, K, Hq, Hk, D, dtype, first=-100, last=0, offset=K - Q, step=False, NB=3, short_map=True)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attention_with_many_buckets_and_short_maps(dtype):
+    _check_attention(2, 90, 110, 2, 2, 16, dtype, NB=70, far=60)
+    _check_attention(2, 90, 110, 3, 1, 16, dtype, NB=4, short_map=True, heads_last=True)
+    _check_attention(1, 40, 40, 1, 1, 8, dtype, NB=1)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attention_of_sharp_and_of_flat_scores(dtype):
+    # one key has all the weight; all have the same
+    _check_attention(1, 100, 150, 2, 1, 64, dtype, scale=4.0)
+    _check_attention(1, 100, 150, 2, 1, 64, dtype, scale=1e-6)
+    _check_attention(1, 64, 5000, 1, 1, 32, dtype, scale=1e-3)      # probabilities of 1/5,000
+
+
+def test_attention_gradients_of_any_size_in_16_bits():
+    """dS goes into a product in 16 bits: neither small nor large gradients lose digits (or overflow) on the way.  (Each factor against the definition of
+    its own gradients: 2^-9 times the values, stored in 16 bits, are off by up to 2^-25 themselves, so results of different factors are not the same.)"""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    from oracle import mrf_sequence_oracle as so
+    torch.manual_seed(0)
+    q, k, v, g = (torch.randn(1, 80, 2, 32, device="cuda:0").half() for _ in range(4))
+    ok, _ = so.attention_pairs(80, 80)
+    for factor in (1.0, 2.0 ** -9, 2.0 ** 9):
+        att = mrf.MrfAttention(q, k, v, 0.2)
+        out, lse = torch.empty_like(q), torch.empty(1, 2, 80, device="cuda:0")
+        ws = torch.empty(mrf.mrf_attention_workspace_bytes(att, True), dtype=torch.uint8, device="cuda:0")
+        mrf.mrf_attention_forward(att, out, lse, ws)
+        grads = [torch.empty_like(q) for _ in range(3)]
+        scaled = (g.float() * factor).half()
+        mrf.mrf_attention_backward(att, scaled, out, lse, *grads, None, ws)
+        want, _, _ = _attention_bounds(_np(q[0]), _np(k[0]), _np(v[0]), _np(scaled[0]), float(att.c.scale), ok, None, "float16", so)
+        for name, t in zip(("grad_q", "grad_k", "grad_v"), grads):
+            _close(t[0], *want[name], "float16", name)
+
+
+def test_attention_nan_stays_in_its_query_and_infinite_scores_bar():
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    torch.manual_seed(1)
+    for dtype in (torch.float32, torch.float16, torch.bfloat16):
+        q, k, v = (torch.randn(2, 70, 2, 32, device="cuda:0").to(dtype) for _ in range(3))
+        out, lse = torch.empty_like(q), torch.empty(2, 2, 70, device="cuda:0")
+        mrf.mrf_attention_forward(mrf.MrfAttention(q, k, v, 0.2, last_offset=0), out, lse, None)
+        clean, clean_lse = out.clone(), lse.clone()
+        # a query, and a key that only later queries of its sequence and head see
+        q[0, 5, 1, 3] = float("nan")
+        k[1, 40, 0, 7] = float("nan")
+        mrf.mrf_attention_forward(mrf.MrfAttention(q, k, v, 0.2, last_offset=0), out, lse, None)
+        bad = torch.zeros(2, 70, 2, dtype=torch.bool, device="cuda:0")
+        bad[0, 5, 1] = True
+        bad[1, 40:, 0] = True
+        assert torch.isnan(out[bad]).all() and torch.equal(out[~bad], clean[~bad])
+        assert torch.isnan(lse[bad.transpose(1, 2)]).all() and torch.equal(lse[~bad.transpose(1, 2)], clean_lse[~bad.transpose(1, 2)])
+
+
+# ---- norm and rotation of heads
+
+def _check_rotation(B, T, Hq, Hk, D, dtype, rotary=None, axes=0, offset=0, interleaved=False, how="dense", gammas=True):
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    from oracle import mrf_sequence_oracle as so
+    print("case rotation", B, T, Hq, Hk, D, dtype, rotary, axes, offset, interleaved, how, flush=True)
+    rng = np.random.default_rng(B * 7919 + T * 101 + D)
+    Td = getattr(torch, dtype)
+    rotary = D - D % (2 * max(axes, 1)) if rotary is None else rotary
+    x = {"q": _put(rng.normal(size=(B, T, Hq, D)), dtype), "k": _put(rng.normal(size=(B, T, Hk, D)), dtype)}
+    g = {"q": _put(rng.normal(size=(B, T, Hq, D)), dtype), "k": _put(rng.normal(size=(B, T, Hk, D)), dtype)}
+    gamma = {n: _put(rng.normal(1.0, 0.3, D), "float32") if gammas else None for n in x}
+    freq = (10000.0 ** (-np.arange(rotary // 2) / max(rotary // 2, 1))).astype(np.float32)
+    inv_freq = torch.from_numpy(freq).cuda() if rotary else None
+    positions = None
+    if axes:
+        positions = torch.from_numpy(rng.integers(-1000, 100000, (B, T, axes)).astype(np.int32)).cuda()
+    xs = {n: _strided(t, how) for n, t in x.items()}
+    out = {n: _guarded(t.shape, Td) for n, t in x.items()}
+    grad = {n: _guarded(t.shape, Td) for n, t in x.items()}
+    grad_gamma = {n: _guarded((D,), torch.float32) for n in x}
+    ws, ws_check = _guarded((mrf.mrf_head_rotation_workspace_bytes(B * T, Hq, Hk, D),), torch.uint8)
+    more = {"positions": positions if axes != 1 else positions[:, :, 0].contiguous(), "position_offset": offset, "interleaved": interleaved}
+    mrf.mrf_head_rotation_forward(xs["q"], xs["k"], gamma["q"], gamma["k"], 1e-6, inv_freq, out["q"][0], out["k"][0], **more)
+    mrf.mrf_head_rotation_backward(g["q"], g["k"], xs["q"], xs["k"], gamma["q"], gamma["k"], 1e-6, inv_freq, grad["q"][0], grad["k"][0], grad_gamma["q"][0],
+                                   grad_gamma["k"][0], ws, **more)
+    torch.cuda.synchronize()
+    ws_check()
+    for group in (out, grad, grad_gamma):
+        for _, check in group.values():
+            check()
+    for n in x:
+        G = _np(gamma[n]) if gammas else np.ones(D)
+        want_gg, bound_gg = np.zeros(D), np.zeros(D)
+        for b in range(B):
+            at = None if positions is None else positions[b].cpu().numpy()
+            X, dY = _np(x[n][b]), _np(g[n][b])
+            want = so.head_rotation(X, G, 1e-6, freq, at, offset, interleaved)
+            # the pair's size, whichever way it is turned: the sum of squares, its root, products; angle within 2^-23 of a turn's 1/8 (series and rounding)
+            a, c = so._pair(rotary, interleaved)
+            def pairs(t):
+                y = np.abs(t).copy()
+                y[..., a] = y[..., c] = np.hypot(t[..., a], t[..., c])
+                return y
+            h = X / np.sqrt((X * X).mean(2, keepdims=True) + 1e-6)
+            _close(out[n][0][b], want, SUM * U * pairs(h * G), dtype, "out_" + n)
+            wx, wg = so.head_rotation_grad(dY, X, G, 1e-6, freq, at, offset, interleaved)
+            s = 1.0 / np.sqrt((X * X).mean(2, keepdims=True) + 1e-6)
+            A = pairs(dY) * np.abs(G)
+            _close(grad[n][0][b], wx, SUM * U * s * (A + 2 * np.abs(h) * (A * np.abs(h)).mean(2, keepdims=True)), dtype, "grad_" + n)
+            want_gg += wg
+            bound_gg += SUM * U * (pairs(dY) * np.abs(h)).sum((0, 1))
+        _close(grad_gamma[n][0], want_gg, bound_gg, what="grad_gamma_" + n)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,T,Hq,Hk,D", [(1, 1, 1, 1, 2), (1, 1, 16, 4, 128), (2, 3, 2, 1, 8), (1, 1536, 2, 2, 16), (2, 100, 4, 2, 64), (3, 33, 5, 1, 96), (1, 50, 3, 3, 10),
+                                         (1, 21, 7, 7, 33), (1, 9, 2, 2, 1), (2, 40, 8, 8, 256), (1, 6, 2, 1, 512), (1, 5, 1, 1, 300), (1, 70, 35, 5, 20), (1, 2000, 4, 4, 40)])
+def test_head_rotation_matches_definition(B, T, Hq, Hk, D, dtype):
+    _check_rotation(B, T, Hq, Hk, D, dtype)
+    _check_rotation(B, T, Hq, Hk, D, dtype, interleaved=True, offset=100003, gammas=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D,rotary,axes", [(16, 0, 0), (16, 8, 0), (128, 64, 1), (64, 32, 2), (48, 36, 3), (40, 20, 1), (24, 6, 1), (9, 4, 2), (128, 2, 0), (12, 12, 2)])
+def test_head_rotation_of_parts_and_by_several_axes(D, rotary, axes, dtype):
+    for interleaved in (False, True):
+        _check_rotation(2, 37, 3, 2, D, dtype, rotary=rotary, axes=axes, interleaved=interleaved, offset=5)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("how", ["heads", "fused", "odd"])
+def test_head_rotation_of_parts_of_a_projection(how, dtype):
+    _check_rotation(2, 37, 4, 2, 64, dtype, how=how)
+    _check_rotation(2, 5, 3, 3, 26, dtype, how=how)
+
+
+@pytest.mark.parametrize("offset", [1 << 30, (1 << 40) - 100, -(1 << 40)])
+def test_head_rotation_far_along(offset):
+    """Angles of 10^12 and more turns: in 64 bits they are good to 10^12 2^-53 of a turn, and the sine to as much."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    T, D = 64, 16
+    x = torch.zeros(1, T, 1, D, device="cuda:0")
+    x[..., :D // 2] = 1.0      # cos and sin come out as they are, times the norm's sqrt(2)
+    freq = torch.tensor([1.0, 0.5, 0.25, 0.125, 1e-3, 1e-5, 1e-7, 1e-9], device="cuda:0")
+    out = torch.empty_like(x)
+    mrf.mrf_head_rotation_forward(x, x[:, :, :0], None, None, 1e-12, freq, out, torch.empty_like(x[:, :, :0]), position_offset=offset)
+    at = np.arange(T) + offset
+    angle = at[:, None] * freq.double().cpu().numpy()      # exact products round once in 64 bits, as here
+    y = _np(out)[0, :, 0] / np.sqrt(2.0)
+    limit = SUM * U + 4 * np.abs(angle) * 2.0 ** -53
+    assert (np.abs(y[:, :8] - np.cos(angle)) <= limit).all() and (np.abs(y[:, 8:] - np.sin(angle)) <= limit).all()
+
+
+# ---- gated recurrence
+
+def _check_scan(outer, T, inner, dtype, complement=True, reverse=False, lengths=None, carried=True, how="dense", keep=2.0):
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    from oracle import mrf_sequence_oracle as so
+    print("case scan", outer, T, inner, dtype, complement, reverse, lengths, carried, how, flush=True)
+    rng = np.random.default_rng(outer * 7 + T * 1009 + inner)
+    Td = getattr(torch, dtype)
+    x, z, g = _put(rng.normal(size=(outer, T, inner)), dtype), _put(keep + 1.5 * rng.normal(size=(outer, T, inner)), dtype), _put(rng.normal(size=(outer, T, inner)), dtype)
+    h0 = _put(rng.normal(size=(outer, inner)), "float32") if carried else None
+    gf = _put(rng.normal(size=(outer, inner)), "float32") if carried else None
+    n = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda:0")
+    if lengths is not None:
+        for o in range(outer):
+            for t in (x, z, g):
+                t[o, max(lengths[o], 0):] = float("nan")
+    xs, zs = x, z
+    if how == "fused":
+        both = torch.full((outer, T, 2 * inner + 1), float("nan"), dtype=Td, device="cuda:0")
+        both[:, :, :inner], both[:, :, inner:2 * inner] = x, z
+        xs, zs = both[:, :, :inner], both[:, :, inner:2 * inner]
+    if how == "steps":      # steps before rows
+        xs, zs = (t.transpose(0, 1).contiguous().transpose(0, 1) for t in (x, z))
+    y, states = _guarded((outer, T, inner), Td), _guarded((outer, mrf.mrf_gated_scan_states(T), inner), torch.float32)
+    final, gi = _guarded((outer, inner), torch.float32), _guarded((outer, inner), torch.float32)
+    gx, gz = _guarded((outer, T, inner), Td), _guarded((outer, T, inner), Td)
+    ws, ws_check = _guarded((mrf.mrf_gated_scan_workspace_bytes(outer, T, inner),), torch.uint8)
+    mrf.mrf_gated_scan_forward(xs, zs, h0, n, y[0], final[0], states[0], ws, complement, reverse)
+    mrf.mrf_gated_scan_backward(g, gf, xs, zs, n, states[0], gx[0], gz[0], gi[0], ws, complement, reverse)
+    torch.cuda.synchronize()
+    for check in (ws_check, y[1], states[1], final[1], gi[1], gx[1], gz[1]):
+        check()
+    for o in range(outer):
+        X, Z, dY = _np(x[o]), _np(z[o]), _np(g[o])
+        m = T if lengths is None else min(max(lengths[o], 0), T)
+        X[m:] = Z[m:] = dY[m:] = 0.0
+        first, last = (None, None) if not carried else (_np(h0[o]), _np(gf[o]))
+        args = dict(complement=complement, reverse=reverse, length=m)
+        want, end = so.gated_scan(X, Z, first, **args)
+        wx, wz, wi = so.gated_scan_grad(dY, X, Z, first, last, **args)
+        # A gate is within 4 u (1 + |z|) of itself, a step adds a rounding.  What earlier steps are off by comes along, gate by gate, just as their sizes do: the
+        # recurrence of the sizes, from terms with that factor.
+        # (the sizes' own recurrence bounds the states; from it, each step's error)
+        S, _ = so.gated_scan(np.abs(X), Z, None if first is None else np.abs(first), **args)
+        before = np.zeros_like(S)
+        order = list(range(m - 1, -1, -1) if reverse else range(m))
+        for i, t in enumerate(order):
+            before[t] = S[order[i - 1]] if i else (0.0 if first is None else np.abs(first))
+        a, rest = so._gate(Z)
+        each = 4 * U * (1 + np.abs(Z))
+        made = each * (a * before + (rest if complement else 1.0) * np.abs(X)) + U * S
+        E, e_end = so.gated_scan(made, Z, None, complement=False, reverse=reverse, length=m)
+        _close(y[0][o], want, E, dtype, "y")
+        assert (_np(y[0][o])[m:] == 0).all() and (_np(gx[0][o])[m:] == 0).all() and (_np(gz[0][o])[m:] == 0).all()
+        _close(final[0][o], end, e_end + U * np.abs(end), what="final")
+        # g: the same recurrence backward, over terms of size |dy|
+        gs = [np.zeros(inner)] * (m + 1)
+        es = [np.zeros(inner)] * (m + 1)
+        gs[m] = np.zeros(inner) if last is None else np.abs(last)
+        size_g, err_g = np.zeros_like(S), np.zeros_like(S)
+        for i in range(m - 1, -1, -1):
+            t = order[i]
+            size_g[t] = np.abs(dY[t]) + gs[i + 1]
+            err_g[t] = es[i + 1] + 2 * U * size_g[t]
+            gs[i] = a[t] * size_g[t]
+            es[i] = a[t] * err_g[t] + (each[t] + U) * gs[i]
+        scale = rest if complement else 1.0
+        _close(gx[0][o], wx, scale * (err_g + (each + U) * size_g), dtype, "grad_x")
+        eb = np.zeros_like(S)
+        for i, t in enumerate(order):
+            eb[t] = E[order[i - 1]] if i else 0.0
+        diff = before + (np.abs(X) if complement else 0.0)
+        _close(gz[0][o], wz, a * rest * (err_g * diff + size_g * (eb + U * diff) + (2 * each + 4 * U) * size_g * diff), dtype, "grad_z")
+        _close(gi[0][o], wi, es[0], what="grad_initial")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("outer,T,inner", [(1, 1, 1), (3, 1, 70), (2, 15, 8), (2, 16, 33), (5, 17, 2), (32, 48, 16), (1, 33, 300), (3, 200, 7), (1, 257, 5), (2, 1000, 8), (1, 4097, 3),
+                                           (7, 31, 64), (1, 640, 96)])
+def test_gated_scan_matches_definition(outer, T, inner, dtype):
+    _check_scan(outer, T, inner, dtype)
+    _check_scan(outer, T, inner, dtype, complement=False, reverse=True, carried=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T", [40, 700])
+def test_gated_scan_of_rows_of_their_own_length(T, dtype):
+    n = [T, 0, 1, T // 2, 16, -3, T + 9, 17]
+    for reverse in (False, True):
+        _check_scan(8, T, 6, dtype, lengths=n, reverse=reverse)
+        _check_scan(8, T, 5, dtype, lengths=n, reverse=reverse, complement=False, carried=False)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("how", ["fused", "steps"])
+def test_gated_scan_of_parts_of_a_projection(how, dtype):
+    for T in (20, 600):
+        _check_scan(3, T, 10, dtype, how=how)
+        _check_scan(3, T, 7, dtype, how=how, reverse=True, lengths=[T, 5, T - 1])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gated_scan_that_forgets_or_remembers_all(dtype):
+    for keep in (-30.0, 12.0):
+        _check_scan(2, 500, 6, dtype, keep=keep)
+        _check_scan(2, 100, 6, dtype, keep=keep, complement=False, reverse=True)
+
+
+def test_gated_scan_state_in_place_step_by_step():
+    """Steps one at a time, the state written over itself, give what one call over all of them gives."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    torch.manual_seed(3)
+    x, z = torch.randn(5, 9, 34, device="cuda:0").half(), torch.randn(5, 9, 34, device="cuda:0").half()
+    start = torch.randn(5, 34, device="cuda:0")
+    y, end = torch.empty_like(x), torch.empty_like(start)
+    mrf.mrf_gated_scan_forward(x, z, start, None, y, end, None, None)
+    state = start.clone()
+    for t in range(9):
+        one = torch.empty(5, 1, 34, dtype=x.dtype, device="cuda:0")
+        mrf.mrf_gated_scan_forward(x[:, t:t + 1], z[:, t:t + 1], state, None, one, state, None, None)
+        assert torch.equal(one[:, 0], y[:, t])
+    assert torch.equal(state, end)
+    # and over a long row, divided into chunks
+    x, z = torch.randn(2, 3000, 6, device="cuda:0"), torch.randn(2, 3000, 6, device="cuda:0")
+    ws = torch.empty(mrf.mrf_gated_scan_workspace_bytes(2, 3000, 6), dtype=torch.uint8, device="cuda:0")
+    assert ws.numel() > 0
+    y, end, state = torch.empty_like(x), torch.empty(2, 6, device="cuda:0"), torch.randn(2, 6, device="cuda:0")
+    mrf.mrf_gated_scan_forward(x, z, state, None, y, end, None, ws)
+    again = torch.empty_like(y)
+    mrf.mrf_gated_scan_forward(x, z, state, None, again, state, None, ws)
+    assert torch.equal(y, again) and torch.equal(state, end)
+
+
+# ---- all of them
+
+def test_empty_sizes():
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    E = lambda *s, t=torch.float32: torch.full(s, 7.0, dtype=t, device="cuda:0")  # noqa: E731
+    bucket_of = torch.zeros(4, dtype=torch.int32, device="cuda:0")
+    for B, Q, K in ((0, 3, 4), (2, 0, 4), (2, 3, 0), (2, 20, 0)):
+        q, k, v, table = E(B, Q, 2, 8), E(B, K, 1, 8), E(B, K, 1, 8), E(2, 3)
+        att = mrf.MrfAttention(q, k, v, 1.0, table=table, bucket_of=bucket_of)
+        out, lse, gq, gk, gv, gt = E(B, Q, 2, 8), E(B, 2, Q), E(B, Q, 2, 8), E(B, K, 1, 8), E(B, K, 1, 8), E(2, 3)
+        ws = torch.empty(mrf.mrf_attention_workspace_bytes(att, True), dtype=torch.uint8, device="cuda:0")
+        mrf.mrf_attention_forward(att, out, lse, ws)
+        mrf.mrf_attention_backward(att, E(B, Q, 2, 8), out, lse, gq, gk, gv, gt, ws)
+        for t in (out, gq, gk, gv, gt):
+            assert (t == 0).all()
+        assert (lse == -float("inf")).all()
+    g = E(5)
+    ws = torch.empty(mrf.mrf_head_rotation_workspace_bytes(0, 2, 1, 5), dtype=torch.uint8, device="cuda:0")
+    mrf.mrf_head_rotation_forward(E(0, 3, 2, 5), E(0, 3, 1, 5), None, None, 1e-6, None, E(0, 3, 2, 5), E(0, 3, 1, 5))
+    mrf.mrf_head_rotation_backward(E(0, 3, 2, 5), E(0, 3, 1, 5), E(0, 3, 2, 5), E(0, 3, 1, 5), None, None, 1e-6, None, None, None, g, None, ws)
+    assert (g == 0).all()
+    start, end, gi = E(2, 3), E(2, 3), E(2, 3)
+    start += 1.0
+    mrf.mrf_gated_scan_forward(E(2, 0, 3), E(2, 0, 3), start, None, E(2, 0, 3), end, E(2, 0, 3), None)
+    mrf.mrf_gated_scan_backward(E(2, 0, 3), start, E(2, 0, 3), E(2, 0, 3), None, E(2, 0, 3), None, None, gi, None)
+    assert torch.equal(start, end) and torch.equal(start, gi)
+    mrf.mrf_gated_scan_forward(E(0, 4, 3), E(0, 4, 3), None, None, E(0, 4, 3), None, None, None)
+
+
+def _everything(seed, dtype):
+    """One pass through the operators as a program chains them, into buffers of its own: rotation, attention, recurrence, and back."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    gen = torch.Generator(device="cuda:0").manual_seed(seed)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda:0").to(dtype)  # noqa: E731
+    B, T, H, Hk, D = 2, 150, 4, 2, 32
+    x, v, z = rand(B, T, H + Hk, D), rand(B, T, Hk, D), rand(B, T, H * D)
+    g = rand(B, T, H * D)
+    f = torch.float32
+    new = lambda *s, t=dtype: torch.empty(s, dtype=t, device="cuda:0")  # noqa: E731
+    gamma = torch.ones(D, device="cuda:0")
+    freq = torch.linspace(1.0, 0.01, D // 2, device="cuda:0")
+    table, bucket_of = torch.randn((H, 8), generator=gen, device="cuda:0"), torch.from_numpy(mrf.mrf_distance_buckets(8, 64, -(T - 1), 2 * T - 1)).cuda()
+    q, k, out, lse, y, states = new(B, T, H, D), new(B, T, Hk, D), new(B, T, H, D), new(B, H, T, t=f), new(B, T, H * D), new(B, mrf.mrf_gated_scan_states(T), H * D, t=f)
+    gy, gz, gq, gk, gv, gt = new(B, T, H * D), new(B, T, H * D), new(B, T, H, D), new(B, T, Hk, D), new(B, T, Hk, D), new(H, 8, t=f)
+    gxq, gxk, ggq, ggk = new(B, T, H, D), new(B, T, Hk, D), new(D, t=f), new(D, t=f)
+    att = mrf.MrfAttention(q, k, v, D ** -0.5, last_offset=0, table=table, bucket_of=bucket_of, map_offset=-(T - 1))
+    ws = [new(max(n, 1), t=torch.uint8) for n in (max(mrf.mrf_attention_workspace_bytes(att, b) for b in (False, True)), mrf.mrf_head_rotation_workspace_bytes(B * T, H, Hk, D),
+                                                  mrf.mrf_gated_scan_workspace_bytes(B, T, H * D))]
+
+    def run():
+        mrf.mrf_head_rotation_forward(x[:, :, :H], x[:, :, H:], gamma, gamma, 1e-6, freq, q, k)
+        mrf.mrf_attention_forward(att, out, lse, ws[0])
+        mrf.mrf_gated_scan_forward(out.view(B, T, H * D), z, None, None, y, None, states, ws[2])
+        mrf.mrf_gated_scan_backward(g, None, out.view(B, T, H * D), z, None, states, gy, gz, None, ws[2])
+        mrf.mrf_attention_backward(att, gy.view(B, T, H, D), out, lse, gq, gk, gv, gt, ws[0])
+        mrf.mrf_head_rotation_backward(gq, gk, x[:, :, :H], x[:, :, H:], gamma, gamma, 1e-6, freq, gxq, gxk, ggq, ggk, ws[1])
+    return run, (x, v, z, g, table), (y, gz, gv, gt, gxq, gxk, ggq, ggk)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_pass_captured_into_a_graph_and_replayed(dtype):
+    torch = _torch()
+    dtype = getattr(torch, dtype)
+    run, inputs, outputs = _everything(5, dtype)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for n in range(4):
+        for t in inputs:
+            t.copy_(torch.randn(t.shape, generator=torch.Generator(device="cuda:0").manual_seed(50 + n), device="cuda:0").to(t.dtype))
+        run()
+        want = [t.clone() for t in outputs]
+        for t in outputs:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want, outputs):
+            assert torch.equal(a, b) and torch.isfinite(a).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_the_same_bits_on_another_stream_and_again(dtype):
+    torch = _torch()
+    dtype = getattr(torch, dtype)
+    run, _, outputs = _everything(6, dtype)
+    run()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outputs]
+    streams, passes = [torch.cuda.Stream() for _ in range(2)], [_everything(6, dtype) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for stream, (one, _, _) in zip(streams, passes):      # two programs at once, each with buffers of its own
+            with torch.cuda.stream(stream):
+                one()
+    torch.cuda.synchronize()
+    for _, _, outs in passes:
+        for a, b in zip(want, outs):
+            assert torch.equal(a, b)

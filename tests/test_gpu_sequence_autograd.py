@@ -1,0 +1,176 @@
+"""The sequence operators through torch.autograd: alone against their fp64 definitions, and together with the learning operators and the message passing."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _leaf(a, dtype="float32"):
+    import torch
+    return torch.from_numpy(np.asarray(a, np.float32)).cuda().to(getattr(torch, dtype)).requires_grad_(True)
+
+
+# relative to the largest value: 32 bits leave 2^-24 per operation, some hundreds of them; 16-bit products and the one rounding of what is stored 2^-8 each
+TOLERANCE = {"float32": 2e-5, "bfloat16": 2.0 ** -6}
+
+
+def _near(got, want, dtype):
+    got = _np(got)
+    assert np.abs(got - want).max() <= TOLERANCE[dtype] * np.abs(want).max(), np.abs(got - want).max() / np.abs(want).max()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_attention_through_autograd(dtype):
+    import torch
+    import paper_1910_10892_amd as mrf
+    from oracle import mrf_sequence_oracle as so
+    from paper_1910_10892_amd.autograd import attention
+    rng = np.random.default_rng(0)
+    B, T, Hq, Hk, D = 2, 40, 4, 2, 24
+    parts = _leaf(rng.normal(size=(B, T, (Hq + 2 * Hk) * D)), dtype)      # one projection
+    table = _leaf(rng.normal(size=(6, Hq)))
+    m = mrf.mrf_distance_buckets(6, 20, -(T - 1), 2 * T - 1)
+    heads = parts.unflatten(2, (Hq + 2 * Hk, D))
+    out, lse = attention(heads[:, :, :Hq], heads[:, :, Hq:Hq + Hk], heads[:, :, Hq + Hk:], causal=True, table=table, bucket_of=torch.from_numpy(m).cuda(),
+                         map_offset=-(T - 1), heads_last=True)
+    assert out.dtype == parts.dtype and not lse.requires_grad
+    up = torch.from_numpy(rng.normal(size=(B, Hq, T, D)).astype(np.float32)).cuda().to(out.dtype).transpose(1, 2)      # (not dense)
+    out.backward(up)
+    want, want_table = np.zeros(parts.shape), np.zeros((Hq, 6))
+    for b in range(B):
+        q, k, v = np.split(_np(parts[b]).reshape(T, -1, D), [Hq, Hq + Hk], 1)
+        ok, d = so.attention_pairs(T, T, None, 0)
+        bias, which = so.attention_bias(d, _np(table).T, m, -(T - 1))
+        _near(out[b], so.attention(q, k, v, D ** -0.5, ok, bias)[0], dtype)
+        gq, gk, gv, ds, _ = so.attention_grad(_np(up[b]), q, k, v, D ** -0.5, ok, bias)
+        want[b] = np.concatenate([gq, gk, gv], 1).reshape(T, -1)
+        want_table += so.table_grad(ds, which, 6)
+    _near(parts.grad, want, dtype)
+    _near(table.grad, want_table.T, "float32")
+    # one input alone asks for a gradient; keys without a table, with another's upstream type
+    k = _leaf(rng.normal(size=(1, 9, 1, 8)))
+    attention(k.detach(), k, k.detach())[0].sum().backward()
+    assert k.grad is not None and torch.isfinite(k.grad).all()
+    with pytest.raises(ValueError):
+        attention(k, k, k, causal=True, last_offset=3)
+    with pytest.raises(ValueError):
+        attention(k, k, k, table=torch.zeros(1, 4, device="cuda:0"))
+    with pytest.raises(mrf.MrfError):
+        attention(k, k, k, scale=0.0)
+    out = attention(k, k, k)[0]
+    (g,) = torch.autograd.grad(out.sum(), k, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_head_rotation_through_autograd(dtype):
+    import torch
+    from oracle import mrf_sequence_oracle as so
+    from paper_1910_10892_amd.autograd import head_rotation
+    rng = np.random.default_rng(1)
+    q, k = _leaf(rng.normal(size=(2, 11, 4, 16)), dtype), _leaf(rng.normal(size=(2, 11, 1, 16)), dtype)
+    gq, gk = _leaf(rng.normal(1.0, 0.2, 16)), _leaf(rng.normal(1.0, 0.2, 16))
+    freq = np.array([1.0, 0.3, 0.1, 1.0, 0.3, 0.1], np.float32)
+    at = rng.integers(0, 50, (2, 11, 2)).astype(np.int32)
+    oq, ok = head_rotation(q, k, gq, gk, inv_freq=torch.from_numpy(freq).cuda(), positions=torch.from_numpy(at).cuda())
+    uq, uk = torch.randn_like(oq), torch.randn_like(ok)
+    torch.autograd.backward([oq, ok], [uq, uk])
+    for x, gamma, o, u in ((q, gq, oq, uq), (k, gk, ok, uk)):
+        want_gamma = np.zeros(16)
+        for b in range(2):
+            _near(o[b], so.head_rotation(_np(x[b]), _np(gamma), 1e-6, freq, at[b]), dtype)
+            wx, wg = so.head_rotation_grad(_np(u[b]), _np(x[b]), _np(gamma), 1e-6, freq, at[b])
+            _near(x.grad[b], wx, dtype)
+            want_gamma += wg
+        _near(gamma.grad, want_gamma, "float32")
+    # only one of the outputs is used
+    x = _leaf(rng.normal(size=(1, 3, 2, 8)))
+    head_rotation(x, x.detach())[0].sum().backward()
+    assert torch.isfinite(x.grad).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("direction", [(0, 1), (0, -1), (1, 0), (-1, 0)])
+def test_scans_through_autograd(direction, dtype):
+    import torch
+    from oracle import mrf_sequence_oracle as so
+    from paper_1910_10892_amd.autograd import gated_scan, scanline_scan
+    rng = np.random.default_rng(2)
+    B, H, W, C = 2, 5, 7, 3
+    x, z = _leaf(rng.normal(size=(B, H, W, C)), dtype), _leaf(rng.normal(size=(B, H, W, C)), dtype)
+    y = scanline_scan(x, z, direction)
+    up = torch.randn_like(y)
+    y.backward(up)
+    along = (lambda t: _np(t).transpose(0, 2, 1, 3)) if direction[0] else _np      # the scanned index last but one
+    X, Z, Y, U, GX, GZ = (along(t) for t in (x, z, y, up, x.grad, z.grad))
+    want = [np.zeros(X.shape) for _ in range(3)]
+    for n in np.ndindex(*X.shape[:2]):
+        want[0][n] = so.gated_scan(X[n], Z[n], reverse=sum(direction) < 0)[0]
+        want[1][n], want[2][n], _ = so.gated_scan_grad(U[n], X[n], Z[n], reverse=sum(direction) < 0)
+    for got, w in zip((Y, GX, GZ), want):
+        assert np.abs(got - w).max() <= TOLERANCE[dtype] * np.abs(w).max()
+    with pytest.raises(ValueError):
+        scanline_scan(x, z, (1, 1))
+    # the state behind the last step, alone, and the state before the first
+    x, z, h0 = _leaf(rng.normal(size=(3, 20, 4)), dtype), _leaf(rng.normal(size=(3, 20, 4)), dtype), _leaf(rng.normal(size=(3, 4)))
+    _, final = gated_scan(x, z, h0, lengths=torch.tensor([20, 3, 0], dtype=torch.int32, device="cuda:0"), complement=False)
+    uf = torch.randn_like(final)
+    final.backward(uf)
+    for o, n in enumerate((20, 3, 0)):
+        args = dict(complement=False, length=n)
+        assert np.abs(_np(final[o]) - so.gated_scan(_np(x[o]), _np(z[o]), _np(h0[o]), **args)[1]).max() <= 2e-5 * 20
+        gx, gz, gi = so.gated_scan_grad(np.zeros((20, 4)), _np(x[o]), _np(z[o]), _np(h0[o]), _np(uf[o]), **args)
+        for got, w in ((x.grad[o], gx), (z.grad[o], gz), (h0.grad[o], gi)):
+            assert np.abs(_np(got) - w).max() <= TOLERANCE[dtype] * max(np.abs(w).max(), 1e-3)
+
+
+def test_scanlines_to_labels_and_back():
+    """Features through norm and rotation by pixel, attention along the rows, recurrences down and up the columns, layer norm, message passing, policy loss: a
+    gradient for every parameter, and the same as by differences of the loss."""
+    import torch
+    from paper_1910_10892_amd import mrf_distance_buckets
+    from paper_1910_10892_amd.autograd import (attention, bucket_pairwise, head_rotation, layer_norm, message_passing, policy_loss, scanline_scan, softmin_logp)
+    torch.manual_seed(4)
+    B, H, W, heads, D, L = 2, 12, 20, 2, 8, 8
+    C = heads * D
+    features = torch.randn(B * H, W, C, device="cuda:0")
+    new = lambda *s: (0.3 * torch.randn(*s, device="cuda:0")).requires_grad_(True)  # noqa: E731
+    params = {"project": new(C, 3 * C), "gate": new(C, C), "score": new(C, L), "gq": new(D), "gk": new(D), "table": new(heads, 8), "values": new(6)}
+    freq = torch.tensor([1.0, 0.2, 1.0, 0.2], device="cuda:0")
+    at = torch.stack(torch.meshgrid(torch.arange(B * H, device="cuda:0") % H, torch.arange(W, device="cuda:0"), indexing="ij"), 2).int()
+    by_row = torch.from_numpy(mrf_distance_buckets(8, W, -(W - 1), 2 * W - 1)).cuda()
+    by_label = torch.from_numpy(mrf_distance_buckets(6, L, -(L - 1), 2 * L - 1)).cuda()
+    labels = torch.randint(0, L, (B, H, W), device="cuda:0", dtype=torch.uint8)
+    advantage = torch.randn(B * H * W, device="cuda:0")
+
+    def costs(p):
+        q, k, v = (features @ p["project"]).unflatten(2, (3 * heads, D)).split(heads, 2)
+        q, k = head_rotation(q, k, 1.0 + p["gq"], 1.0 + p["gk"], inv_freq=freq, positions=at)
+        h, _ = attention(q, k, v, first_offset=-6, last_offset=2, table=p["table"], bucket_of=by_row, map_offset=-(W - 1))
+        h = h.reshape(B, H, W, C)
+        z = h @ p["gate"]
+        h = scanline_scan(h, z, (1, 0)) + scanline_scan(h, z, (-1, 0))
+        unary = layer_norm(h @ p["score"])
+        return message_passing(unary, bucket_pairwise(p["values"], by_label, -(L - 1), L, L), algo="isgmr", K=2)[0]
+
+    # (without the probabilities that the labels were drawn with, the loss has a gradient but, r being 1, no value that moves)
+    old = softmin_logp(costs(params), labels)
+    loss = lambda p: policy_loss(costs(p), labels, advantage, old)[0]  # noqa: E731
+    loss(params).backward()
+    for name, p in params.items():
+        assert p.grad is not None and torch.isfinite(p.grad).all() and p.grad.abs().max() > 0, name
+    # a smooth stretch of the loss (its minima change their place only here and there): along the gradient of all but the pairwise values, the median of several
+    # steps' differences
+    smooth = [n for n in params if n != "values"]
+    size = sum(float((params[n].grad ** 2).sum()) for n in smooth)
+    ratios = []
+    for step in (1e-3, 2e-3, 3e-3, 4e-3, 5e-3):
+        with torch.no_grad():
+            moved = [{n: p + (s * step / size ** 0.5 * p.grad if n in smooth else 0.0) for n, p in params.items()} for s in (1, -1)]
+            ratios.append((float(loss(moved[0])) - float(loss(moved[1]))) / (2 * step * size ** 0.5))
+    assert abs(float(np.median(ratios)) - 1.0) < 0.1, ratios

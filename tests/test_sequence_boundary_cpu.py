@@ -1,0 +1,139 @@
+"""Refusals of the sequence operators' entry points: argument errors are reported before any GPU work, so this runs without a GPU."""
+import ctypes
+
+import pytest
+
+import paper_1910_10892_amd as mrf
+from paper_1910_10892_amd import mrfmp as binding
+
+FAKE = 0x1000      # never dereferenced by the host checks
+INF, NAN = float("inf"), float("nan")
+
+
+def _attention(**given):
+    c = binding._CAttention()
+    values = dict(B=2, Q=40, K=50, Hq=4, Hk=2, D=16, type=0, scale=0.25, q=FAKE, k=FAKE, v=FAKE, first_offset=-(1 << 63), last_offset=(1 << 63) - 1)
+    values.update(given)
+    for name, value in values.items():
+        setattr(c, name, (ctypes.c_int64 * 3)(*value) if name.endswith("stride") else value)
+    return c
+
+
+def test_attention_refusals():
+    lib = mrf.load_library()
+
+    def forward(out=FAKE, ws=FAKE, size=1 << 40, **given):
+        return lib.mrf_attention_forward(ctypes.byref(_attention(**given)), out, None, ws, size, None)
+
+    assert lib.mrf_attention_forward(None, FAKE, None, FAKE, 1 << 40, None) == -1
+    for bad in (dict(B=-1), dict(Q=-1), dict(K=-1), dict(Hq=0), dict(Hk=0), dict(Hk=3), dict(D=0), dict(D=129), dict(Q=0x7fff0001),
+                dict(B=1 << 20, Q=1 << 20), dict(B=1 << 20, K=1 << 20), dict(Hq=65538, Hk=2)):
+        assert forward(**bad) == -2, bad
+        assert lib.mrf_attention_workspace_bytes(ctypes.byref(_attention(**bad)), 1) == 0
+    for bad in (dict(type=3), dict(type=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=INF), dict(scale=NAN), dict(q_stride=(1, -1, 1)),
+                dict(k_stride=(-1, 1, 1)), dict(v_stride=(1, 1, -1)), dict(query_offset=1 << 41), dict(query_offset=-(1 << 41))):
+        assert forward(**bad) == -12, bad
+    table = dict(table=FAKE, bucket_of=FAKE, n_offsets=9, n_buckets=4)
+    assert forward(**{**table, "n_buckets": 0}) == -2 and forward(**{**table, "n_buckets": 65537}) == -2
+    for bad in (dict(n_offsets=0), dict(n_offsets=(1 << 40) + 1), dict(map_offset=(1 << 41) + 1), dict(map_offset=-(1 << 41) - 1)):
+        assert forward(**{**table, **bad}) == -12, bad
+    assert forward(**{**table, "bucket_of": None}) == -1
+    for name in ("q", "k", "v"):
+        assert forward(**{name: None}) == -1
+    assert forward(out=None) == -1
+    # nothing to do
+    assert forward(B=0, q=None, k=None, v=None, out=None) == 0 and forward(Q=0, q=None, out=None) == 0
+    # keys divided among workgroups need room for their parts
+    row = dict(Q=1, K=4096)
+    need = lib.mrf_attention_workspace_bytes(ctypes.byref(_attention(**row)), 0)
+    assert need > 0 and lib.mrf_attention_workspace_bytes(ctypes.byref(_attention()), 0) == 0
+    assert forward(ws=None, **row) == -1 and forward(size=need - 1, **row) == -6
+
+
+def test_attention_backward_refusals():
+    lib = mrf.load_library()
+    need = lib.mrf_attention_workspace_bytes(ctypes.byref(_attention()), 1)
+    assert need > 0
+
+    def backward(g=FAKE, out=FAKE, lse=FAKE, gt=None, ws=FAKE, size=need, **given):
+        return lib.mrf_attention_backward(ctypes.byref(_attention(**given)), g, out, lse, FAKE, FAKE, FAKE, gt, ws, size, None)
+
+    assert backward(g=None) == -1 and backward(out=None) == -1 and backward(lse=None) == -1 and backward(ws=None) == -1
+    assert backward(q=None) == -1 and backward(k=None) == -1 and backward(v=None) == -1 and backward(size=need - 1) == -6
+    assert backward(gt=FAKE) == -1                      # a gradient of no table
+    assert backward(D=0) == -2 and backward(type=7) == -12
+    table = _attention(table=FAKE, bucket_of=FAKE, n_offsets=9, n_buckets=4)
+    assert lib.mrf_attention_workspace_bytes(ctypes.byref(table), 1) > need
+
+
+def _rotation(**given):
+    c = binding._CHeadRotation()
+    values = dict(B=2, T=3, Hq=4, Hk=2, D=16, type=0, q=FAKE, k=FAKE, eps=1e-6, rotary=16, inv_freq=FAKE, n_axes=1)
+    values.update(given)
+    for name, value in values.items():
+        setattr(c, name, (ctypes.c_int64 * 3)(*value) if name.endswith("stride") else value)
+    return c
+
+
+def test_head_rotation_refusals():
+    lib = mrf.load_library()
+
+    def forward(out_q=FAKE, out_k=FAKE, **given):
+        return lib.mrf_head_rotation_forward(ctypes.byref(_rotation(**given)), out_q, out_k, None)
+
+    assert lib.mrf_head_rotation_forward(None, FAKE, FAKE, None) == -1
+    for bad in (dict(B=-1), dict(T=-1), dict(Hq=-1), dict(Hk=-1), dict(D=0), dict(D=513), dict(B=1 << 16, T=1 << 16), dict(Hq=65537)):
+        assert forward(**bad) == -2, bad
+    for bad in (dict(type=3), dict(eps=0.0), dict(eps=-1.0), dict(eps=INF), dict(eps=NAN), dict(rotary=-2), dict(rotary=18), dict(rotary=7), dict(n_axes=0),
+                dict(n_axes=3, positions=FAKE), dict(position_offset=1 << 41), dict(position_offset=-(1 << 41)), dict(q_stride=(1, 1, -1)), dict(k_stride=(-1, 1, 1))):
+        assert forward(**bad) == -12, bad
+    assert forward(n_axes=2) == -1 and forward(q=None) == -1 and forward(k=None) == -1 and forward(inv_freq=None) == -1
+    assert forward(out_q=None) == -1 and forward(out_k=None) == -1
+    assert forward(B=0, q=None, k=None, out_q=None, out_k=None) == 0 and forward(Hq=0, Hk=0, out_q=None, out_k=None) == 0
+
+    need = mrf.mrf_head_rotation_workspace_bytes(6, 4, 2, 16)
+    assert need > 0 and mrf.mrf_head_rotation_workspace_bytes(-1, 4, 2, 16) == 0 and mrf.mrf_head_rotation_workspace_bytes(6, 4, 2, 513) == 0
+
+    def backward(gq=FAKE, gk=FAKE, gg=FAKE, ws=FAKE, size=need, **given):
+        return lib.mrf_head_rotation_backward(ctypes.byref(_rotation(**given)), gq, gk, FAKE, FAKE, gg, None, ws, size, None)
+
+    assert backward(gq=None) == -1 and backward(gk=None) == -1 and backward(ws=None) == -1 and backward(size=need - 1) == -6
+    assert backward(D=0) == -2 and backward(type=-1) == -12
+    assert backward(B=0, gq=None, gk=None, gg=None, ws=None, size=0) == 0
+
+
+def test_gated_scan_refusals():
+    lib = mrf.load_library()
+
+    def forward(outer=2, T=3, inner=4, t=0, x=FAKE, xs=None, z=FAKE, zs=None, y=FAKE, ws=FAKE, size=1 << 40):
+        strides = lambda s: None if s is None else (ctypes.c_int64 * 2)(*s)  # noqa: E731
+        return lib.mrf_gated_scan_forward(outer, T, inner, t, x, strides(xs), z, strides(zs), 1, 0, None, None, y, None, None, ws, size, None)
+
+    for bad in (dict(outer=-1), dict(T=-1), dict(inner=-1), dict(T=1 << 31), dict(outer=1 << 31), dict(inner=1 << 31), dict(outer=1 << 20, inner=1 << 20)):
+        assert forward(**bad) == -2, bad
+        assert mrf.mrf_gated_scan_workspace_bytes(bad.get("outer", 2), bad.get("T", 3), bad.get("inner", 4)) == 0
+    assert forward(t=3) == -12 and forward(xs=(-1, 4)) == -12 and forward(zs=(12, -4)) == -12
+    assert forward(x=None) == -1 and forward(z=None) == -1 and forward(y=None) == -1
+    assert forward(outer=0, x=None, z=None, y=None) == 0 and forward(inner=0, x=None, z=None, y=None) == 0
+    need = mrf.mrf_gated_scan_workspace_bytes(2, 1000, 4)
+    assert need > 0 and mrf.mrf_gated_scan_workspace_bytes(2, 3, 4) == 0
+    assert forward(T=1000, ws=None) == -1 and forward(T=1000, size=need - 1) == -6
+    assert mrf.mrf_gated_scan_states(0) == 0 and mrf.mrf_gated_scan_states(1) == 1 and mrf.mrf_gated_scan_states(-5) == 0
+    assert 16 * mrf.mrf_gated_scan_states(1000) >= 1000
+
+    def backward(gy=FAKE, states=FAKE, x=FAKE, ws=FAKE, size=need):
+        return lib.mrf_gated_scan_backward(2, 1000, 4, 0, gy, None, x, None, FAKE, None, 1, 0, None, states, FAKE, FAKE, None, ws, size, None)
+
+    assert backward(gy=None) == -1 and backward(states=None) == -1 and backward(x=None) == -1 and backward(ws=None) == -1 and backward(size=need - 1) == -6
+
+
+def test_bindings_refuse_tensors_that_do_not_fit():
+    import torch
+    q, k = torch.zeros(2, 5, 4, 8), torch.zeros(2, 6, 2, 8)
+    for call in (lambda: mrf.MrfAttention(q, k, k, 0.5),                                                  # not on the GPU
+                 lambda: mrf.MrfAttention(q[0], k, k, 0.5), lambda: mrf.MrfAttention(q, k, k[:, :5], 0.5), lambda: mrf.MrfAttention(q, k.half(), k, 0.5),
+                 lambda: mrf.mrf_head_rotation_forward(q, q, None, None, 1e-6, None, q, q), lambda: mrf.mrf_head_rotation_forward(q, k, None, None, 1e-6, None, q, k),
+                 lambda: mrf.mrf_gated_scan_forward(q[0], q[0], None, None, q[0], None, None, None), lambda: mrf.mrf_gated_scan_forward(q, q, None, None, q, None, None, None),
+                 lambda: mrf.mrf_gated_scan_forward(q[0], q[1].half(), None, None, q[0], None, None, None)):
+        with pytest.raises(ValueError):
+            call()
