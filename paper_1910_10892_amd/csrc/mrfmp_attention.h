@@ -87,8 +87,10 @@ struct MrfAttnParams {
     const void *dout;
     void *dq, *dk, *dv;
     float *delta;                                 // [B][Hq][Q]
-    float *lines, *diagonals, *dtable;
+    float *lines, *partial, *dtable;              // partial: [Hq][n_buckets][MRF_TABLE_PARTS]
     int strips, line;                             // strips of 32 keys; entries of a line
+    int parts;
+    long long pieces;
 };
 
 // What holds for a sequence: queries and keys that there are, and i + lo <= j <= i + hi for the keys j of query i

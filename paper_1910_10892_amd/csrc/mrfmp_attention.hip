@@ -193,7 +193,7 @@ int attention_check(const mrf_attention *a, MrfAttnParams &P)
     if (!a) return MRF_ERR_NULL_POINTER;
     const long long most = 0x7fff0000LL;
     if (a->B < 0 || a->Q < 0 || a->K < 0 || a->Hq < 1 || a->Hk < 1 || a->Hq % a->Hk || a->D < 1 || a->D > MRF_ATTENTION_LONGEST_HEAD) return MRF_ERR_BAD_SHAPE;
-    if (a->Q > most || a->K > most || a->Hq > 65536) return MRF_ERR_BAD_SHAPE;
+    if (a->Q > most || a->K > most || a->Hq > 32768) return MRF_ERR_BAD_SHAPE;
     if (a->B && (long long)a->Hq * ((a->Q + 31) / 32) > most / a->B) return MRF_ERR_BAD_SHAPE;
     if (a->B && (long long)a->Hq * ((a->K + 31) / 32) > most / a->B) return MRF_ERR_BAD_SHAPE;
     if (!known_type(a->type) || !(a->scale > 0.0f) || !(a->scale < INFINITY)) return MRF_ERR_BAD_ARGUMENT;

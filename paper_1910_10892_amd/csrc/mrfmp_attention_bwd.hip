@@ -316,66 +316,61 @@ template <class T, int DP, bool BIAS, bool TABLE> __global__ void __launch_bound
         }
 }
 
-// Sums of the lines along a diagonal, over the strips of keys that it crosses: [B][Hq][Q + K - 1], entry key - query + Q - 1
-template <int QT> __global__ void __launch_bounds__(256) mrf_attn_diagonals(const MrfAttnParams P)
+// Gradient of the table: what the lines hold of a diagonal, summed over the strips of keys that it crosses, belongs to the bucket of its offset.  A workgroup
+// goes through `per` pieces of 256 offsets of a sequence, a thread its offset's strips; each thread has a sum of its own for each of MRF_TABLE_BUCKETS buckets in
+// LDS, which meet at the end in a fixed tree.  More buckets: a layer of workgroups for each MRF_TABLE_BUCKETS of them.
+constexpr int MRF_TABLE_BUCKETS = 32, MRF_TABLE_PARTS = 256;
+
+template <int QT> __global__ void __launch_bounds__(256) mrf_attn_buckets(const MrfAttnParams P)
 {
-    const long long n = (long long)P.Q + P.K - 1, blocks = (n + 255) / 256;
-    const long long bh = blockIdx.x / blocks, at = (blockIdx.x - bh * blocks) * 256 + threadIdx.x;
-    if (at >= n) return;
-    const MrfAttnBatch s(P, (int)(bh / P.Hq));
-    const float *const lines = P.lines + (size_t)bh * P.strips * P.line;
-    const long long offset = at - (P.Q - 1);
-    // strips whose keys have a query at that offset: key - offset in [0, Q)
-    const long long first = max(offset, 0LL) / 32, last = min(offset + P.Q - 1, (long long)P.K - 1) / 32;
-    float sum = 0.0f;
-    for (long long strip = first; strip <= last; ++strip) {
-        int t0, t1;
-        mrf_attn_query_tiles<QT>(s, (int)(strip / 4 * 128), t0, t1);
-        const long long entry = strip * 32 - offset + 31;
-        if (t0 < t1 && entry >= (long long)t0 * QT && entry < (long long)t1 * QT + 32) sum += lines[strip * P.line + entry];
+    __shared__ float sums[MRF_TABLE_BUCKETS][256];
+    const int tid = threadIdx.x, part = blockIdx.x, h = blockIdx.y, first_bucket = blockIdx.z * MRF_TABLE_BUCKETS;
+    const long long n = (long long)P.Q + P.K - 1, blocks = (n + 255) / 256, all = blocks * P.B;
+    const long long x0 = part * P.pieces, x1 = x0 + P.pieces < all ? x0 + P.pieces : all;
+#pragma unroll
+    for (int k = 0; k < MRF_TABLE_BUCKETS; ++k) sums[k][tid] = 0.0f;
+    for (long long x = x0; x < x1; ++x) {
+        const int b = (int)(x / blocks);
+        const long long at = (x - b * blocks) * 256 + tid;
+        const MrfAttnBatch s(P, b);
+        const long long offset = at - (P.Q - 1);
+        if (at >= n || offset < s.lo || offset > s.hi) continue;
+        long long m = s.map + offset;
+        m = m < 0 ? 0 : m >= P.n_offsets ? P.n_offsets - 1 : m;
+        int k = P.bucket_of[m];
+        k = (k < 0 ? 0 : k >= P.n_buckets ? P.n_buckets - 1 : k) - first_bucket;
+        if (k < 0 || k >= MRF_TABLE_BUCKETS) continue;
+        // strips whose keys have a query at that offset: key - offset in [0, nq)
+        const float *const lines = P.lines + ((size_t)b * P.Hq + h) * P.strips * P.line;
+        const long long first = max(offset, 0LL) / 32, last = min(offset + s.nq - 1, (long long)s.nk - 1);
+        float sum = 0.0f;
+        for (long long strip = first; 32 * strip <= last; ++strip) {
+            int t0, t1;
+            mrf_attn_query_tiles<QT>(s, (int)(strip / 4 * 128), t0, t1);
+            const long long entry = strip * 32 - offset + 31;
+            if (t0 < t1 && entry >= (long long)t0 * QT && entry < (long long)t1 * QT + 32) sum += lines[strip * P.line + entry];
+        }
+        sums[k][tid] += sum;
     }
-    P.diagonals[bh * n + at] = sum;
+    for (int w = 128; w > 0; w /= 2) {
+        __syncthreads();
+        for (int y = tid; y < MRF_TABLE_BUCKETS * w; y += 256) sums[y / w][y % w] += sums[y / w][y % w + w];
+    }
+    __syncthreads();
+    if (tid < MRF_TABLE_BUCKETS && first_bucket + tid < P.n_buckets)
+        P.partial[((size_t)h * P.n_buckets + first_bucket + tid) * MRF_TABLE_PARTS + part] = sums[tid][0];
 }
 
-// Gradient of the table: a workgroup has 32 buckets of a head, 8 threads each; a diagonal's bucket is that of its offset.
-__global__ void __launch_bounds__(256) mrf_attn_buckets(const MrfAttnParams P)
+// a wavefront sums the parts of a bucket (none: 0)
+__global__ void __launch_bounds__(256) mrf_attn_table(const MrfAttnParams P)
 {
-    __shared__ float value[1024];
-    __shared__ int bucket[1024];
-    __shared__ float part[8][33];
-    const int blocks = (P.n_buckets + 31) / 32, h = blockIdx.x / blocks, w = threadIdx.x % 32, slice = threadIdx.x / 32;
-    const int mine = (int)(blockIdx.x % blocks) * 32 + w;
-    const long long n = P.B && P.Q && P.K ? (long long)P.Q + P.K - 1 : 0;
-    double sum = 0.0;
-    for (int b = 0; b < P.B; ++b) {
-        const MrfAttnBatch s(P, b);
-        for (long long base = 0; base < n; base += 1024) {
-            __syncthreads();
-            for (int x = threadIdx.x; x < 1024; x += 256) {
-                const long long at = base + x;
-                int k = -1;
-                if (at < n) {
-                    long long m = s.map + at - (P.Q - 1);
-                    m = m < 0 ? 0 : m >= P.n_offsets ? P.n_offsets - 1 : m;
-                    k = P.bucket_of[m];
-                    k = k < 0 ? 0 : k >= P.n_buckets ? P.n_buckets - 1 : k;
-                    value[x] = P.diagonals[((long long)b * P.Hq + h) * n + at];
-                }
-                bucket[x] = k;
-            }
-            __syncthreads();
-            for (int x = slice * 128; x < slice * 128 + 128; ++x)
-                if (bucket[x] == mine) sum += value[x];
-        }
-    }
-    part[slice][w] = (float)sum;
-    __syncthreads();
-    if (slice == 0 && mine < P.n_buckets) {
-        float total = 0.0f;
-#pragma unroll
-        for (int x = 0; x < 8; ++x) total += part[x][w];
-        P.dtable[P.heads_last ? (size_t)mine * P.Hq + h : (size_t)h * P.n_buckets + mine] = total;
-    }
+    const long long x = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (x >= (long long)P.Hq * P.n_buckets) return;
+    const int lane = threadIdx.x & 63, h = (int)(x / P.n_buckets), k = (int)(x - (long long)h * P.n_buckets);
+    float sum = 0.0f;
+    for (int p = lane; p < P.parts; p += 64) sum += P.partial[x * MRF_TABLE_PARTS + p];
+    sum = mrf_lanes_sum<64>(sum);
+    if (lane == 0) P.dtable[P.heads_last ? (size_t)k * P.Hq + h : (size_t)h * P.n_buckets + k] = sum;
 }
 
 namespace mrf_host {
@@ -395,7 +390,7 @@ size_t attention_backward_bytes(const MrfAttnParams &given)
     size_t n = round256((size_t)P.B * P.Hq * P.Q * sizeof(float));
     if (P.table && P.Q && P.K) {
         attention_lines(P);
-        n += round256((size_t)P.B * P.Hq * P.strips * P.line * sizeof(float)) + (size_t)P.B * P.Hq * ((size_t)P.Q + P.K - 1) * sizeof(float);
+        n += round256((size_t)P.B * P.Hq * P.strips * P.line * sizeof(float)) + (size_t)P.Hq * P.n_buckets * MRF_TABLE_PARTS * sizeof(float);
     }
     return n ? n : 256;
 }
@@ -415,11 +410,19 @@ template <class T, int DP> static int attention_back(const MrfAttnParams &P, hip
         else mrf_attn_bwd_keys<T, DP, false, false><<<grid, 256, 0, st>>>(P);
     }
     if (P.dtable) {
+        MrfAttnParams S = P;
+        S.parts = 0;
         if (pairs) {
-            const long long n = ((long long)P.Q + P.K - 1 + 255) / 256;
-            mrf_attn_diagonals<mrf_attn_bwd_rows<T>()><<<(unsigned)(n * P.B * P.Hq), 256, 0, st>>>(P);
+            // workgroups for the whole card twice over, as far as there are pieces for them
+            const long long all = ((long long)P.Q + P.K - 1 + 255) / 256 * P.B;
+            long long parts = 512 / P.Hq < 1 ? 1 : 512 / P.Hq > MRF_TABLE_PARTS ? MRF_TABLE_PARTS : 512 / P.Hq;
+            if (parts > all) parts = all;
+            S.pieces = (all + parts - 1) / parts;
+            S.parts = (int)((all + S.pieces - 1) / S.pieces);
+            const dim3 grid((unsigned)S.parts, (unsigned)P.Hq, (unsigned)((P.n_buckets + MRF_TABLE_BUCKETS - 1) / MRF_TABLE_BUCKETS));
+            mrf_attn_buckets<mrf_attn_bwd_rows<T>()><<<grid, 256, 0, st>>>(S);
         }
-        mrf_attn_buckets<<<(unsigned)P.Hq * ((P.n_buckets + 31) / 32), 256, 0, st>>>(P);
+        mrf_attn_table<<<(unsigned)(((long long)P.Hq * P.n_buckets + 3) / 4), 256, 0, st>>>(S);
     }
     return launch_status("mrf_attn_bwd");
 }
@@ -451,7 +454,7 @@ int mrf_attention_backward(const mrf_attention *att, const void *grad_out, const
     attention_lines(P);
     P.delta = (float *)workspace;
     P.lines = (float *)((char *)workspace + round256((size_t)P.B * P.Hq * P.Q * sizeof(float)));
-    P.diagonals = (float *)((char *)P.lines + round256((size_t)P.B * P.Hq * P.strips * P.line * sizeof(float)));
+    P.partial = (float *)((char *)P.lines + round256((size_t)P.B * P.Hq * P.strips * P.line * sizeof(float)));
     hipStream_t st = (hipStream_t)hip_stream;
     if (att->type == MRF_F32) return attention_back_typed<float>(P, st);
     return att->type == MRF_F16 ? attention_back_typed<mrf_f16>(P, st) : attention_back_typed<mrf_bf16>(P, st);
