@@ -1,4 +1,4 @@
-"""Build step of libmrfmp: sixteen hipcc compilations side by side and a link, in-tree output next to
+"""Build step of libmrfmp: nineteen hipcc compilations side by side and a link, in-tree output next to
 the sources."""
 from __future__ import annotations
 
@@ -19,6 +19,12 @@ HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall"]
 
 
+# The attention's sums stay where the other instructions reach them: left to itself the compiler keeps them in the accumulation registers and moves hundreds of
+# values a tile to and fro.  (Kernels that have no room for that are units of their own, without this flag.)  None of these kernels may need scratch memory beside
+# accumulation registers: this compiler has made wrong code of such ones.
+UNIT_FLAGS = {"mrfmp_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "mrfmp_attention_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+
+
 def is_stale() -> bool:
     if not os.path.exists(LIB_PATH):
         return True
@@ -36,7 +42,9 @@ def build(verbose: bool = False) -> str:
     flags = [f for f in HIPCC_FLAGS if f != "-shared"]
     jobs = []
     units = [("mrfmp_part%d.o" % part, ["-DMRF_PART=%d" % part], SOURCES) for part in range(1, 10)]
-    units += [(f.replace(".hip", ".o"), [], [f]) for f in LEARN_SOURCES]
+    units += [(f.replace(".hip", ".o"), UNIT_FLAGS.get(f, []), [f]) for f in LEARN_SOURCES]
+    units += [(f.replace(".hip", "_f32.o"), ["-DMRF_ATTENTION_F32"], [f]) for f in UNIT_FLAGS]
+    units.append(("mrfmp_attention_bwd_128.o", ["-DMRF_ATTENTION_128"], ["mrfmp_attention_bwd.hip"]))
     for name, defines, sources in units:
         obj = os.path.join(objdir, name)
         cmd = [hipcc, *flags, *defines, "-c", "-o", obj, *sources]

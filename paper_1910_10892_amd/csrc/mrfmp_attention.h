@@ -55,6 +55,7 @@ template <int PER, class T> __device__ inline void mrf_load_part(const T *row, i
             const T x = row[d + j < D ? d + j : D - 1];
             v[j] = there && d + j < D ? x : (T)0.0f;
         }
+        __builtin_amdgcn_sched_barrier(0);      // (the loads of one part at a time: all at once would take the registers that the sums need)
     }
 }
 
@@ -66,6 +67,38 @@ template <class T> __device__ inline typename MrfFrag<T>::type mrf_load8(const T
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] = v[j];
     return f;
+}
+
+// keeps a branch that all lanes take together: its instructions would otherwise be carried out, and their results left, by every tile that needs none of them
+__device__ inline void mrf_stay_branch() { asm volatile(""); }
+
+// N steps use(n, operands(n)): the operands of GROUP steps are on their way from LDS while the GROUP before is multiplied.  (In the compiler's own order a product waits
+// for its operand's whole way, three times what it takes itself.)
+template <int N, int GROUP, class Get, class Use> __device__ inline void mrf_ahead(const Get &get, const Use &use)
+{
+    static_assert(N % GROUP == 0, "whole groups");
+    if constexpr (GROUP == 1) {      // (32 bits: a step takes longer than its operand's way)
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            use(n, get(n));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        return;
+    }
+    decltype(get(0)) f[2][GROUP];
+#pragma unroll
+    for (int i = 0; i < GROUP; ++i) f[0][i] = get(i);
+#pragma unroll
+    for (int g = 0; g < N / GROUP; ++g) {
+        if (g + 1 < N / GROUP) {
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i) f[(g + 1) & 1][i] = get((g + 1) * GROUP + i);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < GROUP; ++i) use(g * GROUP + i, f[g & 1][i]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
 }
 
 struct MrfAttnParams {
@@ -125,13 +158,27 @@ __device__ inline float mrf_attn_bias(const MrfAttnParams &P, const MrfAttnBatch
     return P.table[P.heads_last ? (size_t)b * P.Hq + h : (size_t)h * P.n_buckets + b] * 1.44269504088896340736f;
 }
 
-// Rows of a tensor in LDS: ROWS of DP entries, 16 bytes apart from one another's place in the banks.  A thread moves chunks of 16 bytes, which wait in
-// its registers between the load and the store.
+// Rows of a tensor in LDS: ROWS of DP entries.  A thread moves chunks of 16 bytes, which wait in its registers between the load and the store.  In 16 bits chunk c
+// of row r lies at place c ^ swap(r): 16 rows' chunks c (an operand along the rows), and four rows' stretches of 32 entries (one across them), then
+// fall on all banks.  (With rows 16 bytes longer instead, half of the reads' cycles were conflicts.)  In 32 bits rows are 16 bytes longer: an operand across them
+// is read entry by entry, from places that are known when it is compiled.
 template <class T, int DP, int ROWS, int NT> struct MrfRows {
-    static constexpr int PER = 16 / (int)sizeof(T), LD = DP + PER, CHUNKS = ROWS * DP / PER, N = (CHUNKS + NT - 1) / NT;
+    static constexpr int PER = 16 / (int)sizeof(T), LD = sizeof(T) == 2 ? DP : DP + PER, CPR = DP / PER, CHUNKS = ROWS * CPR, N = (CHUNKS + NT - 1) / NT;
     typedef T vec __attribute__((ext_vector_type(PER)));
     typedef T uvec __attribute__((ext_vector_type(PER), aligned(sizeof(T))));
     vec r[N];
+
+    static __device__ inline int swap(int row)
+    {
+        if constexpr (CPR >= 16) return (row & 3) << 2 | (row >> 2 & 3);
+        else if constexpr (CPR == 8) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+        else return row >> 2 & 3;
+    }
+    static __device__ inline int place(int row, int chunk)
+    {
+        if constexpr (sizeof(T) == 4) return row * LD + chunk * PER;
+        else return row * LD + (chunk ^ swap(row)) * PER;
+    }
 
     // rows from `at` on, `rows` (1 at least) of them; of a row D entries; the others are 0
     __device__ inline void load(const T *at, long long stride, int rows, int D)
@@ -161,19 +208,18 @@ template <class T, int DP, int ROWS, int NT> struct MrfRows {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int c = (int)threadIdx.x + n * NT, row = c / (DP / PER), d = c % (DP / PER) * PER;
-            *(vec *)(lds + row * LD + d) = r[n];
+            *(vec *)(lds + place(row, d / PER)) = r[n];
         }
     }
     // operand whose 32 rows are rows row0 ..., and whose sum runs over 16 entries from d on
     static __device__ inline typename MrfFrag<T>::type along(const T *lds, int row0, int d)
     {
-        const int lane = threadIdx.x & 63;
-        const T *p = lds + (row0 + (lane & 31)) * LD + d + 8 * (lane >> 5);
+        const int lane = threadIdx.x & 63, row = row0 + (lane & 31), at = d + 8 * (lane >> 5);
         if constexpr (sizeof(T) == 2) {
-            return *(const typename MrfFrag<T>::type *)p;
+            return *(const typename MrfFrag<T>::type *)(lds + place(row, at / PER));
         } else {
             typename MrfFrag<T>::type f;
-            const vec a = *(const vec *)p, b = *(const vec *)(p + 4);
+            const vec a = *(const vec *)(lds + place(row, at / PER)), b = *(const vec *)(lds + place(row, at / PER + 1));
 #pragma unroll
             for (int j = 0; j < 4; ++j) f[j] = a[j], f[4 + j] = b[j];
             return f;
@@ -188,9 +234,10 @@ template <class T, int DP, int ROWS, int NT> struct MrfRows {
             // the transposing read: of 16 lanes, four each point at a row's 16 entries, and each gets the four rows' values of one entry
             typedef short v4 __attribute__((ext_vector_type(4)));
             typedef short v8 __attribute__((ext_vector_type(8)));
-            const T *p = lds + (row0 + 4 * half + (lane >> 2 & 3)) * LD + d + (lane & 16) + 4 * (lane & 3);
+            const int row = row0 + 4 * half + (lane >> 2 & 3), at = d + (lane & 16) + 4 * (lane & 3);
+            const T *p = lds + place(row, at / PER) + at % PER, *n = lds + place(row + 8, at / PER) + at % PER;
             const v4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4 *)p);
-            const v4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4 *)(p + 8 * LD));
+            const v4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4 *)n);
             const v8 ab = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
             f = __builtin_bit_cast(typename MrfFrag<T>::type, ab);
         } else {
@@ -269,4 +316,13 @@ template <class T> __device__ inline void mrf_store4(T *row, int d, int D, const
 
 namespace mrf_host {
 int attention_check(const mrf_attention *a, MrfAttnParams &P);
+
+// Rows of queries go together where there are few on one head of keys, and the keys are then divided so that there are enough workgroups.
+struct AttnPlan { bool pack; int splits; unsigned grid; };
+
+// The kernels in 32 bits (MRF_ATTENTION_F32) and those of the backward pass for heads of more than 64 entries in 16 bits (MRF_ATTENTION_128) are translation units of
+// their own: their sums are held in the accumulation registers, there being no room for them in the others.
+int attention_forward_f32(const MrfAttnParams &P, const AttnPlan &plan, hipStream_t st);
+int attention_backward_f32(const MrfAttnParams &P, hipStream_t st);
+int attention_backward_128(const MrfAttnParams &P, int type, hipStream_t st);
 }

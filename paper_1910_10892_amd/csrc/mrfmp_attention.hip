@@ -11,9 +11,16 @@
 // Keys of a tile: as many as two tiles of keys and values in LDS leave two workgroups (32 bits: one or two) on a compute unit.
 template <class T, int NW> constexpr int mrf_attn_keys() { return sizeof(T) == 4 || NW == 1 ? 32 : 64; }
 
+// Wavefronts of a SIMD: two, where their registers fit (in 32 bits not for 128 entries)
+template <class T, int DP, int NW> constexpr int mrf_attn_waves() { return NW == 1 || (sizeof(T) == 4 && DP == 128) ? 1 : 2; }
+
+// Wavefronts of a workgroup for many queries: with eight, a tile of keys and values of 128 entries takes half the registers on its way to LDS, and two wavefronts
+// fit on a SIMD
+template <class T, int DP> constexpr int mrf_attn_wide() { return sizeof(T) == 2 && DP == 128 ? 8 : 4; }
+
 // NW wavefronts; PACK: a row is a query of a head of the group that shares keys (row = query G + head of the group), else a query of one head;
 // BIAS: with a table.
-template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launch_bounds__(64 * NW) mrf_attn_fwd(const MrfAttnParams P)
+template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launch_bounds__(64 * NW, (mrf_attn_waves<T, DP, NW>())) mrf_attn_fwd(const MrfAttnParams P)
 {
     constexpr int KT = mrf_attn_keys<T, NW>(), NT = 64 * NW, ROWS = 32 * NW, LINE = ROWS + KT;
     typedef MrfRows<T, DP, KT, NT> Rows;
@@ -61,6 +68,10 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
             if ((int)threadIdx.x < LINE) line[buf][threadIdx.x] = bias_next;
     };
 
+    // Of two wavefronts on a SIMD one goes first: it multiplies while the other takes exponentials, instead of both doing the same at a time.
+    if constexpr (NW == 8)
+        if (wv < 4) __builtin_amdgcn_s_setprio(1);
+
     mrf_acc o[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
@@ -79,31 +90,46 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
         if (w0 <= w1 && k0 < s.to(w1) && k0 + KT > s.from(w0)) {
             mrf_acc c[KT / 32];
 #pragma unroll
-            for (int u = 0; u < KT / 32; ++u) {
+            for (int u = 0; u < KT / 32; ++u)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) c[u][e] = 0.0f;
-#pragma unroll
-                for (int d = 0; d < DP / 16; ++d) c[u] = mrf_mma(Rows::along(ldsK[buf], 32 * u, 16 * d), qf[d], c[u]);
-            }
+            constexpr int STEPS = KT / 32 * DP / 16;
+            mrf_ahead<STEPS, (sizeof(T) == 4 ? 1 : DP == 128 ? 2 : STEPS < 4 ? STEPS : 4)>([&](int n) { return Rows::along(ldsK[buf], 32 * (n / (DP / 16)), n % (DP / 16) * 16); },
+                                                      [&](int n, const frag &f) { c[n / (DP / 16)] = mrf_mma(f, qf[n % (DP / 16)], c[n / (DP / 16)]); });
             // keys that this lane's query may see: [from, to) of the tile; all of them, for most tiles
             const bool whole = k0 >= w1 + s.lo && k0 + KT - 1 <= w0 + s.hi && k0 + KT <= s.nk && (w2 == w1 || s.nq == P.Q);
             const int from = i + s.lo - k0, to = there ? min(i + s.hi + 1, s.nk) - k0 : 0;
+            // (without a bias the scores stay products, whose maximum is the scores' too, and the scale goes in with the maximum: one operation)
             float top = -INFINITY;
 #pragma unroll
             for (int u = 0; u < KT / 32; ++u)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int j = 32 * u + mrf_acc_row(e, half);
-                    float x = c[u][e] * P.c;
+                    float x = c[u][e];
                     if constexpr (BIAS) {
-                        if constexpr (PACK) x += mrf_attn_bias(P, s, min(h, P.Hq - 1), (long long)k0 + j - i);
-                        else x += line[buf][ROWS - 1 + j - (wv * 32 + (lane & 31))];
+                        if constexpr (PACK) x = fmaf(x, P.c, mrf_attn_bias(P, s, h, (long long)k0 + j - i));
+                        else x = fmaf(x, P.c, line[buf][ROWS - 1 + j - (wv * 32 + (lane & 31))]);
                     }
-                    if (!whole) x = j >= from && j < to ? x : -INFINITY;
                     c[u][e] = x;
-                    top = fmaxf(top, x);
                 }
-            top = fmaxf(m, mrf_halves_max(top));
+            if (!whole) {
+                mrf_stay_branch();
+#pragma unroll
+                for (int u = 0; u < KT / 32; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int j = 32 * u + mrf_acc_row(e, half);
+                        c[u][e] = j >= from && j < to ? c[u][e] : -INFINITY;
+                    }
+            }
+#pragma unroll
+            for (int u = 0; u < KT / 32; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, c[u][e]);
+            top = mrf_halves_max(top);
+            if constexpr (!BIAS) top *= P.c;
+            top = fmaxf(m, top);
             const float base = top == -INFINITY ? 0.0f : top, low = base - mrf_attn_shift<T>();
             if (__any(top > m)) {
                 const float less = __builtin_amdgcn_exp2f(m - base);
@@ -114,21 +140,28 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
                     for (int e = 0; e < 16; ++e) o[d][e] *= less;
                 m = top;
             }
+            // 16 keys at a time: their probabilities, and their values on the way, while those before are multiplied
+            frag vf[2][DP / 32], p[2];
+            const auto part = [&](int y) {
+                mrf_acc &x = c[y / 2];
 #pragma unroll
-            for (int u = 0; u < KT / 32; ++u)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    c[u][e] = __builtin_amdgcn_exp2f(c[u][e] - low);
-                    l += c[u][e];
+                for (int e = 8 * (y % 2); e < 8 * (y % 2) + 8; ++e) {
+                    x[e] = __builtin_amdgcn_exp2f(BIAS ? x[e] - low : fmaf(x[e], P.c, -low));
+                    l += x[e];
                 }
+                p[y % 2] = mrf_acc_frag<T>(x, y % 2);
 #pragma unroll
-            for (int u = 0; u < KT / 32; ++u)
+                for (int d = 0; d < DP / 32; ++d) vf[y % 2][d] = Rows::across(ldsV[buf], 16 * y, 32 * d);
+            };
+            part(0);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const frag p = mrf_acc_frag<T>(c[u], x);
+            for (int y = 0; y < KT / 16; ++y) {
+                if (y + 1 < KT / 16) part(y + 1);
 #pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) o[d] = mrf_mma(Rows::across(ldsV[buf], 32 * u + 16 * x, 32 * d), p, o[d]);
-                }
+                for (int d = 0; d < DP / 32; ++d) o[d] = mrf_mma(vf[y % 2][d], p[y % 2], o[d]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         if (t + 1 < t1) store(buf ^ 1);
         __syncthreads();
@@ -188,6 +221,32 @@ template <class T> __global__ void __launch_bounds__(256) mrf_attn_join(const Mr
 
 namespace mrf_host {
 
+template <class T, int DP> static int attention_go(const MrfAttnParams &P, const AttnPlan &plan, hipStream_t st)
+{
+    const dim3 grid(plan.grid, (unsigned)P.splits);
+    if (plan.pack) {
+        if (P.table) mrf_attn_fwd<T, DP, 1, true, true><<<grid, 64, 0, st>>>(P);
+        else mrf_attn_fwd<T, DP, 1, true, false><<<grid, 64, 0, st>>>(P);
+        if (P.splits > 1) mrf_attn_join<T><<<(unsigned)(((long long)P.B * P.Hq * P.Q + 3) / 4), 256, 0, st>>>(P);
+    } else {
+        constexpr int NW = mrf_attn_wide<T, DP>();
+        if (P.table) mrf_attn_fwd<T, DP, NW, false, true><<<grid, 64 * NW, 0, st>>>(P);
+        else mrf_attn_fwd<T, DP, NW, false, false><<<grid, 64 * NW, 0, st>>>(P);
+    }
+    return launch_status("mrf_attn_fwd");
+}
+
+template <class T> static int attention_typed(const MrfAttnParams &P, const AttnPlan &plan, hipStream_t st)
+{
+    if (P.D <= 32) return attention_go<T, 32>(P, plan, st);
+    return P.D <= 64 ? attention_go<T, 64>(P, plan, st) : attention_go<T, 128>(P, plan, st);
+}
+
+#ifdef MRF_ATTENTION_F32
+int attention_forward_f32(const MrfAttnParams &P, const AttnPlan &plan, hipStream_t st) { return attention_typed<float>(P, plan, st); }
+}  // namespace mrf_host
+#else
+
 int attention_check(const mrf_attention *a, MrfAttnParams &P)
 {
     if (!a) return MRF_ERR_NULL_POINTER;
@@ -220,43 +279,21 @@ int attention_check(const mrf_attention *a, MrfAttnParams &P)
     return MRF_OK;
 }
 
-// Few rows on one head of keys: they go together, and the keys are divided so that there are enough workgroups.
-struct AttnPlan { bool pack; int splits; unsigned grid; };
-
-static AttnPlan attention_plan(const MrfAttnParams &P)
+static AttnPlan attention_plan(const MrfAttnParams &P, int type)
 {
     const long long rows = (long long)P.Q * P.G;
-    if (P.Q > 16 && rows > 64) return {false, 1, (unsigned)((long long)P.B * P.Hq * ((P.Q + 127) / 128))};
+    const int block = type != MRF_F32 && P.D > 64 ? 256 : 128;      // (as mrf_attn_wide has it)
+    if (P.Q > 16 && rows > 64) return {false, 1, (unsigned)((long long)P.B * P.Hq * ((P.Q + block - 1) / block))};
     const long long groups = (long long)P.B * P.Hk * ((rows + 31) / 32), tiles = (P.K + 31) / 32;
     long long splits = groups ? 2048 / groups : 1;
     if (splits > tiles / 4) splits = tiles / 4;
     return {true, (int)(splits < 1 ? 1 : splits), (unsigned)groups};
 }
 
-static size_t attention_forward_bytes(const MrfAttnParams &P)
+static size_t attention_forward_bytes(const MrfAttnParams &P, int type)
 {
-    const AttnPlan plan = attention_plan(P);
+    const AttnPlan plan = attention_plan(P, type);
     return plan.splits > 1 ? (size_t)plan.splits * P.B * P.Hq * P.Q * (P.D + 2) * sizeof(float) : 0;
-}
-
-template <class T, int DP> static int attention_go(const MrfAttnParams &P, const AttnPlan &plan, hipStream_t st)
-{
-    const dim3 grid(plan.grid, (unsigned)P.splits);
-    if (plan.pack) {
-        if (P.table) mrf_attn_fwd<T, DP, 1, true, true><<<grid, 64, 0, st>>>(P);
-        else mrf_attn_fwd<T, DP, 1, true, false><<<grid, 64, 0, st>>>(P);
-        if (P.splits > 1) mrf_attn_join<T><<<(unsigned)(((long long)P.B * P.Hq * P.Q + 3) / 4), 256, 0, st>>>(P);
-    } else {
-        if (P.table) mrf_attn_fwd<T, DP, 4, false, true><<<grid, 256, 0, st>>>(P);
-        else mrf_attn_fwd<T, DP, 4, false, false><<<grid, 256, 0, st>>>(P);
-    }
-    return launch_status("mrf_attn_fwd");
-}
-
-template <class T> static int attention_typed(const MrfAttnParams &P, const AttnPlan &plan, hipStream_t st)
-{
-    if (P.D <= 32) return attention_go<T, 32>(P, plan, st);
-    return P.D <= 64 ? attention_go<T, 64>(P, plan, st) : attention_go<T, 128>(P, plan, st);
 }
 
 size_t attention_backward_bytes(const MrfAttnParams &P);
@@ -271,7 +308,7 @@ size_t mrf_attention_workspace_bytes(const mrf_attention *att, int backward)
 {
     MrfAttnParams P = {};
     if (attention_check(att, P) != MRF_OK) return 0;
-    return backward ? attention_backward_bytes(P) : attention_forward_bytes(P);
+    return backward ? attention_backward_bytes(P) : attention_forward_bytes(P, att->type);
 }
 
 int mrf_attention_forward(const mrf_attention *att, void *out, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream)
@@ -280,16 +317,17 @@ int mrf_attention_forward(const mrf_attention *att, void *out, float *lse, void 
     const int rc = attention_check(att, P);
     if (rc != MRF_OK || P.B == 0 || P.Q == 0) return rc;
     if (!P.q || !out || (P.K && (!P.k || !P.v))) return MRF_ERR_NULL_POINTER;
-    const AttnPlan plan = attention_plan(P);
+    const AttnPlan plan = attention_plan(P, att->type);
     P.out = out; P.lse = lse; P.splits = plan.splits;
     if (plan.splits > 1) {
         if (!workspace) return MRF_ERR_NULL_POINTER;
-        if (workspace_bytes < attention_forward_bytes(P)) return MRF_ERR_WORKSPACE_TOO_SMALL;
+        if (workspace_bytes < attention_forward_bytes(P, att->type)) return MRF_ERR_WORKSPACE_TOO_SMALL;
         P.part = (float *)workspace;
     }
     hipStream_t st = (hipStream_t)hip_stream;
-    if (att->type == MRF_F32) return attention_typed<float>(P, plan, st);
+    if (att->type == MRF_F32) return attention_forward_f32(P, plan, st);
     return att->type == MRF_F16 ? attention_typed<mrf_f16>(P, plan, st) : attention_typed<mrf_bf16>(P, plan, st);
 }
 
 }  // extern "C"
+#endif

@@ -13,6 +13,8 @@
 
 template <class T> constexpr int mrf_attn_bwd_rows() { return sizeof(T) == 4 ? 32 : 64; }
 
+template <class F> struct MrfTwo { F a, b; };
+
 // ---- dq, and delta
 template <class T, int DP, bool BIAS> __global__ void __launch_bounds__(256) mrf_attn_bwd_queries(const MrfAttnParams P)
 {
@@ -92,34 +94,40 @@ template <class T, int DP, bool BIAS> __global__ void __launch_bounds__(256) mrf
                 mrf_acc c, dp;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) c[e] = dp[e] = 0.0f;
-#pragma unroll
-                for (int d = 0; d < DP / 16; ++d) {
-                    c = mrf_mma(Rows::along(ldsK[buf], 32 * u, 16 * d), qf[d], c);
-                    dp = mrf_mma(Rows::along(ldsV[buf], 32 * u, 16 * d), gf[d], dp);
-                }
+                mrf_ahead<DP / 16, (sizeof(T) == 4 ? 1 : 2)>([&](int d) { return MrfTwo<frag>{Rows::along(ldsK[buf], 32 * u, 16 * d), Rows::along(ldsV[buf], 32 * u, 16 * d)}; },
+                                      [&](int d, const MrfTwo<frag> &f) {
+                                          c = mrf_mma(f.a, qf[d], c);
+                                          dp = mrf_mma(f.b, gf[d], dp);
+                                      });
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const int j = 32 * u + mrf_acc_row(e, half);
                     float x;
                     if constexpr (BIAS) x = fmaf(c[e], P.c, line[buf][ROWS - 1 + j - (wv * 32 + (lane & 31))]) - lse;
                     else x = fmaf(c[e], P.c, -lse);
-                    float p = __builtin_amdgcn_exp2f(x);
-                    if (!whole) p = j >= from && j < to ? p : 0.0f;
-                    c[e] = p;
-                    dp[e] = p * (dp[e] - delta);
+                    c[e] = __builtin_amdgcn_exp2f(x);
+                }
+                if (!whole) {
+                    mrf_stay_branch();
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int j = 32 * u + mrf_acc_row(e, half);
+                        c[e] = j >= from && j < to ? c[e] : 0.0f;
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    dp[e] = c[e] * (dp[e] - delta);
                     left += dp[e];
                 }
                 range.fit(dp, dq);
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const frag sf = mrf_acc_frag<T>(dp, x), pf = mrf_acc_frag<T>(c, x);
-#pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) {
-                        const frag kt = Rows::across(ldsK[buf], 32 * u + 16 * x, 32 * d);
-                        dq[d] = mrf_mma(kt, sf, dq[d]);
-                        if constexpr (MEAN) mean[d] = mrf_mma(kt, pf, mean[d]);
-                    }
-                }
+                const frag sf[2] = {mrf_acc_frag<T>(dp, 0), mrf_acc_frag<T>(dp, 1)}, pf[2] = {mrf_acc_frag<T>(c, 0), mrf_acc_frag<T>(c, 1)};
+                mrf_ahead<DP / 16, (sizeof(T) == 4 ? 1 : 2)>([&](int n) { return Rows::across(ldsK[buf], 32 * u + 16 * (n / (DP / 32)), n % (DP / 32) * 32); },
+                                      [&](int n, const frag &f) {
+                                          const int x = n / (DP / 32), d = n % (DP / 32);
+                                          dq[d] = mrf_mma(f, sf[x], dq[d]);
+                                          if constexpr (MEAN) mean[d] = mrf_mma(f, pf[x], mean[d]);
+                                      });
             }
         }
         if (t + 1 < t1) store(buf ^ 1);
@@ -158,7 +166,8 @@ template <int QT> __device__ inline void mrf_attn_query_tiles(const MrfAttnBatch
 // block the later 31 go on in the next one, whose lanes are 32 less, and 32 are done and written.  An entry of the line: query - (key - first key) + 31.
 constexpr int MRF_SKEW = 71;      // from row to row: the halves of a wavefront, four rows apart, fall on the two halves of the banks
 
-template <class T, int DP, bool BIAS, bool TABLE> __global__ void __launch_bounds__(256) mrf_attn_bwd_keys(const MrfAttnParams P)
+// DK, DV: which of the two it sums.  Both, where their sums and the keys and values fit into the registers, else one launch for each.
+template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV> __global__ void __launch_bounds__(256) mrf_attn_bwd_keys(const MrfAttnParams P)
 {
     constexpr int QT = mrf_attn_bwd_rows<T>(), NT = 256, KEYS = 128, LINE = KEYS + QT;
     typedef MrfRows<T, DP, QT, NT> Rows;
@@ -175,23 +184,23 @@ template <class T, int DP, bool BIAS, bool TABLE> __global__ void __launch_bound
     int t0, t1;
     mrf_attn_query_tiles<QT>(s, k0, t0, t1);
 
-    frag kf[DP / 16] = {}, vf[DP / 16] = {};
+    frag kf[DP / 16] = {}, vf[DK ? DP / 16 : 1] = {};
     if (w0 <= w1) {
         const int at = min(j, w1);
         const T *k = (const T *)P.k + b * P.ks[0] + at * P.ks[1] + hk * P.ks[2], *v = (const T *)P.v + b * P.vs[0] + at * P.vs[1] + hk * P.vs[2];
 #pragma unroll
         for (int t = 0; t < DP / 16; ++t) {
             kf[t] = mrf_load8(k, 16 * t + 8 * half, P.D, j < s.nk);
-            vf[t] = mrf_load8(v, 16 * t + 8 * half, P.D, j < s.nk);
+            if constexpr (DK) vf[t] = mrf_load8(v, 16 * t + 8 * half, P.D, j < s.nk);
         }
     }
     if constexpr (TABLE)
         for (int n = lane; n < 32 * MRF_SKEW; n += 64) skew[wv][n] = 0.0f;
-    mrf_acc dk[DP / 32], dv[DP / 32];
+    mrf_acc dk[DK ? DP / 32 : 1], dv[DV ? DP / 32 : 1];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) dk[d][e] = dv[d][e] = 0.0f;
+        for (int e = 0; e < 16; ++e) dk[DK ? d : 0][e] = dv[DV ? d : 0][e] = 0.0f;
 
     MrfRange<T> range;
     Rows qr, gr;
@@ -243,11 +252,16 @@ template <class T, int DP, bool BIAS, bool TABLE> __global__ void __launch_bound
                     mrf_acc c, dp;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) c[e] = dp[e] = 0.0f;
-#pragma unroll
-                    for (int d = 0; d < DP / 16; ++d) {
-                        c = mrf_mma(Rows::along(ldsQ[buf], 32 * u, 16 * d), kf[d], c);
-                        dp = mrf_mma(Rows::along(ldsG[buf], 32 * u, 16 * d), vf[d], dp);
-                    }
+                    mrf_ahead<DP / 16, (sizeof(T) == 4 ? 1 : 2)>(
+                        [&](int d) {
+                            MrfTwo<frag> f = {Rows::along(ldsQ[buf], 32 * u, 16 * d), {}};
+                            if constexpr (DK) f.b = Rows::along(ldsG[buf], 32 * u, 16 * d);
+                            return f;
+                        },
+                        [&](int d, const MrfTwo<frag> &f) {
+                            c = mrf_mma(f.a, kf[d], c);
+                            if constexpr (DK) dp = mrf_mma(f.b, vf[DK ? d : 0], dp);
+                        });
 #pragma unroll
                     for (int e4 = 0; e4 < 16; e4 += 4) {
                         const int r4 = 32 * u + mrf_acc_row(e4, half);
@@ -259,12 +273,20 @@ template <class T, int DP, bool BIAS, bool TABLE> __global__ void __launch_bound
                             float x;
                             if constexpr (BIAS) x = fmaf(c[e], P.c, line[buf][QT - 1 + (wv * 32 + (lane & 31)) - r]) - lse[n];
                             else x = fmaf(c[e], P.c, -lse[n]);
-                            float p = __builtin_amdgcn_exp2f(x);
-                            if (!whole) p = r >= from && r < to ? p : 0.0f;
-                            c[e] = p;
-                            dp[e] = p * (dp[e] - delta[n]);
+                            c[e] = __builtin_amdgcn_exp2f(x);
+                            dp[e] -= delta[n];
                         }
                     }
+                    if (!whole) {
+                        mrf_stay_branch();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const int r = 32 * u + mrf_acc_row(e, half);
+                            c[e] = r >= from && r < to ? c[e] : 0.0f;
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) dp[e] *= c[e];
                     if constexpr (TABLE) {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
@@ -272,16 +294,25 @@ template <class T, int DP, bool BIAS, bool TABLE> __global__ void __launch_bound
                             skew[wv][r * MRF_SKEW + r - (lane & 31) + 31] = dp[e];
                         }
                     }
-                    range.fit(dp, dk);
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const frag pf = mrf_acc_frag<T>(c, x), sf = mrf_acc_frag<T>(dp, x);
-#pragma unroll
-                        for (int d = 0; d < DP / 32; ++d) {
-                            dv[d] = mrf_mma(Rows::across(ldsG[buf], 32 * u + 16 * x, 32 * d), pf, dv[d]);
-                            dk[d] = mrf_mma(Rows::across(ldsQ[buf], 32 * u + 16 * x, 32 * d), sf, dk[d]);
-                        }
+                    frag pf[2], sf[2];
+                    if constexpr (DK) {
+                        range.fit(dp, dk);
+                        sf[0] = mrf_acc_frag<T>(dp, 0), sf[1] = mrf_acc_frag<T>(dp, 1);
                     }
+                    if constexpr (DV) pf[0] = mrf_acc_frag<T>(c, 0), pf[1] = mrf_acc_frag<T>(c, 1);
+                    mrf_ahead<DP / 16, (sizeof(T) == 4 ? 1 : 2)>(
+                        [&](int n) {
+                            const int row = 32 * u + 16 * (n / (DP / 32)), at = n % (DP / 32) * 32;
+                            MrfTwo<frag> f = {};
+                            if constexpr (DV) f.a = Rows::across(ldsG[buf], row, at);
+                            if constexpr (DK) f.b = Rows::across(ldsQ[buf], row, at);
+                            return f;
+                        },
+                        [&](int n, const MrfTwo<frag> &f) {
+                            const int x = n / (DP / 32), d = n % (DP / 32);
+                            if constexpr (DV) dv[DV ? d : 0] = mrf_mma(f.a, pf[x], dv[DV ? d : 0]);
+                            if constexpr (DK) dk[DK ? d : 0] = mrf_mma(f.b, sf[x], dk[DK ? d : 0]);
+                        });
                 }
                 if constexpr (TABLE) {
                     float sum = goes_on;
@@ -309,10 +340,17 @@ template <class T, int DP, bool BIAS, bool TABLE> __global__ void __launch_bound
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
-            const float x[4] = {dk[d][e] * ks, dk[d][e + 1] * ks, dk[d][e + 2] * ks, dk[d][e + 3] * ks};
-            const float y[4] = {dv[d][e] * vs, dv[d][e + 1] * vs, dv[d][e + 2] * vs, dv[d][e + 3] * vs};
-            if (P.dk) mrf_store4((T *)P.dk + row, 32 * d + mrf_acc_row(e, half), P.D, x);
-            if (P.dv) mrf_store4((T *)P.dv + row, 32 * d + mrf_acc_row(e, half), P.D, y);
+            float x[4];
+            if constexpr (DK) {
+#pragma unroll
+                for (int n = 0; n < 4; ++n) x[n] = dk[DK ? d : 0][e + n] * ks;
+                if (P.dk) mrf_store4((T *)P.dk + row, 32 * d + mrf_acc_row(e, half), P.D, x);
+            }
+            if constexpr (DV) {
+#pragma unroll
+                for (int n = 0; n < 4; ++n) x[n] = dv[DV ? d : 0][e + n] * vs;
+                if (P.dv) mrf_store4((T *)P.dv + row, 32 * d + mrf_acc_row(e, half), P.D, x);
+            }
         }
 }
 
@@ -344,11 +382,17 @@ template <int QT> __global__ void __launch_bounds__(256) mrf_attn_buckets(const 
         const float *const lines = P.lines + ((size_t)b * P.Hq + h) * P.strips * P.line;
         const long long first = max(offset, 0LL) / 32, last = min(offset + s.nq - 1, (long long)s.nk - 1);
         float sum = 0.0f;
-        for (long long strip = first; 32 * strip <= last; ++strip) {
+        for (long long strip = first / 4 * 4; 32 * strip <= last; strip += 4) {      // (a workgroup's four strips have the same tiles)
             int t0, t1;
-            mrf_attn_query_tiles<QT>(s, (int)(strip / 4 * 128), t0, t1);
+            mrf_attn_query_tiles<QT>(s, (int)(32 * strip), t0, t1);
             const long long entry = strip * 32 - offset + 31;
-            if (t0 < t1 && entry >= (long long)t0 * QT && entry < (long long)t1 * QT + 32) sum += lines[strip * P.line + entry];
+            float v[4];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const long long e = entry + 32 * w;
+                v[w] = t0 < t1 && e >= (long long)t0 * QT && e < (long long)t1 * QT + 32 ? lines[(strip + w) * P.line + e] : 0.0f;
+            }
+            sum += (v[0] + v[1]) + (v[2] + v[3]);
         }
         sums[k][tid] += sum;
     }
@@ -362,7 +406,7 @@ template <int QT> __global__ void __launch_bounds__(256) mrf_attn_buckets(const 
 }
 
 // a wavefront sums the parts of a bucket (none: 0)
-__global__ void __launch_bounds__(256) mrf_attn_table(const MrfAttnParams P)
+static __global__ void __launch_bounds__(256) mrf_attn_table(const MrfAttnParams P)
 {
     const long long x = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (x >= (long long)P.Hq * P.n_buckets) return;
@@ -375,26 +419,6 @@ __global__ void __launch_bounds__(256) mrf_attn_table(const MrfAttnParams P)
 
 namespace mrf_host {
 
-static size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
-
-// a line for every strip of 32 keys: an entry for each query, as far as whole tiles reach, and 32 more
-static void attention_lines(MrfAttnParams &P)
-{
-    P.strips = (int)(((long long)P.K + 127) / 128 * 4);
-    P.line = (int)(((long long)P.Q + 63) / 64 * 64 + 32);
-}
-
-size_t attention_backward_bytes(const MrfAttnParams &given)
-{
-    MrfAttnParams P = given;
-    size_t n = round256((size_t)P.B * P.Hq * P.Q * sizeof(float));
-    if (P.table && P.Q && P.K) {
-        attention_lines(P);
-        n += round256((size_t)P.B * P.Hq * P.strips * P.line * sizeof(float)) + (size_t)P.Hq * P.n_buckets * MRF_TABLE_PARTS * sizeof(float);
-    }
-    return n ? n : 256;
-}
-
 template <class T, int DP> static int attention_back(const MrfAttnParams &P, hipStream_t st)
 {
     const bool pairs = P.B && P.Q && P.K;
@@ -405,9 +429,15 @@ template <class T, int DP> static int attention_back(const MrfAttnParams &P, hip
     }
     if (P.B && P.K && (P.dk || P.dv || P.dtable)) {
         const unsigned grid = (unsigned)((long long)P.B * P.Hk * ((P.K + 127) / 128));
-        if (P.dtable && pairs) mrf_attn_bwd_keys<T, DP, true, true><<<grid, 256, 0, st>>>(P);
-        else if (P.table) mrf_attn_bwd_keys<T, DP, true, false><<<grid, 256, 0, st>>>(P);
-        else mrf_attn_bwd_keys<T, DP, false, false><<<grid, 256, 0, st>>>(P);
+        constexpr bool ONE = DP == 128 && sizeof(T) == 4;      // one of the two at a time
+        if (P.dtable && pairs) mrf_attn_bwd_keys<T, DP, true, true, true, DP != 128><<<grid, 256, 0, st>>>(P);
+        else if (P.table) mrf_attn_bwd_keys<T, DP, true, false, true, !ONE><<<grid, 256, 0, st>>>(P);
+        else mrf_attn_bwd_keys<T, DP, false, false, true, !ONE><<<grid, 256, 0, st>>>(P);
+        if constexpr (DP == 128)
+            if (P.dv && (ONE || (P.dtable && pairs))) {
+                if (P.table) mrf_attn_bwd_keys<T, DP, true, false, false, true><<<grid, 256, 0, st>>>(P);
+                else mrf_attn_bwd_keys<T, DP, false, false, false, true><<<grid, 256, 0, st>>>(P);
+            }
     }
     if (P.dtable) {
         MrfAttnParams S = P;
@@ -427,10 +457,43 @@ template <class T, int DP> static int attention_back(const MrfAttnParams &P, hip
     return launch_status("mrf_attn_bwd");
 }
 
-template <class T> static int attention_back_typed(const MrfAttnParams &P, hipStream_t st)
+template <class T> [[maybe_unused]] static int attention_back_typed(const MrfAttnParams &P, hipStream_t st)
 {
     if (P.D <= 32) return attention_back<T, 32>(P, st);
-    return P.D <= 64 ? attention_back<T, 64>(P, st) : attention_back<T, 128>(P, st);
+    if (P.D <= 64) return attention_back<T, 64>(P, st);
+    if constexpr (sizeof(T) == 4) return attention_back<T, 128>(P, st);
+    else return attention_backward_128(P, std::is_same<T, mrf_f16>::value ? MRF_F16 : MRF_BF16, st);
+}
+
+#if defined(MRF_ATTENTION_F32)
+int attention_backward_f32(const MrfAttnParams &P, hipStream_t st) { return attention_back_typed<float>(P, st); }
+}  // namespace mrf_host
+#elif defined(MRF_ATTENTION_128)
+int attention_backward_128(const MrfAttnParams &P, int type, hipStream_t st)
+{
+    return type == MRF_F16 ? attention_back<mrf_f16, 128>(P, st) : attention_back<mrf_bf16, 128>(P, st);
+}
+}  // namespace mrf_host
+#else
+
+static size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// a line for every strip of 32 keys: an entry for each query, as far as whole tiles reach, and 32 more
+static void attention_lines(MrfAttnParams &P)
+{
+    P.strips = (int)(((long long)P.K + 127) / 128 * 4);
+    P.line = (int)(((long long)P.Q + 63) / 64 * 64 + 32);
+}
+
+size_t attention_backward_bytes(const MrfAttnParams &given)
+{
+    MrfAttnParams P = given;
+    size_t n = round256((size_t)P.B * P.Hq * P.Q * sizeof(float));
+    if (P.table && P.Q && P.K) {
+        attention_lines(P);
+        n += round256((size_t)P.B * P.Hq * P.strips * P.line * sizeof(float)) + (size_t)P.Hq * P.n_buckets * MRF_TABLE_PARTS * sizeof(float);
+    }
+    return n ? n : 256;
 }
 
 }  // namespace mrf_host
@@ -456,8 +519,9 @@ int mrf_attention_backward(const mrf_attention *att, const void *grad_out, const
     P.lines = (float *)((char *)workspace + round256((size_t)P.B * P.Hq * P.Q * sizeof(float)));
     P.partial = (float *)((char *)P.lines + round256((size_t)P.B * P.Hq * P.strips * P.line * sizeof(float)));
     hipStream_t st = (hipStream_t)hip_stream;
-    if (att->type == MRF_F32) return attention_back_typed<float>(P, st);
+    if (att->type == MRF_F32) return attention_backward_f32(P, st);
     return att->type == MRF_F16 ? attention_back_typed<mrf_f16>(P, st) : attention_back_typed<mrf_bf16>(P, st);
 }
 
 }  // extern "C"
+#endif
