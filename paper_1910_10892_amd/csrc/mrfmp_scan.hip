@@ -1,16 +1,18 @@
 // Gated linear recurrence along the middle index of [outer][T][inner], forward and backward (see mrf_gated_scan_forward in the header for the
 // formulas).
 //
-// A lane has V neighbouring channels and goes through their steps one after the other, MRF_SCAN_STEPS of them loaded ahead.  Some 20 operations
-// and two transcendental ones an element: bound by memory.  Where there are few channels the steps are divided into chunks: what a chunk
-// does to the state it gets is h -> A h + B, which a first launch finds, a second one strings together, and the third goes through the
-// steps again from the right state.  The states before every MRF_SCAN_STEPS-th step are kept for the backward pass, in 32 bits: it forms the steps
-// between them again in registers, whatever the type of y.
+// A lane has V neighbouring channels, MRF_SCAN_STEPS of their steps in registers.  The wavefronts of a workgroup have the same channels and the steps behind one another's:
+// what a wavefront's steps do to the state they get is h -> A h + B; these meet in LDS, and each goes through its steps from the right state.  So every
+// element is read once, and few channels still make many wavefronts.  Some 20 operations and two transcendental ones an element: bound by memory.
+// Where there are too few channels for that, the steps are divided into chunks: a first launch finds what each does, a second one strings that
+// together, and the third goes through the steps again.  The states before every MRF_SCAN_STEPS-th step are kept for the backward pass, in 32 bits:
+// it forms the steps between them again in registers, whatever the type of y.
 #include "mrfmp_rows.h"
 
 #include <type_traits>
 
 #define MRF_SCAN_STEPS 16
+#define MRF_SCAN_WAVES 8      // of a workgroup, at most
 
 struct MrfScanParams {
     long long outer, T, inner, groups, lanes;      // groups of V channels in a row of `inner`; lanes = outer groups
@@ -47,7 +49,7 @@ template <class X, int V> struct MrfScanLane {
 
     __device__ inline MrfScanLane(const MrfScanParams &P)
     {
-        const long long lane = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+        const long long lane = (long long)blockIdx.x * 64 + (threadIdx.x & 63);
         there = lane < P.lanes;
         o = there ? lane / P.groups : 0;
         i = (int)(lane - o * P.groups) * V;
@@ -111,118 +113,234 @@ template <class X, bool REV> struct MrfScanRows {
     }
 };
 
-template <class X, int V, bool COMPLEMENT, bool REV, bool EFFECT>
-__global__ void __launch_bounds__(256) mrf_scan_fwd(const MrfScanParams P)
+// What the wavefronts of a workgroup do to a state, one behind the other
+template <int V> struct MrfScanParts {
+    float2 part[2][MRF_SCAN_WAVES][V][64];
+
+    // h: the state before all wavefronts' steps, and then that behind them; returned in `mine`: the state before this one's, which do A, B to it
+    __device__ inline void meet(int buf, int wv, int waves, const float (&A)[V], const float (&B)[V], float (&h)[V], float (&mine)[V])
+    {
+        const int lane = threadIdx.x & 63;
+        if (waves == 1) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) mine[j] = h[j], h[j] = fmaf(A[j], h[j], B[j]);
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) part[buf][wv][j][lane] = make_float2(A[j], B[j]);
+        __syncthreads();
+        for (int w = 0; w < waves; ++w)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                if (w == wv) mine[j] = h[j];
+                const float2 p = part[buf][w][j][lane];
+                h[j] = fmaf(p.x, h[j], p.y);
+            }
+    }
+
+    // h, all: what is done to a state so far (all h0 + h), and then by all wavefronts' steps too
+    __device__ inline void pass(int buf, int wv, int waves, const float (&A)[V], const float (&B)[V], float (&h)[V], float (&all)[V])
+    {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int j = 0; j < V; ++j) part[buf][wv][j][lane] = make_float2(A[j], B[j]);
+        __syncthreads();
+        for (int w = 0; w < waves; ++w)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float2 p = part[buf][w][j][lane];
+                h[j] = fmaf(p.x, h[j], p.y);
+                all[j] *= p.x;
+            }
+    }
+};
+
+template <class X, int V, bool COMPLEMENT, bool REV>
+__global__ void __launch_bounds__(64 * MRF_SCAN_WAVES) mrf_scan_fwd(const MrfScanParams P)
 {
     typedef MrfScanLane<X, V> Lane;
+    __shared__ MrfScanParts<V> parts;
     const Lane me(P);
-    if (!me.there) return;
+    const int wv = threadIdx.x >> 6, waves = blockDim.x >> 6, ahead = waves * MRF_SCAN_STEPS;
     const long long from = (long long)blockIdx.y * P.chunk, to = from + P.chunk < P.T ? from + P.chunk : P.T;
-    const long long last = me.n < to ? me.n : to;
-    float h[V], A[V];
+    const long long last = !me.there ? 0 : me.n < to ? me.n : to;
+    float h[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) h[j] = 0.0f, A[j] = 1.0f;
-    if constexpr (!EFFECT) {
+    for (int j = 0; j < V; ++j) h[j] = 0.0f;
+    if (me.there) {
         if (P.chunks > 1) Lane::state(P.carry + blockIdx.y * (P.outer * P.inner) + me.index, h);
         else if (P.start) Lane::state(P.start + me.index, h);
     }
     const MrfScanRows<X, REV> x(P.x, P.x_outer, P.x_step, me.o, me.n, me.i), z(P.z, P.z_outer, P.z_step, me.o, me.n, me.i);
     const long long dense = P.T * P.inner;
     X *const y = (X *)P.y + me.o * dense + me.i;
+    int buf = 0;
 
     const auto run = [&](const typename Lane::Raw &rx, const typename Lane::Raw &rz, const long long u) {
-        if constexpr (!EFFECT)
-            if (P.states) Lane::keep(P.states + (me.o * P.blocks + u / MRF_SCAN_STEPS) * P.inner + me.i, h);
+        float a[MRF_SCAN_STEPS][V], b[MRF_SCAN_STEPS][V], A[V], B[V], mine[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) A[j] = 1.0f, B[j] = 0.0f;
+#pragma unroll
+        for (int s = 0; s < MRF_SCAN_STEPS; ++s)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float rest;
+                mrf_gate(mrf_to_f32((X)rz.v[s][j]), a[s][j], rest);
+                const float v = mrf_to_f32((X)rx.v[s][j]);
+                b[s][j] = COMPLEMENT ? rest * v : v;
+                if (u + s >= last) a[s][j] = 1.0f, b[s][j] = 0.0f;
+                B[j] = fmaf(a[s][j], B[j], b[s][j]);
+                A[j] *= a[s][j];
+            }
+        parts.meet(buf, wv, waves, A, B, h, mine);
+        buf ^= 1;
+        if (!me.there) return;
+        if (P.states && u < to) Lane::keep(P.states + (me.o * P.blocks + u / MRF_SCAN_STEPS) * P.inner + me.i, mine);
 #pragma unroll
         for (int s = 0; s < MRF_SCAN_STEPS; ++s) {
+            if (u + s < last) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) mine[j] = fmaf(a[s][j], mine[j], b[s][j]);
+                Lane::give(y + (REV ? me.n - 1 - (u + s) : u + s) * P.inner, mine);
+            } else if (u + s < to) {
+                const float zero[V] = {};
+                Lane::give(y + (u + s) * P.inner, zero);
+            }
+        }
+        if (waves == 1) {      // (as the steps round it)
+#pragma unroll
+            for (int j = 0; j < V; ++j) h[j] = mine[j];
+        }
+    };
+    typename Lane::Raw xa, za, xb, zb;
+    const auto load = [&](long long u, typename Lane::Raw &rx, typename Lane::Raw &rz) {
+        me.load(x.row0, x.step, u, last, rx);
+        me.load(z.row0, z.step, u, last, rz);
+    };
+    // (`first` is the same in all threads)
+    if (from < to) load(from + wv * MRF_SCAN_STEPS, xa, za);
+    for (long long first = from; first < to; first += 2 * ahead) {
+        const long long u = first + wv * MRF_SCAN_STEPS;
+        const bool more = first + ahead < to;
+        if (more) load(u + ahead, xb, zb);
+        run(xa, za, u);
+        if (first + 2 * ahead < to) load(u + 2 * ahead, xa, za);
+        if (more) run(xb, zb, u + ahead);
+    }
+    if (blockIdx.y == (unsigned)P.chunks - 1 && P.end && wv == 0 && me.there) Lane::keep(P.end + me.index, h);
+}
+
+// What a chunk does to the state it gets: h -> A h + B
+template <class X, int V, bool COMPLEMENT, bool REV> __global__ void __launch_bounds__(64 * MRF_SCAN_WAVES) mrf_scan_fwd_effect(const MrfScanParams P)
+{
+    typedef MrfScanLane<X, V> Lane;
+    __shared__ MrfScanParts<V> parts;
+    const Lane me(P);
+    const int wv = threadIdx.x >> 6, waves = blockDim.x >> 6, ahead = waves * MRF_SCAN_STEPS;
+    const long long from = (long long)blockIdx.y * P.chunk, to = from + P.chunk < P.T ? from + P.chunk : P.T;
+    const long long last = !me.there ? 0 : me.n < to ? me.n : to;
+    float all[V], h[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) all[j] = 1.0f, h[j] = 0.0f;
+    const MrfScanRows<X, REV> x(P.x, P.x_outer, P.x_step, me.o, me.n, me.i), z(P.z, P.z_outer, P.z_step, me.o, me.n, me.i);
+    int buf = 0;
+    for (long long first = from; first < to; first += ahead, buf ^= 1) {
+        const long long u = first + wv * MRF_SCAN_STEPS;
+        typename Lane::Raw rx, rz;
+        float A[V], B[V];
+        me.load(z.row0, z.step, u, last, rz);
+        me.load(x.row0, x.step, u, last, rx);
+#pragma unroll
+        for (int j = 0; j < V; ++j) A[j] = 1.0f, B[j] = 0.0f;
+#pragma unroll
+        for (int s = 0; s < MRF_SCAN_STEPS; ++s)
             if (u + s < last) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
                     float a, rest;
                     mrf_gate(mrf_to_f32((X)rz.v[s][j]), a, rest);
                     const float v = mrf_to_f32((X)rx.v[s][j]);
-                    h[j] = fmaf(a, h[j], COMPLEMENT ? rest * v : v);
+                    B[j] = fmaf(a, B[j], COMPLEMENT ? rest * v : v);
                     A[j] *= a;
                 }
-                if constexpr (!EFFECT) Lane::give(y + (REV ? me.n - 1 - (u + s) : u + s) * P.inner, h);
-            } else if (!EFFECT && u + s < to) {
-                const float zero[V] = {};
-                Lane::give(y + (u + s) * P.inner, zero);
             }
-        }
-    };
-    typename Lane::Raw xa, za, xb, zb;
-    if (from < to) {
-        me.load(x.row0, x.step, from, last, xa);
-        me.load(z.row0, z.step, from, last, za);
+        parts.pass(buf, wv, waves, A, B, h, all);
     }
-    for (long long u = from; u < to; u += 2 * MRF_SCAN_STEPS) {
-        const bool more = u + MRF_SCAN_STEPS < to;
-        if (more) {
-            me.load(x.row0, x.step, u + MRF_SCAN_STEPS, last, xb);
-            me.load(z.row0, z.step, u + MRF_SCAN_STEPS, last, zb);
-        }
-        run(xa, za, u);
-        if (u + 2 * MRF_SCAN_STEPS < to) {
-            me.load(x.row0, x.step, u + 2 * MRF_SCAN_STEPS, last, xa);
-            me.load(z.row0, z.step, u + 2 * MRF_SCAN_STEPS, last, za);
-        }
-        if (more) run(xb, zb, u + MRF_SCAN_STEPS);
-    }
-    if constexpr (EFFECT) {
+    if (me.there && wv == 0) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) P.effect[blockIdx.y * (P.outer * P.inner) + me.index + j] = make_float2(A[j], h[j]);
-    } else if (blockIdx.y == (unsigned)P.chunks - 1 && P.end) {
-        Lane::keep(P.end + me.index, h);
+        for (int j = 0; j < V; ++j) P.effect[blockIdx.y * (P.outer * P.inner) + me.index + j] = make_float2(all[j], h[j]);
     }
 }
 
-// Backward: c is what reaches a step's state from the steps behind it; g = dy + c, and the step before gets a g.
+// Backward: c is what reaches a step's state from the steps behind it; g = dy + c, and the step before gets a g.  The wavefronts have the steps in front of one
+// another's: what a wavefront's steps do to c is c -> A c + B.
 template <class X, int V, bool COMPLEMENT, bool REV>
-__global__ void __launch_bounds__(256) mrf_scan_bwd(const MrfScanParams P)
+__global__ void __launch_bounds__(64 * MRF_SCAN_WAVES) mrf_scan_bwd(const MrfScanParams P)
 {
     typedef MrfScanLane<X, V> Lane;
+    __shared__ MrfScanParts<V> parts;
     const Lane me(P);
-    if (!me.there) return;
+    const int wv = threadIdx.x >> 6, waves = blockDim.x >> 6, ahead = waves * MRF_SCAN_STEPS;
     const long long from = (long long)blockIdx.y * P.chunk, to = from + P.chunk < P.T ? from + P.chunk : P.T;
-    const long long last = me.n < to ? me.n : to;
+    const long long last = !me.there ? 0 : me.n < to ? me.n : to;
     float c[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) c[j] = 0.0f;
-    if (P.chunks > 1) Lane::state(P.carry + blockIdx.y * (P.outer * P.inner) + me.index, c);
-    else if (P.start) Lane::state(P.start + me.index, c);
+    if (me.there) {
+        if (P.chunks > 1) Lane::state(P.carry + blockIdx.y * (P.outer * P.inner) + me.index, c);
+        else if (P.start) Lane::state(P.start + me.index, c);
+    }
     const MrfScanRows<X, REV> x(P.x, P.x_outer, P.x_step, me.o, me.n, me.i), z(P.z, P.z_outer, P.z_step, me.o, me.n, me.i);
     const long long dense = P.T * P.inner;
     const MrfScanRows<X, REV> dy(P.dy, dense, P.inner, me.o, me.n, me.i);
     X *const dx = (X *)P.dx + me.o * dense + me.i, *const dz = (X *)P.dz + me.o * dense + me.i;
+    int buf = 0;
 
-    for (long long u = to > from ? (to - 1) / MRF_SCAN_STEPS * MRF_SCAN_STEPS : from - 1; u >= from; u -= MRF_SCAN_STEPS) {
-        if (u < last) {
-            typename Lane::Raw rx, rz, ry;
-            float h[V], before[MRF_SCAN_STEPS][V], a[MRF_SCAN_STEPS][V], rest[MRF_SCAN_STEPS][V];
+    // (`top` is the same in all threads)
+    for (long long top = to > from ? (to - 1) / MRF_SCAN_STEPS * MRF_SCAN_STEPS : from - 1; top >= from; top -= ahead) {
+        const long long u = top - wv * MRF_SCAN_STEPS;      // (below `from` there is nothing for this wavefront)
+        const bool steps = u >= from && u < last;
+        typename Lane::Raw rx, rz, ry;
+        float h[V], before[MRF_SCAN_STEPS][V], a[MRF_SCAN_STEPS][V], rest[MRF_SCAN_STEPS][V], A[V], B[V], mine[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) A[j] = 1.0f, B[j] = 0.0f;
+        if (steps) {
             me.load(z.row0, z.step, u, last, rz);
-            me.load(x.row0, x.step, u, last, rx);
             me.load(dy.row0, dy.step, u, last, ry);
+            me.load(x.row0, x.step, u, last, rx);
             Lane::state(P.states + (me.o * P.blocks + u / MRF_SCAN_STEPS) * P.inner + me.i, h);
+#pragma unroll
+            for (int s = MRF_SCAN_STEPS - 1; s >= 0; --s)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    mrf_gate(mrf_to_f32((X)rz.v[s][j]), a[s][j], rest[s][j]);
+                    if (u + s < last) {
+                        B[j] = a[s][j] * (mrf_to_f32((X)ry.v[s][j]) + B[j]);
+                        A[j] *= a[s][j];
+                    }
+                }
 #pragma unroll
             for (int s = 0; s < MRF_SCAN_STEPS; ++s)
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    mrf_gate(mrf_to_f32((X)rz.v[s][j]), a[s][j], rest[s][j]);
                     const float v = mrf_to_f32((X)rx.v[s][j]);
                     before[s][j] = h[j];
                     h[j] = fmaf(a[s][j], h[j], COMPLEMENT ? rest[s][j] * v : v);
                 }
+        }
+        parts.meet(buf, wv, waves, A, B, c, mine);
+        buf ^= 1;
+        if (steps) {
 #pragma unroll
             for (int s = MRF_SCAN_STEPS - 1; s >= 0; --s) {
                 if (u + s < last) {
                     float gx[V], gz[V];
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
-                        const float g = mrf_to_f32((X)ry.v[s][j]) + c[j], ag = a[s][j] * g;
+                        const float g = mrf_to_f32((X)ry.v[s][j]) + mine[j], ag = a[s][j] * g;
                         gx[j] = COMPLEMENT ? rest[s][j] * g : g;
                         gz[j] = ag * rest[s][j] * (COMPLEMENT ? before[s][j] - mrf_to_f32((X)rx.v[s][j]) : before[s][j]);
-                        c[j] = ag;
+                        mine[j] = ag;
                     }
                     const long long t = REV ? me.n - 1 - (u + s) : u + s;
                     if (P.dx) Lane::give(dx + t * P.inner, gx);
@@ -230,49 +348,64 @@ __global__ void __launch_bounds__(256) mrf_scan_bwd(const MrfScanParams P)
                 }
             }
         }
-        const float zero[V] = {};
-        for (int s = 0; s < MRF_SCAN_STEPS; ++s)
-            if (u + s >= last && u + s < to) {
-                if (P.dx) Lane::give(dx + (u + s) * P.inner, zero);
-                if (P.dz) Lane::give(dz + (u + s) * P.inner, zero);
-            }
+        if (me.there && u >= from && u + MRF_SCAN_STEPS > last) {
+            const float zero[V] = {};
+            for (int s = 0; s < MRF_SCAN_STEPS; ++s)
+                if (u + s >= last && u + s < to) {
+                    if (P.dx) Lane::give(dx + (u + s) * P.inner, zero);
+                    if (P.dz) Lane::give(dz + (u + s) * P.inner, zero);
+                }
+        }
+        if (waves == 1 && steps) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) c[j] = mine[j];
+        }
     }
-    if (blockIdx.y == 0 && P.end) Lane::keep(P.end + me.index, c);
+    if (blockIdx.y == 0 && P.end && wv == 0 && me.there) Lane::keep(P.end + me.index, c);
 }
 
 // What a chunk does to the gradient that reaches it from behind: c -> A c + B
-template <class X, int V, bool REV>
-__global__ void __launch_bounds__(256) mrf_scan_bwd_effect(const MrfScanParams P)
+template <class X, int V, bool REV> __global__ void __launch_bounds__(64 * MRF_SCAN_WAVES) mrf_scan_bwd_effect(const MrfScanParams P)
 {
     typedef MrfScanLane<X, V> Lane;
+    __shared__ MrfScanParts<V> parts;
     const Lane me(P);
-    if (!me.there) return;
+    const int wv = threadIdx.x >> 6, waves = blockDim.x >> 6, ahead = waves * MRF_SCAN_STEPS;
     const long long from = (long long)blockIdx.y * P.chunk, to = from + P.chunk < P.T ? from + P.chunk : P.T;
-    const long long last = me.n < to ? me.n : to;
-    float A[V], c[V];
+    const long long last = !me.there ? 0 : me.n < to ? me.n : to;
+    float all[V], c[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) A[j] = 1.0f, c[j] = 0.0f;
+    for (int j = 0; j < V; ++j) all[j] = 1.0f, c[j] = 0.0f;
     const MrfScanRows<X, REV> z(P.z, P.z_outer, P.z_step, me.o, me.n, me.i);
     const MrfScanRows<X, REV> dy(P.dy, P.T * P.inner, P.inner, me.o, me.n, me.i);
-    for (long long u = to > from ? (to - 1) / MRF_SCAN_STEPS * MRF_SCAN_STEPS : from - 1; u >= from; u -= MRF_SCAN_STEPS) {
-        if (u >= last) continue;
+    int buf = 0;
+    for (long long top = to > from ? (to - 1) / MRF_SCAN_STEPS * MRF_SCAN_STEPS : from - 1; top >= from; top -= ahead, buf ^= 1) {
+        const long long u = top - wv * MRF_SCAN_STEPS;
         typename Lane::Raw rz, ry;
-        me.load(z.row0, z.step, u, last, rz);
-        me.load(dy.row0, dy.step, u, last, ry);
+        float A[V], B[V];
 #pragma unroll
-        for (int s = MRF_SCAN_STEPS - 1; s >= 0; --s)
-            if (u + s < last) {
+        for (int j = 0; j < V; ++j) A[j] = 1.0f, B[j] = 0.0f;
+        if (u >= from) {
+            me.load(z.row0, z.step, u, last, rz);
+            me.load(dy.row0, dy.step, u, last, ry);
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    float a, rest;
-                    mrf_gate(mrf_to_f32((X)rz.v[s][j]), a, rest);
-                    c[j] = a * (mrf_to_f32((X)ry.v[s][j]) + c[j]);
-                    A[j] *= a;
+            for (int s = MRF_SCAN_STEPS - 1; s >= 0; --s)
+                if (u + s < last) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        float a, rest;
+                        mrf_gate(mrf_to_f32((X)rz.v[s][j]), a, rest);
+                        B[j] = a * (mrf_to_f32((X)ry.v[s][j]) + B[j]);
+                        A[j] *= a;
+                    }
                 }
-            }
+        }
+        parts.pass(buf, wv, waves, A, B, c, all);
     }
+    if (me.there && wv == 0) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) P.effect[blockIdx.y * (P.outer * P.inner) + me.index + j] = make_float2(A[j], c[j]);
+        for (int j = 0; j < V; ++j) P.effect[blockIdx.y * (P.outer * P.inner) + me.index + j] = make_float2(all[j], c[j]);
+    }
 }
 
 // States that the chunks get, from what each does to them, in the order of the chunks (backward: from the last).  A workgroup has 16 channels, 64 threads
@@ -314,13 +447,13 @@ namespace mrf_host {
 
 struct ScanSplit { int chunks; long long chunk; };
 
-// Chunks of the steps: none where the channels alone keep the card busy.
+// Chunks of the steps: none where a workgroup's wavefronts make enough of the channels alone.
 static ScanSplit scan_split(long long outer, long long T, long long inner)
 {
     const long long N = outer * inner;
-    if (N >= 32768 || T <= 256 || N == 0) return {1, T};
-    long long P = (131072 + N - 1) / N;
-    if (P > (T + 63) / 64) P = (T + 63) / 64;
+    if (N >= 8192 || T <= 1024 || N == 0) return {1, T};
+    long long P = (262144 + N - 1) / N;
+    if (P > (T + 127) / 128) P = (T + 127) / 128;
     if (P > 16384) P = 16384;
     const long long chunk = ((T + P - 1) / P + MRF_SCAN_STEPS - 1) / MRF_SCAN_STEPS * MRF_SCAN_STEPS;
     return {(int)((T + chunk - 1) / chunk), chunk};
@@ -330,22 +463,32 @@ static bool scan_sizes_ok(long long outer, long long T, long long inner)
 {
     const long long most = 0x7fffffffLL;
     if (outer < 0 || T < 0 || inner < 0 || outer > most || T > most - 2 * MRF_SCAN_STEPS || inner > most) return false;
-    if (outer && inner > (1LL << 38) / outer) return false;      // (channels: a grid has 2^31 workgroups of 256 at most)
+    if (outer && inner > (1LL << 36) / outer) return false;      // (channels: a grid has 2^31 workgroups of 64 at most)
     return !(outer && inner && T) || T <= (1LL << 60) / (outer * inner);
+}
+
+// Wavefronts of a workgroup: as many as make 4,096 of them, as far as a chunk has steps for them.
+static unsigned scan_waves(const MrfScanParams &P)
+{
+    const long long groups = (P.lanes + 63) / 64 * P.chunks;
+    int waves = 1;
+    while (waves < MRF_SCAN_WAVES && groups * waves < 4096 && waves * MRF_SCAN_STEPS < P.chunk) waves *= 2;
+    return 64 * waves;
 }
 
 template <class X, int V, bool REV> static int scan_forward(MrfScanParams P, bool complement, hipStream_t st)
 {
     P.groups = P.inner / V;
     P.lanes = P.outer * P.groups;
-    const dim3 grid((unsigned)((P.lanes + 255) / 256), (unsigned)P.chunks);
+    const unsigned threads = scan_waves(P);
+    const dim3 grid((unsigned)((P.lanes + 63) / 64), (unsigned)P.chunks);
     if (P.chunks > 1) {
-        if (complement) mrf_scan_fwd<X, V, true, REV, true><<<grid, 256, 0, st>>>(P);
-        else mrf_scan_fwd<X, V, false, REV, true><<<grid, 256, 0, st>>>(P);
+        if (complement) mrf_scan_fwd_effect<X, V, true, REV><<<grid, threads, 0, st>>>(P);
+        else mrf_scan_fwd_effect<X, V, false, REV><<<grid, threads, 0, st>>>(P);
         mrf_scan_carry<false><<<(unsigned)((P.outer * P.inner + 15) / 16), 1024, 0, st>>>(P);
     }
-    if (complement) mrf_scan_fwd<X, V, true, REV, false><<<grid, 256, 0, st>>>(P);
-    else mrf_scan_fwd<X, V, false, REV, false><<<grid, 256, 0, st>>>(P);
+    if (complement) mrf_scan_fwd<X, V, true, REV><<<grid, threads, 0, st>>>(P);
+    else mrf_scan_fwd<X, V, false, REV><<<grid, threads, 0, st>>>(P);
     return launch_status("mrf_scan_fwd");
 }
 
@@ -353,17 +496,18 @@ template <class X, int V, bool REV> static int scan_backward(MrfScanParams P, bo
 {
     P.groups = P.inner / V;
     P.lanes = P.outer * P.groups;
-    const dim3 grid((unsigned)((P.lanes + 255) / 256), (unsigned)P.chunks);
+    const unsigned threads = scan_waves(P);
+    const dim3 grid((unsigned)((P.lanes + 63) / 64), (unsigned)P.chunks);
     if (P.chunks > 1) {
-        mrf_scan_bwd_effect<X, V, REV><<<grid, 256, 0, st>>>(P);
+        mrf_scan_bwd_effect<X, V, REV><<<grid, threads, 0, st>>>(P);
         mrf_scan_carry<true><<<(unsigned)((P.outer * P.inner + 15) / 16), 1024, 0, st>>>(P);
     }
-    if (complement) mrf_scan_bwd<X, V, true, REV><<<grid, 256, 0, st>>>(P);
-    else mrf_scan_bwd<X, V, false, REV><<<grid, 256, 0, st>>>(P);
+    if (complement) mrf_scan_bwd<X, V, true, REV><<<grid, threads, 0, st>>>(P);
+    else mrf_scan_bwd<X, V, false, REV><<<grid, threads, 0, st>>>(P);
     return launch_status("mrf_scan_bwd");
 }
 
-// two channels a lane where 16 bits and an even row allow it: a load of 4 bytes
+// two channels a lane where 16 bits and an even row allow it (a load of 4 bytes), unless that leaves too few workgroups
 template <bool FORWARD> static int scan_launch(const MrfScanParams &P, int type, bool complement, bool reverse, hipStream_t st)
 {
     const auto go = [&](auto x, auto v, auto rev) {
@@ -373,7 +517,7 @@ template <bool FORWARD> static int scan_launch(const MrfScanParams &P, int type,
     };
     const auto typed = [&](auto x) {
         if constexpr (sizeof(x) == 2)
-            if (P.inner % 2 == 0)
+            if (P.inner % 2 == 0 && (P.chunks > 1 || P.outer * P.inner >= 32768))
                 return reverse ? go(x, std::integral_constant<int, 2>{}, std::true_type{}) : go(x, std::integral_constant<int, 2>{}, std::false_type{});
         return reverse ? go(x, std::integral_constant<int, 1>{}, std::true_type{}) : go(x, std::integral_constant<int, 1>{}, std::false_type{});
     };
