@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional, Sequence
 
@@ -22,6 +23,8 @@ _lib = None
 # handle of a device's current stream without a stream object around it, where torch has it (a tenth of a microsecond instead of 2.7, as much as
 # a launch); looked up with the library
 _raw_stream = _current_device = None
+_device_now = None      # the current device without asking whether there is one: for calls that have a tensor on it
+_int32 = _float32 = None      # torch's types, with the library
 
 
 class MrfError(RuntimeError):
@@ -92,8 +95,11 @@ def load_library():
     # the other way round the process ends up with two runtimes and the library's own sees
     # no initialised device.
     import torch
-    global _raw_stream, _current_device
+    global _raw_stream, _current_device, _device_now, _int32, _float32
     _raw_stream, _current_device = getattr(torch._C, "_cuda_getCurrentRawStream", None), torch.cuda.current_device
+    _device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    _int32, _float32 = torch.int32, torch.float32
+    _codes.update({torch.float32: MRF_F32, torch.float16: MRF_F16, torch.bfloat16: MRF_BF16})
     lib = ctypes.CDLL(LIB_PATH)
     vp, sz, ci = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int
     P = ctypes.POINTER(_CProblem)
@@ -157,7 +163,7 @@ def load_library():
     lib.mrf_softmin_policy.argtypes = [i64, i32, vp, ci, vp, ci, vp, i64, vp, vp, vp, f32, f32, f32, f32, vp, vp, vp, vp, sz, vp]
     lib.mrf_softmin_policy_backward.restype = ci
     lib.mrf_softmin_policy_backward.argtypes = [i64, i32, vp, ci, vp, ci, vp, i64, vp, vp, vp, f32, f32, f32, vp, vp, vp, sz, vp]
-    A, R = ctypes.POINTER(_CAttention), ctypes.POINTER(_CHeadRotation)
+    A, R = ctypes.POINTER(_CAttention), ctypes.c_char_p      # (a rotation's description goes as its packed bytes)
     lib.mrf_attention_workspace_bytes.restype = sz
     lib.mrf_attention_workspace_bytes.argtypes = [A, ci]
     lib.mrf_attention_forward.restype = ci
@@ -612,79 +618,108 @@ def _policy_backward(given, cost, labels, advantage, old_logp, ref_logp, mask, g
         _ws_size(workspace), _stream_handle(stream)), "mrf_softmin_policy_backward")
 
 
-# ---- sequence operators: inputs may be parts of a projection (any strides, the last index dense)
+# ---- sequence operators: inputs may be parts of a projection (any strides, the last index dense).  A description is packed in one go and a tensor looked at once:
+# small calls cost what their checks do.
 
 _INT64_MIN, _INT64_MAX = -(1 << 63), (1 << 63) - 1
+_ATTENTION = struct.Struct("@7if3P9q3q5P2q2i")
+_ROTATION = struct.Struct("@6i2P6q2Pf2i2Piq")
+_TWO_STRIDES = ctypes.c_int64 * 2
+_codes = {}      # torch dtype -> code of an element type
 
 
-def _here(*tensors):
-    """All on the current device, whose stream the call goes to."""
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != _current_device()):
-            raise ValueError("tensors must be on the current GPU")
+def _code_of(dtype) -> int:
+    """Code of an element type (filled with the library, which imports torch)."""
+    code = _codes.get(dtype)
+    if code is None:
+        raise ValueError("tensors must be float32, float16 or bfloat16, got %s" % dtype)
+    return code
 
 
-def _strided(t, what):
-    """Address and strides of a tensor whose last index is dense."""
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+def _device_of(t):
+    """The current device, on which the first tensor of a call has to be, as all others (the call goes to its stream)."""
+    at = t.get_device()
+    if at < 0 or at != _device_now():
+        raise ValueError("tensors must be on the current GPU")
+    return at
+
+
+def _refused(t, what, shape, dtype, at):
+    if t.get_device() != at:
+        raise ValueError("%s must be on the current GPU" % what)
+    if t.dtype != dtype:
+        raise ValueError("%s must be %s, got %s" % (what, dtype, t.dtype))
+    if shape is not None and t.shape != shape:
+        raise ValueError("%s has shape %s, expected %s" % (what, tuple(t.shape), tuple(shape)))
+    raise ValueError("%s must be contiguous" % what)
+
+
+def _dense(t, what, shape, dtype, at):
+    """Address of a dense tensor of that shape and type (None: 0)."""
+    if t is None:
+        return 0
+    if t.get_device() != at or t.dtype != dtype or (shape is not None and t.shape != shape) or not t.is_contiguous():
+        _refused(t, what, shape, dtype, at)
+    return t.data_ptr()
+
+
+def _strides(t, what, shape, dtype, at):
+    """Strides of a tensor of that shape and type whose last index is dense."""
+    if t.get_device() != at or t.dtype != dtype or t.shape != shape:
+        _refused(t, what, shape, dtype, at)
+    strides = t.stride()
+    if strides[-1] != 1 and shape[-1] > 1:
         raise ValueError("the last index of %s must be dense" % what)
-    return t.data_ptr(), t.stride()[:-1]
+    return strides[:-1]
 
 
-def _sequences(t, what, B):
-    if t is not None:
-        _same_size(what, t, B)
-    return _ptr(t, "int32")
+def _stream_at(stream, at):
+    """Handle of a stream, or of the current one of the current device."""
+    return _raw_stream(at) if stream is None and _raw_stream is not None else _stream_handle(stream)
+
+
+def _scratch(workspace, at):
+    """Address and bytes of a workspace."""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != at or not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous and on the current GPU")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 class MrfAttention:
     """Mirror of the C struct mrf_attention: q [B,Q,Hq,D], k and v [B,K,Hk,D] of one type at any strides (last index dense), table
     [Hq,n_buckets] float32 (heads_last: [n_buckets,Hq]) or None, bucket_of [n] int32 for the offsets from map_offset on, query_offsets,
     q_lengths, k_lengths [B] int32 or None, first_offset and last_offset numbers or None (no bound).  Made once, it can be called again while
-    its tensors live."""
+    its tensors live (it holds them)."""
 
     def __init__(self, q, k, v, scale, *, first_offset=None, last_offset=None, query_offset=0, query_offsets=None, q_lengths=None, k_lengths=None,
                  table=None, bucket_of=None, map_offset=0, heads_last=False):
         load_library()
         if q.dim() != 4 or k.dim() != 4:
             raise ValueError("q and k must be [batch, token, head, entry]")
-        B, Q, Hq, D = (_size(n) for n in q.shape)
-        K, Hk = _size(k.shape[1]), _size(k.shape[2])
-        _same_size("k", k, B, K, Hk, D)
-        _same_size("v", v, B, K, Hk, D)
-        if k.dtype != q.dtype or v.dtype != q.dtype:
-            raise ValueError("k and v must be %s like q" % q.dtype)
-        _here(q, k, v, query_offsets, q_lengths, k_lengths, table, bucket_of)
-        c = _CAttention(B, Q, K, Hq, Hk, D, _type_of(q, "q"), float(scale))
-        for name, t in (("q", q), ("k", k), ("v", v)):
-            at, strides = _strided(t, name)
-            setattr(c, name, at)
-            setattr(c, name + "_stride", (ctypes.c_int64 * 3)(*strides))
-        c.first_offset = _INT64_MIN if first_offset is None else int(first_offset)
-        c.last_offset = _INT64_MAX if last_offset is None else int(last_offset)
-        c.query_offset = int(query_offset)
-        c.query_offsets, c.q_lengths, c.k_lengths = (_sequences(t, n, B) for t, n in (
-            (query_offsets, "query_offsets"), (q_lengths, "q_lengths"), (k_lengths, "k_lengths")))
+        at, dtype = _device_of(q), q.dtype
+        B, Q, Hq, D = q.shape
+        _, K, Hk, _ = k.shape
+        keys = (B, K, Hk, D)
+        strides = (*_strides(q, "q", q.shape, dtype, at), *_strides(k, "k", keys, dtype, at), *_strides(v, "v", keys, dtype, at))
+        n = offsets = 0
         if table is not None:
             if bucket_of is None:
                 raise ValueError("a table needs bucket_of")
-            n = _size(table.shape[0] if heads_last else table.shape[-1])
-            _same_size("table", table, *((n, Hq) if heads_last else (Hq, n)))
-            c.table, c.bucket_of = _ptr(table, "float32"), _ptr(bucket_of, "int32")
-            c.map_offset, c.n_offsets, c.n_buckets, c.heads_last = int(map_offset), int(bucket_of.numel()), n, int(bool(heads_last))
-        self.c, self.shape = c, (B, Q, K, Hq, Hk, D)
-        self.q, self.k, self.v, self.table = q, k, v, table
-        self._kept = (query_offsets, q_lengths, k_lengths, bucket_of)
-
-    def _like(self, what, t, *shape, dtype=None):
-        """Address of a dense tensor of that shape, of q's type or of float32."""
-        if t is None:
-            return None
-        _same_size(what, t, *shape)
-        if dtype is None and t.dtype != self.q.dtype:
-            raise ValueError("%s must be %s like q, got %s" % (what, self.q.dtype, t.dtype))
-        _here(t)
-        return _ptr(t, dtype)
+            n, offsets = table.shape[0] if heads_last else table.shape[-1], bucket_of.numel()
+        if max(B, Q, K, Hq, D, n) > 0x7fffffff:
+            raise ValueError("sizes are at most 2^31 - 1")
+        of_batch = (B,)
+        i32, f32 = _int32, _float32
+        self.c = _CAttention.from_buffer_copy(_ATTENTION.pack(
+            B, Q, K, Hq, Hk, D, _code_of(dtype), scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), *strides,
+            _INT64_MIN if first_offset is None else int(first_offset), _INT64_MAX if last_offset is None else int(last_offset), int(query_offset),
+            _dense(query_offsets, "query_offsets", of_batch, i32, at), _dense(q_lengths, "q_lengths", of_batch, i32, at),
+            _dense(k_lengths, "k_lengths", of_batch, i32, at), _dense(table, "table", (n, Hq) if heads_last else (Hq, n), f32, at),
+            0 if table is None else _dense(bucket_of, "bucket_of", None, i32, at), int(map_offset), offsets, n, 1 if heads_last else 0))
+        self.shape, self.at, self.dtype, self.table_shape = (B, Q, K, Hq, Hk, D), at, dtype, None if table is None else table.shape
+        self._kept = (q, k, v, query_offsets, q_lengths, k_lengths, table, bucket_of)
 
 
 def mrf_attention_workspace_bytes(att: MrfAttention, backward: bool) -> int:
@@ -694,65 +729,61 @@ def mrf_attention_workspace_bytes(att: MrfAttention, backward: bool) -> int:
 def mrf_attention_forward(att: MrfAttention, out, lse, workspace, stream=None):
     """out [B,Q,Hq,D] like q, lse [B,Hq,Q] float32 or None."""
     B, Q, K, Hq, Hk, D = att.shape
-    _checked(load_library().mrf_attention_forward(
-        ctypes.byref(att.c), att._like("out", out, B, Q, Hq, D), att._like("lse", lse, B, Hq, Q, dtype="float32"), _ptr(workspace, None),
-        _ws_size(workspace), _stream_handle(stream)), "mrf_attention_forward")
+    at = att.at
+    if at != _device_now():
+        raise ValueError("tensors must be on the current GPU")
+    _checked(_lib.mrf_attention_forward(
+        ctypes.byref(att.c), _dense(out, "out", (B, Q, Hq, D), att.dtype, at), _dense(lse, "lse", (B, Hq, Q), _float32, at), *_scratch(workspace, at),
+        _stream_at(stream, at)), "mrf_attention_forward")
 
 
 def mrf_attention_backward(att: MrfAttention, grad_out, out, lse, grad_q, grad_k, grad_v, grad_table, workspace, stream=None):
     """grad_out and out [B,Q,Hq,D], lse [B,Hq,Q] of the forward call; grad_q, grad_k, grad_v of the shapes of q, k, v (dense), grad_table like
     the table, each or None."""
     B, Q, K, Hq, Hk, D = att.shape
-    table = () if att.table is None else tuple(att.table.shape)
-    _checked(load_library().mrf_attention_backward(
-        ctypes.byref(att.c), att._like("grad_out", grad_out, B, Q, Hq, D), att._like("out", out, B, Q, Hq, D),
-        att._like("lse", lse, B, Hq, Q, dtype="float32"), att._like("grad_q", grad_q, B, Q, Hq, D), att._like("grad_k", grad_k, B, K, Hk, D),
-        att._like("grad_v", grad_v, B, K, Hk, D), att._like("grad_table", grad_table, *table, dtype="float32"), _ptr(workspace, None),
-        _ws_size(workspace), _stream_handle(stream)), "mrf_attention_backward")
+    at, dtype, queries, keys = att.at, att.dtype, (B, Q, Hq, D), (B, K, Hk, D)
+    if at != _device_now():
+        raise ValueError("tensors must be on the current GPU")
+    if grad_table is not None and att.table_shape is None:
+        raise ValueError("grad_table without a table")
+    _checked(_lib.mrf_attention_backward(
+        ctypes.byref(att.c), _dense(grad_out, "grad_out", queries, dtype, at), _dense(out, "out", queries, dtype, at),
+        _dense(lse, "lse", (B, Hq, Q), _float32, at), _dense(grad_q, "grad_q", queries, dtype, at), _dense(grad_k, "grad_k", keys, dtype, at),
+        _dense(grad_v, "grad_v", keys, dtype, at), _dense(grad_table, "grad_table", att.table_shape, _float32, at), *_scratch(workspace, at),
+        _stream_at(stream, at)), "mrf_attention_backward")
 
 
 def _head_rotation(q, k, gamma_q, gamma_k, eps, inv_freq, positions, position_offset, interleaved):
-    """The C struct of tensors that fit each other."""
+    """The C struct (its bytes) of tensors that fit each other, their shapes, type and device."""
     load_library()
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q and k must be [batch, token, head, entry]")
-    B, T, Hq, D = (_size(n) for n in q.shape)
-    Hk = _size(k.shape[2])
-    _same_size("k", k, B, T, Hk, D)
-    _same_size("gamma_q", gamma_q, D)
-    _same_size("gamma_k", gamma_k, D)
-    if k.dtype != q.dtype:
-        raise ValueError("k must be %s like q" % q.dtype)
-    _here(q, k, gamma_q, gamma_k, inv_freq, positions)
-    c = _CHeadRotation(B, T, Hq, Hk, D, _type_of(q, "q"))
-    for name, t in (("q", q), ("k", k)):
-        at, strides = _strided(t, name)
-        setattr(c, name, at)
-        setattr(c, name + "_stride", (ctypes.c_int64 * 3)(*strides))
-    c.gamma_q, c.gamma_k, c.eps = _ptr(gamma_q, "float32"), _ptr(gamma_k, "float32"), float(eps)
-    c.rotary, c.interleaved = 0 if inv_freq is None else 2 * _size(inv_freq.numel()), int(bool(interleaved))
-    c.n_axes, c.position_offset = 1, int(position_offset)
-    c.inv_freq, c.positions = _ptr(inv_freq, "float32"), _ptr(positions, "int32")
+    at, dtype, f32 = _device_of(q), q.dtype, _float32
+    queries = q.shape
+    B, T, Hq, D = queries
+    Hk = k.shape[2]
+    keys, entries, axes = (B, T, Hk, D), (D,), 1
     if positions is not None:
-        c.n_axes = _size(positions.shape[2]) if positions.dim() == 3 else 1
-        _same_size("positions", positions, *((B, T, c.n_axes) if positions.dim() == 3 else (B, T)))
-    return c, (B, T, Hq, Hk, D)
-
-
-def _like_heads(what, t, like, *shape):
-    _same_size(what, t, *shape)
-    if t is not None and t.dtype != like.dtype:
-        raise ValueError("%s must be %s like q, got %s" % (what, like.dtype, t.dtype))
-    _here(t)
-    return _ptr(t, None)
+        if positions.dim() == 3:
+            axes = positions.shape[2]
+        places = _dense(positions, "positions", (B, T, axes) if positions.dim() == 3 else (B, T), _int32, at)
+    else:
+        places = 0
+    if max(B, T, Hq, Hk, D) > 0x7fffffff or (inv_freq is not None and inv_freq.numel() > 0x3fffffff):
+        raise ValueError("sizes are at most 2^31 - 1")
+    packed = _ROTATION.pack(
+        B, T, Hq, Hk, D, _code_of(dtype), q.data_ptr(), k.data_ptr(), *_strides(q, "q", queries, dtype, at), *_strides(k, "k", keys, dtype, at),
+        _dense(gamma_q, "gamma_q", entries, f32, at), _dense(gamma_k, "gamma_k", entries, f32, at), eps, 0 if inv_freq is None else 2 * inv_freq.numel(),
+        1 if interleaved else 0, _dense(inv_freq, "inv_freq", None, f32, at), places, axes, int(position_offset))
+    return packed, queries, keys, dtype, at
 
 
 def mrf_head_rotation_forward(q, k, gamma_q, gamma_k, eps, inv_freq, out_q, out_k, positions=None, position_offset=0, interleaved=False, stream=None):
     """q [B,T,Hq,D] and k [B,T,Hk,D] of one type at any strides (last index dense), gamma_q, gamma_k [D] float32 or None, inv_freq [pairs that turn]
     float32 or None (none), out_q and out_k of their shapes, positions [B,T] or [B,T,axes] int32 or None (the token's place)."""
-    c, (B, T, Hq, Hk, D) = _head_rotation(q, k, gamma_q, gamma_k, eps, inv_freq, positions, position_offset, interleaved)
-    _checked(load_library().mrf_head_rotation_forward(ctypes.byref(c), _like_heads("out_q", out_q, q, B, T, Hq, D),
-                                                      _like_heads("out_k", out_k, q, B, T, Hk, D), _stream_handle(stream)), "mrf_head_rotation_forward")
+    packed, queries, keys, dtype, at = _head_rotation(q, k, gamma_q, gamma_k, eps, inv_freq, positions, position_offset, interleaved)
+    _checked(_lib.mrf_head_rotation_forward(packed, _dense(out_q, "out_q", queries, dtype, at), _dense(out_k, "out_k", keys, dtype, at), _stream_at(stream, at)),
+             "mrf_head_rotation_forward")
 
 
 def mrf_head_rotation_workspace_bytes(n_tokens: int, Hq: int, Hk: int, D: int) -> int:
@@ -763,13 +794,12 @@ def mrf_head_rotation_backward(grad_out_q, grad_out_k, q, k, gamma_q, gamma_k, e
                                positions=None, position_offset=0, interleaved=False, stream=None):
     """Arguments of the forward call; grad_out_q, grad_out_k, grad_q, grad_k dense, of the shapes of q and k, grad_gamma_q, grad_gamma_k [D] float32;
     gradients that are not asked for are None."""
-    c, (B, T, Hq, Hk, D) = _head_rotation(q, k, gamma_q, gamma_k, eps, inv_freq, positions, position_offset, interleaved)
-    _same_size("grad_gamma_q", grad_gamma_q, D)
-    _same_size("grad_gamma_k", grad_gamma_k, D)
-    _checked(load_library().mrf_head_rotation_backward(
-        ctypes.byref(c), _like_heads("grad_out_q", grad_out_q, q, B, T, Hq, D), _like_heads("grad_out_k", grad_out_k, q, B, T, Hk, D),
-        _like_heads("grad_q", grad_q, q, B, T, Hq, D), _like_heads("grad_k", grad_k, q, B, T, Hk, D), _ptr(grad_gamma_q, "float32"),
-        _ptr(grad_gamma_k, "float32"), _ptr(workspace, None), _ws_size(workspace), _stream_handle(stream)), "mrf_head_rotation_backward")
+    packed, queries, keys, dtype, at = _head_rotation(q, k, gamma_q, gamma_k, eps, inv_freq, positions, position_offset, interleaved)
+    entries = queries[3:]
+    _checked(_lib.mrf_head_rotation_backward(
+        packed, _dense(grad_out_q, "grad_out_q", queries, dtype, at), _dense(grad_out_k, "grad_out_k", keys, dtype, at),
+        _dense(grad_q, "grad_q", queries, dtype, at), _dense(grad_k, "grad_k", keys, dtype, at), _dense(grad_gamma_q, "grad_gamma_q", entries, _float32, at),
+        _dense(grad_gamma_k, "grad_gamma_k", entries, _float32, at), *_scratch(workspace, at), _stream_at(stream, at)), "mrf_head_rotation_backward")
 
 
 def mrf_gated_scan_states(T: int) -> int:
@@ -780,45 +810,43 @@ def mrf_gated_scan_workspace_bytes(n_outer: int, T: int, n_inner: int) -> int:
     return int(load_library().mrf_gated_scan_workspace_bytes(int(n_outer), int(T), int(n_inner)))
 
 
-def _scan_inputs(x, z, lengths, dense, states, ends):
-    """Sizes, type, and the places of x and z, of tensors that fit each other."""
-    load_library()
-    if x.dim() != 3:
-        raise ValueError("x must be [row, step, channel]")
-    outer, T, inner = (int(n) for n in x.shape)
-    _same_size("z", z, outer, T, inner)
-    if z.dtype != x.dtype:
-        raise ValueError("z must be %s like x" % x.dtype)
-    for name, t in dense:
-        _same_size(name, t, outer, T, inner)
-        if t is not None and t.dtype != x.dtype:
-            raise ValueError("%s must be %s like x, got %s" % (name, x.dtype, t.dtype))
-    for name, t in ends:
-        _same_size(name, t, outer, inner)
-    _same_size("states", states, outer, mrf_gated_scan_states(T), inner)
-    _here(x, z, lengths, states, *(t for _, t in dense), *(t for _, t in ends))
-    (xp, xs), (zp, zs) = _strided(x, "x"), _strided(z, "z")
-    return outer, T, inner, _type_of(x, "x"), xp, (ctypes.c_int64 * 2)(*xs), zp, (ctypes.c_int64 * 2)(*zs), _sequences(lengths, "lengths", outer)
+def _scan_input(t, what, shape, dtype, at):
+    """Address and strides (None: dense) of x or z."""
+    strides = _strides(t, what, shape, dtype, at)
+    return t.data_ptr(), None if t.is_contiguous() else _TWO_STRIDES(*strides)
 
 
 def mrf_gated_scan_forward(x, z, initial, lengths, y, final, states, workspace, complement=True, reverse=False, stream=None):
     """x and z [outer,T,inner] of one type at any strides (last index dense), y dense like them, initial and final [outer,inner] float32 or None (final may be
     initial), lengths [outer] int32 or None, states [outer,mrf_gated_scan_states(T),inner] float32 or None."""
-    outer, T, inner, code, xp, xs, zp, zs, lp = _scan_inputs(x, z, lengths, (("y", y),), states, (("initial", initial), ("final", final)))
-    _checked(load_library().mrf_gated_scan_forward(
-        outer, T, inner, code, xp, xs, zp, zs, int(bool(complement)), int(bool(reverse)), _ptr(initial, "float32"), lp, _ptr(y, None),
-        _ptr(final, "float32"), _ptr(states, "float32"), _ptr(workspace, None), _ws_size(workspace), _stream_handle(stream)), "mrf_gated_scan_forward")
+    load_library()
+    if x.dim() != 3:
+        raise ValueError("x must be [row, step, channel]")
+    at, dtype, shape, f32 = _device_of(x), x.dtype, x.shape, _float32
+    outer, T, inner = shape
+    ends = (outer, inner)
+    _checked(_lib.mrf_gated_scan_forward(
+        outer, T, inner, _code_of(dtype), *_scan_input(x, "x", shape, dtype, at), *_scan_input(z, "z", shape, dtype, at), 1 if complement else 0,
+        1 if reverse else 0, _dense(initial, "initial", ends, f32, at), _dense(lengths, "lengths", (outer,), _int32, at), _dense(y, "y", shape, dtype, at),
+        _dense(final, "final", ends, f32, at), 0 if states is None else _dense(states, "states", (outer, mrf_gated_scan_states(T), inner), f32, at),
+        *_scratch(workspace, at), _stream_at(stream, at)), "mrf_gated_scan_forward")
 
 
 def mrf_gated_scan_backward(grad_y, grad_final, x, z, lengths, states, grad_x, grad_z, grad_initial, workspace, complement=True, reverse=False, stream=None):
     """grad_y, grad_x, grad_z dense like x, grad_final and grad_initial [outer,inner] float32; states of the forward call; gradients that are not
     asked for are None, and grad_final may be."""
-    outer, T, inner, code, xp, xs, zp, zs, lp = _scan_inputs(x, z, lengths, (("grad_y", grad_y), ("grad_x", grad_x), ("grad_z", grad_z)), states,
-                                                             (("grad_final", grad_final), ("grad_initial", grad_initial)))
-    _checked(load_library().mrf_gated_scan_backward(
-        outer, T, inner, code, _ptr(grad_y, None), _ptr(grad_final, "float32"), xp, xs, zp, zs, int(bool(complement)), int(bool(reverse)), lp,
-        _ptr(states, "float32"), _ptr(grad_x, None), _ptr(grad_z, None), _ptr(grad_initial, "float32"), _ptr(workspace, None), _ws_size(workspace),
-        _stream_handle(stream)), "mrf_gated_scan_backward")
+    load_library()
+    if x.dim() != 3:
+        raise ValueError("x must be [row, step, channel]")
+    at, dtype, shape, f32 = _device_of(x), x.dtype, x.shape, _float32
+    outer, T, inner = shape
+    ends = (outer, inner)
+    _checked(_lib.mrf_gated_scan_backward(
+        outer, T, inner, _code_of(dtype), _dense(grad_y, "grad_y", shape, dtype, at), _dense(grad_final, "grad_final", ends, f32, at),
+        *_scan_input(x, "x", shape, dtype, at), *_scan_input(z, "z", shape, dtype, at), 1 if complement else 0, 1 if reverse else 0,
+        _dense(lengths, "lengths", (outer,), _int32, at), _dense(states, "states", (outer, mrf_gated_scan_states(T), inner), f32, at),
+        _dense(grad_x, "grad_x", shape, dtype, at), _dense(grad_z, "grad_z", shape, dtype, at), _dense(grad_initial, "grad_initial", ends, f32, at),
+        *_scratch(workspace, at), _stream_at(stream, at)), "mrf_gated_scan_backward")
 
 
 def mrf_workspace_fault(workspace, stream=None) -> int:

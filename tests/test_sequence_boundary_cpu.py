@@ -79,7 +79,7 @@ def test_head_rotation_refusals():
     lib = mrf.load_library()
 
     def forward(out_q=FAKE, out_k=FAKE, **given):
-        return lib.mrf_head_rotation_forward(ctypes.byref(_rotation(**given)), out_q, out_k, None)
+        return lib.mrf_head_rotation_forward(bytes(_rotation(**given)), out_q, out_k, None)
 
     assert lib.mrf_head_rotation_forward(None, FAKE, FAKE, None) == -1
     for bad in (dict(B=-1), dict(T=-1), dict(Hq=-1), dict(Hk=-1), dict(D=0), dict(D=513), dict(B=1 << 16, T=1 << 16), dict(Hq=65537)):
@@ -95,7 +95,7 @@ def test_head_rotation_refusals():
     assert need > 0 and mrf.mrf_head_rotation_workspace_bytes(-1, 4, 2, 16) == 0 and mrf.mrf_head_rotation_workspace_bytes(6, 4, 2, 513) == 0
 
     def backward(gq=FAKE, gk=FAKE, gg=FAKE, ws=FAKE, size=need, **given):
-        return lib.mrf_head_rotation_backward(ctypes.byref(_rotation(**given)), gq, gk, FAKE, FAKE, gg, None, ws, size, None)
+        return lib.mrf_head_rotation_backward(bytes(_rotation(**given)), gq, gk, FAKE, FAKE, gg, None, ws, size, None)
 
     assert backward(gq=None) == -1 and backward(gk=None) == -1 and backward(ws=None) == -1 and backward(size=need - 1) == -6
     assert backward(D=0) == -2 and backward(type=-1) == -12
@@ -115,14 +115,14 @@ def test_gated_scan_refusals():
     assert forward(t=3) == -12 and forward(xs=(-1, 4)) == -12 and forward(zs=(12, -4)) == -12
     assert forward(x=None) == -1 and forward(z=None) == -1 and forward(y=None) == -1
     assert forward(outer=0, x=None, z=None, y=None) == 0 and forward(inner=0, x=None, z=None, y=None) == 0
-    need = mrf.mrf_gated_scan_workspace_bytes(2, 1000, 4)
+    need = mrf.mrf_gated_scan_workspace_bytes(2, 5000, 4)
     assert need > 0 and mrf.mrf_gated_scan_workspace_bytes(2, 3, 4) == 0
-    assert forward(T=1000, ws=None) == -1 and forward(T=1000, size=need - 1) == -6
+    assert forward(T=5000, ws=None) == -1 and forward(T=5000, size=need - 1) == -6
     assert mrf.mrf_gated_scan_states(0) == 0 and mrf.mrf_gated_scan_states(1) == 1 and mrf.mrf_gated_scan_states(-5) == 0
     assert 16 * mrf.mrf_gated_scan_states(1000) >= 1000
 
     def backward(gy=FAKE, states=FAKE, x=FAKE, ws=FAKE, size=need):
-        return lib.mrf_gated_scan_backward(2, 1000, 4, 0, gy, None, x, None, FAKE, None, 1, 0, None, states, FAKE, FAKE, None, ws, size, None)
+        return lib.mrf_gated_scan_backward(2, 5000, 4, 0, gy, None, x, None, FAKE, None, 1, 0, None, states, FAKE, FAKE, None, ws, size, None)
 
     assert backward(gy=None) == -1 and backward(states=None) == -1 and backward(x=None) == -1 and backward(ws=None) == -1 and backward(size=need - 1) == -6
 
