@@ -1,21 +1,21 @@
 // Norm of queries and keys for each head, and their rotation by position, in one pass, forward and backward (see mrf_head_rotation_forward in the
 // header for the formulas).
 //
-// A head of D entries is D / 2 slots of two entries: those that turn together, and behind them neighbours.  TL lanes share a token, MRF_SLOTS
-// slots each, and go through some of its heads: the angles are formed once for all of them.  Some 30 operations an entry: bound by memory.
+// A head of D entries is D / 2 slots of two entries: those that turn together, and behind them neighbours.  TL lanes share a token, S
+// slots each, and go through some of its heads of queries, or of keys: the angles are formed once for all of them.  Some 30 operations an entry: bound by memory.
 // Angles: position times frequency is formed and reduced to an eighth of a turn in 64 bits (a position of 10^6 leaves 32 bits no digit of the
 // angle behind the point), sine and cosine of the rest by their series.
 #include "mrfmp_rows.h"
 
 #include <type_traits>
 
-#define MRF_SLOTS 4
-#define MRF_ROTATE_PARTS 1024      // workgroups that sum the parameters' gradients, at most
+#define MRF_ROTATE_PARTS 512      // workgroups that sum a parameter's gradient, at most
 
 struct MrfRotateParams {
     long long tokens, T;
     int Hq, Hk, D, half, n_axes, interleaved;      // half: pairs that turn
-    int heads, pieces;                             // heads that a group of lanes goes through; groups of a token
+    int heads, pieces[2];                          // heads that a group of lanes goes through; groups of a token, for its queries and its keys
+    int blocks[2];                                 // workgroups, of queries first
     const void *in[2], *dout[2];                   // queries, keys
     long long at_batch[2], at_token[2], at_head[2];
     const float *gamma[2], *inv_freq;
@@ -23,8 +23,7 @@ struct MrfRotateParams {
     long long position_offset;
     float eps;
     void *out[2];                                  // (gradients of the inputs in the backward pass)
-    float *dgamma[2], *partial;                    // [parts][2][D]
-    int parts;
+    float *dgamma[2], *partial;                    // [2][MRF_ROTATE_PARTS][D]
 };
 
 // sine and cosine of `turns` times 2 pi
@@ -41,14 +40,14 @@ __device__ inline void mrf_turn(double turns, float &c, float &s)
 }
 
 // The slots of a lane: entries e0(j), e1(j) of slot j.  WHOLE: its slots are of one kind and all there, so that its entries are two runs of
-// MRF_SLOTS neighbours.
-template <class X, bool WHOLE> struct MrfSlots {
-    typedef typename MrfVec<X, MRF_SLOTS>::type vec;
+// S neighbours.
+template <class X, int S, bool WHOLE> struct MrfSlots {
+    typedef typename MrfVec<X, S>::type vec;
     struct Raw { vec v[2]; };
     int first, half, D;
     bool split, any;
 
-    __device__ inline MrfSlots(const MrfRotateParams &P, int l) : first(l * MRF_SLOTS), half(P.half), D(P.D)
+    __device__ inline MrfSlots(const MrfRotateParams &P, int l) : first(l * S), half(P.half), D(P.D)
     {
         split = !P.interleaved && first < half;
         any = 2 * first < D;
@@ -61,56 +60,56 @@ template <class X, bool WHOLE> struct MrfSlots {
     __device__ inline void load(const X *at, bool there, Raw &r) const
     {
 #pragma unroll
-        for (int j = 0; j < MRF_SLOTS; ++j) r.v[0][j] = r.v[1][j] = (X)0.0f;
+        for (int j = 0; j < S; ++j) r.v[0][j] = r.v[1][j] = (X)0.0f;
         if (!there || !any) return;
         if constexpr (WHOLE) {
             r.v[0] = *(const vec *)(at + (split ? first : 2 * first));
-            r.v[1] = *(const vec *)(at + (split ? first + half : 2 * first + MRF_SLOTS));
+            r.v[1] = *(const vec *)(at + (split ? first + half : 2 * first + S));
         } else {
 #pragma unroll
-            for (int j = 0; j < MRF_SLOTS; ++j) {
+            for (int j = 0; j < S; ++j) {
                 if (e0(j) < D) r.v[0][j] = at[e0(j)];
                 if (e1(j) < D) r.v[1][j] = at[e1(j)];
             }
         }
     }
     // a[j], b[j]: the two entries of slot j
-    __device__ inline void convert(const Raw &r, float (&a)[MRF_SLOTS], float (&b)[MRF_SLOTS]) const
+    __device__ inline void convert(const Raw &r, float (&a)[S], float (&b)[S]) const
     {
-        float u[2 * MRF_SLOTS];
+        float u[2 * S];
 #pragma unroll
-        for (int j = 0; j < MRF_SLOTS; ++j) u[j] = mrf_to_f32((X)r.v[0][j]), u[MRF_SLOTS + j] = mrf_to_f32((X)r.v[1][j]);
+        for (int j = 0; j < S; ++j) u[j] = mrf_to_f32((X)r.v[0][j]), u[S + j] = mrf_to_f32((X)r.v[1][j]);
 #pragma unroll
-        for (int j = 0; j < MRF_SLOTS; ++j) {
+        for (int j = 0; j < S; ++j) {
             a[j] = !WHOLE || split ? u[j] : u[2 * j];
-            b[j] = !WHOLE || split ? u[MRF_SLOTS + j] : u[2 * j + 1];
+            b[j] = !WHOLE || split ? u[S + j] : u[2 * j + 1];
         }
     }
-    __device__ inline void store(X *at, bool there, const float (&a)[MRF_SLOTS], const float (&b)[MRF_SLOTS]) const
+    __device__ inline void store(X *at, bool there, const float (&a)[S], const float (&b)[S]) const
     {
         if (!there || !any) return;
         if constexpr (WHOLE) {
             vec x, y;
 #pragma unroll
-            for (int j = 0; j < MRF_SLOTS; ++j) {
-                const float low = j % 2 ? b[j / 2] : a[j / 2], high = j % 2 ? b[(MRF_SLOTS + j) / 2] : a[(MRF_SLOTS + j) / 2];
+            for (int j = 0; j < S; ++j) {
+                const float low = j % 2 ? b[j / 2] : a[j / 2], high = j % 2 ? b[(S + j) / 2] : a[(S + j) / 2];
                 x[j] = mrf_from_f32<X>(split ? a[j] : low);
                 y[j] = mrf_from_f32<X>(split ? b[j] : high);
             }
             *(vec *)(at + (split ? first : 2 * first)) = x;
-            *(vec *)(at + (split ? first + half : 2 * first + MRF_SLOTS)) = y;
+            *(vec *)(at + (split ? first + half : 2 * first + S)) = y;
         } else {
 #pragma unroll
-            for (int j = 0; j < MRF_SLOTS; ++j) {
+            for (int j = 0; j < S; ++j) {
                 if (e0(j) < D) at[e0(j)] = mrf_from_f32<X>(a[j]);
                 if (e1(j) < D) at[e1(j)] = mrf_from_f32<X>(b[j]);
             }
         }
     }
-    __device__ inline void parameters(const float *at, float (&a)[MRF_SLOTS], float (&b)[MRF_SLOTS], float fill) const
+    __device__ inline void parameters(const float *at, float (&a)[S], float (&b)[S], float fill) const
     {
 #pragma unroll
-        for (int j = 0; j < MRF_SLOTS; ++j) {
+        for (int j = 0; j < S; ++j) {
             a[j] = at && e0(j) < D ? at[e0(j)] : fill;
             b[j] = at && e1(j) < D ? at[e1(j)] : fill;
         }
@@ -118,102 +117,110 @@ template <class X, bool WHOLE> struct MrfSlots {
 };
 
 // cos and sin of a token's angles (1, 0 in slots that do not turn)
-template <class S> __device__ inline void mrf_angles(const MrfRotateParams &P, const S &slots, long long token, float (&c)[MRF_SLOTS], float (&s)[MRF_SLOTS])
+template <int S, class Slots> __device__ inline void mrf_angles(const MrfRotateParams &P, const Slots &slots, long long token, long long t, float (&c)[S], float (&s)[S])
 {
 #pragma unroll
-    for (int j = 0; j < MRF_SLOTS; ++j) {
+    for (int j = 0; j < S; ++j) {
         const int slot = slots.first + j;
         c[j] = 1.0f;
         s[j] = 0.0f;
         if (slot < P.half) {
-            const long long at = P.positions ? P.positions[token * P.n_axes + slot / (P.half / P.n_axes)] : token % P.T;
+            const long long at = P.positions ? P.positions[token * P.n_axes + (P.n_axes == 1 ? 0 : slot / (P.half / P.n_axes))] : t;
             mrf_turn((double)(at + P.position_offset) * ((double)P.inv_freq[slot] * 0.15915494309189533577), c[j], s[j]);
         }
     }
 }
 
-constexpr int MRF_ROTATE_AHEAD = 4;      // heads whose loads are on their way together
+// heads whose loads are on their way together
+constexpr int MRF_ROTATE_AHEAD = 2, MRF_ROTATE_AHEAD_BACK = 1;
 
-template <class X, int TL, bool WHOLE> __global__ void __launch_bounds__(256) mrf_rotate_fwd(const MrfRotateParams P)
+// Where a group of lanes is: its kind (0: queries, 1: keys), its first piece, and the way to its next one
+template <int TL> struct MrfRotatePlace {
+    int kind, heads;
+    long long g, all, step;
+    __device__ inline MrfRotatePlace(const MrfRotateParams &P)
+    {
+        kind = blockIdx.x >= (unsigned)P.blocks[0];
+        heads = kind ? P.Hk : P.Hq;
+        all = P.tokens * P.pieces[kind];
+        g = (long long)(blockIdx.x - (kind ? P.blocks[0] : 0)) * (256 / TL) + threadIdx.x / TL;
+        step = (long long)P.blocks[kind] * (256 / TL);
+    }
+};
+
+template <class X, int S, int TL, bool WHOLE> __global__ void __launch_bounds__(256) mrf_rotate_fwd(const MrfRotateParams P)
 {
-    typedef MrfSlots<X, WHOLE> Slots;
-    const int l = threadIdx.x % TL, heads = P.Hq + P.Hk;
-    const Slots slots(P, l);
+    typedef MrfSlots<X, S, WHOLE> Slots;
+    const MrfRotatePlace<TL> place(P);
+    const int kind = place.kind;
+    const Slots slots(P, threadIdx.x % TL);
     const float inv = 1.0f / (float)P.D;
-    const long long all = P.tokens * P.pieces;
-    for (long long g = (long long)blockIdx.x * (256 / TL) + threadIdx.x / TL; g < all; g += (long long)gridDim.x * (256 / TL)) {
-        const long long token = g / P.pieces, batch = token / P.T, t = token - batch * P.T;
-        const int h0 = (int)(g - token * P.pieces) * P.heads, h1 = h0 + P.heads < heads ? h0 + P.heads : heads;
-        const auto from = [&](int h) {
-            const int k = h >= P.Hq;
-            return (const X *)P.in[k] + batch * P.at_batch[k] + t * P.at_token[k] + (h - (k ? P.Hq : 0)) * P.at_head[k];
-        };
+    float ga[S], gb[S];
+    slots.parameters(P.gamma[kind], ga, gb, 1.0f);
+    for (long long g = place.g; g < place.all; g += place.step) {
+        const long long token = g / P.pieces[kind], batch = token / P.T, t = token - batch * P.T;
+        const int h0 = (int)(g - token * P.pieces[kind]) * P.heads, h1 = h0 + P.heads < place.heads ? h0 + P.heads : place.heads;
+        const X *const from = (const X *)P.in[kind] + batch * P.at_batch[kind] + t * P.at_token[kind];
+        X *const to = (X *)P.out[kind] + token * place.heads * (long long)P.D;
         typename Slots::Raw r[MRF_ROTATE_AHEAD];
-        float c[MRF_SLOTS], s[MRF_SLOTS];
+        float c[S], s[S];
         for (int h = h0; h < h1; h += MRF_ROTATE_AHEAD) {
 #pragma unroll
-            for (int i = 0; i < MRF_ROTATE_AHEAD; ++i) slots.load(h + i < h1 ? from(h + i) : nullptr, h + i < h1, r[i]);
-            if (h == h0) mrf_angles(P, slots, token, c, s);
+            for (int i = 0; i < MRF_ROTATE_AHEAD; ++i) slots.load(from + (h + i) * P.at_head[kind], h + i < h1, r[i]);
+            if (h == h0) mrf_angles<S>(P, slots, token, t, c, s);
 #pragma unroll
             for (int i = 0; i < MRF_ROTATE_AHEAD; ++i) {
                 if (h + i >= h1) break;
-                const int k = h + i >= P.Hq;
-                float a[MRF_SLOTS], b[MRF_SLOTS], ga[MRF_SLOTS], gb[MRF_SLOTS], sum = 0.0f;
+                float a[S], b[S], sum = 0.0f;
                 slots.convert(r[i], a, b);
-                slots.parameters(P.gamma[k], ga, gb, 1.0f);
 #pragma unroll
-                for (int j = 0; j < MRF_SLOTS; ++j) sum = fmaf(a[j], a[j], fmaf(b[j], b[j], sum));
+                for (int j = 0; j < S; ++j) sum = fmaf(a[j], a[j], fmaf(b[j], b[j], sum));
                 const float rs = rsqrtf(fmaf(mrf_lanes_sum<TL>(sum), inv, P.eps));
 #pragma unroll
-                for (int j = 0; j < MRF_SLOTS; ++j) {
+                for (int j = 0; j < S; ++j) {
                     const float x = a[j] * rs * ga[j], y = b[j] * rs * gb[j];
                     a[j] = fmaf(x, c[j], -(y * s[j]));
                     b[j] = fmaf(x, s[j], y * c[j]);
                 }
-                slots.store((X *)P.out[k] + (token * (k ? P.Hk : P.Hq) + h + i - (k ? P.Hq : 0)) * (long long)P.D, true, a, b);
+                slots.store(to + (h + i) * (long long)P.D, true, a, b);
             }
         }
     }
 }
 
 // Backward: u = dy turned back, a = u gamma, dx = r (a - h mean(a h)) with h = x r.  The sums of u h stay in registers over all tokens of a group.
-template <class X, int TL, bool WHOLE> __global__ void __launch_bounds__(256) mrf_rotate_bwd(const MrfRotateParams P)
+template <class X, int S, int TL, bool WHOLE> __global__ void __launch_bounds__(256) mrf_rotate_bwd(const MrfRotateParams P)
 {
-    typedef MrfSlots<X, WHOLE> Slots;
-    __shared__ float lds[4][2][2 * MRF_SLOTS * TL];
-    const int l = threadIdx.x % TL, heads = P.Hq + P.Hk;
+    typedef MrfSlots<X, S, WHOLE> Slots;
+    __shared__ float lds[4][2 * S * TL];
+    const MrfRotatePlace<TL> place(P);
+    const int kind = place.kind, l = threadIdx.x % TL;
     const Slots slots(P, l);
     const float inv = 1.0f / (float)P.D;
-    float sa[2][MRF_SLOTS] = {}, sb[2][MRF_SLOTS] = {};
-    const long long all = P.tokens * P.pieces;
-    for (long long g = (long long)blockIdx.x * (256 / TL) + threadIdx.x / TL; g < all; g += (long long)gridDim.x * (256 / TL)) {
-        const long long token = g / P.pieces, batch = token / P.T, t = token - batch * P.T;
-        const int h0 = (int)(g - token * P.pieces) * P.heads, h1 = h0 + P.heads < heads ? h0 + P.heads : heads;
-        const auto dense = [&](int h) { return (token * (h >= P.Hq ? P.Hk : P.Hq) + h - (h >= P.Hq ? P.Hq : 0)) * (long long)P.D; };
-        const auto from = [&](int h) {
-            const int k = h >= P.Hq;
-            return (const X *)P.in[k] + batch * P.at_batch[k] + t * P.at_token[k] + (h - (k ? P.Hq : 0)) * P.at_head[k];
-        };
-        typename Slots::Raw r[MRF_ROTATE_AHEAD], d[MRF_ROTATE_AHEAD];
-        float c[MRF_SLOTS], s[MRF_SLOTS];
-        for (int h = h0; h < h1; h += MRF_ROTATE_AHEAD) {
+    float ga[S], gb[S], sa[S] = {}, sb[S] = {};
+    slots.parameters(P.gamma[kind], ga, gb, 1.0f);
+    for (long long g = place.g; g < place.all; g += place.step) {
+        const long long token = g / P.pieces[kind], batch = token / P.T, t = token - batch * P.T;
+        const int h0 = (int)(g - token * P.pieces[kind]) * P.heads, h1 = h0 + P.heads < place.heads ? h0 + P.heads : place.heads;
+        const X *const from = (const X *)P.in[kind] + batch * P.at_batch[kind] + t * P.at_token[kind];
+        const long long dense = token * place.heads * (long long)P.D;
+        typename Slots::Raw r[MRF_ROTATE_AHEAD_BACK], d[MRF_ROTATE_AHEAD_BACK];
+        float c[S], s[S];
+        for (int h = h0; h < h1; h += MRF_ROTATE_AHEAD_BACK) {
 #pragma unroll
-            for (int i = 0; i < MRF_ROTATE_AHEAD; ++i) {
-                const bool there = h + i < h1;
-                slots.load(there ? from(h + i) : nullptr, there, r[i]);
-                slots.load(there ? (const X *)P.dout[h + i >= P.Hq] + dense(h + i) : nullptr, there, d[i]);
+            for (int i = 0; i < MRF_ROTATE_AHEAD_BACK; ++i) {
+                slots.load(from + (h + i) * P.at_head[kind], h + i < h1, r[i]);
+                slots.load((const X *)P.dout[kind] + dense + (h + i) * (long long)P.D, h + i < h1, d[i]);
             }
-            if (h == h0) mrf_angles(P, slots, token, c, s);
+            if (h == h0) mrf_angles<S>(P, slots, token, t, c, s);
 #pragma unroll
-            for (int i = 0; i < MRF_ROTATE_AHEAD; ++i) {
+            for (int i = 0; i < MRF_ROTATE_AHEAD_BACK; ++i) {
                 if (h + i >= h1) break;
-                const int k = h + i >= P.Hq;
-                float a[MRF_SLOTS], b[MRF_SLOTS], ga[MRF_SLOTS], gb[MRF_SLOTS], da[MRF_SLOTS], db[MRF_SLOTS], sum = 0.0f, along = 0.0f;
+                float a[S], b[S], da[S], db[S], sum = 0.0f, along = 0.0f;
                 slots.convert(r[i], a, b);
                 slots.convert(d[i], da, db);
-                slots.parameters(P.gamma[k], ga, gb, 1.0f);
 #pragma unroll
-                for (int j = 0; j < MRF_SLOTS; ++j) {
+                for (int j = 0; j < S; ++j) {
                     const float u = fmaf(da[j], c[j], db[j] * s[j]), v = fmaf(db[j], c[j], -(da[j] * s[j]));
                     sum = fmaf(a[j], a[j], fmaf(b[j], b[j], sum));
                     da[j] = u;
@@ -222,118 +229,114 @@ template <class X, int TL, bool WHOLE> __global__ void __launch_bounds__(256) mr
                 }
                 const float rs = rsqrtf(fmaf(mrf_lanes_sum<TL>(sum), inv, P.eps)), m = mrf_lanes_sum<TL>(along) * inv * rs * rs;
 #pragma unroll
-                for (int j = 0; j < MRF_SLOTS; ++j) {
+                for (int j = 0; j < S; ++j) {
                     const float u = da[j], v = db[j];
                     da[j] = rs * fmaf(-m, a[j], u * ga[j]);
                     db[j] = rs * fmaf(-m, b[j], v * gb[j]);
-                    const float wa = u * (a[j] * rs), wb = v * (b[j] * rs);
-                    sa[0][j] += k ? 0.0f : wa;
-                    sb[0][j] += k ? 0.0f : wb;
-                    sa[1][j] += k ? wa : 0.0f;
-                    sb[1][j] += k ? wb : 0.0f;
+                    sa[j] = fmaf(u, a[j] * rs, sa[j]);
+                    sb[j] = fmaf(v, b[j] * rs, sb[j]);
                 }
-                if (P.out[k]) slots.store((X *)P.out[k] + dense(h + i), true, da, db);
+                if (P.out[kind]) slots.store((X *)P.out[kind] + dense + (h + i) * (long long)P.D, true, da, db);
             }
         }
     }
-    if (!P.partial) return;
+    if (!P.dgamma[kind]) return;
     // lanes of a wavefront with the same slots, then its wavefronts
     const int wv = threadIdx.x >> 6;
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int j = 0; j < MRF_SLOTS; ++j) {
-            float x = sa[k][j], y = sb[k][j];
-            for (int w = TL; w < 64; w *= 2) {
-                x += __shfl_xor(x, w);
-                y += __shfl_xor(y, w);
-            }
-            if ((threadIdx.x & 63) < TL) {
-                lds[wv][k][(2 * j) * TL + l] = x;
-                lds[wv][k][(2 * j + 1) * TL + l] = y;
-            }
+    for (int j = 0; j < S; ++j) {
+        float x = sa[j], y = sb[j];
+        for (int w = TL; w < 64; w *= 2) {
+            x += __shfl_xor(x, w);
+            y += __shfl_xor(y, w);
         }
+        if ((threadIdx.x & 63) < TL) {
+            lds[wv][(2 * j) * TL + l] = x;
+            lds[wv][(2 * j + 1) * TL + l] = y;
+        }
+    }
     __syncthreads();
     if (threadIdx.x >= TL || !slots.any) return;
+    const bool one = P.blocks[kind] == 1;      // (a single workgroup's sums are all there is)
+    float *const to = one ? P.dgamma[kind] : P.partial + ((size_t)kind * MRF_ROTATE_PARTS + blockIdx.x - (kind ? P.blocks[0] : 0)) * P.D;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        float *const to = P.partial + ((size_t)blockIdx.x * 2 + k) * P.D;
+    for (int j = 0; j < S; ++j)
 #pragma unroll
-        for (int j = 0; j < MRF_SLOTS; ++j)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int n = (2 * j + e) * TL + l, column = e ? slots.e1(j) : slots.e0(j);
-                if (column < P.D) to[column] = (lds[0][k][n] + lds[1][k][n]) + (lds[2][k][n] + lds[3][k][n]);
-            }
-    }
+        for (int e = 0; e < 2; ++e) {
+            const int n = (2 * j + e) * TL + l, column = e ? slots.e1(j) : slots.e0(j);
+            if (column < P.D) to[column] = (lds[0][n] + lds[1][n]) + (lds[2][n] + lds[3][n]);
+        }
 }
 
 __global__ void __launch_bounds__(1024) mrf_rotate_sum(const MrfRotateParams P)
 {
     __shared__ float part[64][17];
-    const int w = threadIdx.x % 16, s = threadIdx.x / 16, column = blockIdx.x * 16 + w;      // of 2 D
+    const int kind = blockIdx.y, w = threadIdx.x % 16, s = threadIdx.x / 16, column = blockIdx.x * 16 + w;
+    if (!P.dgamma[kind] || P.blocks[kind] == 1) return;
     float v = 0.0f;
-    if (column < 2 * P.D)
-        for (int p = s; p < P.parts; p += 64) v += P.partial[(size_t)p * 2 * P.D + column];
+    if (column < P.D)
+        for (int p = s; p < P.blocks[kind]; p += 64) v += P.partial[((size_t)kind * MRF_ROTATE_PARTS + p) * P.D + column];
     part[s][w] = v;
     __syncthreads();
     for (int d = 32; d > 0; d /= 2) {
         if (s < d) part[s][w] += part[s + d][w];
         __syncthreads();
     }
-    if (s == 0 && column < 2 * P.D) {
-        float *const to = P.dgamma[column >= P.D];
-        if (to) to[column >= P.D ? column - P.D : column] = part[0][w];
-    }
+    if (s == 0 && column < P.D) P.dgamma[kind][column] = part[0][w];
 }
 
 namespace mrf_host {
 
-static int rotate_lanes(int D)
+template <bool FORWARD, class X, int S, int TL> static int rotate_go(const MrfRotateParams &P, bool whole, hipStream_t st)
 {
-    const int slots = (D + 1) / 2, lanes = (slots + MRF_SLOTS - 1) / MRF_SLOTS;
-    int TL = 1;
-    while (TL < lanes) TL *= 2;
-    return TL;
-}
-
-template <bool FORWARD, class X, int TL> static int rotate_go(const MrfRotateParams &P, bool whole, unsigned grid, hipStream_t st)
-{
+    const unsigned grid = (unsigned)(P.blocks[0] + P.blocks[1]);
     if constexpr (FORWARD) {
-        if (whole) mrf_rotate_fwd<X, TL, true><<<grid, 256, 0, st>>>(P);
-        else mrf_rotate_fwd<X, TL, false><<<grid, 256, 0, st>>>(P);
+        if (whole) mrf_rotate_fwd<X, S, TL, true><<<grid, 256, 0, st>>>(P);
+        else mrf_rotate_fwd<X, S, TL, false><<<grid, 256, 0, st>>>(P);
         return launch_status("mrf_rotate_fwd");
     } else {
-        if (whole) mrf_rotate_bwd<X, TL, true><<<grid, 256, 0, st>>>(P);
-        else mrf_rotate_bwd<X, TL, false><<<grid, 256, 0, st>>>(P);
-        if (P.partial) mrf_rotate_sum<<<(2 * P.D + 15) / 16, 1024, 0, st>>>(P);
+        if (whole) mrf_rotate_bwd<X, S, TL, true><<<grid, 256, 0, st>>>(P);
+        else mrf_rotate_bwd<X, S, TL, false><<<grid, 256, 0, st>>>(P);
+        if ((P.dgamma[0] && P.blocks[0] != 1) || (P.dgamma[1] && P.blocks[1] != 1)) mrf_rotate_sum<<<dim3((P.D + 15) / 16, 2), 1024, 0, st>>>(P);
         return launch_status("mrf_rotate_bwd");
     }
 }
 
-template <bool FORWARD, class X> static int rotate_typed(MrfRotateParams P, hipStream_t st)
+template <bool FORWARD, class X, int S> static int rotate_lanes(MrfRotateParams P, hipStream_t st)
 {
-    const int TL = rotate_lanes(P.D), heads = P.Hq + P.Hk;
+    const int lanes = ((P.D + 1) / 2 + S - 1) / S, heads = P.Hq + P.Hk;
+    int TL = 1;
+    while (TL < lanes) TL *= 2;
     // heads a group: all of a token's where tokens alone keep the card busy (the angles are formed once), else fewer, down to one
-    long long want = (262144 + P.tokens * TL - 1) / (P.tokens * TL);      // groups of a token for 1,024 workgroups
+    long long want = (131072 + P.tokens * TL - 1) / (P.tokens * TL);      // groups of a token for 512 workgroups
     if (want > heads) want = heads;
     P.heads = (int)((heads + want - 1) / want);
-    P.pieces = (heads + P.heads - 1) / P.heads;
-    const long long all = P.tokens * P.pieces, groups = (all + 256 / TL - 1) / (256 / TL);
-    const long long most = FORWARD ? 0x7fffffffLL : MRF_ROTATE_PARTS;
-    const unsigned grid = (unsigned)(groups < most ? groups : most);
-    P.parts = (int)grid;
-    // runs of MRF_SLOTS neighbours: pairs that turn and the rest of a head in whole ones
-    const bool whole = P.D % (2 * MRF_SLOTS) == 0 && (P.interleaved || P.half % MRF_SLOTS == 0);
-    switch (TL) {
-        case 1: return rotate_go<FORWARD, X, 1>(P, whole, grid, st);
-        case 2: return rotate_go<FORWARD, X, 2>(P, whole, grid, st);
-        case 4: return rotate_go<FORWARD, X, 4>(P, whole, grid, st);
-        case 8: return rotate_go<FORWARD, X, 8>(P, whole, grid, st);
-        case 16: return rotate_go<FORWARD, X, 16>(P, whole, grid, st);
-        case 32: return rotate_go<FORWARD, X, 32>(P, whole, grid, st);
-        default: return rotate_go<FORWARD, X, 64>(P, whole, grid, st);
+    if (P.heads > 4) P.heads -= P.heads % 4;
+    const long long most = FORWARD ? 0x3fffffffLL : MRF_ROTATE_PARTS;
+    for (int k = 0; k < 2; ++k) {
+        P.pieces[k] = ((k ? P.Hk : P.Hq) + P.heads - 1) / P.heads;
+        const long long blocks = (P.tokens * P.pieces[k] + 256 / TL - 1) / (256 / TL);
+        P.blocks[k] = (int)(blocks < most ? blocks : most);
     }
+    // runs of S neighbours: pairs that turn and the rest of a head in whole ones
+    const bool whole = P.D % (2 * S) == 0 && (P.interleaved || P.half % S == 0);
+    switch (TL) {
+        case 1: return rotate_go<FORWARD, X, S, 1>(P, whole, st);
+        case 2: return rotate_go<FORWARD, X, S, 2>(P, whole, st);
+        case 4: return rotate_go<FORWARD, X, S, 4>(P, whole, st);
+        case 8: return rotate_go<FORWARD, X, S, 8>(P, whole, st);
+        case 16: return rotate_go<FORWARD, X, S, 16>(P, whole, st);
+        case 32: return rotate_go<FORWARD, X, S, 32>(P, whole, st);
+        default: return rotate_go<FORWARD, X, S, 64>(P, whole, st);
+    }
+}
+
+// runs of 16 bytes where the head has whole ones, else of half of that in 16 bits
+template <bool FORWARD, class X> static int rotate_typed(const MrfRotateParams &P, hipStream_t st)
+{
+    if constexpr (sizeof(X) == 2)
+        if (P.D % 16 == 0 && (P.interleaved || P.half % 8 == 0)) return rotate_lanes<FORWARD, X, 8>(P, st);
+    return rotate_lanes<FORWARD, X, 4>(P, st);
 }
 
 static size_t rotate_workspace(int D) { return (size_t)MRF_ROTATE_PARTS * 2 * D * sizeof(float); }
@@ -408,8 +411,8 @@ int mrf_head_rotation_backward(const mrf_head_rotation *heads, const void *grad_
         if (!workspace) return MRF_ERR_NULL_POINTER;
         if (workspace_bytes < rotate_workspace(P.D)) return MRF_ERR_WORKSPACE_TOO_SMALL;
         P.partial = (float *)workspace;
-        if (none) {      // sums over no tokens
-            mrf_rotate_sum<<<(2 * P.D + 15) / 16, 1024, 0, (hipStream_t)hip_stream>>>(P);
+        if (none) {      // sums over nothing
+            mrf_rotate_sum<<<dim3((P.D + 15) / 16, 2), 1024, 0, (hipStream_t)hip_stream>>>(P);
             return launch_status("mrf_rotate_sum");
         }
     }
