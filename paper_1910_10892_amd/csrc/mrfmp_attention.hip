@@ -196,27 +196,50 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
     if (half == 0 && P.lse) P.lse[((long long)b * P.Hq + h) * P.Q + i] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
 }
 
-// Parts of the keys, joined in their order.  A wavefront has a query of a head; sums of a part count 2^(its maximum - the largest).
+// Parts of the keys, joined in their order: sums of a part count 2^(its maximum - the largest).  A workgroup has a query of a head; a wavefront every fourth part,
+// a lane two entries.
+constexpr int MRF_ATTN_SPLITS = 1024;
 template <class T> __global__ void __launch_bounds__(256) mrf_attn_join(const MrfAttnParams P)
 {
-    const long long n = (long long)P.B * P.Hq * P.Q, at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (at >= n) return;
-    const int lane = threadIdx.x & 63;
+    __shared__ float weight[MRF_ATTN_SPLITS];
+    __shared__ float scratch[2][4], sums[4][128];
+    const long long n = (long long)P.B * P.Hq * P.Q, at = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const float2 *const ends = (const float2 *)P.part;
-    const float *const part = P.part + 2 * P.splits * n;
+    const float *const part = P.part + 2 * P.splits * n + at * P.D;
     float top = -INFINITY, l = 0.0f;
-    for (int s = 0; s < P.splits; ++s) top = fmaxf(top, ends[s * n + at].x);
+    for (int s = tid; s < P.splits; s += 256) top = fmaxf(top, ends[s * n + at].x);
+    top = -mrf_lanes_min<64>(-top);
+    if (lane == 0) scratch[0][wv] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(scratch[0][0], scratch[0][1]), fmaxf(scratch[0][2], scratch[0][3]));
     const float base = top == -INFINITY ? 0.0f : top;
-    for (int s = 0; s < P.splits; ++s) l += ends[s * n + at].y * __builtin_amdgcn_exp2f(ends[s * n + at].x - base);
+    for (int s = tid; s < P.splits; s += 256) {
+        const float2 e = ends[s * n + at];
+        const float w = __builtin_amdgcn_exp2f(e.x - base);
+        weight[s] = w;
+        l = fmaf(e.y, w, l);
+    }
+    l = mrf_lanes_sum<64>(l);
+    if (lane == 0) scratch[1][wv] = l;
+    __syncthreads();
+    l = (scratch[1][0] + scratch[1][1]) + (scratch[1][2] + scratch[1][3]);
+    float x = 0.0f, y = 0.0f;
+    const int d0 = lane < P.D ? lane : 0, d1 = lane + 64 < P.D ? lane + 64 : 0;
+#pragma unroll 4
+    for (int s = wv; s < P.splits; s += 4) {
+        const float w = weight[s], *const p = part + s * n * P.D;
+        x = fmaf(p[d0], w, x);
+        y = fmaf(p[d1], w, y);
+    }
+    sums[wv][lane] = x;
+    sums[wv][lane + 64] = y;
+    __syncthreads();
     const float inv = l > 0.0f ? 1.0f / l : l;
     const long long bh = at / P.Q, i = at - bh * P.Q, b = bh / P.Hq, h = bh - b * P.Hq;
     T *const out = (T *)P.out + ((b * P.Q + i) * P.Hq + h) * P.D;
-    for (int d = lane; d < P.D; d += 64) {
-        float x = 0.0f;
-        for (int s = 0; s < P.splits; ++s) x = fmaf(part[(s * n + at) * P.D + d], __builtin_amdgcn_exp2f(ends[s * n + at].x - base), x);
-        out[d] = mrf_from_f32<T>(x * inv);
-    }
-    if (lane == 0 && P.lse) P.lse[at] = l == 0.0f ? -INFINITY : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+    if (tid < P.D) out[tid] = mrf_from_f32<T>(((sums[0][tid] + sums[1][tid]) + (sums[2][tid] + sums[3][tid])) * inv);
+    if (tid == 0 && P.lse) P.lse[at] = l == 0.0f ? -INFINITY : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
 }
 
 namespace mrf_host {
@@ -227,12 +250,12 @@ template <class T, int DP> static int attention_go(const MrfAttnParams &P, const
     if (plan.pack) {
         if (P.table) mrf_attn_fwd<T, DP, 1, true, true><<<grid, 64, 0, st>>>(P);
         else mrf_attn_fwd<T, DP, 1, true, false><<<grid, 64, 0, st>>>(P);
-        if (P.splits > 1) mrf_attn_join<T><<<(unsigned)(((long long)P.B * P.Hq * P.Q + 3) / 4), 256, 0, st>>>(P);
     } else {
         constexpr int NW = mrf_attn_wide<T, DP>();
         if (P.table) mrf_attn_fwd<T, DP, NW, false, true><<<grid, 64 * NW, 0, st>>>(P);
         else mrf_attn_fwd<T, DP, NW, false, false><<<grid, 64 * NW, 0, st>>>(P);
     }
+    if (P.splits > 1) mrf_attn_join<T><<<(unsigned)((long long)P.B * P.Hq * P.Q), 256, 0, st>>>(P);
     return launch_status("mrf_attn_fwd");
 }
 
@@ -283,11 +306,14 @@ static AttnPlan attention_plan(const MrfAttnParams &P, int type)
 {
     const long long rows = (long long)P.Q * P.G;
     const int block = type != MRF_F32 && P.D > 64 ? 256 : 128;      // (as mrf_attn_wide has it)
-    if (P.Q > 16 && rows > 64) return {false, 1, (unsigned)((long long)P.B * P.Hq * ((P.Q + block - 1) / block))};
-    const long long groups = (long long)P.B * P.Hk * ((rows + 31) / 32), tiles = (P.K + 31) / 32;
-    long long splits = groups ? 2048 / groups : 1;
+    const bool pack = P.Q <= 16 || rows <= 64;
+    const long long groups = pack ? (long long)P.B * P.Hk * ((rows + 31) / 32) : (long long)P.B * P.Hq * ((P.Q + block - 1) / block);
+    // parts of the keys: for eight wavefronts of few rows on a compute unit, or two workgroups of many; of four tiles at least
+    const long long tiles = ((long long)P.K + 31) / 32 / (pack ? 1 : 2);
+    long long splits = groups ? (pack ? 2048 : 512) / groups : 1;
     if (splits > tiles / 4) splits = tiles / 4;
-    return {true, (int)(splits < 1 ? 1 : splits), (unsigned)groups};
+    if (splits > MRF_ATTN_SPLITS) splits = MRF_ATTN_SPLITS;
+    return {pack, (int)(splits < 1 ? 1 : splits), (unsigned)groups};
 }
 
 static size_t attention_forward_bytes(const MrfAttnParams &P, int type)
