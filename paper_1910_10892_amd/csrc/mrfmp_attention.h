@@ -120,6 +120,8 @@ struct MrfAttnParams {
     const void *dout;
     void *dq, *dk, *dv;
     float *delta;                                 // [B][Hq][Q]
+    int shares;                                   // parts of the heads that share keys, one workgroup each:
+    float *share;                                 // [shares][dk, dv][B][K][Hk][D], if more than one
     float *lines, *partial, *dtable;              // partial: [Hq][n_buckets][MRF_TABLE_PARTS]
     int strips, line;                             // strips of 32 keys; entries of a line
     int parts;

@@ -11,6 +11,12 @@
 // Keys of a tile: as many as two tiles of keys and values in LDS leave two workgroups (32 bits: one or two) on a compute unit.
 template <class T, int NW> constexpr int mrf_attn_keys() { return sizeof(T) == 4 || NW == 1 ? 32 : 64; }
 
+// What was summed is scaled only where a maximum rises by more than this (in powers of two): most tiles bring one of 32 queries a new maximum.  Probabilities are then up to
+// 2^8, which takes that much off what they are scaled up by in MRF_F16.
+constexpr float MRF_ATTN_RISE = 8.0f;
+template <class T> constexpr float mrf_attn_shift_forward() { return mrf_attn_shift<T>() > 0.0f ? mrf_attn_shift<T>() - MRF_ATTN_RISE : 0.0f; }
+template <class T> constexpr float mrf_attn_unshift_forward() { return mrf_attn_shift<T>() > 0.0f ? 0x1p-7f : 1.0f; }
+
 // Wavefronts of a SIMD: two, where their registers fit (in 32 bits not for 128 entries)
 template <class T, int DP, int NW> constexpr int mrf_attn_waves() { return NW == 1 || (sizeof(T) == 4 && DP == 128) ? 1 : 2; }
 
@@ -29,7 +35,8 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
     __shared__ float line[2][BIAS && !PACK ? LINE : 1];
     const int lane = threadIdx.x & 63, wv = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5;
     const int heads = PACK ? P.Hk : P.Hq, rows = PACK ? P.Q * P.G : P.Q, blocks = (rows + ROWS - 1) / ROWS;
-    const int bh = blockIdx.x / blocks, block = blocks - 1 - (int)(blockIdx.x % blocks);      // (the longest rows of causal ones first)
+    // (the longest rows of causal ones first, so that the last workgroups to start are short ones; a head's blocks a fixed number apart, on one XCD as a rule)
+    const int bh = blockIdx.x % (P.B * heads), block = blocks - 1 - (int)(blockIdx.x / (P.B * heads));
     const int b = bh / heads, h0 = bh % heads, hk = PACK ? h0 : h0 / P.G;
     const MrfAttnBatch s(P, b);
     const int r0 = block * ROWS, row = r0 + wv * 32 + (lane & 31);
@@ -130,8 +137,8 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
             top = mrf_halves_max(top);
             if constexpr (!BIAS) top *= P.c;
             top = fmaxf(m, top);
-            const float base = top == -INFINITY ? 0.0f : top, low = base - mrf_attn_shift<T>();
-            if (__any(top > m)) {
+            const float base = top == -INFINITY ? 0.0f : top;
+            if (__any(top > m + MRF_ATTN_RISE)) {
                 const float less = __builtin_amdgcn_exp2f(m - base);
                 l *= less;
 #pragma unroll
@@ -140,6 +147,7 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
                     for (int e = 0; e < 16; ++e) o[d][e] *= less;
                 m = top;
             }
+            const float low = (m == -INFINITY ? 0.0f : m) - mrf_attn_shift_forward<T>();
             // 16 keys at a time: their probabilities, and their values on the way, while those before are multiplied
             frag vf[2][DP / 32], p[2];
             const auto part = [&](int y) {
@@ -167,7 +175,7 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
         __syncthreads();
     }
 
-    l = mrf_halves_sum(l) * mrf_attn_unshift<T>();
+    l = mrf_halves_sum(l) * mrf_attn_unshift_forward<T>();
     if (row >= rows) return;
     if (P.splits > 1) {
         const long long n = (long long)P.B * P.Hq * P.Q, at = ((long long)b * P.Hq + h) * P.Q + i;
@@ -178,13 +186,13 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
             for (int e = 0; e < 16; e += 4) {
                 float x[4];
 #pragma unroll
-                for (int n = 0; n < 4; ++n) x[n] = o[d][e + n] * mrf_attn_unshift<T>();
+                for (int n = 0; n < 4; ++n) x[n] = o[d][e + n] * mrf_attn_unshift_forward<T>();
                 mrf_store4(part, 32 * d + mrf_acc_row(e, half), P.D, x);
             }
         if (half == 0) ((float2 *)P.part)[blockIdx.y * n + at] = make_float2(m, l);
         return;
     }
-    const float inv = l > 0.0f ? mrf_attn_unshift<T>() / l : l;      // (no keys: 0; NaN stays)
+    const float inv = l > 0.0f ? mrf_attn_unshift_forward<T>() / l : l;      // (no keys: 0; NaN stays)
     T *const out = (T *)P.out + (((long long)b * P.Q + i) * P.Hq + h) * P.D;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)

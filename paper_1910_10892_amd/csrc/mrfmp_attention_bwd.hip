@@ -24,7 +24,8 @@ template <class T, int DP, bool BIAS> __global__ void __launch_bounds__(256) mrf
     __shared__ __align__(16) T ldsK[2][KT * Rows::LD], ldsV[2][KT * Rows::LD];
     __shared__ float line[2][BIAS ? LINE : 1];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5;
-    const int blocks = (P.Q + ROWS - 1) / ROWS, bh = blockIdx.x / blocks, block = blocks - 1 - (int)(blockIdx.x % blocks);
+    // (the longest rows of causal ones first)
+    const int blocks = (P.Q + ROWS - 1) / ROWS, bh = blockIdx.x % (P.B * P.Hq), block = blocks - 1 - (int)(blockIdx.x / (P.B * P.Hq));
     const int b = bh / P.Hq, h = bh % P.Hq, hk = h / P.G;
     const MrfAttnBatch s(P, b);
     const int r0 = block * ROWS, i = r0 + wv * 32 + (lane & 31);
@@ -94,7 +95,7 @@ template <class T, int DP, bool BIAS> __global__ void __launch_bounds__(256) mrf
                 mrf_acc c, dp;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) c[e] = dp[e] = 0.0f;
-                mrf_ahead<DP / 16, (sizeof(T) == 4 ? 1 : 2)>([&](int d) { return MrfTwo<frag>{Rows::along(ldsK[buf], 32 * u, 16 * d), Rows::along(ldsV[buf], 32 * u, 16 * d)}; },
+                mrf_ahead<DP / 16, (sizeof(T) == 4 ? 1 : DP == 128 ? 4 : 2)>([&](int d) { return MrfTwo<frag>{Rows::along(ldsK[buf], 32 * u, 16 * d), Rows::along(ldsV[buf], 32 * u, 16 * d)}; },
                                       [&](int d, const MrfTwo<frag> &f) {
                                           c = mrf_mma(f.a, qf[d], c);
                                           dp = mrf_mma(f.b, gf[d], dp);
@@ -122,7 +123,7 @@ template <class T, int DP, bool BIAS> __global__ void __launch_bounds__(256) mrf
                 }
                 range.fit(dp, dq);
                 const frag sf[2] = {mrf_acc_frag<T>(dp, 0), mrf_acc_frag<T>(dp, 1)}, pf[2] = {mrf_acc_frag<T>(c, 0), mrf_acc_frag<T>(c, 1)};
-                mrf_ahead<DP / 16, (sizeof(T) == 4 ? 1 : 2)>([&](int n) { return Rows::across(ldsK[buf], 32 * u + 16 * (n / (DP / 32)), n % (DP / 32) * 32); },
+                mrf_ahead<DP / 16, (sizeof(T) == 4 ? 1 : DP == 128 ? 4 : 2)>([&](int n) { return Rows::across(ldsK[buf], 32 * u + 16 * (n / (DP / 32)), n % (DP / 32) * 32); },
                                       [&](int n, const frag &f) {
                                           const int x = n / (DP / 32), d = n % (DP / 32);
                                           dq[d] = mrf_mma(f, sf[x], dq[d]);
@@ -177,7 +178,8 @@ template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV> __global__ v
     __shared__ float line[2][BIAS ? LINE : 1];
     __shared__ float skew[TABLE ? 4 : 1][TABLE ? 32 * MRF_SKEW : 1];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5;
-    const int blocks = (P.K + KEYS - 1) / KEYS, bh = blockIdx.x / blocks, block = (int)(blockIdx.x % blocks);
+    // (the keys that most queries see first; part blockIdx.y of the heads that share them)
+    const int bh = blockIdx.x % (P.B * P.Hk), block = (int)(blockIdx.x / (P.B * P.Hk)), group = P.G / P.shares;
     const int b = bh / P.Hk, hk = bh % P.Hk;
     const MrfAttnBatch s(P, b);
     const int k0 = block * KEYS, j = k0 + wv * 32 + (lane & 31), w0 = k0 + wv * 32, w1 = min(w0 + 31, s.nk - 1);
@@ -205,8 +207,8 @@ template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV> __global__ v
     MrfRange<T> range;
     Rows qr, gr;
     float lse_next = 0.0f, delta_next = 0.0f, bias_next = 0.0f;
-    for (int g = 0; g < P.G; ++g) {
-        const int h = hk * P.G + g;
+    for (int g = 0; g < group; ++g) {
+        const int h = hk * P.G + blockIdx.y * group + g;
         const T *q = (const T *)P.q + b * P.qs[0] + h * P.qs[2], *go = (const T *)P.dout + ((long long)b * P.Q * P.Hq + h) * P.D;
         const long long stat = ((long long)b * P.Hq + h) * P.Q;
         const auto load = [&](int t) {
@@ -252,7 +254,7 @@ template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV> __global__ v
                     mrf_acc c, dp;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) c[e] = dp[e] = 0.0f;
-                    mrf_ahead<DP / 16, (sizeof(T) == 4 ? 1 : 2)>(
+                    mrf_ahead<DP / 16, (sizeof(T) == 4 ? 1 : DP == 128 ? 4 : 2)>(
                         [&](int d) {
                             MrfTwo<frag> f = {Rows::along(ldsQ[buf], 32 * u, 16 * d), {}};
                             if constexpr (DK) f.b = Rows::along(ldsG[buf], 32 * u, 16 * d);
@@ -300,7 +302,7 @@ template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV> __global__ v
                         sf[0] = mrf_acc_frag<T>(dp, 0), sf[1] = mrf_acc_frag<T>(dp, 1);
                     }
                     if constexpr (DV) pf[0] = mrf_acc_frag<T>(c, 0), pf[1] = mrf_acc_frag<T>(c, 1);
-                    mrf_ahead<DP / 16, (sizeof(T) == 4 ? 1 : 2)>(
+                    mrf_ahead<DP / 16, (sizeof(T) == 4 ? 1 : DP == 128 ? 4 : 2)>(
                         [&](int n) {
                             const int row = 32 * u + 16 * (n / (DP / 32)), at = n % (DP / 32) * 32;
                             MrfTwo<frag> f = {};
@@ -334,24 +336,49 @@ template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV> __global__ v
             if (half == 0 && t0 < t1) to_line[t1 * QT + lane] = goes_on * mrf_attn_unshift<T>();
     }
     if (j >= P.K) return;
-    const long long row = (((long long)b * P.K + j) * P.Hk + hk) * P.D;
+    const long long row = (((long long)b * P.K + j) * P.Hk + hk) * P.D, all = (long long)P.B * P.K * P.Hk * P.D;
     const float ks = P.scale * mrf_attn_unshift<T>() * range.undo(), vs = mrf_attn_unshift<T>();
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
             float x[4];
+            const int at = 32 * d + mrf_acc_row(e, half);
             if constexpr (DK) {
 #pragma unroll
                 for (int n = 0; n < 4; ++n) x[n] = dk[DK ? d : 0][e + n] * ks;
-                if (P.dk) mrf_store4((T *)P.dk + row, 32 * d + mrf_acc_row(e, half), P.D, x);
+                if (P.shares > 1) mrf_store4(P.share + 2 * blockIdx.y * all + row, at, P.D, x);
+                else if (P.dk) mrf_store4((T *)P.dk + row, at, P.D, x);
             }
             if constexpr (DV) {
 #pragma unroll
                 for (int n = 0; n < 4; ++n) x[n] = dv[DV ? d : 0][e + n] * vs;
-                if (P.dv) mrf_store4((T *)P.dv + row, 32 * d + mrf_acc_row(e, half), P.D, x);
+                if (P.shares > 1) mrf_store4(P.share + (2 * blockIdx.y + 1) * all + row, at, P.D, x);
+                else if (P.dv) mrf_store4((T *)P.dv + row, at, P.D, x);
             }
         }
+}
+
+// Sums of the parts that several workgroups made of a head of keys, in their order: dk, dv
+template <class T> __global__ void __launch_bounds__(256) mrf_attn_shares(const MrfAttnParams P)
+{
+    typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
+    const long long all = (long long)P.B * P.K * P.Hk * P.D, at = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (at >= all) return;
+    T *const out = (T *)(blockIdx.y ? P.dv : P.dk);
+    const int left = all - at < 4 ? (int)(all - at) : 4;
+    float x[4] = {};
+    for (int s = 0; s < P.shares; ++s) {
+        const float *const p = P.share + (2 * s + blockIdx.y) * all + at;
+        if (left == 4) {
+            const vec v = *(const vec *)p;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] += v[j];
+        } else {
+            for (int j = 0; j < left; ++j) x[j] += p[j];
+        }
+    }
+    if (out) mrf_store4(out + at, 0, left, x);
 }
 
 // Gradient of the table: what the lines hold of a diagonal, summed over the strips of keys that it crosses, belongs to the bucket of its offset.  A workgroup
@@ -428,7 +455,7 @@ template <class T, int DP> static int attention_back(const MrfAttnParams &P, hip
         else mrf_attn_bwd_queries<T, DP, false><<<grid, 256, 0, st>>>(P);
     }
     if (P.B && P.K && (P.dk || P.dv || P.dtable)) {
-        const unsigned grid = (unsigned)((long long)P.B * P.Hk * ((P.K + 127) / 128));
+        const dim3 grid((unsigned)((long long)P.B * P.Hk * ((P.K + 127) / 128)), (unsigned)P.shares);
         constexpr bool ONE = DP == 128 && sizeof(T) == 4;      // one of the two at a time
         if (P.dtable && pairs) mrf_attn_bwd_keys<T, DP, true, true, true, DP != 128><<<grid, 256, 0, st>>>(P);
         else if (P.table) mrf_attn_bwd_keys<T, DP, true, false, true, !ONE><<<grid, 256, 0, st>>>(P);
@@ -438,6 +465,10 @@ template <class T, int DP> static int attention_back(const MrfAttnParams &P, hip
                 if (P.table) mrf_attn_bwd_keys<T, DP, true, false, false, true><<<grid, 256, 0, st>>>(P);
                 else mrf_attn_bwd_keys<T, DP, false, false, false, true><<<grid, 256, 0, st>>>(P);
             }
+        if (P.shares > 1 && (P.dk || P.dv)) {
+            const long long n = ((long long)P.B * P.K * P.Hk * P.D + 1023) / 1024;
+            mrf_attn_shares<T><<<dim3((unsigned)n, 2), 256, 0, st>>>(P);
+        }
     }
     if (P.dtable) {
         MrfAttnParams S = P;
@@ -485,10 +516,26 @@ static void attention_lines(MrfAttnParams &P)
     P.line = (int)(((long long)P.Q + 63) / 64 * 64 + 32);
 }
 
+// Workgroups that share the heads of queries on a head of keys: as many as it takes for four on a compute unit, since some have far more queries to go through
+// than others where those see only keys before them.
+static int attention_shares(const MrfAttnParams &P)
+{
+    const long long grid = (long long)P.B * P.Hk * ((P.K + 127) / 128);
+    int shares = 1;
+    for (int n = 2; n <= P.G && grid * shares < 1024; ++n)
+        if (P.G % n == 0) shares = n;
+    return shares;
+}
+
+static size_t attention_share_bytes(const MrfAttnParams &P, int shares)
+{
+    return shares > 1 ? round256(2 * (size_t)shares * P.B * P.K * P.Hk * P.D * sizeof(float)) : 0;
+}
+
 size_t attention_backward_bytes(const MrfAttnParams &given)
 {
     MrfAttnParams P = given;
-    size_t n = round256((size_t)P.B * P.Hq * P.Q * sizeof(float));
+    size_t n = round256((size_t)P.B * P.Hq * P.Q * sizeof(float)) + attention_share_bytes(P, attention_shares(P));
     if (P.table && P.Q && P.K) {
         attention_lines(P);
         n += round256((size_t)P.B * P.Hq * P.strips * P.line * sizeof(float)) + (size_t)P.Hq * P.n_buckets * MRF_TABLE_PARTS * sizeof(float);
@@ -516,7 +563,9 @@ int mrf_attention_backward(const mrf_attention *att, const void *grad_out, const
     P.dout = grad_out; P.out = (void *)out; P.lse = (float *)lse; P.dq = grad_q; P.dk = grad_k; P.dv = grad_v; P.dtable = grad_table;
     attention_lines(P);
     P.delta = (float *)workspace;
-    P.lines = (float *)((char *)workspace + round256((size_t)P.B * P.Hq * P.Q * sizeof(float)));
+    P.shares = attention_shares(P);
+    P.share = (float *)((char *)workspace + round256((size_t)P.B * P.Hq * P.Q * sizeof(float)));
+    P.lines = (float *)((char *)P.share + attention_share_bytes(P, P.shares));
     P.partial = (float *)((char *)P.lines + round256((size_t)P.B * P.Hq * P.strips * P.line * sizeof(float)));
     hipStream_t st = (hipStream_t)hip_stream;
     if (att->type == MRF_F32) return attention_backward_f32(P, st);
