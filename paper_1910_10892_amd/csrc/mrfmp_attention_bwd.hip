@@ -516,13 +516,13 @@ static void attention_lines(MrfAttnParams &P)
     P.line = (int)(((long long)P.Q + 63) / 64 * 64 + 32);
 }
 
-// Workgroups that share the heads of queries on a head of keys: as many as it takes for four on a compute unit, since some have far more queries to go through
+// Workgroups that share the heads of queries on a head of keys: as many as it takes for two on a compute unit, since some have far more queries to go through
 // than others where those see only keys before them.
 static int attention_shares(const MrfAttnParams &P)
 {
     const long long grid = (long long)P.B * P.Hk * ((P.K + 127) / 128);
     int shares = 1;
-    for (int n = 2; n <= P.G && grid * shares < 1024; ++n)
+    for (int n = 2; n <= P.G && grid * shares < 512; ++n)
         if (P.G % n == 0) shares = n;
     return shares;
 }
