@@ -150,15 +150,54 @@ struct MrfAttnBatch {
     __device__ inline int to(int i1) const { return min(i1 + hi + 1, nk); }
 };
 
-// the value of the bias at j - i = d, times log2(e); of head h
-__device__ inline float mrf_attn_bias(const MrfAttnParams &P, const MrfAttnBatch &s, int h, long long d)
+// the bucket of j - i = d; a bucket's value of head h, times log2(e)
+__device__ inline int mrf_attn_bucket(const MrfAttnParams &P, const MrfAttnBatch &s, long long d)
 {
     long long at = s.map + d;
     at = at < 0 ? 0 : at >= P.n_offsets ? P.n_offsets - 1 : at;
-    int b = P.bucket_of[at];
-    b = b < 0 ? 0 : b >= P.n_buckets ? P.n_buckets - 1 : b;
-    return P.table[P.heads_last ? (size_t)b * P.Hq + h : (size_t)h * P.n_buckets + b] * 1.44269504088896340736f;
+    const int b = P.bucket_of[at];
+    return b < 0 ? 0 : b >= P.n_buckets ? P.n_buckets - 1 : b;
 }
+__device__ inline float mrf_attn_level(const MrfAttnParams &P, int h, int bucket)
+{
+    return P.table[P.heads_last ? (size_t)bucket * P.Hq + h : (size_t)h * P.n_buckets + bucket] * 1.44269504088896340736f;
+}
+__device__ inline float mrf_attn_bias(const MrfAttnParams &P, const MrfAttnBatch &s, int h, long long d)
+{
+    return mrf_attn_level(P, h, mrf_attn_bucket(P, s, d));
+}
+
+// The bias along a tile: its values at N offsets in a row, and whether these are all of one bucket -- as most are, far from the queries: then there is nothing to look up
+// for each pair.  Threads 0 .. N - 1 fetch, then put; all may ask behind the next barrier.
+template <int N> struct MrfLine {
+    static constexpr int WAVES = (N + 63) / 64;
+    float value[2][N];
+    int same[2][WAVES];
+    struct Next { float value; int same; };
+    __device__ inline void fetch(const MrfAttnParams &P, const MrfAttnBatch &s, int h, long long first, Next &n) const
+    {
+        if ((int)threadIdx.x < N) {
+            const int b = mrf_attn_bucket(P, s, first + (int)threadIdx.x), other = __builtin_amdgcn_readfirstlane(b);
+            n.value = mrf_attn_level(P, h, b);
+            n.same = __any(b != other) ? -1 : other;
+        }
+    }
+    __device__ inline void put(int buf, const Next &n)
+    {
+        if ((int)threadIdx.x < N) {
+            value[buf][threadIdx.x] = n.value;
+            if ((threadIdx.x & 63) == 0) same[buf][threadIdx.x >> 6] = n.same;
+        }
+    }
+    __device__ inline bool flat(int buf) const
+    {
+        const int first = same[buf][0];
+        bool all = first >= 0;
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) all = all && same[buf][w] == first;
+        return __builtin_amdgcn_readfirstlane(all ? 1 : 0) != 0;
+    }
+};
 
 // Rows of a tensor in LDS: ROWS of DP entries.  A thread moves chunks of 16 bytes, which wait in its registers between the load and the store.  In 16 bits chunk c
 // of row r lies at place c ^ swap(r): 16 rows' chunks c (an operand along the rows), and four rows' stretches of 32 entries (one across them), then
@@ -213,41 +252,75 @@ template <class T, int DP, int ROWS, int NT> struct MrfRows {
             *(vec *)(lds + place(row, d / PER)) = r[n];
         }
     }
-    // operand whose 32 rows are rows row0 ..., and whose sum runs over 16 entries from d on
-    static __device__ inline typename MrfFrag<T>::type along(const T *lds, int row0, int d)
+};
+
+// Where a lane's parts of the operands lie, in elements: worked out once, moved from one of the two tiles in LDS to the other, and otherwise only the constant part of an
+// address changes.
+template <class T, int DP, int LD> struct MrfPlaces {
+    static constexpr bool SMALL = sizeof(T) == 2;
+    static constexpr int A = SMALL ? DP / 16 : 1, C = SMALL ? DP / 32 : 1;
+    typedef typename MrfFrag<T>::type frag;
+    int a[A], c[C][2];
+
+    template <class Rows> __device__ inline void init()
     {
-        const int lane = threadIdx.x & 63, row = row0 + (lane & 31), at = d + 8 * (lane >> 5);
-        if constexpr (sizeof(T) == 2) {
-            return *(const typename MrfFrag<T>::type *)(lds + place(row, at / PER));
-        } else {
-            typename MrfFrag<T>::type f;
-            const vec a = *(const vec *)(lds + place(row, at / PER)), b = *(const vec *)(lds + place(row, at / PER + 1));
+        const int lane = threadIdx.x & 63, half = lane >> 5;
+        if constexpr (SMALL) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) f[j] = a[j], f[4 + j] = b[j];
+            for (int n = 0; n < A; ++n) a[n] = Rows::place(lane & 31, 2 * n + half);
+#pragma unroll
+            for (int n = 0; n < C; ++n)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int at = 32 * n + (lane & 16) + 4 * (lane & 3);
+                    c[n][x] = Rows::place(4 * half + (lane >> 2 & 3) + 8 * x, at / 8) + at % 8;
+                }
+        } else {
+            a[0] = Rows::place(lane & 31, 2 * half);
+            c[0][0] = 4 * half * LD + (lane & 31);
+        }
+    }
+    __device__ inline void move(int by)
+    {
+#pragma unroll
+        for (int n = 0; n < A; ++n) a[n] += by;
+#pragma unroll
+        for (int n = 0; n < C; ++n) {
+            c[n][0] += by;
+            if constexpr (SMALL) c[n][1] += by;
+        }
+    }
+    // operand whose 32 rows are the tile's rows (of `lds`, a multiple of 16 rows on), and whose sum runs over entries 16 n ..
+    __device__ inline frag along(const T *lds, int n) const
+    {
+        if constexpr (SMALL) {
+            return *(const frag *)(lds + a[n]);
+        } else {
+            typedef float vec __attribute__((ext_vector_type(4)));
+            const vec x = *(const vec *)(lds + a[0] + 16 * n), y = *(const vec *)(lds + a[0] + 16 * n + 4);
+            frag f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[j] = x[j], f[4 + j] = y[j];
             return f;
         }
     }
-    // operand whose 32 rows are the entries d ..., and whose sum runs over rows row0 + 4 half + {0 .. 3, 8 .. 11}
-    static __device__ inline typename MrfFrag<T>::type across(const T *lds, int row0, int d)
+    // operand whose 32 rows are entries 32 n .., and whose sum runs over rows 4 half + {0 .. 3, 8 .. 11}
+    __device__ inline frag across(const T *lds, int n) const
     {
-        const int lane = threadIdx.x & 63, half = lane >> 5;
-        typename MrfFrag<T>::type f;
-        if constexpr (sizeof(T) == 2) {
+        if constexpr (SMALL) {
             // the transposing read: of 16 lanes, four each point at a row's 16 entries, and each gets the four rows' values of one entry
             typedef short v4 __attribute__((ext_vector_type(4)));
             typedef short v8 __attribute__((ext_vector_type(8)));
-            const int row = row0 + 4 * half + (lane >> 2 & 3), at = d + (lane & 16) + 4 * (lane & 3);
-            const T *p = lds + place(row, at / PER) + at % PER, *n = lds + place(row + 8, at / PER) + at % PER;
-            const v4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4 *)p);
-            const v4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4 *)n);
-            const v8 ab = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-            f = __builtin_bit_cast(typename MrfFrag<T>::type, ab);
+            const v4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4 *)(lds + c[n][0]));
+            const v4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4 *)(lds + c[n][1]));
+            const v8 xy = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+            return __builtin_bit_cast(frag, xy);
         } else {
-            const T *p = lds + (row0 + 4 * half) * LD + d + (lane & 31);
+            frag f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = p[(8 * (j / 4) + j % 4) * LD];
+            for (int j = 0; j < 8; ++j) f[j] = lds[c[0][0] + 32 * n + (8 * (j / 4) + j % 4) * LD];
+            return f;
         }
-        return f;
     }
 };
 

@@ -31,8 +31,11 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
     constexpr int KT = mrf_attn_keys<T, NW>(), NT = 64 * NW, ROWS = 32 * NW, LINE = ROWS + KT;
     typedef MrfRows<T, DP, KT, NT> Rows;
     typedef typename MrfFrag<T>::type frag;
-    __shared__ __align__(16) T ldsK[2][KT * Rows::LD], ldsV[2][KT * Rows::LD];
-    __shared__ float line[2][BIAS && !PACK ? LINE : 1];
+    constexpr int TILE = KT * Rows::LD;
+    __shared__ __align__(16) T lds[2][2][TILE];      // keys, values
+    __shared__ MrfLine<BIAS && !PACK ? LINE : 1> line;
+    MrfPlaces<T, DP, Rows::LD> places;
+    places.template init<Rows>();
     const int lane = threadIdx.x & 63, wv = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5;
     const int heads = PACK ? P.Hk : P.Hq, rows = PACK ? P.Q * P.G : P.Q, blocks = (rows + ROWS - 1) / ROWS;
     // (the longest rows of causal ones first, so that the last workgroups to start are short ones; a head's blocks a fixed number apart, on one XCD as a rule)
@@ -61,18 +64,16 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
     }
     const T *k = (const T *)P.k + b * P.ks[0] + hk * P.ks[2], *v = (const T *)P.v + b * P.vs[0] + hk * P.vs[2];
     Rows kr, vr;
-    float bias_next = 0.0f;
+    typename decltype(line)::Next bias_next = {};
     const auto load = [&](int t) {
         kr.load(k + (long long)t * KT * P.ks[1], P.ks[1], s.nk - t * KT, P.D);
         vr.load(v + (long long)t * KT * P.vs[1], P.vs[1], s.nk - t * KT, P.D);
-        if constexpr (BIAS && !PACK)
-            if ((int)threadIdx.x < LINE) bias_next = mrf_attn_bias(P, s, h0, (long long)t * KT - r0 - (ROWS - 1) + (int)threadIdx.x);
+        if constexpr (BIAS && !PACK) line.fetch(P, s, h0, (long long)t * KT - r0 - (ROWS - 1), bias_next);
     };
     const auto store = [&](int buf) {
-        kr.store(ldsK[buf]);
-        vr.store(ldsV[buf]);
-        if constexpr (BIAS && !PACK)
-            if ((int)threadIdx.x < LINE) line[buf][threadIdx.x] = bias_next;
+        kr.store(lds[buf][0]);
+        vr.store(lds[buf][1]);
+        if constexpr (BIAS && !PACK) line.put(buf, bias_next);
     };
 
     // Of two wavefronts on a SIMD one goes first: it multiplies while the other takes exponentials, instead of both doing the same at a time.
@@ -101,25 +102,33 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
 #pragma unroll
                 for (int e = 0; e < 16; ++e) c[u][e] = 0.0f;
             constexpr int STEPS = KT / 32 * DP / 16;
-            mrf_ahead<STEPS, (sizeof(T) == 4 ? 1 : DP == 128 ? 2 : STEPS < 4 ? STEPS : 4)>([&](int n) { return Rows::along(ldsK[buf], 32 * (n / (DP / 16)), n % (DP / 16) * 16); },
-                                                      [&](int n, const frag &f) { c[n / (DP / 16)] = mrf_mma(f, qf[n % (DP / 16)], c[n / (DP / 16)]); });
+            mrf_ahead<STEPS, (sizeof(T) == 4 ? 1 : DP == 128 ? 2 : STEPS < 4 ? STEPS : 4)>(
+                [&](int n) { return places.along(lds[0][0] + 32 * (n / (DP / 16)) * Rows::LD, n % (DP / 16)); },
+                [&](int n, const frag &f) { c[n / (DP / 16)] = mrf_mma(f, qf[n % (DP / 16)], c[n / (DP / 16)]); });
             // keys that this lane's query may see: [from, to) of the tile; all of them, for most tiles
             const bool whole = k0 >= w1 + s.lo && k0 + KT - 1 <= w0 + s.hi && k0 + KT <= s.nk && (w2 == w1 || s.nq == P.Q);
             const int from = i + s.lo - k0, to = there ? min(i + s.hi + 1, s.nk) - k0 : 0;
-            // (without a bias the scores stay products, whose maximum is the scores' too, and the scale goes in with the maximum: one operation)
-            float top = -INFINITY;
+            // (without a bias, or with the same for all, the scores stay products, whose maximum is the scores' too, and the rest goes in with the maximum: one operation)
+            float top = -INFINITY, times = P.c, plus = 0.0f;
+            if constexpr (BIAS && PACK) {
+                times = 1.0f;
 #pragma unroll
-            for (int u = 0; u < KT / 32; ++u)
+                for (int u = 0; u < KT / 32; ++u)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int j = 32 * u + mrf_acc_row(e, half);
-                    float x = c[u][e];
-                    if constexpr (BIAS) {
-                        if constexpr (PACK) x = fmaf(x, P.c, mrf_attn_bias(P, s, h, (long long)k0 + j - i));
-                        else x = fmaf(x, P.c, line[buf][ROWS - 1 + j - (wv * 32 + (lane & 31))]);
-                    }
-                    c[u][e] = x;
+                    for (int e = 0; e < 16; ++e) c[u][e] = fmaf(c[u][e], P.c, mrf_attn_bias(P, s, h, (long long)k0 + 32 * u + mrf_acc_row(e, half) - i));
+            } else if constexpr (BIAS) {
+                if (line.flat(buf)) {
+                    plus = line.value[buf][0];
+                } else {
+                    mrf_stay_branch();
+                    times = 1.0f;
+                    const float *const at = line.value[buf] + ROWS - 1 - (wv * 32 + (lane & 31));
+#pragma unroll
+                    for (int u = 0; u < KT / 32; ++u)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) c[u][e] = fmaf(c[u][e], P.c, at[32 * u + mrf_acc_row(e, half)]);
                 }
+            }
             if (!whole) {
                 mrf_stay_branch();
 #pragma unroll
@@ -135,8 +144,7 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
 #pragma unroll
                 for (int e = 0; e < 16; ++e) top = fmaxf(top, c[u][e]);
             top = mrf_halves_max(top);
-            if constexpr (!BIAS) top *= P.c;
-            top = fmaxf(m, top);
+            top = fmaxf(m, fmaf(top, times, plus));
             const float base = top == -INFINITY ? 0.0f : top;
             if (__any(top > m + MRF_ATTN_RISE)) {
                 const float less = __builtin_amdgcn_exp2f(m - base);
@@ -147,19 +155,19 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
                     for (int e = 0; e < 16; ++e) o[d][e] *= less;
                 m = top;
             }
-            const float low = (m == -INFINITY ? 0.0f : m) - mrf_attn_shift_forward<T>();
+            const float low = (m == -INFINITY ? 0.0f : m) - mrf_attn_shift_forward<T>() - plus;
             // 16 keys at a time: their probabilities, and their values on the way, while those before are multiplied
             frag vf[2][DP / 32], p[2];
             const auto part = [&](int y) {
                 mrf_acc &x = c[y / 2];
 #pragma unroll
                 for (int e = 8 * (y % 2); e < 8 * (y % 2) + 8; ++e) {
-                    x[e] = __builtin_amdgcn_exp2f(BIAS ? x[e] - low : fmaf(x[e], P.c, -low));
+                    x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], times, -low));
                     l += x[e];
                 }
                 p[y % 2] = mrf_acc_frag<T>(x, y % 2);
 #pragma unroll
-                for (int d = 0; d < DP / 32; ++d) vf[y % 2][d] = Rows::across(ldsV[buf], 16 * y, 32 * d);
+                for (int d = 0; d < DP / 32; ++d) vf[y % 2][d] = places.across(lds[0][1] + 16 * y * Rows::LD, d);
             };
             part(0);
             __builtin_amdgcn_sched_barrier(0);
@@ -172,6 +180,7 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
             }
         }
         if (t + 1 < t1) store(buf ^ 1);
+        places.move(buf ? -2 * TILE : 2 * TILE);
         __syncthreads();
     }
 

@@ -15,14 +15,20 @@ template <class T> constexpr int mrf_attn_bwd_rows() { return sizeof(T) == 4 ? 3
 
 template <class F> struct MrfTwo { F a, b; };
 
+// steps whose operands are read ahead together
+template <class T, int DP> constexpr int mrf_attn_group() { return sizeof(T) == 4 ? 1 : DP == 128 ? 4 : 2; }
+
 // ---- dq, and delta
 template <class T, int DP, bool BIAS> __global__ void __launch_bounds__(256) mrf_attn_bwd_queries(const MrfAttnParams P)
 {
     constexpr int KT = mrf_attn_bwd_rows<T>(), NT = 256, ROWS = 128, LINE = ROWS + KT;
     typedef MrfRows<T, DP, KT, NT> Rows;
     typedef typename MrfFrag<T>::type frag;
-    __shared__ __align__(16) T ldsK[2][KT * Rows::LD], ldsV[2][KT * Rows::LD];
-    __shared__ float line[2][BIAS ? LINE : 1];
+    constexpr int TILE = KT * Rows::LD, U = KT / 32, STEPS = DP / 16;
+    __shared__ __align__(16) T lds[2][2][TILE];      // keys, values
+    __shared__ MrfLine<BIAS ? LINE : 1> line;
+    MrfPlaces<T, DP, Rows::LD> places;
+    places.template init<Rows>();
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5;
     // (the longest rows of causal ones first)
     const int blocks = (P.Q + ROWS - 1) / ROWS, bh = blockIdx.x % (P.B * P.Hq), block = blocks - 1 - (int)(blockIdx.x / (P.B * P.Hq));
@@ -57,18 +63,16 @@ template <class T, int DP, bool BIAS> __global__ void __launch_bounds__(256) mrf
     const int t0 = s.from(r0) / KT, t1 = r0 <= i1 ? (s.to(i1) + KT - 1) / KT : 0;
     const T *k = (const T *)P.k + b * P.ks[0] + hk * P.ks[2], *v = (const T *)P.v + b * P.vs[0] + hk * P.vs[2];
     Rows kr, vr;
-    float bias_next = 0.0f;
+    typename decltype(line)::Next bias_next = {};
     const auto load = [&](int t) {
         kr.load(k + (long long)t * KT * P.ks[1], P.ks[1], s.nk - t * KT, P.D);
         vr.load(v + (long long)t * KT * P.vs[1], P.vs[1], s.nk - t * KT, P.D);
-        if constexpr (BIAS)
-            if ((int)threadIdx.x < LINE) bias_next = mrf_attn_bias(P, s, h, (long long)t * KT - r0 - (ROWS - 1) + (int)threadIdx.x);
+        if constexpr (BIAS) line.fetch(P, s, h, (long long)t * KT - r0 - (ROWS - 1), bias_next);
     };
     const auto store = [&](int buf) {
-        kr.store(ldsK[buf]);
-        vr.store(ldsV[buf]);
-        if constexpr (BIAS)
-            if ((int)threadIdx.x < LINE) line[buf][threadIdx.x] = bias_next;
+        kr.store(lds[buf][0]);
+        vr.store(lds[buf][1]);
+        if constexpr (BIAS) line.put(buf, bias_next);
     };
     constexpr bool MEAN = sizeof(T) == 2;
     mrf_acc dq[DP / 32], mean[MEAN ? DP / 32 : 1];      // sums of dS k, and of P k
@@ -90,24 +94,27 @@ template <class T, int DP, bool BIAS> __global__ void __launch_bounds__(256) mrf
         if (w0 <= w1 && k0 < s.to(w1) && k0 + KT > s.from(w0)) {
             const bool whole = k0 >= w1 + s.lo && k0 + KT - 1 <= w0 + s.hi && k0 + KT <= s.nk;
             const int from = i + s.lo - k0, to = min(i + s.hi + 1, s.nk) - k0;
+            const bool flat = !BIAS || line.flat(buf);
+            const float times = flat ? P.c : 1.0f, less = BIAS && flat ? lse - line.value[buf][0] : lse;
 #pragma unroll 1
-            for (int u = 0; u < KT / 32; ++u) {
+            for (int u = 0; u < U; ++u) {
+                const T *const at = lds[0][0] + 32 * u * Rows::LD;
                 mrf_acc c, dp;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) c[e] = dp[e] = 0.0f;
-                mrf_ahead<DP / 16, (sizeof(T) == 4 ? 1 : DP == 128 ? 4 : 2)>([&](int d) { return MrfTwo<frag>{Rows::along(ldsK[buf], 32 * u, 16 * d), Rows::along(ldsV[buf], 32 * u, 16 * d)}; },
-                                      [&](int d, const MrfTwo<frag> &f) {
-                                          c = mrf_mma(f.a, qf[d], c);
-                                          dp = mrf_mma(f.b, gf[d], dp);
-                                      });
+                mrf_ahead<STEPS, mrf_attn_group<T, DP>()>([&](int n) { return MrfTwo<frag>{places.along(at, n), places.along(at + TILE, n)}; },
+                                                          [&](int n, const MrfTwo<frag> &f) {
+                                                              c = mrf_mma(f.a, qf[n], c);
+                                                              dp = mrf_mma(f.b, gf[n], dp);
+                                                          });
+                if (BIAS && !flat) {
+                    mrf_stay_branch();
+                    const float *const values = line.value[buf] + ROWS - 1 - (wv * 32 + (lane & 31)) + 32 * u;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int j = 32 * u + mrf_acc_row(e, half);
-                    float x;
-                    if constexpr (BIAS) x = fmaf(c[e], P.c, line[buf][ROWS - 1 + j - (wv * 32 + (lane & 31))]) - lse;
-                    else x = fmaf(c[e], P.c, -lse);
-                    c[e] = __builtin_amdgcn_exp2f(x);
+                    for (int e = 0; e < 16; ++e) c[e] = fmaf(c[e], P.c, values[mrf_acc_row(e, half)]);
                 }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) c[e] = __builtin_amdgcn_exp2f(fmaf(c[e], times, -less));
                 if (!whole) {
                     mrf_stay_branch();
 #pragma unroll
@@ -123,15 +130,16 @@ template <class T, int DP, bool BIAS> __global__ void __launch_bounds__(256) mrf
                 }
                 range.fit(dp, dq);
                 const frag sf[2] = {mrf_acc_frag<T>(dp, 0), mrf_acc_frag<T>(dp, 1)}, pf[2] = {mrf_acc_frag<T>(c, 0), mrf_acc_frag<T>(c, 1)};
-                mrf_ahead<DP / 16, (sizeof(T) == 4 ? 1 : DP == 128 ? 4 : 2)>([&](int n) { return Rows::across(ldsK[buf], 32 * u + 16 * (n / (DP / 32)), n % (DP / 32) * 32); },
-                                      [&](int n, const frag &f) {
-                                          const int x = n / (DP / 32), d = n % (DP / 32);
-                                          dq[d] = mrf_mma(f, sf[x], dq[d]);
-                                          if constexpr (MEAN) mean[d] = mrf_mma(f, pf[x], mean[d]);
-                                      });
+                mrf_ahead<STEPS, mrf_attn_group<T, DP>()>([&](int n) { return places.across(at + 16 * (n / (DP / 32)) * Rows::LD, n % (DP / 32)); },
+                                                          [&](int n, const frag &f) {
+                                                              const int x = n / (DP / 32), d = n % (DP / 32);
+                                                              dq[d] = mrf_mma(f, sf[x], dq[d]);
+                                                              if constexpr (MEAN) mean[MEAN ? d : 0] = mrf_mma(f, pf[x], mean[MEAN ? d : 0]);
+                                                          });
             }
         }
         if (t + 1 < t1) store(buf ^ 1);
+        places.move(buf ? -2 * TILE : 2 * TILE);
         __syncthreads();
     }
     left = mrf_halves_sum(left) * mrf_attn_unshift<T>();
@@ -173,15 +181,18 @@ template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV> __global__ v
     constexpr int QT = mrf_attn_bwd_rows<T>(), NT = 256, KEYS = 128, LINE = KEYS + QT;
     typedef MrfRows<T, DP, QT, NT> Rows;
     typedef typename MrfFrag<T>::type frag;
-    __shared__ __align__(16) T ldsQ[2][QT * Rows::LD], ldsG[2][QT * Rows::LD];
+    constexpr int TILE = QT * Rows::LD, U = QT / 32, STEPS = DP / 16;
+    __shared__ __align__(16) T lds[2][2][TILE];      // queries, gradients of the outputs
     __shared__ __align__(16) float ldsL[2][QT], ldsD[2][QT];
-    __shared__ float line[2][BIAS ? LINE : 1];
+    __shared__ MrfLine<BIAS ? LINE : 1> line;
     __shared__ float skew[TABLE ? 4 : 1][TABLE ? 32 * MRF_SKEW : 1];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5;
     // (the keys that most queries see first; part blockIdx.y of the heads that share them)
     const int bh = blockIdx.x % (P.B * P.Hk), block = (int)(blockIdx.x / (P.B * P.Hk)), group = P.G / P.shares;
     const int b = bh / P.Hk, hk = bh % P.Hk;
     const MrfAttnBatch s(P, b);
+    MrfPlaces<T, DP, Rows::LD> places;
+    places.template init<Rows>();
     const int k0 = block * KEYS, j = k0 + wv * 32 + (lane & 31), w0 = k0 + wv * 32, w1 = min(w0 + 31, s.nk - 1);
     int t0, t1;
     mrf_attn_query_tiles<QT>(s, k0, t0, t1);
@@ -206,7 +217,9 @@ template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV> __global__ v
 
     MrfRange<T> range;
     Rows qr, gr;
-    float lse_next = 0.0f, delta_next = 0.0f, bias_next = 0.0f;
+    float lse_next = 0.0f, delta_next = 0.0f;
+    typename decltype(line)::Next bias_next = {};
+    int now = 0;      // which of the two tiles `places` are in
     for (int g = 0; g < group; ++g) {
         const int h = hk * P.G + blockIdx.y * group + g;
         const T *q = (const T *)P.q + b * P.qs[0] + h * P.qs[2], *go = (const T *)P.dout + ((long long)b * P.Q * P.Hq + h) * P.D;
@@ -220,50 +233,58 @@ template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV> __global__ v
                 lse_next = lse_next == -INFINITY ? INFINITY : lse_next - mrf_attn_shift<T>();
                 delta_next = i < s.nq ? P.delta[stat + i] : 0.0f;
             }
-            if constexpr (BIAS)
-                if ((int)threadIdx.x < LINE) bias_next = mrf_attn_bias(P, s, h, (long long)k0 - t * QT - (QT - 1) + (int)threadIdx.x);
+            if constexpr (BIAS) line.fetch(P, s, h, (long long)k0 - t * QT - (QT - 1), bias_next);
         };
         const auto store = [&](int buf) {
-            qr.store(ldsQ[buf]);
-            gr.store(ldsG[buf]);
+            qr.store(lds[buf][0]);
+            gr.store(lds[buf][1]);
             if ((int)threadIdx.x < QT) {
                 ldsL[buf][threadIdx.x] = lse_next;
                 ldsD[buf][threadIdx.x] = delta_next;
             }
-            if constexpr (BIAS)
-                if ((int)threadIdx.x < LINE) line[buf][threadIdx.x] = bias_next;
+            if constexpr (BIAS) line.put(buf, bias_next);
         };
         float *const to_line = TABLE ? P.lines + (((size_t)b * P.Hq + h) * P.strips + block * 4 + wv) * P.line : nullptr;
         float goes_on = 0.0f;
         if (t0 < t1) {
             load(t0);
-            store(0);
+            store(now);
         }
         __syncthreads();
         for (int t = t0; t < t1; ++t) {
-            const int buf = (t - t0) & 1, q0 = t * QT;
+            const int buf = now, q0 = t * QT;
             if (t + 1 < t1) load(t + 1);
             const int q1 = min(q0 + QT, s.nq) - 1;
             const bool any = w0 <= w1 && q1 + s.hi >= w0 && q0 + s.lo <= w1;
             const bool whole = any && w0 >= q1 + s.lo && w0 + 31 <= q0 + s.hi && q0 + QT <= s.nq && w0 + 32 <= s.nk;
             // queries that may see this lane's key: [from, to) of the tile
             const int from = j - s.hi - q0, to = j < s.nk ? min(j - s.lo + 1, s.nq) - q0 : 0;
+            const bool flat = !BIAS || line.flat(buf);
+            const float times = flat ? P.c : 1.0f, level = BIAS && flat ? line.value[buf][0] : 0.0f;
 #pragma unroll 1
-            for (int u = 0; u < QT / 32; ++u) {
+            for (int u = 0; u < U; ++u) {
+                float sum = goes_on;
                 if (any) {
+                    const T *const at = lds[0][0] + 32 * u * Rows::LD;
                     mrf_acc c, dp;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) c[e] = dp[e] = 0.0f;
-                    mrf_ahead<DP / 16, (sizeof(T) == 4 ? 1 : DP == 128 ? 4 : 2)>(
-                        [&](int d) {
-                            MrfTwo<frag> f = {Rows::along(ldsQ[buf], 32 * u, 16 * d), {}};
-                            if constexpr (DK) f.b = Rows::along(ldsG[buf], 32 * u, 16 * d);
+                    mrf_ahead<STEPS, mrf_attn_group<T, DP>()>(
+                        [&](int n) {
+                            MrfTwo<frag> f = {places.along(at, n), {}};
+                            if constexpr (DK) f.b = places.along(at + TILE, n);
                             return f;
                         },
-                        [&](int d, const MrfTwo<frag> &f) {
-                            c = mrf_mma(f.a, kf[d], c);
-                            if constexpr (DK) dp = mrf_mma(f.b, vf[DK ? d : 0], dp);
+                        [&](int n, const MrfTwo<frag> &f) {
+                            c = mrf_mma(f.a, kf[n], c);
+                            if constexpr (DK) dp = mrf_mma(f.b, vf[DK ? n : 0], dp);
                         });
+                    if (BIAS && !flat) {
+                        mrf_stay_branch();
+                        const float *const values = line.value[buf] + QT - 1 + (wv * 32 + (lane & 31)) - 32 * u;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) c[e] = fmaf(c[e], P.c, values[-mrf_acc_row(e, half)]);
+                    }
 #pragma unroll
                     for (int e4 = 0; e4 < 16; e4 += 4) {
                         const int r4 = 32 * u + mrf_acc_row(e4, half);
@@ -271,12 +292,8 @@ template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV> __global__ v
                         const float lse[4] = {L.x, L.y, L.z, L.w}, delta[4] = {D.x, D.y, D.z, D.w};
 #pragma unroll
                         for (int n = 0; n < 4; ++n) {
-                            const int e = e4 + n, r = r4 + n;
-                            float x;
-                            if constexpr (BIAS) x = fmaf(c[e], P.c, line[buf][QT - 1 + (wv * 32 + (lane & 31)) - r]) - lse[n];
-                            else x = fmaf(c[e], P.c, -lse[n]);
-                            c[e] = __builtin_amdgcn_exp2f(x);
-                            dp[e] -= delta[n];
+                            c[e4 + n] = __builtin_amdgcn_exp2f(fmaf(c[e4 + n], times, BIAS ? level - lse[n] : -lse[n]));
+                            dp[e4 + n] -= delta[n];
                         }
                     }
                     if (!whole) {
@@ -290,10 +307,27 @@ template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV> __global__ v
 #pragma unroll
                     for (int e = 0; e < 16; ++e) dp[e] *= c[e];
                     if constexpr (TABLE) {
+                        // Where all offsets of the tile have a bucket, and all its pairs count, it does not matter on which of its diagonals they are.
+                        if (flat && whole) {
+                            float mine = 0.0f;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const int r = mrf_acc_row(e, half);
-                            skew[wv][r * MRF_SKEW + r - (lane & 31) + 31] = dp[e];
+                            for (int e = 0; e < 16; ++e) mine += dp[e];
+                            mine = mrf_halves_sum(mine);
+                            sum += half == 0 ? mine : 0.0f;
+                        } else {
+                            mrf_stay_branch();
+                            float *const skewed = skew[TABLE ? wv : 0];
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                const int r = mrf_acc_row(e, half);
+                                skewed[r * MRF_SKEW + r - (lane & 31) + 31] = dp[e];
+                            }
+                            mrf_wave_lds_fence();
+                            float part[4] = {};
+#pragma unroll
+                            for (int r = 0; r < 32; ++r) part[r % 4] += skewed[r * MRF_SKEW + lane];
+                            sum += (part[0] + part[1]) + (part[2] + part[3]);
+                            mrf_wave_lds_fence();
                         }
                     }
                     frag pf[2], sf[2];
@@ -302,12 +336,12 @@ template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV> __global__ v
                         sf[0] = mrf_acc_frag<T>(dp, 0), sf[1] = mrf_acc_frag<T>(dp, 1);
                     }
                     if constexpr (DV) pf[0] = mrf_acc_frag<T>(c, 0), pf[1] = mrf_acc_frag<T>(c, 1);
-                    mrf_ahead<DP / 16, (sizeof(T) == 4 ? 1 : DP == 128 ? 4 : 2)>(
+                    mrf_ahead<STEPS, mrf_attn_group<T, DP>()>(
                         [&](int n) {
-                            const int row = 32 * u + 16 * (n / (DP / 32)), at = n % (DP / 32) * 32;
+                            const T *const row = at + 16 * (n / (DP / 32)) * Rows::LD;
                             MrfTwo<frag> f = {};
-                            if constexpr (DV) f.a = Rows::across(ldsG[buf], row, at);
-                            if constexpr (DK) f.b = Rows::across(ldsQ[buf], row, at);
+                            if constexpr (DV) f.a = places.across(row + TILE, n % (DP / 32));
+                            if constexpr (DK) f.b = places.across(row, n % (DP / 32));
                             return f;
                         },
                         [&](int n, const MrfTwo<frag> &f) {
@@ -317,19 +351,16 @@ template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV> __global__ v
                         });
                 }
                 if constexpr (TABLE) {
-                    float sum = goes_on;
-                    if (any) {
-                        mrf_wave_lds_fence();
-#pragma unroll 8
-                        for (int r = 0; r < 32; ++r) sum += skew[wv][r * MRF_SKEW + lane];
-                        mrf_wave_lds_fence();
-                    }
                     if (half == 0) to_line[q0 + 32 * u + lane] = sum * mrf_attn_unshift<T>();
                     goes_on = __shfl(sum, lane | 32);
                     if (half) goes_on = 0.0f;
                 }
             }
-            if (t + 1 < t1) store(buf ^ 1);
+            if (t + 1 < t1) {
+                store(buf ^ 1);
+                now ^= 1;
+                places.move(now ? 2 * TILE : -2 * TILE);
+            }
             __syncthreads();
         }
         if constexpr (TABLE)
