@@ -168,19 +168,27 @@ __device__ inline float mrf_attn_bias(const MrfAttnParams &P, const MrfAttnBatch
 }
 
 // The bias along a tile: its values at N offsets in a row, and whether these are all of one bucket -- as most are, far from the queries: then there is nothing to look up
-// for each pair.  Threads 0 .. N - 1 fetch, then put; all may ask behind the next barrier.
+// for each pair.  Threads 0 .. N - 1 fetch, then put; all may ask behind the next barrier.  The buckets of a tile are fetched a tile before its values, which would otherwise
+// wait for them.
 template <int N> struct MrfLine {
     static constexpr int WAVES = (N + 63) / 64;
     float value[2][N];
     int same[2][WAVES];
-    struct Next { float value; int same; };
-    __device__ inline void fetch(const MrfAttnParams &P, const MrfAttnBatch &s, int h, long long first, Next &n) const
+    struct Next { int bucket; float value; int same; };
+    // buckets of the offsets from `first` on
+    __device__ inline void ahead(const MrfAttnParams &P, const MrfAttnBatch &s, long long first, Next &n) const
+    {
+        if ((int)threadIdx.x < N) n.bucket = mrf_attn_bucket(P, s, first + (int)threadIdx.x);
+    }
+    // values of those, and buckets of the offsets from `following` on
+    __device__ inline void fetch(const MrfAttnParams &P, const MrfAttnBatch &s, int h, long long following, Next &n) const
     {
         if ((int)threadIdx.x < N) {
-            const int b = mrf_attn_bucket(P, s, first + (int)threadIdx.x), other = __builtin_amdgcn_readfirstlane(b);
-            n.value = mrf_attn_level(P, h, b);
-            n.same = __any(b != other) ? -1 : other;
+            const int other = __builtin_amdgcn_readfirstlane(n.bucket);
+            n.value = mrf_attn_level(P, h, n.bucket);
+            n.same = __any(n.bucket != other) ? -1 : other;
         }
+        ahead(P, s, following, n);
     }
     __device__ inline void put(int buf, const Next &n)
     {

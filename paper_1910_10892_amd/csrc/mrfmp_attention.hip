@@ -68,7 +68,7 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
     const auto load = [&](int t) {
         kr.load(k + (long long)t * KT * P.ks[1], P.ks[1], s.nk - t * KT, P.D);
         vr.load(v + (long long)t * KT * P.vs[1], P.vs[1], s.nk - t * KT, P.D);
-        if constexpr (BIAS && !PACK) line.fetch(P, s, h0, (long long)t * KT - r0 - (ROWS - 1), bias_next);
+        if constexpr (BIAS && !PACK) line.fetch(P, s, h0, (long long)(t + 1) * KT - r0 - (ROWS - 1), bias_next);
     };
     const auto store = [&](int buf) {
         kr.store(lds[buf][0]);
@@ -88,6 +88,7 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
     float m = -INFINITY, l = 0.0f;      // maximum so far (in units of log2), and this lane's part of the sum
 
     if (t0 < t1) {
+        if constexpr (BIAS && !PACK) line.ahead(P, s, (long long)t0 * KT - r0 - (ROWS - 1), bias_next);
         load(t0);
         store(0);
     }

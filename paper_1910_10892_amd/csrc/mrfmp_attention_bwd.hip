@@ -67,7 +67,7 @@ template <class T, int DP, bool BIAS> __global__ void __launch_bounds__(256) mrf
     const auto load = [&](int t) {
         kr.load(k + (long long)t * KT * P.ks[1], P.ks[1], s.nk - t * KT, P.D);
         vr.load(v + (long long)t * KT * P.vs[1], P.vs[1], s.nk - t * KT, P.D);
-        if constexpr (BIAS) line.fetch(P, s, h, (long long)t * KT - r0 - (ROWS - 1), bias_next);
+        if constexpr (BIAS) line.fetch(P, s, h, (long long)(t + 1) * KT - r0 - (ROWS - 1), bias_next);
     };
     const auto store = [&](int buf) {
         kr.store(lds[buf][0]);
@@ -84,6 +84,7 @@ template <class T, int DP, bool BIAS> __global__ void __launch_bounds__(256) mrf
     float left = 0.0f;      // sum of dS
 
     if (t0 < t1) {
+        if constexpr (BIAS) line.ahead(P, s, (long long)t0 * KT - r0 - (ROWS - 1), bias_next);
         load(t0);
         store(0);
     }
@@ -233,7 +234,7 @@ template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV> __global__ v
                 lse_next = lse_next == -INFINITY ? INFINITY : lse_next - mrf_attn_shift<T>();
                 delta_next = i < s.nq ? P.delta[stat + i] : 0.0f;
             }
-            if constexpr (BIAS) line.fetch(P, s, h, (long long)k0 - t * QT - (QT - 1), bias_next);
+            if constexpr (BIAS) line.fetch(P, s, h, (long long)k0 - (long long)(t + 1) * QT - (QT - 1), bias_next);
         };
         const auto store = [&](int buf) {
             qr.store(lds[buf][0]);
@@ -247,6 +248,7 @@ template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV> __global__ v
         float *const to_line = TABLE ? P.lines + (((size_t)b * P.Hq + h) * P.strips + block * 4 + wv) * P.line : nullptr;
         float goes_on = 0.0f;
         if (t0 < t1) {
+            if constexpr (BIAS) line.ahead(P, s, (long long)k0 - (long long)t0 * QT - (QT - 1), bias_next);
             load(t0);
             store(now);
         }
