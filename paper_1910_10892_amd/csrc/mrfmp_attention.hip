@@ -260,6 +260,43 @@ template <class T> __global__ void __launch_bounds__(256) mrf_attn_join(const Mr
     if (tid == 0 && P.lse) P.lse[at] = l == 0.0f ? -INFINITY : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
 }
 
+// The same for few parts of many queries: a wavefront has a query of a head, a lane two entries.
+constexpr int MRF_ATTN_FEW = 8;
+template <class T> __global__ void __launch_bounds__(256) mrf_attn_join_few(const MrfAttnParams P)
+{
+    const long long n = (long long)P.B * P.Hq * P.Q, at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (at >= n) return;
+    const int lane = threadIdx.x & 63, d0 = lane < P.D ? lane : 0, d1 = lane + 64 < P.D ? lane + 64 : 0;
+    const float2 *const ends = (const float2 *)P.part;
+    const float *const part = P.part + 2 * P.splits * n + at * P.D;
+    float2 end[MRF_ATTN_FEW];
+    float x[MRF_ATTN_FEW], y[MRF_ATTN_FEW], top = -INFINITY, l = 0.0f, sx = 0.0f, sy = 0.0f;
+#pragma unroll
+    for (int s = 0; s < MRF_ATTN_FEW; ++s) {
+        const int t = s < P.splits ? s : 0;
+        end[s] = ends[t * n + at];
+        x[s] = part[t * n * P.D + d0];
+        y[s] = part[t * n * P.D + d1];
+    }
+#pragma unroll
+    for (int s = 0; s < MRF_ATTN_FEW; ++s) top = fmaxf(top, end[s].x);
+    const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+    for (int s = 0; s < MRF_ATTN_FEW; ++s)
+        if (s < P.splits) {
+            const float w = __builtin_amdgcn_exp2f(end[s].x - base);
+            l = fmaf(end[s].y, w, l);
+            sx = fmaf(x[s], w, sx);
+            sy = fmaf(y[s], w, sy);
+        }
+    const float inv = l > 0.0f ? 1.0f / l : l;
+    const long long bh = at / P.Q, i = at - bh * P.Q, b = bh / P.Hq, h = bh - b * P.Hq;
+    T *const out = (T *)P.out + ((b * P.Q + i) * P.Hq + h) * P.D;
+    if (lane < P.D) out[lane] = mrf_from_f32<T>(sx * inv);
+    if (lane + 64 < P.D) out[lane + 64] = mrf_from_f32<T>(sy * inv);
+    if (lane == 0 && P.lse) P.lse[at] = l == 0.0f ? -INFINITY : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+}
+
 namespace mrf_host {
 
 template <class T, int DP> static int attention_go(const MrfAttnParams &P, const AttnPlan &plan, hipStream_t st)
@@ -273,7 +310,9 @@ template <class T, int DP> static int attention_go(const MrfAttnParams &P, const
         if (P.table) mrf_attn_fwd<T, DP, NW, false, true><<<grid, 64 * NW, 0, st>>>(P);
         else mrf_attn_fwd<T, DP, NW, false, false><<<grid, 64 * NW, 0, st>>>(P);
     }
-    if (P.splits > 1) mrf_attn_join<T><<<(unsigned)((long long)P.B * P.Hq * P.Q), 256, 0, st>>>(P);
+    const long long queries = (long long)P.B * P.Hq * P.Q;
+    if (P.splits > MRF_ATTN_FEW) mrf_attn_join<T><<<(unsigned)queries, 256, 0, st>>>(P);
+    else if (P.splits > 1) mrf_attn_join_few<T><<<(unsigned)((queries + 3) / 4), 256, 0, st>>>(P);
     return launch_status("mrf_attn_fwd");
 }
 
@@ -326,9 +365,9 @@ static AttnPlan attention_plan(const MrfAttnParams &P, int type)
     const int block = type != MRF_F32 && P.D > 64 ? 256 : 128;      // (as mrf_attn_wide has it)
     const bool pack = P.Q <= 16 || rows <= 64;
     const long long groups = pack ? (long long)P.B * P.Hk * ((rows + 31) / 32) : (long long)P.B * P.Hq * ((P.Q + block - 1) / block);
-    // parts of the keys: for eight wavefronts of few rows on a compute unit, or two workgroups of many; of four tiles at least
+    // parts of the keys: for eight wavefronts of few rows on a compute unit, or a workgroup of many; of four tiles at least
     const long long tiles = ((long long)P.K + 31) / 32 / (pack ? 1 : 2);
-    long long splits = groups ? (pack ? 2048 : 512) / groups : 1;
+    long long splits = groups ? (pack ? 2048 : 256) / groups : 1;
     if (splits > tiles / 4) splits = tiles / 4;
     if (splits > MRF_ATTN_SPLITS) splits = MRF_ATTN_SPLITS;
     return {pack, (int)(splits < 1 ? 1 : splits), (unsigned)groups};

@@ -177,7 +177,8 @@ template <int QT> __device__ inline void mrf_attn_query_tiles(const MrfAttnBatch
 constexpr int MRF_SKEW = 71;      // from row to row: the halves of a wavefront, four rows apart, fall on the two halves of the banks
 
 // DK, DV: which of the two it sums.  Both, where their sums and the keys and values fit into the registers, else one launch for each.
-template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV> __global__ void __launch_bounds__(256) mrf_attn_bwd_keys(const MrfAttnParams P)
+template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV>
+__global__ void __launch_bounds__(256, (sizeof(T) == 2 && DP <= 64 ? 2 : 1)) mrf_attn_bwd_keys(const MrfAttnParams P)
 {
     constexpr int QT = mrf_attn_bwd_rows<T>(), NT = 256, KEYS = 128, LINE = KEYS + QT;
     typedef MrfRows<T, DP, QT, NT> Rows;
