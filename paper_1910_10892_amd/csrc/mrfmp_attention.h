@@ -44,11 +44,25 @@ template <class T> __device__ inline typename MrfFrag<T>::type mrf_acc_frag(cons
 template <int PER, class T> __device__ inline void mrf_load_part(const T *row, int d, int D, bool there, T (&v)[PER])
 {
     typedef T vec __attribute__((ext_vector_type(PER), aligned(sizeof(T))));
+    constexpr int WORDS = PER * (int)sizeof(T) / 4;
     if (D % PER == 0) {
         there = there && d < D;
         const vec x = *(const vec *)(row + (d < D ? d : 0));
+        unsigned w[WORDS];
+        __builtin_memcpy(w, &x, sizeof(w));
 #pragma unroll
-        for (int j = 0; j < PER; ++j) v[j] = there ? x[j] : (T)0.0f;
+        for (int j = 0; j < WORDS; ++j) w[j] = there ? w[j] : 0u;
+        __builtin_memcpy(v, w, sizeof(w));
+    } else if (D % (PER / 2) == 0) {      // halves of that
+        typedef T hvec __attribute__((ext_vector_type(PER / 2), aligned(sizeof(T))));
+        const bool first = there && d < D, second = there && d + PER / 2 < D;
+        const hvec x = *(const hvec *)(row + (d < D ? d : 0)), y = *(const hvec *)(row + (d + PER / 2 < D ? d + PER / 2 : 0));
+        unsigned w[WORDS];
+        __builtin_memcpy(w, &x, sizeof(w) / 2);
+        __builtin_memcpy(w + WORDS / 2, &y, sizeof(w) / 2);
+#pragma unroll
+        for (int j = 0; j < WORDS; ++j) w[j] = (j < WORDS / 2 ? first : second) ? w[j] : 0u;
+        __builtin_memcpy(v, w, sizeof(w));
     } else {
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
@@ -229,17 +243,34 @@ template <class T, int DP, int ROWS, int NT> struct MrfRows {
         else return row * LD + (chunk ^ swap(row)) * PER;
     }
 
-    // rows from `at` on, `rows` (1 at least) of them; of a row D entries; the others are 0
+    int there;      // rows that there are, or -1 where all of the tile is as it was loaded
+    int entries;
+
+    // rows from `at` on, `rows` (1 at least) of them; of a row D entries; the others are 0.  (Whole chunks that are not there are read from elsewhere in the tensor,
+    // and put right only when they are stored: nothing waits for a load before that.)
     __device__ inline void load(const T *at, long long stride, int rows, int D)
     {
         static_assert(CHUNKS % NT == 0, "chunks of a tile");
-        if (rows >= ROWS && D == DP) {
+        there = -1;
+        entries = D;
+        if (D % (PER / 2) == 0 && (rows < ROWS || D < DP)) there = rows;
+        if (D % PER == 0) {
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 const int c = (int)threadIdx.x + n * NT, row = c / (DP / PER), d = c % (DP / PER) * PER;
-                const uvec u = *(const uvec *)(at + row * stride + d);
+                const uvec u = *(const uvec *)(at + min(row, rows - 1) * stride + (d < D ? d : 0));
 #pragma unroll
                 for (int j = 0; j < PER; ++j) r[n][j] = u[j];
+            }
+        } else if (D % (PER / 2) == 0) {      // by halves
+            typedef T hvec __attribute__((ext_vector_type(PER / 2), aligned(sizeof(T))));
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int c = (int)threadIdx.x + n * NT, row = c / (DP / PER), d = c % (DP / PER) * PER;
+                const T *const p = at + min(row, rows - 1) * stride;
+                const hvec u = *(const hvec *)(p + (d < D ? d : 0)), v = *(const hvec *)(p + (d + PER / 2 < D ? d + PER / 2 : 0));
+#pragma unroll
+                for (int j = 0; j < PER / 2; ++j) r[n][j] = u[j], r[n][PER / 2 + j] = v[j];
             }
         } else {
 #pragma unroll
@@ -252,8 +283,21 @@ template <class T, int DP, int ROWS, int NT> struct MrfRows {
             }
         }
     }
-    __device__ inline void store(T *lds) const
+    __device__ inline void store(T *lds)
     {
+        if (there >= 0) {
+            mrf_stay_branch();
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int c = (int)threadIdx.x + n * NT, row = c / (DP / PER), d = c % (DP / PER) * PER;
+                const bool first = row < there && d < entries, second = row < there && d + PER / 2 < entries;
+                unsigned w[4];
+                __builtin_memcpy(w, &r[n], 16);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = (j < 2 ? first : second) ? w[j] : 0u;
+                __builtin_memcpy(&r[n], w, 16);
+            }
+        }
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int c = (int)threadIdx.x + n * NT, row = c / (DP / PER), d = c % (DP / PER) * PER;

@@ -34,6 +34,10 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
     constexpr int TILE = KT * Rows::LD;
     __shared__ __align__(16) T lds[2][2][TILE];      // keys, values
     __shared__ MrfLine<BIAS && !PACK ? LINE : 1> line;
+    // few queries, of several heads: the buckets at a tile's offsets, and the values of the group's heads where there is room for them
+    constexpr int LEVELS = 512;
+    __shared__ int ids[2][PACK && BIAS ? NW : 1][64];
+    __shared__ float levels[PACK && BIAS ? LEVELS : 1];
     MrfPlaces<T, DP, Rows::LD> places;
     places.template init<Rows>();
     const int lane = threadIdx.x & 63, wv = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5;
@@ -69,11 +73,13 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
         kr.load(k + (long long)t * KT * P.ks[1], P.ks[1], s.nk - t * KT, P.D);
         vr.load(v + (long long)t * KT * P.vs[1], P.vs[1], s.nk - t * KT, P.D);
         if constexpr (BIAS && !PACK) line.fetch(P, s, h0, (long long)(t + 1) * KT - r0 - (ROWS - 1), bias_next);
+        if constexpr (BIAS && PACK) bias_next.bucket = mrf_attn_bucket(P, s, (long long)t * KT - w2 + lane);
     };
     const auto store = [&](int buf) {
         kr.store(lds[buf][0]);
         vr.store(lds[buf][1]);
         if constexpr (BIAS && !PACK) line.put(buf, bias_next);
+        if constexpr (BIAS && PACK) ids[buf][wv][lane] = bias_next.bucket;
     };
 
     // Of two wavefronts on a SIMD one goes first: it multiplies while the other takes exponentials, instead of both doing the same at a time.
@@ -87,6 +93,11 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
         for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
     float m = -INFINITY, l = 0.0f;      // maximum so far (in units of log2), and this lane's part of the sum
 
+    const bool room = BIAS && PACK && (long long)P.G * P.n_buckets <= LEVELS;
+    if constexpr (BIAS && PACK) {
+        if (room)
+            for (int n = lane; n < P.G * P.n_buckets; n += 64) levels[n] = mrf_attn_level(P, hk * P.G + n / P.n_buckets, n % P.n_buckets);
+    }
     if (t0 < t1) {
         if constexpr (BIAS && !PACK) line.ahead(P, s, (long long)t0 * KT - r0 - (ROWS - 1), bias_next);
         load(t0);
@@ -112,11 +123,22 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
             // (without a bias, or with the same for all, the scores stay products, whose maximum is the scores' too, and the rest goes in with the maximum: one operation)
             float top = -INFINITY, times = P.c, plus = 0.0f;
             if constexpr (BIAS && PACK) {
-                times = 1.0f;
+                // (keys of the tile less queries of the wavefront are 63 offsets at most, from k0 - w2 on)
+                const auto level = [&](int id) { return room ? levels[row % P.G * P.n_buckets + id] : mrf_attn_level(P, h, id); };
+                const int id = ids[buf][wv][lane], other = __builtin_amdgcn_readfirstlane(id);
+                if (!__any(id != other)) {
+                    plus = level(other);
+                } else {
+                    mrf_stay_branch();
+                    times = 1.0f;
 #pragma unroll
-                for (int u = 0; u < KT / 32; ++u)
+                    for (int u = 0; u < KT / 32; ++u)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) c[u][e] = fmaf(c[u][e], P.c, mrf_attn_bias(P, s, h, (long long)k0 + 32 * u + mrf_acc_row(e, half) - i));
+                        for (int e = 0; e < 16; ++e) {
+                            const int at = 32 * u + mrf_acc_row(e, half) - i + w2;
+                            c[u][e] = fmaf(c[u][e], P.c, level(ids[buf][wv][at > 63 ? 63 : at < 0 ? 0 : at]));
+                        }
+                }
             } else if constexpr (BIAS) {
                 if (line.flat(buf)) {
                     plus = line.value[buf][0];
@@ -303,8 +325,9 @@ template <class T, int DP> static int attention_go(const MrfAttnParams &P, const
 {
     const dim3 grid(plan.grid, (unsigned)P.splits);
     if (plan.pack) {
-        if (P.table) mrf_attn_fwd<T, DP, 1, true, true><<<grid, 64, 0, st>>>(P);
-        else mrf_attn_fwd<T, DP, 1, true, false><<<grid, 64, 0, st>>>(P);
+        constexpr int NW = sizeof(T) == 4 && DP == 128 ? 2 : 1;      // (a tile on its way takes half of the registers then)
+        if (P.table) mrf_attn_fwd<T, DP, NW, true, true><<<grid, 64 * NW, 0, st>>>(P);
+        else mrf_attn_fwd<T, DP, NW, true, false><<<grid, 64 * NW, 0, st>>>(P);
     } else {
         constexpr int NW = mrf_attn_wide<T, DP>();
         if (P.table) mrf_attn_fwd<T, DP, NW, false, true><<<grid, 64 * NW, 0, st>>>(P);
@@ -362,9 +385,9 @@ int attention_check(const mrf_attention *a, MrfAttnParams &P)
 static AttnPlan attention_plan(const MrfAttnParams &P, int type)
 {
     const long long rows = (long long)P.Q * P.G;
-    const int block = type != MRF_F32 && P.D > 64 ? 256 : 128;      // (as mrf_attn_wide has it)
-    const bool pack = P.Q <= 16 || rows <= 64;
-    const long long groups = pack ? (long long)P.B * P.Hk * ((rows + 31) / 32) : (long long)P.B * P.Hq * ((P.Q + block - 1) / block);
+    const int block = type != MRF_F32 && P.D > 64 ? 256 : 128, few = type == MRF_F32 && P.D > 64 ? 64 : 32;      // (as attention_go has it)
+    const bool pack = P.Q <= 16;
+    const long long groups = pack ? (long long)P.B * P.Hk * ((rows + few - 1) / few) : (long long)P.B * P.Hq * ((P.Q + block - 1) / block);
     // parts of the keys: for eight wavefronts of few rows on a compute unit, or a workgroup of many; of four tiles at least
     const long long tiles = ((long long)P.K + 31) / 32 / (pack ? 1 : 2);
     long long splits = groups ? (pack ? 2048 : 256) / groups : 1;
