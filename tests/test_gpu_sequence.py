@@ -456,7 +456,7 @@ def test_gated_scan_matches_definition(outer, T, inner, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("T", [40, 700])
+@pytest.mark.parametrize("T", [1, 40, 700, 1500])
 def test_gated_scan_of_rows_of_their_own_length(T, dtype):
     n = [T, 0, 1, T // 2, 16, -3, T + 9, 17]
     for reverse in (False, True):
