@@ -115,6 +115,22 @@ template <int N, int GROUP, class Get, class Use> __device__ inline void mrf_ahe
     }
 }
 
+// Which rows of a result, of 32, lie in [from, to): a word for each lane, and for entry e all bits or none of them (an operation; a comparison, with its mask in
+// scalar registers, takes three).
+__device__ inline unsigned mrf_rows_between(int from, int to, int half)
+{
+    from = min(max(from, 0), 32);
+    to = min(max(to, 0), 32);
+    const unsigned below = to == 32 ? ~0u : (1u << to) - 1u, first = from == 32 ? ~0u : (1u << from) - 1u;
+    return (below & ~first) >> (4 * half);
+}
+__device__ inline unsigned mrf_row_bits(unsigned rows, int e) { return (unsigned)__builtin_amdgcn_sbfe((int)rows, 8 * (e / 4) + e % 4, 1); }
+__device__ inline float mrf_keep(unsigned bits, float x) { return __builtin_bit_cast(float, bits & __builtin_bit_cast(unsigned, x)); }
+__device__ inline float mrf_keep_or_lowest(unsigned bits, float x)      // (-infinity where not)
+{
+    return __builtin_bit_cast(float, (bits & __builtin_bit_cast(unsigned, x)) | (~bits & 0xff800000u));
+}
+
 struct MrfAttnParams {
     int B, Q, K, Hq, Hk, G, D;
     float scale, c;                               // c = scale log2(e)

@@ -17,8 +17,9 @@ constexpr float MRF_ATTN_RISE = 8.0f;
 template <class T> constexpr float mrf_attn_shift_forward() { return mrf_attn_shift<T>() > 0.0f ? mrf_attn_shift<T>() - MRF_ATTN_RISE : 0.0f; }
 template <class T> constexpr float mrf_attn_unshift_forward() { return mrf_attn_shift<T>() > 0.0f ? 0x1p-7f : 1.0f; }
 
-// Wavefronts of a SIMD: two, where their registers fit (in 32 bits not for 128 entries)
-template <class T, int DP, int NW> constexpr int mrf_attn_waves() { return NW == 1 || (sizeof(T) == 4 && DP == 128) ? 1 : 2; }
+// Wavefronts of a SIMD: two, where their registers fit (in 32 bits not for 128 entries); three for heads of up to 32 entries, which wait more than they multiply
+// (192 sequences of 624 queries, 4 heads of 32 in a band of 255, with a bias: 104 us with two, 78 with three, 89 with four, whose registers no longer fit).
+template <class T, int DP, int NW> constexpr int mrf_attn_waves() { return NW == 1 || (sizeof(T) == 4 && DP == 128) ? 1 : sizeof(T) == 2 && DP == 32 ? 3 : 2; }
 
 // Wavefronts of a workgroup for many queries: with eight, a tile of keys and values of 128 entries takes half the registers on its way to LDS, and two wavefronts
 // fit on a SIMD
@@ -155,12 +156,11 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
             if (!whole) {
                 mrf_stay_branch();
 #pragma unroll
-                for (int u = 0; u < KT / 32; ++u)
+                for (int u = 0; u < KT / 32; ++u) {
+                    const unsigned rows_in = mrf_rows_between(from - 32 * u, to - 32 * u, half);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int j = 32 * u + mrf_acc_row(e, half);
-                        c[u][e] = j >= from && j < to ? c[u][e] : -INFINITY;
-                    }
+                    for (int e = 0; e < 16; ++e) c[u][e] = mrf_keep_or_lowest(mrf_row_bits(rows_in, e), c[u][e]);
+                }
             }
 #pragma unroll
             for (int u = 0; u < KT / 32; ++u)

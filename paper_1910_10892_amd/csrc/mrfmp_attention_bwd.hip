@@ -19,7 +19,8 @@ template <class F> struct MrfTwo { F a, b; };
 template <class T, int DP> constexpr int mrf_attn_group() { return sizeof(T) == 4 ? 1 : DP == 128 ? 4 : 2; }
 
 // ---- dq, and delta
-template <class T, int DP, bool BIAS> __global__ void __launch_bounds__(256) mrf_attn_bwd_queries(const MrfAttnParams P)
+template <class T, int DP, bool BIAS>
+__global__ void __launch_bounds__(256, (sizeof(T) == 4 || DP == 128 ? 1 : DP == 64 ? 2 : 3)) mrf_attn_bwd_queries(const MrfAttnParams P)
 {
     constexpr int KT = mrf_attn_bwd_rows<T>(), NT = 256, ROWS = 128, LINE = ROWS + KT;
     typedef MrfRows<T, DP, KT, NT> Rows;
@@ -118,11 +119,9 @@ template <class T, int DP, bool BIAS> __global__ void __launch_bounds__(256) mrf
                 for (int e = 0; e < 16; ++e) c[e] = __builtin_amdgcn_exp2f(fmaf(c[e], times, -less));
                 if (!whole) {
                     mrf_stay_branch();
+                    const unsigned rows_in = mrf_rows_between(from - 32 * u, to - 32 * u, half);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int j = 32 * u + mrf_acc_row(e, half);
-                        c[e] = j >= from && j < to ? c[e] : 0.0f;
-                    }
+                    for (int e = 0; e < 16; ++e) c[e] = mrf_keep(mrf_row_bits(rows_in, e), c[e]);
                 }
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
@@ -173,12 +172,18 @@ template <int QT> __device__ inline void mrf_attn_query_tiles(const MrfAttnBatch
 //
 // TABLE: dS of 32 queries x 32 keys is put into LDS with each query's row moved by one against the next, so that a column holds a diagonal (places that none
 // falls on stay 0), and a lane sums a column.  A wavefront has 32 keys and goes through the queries upwards: of the 63 diagonals of a
-// block the later 31 go on in the next one, whose lanes are 32 less, and 32 are done and written.  An entry of the line: query - (key - first key) + 31.
-constexpr int MRF_SKEW = 71;      // from row to row: the halves of a wavefront, four rows apart, fall on the two halves of the banks
+// block (of the last lane there is none) the later 31 go on in the next one, whose lanes are 32 less, and 32 are done and written.  An entry of the line: query - (key - first key) + 31.
+// 63 entries a row, and 32 that are left free each time after rows 3, 11, 19 and 27: so the halves of a wavefront, four rows apart, fall on the two halves of the banks.
+__host__ __device__ constexpr int mrf_skew(int row) { return 63 * row + 32 * ((row + 4) / 8); }
+constexpr int MRF_SKEWED = mrf_skew(31) + 63;
 
+// Wavefronts of a SIMD.  Heads of up to 32 entries wait for the look-ups and for LDS more than for products: 192 sequences of 624 keys, 4 heads of 32 in a
+// band of 255, take 146 us with three (the compiler keeps 30 words in memory) and 177 with two; the queries' kernel 98 with three, 120 with four, 125 with two.
+// Without a table's gradient but with a bias three cost more than they give.
+//
 // DK, DV: which of the two it sums.  Both, where their sums and the keys and values fit into the registers, else one launch for each.
 template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV>
-__global__ void __launch_bounds__(256, (sizeof(T) == 2 && DP <= 64 ? 2 : 1)) mrf_attn_bwd_keys(const MrfAttnParams P)
+__global__ void __launch_bounds__(256, (sizeof(T) == 4 || DP == 128 ? 1 : DP == 64 || (BIAS && !TABLE) ? 2 : 3)) mrf_attn_bwd_keys(const MrfAttnParams P)
 {
     constexpr int QT = mrf_attn_bwd_rows<T>(), NT = 256, KEYS = 128, LINE = KEYS + QT;
     typedef MrfRows<T, DP, QT, NT> Rows;
@@ -187,7 +192,7 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 2 && DP <= 64 ? 2 : 1)) mrf
     __shared__ __align__(16) T lds[2][2][TILE];      // queries, gradients of the outputs
     __shared__ __align__(16) float ldsL[2][QT], ldsD[2][QT];
     __shared__ MrfLine<BIAS ? LINE : 1> line;
-    __shared__ float skew[TABLE ? 4 : 1][TABLE ? 32 * MRF_SKEW : 1];
+    __shared__ float skew[TABLE ? 4 : 1][TABLE ? MRF_SKEWED : 1];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), half = lane >> 5;
     // (the keys that most queries see first; part blockIdx.y of the heads that share them)
     const int bh = blockIdx.x % (P.B * P.Hk), block = (int)(blockIdx.x / (P.B * P.Hk)), group = P.G / P.shares;
@@ -210,7 +215,7 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 2 && DP <= 64 ? 2 : 1)) mrf
         }
     }
     if constexpr (TABLE)
-        for (int n = lane; n < 32 * MRF_SKEW; n += 64) skew[wv][n] = 0.0f;
+        for (int n = lane; n < MRF_SKEWED; n += 64) skew[wv][n] = 0.0f;
     mrf_acc dk[DK ? DP / 32 : 1], dv[DV ? DP / 32 : 1];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
@@ -301,11 +306,9 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 2 && DP <= 64 ? 2 : 1)) mrf
                     }
                     if (!whole) {
                         mrf_stay_branch();
+                        const unsigned rows_in = mrf_rows_between(from - 32 * u, to - 32 * u, half);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const int r = 32 * u + mrf_acc_row(e, half);
-                            c[e] = r >= from && r < to ? c[e] : 0.0f;
-                        }
+                        for (int e = 0; e < 16; ++e) c[e] = mrf_keep(mrf_row_bits(rows_in, e), c[e]);
                     }
 #pragma unroll
                     for (int e = 0; e < 16; ++e) dp[e] *= c[e];
@@ -323,13 +326,13 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 2 && DP <= 64 ? 2 : 1)) mrf
 #pragma unroll
                             for (int e = 0; e < 16; ++e) {
                                 const int r = mrf_acc_row(e, half);
-                                skewed[r * MRF_SKEW + r - (lane & 31) + 31] = dp[e];
+                                skewed[mrf_skew(r) + r - (lane & 31) + 31] = dp[e];
                             }
                             mrf_wave_lds_fence();
                             float part[4] = {};
 #pragma unroll
-                            for (int r = 0; r < 32; ++r) part[r % 4] += skewed[r * MRF_SKEW + lane];
-                            sum += (part[0] + part[1]) + (part[2] + part[3]);
+                            for (int r = 0; r < 32; ++r) part[r % 4] += skewed[mrf_skew(r) + min(lane, 62)];
+                            sum += lane < 63 ? (part[0] + part[1]) + (part[2] + part[3]) : 0.0f;
                             mrf_wave_lds_fence();
                         }
                     }
