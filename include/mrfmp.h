@@ -359,19 +359,22 @@ int mrf_softmin_policy_backward(int64_t n_pixels, int32_t L, const void *cost, i
  * Key j counts for query i of batch b if  first_offset <= d <= last_offset  with  d = j - i - query_offset - query_offsets[b],
  * i < q_lengths[b] and j < k_lengths[b].  last_offset = 0: causal.  first_offset = -(n - 1) as well: the n keys up to the query's own.  Over those keys
  *   s(i,j) = scale q_i . k_j + table[h][bucket(d)],  lse_i = log sum_j exp(s(i,j)),  P(i,j) = exp(s(i,j) - lse_i),  out_i = sum_j P(i,j) v_j
- * A query without a key: out_i = 0, lse_i = -infinity, no gradients.  A single query of a long cache (Q = 1, query_offset = its position) divides the keys
+ * A query without a key: out_i = 0, lse_i = -infinity, no gradients.  What does not count is weighted with 0: a NaN or an infinity in a key or value (query or
+ * grad_out) within the lengths may reach queries (keys) that it does not count for.  lse has 32 bits: probabilities of scores of size 2^n are right to 2^(n - 23).  A single query of a long cache (Q = 1, query_offset = its position) divides the keys
  * among workgroups. */
 typedef struct {
-    int32_t B, Q, K, Hq, Hk, D;       /* D 1..MRF_ATTENTION_LONGEST_HEAD, Hk divides Hq; B, Q, K may be 0 */
+    int32_t B, Q, K, Hq, Hk, D;       /* D 1..MRF_ATTENTION_LONGEST_HEAD, Hk divides Hq, Hq up to 32768; B, Q, K may be 0; Q + K at most 2^31 - 2^16, and
+                                         B Hq ceil(max(Q, K) / 128) below 2^24, else MRF_ERR_BAD_SHAPE */
     int32_t type;                     /* of q, k, v, out and their gradients: MRF_F32, MRF_F16, MRF_BF16 */
-    float scale;                      /* > 0 and finite, else MRF_ERR_BAD_ARGUMENT */
+    float scale;                      /* > 0 and finite, times log2(e) too, else MRF_ERR_BAD_ARGUMENT */
     const void *q, *k, *v;            /* DEVICE [B][Q][Hq][D], [B][K][Hk][D], [B][K][Hk][D] at strides q_stride .. */
     int64_t q_stride[3], k_stride[3], v_stride[3];      /* batch, token, head */
     int64_t first_offset, last_offset;
     int64_t query_offset;             /* within 2^40 of 0, else MRF_ERR_BAD_ARGUMENT */
     const int32_t *query_offsets;     /* DEVICE [B] or NULL (0) */
     const int32_t *q_lengths, *k_lengths;      /* DEVICE [B] or NULL (Q, K) */
-    const float *table;               /* DEVICE [Hq][n_buckets], or [n_buckets][Hq] with heads_last, or NULL: no bias */
+    const float *table;               /* DEVICE [Hq][n_buckets], or [n_buckets][Hq] with heads_last, or NULL: no bias.  -2^20 or
+                                         less (-infinity, a type's lowest value): pairs of that bucket do not count */
     const int32_t *bucket_of;         /* DEVICE [n_offsets]: bucket of d = map_offset + n; clamped to [0, n_buckets).  A d before the map's first has that
                                          one's bucket, one behind its last that one's */
     int64_t map_offset, n_offsets;    /* within 2^41 of 0; 1..2^40 */
@@ -379,7 +382,8 @@ typedef struct {
 } mrf_attention;
 
 /* Bytes of DEVICE workspace (256-byte aligned) of the forward (backward = 0) or backward pass; 0 if the description is invalid, or none is needed.  Backward, with
- * a table: an eighth of a byte for each pair of a query and a key, and a few for each query and key. */
+ * a table: an eighth of a byte for each pair of a query and a key, and a few for each query and key; where few keys have many queries, the 32-bit sums of
+ * grad_k and grad_v that parts of the queries' heads make. */
 size_t mrf_attention_workspace_bytes(const mrf_attention *att, int backward);
 
 /*   out   DEVICE [B][Q][Hq][D], assigned
@@ -426,7 +430,7 @@ size_t mrf_head_rotation_workspace_bytes(int64_t n_tokens, int32_t Hq, int32_t H
 int mrf_head_rotation_backward(const mrf_head_rotation *heads, const void *grad_out_q, const void *grad_out_k, void *grad_q, void *grad_k,
                                float *grad_gamma_q, float *grad_gamma_k, void *workspace, size_t workspace_bytes, void *hip_stream);
 
-/* Gated linear recurrence along the T steps of x, z [n_outer][T][n_inner], from the first to the last, or with reverse from the last to the first:
+/* Gated linear recurrence along the T steps of x, z [n_outer][T][n_inner] (n_outer n_inner below 2^31), from the first to the last, or with reverse from the last to the first:
  *   a = 1 / (1 + exp(-z)),  h_t = a_t h_(t-1) + (1 - a_t) x_t  with complement,  a_t h_(t-1) + x_t without;  y_t = h_t,  h_(-1) = initial
  * Scanlines of an image [B][H][W][C]: rows are n_outer = B H, T = W, n_inner = C; columns n_outer = B, T = H, n_inner = W C.  One step (T = 1) with initial and
  * final_state is the form for single tokens.  The state is 32 bits from the first step to the last.

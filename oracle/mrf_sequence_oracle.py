@@ -26,9 +26,10 @@ def attention_pairs(Q, K, first=None, last=None, offset=0, q_length=None, k_leng
 
 
 def attention_bias(d, table, bucket_of, map_offset):
-    """Values [Hq][..] of a table [Hq][n_buckets] at the offsets d, the map's ends beyond them."""
+    """Values [Hq][..] of a table [Hq][n_buckets] at the offsets d, the map's ends beyond them; -infinity from -2^20 down."""
     which = np.clip(np.asarray(bucket_of)[np.clip(d - map_offset, 0, len(bucket_of) - 1)], 0, table.shape[1] - 1)
-    return np.asarray(table, np.float64)[:, which], which
+    table = np.asarray(table, np.float64)
+    return np.where(table <= -2.0 ** 20, -np.inf, table)[:, which], which
 
 
 def attention(q, k, v, scale, ok, bias=None):

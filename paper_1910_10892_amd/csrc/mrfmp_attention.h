@@ -180,7 +180,9 @@ struct MrfAttnBatch {
     __device__ inline int to(int i1) const { return min(i1 + hi + 1, nk); }
 };
 
-// the bucket of j - i = d; a bucket's value of head h, times log2(e)
+// the bucket of j - i = d; a bucket's value of head h, times log2(e).  From MRF_ATTN_LEAST down a value leaves its pairs out: a row with nothing else would have a
+// log-sum-exp of that size, whose 32 bits cannot tell its probabilities apart (nor from NaN, at the type's lowest value).
+constexpr float MRF_ATTN_LEAST = -1048576.0f;
 __device__ inline int mrf_attn_bucket(const MrfAttnParams &P, const MrfAttnBatch &s, long long d)
 {
     long long at = s.map + d;
@@ -190,7 +192,8 @@ __device__ inline int mrf_attn_bucket(const MrfAttnParams &P, const MrfAttnBatch
 }
 __device__ inline float mrf_attn_level(const MrfAttnParams &P, int h, int bucket)
 {
-    return P.table[P.heads_last ? (size_t)bucket * P.Hq + h : (size_t)h * P.n_buckets + bucket] * 1.44269504088896340736f;
+    const float value = P.table[P.heads_last ? (size_t)bucket * P.Hq + h : (size_t)h * P.n_buckets + bucket];
+    return value <= MRF_ATTN_LEAST ? -INFINITY : value * 1.44269504088896340736f;
 }
 __device__ inline float mrf_attn_bias(const MrfAttnParams &P, const MrfAttnBatch &s, int h, long long d)
 {

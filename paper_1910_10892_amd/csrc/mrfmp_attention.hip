@@ -355,10 +355,11 @@ int attention_check(const mrf_attention *a, MrfAttnParams &P)
     if (!a) return MRF_ERR_NULL_POINTER;
     const long long most = 0x7fff0000LL;
     if (a->B < 0 || a->Q < 0 || a->K < 0 || a->Hq < 1 || a->Hk < 1 || a->Hq % a->Hk || a->D < 1 || a->D > MRF_ATTENTION_LONGEST_HEAD) return MRF_ERR_BAD_SHAPE;
-    if (a->Q > most || a->K > most || a->Hq > 32768) return MRF_ERR_BAD_SHAPE;
-    if (a->B && (long long)a->Hq * ((a->Q + 31) / 32) > most / a->B) return MRF_ERR_BAD_SHAPE;
-    if (a->B && (long long)a->Hq * ((a->K + 31) / 32) > most / a->B) return MRF_ERR_BAD_SHAPE;
-    if (!known_type(a->type) || !(a->scale > 0.0f) || !(a->scale < INFINITY)) return MRF_ERR_BAD_ARGUMENT;
+    if ((long long)a->Q + a->K > most || a->Hq > 32768) return MRF_ERR_BAD_SHAPE;
+    // (workgroups of 256 threads: a grid has fewer than 2^32)
+    const long long groups = 0xffffff, rows = a->Q > a->K ? a->Q : a->K;
+    if (a->B && a->Hq * ((rows + 127) / 128) > groups / a->B) return MRF_ERR_BAD_SHAPE;
+    if (!known_type(a->type) || !(a->scale > 0.0f) || !(a->scale * 1.44269504088896340736f < INFINITY)) return MRF_ERR_BAD_ARGUMENT;
     const long long far = 1LL << 40;
     if (a->query_offset > far || a->query_offset < -far) return MRF_ERR_BAD_ARGUMENT;
     for (int i = 0; i < 3; ++i)

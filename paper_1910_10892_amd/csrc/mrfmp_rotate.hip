@@ -312,7 +312,7 @@ template <bool FORWARD, class X, int S> static int rotate_lanes(MrfRotateParams 
     if (want > heads) want = heads;
     P.heads = (int)((heads + want - 1) / want);
     if (P.heads > 4) P.heads -= P.heads % 4;
-    const long long most = FORWARD ? 0x3fffffffLL : MRF_ROTATE_PARTS;
+    const long long most = FORWARD ? 1 << 22 : MRF_ROTATE_PARTS;      // (a grid has fewer than 2^32 threads)
     for (int k = 0; k < 2; ++k) {
         P.pieces[k] = ((k ? P.Hk : P.Hq) + P.heads - 1) / P.heads;
         const long long blocks = (P.tokens * P.pieces[k] + 256 / TL - 1) / (256 / TL);

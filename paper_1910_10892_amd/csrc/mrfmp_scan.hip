@@ -443,7 +443,8 @@ __global__ void __launch_bounds__(1024) mrf_scan_carry(const MrfScanParams P)
     }
 }
 
-// A single step, forward and backward: a lane has V channels, and nothing is prepared for more (with the kernels above a million channels took 26 us forward and 24 back).
+// A single step, forward and backward: a lane has V channels, and nothing is prepared for more: a million channels take 17 us forward
+// and backward together, and took 50 with the kernels above.
 template <class X, int V, bool COMPLEMENT, bool BACK> __global__ void __launch_bounds__(256) mrf_scan_one(const MrfScanParams P)
 {
     typedef MrfScanLane<X, V> Lane;
@@ -512,7 +513,7 @@ static bool scan_sizes_ok(long long outer, long long T, long long inner)
 {
     const long long most = 0x7fffffffLL;
     if (outer < 0 || T < 0 || inner < 0 || outer > most || T > most - 2 * MRF_SCAN_STEPS || inner > most) return false;
-    if (outer && inner > (1LL << 36) / outer) return false;      // (channels: a grid has 2^31 workgroups of 64 at most)
+    if (outer && inner > most / outer) return false;      // (channels: a grid has fewer than 2^32 threads)
     return !(outer && inner && T) || T <= (1LL << 60) / (outer * inner);
 }
 

@@ -274,6 +274,104 @@ def test_attention_nan_stays_in_its_query_and_infinite_scores_bar():
         assert torch.isnan(lse[bad.transpose(1, 2)]).all() and torch.equal(lse[~bad.transpose(1, 2)], clean_lse[~bad.transpose(1, 2)])
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("Q,K,Hk", [(90, 130, 4), (1, 700, 4), (1, 700, 2), (3, 40, 1), (200, 64, 2)])
+def test_attention_buckets_that_bar_their_pairs(Q, K, Hk, dtype):
+    """Values of -infinity, of a type's lowest value, of -2^20 leave out their pairs; a head may bar all of them, or all that a query has."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    from oracle import mrf_sequence_oracle as so
+    print("case barred", Q, K, Hk, dtype, flush=True)
+    rng = np.random.default_rng(Q + K)
+    Hq, D, NB, T = 4, 24, 4, getattr(torch, dtype)
+    q, k, v, g = (_put(rng.normal(size=s), dtype) for s in ((1, Q, Hq, D), (1, K, Hk, D), (1, K, Hk, D), (1, Q, Hq, D)))
+    low = float(torch.finfo(torch.float32).min)
+    values = rng.normal(size=(Hq, NB))
+    values[0, 1], values[1] = -np.inf, [low, -1e9, -np.inf, float(torch.finfo(torch.bfloat16).min)]
+    values[2, [0, 2]], values[3, [0, 1, 2]] = [-2.0 ** 20, low], -1e9
+    table = _put(values, "float32")
+    near = np.array([(abs(d) // 16) % 4 if abs(d) < 64 else 2 for d in range(-(Q - 1), K)], np.int32)      # (one bucket far away)
+    bucket_of = torch.from_numpy(near).cuda()
+    att = mrf.MrfAttention(q, k, v, 0.2, table=table, bucket_of=bucket_of, map_offset=-(Q - 1))
+    got = {"out": torch.empty_like(q), "grad_q": torch.empty_like(q), "grad_k": torch.empty_like(k), "grad_v": torch.empty_like(k)}
+    lse, grad_table = torch.empty(1, Hq, Q, device="cuda:0"), torch.empty_like(table)
+    ws = torch.empty(max(mrf.mrf_attention_workspace_bytes(att, b) for b in (False, True)), dtype=torch.uint8, device="cuda:0")
+    mrf.mrf_attention_forward(att, got["out"], lse, ws)
+    mrf.mrf_attention_backward(att, g, got["out"], lse, got["grad_q"], got["grad_k"], got["grad_v"], grad_table, ws)
+    ok, d = so.attention_pairs(Q, K)
+    bias, which = so.attention_bias(d, values, near, -(Q - 1))
+    G = Hq // Hk
+    sums = {n: [np.zeros((K, Hk, D)), np.zeros((K, Hk, D))] for n in ("grad_k", "grad_v")}
+    for h in range(Hq):
+        mine = np.isfinite(bias[h])
+        one = lambda t, x: _np(t[0])[:, x:x + 1]  # noqa: E731
+        want, ds, eds = _attention_bounds(one(q, h), one(k, h // G), one(v, h // G), one(g, h), float(att.c.scale), mine, np.where(mine, bias[h], 0.0)[None], dtype, so)
+        value, bound = want["lse"]
+        here, some = _np(lse[0, h]), mine.any(1)
+        assert (here[~some] == -np.inf).all()
+        _close(lse[0, h][torch.from_numpy(some).cuda()], value[0][some], bound[0][some], what="lse")
+        for name in ("out", "grad_q"):
+            _close(got[name][0][:, h:h + 1], *want[name], dtype, name)
+            assert (_np(got[name][0])[~some, h] == 0).all()
+        for name in sums:
+            for total, part in zip(sums[name], want[name]):
+                total[:, h // G] += part[:, 0]
+        _close(grad_table[h], so.table_grad(ds, which, NB)[0], so.table_grad(eds + SUM * U * np.abs(ds), which, NB)[0], what="grad_table")
+    for name, (value, bound) in sums.items():
+        _close(got[name][0], value, bound, dtype, name)
+
+
+@pytest.mark.parametrize("dtype", ["float16", "float32"])
+def test_strides_beyond_32_bits_and_of_zero(dtype):
+    """Inputs whose tokens lie further apart than 32 bits of elements count, or all of whose sequences are one, give the bits of dense ones."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    T, far, n, H, D = getattr(torch, dtype), (1 << 26) + 24, 70, 2, 16
+    whole = torch.empty(far * n, dtype=T, device="cuda:0")      # (up to 19 GB, of which little is touched)
+    assert far * (n - 1) > 1 << 32
+    gen = torch.Generator(device="cuda:0").manual_seed(9)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda:0").to(T)  # noqa: E731
+
+    def apart(t, at):
+        view = whole.as_strided((1, n, H, D), (0, far, D, 1), at)
+        view.copy_(t)
+        return view
+
+    def results(q, k, v, g, x, z):
+        new = lambda *s, t=T: torch.empty(s, dtype=t, device="cuda:0")  # noqa: E731
+        B = q.shape[0]
+        att = mrf.MrfAttention(q, k, v, 0.25, last_offset=0)
+        out, lse, gq, gk, gv = new(B, n, H, D), new(B, H, n, t=torch.float32), new(B, n, H, D), new(B, n, H, D), new(B, n, H, D)
+        ws = new(mrf.mrf_attention_workspace_bytes(att, True), t=torch.uint8)
+        mrf.mrf_attention_forward(att, out, lse, ws)
+        mrf.mrf_attention_backward(att, g, out, lse, gq, gk, gv, None, ws)
+        few = new(B, 1, H, D)
+        mrf.mrf_attention_forward(mrf.MrfAttention(q[:, -1:], k, v, 0.25), few, None, None)
+        freq = torch.linspace(1.0, 0.01, D // 2, device="cuda:0")
+        rq, rk, dq, dk = new(B, n, H, D), new(B, n, H, D), new(B, n, H, D), new(B, n, H, D)
+        mrf.mrf_head_rotation_forward(q, k, None, None, 1e-6, freq, rq, rk)
+        mrf.mrf_head_rotation_backward(g, g, q, k, None, None, 1e-6, freq, dq, dk, None, None, None)
+        y, states, gx, gz = new(B, n, H * D), new(B, mrf.mrf_gated_scan_states(n), H * D, t=torch.float32), new(B, n, H * D), new(B, n, H * D)
+        mrf.mrf_gated_scan_forward(x, z, None, None, y, None, states, None)
+        mrf.mrf_gated_scan_backward(g.flatten(2), None, x, z, None, states, gx, gz, None, None)
+        return out, lse, gq, gk, gv, few, rq, rk, dq, dk, y, gx, gz
+
+    q, k, v, g = (rand(1, n, H, D) for _ in range(4))
+    want = results(q, k, v, g, q.flatten(2), k.flatten(2))
+    wide = [apart(t, 64 * i) for i, t in enumerate((q, k, v))]
+    flat = [whole.as_strided((1, n, H * D), (0, far, 1), 64 * i) for i in range(2)]
+    for a, b in zip(want, results(*wide, g, *flat)):
+        assert torch.equal(a, b)
+    del wide, flat, whole
+    # one sequence for all of a batch
+    B = 3
+    same = [t.expand(B, -1, -1, -1) for t in (q, k, v)]
+    g = rand(B, n, H, D)
+    want = results(*(t.contiguous() for t in same), g, *(t.contiguous().flatten(2) for t in same[:2]))
+    for a, b in zip(want, results(*same, g, *(t.flatten(2).expand(B, -1, -1) for t in (q, k)))):
+        assert torch.equal(a, b)
+
+
 # ---- norm and rotation of heads
 
 def _check_rotation(B, T, Hq, Hk, D, dtype, rotary=None, axes=0, offset=0, interleaved=False, how="dense", gammas=True):

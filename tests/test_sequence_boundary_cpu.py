@@ -27,10 +27,10 @@ def test_attention_refusals():
 
     assert lib.mrf_attention_forward(None, FAKE, None, FAKE, 1 << 40, None) == -1
     for bad in (dict(B=-1), dict(Q=-1), dict(K=-1), dict(Hq=0), dict(Hk=0), dict(Hk=3), dict(D=0), dict(D=129), dict(Q=0x7fff0001),
-                dict(B=1 << 20, Q=1 << 20), dict(B=1 << 20, K=1 << 20), dict(Hq=65538, Hk=2)):
+                dict(B=1 << 20, Q=1 << 20), dict(B=1 << 20, K=1 << 20), dict(Hq=65538, Hk=2), dict(Q=1 << 30, K=0x3fff0001), dict(B=1 << 22), dict(B=1 << 14, Q=32769)):
         assert forward(**bad) == -2, bad
         assert lib.mrf_attention_workspace_bytes(ctypes.byref(_attention(**bad)), 1) == 0
-    for bad in (dict(type=3), dict(type=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=INF), dict(scale=NAN), dict(q_stride=(1, -1, 1)),
+    for bad in (dict(type=3), dict(type=-1), dict(scale=0.0), dict(scale=-1.0), dict(scale=INF), dict(scale=NAN), dict(scale=3e38), dict(q_stride=(1, -1, 1)),
                 dict(k_stride=(-1, 1, 1)), dict(v_stride=(1, 1, -1)), dict(query_offset=1 << 41), dict(query_offset=-(1 << 41))):
         assert forward(**bad) == -12, bad
     table = dict(table=FAKE, bucket_of=FAKE, n_offsets=9, n_buckets=4)
@@ -109,7 +109,7 @@ def test_gated_scan_refusals():
         strides = lambda s: None if s is None else (ctypes.c_int64 * 2)(*s)  # noqa: E731
         return lib.mrf_gated_scan_forward(outer, T, inner, t, x, strides(xs), z, strides(zs), 1, 0, None, None, y, None, None, ws, size, None)
 
-    for bad in (dict(outer=-1), dict(T=-1), dict(inner=-1), dict(T=1 << 31), dict(outer=1 << 31), dict(inner=1 << 31), dict(outer=1 << 20, inner=1 << 20)):
+    for bad in (dict(outer=-1), dict(T=-1), dict(inner=-1), dict(T=1 << 31), dict(outer=1 << 31), dict(inner=1 << 31), dict(outer=1 << 20, inner=1 << 20), dict(outer=2, inner=1 << 30)):
         assert forward(**bad) == -2, bad
         assert mrf.mrf_gated_scan_workspace_bytes(bad.get("outer", 2), bad.get("T", 3), bad.get("inner", 4)) == 0
     assert forward(t=3) == -12 and forward(xs=(-1, 4)) == -12 and forward(zs=(12, -4)) == -12
