@@ -360,8 +360,8 @@ int mrf_softmin_policy_backward(int64_t n_pixels, int32_t L, const void *cost, i
  * i < q_lengths[b] and j < k_lengths[b].  last_offset = 0: causal.  first_offset = -(n - 1) as well: the n keys up to the query's own.  Over those keys
  *   s(i,j) = scale q_i . k_j + table[h][bucket(d)],  lse_i = log sum_j exp(s(i,j)),  P(i,j) = exp(s(i,j) - lse_i),  out_i = sum_j P(i,j) v_j
  * A query without a key: out_i = 0, lse_i = -infinity, no gradients.  What does not count is weighted with 0: a NaN or an infinity in a key or value (query or
- * grad_out) within the lengths may reach queries (keys) that it does not count for.  lse has 32 bits: probabilities of scores of size 2^n are right to 2^(n - 23).  A single query of a long cache (Q = 1, query_offset = its position) divides the keys
- * among workgroups. */
+ * grad_out) within the lengths may reach queries (keys) that it does not count for.  lse has 32 bits: probabilities of scores of size 2^n are right to 2^(n - 23).
+ * A single query of a long cache (Q = 1, query_offset = its position) divides the keys among workgroups. */
 typedef struct {
     int32_t B, Q, K, Hq, Hk, D;       /* D 1..MRF_ATTENTION_LONGEST_HEAD, Hk divides Hq, Hq up to 32768; B, Q, K may be 0; Q + K at most 2^31 - 2^16, and
                                          B Hq ceil(max(Q, K) / 128) below 2^24, else MRF_ERR_BAD_SHAPE */

@@ -17,9 +17,10 @@ constexpr float MRF_ATTN_RISE = 8.0f;
 template <class T> constexpr float mrf_attn_shift_forward() { return mrf_attn_shift<T>() > 0.0f ? mrf_attn_shift<T>() - MRF_ATTN_RISE : 0.0f; }
 template <class T> constexpr float mrf_attn_unshift_forward() { return mrf_attn_shift<T>() > 0.0f ? 0x1p-7f : 1.0f; }
 
-// Wavefronts of a SIMD: two, where their registers fit (in 32 bits not for 128 entries); three for heads of up to 32 entries, which wait more than they multiply
-// (192 sequences of 624 queries, 4 heads of 32 in a band of 255, with a bias: 104 us with two, 78 with three, 89 with four, whose registers no longer fit).
-template <class T, int DP, int NW> constexpr int mrf_attn_waves() { return NW == 1 || (sizeof(T) == 4 && DP == 128) ? 1 : sizeof(T) == 2 && DP == 32 ? 3 : 2; }
+// Wavefronts of a SIMD: two, where their registers fit (in 32 bits not for 128 entries); three for heads of up to 64 entries in 16 bits, which wait more than they
+// multiply: 192 sequences of 624 queries, 4 heads of 32 in a band of 255, with a bias, 104 us with two, 75 with three, 89 with four; 4 sequences of up to 2,048, 16 heads
+// of 64, with a bias, 117 us with two, 89 with three, all of 2,048 without a bias 113 and 105, with one 129 and 133 (some of the registers are in memory then).
+template <class T, int DP, int NW> constexpr int mrf_attn_waves() { return NW == 1 || (sizeof(T) == 4 && DP == 128) ? 1 : sizeof(T) == 2 && DP <= 64 ? 3 : 2; }
 
 // Wavefronts of a workgroup for many queries: with eight, a tile of keys and values of 128 entries takes half the registers on its way to LDS, and two wavefronts
 // fit on a SIMD
@@ -83,10 +84,6 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
         if constexpr (BIAS && PACK) ids[buf][wv][lane] = bias_next.bucket;
     };
 
-    // Of two wavefronts on a SIMD one goes first: it multiplies while the other takes exponentials, instead of both doing the same at a time.
-    if constexpr (NW == 8)
-        if (wv < 4) __builtin_amdgcn_s_setprio(1);
-
     mrf_acc o[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
@@ -148,9 +145,11 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
                     times = 1.0f;
                     const float *const at = line.value[buf] + ROWS - 1 - (wv * 32 + (lane & 31));
 #pragma unroll
-                    for (int u = 0; u < KT / 32; ++u)
+                    for (int u = 0; u < KT / 32; ++u) {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) c[u][e] = fmaf(c[u][e], P.c, at[32 * u + mrf_acc_row(e, half)]);
+                        __builtin_amdgcn_sched_barrier(0);      // (not all values at a time: they would not fit)
+                    }
                 }
             }
             if (!whole) {
