@@ -444,19 +444,26 @@ template <int QT> __global__ void __launch_bounds__(256) mrf_attn_buckets(const 
         if (k < 0 || k >= MRF_TABLE_BUCKETS) continue;
         // strips whose keys have a query at that offset: key - offset in [0, nq)
         const float *const lines = P.lines + ((size_t)b * P.Hq + h) * P.strips * P.line;
-        const long long first = max(offset, 0LL) / 32, last = min(offset + s.nq - 1, (long long)s.nk - 1);
+        const int first = (int)(max(offset, 0LL) / 128 * 4), last = (int)min(offset + s.nq - 1, (long long)s.nk - 1);
         float sum = 0.0f;
-        for (long long strip = first / 4 * 4; 32 * strip <= last; strip += 4) {      // (a workgroup's four strips have the same tiles)
-            int t0, t1;
-            mrf_attn_query_tiles<QT>(s, (int)(32 * strip), t0, t1);
-            const long long entry = strip * 32 - offset + 31;
-            float v[4];
+        // (a workgroup's four strips have the same tiles; the loads of two workgroups' are on their way together)
+        for (int strip = first; strip <= last / 32 && last >= 0; strip += 8) {
+            float v[8];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const long long e = entry + 32 * w;
-                v[w] = t0 < t1 && e >= (long long)t0 * QT && e < (long long)t1 * QT + 32 ? lines[(strip + w) * P.line + e] : 0.0f;
+            for (int y = 0; y < 2; ++y) {
+                int t0, t1;
+                mrf_attn_query_tiles<QT>(s, 32 * (strip + 4 * y), t0, t1);
+                const int entry = (int)(32 * (strip + 4 * y) - offset + 31);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int e = entry + 32 * w;
+                    const bool in = t0 < t1 && e >= t0 * QT && e < t1 * QT + 32;
+                    const float value = lines[in ? (strip + 4 * y + w) * (long long)P.line + e : 0];
+                    v[4 * y + w] = in ? value : 0.0f;
+                }
             }
-            sum += (v[0] + v[1]) + (v[2] + v[3]);
+#pragma unroll
+            for (int y = 0; y < 2; ++y) sum += (v[4 * y] + v[4 * y + 1]) + (v[4 * y + 2] + v[4 * y + 3]);
         }
         sums[k][tid] += sum;
     }
@@ -511,9 +518,10 @@ template <class T, int DP> static int attention_back(const MrfAttnParams &P, hip
         MrfAttnParams S = P;
         S.parts = 0;
         if (pairs) {
-            // workgroups for the whole card twice over, as far as there are pieces for them
+            // workgroups for the whole card four times over, as far as there are pieces for them (16 heads of 2,048 queries and keys in 4 batches: 22 us with half of
+            // that and the strips of one workgroup at a time, 15 now)
             const long long all = ((long long)P.Q + P.K - 1 + 255) / 256 * P.B;
-            long long parts = 512 / P.Hq < 1 ? 1 : 512 / P.Hq > MRF_TABLE_PARTS ? MRF_TABLE_PARTS : 512 / P.Hq;
+            long long parts = 1024 / P.Hq < 1 ? 1 : 1024 / P.Hq > MRF_TABLE_PARTS ? MRF_TABLE_PARTS : 1024 / P.Hq;
             if (parts > all) parts = all;
             S.pieces = (all + parts - 1) / parts;
             S.parts = (int)((all + S.pieces - 1) / S.pieces);
