@@ -39,29 +39,34 @@ template <class T> __device__ inline typename MrfFrag<T>::type mrf_acc_frag(cons
     return f;
 }
 
+// Entries moved down by `bytes` (the same in all lanes), where `mine`, with 0 behind them
+template <int WORDS, class Words> __device__ inline void mrf_move_down(Words &w, int bytes, bool mine)
+{
+#pragma unroll
+    for (int by = WORDS / 2; by >= 1; by /= 2) {
+        const bool go = mine && (bytes / 4 & by);
+#pragma unroll
+        for (int j = 0; j < WORDS; ++j) w[j] = go ? (j + by < WORDS ? w[j + by < WORDS ? j + by : 0] : 0u) : w[j];
+    }
+    const bool go = mine && (bytes & 2);
+#pragma unroll
+    for (int j = 0; j < WORDS; ++j) w[j] = go ? __builtin_amdgcn_alignbit(j + 1 < WORDS ? w[j + 1 < WORDS ? j + 1 : 0] : 0u, w[j], 16) : w[j];
+}
+
 // PER entries from d on of a row of D that starts at `row`, 0 behind its end and where it is not `there`.  Nothing is left out by a branch: what is not
 // there is read from the row's start (its end) instead, so `row` has to be a row at any rate.
 template <int PER, class T> __device__ inline void mrf_load_part(const T *row, int d, int D, bool there, T (&v)[PER])
 {
     typedef T vec __attribute__((ext_vector_type(PER), aligned(sizeof(T))));
     constexpr int WORDS = PER * (int)sizeof(T) / 4;
-    if (D % PER == 0) {
-        there = there && d < D;
-        const vec x = *(const vec *)(row + (d < D ? d : 0));
+    if (D >= PER) {      // a row's last chunk, where it is no whole one: its last PER entries, moved down
+        const vec x = *(const vec *)(row + min(d, D - PER));
         unsigned w[WORDS];
         __builtin_memcpy(w, &x, sizeof(w));
+        if (D % PER) mrf_move_down<WORDS>(w, (PER - D % PER) * (int)sizeof(T), d + PER > D);
+        there = there && d < D;
 #pragma unroll
         for (int j = 0; j < WORDS; ++j) w[j] = there ? w[j] : 0u;
-        __builtin_memcpy(v, w, sizeof(w));
-    } else if (D % (PER / 2) == 0) {      // halves of that
-        typedef T hvec __attribute__((ext_vector_type(PER / 2), aligned(sizeof(T))));
-        const bool first = there && d < D, second = there && d + PER / 2 < D;
-        const hvec x = *(const hvec *)(row + (d < D ? d : 0)), y = *(const hvec *)(row + (d + PER / 2 < D ? d + PER / 2 : 0));
-        unsigned w[WORDS];
-        __builtin_memcpy(w, &x, sizeof(w) / 2);
-        __builtin_memcpy(w + WORDS / 2, &y, sizeof(w) / 2);
-#pragma unroll
-        for (int j = 0; j < WORDS; ++j) w[j] = (j < WORDS / 2 ? first : second) ? w[j] : 0u;
         __builtin_memcpy(v, w, sizeof(w));
     } else {
 #pragma unroll
@@ -265,36 +270,29 @@ template <class T, int DP, int ROWS, int NT> struct MrfRows {
     int there;      // rows that there are, or -1 where all of the tile is as it was loaded
     int entries;
 
-    // rows from `at` on, `rows` (1 at least) of them; of a row D entries; the others are 0.  (Whole chunks that are not there are read from elsewhere in the tensor,
-    // and put right only when they are stored: nothing waits for a load before that.)
-    __device__ inline void load(const T *at, long long stride, int rows, int D)
+    // rows from `at` on, `rows` (1 at least) of them; of a row D entries; the others are 0.  (Chunks that are not there are read from elsewhere in the tensor, a row's
+    // last one that is no whole one as its last PER entries, and put right only when they are stored: nothing waits for a load before that.  Entries one by one are 2 to 5
+    // times slower: 47 sequences of 41 queries and 739 keys, 35 heads of 103, 576 us and 286.)
+    __device__ __forceinline__ void load(const T *at, long long stride, int rows, int D)
     {
         static_assert(CHUNKS % NT == 0, "chunks of a tile");
         there = -1;
         entries = D;
-        if (D % (PER / 2) == 0 && (rows < ROWS || D < DP)) there = rows;
-        if (D % PER == 0) {
+        if (D >= PER) {
+            if (rows < ROWS || D < DP) there = rows;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 const int c = (int)threadIdx.x + n * NT, row = c / (DP / PER), d = c % (DP / PER) * PER;
-                const uvec u = *(const uvec *)(at + min(row, rows - 1) * stride + (d < D ? d : 0));
+                const uvec u = *(const uvec *)(at + min(row, rows - 1) * stride + min(d, D - PER));
 #pragma unroll
                 for (int j = 0; j < PER; ++j) r[n][j] = u[j];
             }
-        } else if (D % (PER / 2) == 0) {      // by halves
-            typedef T hvec __attribute__((ext_vector_type(PER / 2), aligned(sizeof(T))));
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int c = (int)threadIdx.x + n * NT, row = c / (DP / PER), d = c % (DP / PER) * PER;
-                const T *const p = at + min(row, rows - 1) * stride;
-                const hvec u = *(const hvec *)(p + (d < D ? d : 0)), v = *(const hvec *)(p + (d + PER / 2 < D ? d + PER / 2 : 0));
-#pragma unroll
-                for (int j = 0; j < PER / 2; ++j) r[n][j] = u[j], r[n][PER / 2 + j] = v[j];
-            }
         } else {
+            int thread = threadIdx.x;
+            asm volatile("" : "+v"(thread));      // (what follows from it is not worked out ahead: it would take the registers of tiles that do not come here)
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                const int c = (int)threadIdx.x + n * NT, row = c / (DP / PER), d = c % (DP / PER) * PER;
+                const int c = thread + n * NT, row = c / (DP / PER), d = c % (DP / PER) * PER;
                 T v[PER];
                 mrf_load_part<PER>(at + (row < rows ? row : 0) * stride, d, D, row < rows, v);
 #pragma unroll
@@ -302,19 +300,28 @@ template <class T, int DP, int ROWS, int NT> struct MrfRows {
             }
         }
     }
-    __device__ inline void store(T *lds)
+    __device__ __forceinline__ void store(T *lds)
     {
         if (there >= 0) {
             mrf_stay_branch();
+            typedef unsigned words __attribute__((ext_vector_type(4)));
+            if (entries % PER) {
+                mrf_stay_branch();
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    words w = __builtin_bit_cast(words, r[n]);
+                    mrf_move_down<4>(w, (PER - entries % PER) * (int)sizeof(T), ((int)threadIdx.x + n * NT) % (DP / PER) * PER + PER > entries);
+                    r[n] = __builtin_bit_cast(vec, w);
+                }
+            }
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 const int c = (int)threadIdx.x + n * NT, row = c / (DP / PER), d = c % (DP / PER) * PER;
-                const bool first = row < there && d < entries, second = row < there && d + PER / 2 < entries;
-                unsigned w[4];
-                __builtin_memcpy(w, &r[n], 16);
+                const bool in = row < there && d < entries;
+                words w = __builtin_bit_cast(words, r[n]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) w[j] = (j < 2 ? first : second) ? w[j] : 0u;
-                __builtin_memcpy(&r[n], w, 16);
+                for (int j = 0; j < 4; ++j) w[j] = in ? w[j] : 0u;
+                r[n] = __builtin_bit_cast(vec, w);
             }
         }
 #pragma unroll

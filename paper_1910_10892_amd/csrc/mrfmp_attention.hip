@@ -71,13 +71,13 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
     const T *k = (const T *)P.k + b * P.ks[0] + hk * P.ks[2], *v = (const T *)P.v + b * P.vs[0] + hk * P.vs[2];
     Rows kr, vr;
     typename decltype(line)::Next bias_next = {};
-    const auto load = [&](int t) {
+    const auto load = [&](int t) __attribute__((always_inline)) {
         kr.load(k + (long long)t * KT * P.ks[1], P.ks[1], s.nk - t * KT, P.D);
         vr.load(v + (long long)t * KT * P.vs[1], P.vs[1], s.nk - t * KT, P.D);
         if constexpr (BIAS && !PACK) line.fetch(P, s, h0, (long long)(t + 1) * KT - r0 - (ROWS - 1), bias_next);
         if constexpr (BIAS && PACK) bias_next.bucket = mrf_attn_bucket(P, s, (long long)t * KT - w2 + lane);
     };
-    const auto store = [&](int buf) {
+    const auto store = [&](int buf) __attribute__((always_inline)) {
         kr.store(lds[buf][0]);
         vr.store(lds[buf][1]);
         if constexpr (BIAS && !PACK) line.put(buf, bias_next);

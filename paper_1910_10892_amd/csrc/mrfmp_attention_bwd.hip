@@ -65,12 +65,12 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 || DP == 128 ? 1 : DP == 
     const T *k = (const T *)P.k + b * P.ks[0] + hk * P.ks[2], *v = (const T *)P.v + b * P.vs[0] + hk * P.vs[2];
     Rows kr, vr;
     typename decltype(line)::Next bias_next = {};
-    const auto load = [&](int t) {
+    const auto load = [&](int t) __attribute__((always_inline)) {
         kr.load(k + (long long)t * KT * P.ks[1], P.ks[1], s.nk - t * KT, P.D);
         vr.load(v + (long long)t * KT * P.vs[1], P.vs[1], s.nk - t * KT, P.D);
         if constexpr (BIAS) line.fetch(P, s, h, (long long)(t + 1) * KT - r0 - (ROWS - 1), bias_next);
     };
-    const auto store = [&](int buf) {
+    const auto store = [&](int buf) __attribute__((always_inline)) {
         kr.store(lds[buf][0]);
         vr.store(lds[buf][1]);
         if constexpr (BIAS) line.put(buf, bias_next);
@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 || DP == 128 ? 1 : DP == 
         const int h = hk * P.G + blockIdx.y * group + g;
         const T *q = (const T *)P.q + b * P.qs[0] + h * P.qs[2], *go = (const T *)P.dout + ((long long)b * P.Q * P.Hq + h) * P.D;
         const long long stat = ((long long)b * P.Hq + h) * P.Q;
-        const auto load = [&](int t) {
+        const auto load = [&](int t) __attribute__((always_inline)) {
             qr.load(q + (long long)t * QT * P.qs[1], P.qs[1], s.nq - t * QT, P.D);
             gr.load(go + (long long)t * QT * P.Hq * P.D, (long long)P.Hq * P.D, s.nq - t * QT, P.D);
             if ((int)threadIdx.x < QT) {
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 || DP == 128 ? 1 : DP == 
             }
             if constexpr (BIAS) line.fetch(P, s, h, (long long)k0 - (long long)(t + 1) * QT - (QT - 1), bias_next);
         };
-        const auto store = [&](int buf) {
+        const auto store = [&](int buf) __attribute__((always_inline)) {
             qr.store(lds[buf][0]);
             gr.store(lds[buf][1]);
             if ((int)threadIdx.x < QT) {
