@@ -386,7 +386,10 @@ static AttnPlan attention_plan(const MrfAttnParams &P, int type)
 {
     const long long rows = (long long)P.Q * P.G;
     const int block = type != MRF_F32 && P.D > 64 ? 256 : 128, few = type == MRF_F32 && P.D > 64 ? 64 : 32;      // (as attention_go has it)
-    const bool pack = P.Q <= 16;
+    // Few queries: a wavefront of its own for 32 of them and the heads that share their keys, instead of a workgroup for a head.  47 sequences of 739 keys, 32 heads, us as a
+    // workgroup / as wavefronts: 32 queries of 64 entries 67 / 67 (8 heads on a key head 52 / 37), of 128 151 / 126 (122 / 79), in 32 bits 687 / 389; 64 queries of 64 entries
+    // 73 / 108 (55 / 63), of 128 154 / 227 (127 / 121), in 32 bits 701 / 399; 100 of 128 (144 / 195).
+    const bool pack = P.Q <= 32 || (P.Q <= 64 && P.D > 64 && (type == MRF_F32 || P.G > 1));
     const long long groups = pack ? (long long)P.B * P.Hk * ((rows + few - 1) / few) : (long long)P.B * P.Hq * ((P.Q + block - 1) / block);
     // parts of the keys: for eight wavefronts of few rows on a compute unit, or a workgroup of many; of four tiles at least
     const long long tiles = ((long long)P.K + 31) / 32 / (pack ? 1 : 2);
