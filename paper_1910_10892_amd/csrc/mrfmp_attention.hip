@@ -4,6 +4,11 @@
 // see, tile after tile, in one pass: maximum and sum of the exponentials of a query run along, and what was summed is scaled where the
 // maximum rises.  Scores are formed as keys x queries, so that a lane has a single query: its maximum and sum are within two lanes, and its
 // probabilities are an operand of the second product as they are.
+//
+// What bounds it: with 128 entries the matrix units, fed from LDS at the rate they multiply at; with 32 the exponential and the six operations around it, which take
+// longer than the products; in 32 bits the matrix units.  4 sequences of 2,048, 16 heads, without a mask: heads of 32 in 70 us (490 TFLOP/s), 64 105 (650), 128 154 (890; a
+// plain product of 8,192^3 reaches 1,082); 64 in 32 bits 550 (125; 153).  A single query of 16 heads on each of 16 caches of up to 16,411 keys, 4 heads of 128: 77 us, 4.4
+// TB/s, and 5 to join the parts (a copy reaches 5.1).
 #include "mrfmp_attention.h"
 
 #include <type_traits>
@@ -18,8 +23,8 @@ template <class T> constexpr float mrf_attn_shift_forward() { return mrf_attn_sh
 template <class T> constexpr float mrf_attn_unshift_forward() { return mrf_attn_shift<T>() > 0.0f ? 0x1p-7f : 1.0f; }
 
 // Wavefronts of a SIMD: two, where their registers fit (in 32 bits not for 128 entries); three for heads of up to 64 entries in 16 bits, which wait more than they
-// multiply: 192 sequences of 624 queries, 4 heads of 32 in a band of 255, with a bias, 104 us with two, 75 with three, 89 with four; 4 sequences of up to 2,048, 16 heads
-// of 64, with a bias, 117 us with two, 89 with three, all of 2,048 without a bias 113 and 105, with one 129 and 133 (some of the registers are in memory then).
+// multiply: 192 sequences of 624 queries, 4 heads of 32 in a band of 97, with a bias, 104 us with two, 75 with three, 89 with four; 4 sequences of up to 2,048, 16 heads
+// of 64, with a bias, 117 us with two, 89 with three, all of 2,048 without a bias 113 and 105.
 template <class T, int DP, int NW> constexpr int mrf_attn_waves() { return NW == 1 || (sizeof(T) == 4 && DP == 128) ? 1 : sizeof(T) == 2 && DP <= 64 ? 3 : 2; }
 
 // Wavefronts of a workgroup for many queries: with eight, a tile of keys and values of 128 entries takes half the registers on its way to LDS, and two wavefronts

@@ -7,6 +7,10 @@
 //   keys     a workgroup has 128 keys of a head of keys and goes through the queries of all heads that share it:  scores, dP, dv, dk; and, for the table's
 //            gradient, sums of dS down the diagonals (below).
 // Five products would do; the scores and dP are formed twice, which spares sums over workgroups in an order that changes.
+//
+// What bounds it: matrix units and LDS, with what a wavefront does between its products beside them only where two or three share a SIMD (heads of 128 have the registers of
+// one).  4 sequences of 2,048, 16 heads, without a mask, queries / keys in us: heads of 32 107 / 132, 64 194 / 223 (four products each: 710 / 620 TFLOP/s), 128 340 / 435
+// (810 / 630); 64 in 32 bits 830 / 1,275.  With a bias and its table's gradient heads of 64 take 200 / 295.
 #include "mrfmp_attention.h"
 
 #include <type_traits>
@@ -178,7 +182,7 @@ __host__ __device__ constexpr int mrf_skew(int row) { return 63 * row + 32 * ((r
 constexpr int MRF_SKEWED = mrf_skew(31) + 63;
 
 // Wavefronts of a SIMD.  Heads of up to 32 entries wait for the look-ups and for LDS more than for products: 192 sequences of 624 keys, 4 heads of 32 in a
-// band of 255, take 146 us with three and 177 with two; the queries' kernel 98 with three, 120 with four, 125 with two.  Heads of 64 have no room for three: the queries'
+// band of 97, take 146 us with three and 177 with two; the queries' kernel 98 with three, 120 with four, 125 with two.  Heads of 64 have no room for three: the queries'
 // kernel takes 482 us then instead of 194 (4 sequences of 2,048, 16 heads).
 //
 // DK, DV: which of the two it sums.  Both, where their sums and the keys and values fit into the registers, else one launch for each.

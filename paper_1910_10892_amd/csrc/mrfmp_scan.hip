@@ -6,7 +6,9 @@
 // element is read once, and few channels still make many wavefronts.  Some 20 operations and two transcendental ones an element: bound by memory.
 // Where there are too few channels for that, the steps are divided into chunks: a first launch finds what each does, a second one strings that
 // together, and the third goes through the steps again.  The states before every MRF_SCAN_STEPS-th step are kept for the backward pass, in 32 bits:
-// it forms the steps between them again in registers, whatever the type of y.
+// it forms the steps between them again in registers, whatever the type of y.  4 x 512 steps of 16,384 channels, 16 bits: forward 56 us (3.7 TB/s), backward 88 (3.9), in 32
+// bits 222 together (4.8; a copy reaches 5.1); 65,537 steps of 256 channels, 32 bits, divided: forward 37 + 8 + 34, backward 25 + 8 + 67.  Four channels a lane in 16 bits
+// took twice as long (333 us instead of 147: half the wavefronts, and registers in memory).
 #include "mrfmp_rows.h"
 
 #include <type_traits>
