@@ -3,7 +3,9 @@ of the paper: the final costs c of ISGMR / TRWP as a differentiable function of 
 potentials, the edge weights and the pairwise function.
 
 layer_norm, bucket_pairwise and policy_loss wrap the learning operators around it in the same way:
-scores to unaries, a few values to a pairwise function, rewards to a gradient of the costs.
+scores to unaries, a few values to a pairwise function, rewards to a gradient of the costs.  So do
+attention, head_rotation, gated_scan and scanline_scan with the sequence operators in front of them.  (A backward
+pass that is captured into a graph: with torch.autograd.grad, while no eager graph of the same leaves lives.)
 
 Marshalling only: the forward call is mrf_isgmr_forward / mrf_trwp_forward (which store the
 argmin indices p, q, Alg. 1 / 2), the backward call is mrf_isgmr_backward /
@@ -264,21 +266,22 @@ def _given(name, **tensors):
                 raise ValueError("%s has no gradient with respect to %s: detach it" % (name, what))
 
 
+_GIVEN = ("query_offsets", "q_lengths", "k_lengths", "bucket_of")      # kept for the backward call, which notices if they have changed
+
+
 class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, table, how):
-        scale, band, query_offset, query_offsets, q_lengths, k_lengths, bucket_of, map_offset, heads_last = how
+        scale, make, *given = how
         q, k, v = (_dense_last(t) for t in (q, k, v))
         table = None if table is None else table.contiguous()
-        make = dict(first_offset=band[0], last_offset=band[1], query_offset=query_offset, query_offsets=query_offsets, q_lengths=q_lengths, k_lengths=k_lengths,
-                    bucket_of=bucket_of, map_offset=map_offset, heads_last=heads_last)
-        att = _m.MrfAttention(q, k, v, scale, table=table, **make)
+        att = _m.MrfAttention(q, k, v, scale, table=table, **make, **dict(zip(_GIVEN, given)))
         B, Q, K, Hq, Hk, D = att.shape
         out = torch.empty((B, Q, Hq, D), dtype=q.dtype, device=q.device)
         lse = torch.empty((B, Hq, Q), dtype=torch.float32, device=q.device)
         n = _m.mrf_attention_workspace_bytes(att, False)
         _m.mrf_attention_forward(att, out, lse, torch.empty(n, dtype=torch.uint8, device=q.device) if n else None)
-        ctx.save_for_backward(q, k, v, table, out, lse)
+        ctx.save_for_backward(q, k, v, table, out, lse, *given)
         ctx.scale, ctx.make = scale, make
         ctx.mark_non_differentiable(lse)
         return out, lse
@@ -286,8 +289,8 @@ class _Attention(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, grad_out, _grad_lse):
-        q, k, v, table, out, lse = ctx.saved_tensors
-        att = _m.MrfAttention(q, k, v, ctx.scale, table=table, **ctx.make)
+        q, k, v, table, out, lse, *given = ctx.saved_tensors
+        att = _m.MrfAttention(q, k, v, ctx.scale, table=table, **ctx.make, **dict(zip(_GIVEN, given)))
         dense = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
         gq, gk, gv, gt = (dense(t) if need else None for t, need in zip((q, k, v, table), ctx.needs_input_grad[:4]))
         ws = torch.empty(_m.mrf_attention_workspace_bytes(att, True), dtype=torch.uint8, device=q.device)
@@ -303,8 +306,8 @@ def attention(q, k, v, *, scale=None, causal=False, first_offset=None, last_offs
     if causal and last_offset is not None:
         raise ValueError("causal and last_offset exclude each other")
     query_offsets, q_lengths, k_lengths, bucket_of = (None if t is None else t.contiguous() for t in (query_offsets, q_lengths, k_lengths, bucket_of))
-    return _Attention.apply(q, k, v, table, (float(q.shape[-1] ** -0.5 if scale is None else scale), (first_offset, 0 if causal else last_offset), int(query_offset),
-                                             query_offsets, q_lengths, k_lengths, bucket_of, int(map_offset), bool(heads_last)))
+    make = dict(first_offset=first_offset, last_offset=0 if causal else last_offset, query_offset=int(query_offset), map_offset=int(map_offset), heads_last=bool(heads_last))
+    return _Attention.apply(q, k, v, table, (float(q.shape[-1] ** -0.5 if scale is None else scale), make, query_offsets, q_lengths, k_lengths, bucket_of))
 
 
 class _HeadRotation(torch.autograd.Function):

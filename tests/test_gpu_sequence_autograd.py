@@ -174,3 +174,64 @@ def test_scanlines_to_labels_and_back():
             moved = [{n: p + (s * step / size ** 0.5 * p.grad if n in smooth else 0.0) for n, p in params.items()} for s in (1, -1)]
             ratios.append((float(loss(moved[0])) - float(loss(moved[1]))) / (2 * step * size ** 0.5))
     assert abs(float(np.median(ratios)) - 1.0) < 0.1, ratios
+
+
+def test_lengths_that_change_before_the_backward_pass_are_noticed():
+    import torch
+    from paper_1910_10892_amd.autograd import attention, gated_scan, head_rotation
+    x = torch.randn(2, 6, 2, 8, device="cuda:0", requires_grad=True)
+    int32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda:0")  # noqa: E731
+    table = torch.zeros(2, 3, device="cuda:0")
+    for name in ("q_lengths", "k_lengths", "query_offsets", "bucket_of"):
+        n = int32(4, 5)
+        out, _ = attention(x, x, x, **{name: n}, **({"table": table} if name == "bucket_of" else {}))
+        n.add_(1)
+        with pytest.raises(RuntimeError, match="inplace"):
+            out.sum().backward()
+    n = int32(4, 5)
+    y, _ = gated_scan(x.flatten(2), x.flatten(2), lengths=n)
+    n.add_(1)
+    with pytest.raises(RuntimeError, match="inplace"):
+        y.sum().backward()
+    at = torch.zeros(2, 6, dtype=torch.int32, device="cuda:0")
+    q, _ = head_rotation(x, x, inv_freq=torch.ones(4, device="cuda:0"), positions=at)
+    at.add_(1)
+    with pytest.raises(RuntimeError, match="inplace"):
+        q.sum().backward()
+
+
+def test_both_passes_through_autograd_captured_into_a_graph():
+    """Captured with torch.autograd.grad; every replay gives the bits of an eager pass on the same inputs."""
+    import torch
+    import paper_1910_10892_amd as mrf
+    from paper_1910_10892_amd.autograd import attention, gated_scan, head_rotation
+    B, T, H, D = 2, 70, 2, 16
+    x, z, up, table = (torch.randn(s, device="cuda:0") for s in ((B, T, 3 * H, D), (B, T, H * D), (B, T, H * D), (H, 8)))
+    bucket_of = torch.from_numpy(mrf.mrf_distance_buckets(8, 64, -(T - 1), 2 * T - 1)).cuda()
+    gamma, freq = torch.ones(D, device="cuda:0"), torch.linspace(1.0, 0.1, D // 2, device="cuda:0")
+
+    def both():
+        leaves = [t.detach().requires_grad_(True) for t in (x, z, table, gamma)]
+        a, g, tab, gam = leaves
+        q, k = head_rotation(a[:, :, :H], a[:, :, H:2 * H], gam, gam, inv_freq=freq)
+        out, _ = attention(q, k, a[:, :, 2 * H:], causal=True, table=tab, bucket_of=bucket_of, map_offset=-(T - 1))
+        y, _ = gated_scan(out.flatten(2), g)
+        return [y.detach(), *torch.autograd.grad(y, leaves, up)]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = both()
+    for n in range(4):
+        for t in (x, z, up, table):
+            t.copy_(torch.randn(t.shape, generator=torch.Generator(device="cuda:0").manual_seed(n), device="cuda:0"))
+        want = both()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want, captured):
+            assert torch.isfinite(a).all() and torch.equal(a, b)
