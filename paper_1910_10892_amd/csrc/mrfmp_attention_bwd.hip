@@ -184,10 +184,11 @@ constexpr int MRF_SKEWED = mrf_skew(31) + 63;
 // Wavefronts of a SIMD.  Heads of up to 32 entries wait for the look-ups and for LDS more than for products: 192 sequences of 624 keys, 4 heads of 32 in a
 // band of 97, take 146 us with three and 177 with two; the queries' kernel 98 with three, 120 with four, 125 with two.  Heads of 64 have no room for three: the queries'
 // kernel takes 482 us then instead of 194 (4 sequences of 2,048, 16 heads).
+// Heads of 128 have room for two where dv is a launch of its own: 2 sequences of 4,160, 4 heads on one of 128, 208 us instead of 380.
 //
 // DK, DV: which of the two it sums.  Both, where their sums and the keys and values fit into the registers, else one launch for each.
 template <class T, int DP, bool BIAS, bool TABLE, bool DK, bool DV>
-__global__ void __launch_bounds__(256, (sizeof(T) == 4 || DP == 128 ? 1 : DP == 64 ? 2 : 3)) mrf_attn_bwd_keys(const MrfAttnParams P)
+__global__ void __launch_bounds__(256, (sizeof(T) == 4 || (DP == 128 && DK) ? 1 : DP >= 64 ? 2 : 3)) mrf_attn_bwd_keys(const MrfAttnParams P)
 {
     constexpr int QT = mrf_attn_bwd_rows<T>(), NT = 256, KEYS = 128, LINE = KEYS + QT;
     typedef MrfRows<T, DP, QT, NT> Rows;
