@@ -396,9 +396,10 @@ static AttnPlan attention_plan(const MrfAttnParams &P, int type)
     // 73 / 108 (55 / 63), of 128 154 / 227 (127 / 121), in 32 bits 701 / 399; 100 of 128 (144 / 195).
     const bool pack = P.Q <= 32 || (P.Q <= 64 && P.D > 64 && (type == MRF_F32 || P.G > 1));
     const long long groups = pack ? (long long)P.B * P.Hk * ((rows + few - 1) / few) : (long long)P.B * P.Hq * ((P.Q + block - 1) / block);
-    // parts of the keys: for eight wavefronts of few rows on a compute unit, or a workgroup of many; of four tiles at least
+    // parts of the keys: for eight wavefronts of few rows on a compute unit, or a workgroup of many (two, where heads are short and keys enough to pay for joining the parts:
+    // 4,096 queries and keys, 4 heads of 64, 52 us with one and 45 with two, with a bias 70 and 53; 300 queries on 3,000 keys, 16 heads, 22 and 25); of four tiles at least
     const long long tiles = ((long long)P.K + 31) / 32 / (pack ? 1 : 2);
-    long long splits = groups ? (pack ? 2048 : 256) / groups : 1;
+    long long splits = groups ? (pack ? 2048 : P.D <= 64 && P.K >= 4096 ? 512 : 256) / groups : 1;
     if (splits > tiles / 4) splits = tiles / 4;
     if (splits > MRF_ATTN_SPLITS) splits = MRF_ATTN_SPLITS;
     return {pack, (int)(splits < 1 ? 1 : splits), (unsigned)groups};

@@ -208,7 +208,7 @@ def test_attention_of_parts_of_a_projection(how, dtype):
 
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("B,Q,K,Hq,Hk,D", [(1, 1, 4099, 16, 4, 128), (3, 1, 5000, 8, 8, 64), (2, 1, 1, 4, 1, 32), (2, 5, 3000, 35, 5, 20), (1, 16, 700, 8, 1, 40),
-                                           (1, 2, 20000, 2, 1, 16), (1, 33, 2000, 2, 1, 64), (2, 32, 300, 6, 2, 24), (1, 27, 1300, 3, 3, 103), (2, 61, 500, 10, 2, 128), (1, 64, 200, 2, 2, 70)])
+                                           (1, 2, 20000, 2, 1, 16), (1, 33, 2000, 2, 1, 64), (2, 32, 300, 6, 2, 24), (1, 27, 1300, 3, 3, 103), (1, 140, 4200, 2, 2, 48), (2, 61, 500, 10, 2, 128), (1, 64, 200, 2, 2, 70)])
 def test_attention_of_few_queries_on_a_long_cache(B, Q, K, Hq, Hk, D, dtype):
     offsets = [-(17 * b) for b in range(B)]
     n = [K + o for o in offsets]
