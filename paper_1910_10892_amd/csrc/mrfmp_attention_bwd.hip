@@ -274,7 +274,9 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 || (DP == 128 && DK) ? 1 
             const int from = j - s.hi - q0, to = j < s.nk ? min(j - s.lo + 1, s.nq) - q0 : 0;
             const bool flat = !BIAS || line.flat(buf);
             const float times = flat ? P.c : 1.0f, level = BIAS && flat ? line.value[buf][0] : 0.0f;
-#pragma unroll 1
+            // (heads of 128: 432 us and 420 for 4 sequences of 2,048, 16 heads; the queries' kernel, which has more to keep, 343 and 416)
+            constexpr int TOGETHER = sizeof(T) == 2 && DP == 128 && DK && DV ? 2 : 1;
+#pragma unroll TOGETHER
             for (int u = 0; u < U; ++u) {
                 float sum = goes_on;
                 if (any) {
