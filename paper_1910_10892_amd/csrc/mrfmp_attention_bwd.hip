@@ -19,12 +19,12 @@ template <class T> constexpr int mrf_attn_bwd_rows() { return sizeof(T) == 4 ? 3
 
 template <class F> struct MrfTwo { F a, b; };
 
-// steps whose operands are read ahead together
-template <class T, int DP> constexpr int mrf_attn_group() { return sizeof(T) == 4 ? 1 : DP == 128 ? 4 : 2; }
+// steps whose operands are read ahead together (of 128 entries, 4 sequences of 2,048, 16 heads: two 338 and 412 us, four 342 and 420, eight 344 and 423)
+template <class T, int DP> constexpr int mrf_attn_group() { return sizeof(T) == 4 ? 1 : 2; }
 
 // ---- dq, and delta
 template <class T, int DP, bool BIAS>
-__global__ void __launch_bounds__(256, (sizeof(T) == 4 || DP == 128 ? 1 : DP == 64 ? 2 : 3)) mrf_attn_bwd_queries(const MrfAttnParams P)
+__global__ void __launch_bounds__(256, (sizeof(T) == 4 || DP == 128 ? 1 : 2)) mrf_attn_bwd_queries(const MrfAttnParams P)
 {
     constexpr int KT = mrf_attn_bwd_rows<T>(), NT = 256, ROWS = 128, LINE = ROWS + KT;
     typedef MrfRows<T, DP, KT, NT> Rows;
@@ -182,8 +182,8 @@ __host__ __device__ constexpr int mrf_skew(int row) { return 63 * row + 32 * ((r
 constexpr int MRF_SKEWED = mrf_skew(31) + 63;
 
 // Wavefronts of a SIMD.  Heads of up to 32 entries wait for the look-ups and for LDS more than for products: 192 sequences of 624 keys, 4 heads of 32 in a
-// band of 97, take 146 us with three and 177 with two; the queries' kernel 98 with three, 120 with four, 125 with two.  Heads of 64 have no room for three: the queries'
-// kernel takes 482 us then instead of 194 (4 sequences of 2,048, 16 heads).
+// band of 97, take 146 us with three and 177 with two.  Heads of 64 have no room for three (nor has the queries' kernel: 482 us then instead of 194 for 4 sequences
+// of 2,048, 16 heads of 64; for heads of 32 three are as fast as two).
 // Heads of 128 have room for two where dv is a launch of its own: 2 sequences of 4,160, 4 heads on one of 128, 208 us instead of 380.
 //
 // DK, DV: which of the two it sums.  Both, where their sums and the keys and values fit into the registers, else one launch for each.
