@@ -9,8 +9,8 @@
 // Five products would do; the scores and dP are formed twice, which spares sums over workgroups in an order that changes.
 //
 // What bounds it: matrix units and LDS, with what a wavefront does between its products beside them only where two or three share a SIMD (heads of 128 have the registers of
-// one).  4 sequences of 2,048, 16 heads, without a mask, queries / keys in us: heads of 32 107 / 132, 64 194 / 223 (four products each: 710 / 620 TFLOP/s), 128 340 / 435
-// (810 / 630); 64 in 32 bits 830 / 1,275.  With a bias and its table's gradient heads of 64 take 200 / 295.
+// one).  4 sequences of 2,048, 16 heads, without a mask, queries / keys in us: heads of 32 107 / 132, 64 194 / 223 (four products each: 710 / 620 TFLOP/s), 128 338 / 412
+// (810 / 670); 64 in 32 bits 830 / 1,275.  With a bias and its table's gradient heads of 64 take 200 / 295.
 #include "mrfmp_attention.h"
 
 #include <type_traits>
