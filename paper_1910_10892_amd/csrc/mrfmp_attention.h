@@ -402,6 +402,14 @@ template <class T, int DP, int LD> struct MrfPlaces {
     }
 };
 
+// A sum of many terms: what an addition rounds off (`lost`) is taken off the next term
+__device__ inline void mrf_add(float &sum, float &lost, float term)
+{
+    const float more = term - lost, all = sum + more;
+    lost = (all - sum) - more;
+    sum = all;
+}
+
 // Probabilities are at most 1, and most of many keys far below: for a product in MRF_F16 they are taken times 2^15, where all that matter keep their digits
 // (2^-14, the least number with all of them, would be a probability already with 16,384 keys).
 template <class T> constexpr float mrf_attn_shift() { return 0.0f; }

@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 || DP == 128 ? 1 : 2)) mr
 #pragma unroll
         for (int e = 0; e < 16; ++e) dq[d][e] = mean[MEAN ? d : 0][e] = 0.0f;
     MrfRange<T> range;
-    float left = 0.0f;      // sum of dS
+    float left = 0.0f, lost = 0.0f;      // sum of dS, a block of 32 keys at a time: it rises and falls again, and what is left shall be no roundings of its way
 
     if (t0 < t1) {
         if constexpr (BIAS) line.ahead(P, s, (long long)t0 * KT - r0 - (ROWS - 1), bias_next);
@@ -127,11 +127,13 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 || DP == 128 ? 1 : 2)) mr
 #pragma unroll
                     for (int e = 0; e < 16; ++e) c[e] = mrf_keep(mrf_row_bits(rows_in, e), c[e]);
                 }
+                float of_block = 0.0f;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     dp[e] = c[e] * (dp[e] - delta);
-                    left += dp[e];
+                    of_block += dp[e];
                 }
+                mrf_add(left, lost, of_block);
                 range.fit(dp, dq);
                 const frag sf[2] = {mrf_acc_frag<T>(dp, 0), mrf_acc_frag<T>(dp, 1)}, pf[2] = {mrf_acc_frag<T>(c, 0), mrf_acc_frag<T>(c, 1)};
                 mrf_ahead<STEPS, mrf_attn_group<T, DP>()>([&](int n) { return places.across(at + 16 * (n / (DP / 32)) * Rows::LD, n % (DP / 32)); },
