@@ -29,6 +29,14 @@ __device__ inline mrf_acc mrf_mma(const MrfFrag<float>::type &a, const MrfFrag<f
     return c;
 }
 
+// Sums over many tiles.  In 32 bits a tile's product is a sum of its own, and these are added in 64 bits (a conversion and an addition an entry and tile, and twice the registers: 4
+// sequences of 2,048, 16 heads of 64, forward 549 -> 607 us, both passes 2,640 -> 2,930; placed one by one between the matrix instructions of the next block, 612 and 2,980).  Terms
+// of one sign and size are rounded the same way each time: 32,768 of them, each added to all before it, were off by 2e-4 of their sum.  In 16 bits a matrix instruction adds 16
+// terms at once to what it has summed, and the terms' own roundings (2^-9 or 2^-12 of each) are more than that leaves.
+typedef double mrf_long_acc __attribute__((ext_vector_type(16)));
+template <class T> struct MrfSum { typedef mrf_acc type; };
+template <> struct MrfSum<float> { typedef mrf_long_acc type; };
+
 __device__ inline int mrf_acc_row(int e, int half) { return 8 * (e / 4) + 4 * half + e % 4; }
 
 template <class T> __device__ inline typename MrfFrag<T>::type mrf_acc_frag(const mrf_acc &c, int t)
@@ -432,7 +440,7 @@ __device__ inline float mrf_halves_max(float v)
 // falls.  Other types have the range of 32 bits.
 template <class T> struct MrfRange {
     float f = 1.0f, top = 0.0f;      // the factor; values up to `top` are in range with it
-    template <int N> __device__ inline void fit(mrf_acc &x, mrf_acc (&sums)[N])
+    template <class Sum, int N> __device__ inline void fit(mrf_acc &x, Sum (&sums)[N])
     {
         if constexpr (sizeof(T) == 2 && mrf_attn_shift<T>() != 0.0f) {
             float big = 0.0f;
@@ -458,6 +466,21 @@ template <class T> struct MrfRange {
     }
     __device__ inline float undo() const { return 1.0f / f; }
 };
+
+// In 32 bits: what a tile of 32 rows at `rows` adds to the sums, f being its other operand (parts 0 and 1 of 16 rows)
+template <int DP, class Places, int N> __device__ inline void mrf_add_block(const Places &places, const float *rows, int ld, const MrfFrag<float>::type (&f)[2], mrf_long_acc (&sums)[N])
+{
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) {
+        mrf_acc x;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = 0.0f;
+#pragma unroll
+        for (int y = 0; y < 2; ++y) x = mrf_mma(places.across(rows + 16 * y * ld, d), f[y], x);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sums[d][e] += x[e];
+    }
+}
 
 // entries d .. d + 3 of a row of D
 template <class T> __device__ inline void mrf_store4(T *row, int d, int D, const float (&v)[4])

@@ -89,7 +89,7 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
         if constexpr (BIAS && PACK) ids[buf][wv][lane] = bias_next.bucket;
     };
 
-    mrf_acc o[DP / 32];
+    typename MrfSum<T>::type o[DP / 32];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
@@ -186,10 +186,9 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
                 m = top;
             }
             const float low = (m == -INFINITY ? 0.0f : m) - mrf_attn_shift_forward<T>() - plus;
-            // 16 keys at a time: their probabilities, and their values on the way, while those before are multiplied
-            frag vf[2][DP / 32], p[2];
+            frag p[2];
             float of_tile = 0.0f;
-            const auto part = [&](int y) {
+            const auto probabilities = [&](int y) {
                 mrf_acc &x = c[y / 2];
 #pragma unroll
                 for (int e = 8 * (y % 2); e < 8 * (y % 2) + 8; ++e) {
@@ -197,17 +196,29 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
                     of_tile += x[e];
                 }
                 p[y % 2] = mrf_acc_frag<T>(x, y % 2);
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d) vf[y % 2][d] = places.across(lds[0][1] + 16 * y * Rows::LD, d);
             };
-            part(0);
-            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (sizeof(T) == 4) {
+                static_assert(KT == 32, "two parts");
+                probabilities(0);
+                probabilities(1);
+                mrf_add_block<DP>(places, lds[0][1], Rows::LD, p, o);
+            } else {
+                // 16 keys at a time: their probabilities, and their values on the way, while those before are multiplied
+                frag vf[2][DP / 32];
+                const auto part = [&](int y) {
+                    probabilities(y);
 #pragma unroll
-            for (int y = 0; y < KT / 16; ++y) {
-                if (y + 1 < KT / 16) part(y + 1);
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d) o[d] = mrf_mma(vf[y % 2][d], p[y % 2], o[d]);
+                    for (int d = 0; d < DP / 32; ++d) vf[y % 2][d] = places.across(lds[0][1] + 16 * y * Rows::LD, d);
+                };
+                part(0);
                 __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int y = 0; y < KT / 16; ++y) {
+                    if (y + 1 < KT / 16) part(y + 1);
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) o[d] = mrf_mma(vf[y % 2][d], p[y % 2], o[d]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
             mrf_add(l, lost, of_tile);
         }
@@ -227,7 +238,7 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
             for (int e = 0; e < 16; e += 4) {
                 float x[4];
 #pragma unroll
-                for (int n = 0; n < 4; ++n) x[n] = o[d][e + n] * mrf_attn_unshift_forward<T>();
+                for (int n = 0; n < 4; ++n) x[n] = (float)o[d][e + n] * mrf_attn_unshift_forward<T>();
                 mrf_store4(part, 32 * d + mrf_acc_row(e, half), P.D, x);
             }
         if (half == 0) ((float2 *)P.part)[blockIdx.y * n + at] = make_float2(m, l);
@@ -239,7 +250,7 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
-            const float x[4] = {o[d][e] * inv, o[d][e + 1] * inv, o[d][e + 2] * inv, o[d][e + 3] * inv};
+            const float x[4] = {(float)o[d][e] * inv, (float)o[d][e + 1] * inv, (float)o[d][e + 2] * inv, (float)o[d][e + 3] * inv};
             mrf_store4(out, 32 * d + mrf_acc_row(e, half), P.D, x);
         }
     if (half == 0 && P.lse) P.lse[((long long)b * P.Hq + h) * P.Q + i] = l == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;

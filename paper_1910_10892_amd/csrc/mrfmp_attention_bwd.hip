@@ -80,11 +80,12 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 || DP == 128 ? 1 : 2)) mr
         if constexpr (BIAS) line.put(buf, bias_next);
     };
     constexpr bool MEAN = sizeof(T) == 2;
-    mrf_acc dq[DP / 32], mean[MEAN ? DP / 32 : 1];      // sums of dS k, and of P k
+    typename MrfSum<T>::type dq[DP / 32];      // sums of dS k, and of P k
+    mrf_acc mean[MEAN ? DP / 32 : 1];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) dq[d][e] = mean[MEAN ? d : 0][e] = 0.0f;
+        for (int e = 0; e < 16; ++e) dq[d][e] = 0.0f, mean[MEAN ? d : 0][e] = 0.0f;
     MrfRange<T> range;
     float left = 0.0f, lost = 0.0f;      // sum of dS, a block of 32 keys at a time: it rises and falls again, and what is left shall be no roundings of its way
 
@@ -136,12 +137,15 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 || DP == 128 ? 1 : 2)) mr
                 mrf_add(left, lost, of_block);
                 range.fit(dp, dq);
                 const frag sf[2] = {mrf_acc_frag<T>(dp, 0), mrf_acc_frag<T>(dp, 1)}, pf[2] = {mrf_acc_frag<T>(c, 0), mrf_acc_frag<T>(c, 1)};
-                mrf_ahead<STEPS, mrf_attn_group<T, DP>()>([&](int n) { return places.across(at + 16 * (n / (DP / 32)) * Rows::LD, n % (DP / 32)); },
-                                                          [&](int n, const frag &f) {
-                                                              const int x = n / (DP / 32), d = n % (DP / 32);
-                                                              dq[d] = mrf_mma(f, sf[x], dq[d]);
-                                                              if constexpr (MEAN) mean[MEAN ? d : 0] = mrf_mma(f, pf[x], mean[MEAN ? d : 0]);
-                                                          });
+                if constexpr (MEAN)
+                    mrf_ahead<STEPS, mrf_attn_group<T, DP>()>([&](int n) { return places.across(at + 16 * (n / (DP / 32)) * Rows::LD, n % (DP / 32)); },
+                                                              [&](int n, const frag &f) {
+                                                                  const int x = n / (DP / 32), d = n % (DP / 32);
+                                                                  dq[d] = mrf_mma(f, sf[x], dq[d]);
+                                                                  mean[d] = mrf_mma(f, pf[x], mean[d]);
+                                                              });
+                else
+                    mrf_add_block<DP>(places, at, Rows::LD, sf, dq);
             }
         }
         if (t + 1 < t1) store(buf ^ 1);
@@ -160,7 +164,7 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 || DP == 128 ? 1 : 2)) mr
         for (int e = 0; e < 16; e += 4) {
             float x[4];
 #pragma unroll
-            for (int n = 0; n < 4; ++n) x[n] = (MEAN ? fmaf(-left, mean[MEAN ? d : 0][e + n], dq[d][e + n] * undo) : dq[d][e + n]) * scale;
+            for (int n = 0; n < 4; ++n) x[n] = (MEAN ? fmaf(-left, mean[MEAN ? d : 0][e + n], (float)dq[d][e + n] * undo) : (float)dq[d][e + n]) * scale;
             mrf_store4(out, 32 * d + mrf_acc_row(e, half), P.D, x);
         }
 }
@@ -223,11 +227,11 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 || (DP == 128 && DK) ? 1 
     }
     if constexpr (TABLE)
         for (int n = lane; n < MRF_SKEWED; n += 64) skew[wv][n] = 0.0f;
-    mrf_acc dk[DK ? DP / 32 : 1], dv[DV ? DP / 32 : 1];
+    typename MrfSum<T>::type dk[DK ? DP / 32 : 1], dv[DV ? DP / 32 : 1];
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) dk[DK ? d : 0][e] = dv[DV ? d : 0][e] = 0.0f;
+        for (int e = 0; e < 16; ++e) dk[DK ? d : 0][e] = 0.0f, dv[DV ? d : 0][e] = 0.0f;
 
     MrfRange<T> range;
     Rows qr, gr;
@@ -351,19 +355,24 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 || (DP == 128 && DK) ? 1 
                         sf[0] = mrf_acc_frag<T>(dp, 0), sf[1] = mrf_acc_frag<T>(dp, 1);
                     }
                     if constexpr (DV) pf[0] = mrf_acc_frag<T>(c, 0), pf[1] = mrf_acc_frag<T>(c, 1);
-                    mrf_ahead<STEPS, mrf_attn_group<T, DP>()>(
-                        [&](int n) {
-                            const T *const row = at + 16 * (n / (DP / 32)) * Rows::LD;
-                            MrfTwo<frag> f = {};
-                            if constexpr (DV) f.a = places.across(row + TILE, n % (DP / 32));
-                            if constexpr (DK) f.b = places.across(row, n % (DP / 32));
-                            return f;
-                        },
-                        [&](int n, const MrfTwo<frag> &f) {
-                            const int x = n / (DP / 32), d = n % (DP / 32);
-                            if constexpr (DV) dv[DV ? d : 0] = mrf_mma(f.a, pf[x], dv[DV ? d : 0]);
-                            if constexpr (DK) dk[DK ? d : 0] = mrf_mma(f.b, sf[x], dk[DK ? d : 0]);
-                        });
+                    if constexpr (sizeof(T) == 4) {
+                        if constexpr (DV) mrf_add_block<DP>(places, at + TILE, Rows::LD, pf, dv);
+                        if constexpr (DK) mrf_add_block<DP>(places, at, Rows::LD, sf, dk);
+                    } else {
+                        mrf_ahead<STEPS, mrf_attn_group<T, DP>()>(
+                            [&](int n) {
+                                const T *const row = at + 16 * (n / (DP / 32)) * Rows::LD;
+                                MrfTwo<frag> f = {};
+                                if constexpr (DV) f.a = places.across(row + TILE, n % (DP / 32));
+                                if constexpr (DK) f.b = places.across(row, n % (DP / 32));
+                                return f;
+                            },
+                            [&](int n, const MrfTwo<frag> &f) {
+                                const int x = n / (DP / 32), d = n % (DP / 32);
+                                if constexpr (DV) dv[DV ? d : 0] = mrf_mma(f.a, pf[x], dv[DV ? d : 0]);
+                                if constexpr (DK) dk[DK ? d : 0] = mrf_mma(f.b, sf[x], dk[DK ? d : 0]);
+                            });
+                    }
                 }
                 if constexpr (TABLE) {
                     if (half == 0) to_line[q0 + 32 * u + lane] = sum * mrf_attn_unshift<T>();
@@ -392,13 +401,13 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 || (DP == 128 && DK) ? 1 
             const int at = 32 * d + mrf_acc_row(e, half);
             if constexpr (DK) {
 #pragma unroll
-                for (int n = 0; n < 4; ++n) x[n] = dk[DK ? d : 0][e + n] * ks;
+                for (int n = 0; n < 4; ++n) x[n] = (float)dk[DK ? d : 0][e + n] * ks;
                 if (P.shares > 1) mrf_store4(P.share + 2 * blockIdx.y * all + row, at, P.D, x);
                 else if (P.dk) mrf_store4((T *)P.dk + row, at, P.D, x);
             }
             if constexpr (DV) {
 #pragma unroll
-                for (int n = 0; n < 4; ++n) x[n] = dv[DV ? d : 0][e + n] * vs;
+                for (int n = 0; n < 4; ++n) x[n] = (float)dv[DV ? d : 0][e + n] * vs;
                 if (P.shares > 1) mrf_store4(P.share + (2 * blockIdx.y + 1) * all + row, at, P.D, x);
                 else if (P.dv) mrf_store4((T *)P.dv + row, at, P.D, x);
             }

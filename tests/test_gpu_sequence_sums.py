@@ -3,7 +3,7 @@ quarter of n units in the last place.  Held to the same SUM u as every other sum
 import numpy as np
 import pytest
 
-from test_gpu_sequence import TYPES, _attention_bounds, _close, _np
+from test_gpu_sequence import SUM, TYPES, U, _attention_bounds, _close, _np
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +49,74 @@ def _many_keys(D, level, same, dtype):
 def test_sum_over_many_keys_of_one_probability(D, level, dtype):
     _, lse = _many_keys(D, level, False, dtype)
     _close(*lse, what="lse")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("same", [True, False])
+@pytest.mark.parametrize("level", [0.7, 0.9])
+@pytest.mark.parametrize("D", [8, 64, 128])
+def test_values_of_many_keys_of_one_probability(D, level, same, dtype):
+    out, _ = _many_keys(D, level, same, dtype)
+    _close(*out, dtype, "out")
+
+
+def _backward(att, g, Q, K, D, dtype, grad_table=None):
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    T = getattr(torch, dtype)
+    out, lse = torch.empty(1, Q, 1, D, dtype=T, device="cuda:0"), torch.empty(1, 1, Q, device="cuda:0")
+    ws = torch.empty(max(mrf.mrf_attention_workspace_bytes(att, b) for b in (False, True)), dtype=torch.uint8, device="cuda:0")
+    grads = [torch.empty(1, n, 1, D, dtype=T, device="cuda:0") for n in (Q, K, K)]
+    mrf.mrf_attention_forward(att, out, lse, ws)
+    mrf.mrf_attention_backward(att, g, out, lse, *grads, grad_table, ws)
+    return [t[0] for t in grads]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [8, 64, 128])
+def test_gradient_of_a_query_from_many_keys(D, dtype):
+    """dS of one size, of the keys' own sign, on the way to grad_q; it rises and falls again on the way to its own sum, of which nothing is left."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    from oracle import mrf_sequence_oracle as so
+    print("case one query's gradient", D, dtype, flush=True)
+    K, Q = 32768, 3
+    sign = np.where(np.arange(K) < K // 2, 1.0, -1.0)
+    q, k, v, g = np.zeros((1, Q, 1, D)), np.zeros((1, K, 1, D)), np.zeros((1, K, 1, D)), np.zeros((1, Q, 1, D))
+    k[0, :, 0, 1:], v[0, :, 0, 0], g[..., 0] = 1.3 * sign[:, None], 1.1 * sign, 0.9
+    (q, qn), (k, kn), (v, vn), (g, gn) = (_values(x, dtype) for x in (q, k, v, g))
+    att = mrf.MrfAttention(q, k, v, 0.35)
+    ok, _ = so.attention_pairs(Q, K)
+    want, _, _ = _attention_bounds(qn[0], kn[0], vn[0], gn[0], float(att.c.scale), ok, None, dtype, so)
+    for name, got in zip(("grad_q", "grad_k", "grad_v"), _backward(att, g, Q, K, D, dtype)):
+        _close(got, *want[name], dtype, name)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("with_table", [False, True])
+@pytest.mark.parametrize("D", [8, 64, 128])
+def test_gradients_of_keys_from_many_queries(D, with_table, dtype):
+    """All queries are the same: grad_k and grad_v are sums of 32,768 terms of one size and sign."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    from oracle import mrf_sequence_oracle as so
+    print("case gradients of keys", D, with_table, dtype, flush=True)
+    K, Q = 70, 32768
+    rng = np.random.default_rng(D)
+    k, v = rng.normal(size=(1, K, 1, D)) * (1.0 / np.sqrt(D)), rng.normal(size=(1, K, 1, D))
+    q, g = np.broadcast_to(0.5 + rng.random((1, 1, 1, D)), (1, Q, 1, D)), np.broadcast_to(0.5 + rng.random((1, 1, 1, D)), (1, Q, 1, D))
+    (q, qn), (k, kn), (v, vn), (g, gn) = (_values(x, dtype) for x in (q, k, v, g))
+    table = bucket_of = grad_table = None
+    if with_table:      # (a bucket, whose value so changes nothing, and which has no gradient)
+        table, bucket_of = torch.zeros(1, 1, device="cuda:0"), torch.zeros(1, dtype=torch.int32, device="cuda:0")
+        grad_table = torch.empty_like(table)
+    att = mrf.MrfAttention(q, k, v, 0.35, table=table, bucket_of=bucket_of)
+    got = _backward(att, g, Q, K, D, dtype, grad_table)
+    # a query's share, Q times
+    ok, _ = so.attention_pairs(1, K)
+    want, ds, eds = _attention_bounds(qn[0, :1], kn[0], vn[0], gn[0, :1], float(att.c.scale), ok, None, dtype, so)
+    for name, t in zip(("grad_k", "grad_v"), got[1:]):
+        _close(t, Q * want[name][0], Q * want[name][1], dtype, name)
+    _close(got[0], *(np.broadcast_to(t[0], got[0].shape) for t in want["grad_q"]), dtype, "grad_q")
+    if with_table:
+        _close(grad_table, np.zeros((1, 1)), Q * (eds + SUM * U * np.abs(ds)).sum() * np.ones((1, 1)), what="grad_table")
