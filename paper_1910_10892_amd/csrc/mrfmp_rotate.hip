@@ -189,7 +189,8 @@ template <class X, int S, int TL, bool WHOLE> __global__ void __launch_bounds__(
     }
 }
 
-// Backward: u = dy turned back, a = u gamma, dx = r (a - h mean(a h)) with h = x r.  The sums of u h stay in registers over all tokens of a group.
+// Backward: u = dy turned back, a = u gamma, dx = r (a - h mean(a h)) with h = x r.  The sums of u h of a piece's heads are added in 32
+// bits, those of a group's pieces in 64 (terms that are all alike are rounded the same way each time: 128 pieces of 16 heads left the sum off by 2e-5).
 template <class X, int S, int TL, bool WHOLE> __global__ void __launch_bounds__(256) mrf_rotate_bwd(const MrfRotateParams P)
 {
     typedef MrfSlots<X, S, WHOLE> Slots;
@@ -198,7 +199,11 @@ template <class X, int S, int TL, bool WHOLE> __global__ void __launch_bounds__(
     const int kind = place.kind, l = threadIdx.x % TL;
     const Slots slots(P, l);
     const float inv = 1.0f / (float)P.D;
-    float ga[S], gb[S], sa[S] = {}, sb[S] = {};
+    float ga[S], gb[S];
+    // A thread's sums, its own.  (In registers they would cost 16 + 4 heads of 128 a wavefront a SIMD: both passes over 8,192 tokens 54 us, and 50 so; 49 with sums of 32 bits.)
+    __shared__ double all[2 * S][256];
+#pragma unroll
+    for (int j = 0; j < 2 * S; ++j) all[j][threadIdx.x] = 0.0;
     slots.parameters(P.gamma[kind], ga, gb, 1.0f);
     for (long long g = place.g; g < place.all; g += place.step) {
         const long long token = g / P.pieces[kind], batch = token / P.T, t = token - batch * P.T;
@@ -206,7 +211,7 @@ template <class X, int S, int TL, bool WHOLE> __global__ void __launch_bounds__(
         const X *const from = (const X *)P.in[kind] + batch * P.at_batch[kind] + t * P.at_token[kind];
         const long long dense = token * place.heads * (long long)P.D;
         typename Slots::Raw r[MRF_ROTATE_AHEAD_BACK], d[MRF_ROTATE_AHEAD_BACK];
-        float c[S], s[S];
+        float c[S], s[S], sa[S] = {}, sb[S] = {};
         for (int h = h0; h < h1; h += MRF_ROTATE_AHEAD_BACK) {
 #pragma unroll
             for (int i = 0; i < MRF_ROTATE_AHEAD_BACK; ++i) {
@@ -240,13 +245,18 @@ template <class X, int S, int TL, bool WHOLE> __global__ void __launch_bounds__(
                 if (P.out[kind]) slots.store((X *)P.out[kind] + dense + (h + i) * (long long)P.D, true, da, db);
             }
         }
+#pragma unroll
+        for (int j = 0; j < S; ++j) {
+            unsafeAtomicAdd(&all[2 * j][threadIdx.x], (double)sa[j]);
+            unsafeAtomicAdd(&all[2 * j + 1][threadIdx.x], (double)sb[j]);
+        }
     }
     if (!P.dgamma[kind]) return;
     // lanes of a wavefront with the same slots, then its wavefronts
     const int wv = threadIdx.x >> 6;
 #pragma unroll
     for (int j = 0; j < S; ++j) {
-        float x = sa[j], y = sb[j];
+        float x = (float)all[2 * j][threadIdx.x], y = (float)all[2 * j + 1][threadIdx.x];
         for (int w = TL; w < 64; w *= 2) {
             x += __shfl_xor(x, w);
             y += __shfl_xor(y, w);

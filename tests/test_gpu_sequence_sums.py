@@ -120,3 +120,22 @@ def test_gradients_of_keys_from_many_queries(D, with_table, dtype):
     _close(got[0], *(np.broadcast_to(t[0], got[0].shape) for t in want["grad_q"]), dtype, "grad_q")
     if with_table:
         _close(grad_table, np.zeros((1, 1)), Q * (eds + SUM * U * np.abs(ds)).sum() * np.ones((1, 1)), what="grad_table")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gradient_of_a_norm_from_many_tokens(dtype):
+    """All tokens are the same: the gradients of gamma are sums of 4,194,304 terms of one size and sign."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    from oracle import mrf_sequence_oracle as so
+    print("case gamma", dtype, flush=True)
+    T, H, D = 262144, 16, 512
+    rng = np.random.default_rng(5)
+    (x, xn), (g, gn) = (_values(0.5 + rng.random((1, 1, 1, D)), dtype) for _ in range(2))
+    gamma, _ = _values(np.ones(D), "float32")
+    none = torch.empty(1, T, 0, D, dtype=x.dtype, device="cuda:0")
+    grad_gamma = torch.empty(D, device="cuda:0")
+    ws = torch.empty(mrf.mrf_head_rotation_workspace_bytes(T, H, 0, D), dtype=torch.uint8, device="cuda:0")
+    mrf.mrf_head_rotation_backward(g.expand(1, T, H, D).contiguous(), none, x.expand(1, T, H, D), none, gamma, None, 1e-6, None, None, None, grad_gamma, None, ws)
+    _, want = so.head_rotation_grad(gn[0], xn[0], np.ones(D), 1e-6, np.zeros(0))
+    _close(grad_gamma, T * H * want, T * H * SUM * U * np.abs(want), what="grad_gamma")
