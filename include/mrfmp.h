@@ -381,16 +381,19 @@ typedef struct {
     int32_t n_buckets, heads_last;    /* n_buckets 1..65536 */
 } mrf_attention;
 
-/* Bytes of DEVICE workspace (256-byte aligned) of the forward (backward = 0) or backward pass; 0 if the description is invalid, or none is needed.  Backward, with
- * a table: an eighth of a byte for each pair of a query and a key, and a few for each query and key; where few keys have many queries, the 32-bit sums of
- * grad_k and grad_v that parts of the queries' heads make. */
+#define MRF_BACKWARD_KEEPS_TABLE 2
+
+/* Bytes of DEVICE workspace (256-byte aligned) of the forward (backward = 0) or backward pass (1; MRF_BACKWARD_KEEPS_TABLE: the one without grad_table); 0 if the
+ * description is invalid, or none is needed.  Backward: 4 bytes for each query of a head; where few keys have many queries, the 32-bit sums of grad_k and grad_v that parts of
+ * the queries' heads make; and with grad_table, for each 32 keys, 4 bytes for each query that may see one of 128 of them (without a band of two ends: all of them, so an
+ * eighth of a byte for each pair of a query and a key of a head), and up to 1 KB for each entry of the table. */
 size_t mrf_attention_workspace_bytes(const mrf_attention *att, int backward);
 
 /*   out   DEVICE [B][Q][Hq][D], assigned
  *   lse   DEVICE [B][Hq][Q] float or NULL, assigned: which the backward call reads */
 int mrf_attention_forward(const mrf_attention *att, void *out, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream);
 
-/* Its gradients; the probabilities are formed again, nothing of Q x K is kept:
+/* Its gradients; the probabilities are formed again, and no score or probability is kept:
  *   dP(i,j) = grad_out_i . v_j,  dS(i,j) = P(i,j) (dP(i,j) - sum_j P(i,j) dP(i,j)),
  *   grad_q_i = scale sum_j dS(i,j) k_j,  grad_k_j = scale sum_i dS(i,j) q_i,  grad_v_j = sum_i P(i,j) grad_out_i  (over the heads that share k_j, v_j too),
  *   grad_table[h][n] = sum of dS(i,j) over batches and pairs of bucket n

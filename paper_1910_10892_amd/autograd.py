@@ -293,7 +293,7 @@ class _Attention(torch.autograd.Function):
         att = _m.MrfAttention(q, k, v, ctx.scale, table=table, **ctx.make, **dict(zip(_GIVEN, given)))
         dense = lambda t: torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
         gq, gk, gv, gt = (dense(t) if need else None for t, need in zip((q, k, v, table), ctx.needs_input_grad[:4]))
-        ws = torch.empty(_m.mrf_attention_workspace_bytes(att, True), dtype=torch.uint8, device=q.device)
+        ws = torch.empty(_m.mrf_attention_workspace_bytes(att, True, gt is not None), dtype=torch.uint8, device=q.device)
         _m.mrf_attention_backward(att, grad_out.contiguous().to(q.dtype), out, lse, gq, gk, gv, gt, ws)
         return gq, gk, gv, gt, None
 

@@ -165,7 +165,7 @@ struct MrfAttnParams {
     float *delta;                                 // [B][Hq][Q]
     int shares;                                   // parts of the heads that share keys, one workgroup each:
     float *share;                                 // [shares][dk, dv][B][K][Hk][D], if more than one
-    float *lines, *partial, *dtable;              // partial: [Hq][n_buckets][MRF_TABLE_PARTS]
+    float *lines, *partial, *dtable;              // [B][Hq][strips][line], [Hq][n_buckets][parts]
     int strips, line;                             // strips of 32 keys; entries of a line
     int parts;
     long long pieces;

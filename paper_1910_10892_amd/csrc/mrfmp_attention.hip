@@ -427,7 +427,7 @@ static size_t attention_forward_bytes(const MrfAttnParams &P, int type)
     return plan.splits > 1 ? (size_t)plan.splits * P.B * P.Hq * P.Q * (P.D + 2) * sizeof(float) : 0;
 }
 
-size_t attention_backward_bytes(const MrfAttnParams &P);
+size_t attention_backward_bytes(const MrfAttnParams &P, bool table_gradient);
 
 }  // namespace mrf_host
 
@@ -439,7 +439,7 @@ size_t mrf_attention_workspace_bytes(const mrf_attention *att, int backward)
 {
     MrfAttnParams P = {};
     if (attention_check(att, P) != MRF_OK) return 0;
-    return backward ? attention_backward_bytes(P) : attention_forward_bytes(P, att->type);
+    return backward ? attention_backward_bytes(P, backward != MRF_BACKWARD_KEEPS_TABLE) : attention_forward_bytes(P, att->type);
 }
 
 int mrf_attention_forward(const mrf_attention *att, void *out, float *lse, void *workspace, size_t workspace_bytes, void *hip_stream)

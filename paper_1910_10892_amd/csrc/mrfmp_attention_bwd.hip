@@ -182,7 +182,8 @@ template <int QT> __device__ inline void mrf_attn_query_tiles(const MrfAttnBatch
 //
 // TABLE: dS of 32 queries x 32 keys is put into LDS with each query's row moved by one against the next, so that a column holds a diagonal (places that none
 // falls on stay 0), and a lane sums a column.  A wavefront has 32 keys and goes through the queries upwards: of the 63 diagonals of a
-// block (of the last lane there is none) the later 31 go on in the next one, whose lanes are 32 less, and 32 are done and written.  An entry of the line: query - (key - first key) + 31.
+// block (of the last lane there is none) the later 31 go on in the next one, whose lanes are 32 less, and 32 are done and written.  An entry of the line: query - (key - first key) + 31, less the
+// first query of the strip's tiles.
 // 63 entries a row, and 32 that are left free each time after rows 3, 11, 19 and 27: so the halves of a wavefront, four rows apart, fall on the two halves of the banks.
 __host__ __device__ constexpr int mrf_skew(int row) { return 63 * row + 32 * ((row + 4) / 8); }
 constexpr int MRF_SKEWED = mrf_skew(31) + 63;
@@ -375,7 +376,7 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 || (DP == 128 && DK) ? 1 
                     }
                 }
                 if constexpr (TABLE) {
-                    if (half == 0) to_line[q0 + 32 * u + lane] = sum * mrf_attn_unshift<T>();
+                    if (half == 0) to_line[(t - t0) * QT + 32 * u + lane] = sum * mrf_attn_unshift<T>();
                     goes_on = __shfl(sum, lane | 32);
                     if (half) goes_on = 0.0f;
                 }
@@ -388,7 +389,7 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 || (DP == 128 && DK) ? 1 
             __syncthreads();
         }
         if constexpr (TABLE)
-            if (half == 0 && t0 < t1) to_line[t1 * QT + lane] = goes_on * mrf_attn_unshift<T>();
+            if (half == 0 && t0 < t1) to_line[(t1 - t0) * QT + lane] = goes_on * mrf_attn_unshift<T>();
     }
     if (j >= P.K) return;
     const long long row = (((long long)b * P.K + j) * P.Hk + hk) * P.D, all = (long long)P.B * P.K * P.Hk * P.D;
@@ -439,7 +440,7 @@ template <class T> __global__ void __launch_bounds__(256) mrf_attn_shares(const 
 // Gradient of the table: what the lines hold of a diagonal, summed over the strips of keys that it crosses, belongs to the bucket of its offset.  A workgroup
 // goes through `per` pieces of 256 offsets of a sequence, a thread its offset's strips; each thread has a sum of its own for each of MRF_TABLE_BUCKETS buckets in
 // LDS, which meet at the end in a fixed tree.  More buckets: a layer of workgroups for each MRF_TABLE_BUCKETS of them.
-constexpr int MRF_TABLE_BUCKETS = 32, MRF_TABLE_PARTS = 256;
+constexpr int MRF_TABLE_BUCKETS = 32;
 
 template <int QT> __global__ void __launch_bounds__(256) mrf_attn_buckets(const MrfAttnParams P)
 {
@@ -476,7 +477,7 @@ template <int QT> __global__ void __launch_bounds__(256) mrf_attn_buckets(const 
                 for (int w = 0; w < 4; ++w) {
                     const int e = entry + 32 * w;
                     const bool in = t0 < t1 && e >= t0 * QT && e < t1 * QT + 32;
-                    const float value = lines[in ? (strip + 4 * y + w) * (long long)P.line + e : 0];
+                    const float value = lines[in ? (strip + 4 * y + w) * (long long)P.line + e - t0 * QT : 0];
                     v[4 * y + w] = in ? value : 0.0f;
                 }
             }
@@ -491,7 +492,7 @@ template <int QT> __global__ void __launch_bounds__(256) mrf_attn_buckets(const 
     }
     __syncthreads();
     if (tid < MRF_TABLE_BUCKETS && first_bucket + tid < P.n_buckets)
-        P.partial[((size_t)h * P.n_buckets + first_bucket + tid) * MRF_TABLE_PARTS + part] = sums[tid][0];
+        P.partial[((size_t)h * P.n_buckets + first_bucket + tid) * P.parts + part] = sums[tid][0];
 }
 
 // a wavefront sums the parts of a bucket (none: 0)
@@ -501,7 +502,7 @@ static __global__ void __launch_bounds__(256) mrf_attn_table(const MrfAttnParams
     if (x >= (long long)P.Hq * P.n_buckets) return;
     const int lane = threadIdx.x & 63, h = (int)(x / P.n_buckets), k = (int)(x - (long long)h * P.n_buckets);
     float sum = 0.0f;
-    for (int p = lane; p < P.parts; p += 64) sum += P.partial[x * MRF_TABLE_PARTS + p];
+    for (int p = lane; p < P.parts; p += 64) sum += P.partial[x * P.parts + p];
     sum = mrf_lanes_sum<64>(sum);
     if (lane == 0) P.dtable[P.heads_last ? (size_t)k * P.Hq + h : (size_t)h * P.n_buckets + k] = sum;
 }
@@ -533,20 +534,11 @@ template <class T, int DP> static int attention_back(const MrfAttnParams &P, hip
         }
     }
     if (P.dtable) {
-        MrfAttnParams S = P;
-        S.parts = 0;
         if (pairs) {
-            // workgroups for the whole card four times over, as far as there are pieces for them (16 heads of 2,048 queries and keys in 4 batches: 22 us with half of
-            // that and the strips of one workgroup at a time, 15 now)
-            const long long all = ((long long)P.Q + P.K - 1 + 255) / 256 * P.B;
-            long long parts = 1024 / P.Hq < 1 ? 1 : 1024 / P.Hq > MRF_TABLE_PARTS ? MRF_TABLE_PARTS : 1024 / P.Hq;
-            if (parts > all) parts = all;
-            S.pieces = (all + parts - 1) / parts;
-            S.parts = (int)((all + S.pieces - 1) / S.pieces);
-            const dim3 grid((unsigned)S.parts, (unsigned)P.Hq, (unsigned)((P.n_buckets + MRF_TABLE_BUCKETS - 1) / MRF_TABLE_BUCKETS));
-            mrf_attn_buckets<mrf_attn_bwd_rows<T>()><<<grid, 256, 0, st>>>(S);
+            const dim3 grid((unsigned)P.parts, (unsigned)P.Hq, (unsigned)((P.n_buckets + MRF_TABLE_BUCKETS - 1) / MRF_TABLE_BUCKETS));
+            mrf_attn_buckets<mrf_attn_bwd_rows<T>()><<<grid, 256, 0, st>>>(P);
         }
-        mrf_attn_table<<<(unsigned)(((long long)P.Hq * P.n_buckets + 3) / 4), 256, 0, st>>>(S);
+        mrf_attn_table<<<(unsigned)(((long long)P.Hq * P.n_buckets + 3) / 4), 256, 0, st>>>(P);
     }
     return launch_status("mrf_attn_bwd");
 }
@@ -572,11 +564,24 @@ int attention_backward_128(const MrfAttnParams &P, int type, hipStream_t st)
 
 static size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// a line for every strip of 32 keys: an entry for each query, as far as whole tiles reach, and 32 more
+// A line for every strip of 32 keys: an entry for each query, as far as whole tiles reach, and 32 more.  The tiles are those that the 128 keys around the strip may be seen from:
+// where the band has two ends, 128 queries and its width, in tiles that these begin and end anywhere in.
 static void attention_lines(MrfAttnParams &P)
 {
+    const long long queries = ((long long)P.Q + 63) / 64 * 64, seen = P.last - P.first + 128, band = seen < 0 ? 0 : (seen + 126) / 64 * 64;
     P.strips = (int)(((long long)P.K + 127) / 128 * 4);
-    P.line = (int)(((long long)P.Q + 63) / 64 * 64 + 32);
+    P.line = (int)(band < queries ? band : queries) + 32;
+}
+
+// Workgroups of a head that sum the table's gradient, and pieces of 256 offsets that each goes through: workgroups for the whole card four times over, as far as there are
+// pieces for them (16 heads of 2,048 queries and keys in 4 batches: 22 us with half of that and the strips of one workgroup at a time, 15 now)
+static void attention_parts(MrfAttnParams &P)
+{
+    const long long all = P.Q && P.K ? ((long long)P.Q + P.K - 1 + 255) / 256 * P.B : 0;
+    long long parts = 1024 / P.Hq < 1 ? 1 : 1024 / P.Hq > 256 ? 256 : 1024 / P.Hq;
+    if (parts > all) parts = all;
+    P.pieces = parts ? (all + parts - 1) / parts : 0;
+    P.parts = parts ? (int)((all + P.pieces - 1) / P.pieces) : 0;
 }
 
 // Workgroups that share the heads of queries on a head of keys: as many as it takes for two on a compute unit, since some have far more queries to go through
@@ -595,13 +600,14 @@ static size_t attention_share_bytes(const MrfAttnParams &P, int shares)
     return shares > 1 ? round256(2 * (size_t)shares * P.B * P.K * P.Hk * P.D * sizeof(float)) : 0;
 }
 
-size_t attention_backward_bytes(const MrfAttnParams &given)
+size_t attention_backward_bytes(const MrfAttnParams &given, bool table_gradient)
 {
     MrfAttnParams P = given;
     size_t n = round256((size_t)P.B * P.Hq * P.Q * sizeof(float)) + attention_share_bytes(P, attention_shares(P));
-    if (P.table && P.Q && P.K) {
+    if (P.table && table_gradient && P.B && P.Q && P.K) {
         attention_lines(P);
-        n += round256((size_t)P.B * P.Hq * P.strips * P.line * sizeof(float)) + (size_t)P.Hq * P.n_buckets * MRF_TABLE_PARTS * sizeof(float);
+        attention_parts(P);
+        n += round256((size_t)P.B * P.Hq * P.strips * P.line * sizeof(float)) + (size_t)P.Hq * P.n_buckets * P.parts * sizeof(float);
     }
     return n ? n : 256;
 }
@@ -622,9 +628,10 @@ int mrf_attention_backward(const mrf_attention *att, const void *grad_out, const
     if (P.B && P.Q && (!P.q || !grad_out || !out || !lse)) return MRF_ERR_NULL_POINTER;
     if (P.B && P.K && (!P.k || !P.v)) return MRF_ERR_NULL_POINTER;
     if (!workspace) return MRF_ERR_NULL_POINTER;
-    if (workspace_bytes < attention_backward_bytes(P)) return MRF_ERR_WORKSPACE_TOO_SMALL;
+    if (workspace_bytes < attention_backward_bytes(P, grad_table != nullptr)) return MRF_ERR_WORKSPACE_TOO_SMALL;
     P.dout = grad_out; P.out = (void *)out; P.lse = (float *)lse; P.dq = grad_q; P.dk = grad_k; P.dv = grad_v; P.dtable = grad_table;
     attention_lines(P);
+    attention_parts(P);
     P.delta = (float *)workspace;
     P.shares = attention_shares(P);
     P.share = (float *)((char *)workspace + round256((size_t)P.B * P.Hq * P.Q * sizeof(float)));

@@ -625,6 +625,7 @@ _INT64_MIN, _INT64_MAX = -(1 << 63), (1 << 63) - 1
 _ATTENTION = struct.Struct("@7if3P9q3q5P2q2i")
 _ROTATION = struct.Struct("@6i2P6q2Pf2i2Piq")
 _TWO_STRIDES = ctypes.c_int64 * 2
+_BACKWARD_KEEPS_TABLE = 2      # MRF_BACKWARD_KEEPS_TABLE
 _codes = {}      # torch dtype -> code of an element type
 
 
@@ -722,8 +723,9 @@ class MrfAttention:
         self._kept = (q, k, v, query_offsets, q_lengths, k_lengths, table, bucket_of)
 
 
-def mrf_attention_workspace_bytes(att: MrfAttention, backward: bool) -> int:
-    return int(load_library().mrf_attention_workspace_bytes(ctypes.byref(att.c), int(bool(backward))))
+def mrf_attention_workspace_bytes(att: MrfAttention, backward: bool, grad_table: bool = True) -> int:
+    """grad_table: whether the backward call is given one (it then needs room for sums by offset)."""
+    return int(load_library().mrf_attention_workspace_bytes(ctypes.byref(att.c), 0 if not backward else 1 if grad_table else _BACKWARD_KEEPS_TABLE))
 
 
 def mrf_attention_forward(att: MrfAttention, out, lse, workspace, stream=None):

@@ -709,3 +709,34 @@ def test_the_same_bits_on_another_stream_and_again(dtype):
     for _, _, outs in passes:
         for a, b in zip(want, outs):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("first,last,offset", [(-30, 20, 0), (0, 0, 0), (-1, 62, -100), (7, 150, 300), (-3, -3, 5)])
+def test_table_gradient_of_bands_along_many_tiles(first, last, offset, dtype):
+    """The sums by offset have room for the queries that a band lets see 128 keys (the workspace is exactly what is asked for, guarded on both sides)."""
+    _check_attention(1, 550, 500, 1, 1, 16, dtype, first, last, offset, NB=9)
+    _check_attention(3, 500, 450, 2, 1, 8, dtype, first, last, offset, NB=5, ragged=([500, 1, 317], [450, 449, 300], [0, 64, -31]))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_table_whose_gradient_is_not_asked_for(dtype):
+    """Workspace without the sums by offset; the other gradients are the same bits."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    torch.manual_seed(2)
+    q, k, v, g = (torch.randn(2, 300, h, 32, device="cuda:0").to(getattr(torch, dtype)) for h in (4, 2, 2, 4))
+    table, bucket_of = torch.randn(4, 8, device="cuda:0"), torch.from_numpy(mrf.mrf_distance_buckets(8, 64, -299, 599)).cuda()
+    att = mrf.MrfAttention(q, k, v, 0.2, table=table, bucket_of=bucket_of, map_offset=-299)
+    out, lse = torch.empty_like(q), torch.empty(2, 4, 300, device="cuda:0")
+    mrf.mrf_attention_forward(att, out, lse, torch.empty(mrf.mrf_attention_workspace_bytes(att, False) + 1, dtype=torch.uint8, device="cuda:0"))
+    results = []
+    for gt in (torch.empty_like(table), None):
+        ws, check = _guarded((mrf.mrf_attention_workspace_bytes(att, True, gt is not None),), torch.uint8)
+        results.append([torch.empty_like(t) for t in (q, k, v)])
+        mrf.mrf_attention_backward(att, g, out, lse, *results[-1], gt, ws)
+        torch.cuda.synchronize()
+        check()
+    assert mrf.mrf_attention_workspace_bytes(att, True, False) < mrf.mrf_attention_workspace_bytes(att, True)
+    for a, b in zip(*results):
+        assert torch.equal(a, b)

@@ -137,3 +137,25 @@ def test_bindings_refuse_tensors_that_do_not_fit():
                  lambda: mrf.mrf_gated_scan_forward(q[0], q[1].half(), None, None, q[0], None, None, None)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_attention_backward_workspace_is_for_the_gradients_that_are_asked_for():
+    lib = mrf.load_library()
+    size = lambda backward, **given: lib.mrf_attention_workspace_bytes(ctypes.byref(_attention(**given)), backward)  # noqa: E731
+    table = dict(table=FAKE, bucket_of=FAKE, n_offsets=9, n_buckets=4)
+    long = dict(B=1, Hq=32, Hk=32, Q=32768, K=32768)
+    # without the table's gradient: as without a table
+    assert size(2, **table, **long) == size(1, **long) < 1 << 23
+    keeps = size(2, **table)
+    assert size(1, **table) > keeps > 0
+    back = lambda gt, n: lib.mrf_attention_backward(ctypes.byref(_attention(**table)), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, gt, FAKE, n, None)  # noqa: E731
+    assert back(None, keeps - 1) == -6 and back(FAKE, size(1, **table) - 1) == -6 and back(FAKE, keeps) == -6
+    # a band: for each 32 keys the queries that see 128 of them, not all there are
+    bands = [size(1, **table, B=1, Hq=32, Hk=32, Q=n, K=n, first_offset=-96, last_offset=0) - size(2, B=1, Hq=32, Hk=32, Q=n, K=n) for n in (8192, 32768)]
+    assert bands[1] < 4.1 * bands[0] and bands[1] < 32 * 1024 * (96 + 128 + 3 * 64) * 4 + (1 << 20)
+    for first, last in ((-(1 << 63), (1 << 63) - 1), (-(1 << 41), 1 << 41), (-40000, 40000), (-(1 << 63), 0)):
+        assert size(1, **table, **long, first_offset=first, last_offset=last) == size(1, **table, **long)
+    assert size(1, **table, **long, first_offset=5, last_offset=-500) < size(1, **table, **long, first_offset=0, last_offset=0)
+    # a large table: as many parts of it as there are offsets for
+    many = {**table, "n_buckets": 65536}
+    assert size(1, **many) - size(2, **many) < 4 * 65536 * 4 * 8
