@@ -495,16 +495,18 @@ template <int QT> __global__ void __launch_bounds__(256) mrf_attn_buckets(const 
         P.partial[((size_t)h * P.n_buckets + first_bucket + tid) * P.parts + part] = sums[tid][0];
 }
 
-// a wavefront sums the parts of a bucket (none: 0)
+// A wavefront sums the parts of a bucket (none: 0), and goes on to another where there are more than a grid has wavefronts.
+constexpr long long MRF_TABLE_GROUPS = 1 << 22;
 static __global__ void __launch_bounds__(256) mrf_attn_table(const MrfAttnParams P)
 {
-    const long long x = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (x >= (long long)P.Hq * P.n_buckets) return;
-    const int lane = threadIdx.x & 63, h = (int)(x / P.n_buckets), k = (int)(x - (long long)h * P.n_buckets);
-    float sum = 0.0f;
-    for (int p = lane; p < P.parts; p += 64) sum += P.partial[x * P.parts + p];
-    sum = mrf_lanes_sum<64>(sum);
-    if (lane == 0) P.dtable[P.heads_last ? (size_t)k * P.Hq + h : (size_t)h * P.n_buckets + k] = sum;
+    const int lane = threadIdx.x & 63;
+    for (long long x = (long long)blockIdx.x * 4 + (threadIdx.x >> 6); x < (long long)P.Hq * P.n_buckets; x += gridDim.x * 4LL) {
+        const int h = (int)(x / P.n_buckets), k = (int)(x - (long long)h * P.n_buckets);
+        float sum = 0.0f;
+        for (int p = lane; p < P.parts; p += 64) sum += P.partial[x * P.parts + p];
+        sum = mrf_lanes_sum<64>(sum);
+        if (lane == 0) P.dtable[P.heads_last ? (size_t)k * P.Hq + h : (size_t)h * P.n_buckets + k] = sum;
+    }
 }
 
 namespace mrf_host {
@@ -538,7 +540,8 @@ template <class T, int DP> static int attention_back(const MrfAttnParams &P, hip
             const dim3 grid((unsigned)P.parts, (unsigned)P.Hq, (unsigned)((P.n_buckets + MRF_TABLE_BUCKETS - 1) / MRF_TABLE_BUCKETS));
             mrf_attn_buckets<mrf_attn_bwd_rows<T>()><<<grid, 256, 0, st>>>(P);
         }
-        mrf_attn_table<<<(unsigned)(((long long)P.Hq * P.n_buckets + 3) / 4), 256, 0, st>>>(P);
+        const long long groups = ((long long)P.Hq * P.n_buckets + 3) / 4;
+        mrf_attn_table<<<(unsigned)(groups < MRF_TABLE_GROUPS ? groups : MRF_TABLE_GROUPS), 256, 0, st>>>(P);
     }
     return launch_status("mrf_attn_bwd");
 }

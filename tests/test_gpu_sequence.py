@@ -740,3 +740,17 @@ def test_a_table_whose_gradient_is_not_asked_for(dtype):
     assert mrf.mrf_attention_workspace_bytes(att, True, False) < mrf.mrf_attention_workspace_bytes(att, True)
     for a, b in zip(*results):
         assert torch.equal(a, b)
+
+
+def test_gradient_of_a_table_of_2_to_the_26_entries():
+    """More than a grid has wavefronts (of nothing: there are no sequences)."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    q = torch.empty(0, 1, 1024, 4, device="cuda:0")
+    table, bucket_of = torch.zeros(1024, 65536, device="cuda:0"), torch.zeros(1, dtype=torch.int32, device="cuda:0")
+    grad_table = torch.full_like(table, 7.0)
+    att = mrf.MrfAttention(q, q, q, 1.0, table=table, bucket_of=bucket_of)
+    ws = torch.empty(mrf.mrf_attention_workspace_bytes(att, True), dtype=torch.uint8, device="cuda:0")
+    lse = torch.empty(0, 1024, 1, device="cuda:0")
+    mrf.mrf_attention_backward(att, q, q, lse, None, None, None, grad_table, ws)
+    assert (grad_table == 0).all()
