@@ -364,7 +364,8 @@ int mrf_softmin_policy_backward(int64_t n_pixels, int32_t L, const void *cost, i
  * A single query of a long cache (Q = 1, query_offset = its position) divides the keys among workgroups. */
 typedef struct {
     int32_t B, Q, K, Hq, Hk, D;       /* D 1..MRF_ATTENTION_LONGEST_HEAD, Hk divides Hq, Hq up to 32768; B, Q, K may be 0; Q + K at most 2^31 - 2^16, and
-                                         B Hq ceil(max(Q, K) / 128) below 2^24, else MRF_ERR_BAD_SHAPE */
+                                         B Hq ceil(max(Q, K) / 128) below 2^24, and B Hq ceil(Q / 256) below 2^23 for D > 64 in 16 bits with
+                                         more than 32 queries (64, of heads that share keys), else MRF_ERR_BAD_SHAPE */
     int32_t type;                     /* of q, k, v, out and their gradients: MRF_F32, MRF_F16, MRF_BF16 */
     float scale;                      /* > 0 and finite, times log2(e) too, else MRF_ERR_BAD_ARGUMENT */
     const void *q, *k, *v;            /* DEVICE [B][Q][Hq][D], [B][K][Hk][D], [B][K][Hk][D] at strides q_stride .. */

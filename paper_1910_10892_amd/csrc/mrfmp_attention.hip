@@ -379,6 +379,9 @@ int attention_check(const mrf_attention *a, MrfAttnParams &P)
     // (workgroups of 256 threads: a grid has fewer than 2^32)
     const long long groups = 0xffffff, rows = a->Q > a->K ? a->Q : a->K;
     if (a->B && a->Hq * ((rows + 127) / 128) > groups / a->B) return MRF_ERR_BAD_SHAPE;
+    // (and those of many queries of heads of more than 64 entries in 16 bits, forward, 512)
+    const bool wide = a->D > 64 && a->type != MRF_F32 && a->Q > (a->Hq > a->Hk ? 64 : 32);
+    if (wide && a->B && a->Hq * (((long long)a->Q + 255) / 256) > groups / 2 / a->B) return MRF_ERR_BAD_SHAPE;
     if (!known_type(a->type) || !(a->scale > 0.0f) || !(a->scale * 1.44269504088896340736f < INFINITY)) return MRF_ERR_BAD_ARGUMENT;
     const long long far = 1LL << 40;
     if (a->query_offset > far || a->query_offset < -far) return MRF_ERR_BAD_ARGUMENT;

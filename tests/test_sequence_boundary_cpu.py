@@ -159,3 +159,22 @@ def test_attention_backward_workspace_is_for_the_gradients_that_are_asked_for():
     # a large table: as many parts of it as there are offsets for
     many = {**table, "n_buckets": 65536}
     assert size(1, **many) - size(2, **many) < 4 * 65536 * 4 * 8
+
+
+def test_attention_refuses_more_workgroups_than_a_grid_holds():
+    """Workgroups of 512 threads are 2^23 - 1 at most."""
+    lib = mrf.load_library()
+
+    def forward(**given):
+        return lib.mrf_attention_forward(ctypes.byref(_attention(**given)), FAKE, None, FAKE, 1 << 40, None)
+
+    for bad in (dict(B=1 << 15, Hq=256, Hk=256, Q=100), dict(B=1 << 15, Hq=256, Hk=256, Q=33), dict(B=1 << 15, Hq=256, Hk=128, Q=65), dict(B=1 << 15, Hq=128, Hk=128, Q=257)):
+        for t in (1, 2):
+            for D in (65, 128):
+                assert forward(**bad, type=t, D=D) == -2, bad
+                assert lib.mrf_attention_workspace_bytes(ctypes.byref(_attention(**bad, type=t, D=D)), 1) == 0
+        # narrower workgroups, of 32 bits and of shorter heads, still fit
+        assert lib.mrf_attention_workspace_bytes(ctypes.byref(_attention(**bad, type=0, D=128)), 1) > 0
+        assert lib.mrf_attention_workspace_bytes(ctypes.byref(_attention(**bad, type=1, D=64)), 1) > 0
+    for good in (dict(B=1 << 15, Hq=255, Hk=255, Q=256), dict(B=1 << 15, Hq=256, Hk=256, Q=32), dict(B=1 << 15, Hq=256, Hk=128, Q=64)):
+        assert lib.mrf_attention_workspace_bytes(ctypes.byref(_attention(**good, type=1, D=128, K=1)), 1) > 0
