@@ -350,20 +350,20 @@ def head_rotation(q, k, gamma_q=None, gamma_k=None, *, eps=1e-6, inv_freq=None, 
 class _GatedScan(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, z, initial, lengths, how):
-        complement, reverse = how
+        complement, reverse, recorded = how
         x, z = _dense_last(x), _dense_last(z)
         initial = None if initial is None else initial.contiguous()
         outer, T, inner = x.shape
         y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         final = torch.empty((outer, inner), dtype=torch.float32, device=x.device)
         states = None
-        if any(ctx.needs_input_grad[:3]):
+        if recorded and any(ctx.needs_input_grad[:3]):      # (inputs ask for gradients under no_grad too)
             states = torch.empty((outer, _m.mrf_gated_scan_states(T), inner), dtype=torch.float32, device=x.device)
         ctx.ws_bytes = _m.mrf_gated_scan_workspace_bytes(outer, T, inner)
         ws = torch.empty(ctx.ws_bytes, dtype=torch.uint8, device=x.device) if ctx.ws_bytes else None
         _m.mrf_gated_scan_forward(x, z, initial, lengths, y, final, states, ws, complement, reverse)
         ctx.save_for_backward(x, z, lengths, states)
-        ctx.how, ctx.carried = how, initial is not None
+        ctx.how, ctx.carried = how[:2], initial is not None
         ctx.set_materialize_grads(False)
         return y, final
 
@@ -387,7 +387,7 @@ def gated_scan(x, z, initial=None, *, lengths=None, complement=True, reverse=Fal
     """(y [rows,T,channels], final [rows,channels] float32): h_t = a_t h_(t-1) + (1 - a_t) x_t with a = sigmoid(z) (complement=False: + x_t) along
     T of x, z [rows,T,channels], as mrf_gated_scan_forward states it; initial [rows,channels] float32 or None, lengths [rows] int32 or None.  Gradients flow from
     both to x, z and initial."""
-    return _GatedScan.apply(x, z, initial, None if lengths is None else lengths.contiguous(), (bool(complement), bool(reverse)))
+    return _GatedScan.apply(x, z, initial, None if lengths is None else lengths.contiguous(), (bool(complement), bool(reverse), torch.is_grad_enabled()))
 
 
 def scanline_scan(x, z, direction, *, complement=True):

@@ -178,3 +178,16 @@ def test_attention_refuses_more_workgroups_than_a_grid_holds():
         assert lib.mrf_attention_workspace_bytes(ctypes.byref(_attention(**bad, type=1, D=64)), 1) > 0
     for good in (dict(B=1 << 15, Hq=255, Hk=255, Q=256), dict(B=1 << 15, Hq=256, Hk=256, Q=32), dict(B=1 << 15, Hq=256, Hk=128, Q=64)):
         assert lib.mrf_attention_workspace_bytes(ctypes.byref(_attention(**good, type=1, D=128, K=1)), 1) > 0
+
+
+def test_gated_scan_keeps_no_states_where_no_gradient_is_recorded(monkeypatch):
+    import torch
+    from paper_1910_10892_amd import autograd
+    given = []
+    monkeypatch.setattr(autograd._m, "mrf_gated_scan_forward", lambda x, z, initial, lengths, y, final, states, *rest: given.append(states))
+    x, z = torch.zeros(2, 40, 4, requires_grad=True), torch.zeros(2, 40, 4, requires_grad=True)
+    with torch.no_grad():
+        autograd.gated_scan(x, z)
+    autograd.gated_scan(x.detach(), z.detach())
+    autograd.gated_scan(x, z.detach())
+    assert given[:2] == [None, None] and given[2].shape == (2, mrf.mrf_gated_scan_states(40), 4)
