@@ -191,3 +191,118 @@ def test_gated_scan_keeps_no_states_where_no_gradient_is_recorded(monkeypatch):
     autograd.gated_scan(x.detach(), z.detach())
     autograd.gated_scan(x, z.detach())
     assert given[:2] == [None, None] and given[2].shape == (2, mrf.mrf_gated_scan_states(40), 4)
+
+
+@pytest.fixture
+def bound(monkeypatch):
+    """The bindings with tensors of the CPU in place of the GPU's, and calls of the library that work on data noted down instead of made."""
+    real, calls = mrf.load_library(), []
+
+    class Library:
+        def __getattr__(self, name):
+            if name.endswith(("_bytes", "_states", "_strerror")):
+                return getattr(real, name)
+            return lambda *args: calls.append(name) or 0
+
+    monkeypatch.setattr(binding, "_lib", Library())
+    for name in ("_device_of", "_device_now", "_stream_at"):
+        monkeypatch.setattr(binding, name, lambda *args: -1)      # (where a tensor of the CPU says that it is)
+    return calls
+
+
+def _refuses(calls, call, good, wrong):
+    """The call with its good arguments is made; with one of them wrong at a time it is refused for that one."""
+    call(**good)
+    assert len(calls) == 1
+    for name, value, match in wrong:
+        with pytest.raises(ValueError, match=match):
+            call(**{**good, name: value})
+        assert len(calls) == 1, (name, match)
+
+
+def _wrong(name, t, more=()):
+    """Another shape, another type, other strides of a dense tensor."""
+    import torch
+    other = torch.int32 if t.dtype == torch.float32 else torch.float32
+    yield name, t.new_zeros((*t.shape[:-1], t.shape[-1] + 1)), "%s has shape" % name
+    yield name, t.to(other), "%s must be torch" % name
+    if t.dim() > 1:
+        yield name, t.transpose(0, 1).contiguous().transpose(0, 1), "%s must be contiguous" % name
+    yield from more
+
+
+def test_attention_bindings_refuse_one_wrong_tensor(bound):
+    import torch
+    q, k, v = torch.zeros(2, 5, 4, 8), torch.zeros(2, 6, 2, 8), torch.zeros(2, 6, 2, 8)
+    int32 = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    with pytest.raises(ValueError, match="tensors must be float32"):
+        mrf.MrfAttention(q.double(), k.double(), v.double(), 0.5)
+    good = dict(q=q, k=k, v=v, table=torch.zeros(4, 3), bucket_of=int32(11), query_offsets=int32(2), q_lengths=int32(2), k_lengths=int32(2),
+                out=torch.zeros(2, 5, 4, 8), lse=torch.zeros(2, 4, 5), scale=0.5)
+
+    def forward(out, lse, scale, q, k, v, **more):
+        att = mrf.MrfAttention(q, k, v, scale, **more)
+        mrf.mrf_attention_forward(att, out, lse, None)
+
+    wide = lambda t: torch.zeros(*t.shape[:-1], 2 * t.shape[-1])[..., ::2]  # noqa: E731
+    wrong = [("q", q[0], "must be"), ("k", k[0], "must be"), ("v", v[0], "v has shape"), ("k", k[:1], "k has shape"), ("k", k[..., :7], "k has shape"), ("v", v[:, :5], "v has shape"),
+             ("v", v[:, :, :1], "v has shape"), ("q", q.double(), "must be torch.float64"), ("k", k.half(), "k must be torch"), ("v", v.bfloat16(), "v must be torch"),
+             ("q", wide(q), "last index of q"), ("k", wide(k), "last index of k"), ("v", wide(v), "last index of v"), ("bucket_of", None, "bucket_of"),
+             ("bucket_of", torch.zeros(11, dtype=torch.int64), "bucket_of must be torch"), ("bucket_of", int32(22)[::2], "bucket_of must be contiguous"),
+             ("table", torch.zeros(3, 3), "table has shape"), ("table", torch.zeros(3, 4).t(), "table must be contiguous"),
+             ("table", torch.zeros(4, 3).half(), "table must be torch"),
+             *_wrong("out", good["out"]), *_wrong("lse", good["lse"])]
+    for name in ("query_offsets", "q_lengths", "k_lengths"):
+        wrong += [(name, int32(3), "%s has shape" % name), (name, torch.zeros(2, dtype=torch.int64), "%s must be torch" % name), (name, int32(4)[::2], "%s must be contiguous" % name)]
+    _refuses(bound, forward, good, wrong)
+
+
+def test_attention_backward_bindings_refuse_one_wrong_tensor(bound):
+    import torch
+    q, k = torch.zeros(2, 5, 4, 8), torch.zeros(2, 6, 2, 8)
+    att = mrf.MrfAttention(q, k, k, 0.5, table=torch.zeros(4, 3), bucket_of=torch.zeros(11, dtype=torch.int32))
+    new = torch.zeros_like
+    good = dict(grad_out=new(q), out=new(q), lse=torch.zeros(2, 4, 5), grad_q=new(q), grad_k=new(k), grad_v=new(k), grad_table=torch.zeros(4, 3), workspace=torch.zeros(64, dtype=torch.uint8))
+    wrong = [w for name, t in good.items() if name != "workspace" for w in _wrong(name, t)]
+    wrong.append(("workspace", torch.zeros(4, 8)[:, ::2], "workspace must be contiguous"))
+    _refuses(bound, lambda **a: mrf.mrf_attention_backward(att, **a), good, wrong)
+    with pytest.raises(ValueError, match="without a table"):
+        mrf.mrf_attention_backward(mrf.MrfAttention(q, k, k, 0.5), **good)
+    assert len(bound) == 1
+
+
+def test_head_rotation_bindings_refuse_one_wrong_tensor(bound):
+    import torch
+    q, k = torch.zeros(2, 5, 4, 8), torch.zeros(2, 5, 2, 8)
+    new = torch.zeros_like
+    inputs = dict(q=q, k=k, gamma_q=torch.ones(8), gamma_k=torch.ones(8), eps=1e-6, inv_freq=torch.ones(4), positions=torch.zeros(2, 5, 2, dtype=torch.int32))
+    wide = torch.zeros(2, 5, 4, 16)[..., ::2]
+    wrong = [("q", q[0], "must be"), ("k", k[0], "must be"), ("k", k[:, :4], "k has shape"), ("k", k[..., :7], "k has shape"), ("q", q.double(), "must be torch.float64"),
+             ("k", k.half(), "k must be torch"), ("q", wide, "last index of q"), ("k", wide[:, :, :2], "last index of k"), ("inv_freq", torch.ones(4).half(), "inv_freq must be torch"),
+             ("inv_freq", torch.ones(8)[::2], "inv_freq must be contiguous"), ("positions", torch.zeros(2, 4, dtype=torch.int32), "positions has shape"),
+             ("positions", torch.zeros(2, 5), "positions must be torch"), ("positions", torch.zeros(2, 5, 4, dtype=torch.int32)[..., ::2], "positions must be contiguous")]
+    for name in ("gamma_q", "gamma_k"):
+        wrong += [*_wrong(name, torch.ones(8)), (name, torch.ones(16)[::2], "%s must be contiguous" % name)]
+    forward = {**inputs, "out_q": new(q), "out_k": new(k)}
+    _refuses(bound, mrf.mrf_head_rotation_forward, forward, wrong + [*_wrong("out_q", q), *_wrong("out_k", k)])
+    bound.clear()
+    grads = dict(grad_out_q=new(q), grad_out_k=new(k), grad_q=new(q), grad_k=new(k), grad_gamma_q=torch.ones(8), grad_gamma_k=torch.ones(8))
+    _refuses(bound, mrf.mrf_head_rotation_backward, {**inputs, **grads, "workspace": torch.zeros(64, dtype=torch.uint8)}, wrong + [w for n, t in grads.items() for w in _wrong(n, t)])
+
+
+def test_gated_scan_bindings_refuse_one_wrong_tensor(bound):
+    import torch
+    x = torch.zeros(2, 40, 4)
+    new = torch.zeros_like
+    ends, states, lengths = torch.zeros(2, 4), torch.zeros(2, mrf.mrf_gated_scan_states(40), 4), torch.zeros(2, dtype=torch.int32)
+    wide = torch.zeros(2, 40, 8)[..., ::2]
+    inputs = dict(x=x, z=new(x), lengths=lengths, states=states, workspace=None)
+    wrong = [("x", x[0], "must be"), ("z", x[0], "z has shape"), ("z", x[:, :39], "z has shape"), ("z", x.half(), "z must be torch"), ("x", x.double(), "tensors must be float32"),
+             ("x", wide, "last index of x"), ("z", wide, "last index of z"), ("lengths", lengths.long(), "lengths must be torch"), ("lengths", torch.zeros(3, dtype=torch.int32), "lengths has shape"),
+             ("lengths", torch.zeros(4, dtype=torch.int32)[::2], "lengths must be contiguous"), *_wrong("states", states)]
+    more = lambda given: wrong + [w for n, t in given.items() for w in _wrong(n, t)]  # noqa: E731
+    forward = dict(initial=ends, y=new(x), final=new(ends))
+    _refuses(bound, mrf.mrf_gated_scan_forward, {**inputs, **forward}, more(forward))
+    bound.clear()
+    grads = dict(grad_y=new(x), grad_final=new(ends), grad_x=new(x), grad_z=new(x), grad_initial=new(ends))
+    _refuses(bound, mrf.mrf_gated_scan_backward, {**inputs, **grads}, more(grads))
