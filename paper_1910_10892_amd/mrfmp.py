@@ -637,6 +637,14 @@ def _code_of(dtype) -> int:
     return code
 
 
+def _packed(form, *values) -> bytes:
+    """A description's bytes."""
+    try:
+        return form.pack(*values)
+    except struct.error as e:
+        raise ValueError("offsets have 64 bits: %s" % e) from None
+
+
 def _device_of(t):
     """The current device, on which the first tensor of a call has to be, as all others (the call goes to its stream)."""
     at = t.get_device()
@@ -706,15 +714,15 @@ class MrfAttention:
         strides = (*_strides(q, "q", q.shape, dtype, at), *_strides(k, "k", keys, dtype, at), *_strides(v, "v", keys, dtype, at))
         n = offsets = 0
         if table is not None:
-            if bucket_of is None:
-                raise ValueError("a table needs bucket_of")
+            if bucket_of is None or table.dim() != 2:
+                raise ValueError("a table must be two-dimensional, and needs bucket_of")
             n, offsets = table.shape[0] if heads_last else table.shape[-1], bucket_of.numel()
         if max(B, Q, K, Hq, D, n) > 0x7fffffff:
             raise ValueError("sizes are at most 2^31 - 1")
         of_batch = (B,)
         i32, f32 = _int32, _float32
-        self.c = _CAttention.from_buffer_copy(_ATTENTION.pack(
-            B, Q, K, Hq, Hk, D, _code_of(dtype), scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), *strides,
+        self.c = _CAttention.from_buffer_copy(_packed(
+            _ATTENTION, B, Q, K, Hq, Hk, D, _code_of(dtype), scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), *strides,
             _INT64_MIN if first_offset is None else int(first_offset), _INT64_MAX if last_offset is None else int(last_offset), int(query_offset),
             _dense(query_offsets, "query_offsets", of_batch, i32, at), _dense(q_lengths, "q_lengths", of_batch, i32, at),
             _dense(k_lengths, "k_lengths", of_batch, i32, at), _dense(table, "table", (n, Hq) if heads_last else (Hq, n), f32, at),
@@ -773,8 +781,8 @@ def _head_rotation(q, k, gamma_q, gamma_k, eps, inv_freq, positions, position_of
         places = 0
     if max(B, T, Hq, Hk, D) > 0x7fffffff or (inv_freq is not None and inv_freq.numel() > 0x3fffffff):
         raise ValueError("sizes are at most 2^31 - 1")
-    packed = _ROTATION.pack(
-        B, T, Hq, Hk, D, _code_of(dtype), q.data_ptr(), k.data_ptr(), *_strides(q, "q", queries, dtype, at), *_strides(k, "k", keys, dtype, at),
+    packed = _packed(
+        _ROTATION, B, T, Hq, Hk, D, _code_of(dtype), q.data_ptr(), k.data_ptr(), *_strides(q, "q", queries, dtype, at), *_strides(k, "k", keys, dtype, at),
         _dense(gamma_q, "gamma_q", entries, f32, at), _dense(gamma_k, "gamma_k", entries, f32, at), eps, 0 if inv_freq is None else 2 * inv_freq.numel(),
         1 if interleaved else 0, _dense(inv_freq, "inv_freq", None, f32, at), places, axes, int(position_offset))
     return packed, queries, keys, dtype, at

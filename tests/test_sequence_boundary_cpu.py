@@ -277,7 +277,7 @@ def test_head_rotation_bindings_refuse_one_wrong_tensor(bound):
     new = torch.zeros_like
     inputs = dict(q=q, k=k, gamma_q=torch.ones(8), gamma_k=torch.ones(8), eps=1e-6, inv_freq=torch.ones(4), positions=torch.zeros(2, 5, 2, dtype=torch.int32))
     wide = torch.zeros(2, 5, 4, 16)[..., ::2]
-    wrong = [("q", q[0], "must be"), ("k", k[0], "must be"), ("k", k[:, :4], "k has shape"), ("k", k[..., :7], "k has shape"), ("q", q.double(), "must be torch.float64"),
+    wrong = [("q", q[0], "must be"), ("k", k[0], "must be"), ("k", k[:, :4], "k has shape"), ("k", k[..., :7], "k has shape"), ("q", q.double(), "tensors must be float32"),
              ("k", k.half(), "k must be torch"), ("q", wide, "last index of q"), ("k", wide[:, :, :2], "last index of k"), ("inv_freq", torch.ones(4).half(), "inv_freq must be torch"),
              ("inv_freq", torch.ones(8)[::2], "inv_freq must be contiguous"), ("positions", torch.zeros(2, 4, dtype=torch.int32), "positions has shape"),
              ("positions", torch.zeros(2, 5), "positions must be torch"), ("positions", torch.zeros(2, 5, 4, dtype=torch.int32)[..., ::2], "positions must be contiguous")]
@@ -306,3 +306,18 @@ def test_gated_scan_bindings_refuse_one_wrong_tensor(bound):
     bound.clear()
     grads = dict(grad_y=new(x), grad_final=new(ends), grad_x=new(x), grad_z=new(x), grad_initial=new(ends))
     _refuses(bound, mrf.mrf_gated_scan_backward, {**inputs, **grads}, more(grads))
+
+
+def test_numbers_that_a_description_cannot_hold_are_refused_as_such(bound):
+    import torch
+    q, k, table, bucket_of = torch.zeros(2, 5, 4, 8), torch.zeros(2, 6, 2, 8), torch.zeros(4, 3), torch.zeros(11, dtype=torch.int32)
+    attention = dict(q=q, k=k, v=k, scale=0.5, table=table, bucket_of=bucket_of)
+    for wrong in (dict(first_offset=1 << 63), dict(last_offset=-(1 << 64)), dict(query_offset=1 << 70), dict(map_offset=1 << 63),
+                  dict(table=torch.zeros(3)), dict(table=torch.zeros(()))):
+        with pytest.raises(ValueError):
+            mrf.MrfAttention(**{**attention, **wrong})
+    mrf.MrfAttention(**attention, first_offset=-(1 << 63), last_offset=(1 << 63) - 1)
+    for wrong in (dict(position_offset=1 << 63), dict(position_offset=-(1 << 64))):
+        with pytest.raises(ValueError):
+            mrf.mrf_head_rotation_forward(q, q, None, None, **{**dict(eps=1e-6, inv_freq=None, out_q=q, out_k=q), **wrong})
+    assert bound == []
