@@ -677,7 +677,7 @@ def _strides(t, what, shape, dtype, at):
     if t.get_device() != at or t.dtype != dtype or t.shape != shape:
         _refused(t, what, shape, dtype, at)
     strides = t.stride()
-    if strides[-1] != 1 and shape[-1] > 1:
+    if strides[-1] != 1 and shape[-1] > 1 and t.numel():
         raise ValueError("the last index of %s must be dense" % what)
     return strides[:-1]
 

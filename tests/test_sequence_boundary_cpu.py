@@ -321,3 +321,15 @@ def test_numbers_that_a_description_cannot_hold_are_refused_as_such(bound):
         with pytest.raises(ValueError):
             mrf.mrf_head_rotation_forward(q, q, None, None, **{**dict(eps=1e-6, inv_freq=None, out_q=q, out_k=q), **wrong})
     assert bound == []
+
+
+def test_strides_of_tensors_without_elements_do_not_matter(bound):
+    import torch
+    q, x = torch.zeros(2, 5, 4, 8), torch.zeros(2, 40, 4)
+    none = torch.empty_strided((2, 5, 0, 8), (0, 0, 0, 3))
+    mrf.mrf_head_rotation_forward(q, none, None, None, 1e-6, None, q, none)
+    no_keys = torch.empty_strided((2, 0, 2, 8), (0, 0, 0, 3))
+    mrf.mrf_attention_forward(mrf.MrfAttention(q, no_keys, no_keys, 0.5), q, None, None)
+    no_steps = torch.empty_strided((2, 0, 4), (0, 0, 3))
+    mrf.mrf_gated_scan_forward(no_steps, no_steps, None, None, x[:, :0].contiguous(), None, None, None)
+    assert len(bound) == 3
