@@ -3,6 +3,7 @@ the sources."""
 from __future__ import annotations
 
 import os
+import re
 import subprocess
 
 CSRC = os.path.join(os.path.dirname(os.path.abspath(__file__)), "csrc")
@@ -21,8 +22,27 @@ HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
 
 # The attention's sums stay where the other instructions reach them: left to itself the compiler keeps them in the accumulation registers and moves hundreds of
 # values a tile to and fro.  (Kernels that have no room for that are units of their own, without this flag.)  None of these kernels may need scratch memory beside
-# accumulation registers: this compiler has made wrong code of such ones.
+# accumulation registers: this compiler has made wrong code of such ones, so the build fails if there is one.
 UNIT_FLAGS = {"mrfmp_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "mrfmp_attention_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+
+
+REPORT_FLAG = "-Rpass-analysis=kernel-resource-usage"
+
+
+def kernels_with_scratch_and_accumulation(report: str) -> list[str]:
+    """Names of the kernels that the compiler's resource report has with both."""
+    found, name, used = [], None, {}
+    for line in report.splitlines():
+        m = re.search(r"remark: .*?(Function Name|AGPRs|ScratchSize \[bytes/lane\]): (\S+)", line)
+        if not m:
+            continue
+        if m.group(1) == "Function Name":
+            name, used = m.group(2), {}
+            continue
+        used[m.group(1)[:5]] = int(m.group(2))
+        if len(used) == 2 and all(used.values()):
+            found.append(name)
+    return found
 
 
 def is_stale() -> bool:
@@ -48,15 +68,22 @@ def build(verbose: bool = False) -> str:
     for name, defines, sources in units:
         obj = os.path.join(objdir, name)
         cmd = [hipcc, *flags, *defines, "-c", "-o", obj, *sources]
+        if sources[0] in UNIT_FLAGS:
+            cmd.insert(1, REPORT_FLAG)
         jobs.append((obj, subprocess.Popen(cmd, cwd=CSRC, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-    failed = False
+    failed, both, reported = False, [], 0
     for obj, proc in jobs:
         out, _ = proc.communicate()
+        if REPORT_FLAG in proc.args:
+            both += kernels_with_scratch_and_accumulation(out)
+            reported += out.count("Function Name")
         if verbose or proc.returncode != 0:
             print(out)
         failed = failed or proc.returncode != 0
     if failed:
         raise RuntimeError("hipcc failed compiling libmrfmp")
+    if both or not reported:
+        raise RuntimeError("kernels with scratch memory beside accumulation registers: %s" % (both or "no report of the compiler's to tell by"))
     cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB_PATH, *[obj for obj, _ in jobs]]
     res = subprocess.run(cmd, cwd=CSRC, capture_output=True, text=True)
     if verbose or res.returncode != 0:
