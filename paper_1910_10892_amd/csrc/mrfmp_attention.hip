@@ -257,12 +257,13 @@ template <class T, int DP, int NW, bool PACK, bool BIAS> __global__ void __launc
 }
 
 // Parts of the keys, joined in their order: sums of a part count 2^(its maximum - the largest).  A workgroup has a query of a head; a wavefront every fourth part,
-// a lane two entries.
+// a lane two entries, which it adds in 64 bits (256 parts that are all alike, each rounded the same way, left sums of 32 bits off by up to 60 units in their last place).
 constexpr int MRF_ATTN_SPLITS = 1024;
 template <class T> __global__ void __launch_bounds__(256) mrf_attn_join(const MrfAttnParams P)
 {
     __shared__ float weight[MRF_ATTN_SPLITS];
-    __shared__ float scratch[2][4], sums[4][128];
+    __shared__ float scratch[2][4];
+    __shared__ double sums[4][128];
     const long long n = (long long)P.B * P.Hq * P.Q, at = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const float2 *const ends = (const float2 *)P.part;
@@ -284,13 +285,14 @@ template <class T> __global__ void __launch_bounds__(256) mrf_attn_join(const Mr
     if (lane == 0) scratch[1][wv] = l;
     __syncthreads();
     l = (scratch[1][0] + scratch[1][1]) + (scratch[1][2] + scratch[1][3]);
-    float x = 0.0f, y = 0.0f;
+    double x = 0.0, y = 0.0;
     const int d0 = lane < P.D ? lane : 0, d1 = lane + 64 < P.D ? lane + 64 : 0;
 #pragma unroll 4
     for (int s = wv; s < P.splits; s += 4) {
-        const float w = weight[s], *const p = part + s * n * P.D;
-        x = fmaf(p[d0], w, x);
-        y = fmaf(p[d1], w, y);
+        const float *const p = part + s * n * P.D;
+        const double w = weight[s];
+        x = fma(p[d0], w, x);
+        y = fma(p[d1], w, y);
     }
     sums[wv][lane] = x;
     sums[wv][lane + 64] = y;
@@ -298,7 +300,7 @@ template <class T> __global__ void __launch_bounds__(256) mrf_attn_join(const Mr
     const float inv = l > 0.0f ? 1.0f / l : l;
     const long long bh = at / P.Q, i = at - bh * P.Q, b = bh / P.Hq, h = bh - b * P.Hq;
     T *const out = (T *)P.out + ((b * P.Q + i) * P.Hq + h) * P.D;
-    if (tid < P.D) out[tid] = mrf_from_f32<T>(((sums[0][tid] + sums[1][tid]) + (sums[2][tid] + sums[3][tid])) * inv);
+    if (tid < P.D) out[tid] = mrf_from_f32<T>((float)((sums[0][tid] + sums[1][tid]) + (sums[2][tid] + sums[3][tid])) * inv);
     if (tid == 0 && P.lse) P.lse[at] = l == 0.0f ? -INFINITY : (base + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
 }
 

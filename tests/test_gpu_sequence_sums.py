@@ -139,3 +139,20 @@ def test_gradient_of_a_norm_from_many_tokens(dtype):
     mrf.mrf_head_rotation_backward(g.expand(1, T, H, D).contiguous(), none, x.expand(1, T, H, D), none, gamma, None, 1e-6, None, None, None, grad_gamma, None, ws)
     _, want = so.head_rotation_grad(gn[0], xn[0], np.ones(D), 1e-6, np.zeros(0))
     _close(grad_gamma, T * H * want, T * H * SUM * U * np.abs(want), what="grad_gamma")
+
+
+def test_parts_of_a_long_cache_that_are_all_alike():
+    """A row of 131,072 keys of one probability and one value, in 1,024 parts.  Probabilities are exact (1 before they are divided by their sum), so the rest is the sums' own."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    K, D = 131072, 128
+    rng = np.random.default_rng(3)
+    q = torch.zeros(1, 1, 1, D, device="cuda:0")
+    k = torch.zeros(1, K, 1, D, device="cuda:0")
+    v, vn = _values(np.broadcast_to(1.0 + rng.random((1, 1, 1, D)), (1, K, 1, D)), "float32")
+    att = mrf.MrfAttention(q, k, v, 0.35)
+    n = mrf.mrf_attention_workspace_bytes(att, False)
+    assert n == 1024 * (D + 2) * 4
+    out, lse = torch.empty_like(q), torch.empty(1, 1, 1, device="cuda:0")
+    mrf.mrf_attention_forward(att, out, lse, torch.empty(n, dtype=torch.uint8, device="cuda:0"))
+    _close(out, vn[:, :1], SUM * U * vn[:, :1], what="out")
