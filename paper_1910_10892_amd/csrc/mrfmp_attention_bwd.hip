@@ -415,7 +415,7 @@ __global__ void __launch_bounds__(256, (sizeof(T) == 4 || (DP == 128 && DK) ? 1 
         }
 }
 
-// Sums of the parts that several workgroups made of a head of keys, in their order: dk, dv
+// Sums of the parts that several workgroups (512 at most) made of a head of keys, in their order, in 64 bits: dk, dv
 template <class T> __global__ void __launch_bounds__(256) mrf_attn_shares(const MrfAttnParams P)
 {
     typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
@@ -423,7 +423,7 @@ template <class T> __global__ void __launch_bounds__(256) mrf_attn_shares(const 
     if (at >= all) return;
     T *const out = (T *)(blockIdx.y ? P.dv : P.dk);
     const int left = all - at < 4 ? (int)(all - at) : 4;
-    float x[4] = {};
+    double x[4] = {};
     for (int s = 0; s < P.shares; ++s) {
         const float *const p = P.share + (2 * s + blockIdx.y) * all + at;
         if (left == 4) {
@@ -434,7 +434,8 @@ template <class T> __global__ void __launch_bounds__(256) mrf_attn_shares(const 
             for (int j = 0; j < left; ++j) x[j] += p[j];
         }
     }
-    if (out) mrf_store4(out + at, 0, left, x);
+    const float sums[4] = {(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
+    if (out) mrf_store4(out + at, 0, left, sums);
 }
 
 // Gradient of the table: what the lines hold of a diagonal, summed over the strips of keys that it crosses, belongs to the bucket of its offset.  A workgroup

@@ -156,3 +156,24 @@ def test_parts_of_a_long_cache_that_are_all_alike():
     out, lse = torch.empty_like(q), torch.empty(1, 1, 1, device="cuda:0")
     mrf.mrf_attention_forward(att, out, lse, torch.empty(n, dtype=torch.uint8, device="cuda:0"))
     _close(out, vn[:, :1], SUM * U * vn[:, :1], what="out")
+
+
+def test_heads_that_share_keys_and_are_all_alike():
+    """512 heads on one, each summed by a workgroup of its own: 512 times what one of them gives (whose bits these are)."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    torch.manual_seed(1)
+    Q, K, H, D = 40, 100, 512, 64
+    q, k, v, g = (torch.randn(1, n, 1, D, device="cuda:0") for n in (Q, K, K, Q))
+    results = []
+    for heads in (1, H):
+        att = mrf.MrfAttention(q.expand(1, Q, heads, D), k, v, 0.125)
+        out, lse = torch.empty(1, Q, heads, D, device="cuda:0"), torch.empty(1, heads, Q, device="cuda:0")
+        ws = torch.empty(max(mrf.mrf_attention_workspace_bytes(att, b) for b in (False, True)), dtype=torch.uint8, device="cuda:0")
+        grads = [torch.empty_like(k), torch.empty_like(v)]
+        mrf.mrf_attention_forward(att, out, lse, ws)
+        mrf.mrf_attention_backward(att, g.expand(1, Q, heads, D).contiguous(), out, lse, None, *grads, None, ws)
+        results.append(grads)
+    for one, all_heads in zip(*results):
+        want = H * _np(one)
+        _close(all_heads, want, SUM * U * np.abs(want))
