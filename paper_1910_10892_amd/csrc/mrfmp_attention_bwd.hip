@@ -439,8 +439,9 @@ template <class T> __global__ void __launch_bounds__(256) mrf_attn_shares(const 
 }
 
 // Gradient of the table: what the lines hold of a diagonal, summed over the strips of keys that it crosses, belongs to the bucket of its offset.  A workgroup
-// goes through `per` pieces of 256 offsets of a sequence, a thread its offset's strips; each thread has a sum of its own for each of MRF_TABLE_BUCKETS buckets in
-// LDS, which meet at the end in a fixed tree.  More buckets: a layer of workgroups for each MRF_TABLE_BUCKETS of them.
+// goes through `pieces` pieces of 256 offsets of a sequence, a thread its offset's strips, which it adds in 64 bits as long as the bucket stays the same (512 strips that
+// are all alike, each rounded the same way, left sums of 32 bits off by 1e-5); each thread has a sum of its own for each of MRF_TABLE_BUCKETS buckets in LDS, which meet at the end
+// in a fixed tree.  More buckets: a layer of workgroups for each MRF_TABLE_BUCKETS of them.
 constexpr int MRF_TABLE_BUCKETS = 32;
 
 template <int QT> __global__ void __launch_bounds__(256) mrf_attn_buckets(const MrfAttnParams P)
@@ -451,6 +452,8 @@ template <int QT> __global__ void __launch_bounds__(256) mrf_attn_buckets(const 
     const long long x0 = part * P.pieces, x1 = x0 + P.pieces < all ? x0 + P.pieces : all;
 #pragma unroll
     for (int k = 0; k < MRF_TABLE_BUCKETS; ++k) sums[k][tid] = 0.0f;
+    int bucket = 0;
+    double sum = 0.0;      // of `bucket`
     for (long long x = x0; x < x1; ++x) {
         const int b = (int)(x / blocks);
         const long long at = (x - b * blocks) * 256 + tid;
@@ -465,7 +468,11 @@ template <int QT> __global__ void __launch_bounds__(256) mrf_attn_buckets(const 
         // strips whose keys have a query at that offset: key - offset in [0, nq)
         const float *const lines = P.lines + ((size_t)b * P.Hq + h) * P.strips * P.line;
         const int first = (int)(max(offset, 0LL) / 128 * 4), last = (int)min(offset + s.nq - 1, (long long)s.nk - 1);
-        float sum = 0.0f;
+        if (k != bucket) {
+            sums[bucket][tid] += (float)sum;
+            bucket = k;
+            sum = 0.0;
+        }
         // (a workgroup's four strips have the same tiles; the loads of two workgroups' are on their way together)
         for (int strip = first; strip <= last / 32 && last >= 0; strip += 8) {
             float v[8];
@@ -485,8 +492,8 @@ template <int QT> __global__ void __launch_bounds__(256) mrf_attn_buckets(const 
 #pragma unroll
             for (int y = 0; y < 2; ++y) sum += (v[4 * y] + v[4 * y + 1]) + (v[4 * y + 2] + v[4 * y + 3]);
         }
-        sums[k][tid] += sum;
     }
+    sums[bucket][tid] += (float)sum;
     for (int w = 128; w > 0; w /= 2) {
         __syncthreads();
         for (int y = tid; y < MRF_TABLE_BUCKETS * w; y += 256) sums[y / w][y % w] += sums[y / w][y % w + w];

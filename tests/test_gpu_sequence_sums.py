@@ -177,3 +177,36 @@ def test_heads_that_share_keys_and_are_all_alike():
     for one, all_heads in zip(*results):
         want = H * _np(one)
         _close(all_heads, want, SUM * U * np.abs(want))
+
+
+def test_offsets_of_a_long_band_that_are_all_alike():
+    """Queries see the four keys around them, with a probability of 1/4 (to 4 u: lse and the exponential); gradients and values turn by a quarter from one to the next, so dP, and
+    with it dS, is the same for all pairs of an offset."""
+    torch = _torch()
+    import paper_1910_10892_amd as mrf
+    n, H, D = 131072, 8, 4
+    turn = np.array([[1.0, 0.0], [0.0, 1.0], [-1.0, 0.0], [0.0, -1.0]])[np.arange(n) % 4]
+    size = 1.0 + np.random.default_rng(2).random(H)
+    v, g = np.zeros((1, n, 1, D)), np.zeros((1, n, H, D))
+    v[0, :, 0, :2], g[0, :, :, :2] = turn, turn[:, None] * size[:, None]
+    (v, _), (g, gn) = (_values(x, "float32") for x in (v, g))
+    size = gn[0, 0, :, 0]
+    table, bucket_of = torch.zeros(H, 4, device="cuda:0"), torch.arange(4, dtype=torch.int32, device="cuda:0")
+    q = torch.zeros(1, n, H, D, device="cuda:0")
+    att = mrf.MrfAttention(q, torch.zeros_like(v), v, 0.5, first_offset=-2, last_offset=1, table=table, bucket_of=bucket_of, map_offset=-2)
+    out, lse, grad_table = torch.empty_like(q), torch.empty(1, H, n, device="cuda:0"), torch.empty_like(table)
+    ws = torch.empty(max(mrf.mrf_attention_workspace_bytes(att, b) for b in (False, True)), dtype=torch.uint8, device="cuda:0")
+    mrf.mrf_attention_forward(att, out, lse, ws)
+    mrf.mrf_attention_backward(att, g, out, lse, None, None, None, grad_table, ws)
+    # whole rows are queries 2 .. n - 2, whose dP sums to 0; the others, one by one
+    d = np.arange(-2, 2)
+    dp = np.cos(np.pi / 2 * d).round()
+    want, sizes = (n - 3) * dp / 4, (n - 3) * np.abs(dp) / 4
+    for i in (0, 1, n - 1):
+        ok = (i + d >= 0) & (i + d < n)
+        p = ok / ok.sum()
+        ds = p * (dp - (p * dp).sum())
+        want, sizes = want + ds, sizes + np.abs(ds)
+    # dS is off by the probability's 4 u, delta's (a sum of four) and its own roundings: 16 u of 1/4 (1 + |dP|)
+    bound = (16 * (n / 4 + sizes) + SUM * sizes) * U
+    _close(grad_table, size[:, None] * want[None], size[:, None] * bound[None], what="grad_table")
