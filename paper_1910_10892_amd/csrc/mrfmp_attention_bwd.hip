@@ -10,7 +10,7 @@
 //
 // What bounds it: matrix units and LDS, with what a wavefront does between its products beside them only where two or three share a SIMD (heads of 128 have the registers of
 // one).  4 sequences of 2,048, 16 heads, without a mask, queries / keys in us: heads of 32 107 / 132, 64 194 / 223 (four products each: 710 / 620 TFLOP/s), 128 338 / 412
-// (810 / 670); 64 in 32 bits 830 / 1,275.  With a bias and its table's gradient heads of 64 take 200 / 295.
+// (810 / 670); 64 in 32 bits 850 / 1,470.  With a bias and its table's gradient heads of 64 take 200 / 295.
 #include "mrfmp_attention.h"
 
 #include <type_traits>
@@ -191,6 +191,7 @@ constexpr int MRF_SKEWED = mrf_skew(31) + 63;
 // Wavefronts of a SIMD.  Heads of up to 32 entries wait for the look-ups and for LDS more than for products: 192 sequences of 624 keys, 4 heads of 32 in a
 // band of 97, take 146 us with three and 177 with two.  Heads of 64 have no room for three (nor has the queries' kernel: 482 us then instead of 194 for 4 sequences
 // of 2,048, 16 heads of 64; for heads of 32 three are as fast as two).
+// The keys' kernel for heads of 32 with the table's gradient keeps 60 bytes a lane in scratch memory for it (and has no accumulation registers, beside which that would not do).
 // Heads of 128 have room for two where dv is a launch of its own: 2 sequences of 4,160, 4 heads on one of 128, 208 us instead of 380.
 //
 // DK, DV: which of the two it sums.  Both, where their sums and the keys and values fit into the registers, else one launch for each.

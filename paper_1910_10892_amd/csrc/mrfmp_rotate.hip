@@ -5,7 +5,7 @@
 // slots each, and go through some of its heads of queries, or of keys: the angles are formed once for all of them.  Some 30 operations an entry: bound by memory.
 // Angles: position times frequency is formed and reduced to an eighth of a turn in 64 bits (a position of 10^6 leaves 32 bits no digit of the
 // angle behind the point), sine and cosine of the rest by their series.  16 + 4 heads of 128 of 8,192 tokens out of one projection, 16 bits: forward 22 us (3.8 TB/s),
-// backward 28 (4.5) and 4.5 for the sums of the parameters' gradients (a copy reaches 5.1).
+// backward 28 (4.5) and 4.7 for the sums of the parameters' gradients (a copy reaches 5.1).
 #include "mrfmp_rows.h"
 
 #include <type_traits>
