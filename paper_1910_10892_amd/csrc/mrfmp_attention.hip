@@ -6,7 +6,8 @@
 // probabilities are an operand of the second product as they are.
 //
 // What bounds it: with 128 entries the matrix units, fed from LDS at the rate they multiply at; with 32 the exponential and the six operations around it, which take
-// longer than the products; in 32 bits the matrix units; in bands, with look-ups of a bias and with few tiles a workgroup the waiting (40 to 60 % of the wavefronts' cycles).  4 sequences of 2,048, 16 heads, without a mask: heads of 32 in 70 us (490 TFLOP/s), 64 105 (650), 128 154 (890; a
+// longer than the products; in 32 bits the matrix units; in bands, with look-ups of a bias and with few tiles a workgroup the waiting (40 to 60 % of the wavefronts' cycles).  4
+// sequences of 2,048, 16 heads, without a mask: heads of 32 in 70 us (490 TFLOP/s), 64 105 (650), 128 154 (890; a
 // plain product of 8,192^3 reaches 1,082); 64 in 32 bits 607 (113; 153).  A single query of 16 heads on each of 16 caches of up to 16,411 keys, 4 heads of 128: 75 us, 4.4
 // TB/s, and 5 to join the parts (a copy reaches 5.1).
 #include "mrfmp_attention.h"
