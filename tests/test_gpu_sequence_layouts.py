@@ -15,7 +15,7 @@ def _lengths(B, n, seed):
     return m.tolist()
 
 
-@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dtype", ["float32", "float16"])      # (bfloat16 is as float16 but for the range; it has the next test)
 @pytest.mark.parametrize("B,Q,K,Hq,Hk,D,NB", [(128, 90, 140, 6, 2, 16, 0), (128, 90, 250, 6, 2, 16, 7), (64, 70, 140, 8, 2, 64, 7), (64, 70, 140, 8, 2, 128, 0), (64, 70, 140, 8, 2, 128, 7),
                                               (260, 33, 140, 4, 1, 24, 0)])
 def test_attention_backward_with_several_heads_in_a_workgroup(B, Q, K, Hq, Hk, D, NB, dtype):
@@ -25,7 +25,7 @@ def test_attention_backward_with_several_heads_in_a_workgroup(B, Q, K, Hq, Hk, D
     _check_attention(B, Q, K, Hq, Hk, D, dtype, last=0, offset=K - Q, ragged=(_lengths(B, Q, 1), _lengths(B, K, 2), offsets), NB=NB)
 
 
-@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 def test_attention_backward_of_whole_and_banded_sequences_with_several_heads_in_a_workgroup(dtype):
     _check_attention(128, 70, 140, 4, 2, 32, dtype, NB=4, heads_last=True, how="fused")
     _check_attention(128, 75, 140, 4, 2, 32, dtype, first=-40, last=9, NB=3)
